@@ -453,6 +453,61 @@ const char* linfusion_attn_variant_name(const linfusion_attn_t* h);
 /* Number of kernel launches one forward() enqueues for this handle. */
 int32_t linfusion_attn_launches_per_forward(const linfusion_attn_t* h);
 
+/*
+ * Backward pass: the gradients dQ, dK, dV of a loss from the gradient dY of the output, for the operator
+ * that `desc` describes (both layouts, both storage types, every supported pair of widths, both phi, with or
+ * without the normalizer).  With f = phi(Q_i), g = dY_i, den = f . z + eps and the state S | z of Prop. 2 / Eq. 5:
+ *
+ *     t = S g,   w = 1 / den,   c = w (f . t)             (without the normalizer: w = 1, c = 0)
+ *     dQ_i = phi'(Q_i) * w (t - c z)          dS = sum_i (w f)^T g,   dz = - sum_i c w f
+ *     dK_j = phi'(K_j) * (dS V_j + dz)        dV_j = dS^T phi(K_j)
+ *
+ * phi'(x) of elu + 1 is 1 for x > 0, exp(x) otherwise.  Neither Y nor anything of size N x N is needed.
+ *
+ * These calls take a descriptor and no handle (its variant bits play no part), allocate nothing, keep nothing
+ * between calls, and may run at the same time on any streams as long as each has a workspace of its own; they
+ * can be captured into a CUDA graph.  Like forward() they only enqueue work, on desc->device, and give the same bits for
+ * the same inputs.  q, dq, k, dk: [B,H,N,d'] and v, dy, dv: [B,H,N,d] (token-major: [B,N,H,.]) device memory of
+ * the storage type, dense; `state`, `grad_state`: fp32 device memory laid out as state_buffer() does, [B*H][d'*d, then d'],
+ * always unscaled; all 16-byte aligned.  Outputs are written in full and overlap nothing else of the call.
+ * workspace: device memory, 256-byte aligned, of backward_workspace_bytes(), free again when the
+ * call's kernels have run.
+ * The products run on the tensor cores with every computed operand as head + tail of the storage type
+ * (about 16 significant bits in bf16, 21 in fp16) and fp32 sums.  With one token Y_1 = V_1 den / (den + eps) whatever
+ * Q and K are: dQ and dK are then differences of equal numbers, zero up to fp32 rounding.
+ * With fp16 storage gradients below 6e-8 are lost in dQ, dK, dV as in any fp16 tensor: scale the loss.
+ * Errors: INVALID_ARG (null, misaligned or overlapping pointers, sizes, eps), UNSUPPORTED (as create()), ALLOC (workspace
+ * too small), CUDA.
+ *
+ * backward(): everything.  `state` may be the saved state of the forward pass (a copy of state_buffer(), summed over
+ * devices where the tokens are sharded), or NULL: it is then recomputed from k and v.
+ */
+linfusion_status_t linfusion_attn_backward(const linfusion_attn_desc_t* desc, const void* q, const void* k, const void* v,
+                                           const void* dy, const float* state, void* dq, void* dk, void* dv, void* workspace,
+                                           size_t workspace_bytes, void* cuda_stream);
+/*
+ * The same in parts, for token-sharded use (Sec. 4.3: S | z and dS | dz are what devices exchange, whatever N is):
+ *   1. backward_state(k, v -> state)                 the local S | z; the caller sums it over devices (or keeps the forward's sum)
+ *   2. backward_q(q, dy, state -> dq, grad_state)    dQ, and the local dS | dz, which the caller sums over devices
+ *   3. backward_kv(k, v, grad_state -> dk, dv)
+ */
+linfusion_status_t linfusion_attn_backward_state(const linfusion_attn_desc_t* desc, const void* k, const void* v, float* state,
+                                                 void* workspace, size_t workspace_bytes, void* cuda_stream);
+linfusion_status_t linfusion_attn_backward_q(const linfusion_attn_desc_t* desc, const void* q, const void* dy, const float* state,
+                                             void* dq, float* grad_state, void* workspace, size_t workspace_bytes,
+                                             void* cuda_stream);
+linfusion_status_t linfusion_attn_backward_kv(const linfusion_attn_desc_t* desc, const void* k, const void* v,
+                                              const float* grad_state, void* dk, void* dv, void* workspace,
+                                              size_t workspace_bytes, void* cuda_stream);
+/*
+ * Enqueue a copy of the handle's state buffer (S | z of its last forward() or state(), in every variant; summed over
+ * devices where the caller has summed it) to `state`, fp32 device memory of the state buffer's length: what a backward
+ * pass needs of the forward pass.  Errors: INVALID_ARG, CUDA.
+ */
+linfusion_status_t linfusion_attn_save_state(linfusion_attn_t* h, float* state, void* cuda_stream);
+/* Bytes of workspace for `desc` on a device with `sm_count` SMs (<= 0: 148).  Pure host computation. */
+linfusion_status_t linfusion_attn_backward_workspace_bytes(const linfusion_attn_desc_t* desc, int sm_count, size_t* bytes);
+
 #ifdef __cplusplus
 }
 #endif

@@ -31,6 +31,8 @@ EXPORTED = [
     "linfusion_attn_state", "linfusion_attn_apply", "linfusion_attn_state_buffer",
     "linfusion_attn_apply_peers", "linfusion_attn_selftest_wait", "linfusion_attn_selftest_counter_wait",
     "linfusion_attn_state_x", "linfusion_attn_apply_x", "linfusion_attn_branch_x", "linfusion_attn_forward_x",
+    "linfusion_attn_save_state", "linfusion_attn_backward", "linfusion_attn_backward_state", "linfusion_attn_backward_q",
+    "linfusion_attn_backward_kv", "linfusion_attn_backward_workspace_bytes",
     "linfusion_attn_checked_build", "linfusion_attn_checked_violations", "linfusion_attn_checked_shrink_y",
 ]
 
@@ -133,6 +135,19 @@ def load_library() -> ctypes.CDLL:
     lib.linfusion_attn_branch_x.argtypes = [vp, vp, vp, vp, vp, vp, ctypes.c_float, ctypes.c_float, vp, vp]
     lib.linfusion_attn_forward_x.restype = st
     lib.linfusion_attn_forward_x.argtypes = [vp, vp, ctypes.POINTER(ModuleWeights), vp, vp]
+    lib.linfusion_attn_save_state.restype = st
+    lib.linfusion_attn_save_state.argtypes = [vp, vp, vp]
+    sz = ctypes.c_size_t
+    lib.linfusion_attn_backward.restype = st
+    lib.linfusion_attn_backward.argtypes = [ctypes.POINTER(Desc)] + [vp] * 9 + [sz, vp]
+    lib.linfusion_attn_backward_state.restype = st
+    lib.linfusion_attn_backward_state.argtypes = [ctypes.POINTER(Desc)] + [vp] * 4 + [sz, vp]
+    lib.linfusion_attn_backward_q.restype = st
+    lib.linfusion_attn_backward_q.argtypes = [ctypes.POINTER(Desc)] + [vp] * 6 + [sz, vp]
+    lib.linfusion_attn_backward_kv.restype = st
+    lib.linfusion_attn_backward_kv.argtypes = [ctypes.POINTER(Desc)] + [vp] * 6 + [sz, vp]
+    lib.linfusion_attn_backward_workspace_bytes.restype = st
+    lib.linfusion_attn_backward_workspace_bytes.argtypes = [ctypes.POINTER(Desc), st, ctypes.POINTER(sz)]
     lib.linfusion_attn_checked_build.restype = ctypes.c_int32
     lib.linfusion_attn_checked_build.argtypes = []
     lib.linfusion_attn_checked_violations.restype = st
@@ -281,6 +296,7 @@ class LinFusionAttention:
         self._lib = load_library()
         self._h = linfusion_attn_create(self.desc)
         self._lent_ws = None
+        self._backward_bytes = None
 
     # -- properties -------------------------------------------------------------------------
     @property
@@ -461,6 +477,120 @@ class LinFusionAttention:
         if rc != OK:
             raise LinFusionError(rc, "linfusion_attn_apply_peers")
         return y
+
+    # -- backward pass ------------------------------------------------------------------------
+    def state_floats(self):
+        """Shape of a saved S | z (and of its gradient): fp32 [B*H, d'*d + d'], S row-major, then z."""
+        return (self.desc.B * self.desc.H, self.dk * self.desc.d + self.dk)
+
+    def save_state(self, out=None, stream: Optional[int] = None):
+        """A copy of the state S | z that the last ``forward`` / ``state`` of this handle left (the summed one where
+        the caller has summed it), enqueued on the stream behind it: fp32, ``state_floats()``.  It is what
+        ``backward`` needs of the forward pass besides its inputs."""
+        import torch
+        device = torch.device("cuda", self.desc.device)
+        if out is None:
+            out = torch.empty(self.state_floats(), dtype=torch.float32, device=device)
+        else:
+            self._check_state(out, "out", device)
+        if stream is None:
+            stream = torch.cuda.current_stream(device).cuda_stream
+        rc = self._lib.linfusion_attn_save_state(self._h, out.data_ptr(), stream)
+        if rc != OK:
+            raise LinFusionError(rc, "linfusion_attn_save_state")
+        return out
+
+    def _check_state(self, t, name, device):
+        import torch
+        if tuple(t.shape) != self.state_floats() or t.dtype != torch.float32 or not t.is_contiguous() or t.device != device:
+            raise ValueError(f"{name}: expected a contiguous fp32 tensor of shape {self.state_floats()} on {device}")
+
+    def backward_workspace_bytes(self) -> int:
+        """Bytes of workspace that the backward calls take."""
+        if self._backward_bytes is None:
+            import torch
+            sms = torch.cuda.get_device_properties(self.desc.device).multi_processor_count
+            n = ctypes.c_size_t(0)
+            rc = self._lib.linfusion_attn_backward_workspace_bytes(ctypes.byref(self.desc), sms, ctypes.byref(n))
+            if rc != OK:
+                raise LinFusionError(rc, "linfusion_attn_backward_workspace_bytes")
+            self._backward_bytes = int(n.value)
+        return self._backward_bytes
+
+    def _backward_args(self, tensors, states, outs, workspace, stream):
+        """Checks; the outputs and the workspace that were not given; the stream."""
+        import torch
+        device = torch.device("cuda", self.desc.device)
+        for t, name, like in tensors:
+            self._check(t, like)
+            if t.device != device:
+                raise ValueError(f"{name}: expected a tensor on {device}")
+        for t, name in states:
+            self._check_state(t, name, device)
+        made = []
+        for t, name, like in outs:
+            if like == "state":
+                if t is None:
+                    t = torch.empty(self.state_floats(), dtype=torch.float32, device=device)
+                self._check_state(t, name, device)
+            else:
+                if t is None:
+                    t = torch.empty(self.shape_qk if like in ("q", "k") else self.shape, dtype=tensors[0][0].dtype, device=device)
+                self._check(t, like)
+                if t.device != device:
+                    raise ValueError(f"{name}: expected a tensor on {device}")
+            made.append(t)
+        if workspace is None:
+            workspace = torch.empty(self.backward_workspace_bytes(), dtype=torch.uint8, device=device)
+        elif workspace.device != device or not workspace.is_contiguous():
+            raise ValueError(f"workspace: expected a contiguous tensor on {device}")
+        if stream is None:
+            stream = torch.cuda.current_stream(device).cuda_stream
+        return made, (workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream)
+
+    def backward(self, q, k, v, dy, state=None, dq=None, dk=None, dv=None, workspace=None, stream: Optional[int] = None):
+        """(dq, dk, dv) from the gradient dy of the output.  ``state``: what ``save_state`` returned after the
+        forward pass, or None to have it recomputed from k and v.  Uses nothing of the handle but its shape, so
+        calls may overlap each other and forwards; ``workspace`` (a CUDA tensor of ``backward_workspace_bytes``)
+        is allocated for the call when not given."""
+        states = [] if state is None else [(state, "state")]
+        (dq, dk, dv), tail = self._backward_args(
+            [(q, "q", "q"), (k, "k", "k"), (v, "v", "v"), (dy, "dy", "v")], states,
+            [(dq, "dq", "q"), (dk, "dk", "k"), (dv, "dv", "v")], workspace, stream)
+        rc = self._lib.linfusion_attn_backward(
+            ctypes.byref(self.desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), dy.data_ptr(),
+            None if state is None else state.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), *tail)
+        if rc != OK:
+            raise LinFusionError(rc, "linfusion_attn_backward")
+        return dq, dk, dv
+
+    def backward_state(self, k, v, state=None, workspace=None, stream: Optional[int] = None):
+        """S | z of the local tokens, for a backward pass that kept none (``sharding``: sum it over devices)."""
+        (state,), tail = self._backward_args([(k, "k", "k"), (v, "v", "v")], [], [(state, "state", "state")], workspace, stream)
+        rc = self._lib.linfusion_attn_backward_state(ctypes.byref(self.desc), k.data_ptr(), v.data_ptr(), state.data_ptr(), *tail)
+        if rc != OK:
+            raise LinFusionError(rc, "linfusion_attn_backward_state")
+        return state
+
+    def backward_q(self, q, dy, state, dq=None, grad_state=None, workspace=None, stream: Optional[int] = None):
+        """(dq, dS | dz of the local tokens) given the state; the second is to be summed over devices."""
+        (dq, grad_state), tail = self._backward_args([(q, "q", "q"), (dy, "dy", "v")], [(state, "state")],
+                                                     [(dq, "dq", "q"), (grad_state, "grad_state", "state")], workspace, stream)
+        rc = self._lib.linfusion_attn_backward_q(ctypes.byref(self.desc), q.data_ptr(), dy.data_ptr(), state.data_ptr(),
+                                                 dq.data_ptr(), grad_state.data_ptr(), *tail)
+        if rc != OK:
+            raise LinFusionError(rc, "linfusion_attn_backward_q")
+        return dq, grad_state
+
+    def backward_kv(self, k, v, grad_state, dk=None, dv=None, workspace=None, stream: Optional[int] = None):
+        """(dk, dv) given the (summed) state gradient."""
+        (dk, dv), tail = self._backward_args([(k, "k", "k"), (v, "v", "v")], [(grad_state, "grad_state")],
+                                             [(dk, "dk", "k"), (dv, "dv", "v")], workspace, stream)
+        rc = self._lib.linfusion_attn_backward_kv(ctypes.byref(self.desc), k.data_ptr(), v.data_ptr(), grad_state.data_ptr(),
+                                                  dk.data_ptr(), dv.data_ptr(), *tail)
+        if rc != OK:
+            raise LinFusionError(rc, "linfusion_attn_backward_kv")
+        return dk, dv
 
     def state_buffer(self):
         """(device address, number of floats) of the fp32 S | z buffer: [B*H][d*d + d]."""

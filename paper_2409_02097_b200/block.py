@@ -1,0 +1,357 @@
+"""ctypes binding over the C ABI in ``include/linfusion_block.h``: the operators that stand before and
+after the attention inside a transformer block.
+
+``AxialRope``  rotary positions with several axes (time, height, width) on Q and K
+``BlockNorm``  the norms before and after a block, fused with modulation, gate and residual scale
+
+Both have a ``backward``.  Argument marshalling only: the arithmetic is in the CUDA library, and there is
+no CPU fallback.  Objects hold a configuration and no device memory, so one may serve any streams and
+threads at once.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Dict, Optional, Sequence, Tuple
+
+from . import attn
+from .attn import DTYPE_FP16, LinFusionError, OK
+
+MAX_AXES = 4
+NORM_NONE, NORM_LAYER, NORM_RMS = 0, 1, 2
+NORMS = {"none": NORM_NONE, "layer": NORM_LAYER, "rms": NORM_RMS, None: NORM_NONE}
+
+EXPORTED = ["linfusion_rope", "linfusion_block_norm", "linfusion_block_norm_backward", "linfusion_block_norm_workspace_bytes"]
+
+_i32, _i64, _vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
+
+
+class RopeDesc(ctypes.Structure):
+    """Mirror of ``linfusion_rope_desc_t``."""
+    _fields_ = [("B", _i32), ("N", _i32), ("d", _i32), ("n_axes", _i32), ("pairs", _i32 * MAX_AXES), ("interleaved", _i32),
+                ("backward", _i32), ("theta", ctypes.c_double), ("flags", ctypes.c_uint32)]
+
+
+class RopeTensor(ctypes.Structure):
+    """Mirror of ``linfusion_rope_tensor_t``."""
+    _fields_ = [("in_", _vp), ("out", _vp), ("heads", _i32), ("in_batch", _i64), ("in_token", _i64), ("in_head", _i64),
+                ("out_batch", _i64), ("out_token", _i64), ("out_head", _i64)]
+
+
+class NormDesc(ctypes.Structure):
+    """Mirror of ``linfusion_block_norm_desc_t``."""
+    _fields_ = [("B", _i32), ("N", _i32), ("C", _i32), ("pre", _i32), ("post", _i32), ("eps", ctypes.c_float),
+                ("residual_scale", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
+class Rows(ctypes.Structure):
+    """Mirror of ``linfusion_rows_t``."""
+    _fields_ = [("p", _vp), ("batch", _i64), ("row", _i64)]
+
+
+class Channels(ctypes.Structure):
+    """Mirror of ``linfusion_channels_t``."""
+    _fields_ = [("p", _vp), ("batch", _i64)]
+
+
+class NormVectors(ctypes.Structure):
+    """Mirror of ``linfusion_block_norm_vectors_t``."""
+    _fields_ = [("gate", Channels), ("scale", Channels), ("shift", Channels), ("pre_weight", _vp), ("pre_bias", _vp),
+                ("post_weight", _vp), ("post_bias", _vp)]
+
+
+class NormGrads(ctypes.Structure):
+    """Mirror of ``linfusion_block_norm_grads_t``."""
+    _fields_ = [("gate", _vp), ("scale", _vp), ("shift", _vp), ("pre_weight", _vp), ("pre_bias", _vp), ("post_weight", _vp),
+                ("post_bias", _vp)]
+
+
+_lib = None
+
+
+def load_library() -> ctypes.CDLL:
+    global _lib
+    if _lib is None:
+        lib, P = attn.load_library(), ctypes.POINTER
+        lib.linfusion_rope.restype = ctypes.c_int
+        lib.linfusion_rope.argtypes = [P(RopeDesc), P(RopeTensor), P(RopeTensor), _vp, _i64, _vp]
+        lib.linfusion_block_norm.restype = ctypes.c_int
+        lib.linfusion_block_norm.argtypes = [P(NormDesc), P(Rows), P(Rows), P(NormVectors), P(Rows), P(Rows), _vp]
+        lib.linfusion_block_norm_backward.restype = ctypes.c_int
+        lib.linfusion_block_norm_backward.argtypes = [P(NormDesc), P(Rows), P(Rows), P(NormVectors), P(Rows), P(Rows), P(Rows),
+                                                      P(Rows), P(NormGrads), _vp, ctypes.c_size_t, _vp]
+        lib.linfusion_block_norm_workspace_bytes.restype = ctypes.c_int
+        lib.linfusion_block_norm_workspace_bytes.argtypes = [P(NormDesc), _i32, P(ctypes.c_size_t)]
+        _lib = lib
+    return _lib
+
+
+def _check_rc(rc: int, what: str) -> None:
+    if rc != OK:
+        raise LinFusionError(rc, what)
+
+
+def _torch_dtype(name: str):
+    import torch
+    if name not in ("bf16", "fp16"):
+        raise ValueError("dtype must be 'bf16' or 'fp16'")
+    return torch.float16 if name == "fp16" else torch.bfloat16
+
+
+def _check_tensor(t, name, dtype, device=None):
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: expected a CUDA tensor")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name}: on {t.device}, the others are on {device}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the channels of a row must be contiguous")
+
+
+class _on:
+    """The device of the call's tensors made current for its length, where it is not."""
+
+    def __init__(self, device):
+        import torch
+        self._guard = torch.cuda.device(device) if torch.cuda.current_device() != device.index else None
+
+    def __enter__(self):
+        if self._guard is not None:
+            self._guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self._guard is not None:
+            self._guard.__exit__(*exc)
+
+
+def _stream(device, stream):
+    import torch
+    return torch.cuda.current_stream(device).cuda_stream if stream is None else stream
+
+
+class AxialRope:
+    """Rotary positions with several axes for heads of width ``d``.
+
+    ``pairs``: how many pairs of channels each axis turns, e.g. ``(16, 24, 24)`` for time, height and width
+    of a head of 128; channels beyond ``2 * sum(pairs)`` pass unchanged.  The i-th of an axis' n pairs turns by
+    ``position * theta ** (-i / n)``.  Pairs are channels (2p, 2p + 1) with ``interleaved``, else (p, p + P).
+
+    ``positions``: fp32 CUDA tensor [N, axes], or [B, N, axes] for positions of each batch entry.
+    Q and K: [B, H, N, d] (``head_major``) or [B, N, H, d] (``token_major``), with any strides that are
+    multiples of 8 elements (views of one packed projection are fine) and head counts of their own; either may be
+    None.  Outputs may be the inputs (in place).
+    """
+
+    def __init__(self, d: int, pairs: Sequence[int], theta: float = 10000.0, interleaved: bool = True,
+                 layout: str = "head_major", dtype: str = "bf16"):
+        if layout not in ("head_major", "token_major"):
+            raise ValueError("layout must be 'head_major' or 'token_major'")
+        pairs = [int(p) for p in pairs]
+        if not 1 <= len(pairs) <= MAX_AXES or any(p < 0 for p in pairs) or not 2 <= 2 * sum(pairs) <= int(d):
+            raise ValueError(f"pairs: 1 to {MAX_AXES} axes with 1 to d / 2 = {int(d) // 2} pairs in all")
+        self.d, self.pairs, self.theta, self.layout, self.dtype = int(d), tuple(pairs), float(theta), layout, dtype
+        self.interleaved = bool(interleaved)
+        self._torch_dtype = _torch_dtype(dtype)
+        self._padded = (_i32 * MAX_AXES)(*pairs)
+        self._flags = DTYPE_FP16 if dtype == "fp16" else 0
+        self._lib = load_library()
+
+    def _axes(self, t):
+        """(batch, tokens, heads) axes' sizes and strides."""
+        s, st = t.shape, t.stride()
+        return ((s[0], s[2], s[1]), (st[0], st[2], st[1])) if self.layout == "head_major" else ((s[0], s[1], s[2]), st[:3])
+
+    def _tensor(self, t, out, name, B, N, device):
+        import torch
+        if t.dim() != 4 or t.shape[-1] != self.d:
+            raise ValueError(f"{name}: expected four axes, the last of {self.d} channels, got {tuple(t.shape)}")
+        _check_tensor(t, name, self._torch_dtype, device)
+        (b, n, h), strides = self._axes(t)
+        if (b, n) != (B, N):
+            raise ValueError(f"{name}: expected {B} x {N} tokens, got {b} x {n}")
+        if out is None:
+            out = torch.empty(t.shape, dtype=t.dtype, device=t.device)
+        else:
+            if out.shape != t.shape:
+                raise ValueError(f"{name}: the output's shape is {tuple(out.shape)}, the input's {tuple(t.shape)}")
+            _check_tensor(out, name + " output", self._torch_dtype, device)
+        return out, RopeTensor(t.data_ptr(), out.data_ptr(), h, *strides, *self._axes(out)[1])
+
+    def _run(self, q, k, positions, q_out, k_out, backward, stream):
+        import torch
+        some = q if q is not None else k
+        if some is None:
+            raise ValueError("neither q nor k is given")
+        if some.dim() != 4:
+            raise ValueError(f"expected four axes, got {tuple(some.shape)}")
+        (B, N, _), _s = self._axes(some)
+        device = some.device
+        axes = len(self.pairs)
+        if positions.dtype != torch.float32 or not positions.is_cuda or not positions.is_contiguous() or positions.device != device:
+            raise ValueError("positions: expected a contiguous fp32 CUDA tensor on the device of q and k")
+        if tuple(positions.shape) == (N, axes):
+            pos_batch = 0
+        elif tuple(positions.shape) == (B, N, axes):
+            pos_batch = N * axes
+        else:
+            raise ValueError(f"positions: expected {(N, axes)} or {(B, N, axes)}, got {tuple(positions.shape)}")
+        if B == 0 or N == 0:
+            raise ValueError("no tokens")
+        tq = tk = None
+        if q is not None:
+            q_out, tq = self._tensor(q, q_out, "q", B, N, device)
+        if k is not None:
+            k_out, tk = self._tensor(k, k_out, "k", B, N, device)
+        desc = RopeDesc(B, N, self.d, axes, self._padded, self.interleaved, backward, self.theta, self._flags)
+        with _on(device):
+            rc = self._lib.linfusion_rope(ctypes.byref(desc), None if tq is None else ctypes.byref(tq),
+                                          None if tk is None else ctypes.byref(tk), positions.data_ptr(), pos_batch,
+                                          _stream(device, stream))
+        _check_rc(rc, "linfusion_rope")
+        return (q_out if q is not None else None), (k_out if k is not None else None)
+
+    def forward(self, q, k, positions, q_out=None, k_out=None, stream: Optional[int] = None):
+        """(rotated q, rotated k), None where none was given."""
+        return self._run(q, k, positions, q_out, k_out, 0, stream)
+
+    def backward(self, dq, dk, positions, dq_out=None, dk_out=None, stream: Optional[int] = None):
+        """Gradients of q and k from those of the rotated q and k."""
+        return self._run(dq, dk, positions, dq_out, dk_out, 1, stream)
+
+
+class BlockNorm:
+    """The norms before and after a block of a residual stream x [B, N, C], ``a`` the block's output:
+
+        y = residual_scale * x + gate * (Post(a) * post_weight + post_bias)       (y = x without ``a``)
+        n = (Pre(y) * pre_weight + pre_bias) * (1 + scale) + shift
+
+    ``pre`` / ``post``: "none", "layer" or "rms".  Tensors have any batch and row strides that are multiples of 8
+    elements.  gate, scale and shift are [B, C] (views of one projection are fine) or [C] for all batch entries,
+    the weights and biases [C]; all in the storage type, absent where None.  Gradients of vectors are fp32.
+    """
+
+    def __init__(self, C: int, pre: Optional[str] = "layer", post: Optional[str] = "none", eps: float = 1e-6,
+                 residual_scale: float = 1.0, dtype: str = "bf16"):
+        for n in (pre, post):
+            if n not in NORMS:
+                raise ValueError("pre and post must be 'none', 'layer' or 'rms'")
+        self.C, self.pre, self.post = int(C), NORMS[pre], NORMS[post]
+        self.eps, self.residual_scale, self.dtype = float(eps), float(residual_scale), dtype
+        self._torch_dtype = _torch_dtype(dtype)
+        self._flags = DTYPE_FP16 if dtype == "fp16" else 0
+        self._lib = load_library()
+
+    def _desc(self, B, N):
+        return NormDesc(B, N, self.C, self.pre, self.post, self.eps, self.residual_scale, self._flags)
+
+    def workspace_bytes(self, B: int, N: int, sm_count: int = 0) -> int:
+        """Bytes of workspace that ``backward`` takes for B x N rows."""
+        n = ctypes.c_size_t(0)
+        _check_rc(self._lib.linfusion_block_norm_workspace_bytes(ctypes.byref(self._desc(int(B), int(N))), int(sm_count),
+                                                                 ctypes.byref(n)), "linfusion_block_norm_workspace_bytes")
+        return int(n.value)
+
+    def _rows(self, t, name, shape, device):
+        if t is None:
+            return None
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name}: expected {shape}, got {tuple(t.shape)}")
+        _check_tensor(t, name, self._torch_dtype, device)
+        return Rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+    def _channels(self, t, name, B, device):
+        if t is None:
+            return (None, 0)
+        _check_tensor(t, name, self._torch_dtype, device)
+        if tuple(t.shape) == (self.C,):
+            return (t.data_ptr(), 0)
+        if tuple(t.shape) == (B, self.C):
+            # a stride of zero means one vector for all entries; a batch of one needs none of its own
+            return (t.data_ptr(), t.stride(0) if B > 1 else self.C)
+        raise ValueError(f"{name}: expected {(B, self.C)} or {(self.C,)}, got {tuple(t.shape)}")
+
+    def _weight(self, t, name, device):
+        if t is None:
+            return None
+        if tuple(t.shape) != (self.C,):
+            raise ValueError(f"{name}: expected {(self.C,)}, got {tuple(t.shape)}")
+        _check_tensor(t, name, self._torch_dtype, device)
+        return t.data_ptr()
+
+    def _vectors(self, B, device, gate, scale, shift, pre_weight, pre_bias, post_weight, post_bias):
+        return NormVectors(self._channels(gate, "gate", B, device), self._channels(scale, "scale", B, device),
+                           self._channels(shift, "shift", B, device), self._weight(pre_weight, "pre_weight", device),
+                           self._weight(pre_bias, "pre_bias", device), self._weight(post_weight, "post_weight", device),
+                           self._weight(post_bias, "post_bias", device))
+
+    @staticmethod
+    def _shape(t):
+        if t.dim() != 3 or t.shape[0] == 0 or t.shape[1] == 0:
+            raise ValueError(f"expected [B, N, C] with at least one row, got {tuple(t.shape)}")
+        return tuple(t.shape)
+
+    def forward(self, x, a=None, gate=None, scale=None, shift=None, pre_weight=None, pre_bias=None, post_weight=None,
+                post_bias=None, y=None, n=None, stream: Optional[int] = None) -> Tuple:
+        """(y, n): the stream after the block (``x`` itself without ``a``) and the next block's input (None
+        without ``pre``).  ``y`` may be given as ``x`` or ``a`` (in place)."""
+        import torch
+        shape, device = self._shape(x), x.device
+        ref = ctypes.byref
+        vec = self._vectors(shape[0], device, gate, scale, shift, pre_weight, pre_bias, post_weight, post_bias)
+        if a is not None and y is None:
+            y = torch.empty(shape, dtype=x.dtype, device=device)
+        if self.pre != NORM_NONE and n is None:
+            n = torch.empty(shape, dtype=x.dtype, device=device)
+        rows = [self._rows(t, name, shape, device) for t, name in ((x, "x"), (a, "a"), (y, "y"), (n, "n"))]
+        rx, ra, ry, rn = (None if r is None else ref(r) for r in rows)
+        with _on(device):
+            rc = self._lib.linfusion_block_norm(ref(self._desc(shape[0], shape[1])), rx, ra, ref(vec), ry, rn,
+                                                _stream(device, stream))
+        _check_rc(rc, "linfusion_block_norm")
+        return (y if a is not None else x), n
+
+    def backward(self, y, a=None, gate=None, scale=None, shift=None, pre_weight=None, pre_bias=None, post_weight=None,
+                 post_bias=None, dy=None, dn=None, dx=None, da=None, need_vectors: bool = True, workspace=None,
+                 stream: Optional[int] = None) -> Dict:
+        """Gradients by name: ``x``, ``a`` where it was given, and each given vector's in fp32 (``need_vectors``).
+
+        ``y`` is the stream as ``forward`` returned it (not needed without ``pre``), ``dy`` its gradient from
+        everything but ``n`` (None: zero), ``dn`` the gradient of ``n``.  ``dx`` may be given as ``dy`` and ``da`` as
+        ``a`` (in place).  ``workspace``: a CUDA tensor of at least ``workspace_bytes``, else one is allocated."""
+        import torch
+        some = dn if dn is not None else dy
+        if some is None:
+            raise ValueError("neither dy nor dn is given")
+        shape, device = self._shape(some), some.device
+        B, ref = shape[0], ctypes.byref
+        vec = self._vectors(B, device, gate, scale, shift, pre_weight, pre_bias, post_weight, post_bias)
+        if dx is None:
+            dx = torch.empty(shape, dtype=some.dtype, device=device)
+        if a is not None and da is None:
+            da = torch.empty(shape, dtype=some.dtype, device=device)
+        out, grads, ws, ws_bytes = {"x": dx}, None, None, 0
+        if a is not None:
+            out["a"] = da
+        if need_vectors:
+            given = [(name, t) for name, t in (("gate", gate), ("scale", scale), ("shift", shift), ("pre_weight", pre_weight),
+                                               ("pre_bias", pre_bias), ("post_weight", post_weight), ("post_bias", post_bias))
+                     if t is not None]
+            if given:
+                grads = NormGrads()
+                for name, t in given:
+                    out[name] = torch.empty(t.shape, dtype=torch.float32, device=device)
+                    setattr(grads, name, out[name].data_ptr())
+                if workspace is None:
+                    sms = torch.cuda.get_device_properties(device).multi_processor_count
+                    workspace = torch.empty(self.workspace_bytes(B, shape[1], sms), dtype=torch.uint8, device=device)
+                elif not workspace.is_cuda or workspace.device != device or not workspace.is_contiguous():
+                    raise ValueError("workspace: expected a contiguous CUDA tensor on the device of the others")
+                ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        rows = [self._rows(t, name, shape, device) for t, name in ((y, "y"), (a, "a"), (dy, "dy"), (dn, "dn"), (dx, "dx"), (da, "da"))]
+        ry, ra, rdy, rdn, rdx, rda = (None if r is None else ref(r) for r in rows)
+        with _on(device):
+            rc = self._lib.linfusion_block_norm_backward(ref(self._desc(B, shape[1])), ry, ra, ref(vec), rdy, rdn, rdx, rda,
+                                                         None if grads is None else ref(grads), ws, ws_bytes,
+                                                         _stream(device, stream))
+        _check_rc(rc, "linfusion_block_norm_backward")
+        return out

@@ -1,0 +1,329 @@
+// Host side of the backward pass declared in include/linfusion_attn.h: argument checks, the fixed split of
+// the tokens, workspace layout and launches.
+#include "../../include/linfusion_attn.h"
+
+#include "backward_kernels.cuh"
+#include "host_util.h"
+
+using namespace lf;
+
+namespace {
+
+int feature_width(const linfusion_attn_desc_t& d) { return d.d_qk > 0 ? d.d_qk : d.d; }
+
+int kernel_kind(const linfusion_attn_desc_t& d)
+{
+    return make_kind(d.phi == LINFUSION_PHI_IDENTITY ? kPhiIdentity : kPhiEluPlusOne,
+                     (d.flags & LINFUSION_DTYPE_FP16) != 0u ? kDtypeFp16 : kDtypeBf16);
+}
+
+SlabLayout slab_layout(const linfusion_attn_desc_t& d, int width)
+{
+    SlabLayout L;
+    L.H = d.H;
+    if ((d.flags & LINFUSION_LAYOUT_TOKEN_MAJOR) != 0u) {
+        L.batch_stride = static_cast<long long>(d.N) * d.H * width;
+        L.head_stride = width;
+        L.row_stride = d.H * width;
+    } else {
+        L.batch_stride = static_cast<long long>(d.H) * d.N * width;
+        L.head_stride = static_cast<long long>(d.N) * width;
+        L.row_stride = width;
+    }
+    return L;
+}
+
+// What follows from (descriptor, SM count) alone.
+struct BackwardPlan {
+    int slabs, dk, dv, floats;  // floats of S | z of a slab
+    int chunks_q, chunks_kv;    // CTAs per slab of the two streams
+    size_t partials_off, state_off, grad_off, total;
+};
+
+template <int DK, int DV>
+void plan_chunks(const linfusion_attn_desc_t& d, int sm_count, BackwardPlan* p)
+{
+    using C = BackwardCfg<DK, DV>;
+    // CTAs that an SM holds: two at most of the wide ones by registers, three of the narrow ones.
+    const int per_sm = C::WQ <= 4 ? 3 : C::WQ <= 6 ? 2 : 1;
+    const int tiles = (d.N + C::TILE - 1) / C::TILE;
+    int chunks = (per_sm * sm_count + p->slabs - 1) / p->slabs;
+    chunks = chunks > tiles ? tiles : chunks;
+    p->chunks_q = p->chunks_kv = chunks < 1 ? 1 : chunks;
+}
+
+#define LF_DISPATCH_WIDTHS(dk, dv, CALL)  \
+    switch ((dk) * 1000 + (dv)) {         \
+        case 32032: CALL(32, 32); break;   \
+        case 40040: CALL(40, 40); break;   \
+        case 64064: CALL(64, 64); break;   \
+        case 80080: CALL(80, 80); break;   \
+        case 128128: CALL(128, 128); break; \
+        case 160160: CALL(160, 160); break; \
+        case 128064: CALL(128, 64); break; \
+        case 80040: CALL(80, 40); break;   \
+        case 32064: CALL(32, 64); break;   \
+        default: break;                    \
+    }
+
+linfusion_status_t make_backward_plan(const linfusion_attn_desc_t* desc, int sm_count, BackwardPlan* p)
+{
+    if (desc == nullptr) return LINFUSION_ERR_INVALID_ARG;
+    // The checks of create(); the forward variant plays no part here.
+    if ((desc->flags & LINFUSION_VARIANT_MASK) > LINFUSION_VARIANT_FUSED) return LINFUSION_ERR_UNSUPPORTED;
+    linfusion_attn_desc_t d = *desc;
+    d.flags = (d.flags & ~LINFUSION_VARIANT_MASK) | LINFUSION_VARIANT_SPLIT;
+    size_t unused = 0;
+    const linfusion_status_t st = linfusion_attn_workspace_bytes(&d, sm_count, &unused);
+    if (st != LINFUSION_OK) return st;
+    if (sm_count <= 0) sm_count = 148;
+    p->slabs = d.B * d.H;
+    p->dk = feature_width(d);
+    p->dv = d.d;
+    p->floats = grad_state_floats(p->dk, p->dv);
+#define LF_CALL(DK, DV) plan_chunks<DK, DV>(d, sm_count, p)
+    LF_DISPATCH_WIDTHS(p->dk, p->dv, LF_CALL)
+#undef LF_CALL
+    const size_t state = align_up_256(static_cast<size_t>(p->slabs) * p->floats * sizeof(float));
+    p->state_off = 0;
+    p->grad_off = state;
+    p->partials_off = 2 * state;
+    p->total = 2 * state + state * static_cast<size_t>(p->chunks_q);
+    return LINFUSION_OK;
+}
+
+template <int DK, int DV, int KIND, bool GRAD>
+cudaError_t launch_state(const linfusion_attn_desc_t& d, const BackwardPlan& p, const void* q, const void* dy, const float* state,
+                         void* dq, float* partials, float* out, cudaStream_t s)
+{
+    using C = BackwardCfg<DK, DV>;
+    static std::atomic<uint64_t> done{0};
+    cudaError_t e = allow_smem(backward_state_kernel<DK, DV, KIND, GRAD>, C::SMEM_Q, d.device, &done);
+    if (e != cudaSuccess) return e;
+    BackwardScales sc;
+    sc.eps = (d.flags & LINFUSION_FLAG_UNNORMALIZED) != 0u ? kEpsUnnormalized : d.eps;
+    sc.scaled = kind_dtype(KIND) == kDtypeFp16 ? 1 : 0;
+    e = launch_pdl(backward_state_kernel<DK, DV, KIND, GRAD>, dim3(p.chunks_q, p.slabs), dim3(32 * C::WQ), C::SMEM_Q, s,
+                   static_cast<const __nv_bfloat16*>(q), static_cast<const __nv_bfloat16*>(dy), state,
+                   static_cast<__nv_bfloat16*>(dq), p.chunks_q == 1 ? out : partials, d.N, p.chunks_q, slab_layout(d, DK),
+                   slab_layout(d, DV), sc);
+    if (e != cudaSuccess || p.chunks_q == 1) return e;
+    return launch_pdl(backward_reduce_kernel, dim3((p.floats + 255) / 256, p.slabs), dim3(256), 0, s, partials, out, p.floats,
+                      p.chunks_q);
+}
+
+template <int DK, int DV, int KIND>
+cudaError_t launch_kv(const linfusion_attn_desc_t& d, const BackwardPlan& p, const void* k, const void* v, const float* grad_state,
+                      void* dk, void* dv, cudaStream_t s)
+{
+    using C = BackwardCfg<DK, DV>;
+    static std::atomic<uint64_t> done{0};
+    cudaError_t e = allow_smem(backward_kv_kernel<DK, DV, KIND>, C::SMEM_KV, d.device, &done);
+    if (e != cudaSuccess) return e;
+    BackwardScales sc;
+    sc.eps = d.eps;
+    sc.scaled = kind_dtype(KIND) == kDtypeFp16 ? 1 : 0;
+    return launch_pdl(backward_kv_kernel<DK, DV, KIND>, dim3(p.chunks_kv, p.slabs), dim3(32 * C::WKV), C::SMEM_KV, s,
+                      static_cast<const __nv_bfloat16*>(k), static_cast<const __nv_bfloat16*>(v), grad_state,
+                      static_cast<__nv_bfloat16*>(dk), static_cast<__nv_bfloat16*>(dv), d.N, p.chunks_kv, slab_layout(d, DK),
+                      slab_layout(d, DV), sc);
+}
+
+#define LF_DISPATCH_KINDS(kind, CALL) \
+    switch (kind) {                   \
+        case 0: CALL(0); break;       \
+        case 1: CALL(1); break;       \
+        case 2: CALL(2); break;       \
+        case 3: CALL(3); break;       \
+        default: break;               \
+    }
+
+// grad: Q, dY -> dQ and dS | dz.  Otherwise K, V -> S | z.
+template <bool GRAD>
+cudaError_t run_state(const linfusion_attn_desc_t& d, const BackwardPlan& p, const void* q, const void* dy, const float* state,
+                      void* dq, float* partials, float* out, cudaStream_t s)
+{
+    cudaError_t e = cudaErrorInvalidValue;
+#define LF_KIND(KV) e = launch_state<kDK, kDV, KV, GRAD>(d, p, q, dy, state, dq, partials, out, s)
+#define LF_CALL(DKV, DVV)                          \
+    {                                              \
+        constexpr int kDK = DKV, kDV = DVV;        \
+        LF_DISPATCH_KINDS(kernel_kind(d), LF_KIND) \
+    }
+    LF_DISPATCH_WIDTHS(p.dk, p.dv, LF_CALL)
+#undef LF_CALL
+#undef LF_KIND
+    return e;
+}
+
+cudaError_t run_kv(const linfusion_attn_desc_t& d, const BackwardPlan& p, const void* k, const void* v, const float* grad_state,
+                   void* dk, void* dv, cudaStream_t s)
+{
+    cudaError_t e = cudaErrorInvalidValue;
+#define LF_KIND(KV) e = launch_kv<kDK, kDV, KV>(d, p, k, v, grad_state, dk, dv, s)
+#define LF_CALL(DKV, DVV)                          \
+    {                                              \
+        constexpr int kDK = DKV, kDV = DVV;        \
+        LF_DISPATCH_KINDS(kernel_kind(d), LF_KIND) \
+    }
+    LF_DISPATCH_WIDTHS(p.dk, p.dv, LF_CALL)
+#undef LF_CALL
+#undef LF_KIND
+    return e;
+}
+
+struct Span {
+    const void* p;
+    size_t bytes;
+    bool output;
+};
+
+// Every pointer set and aligned; no output overlaps an input or another output.
+bool spans_ok(const Span* spans, int n)
+{
+    for (int i = 0; i < n; ++i)
+        if (spans[i].p == nullptr || !is_aligned(spans[i].p, 16)) return false;
+    for (int i = 0; i < n; ++i)
+        for (int j = 0; j < i; ++j)
+            if ((spans[i].output || spans[j].output) && overlaps(spans[i].p, spans[i].bytes, spans[j].p, spans[j].bytes))
+                return false;
+    return true;
+}
+
+struct Call {
+    BackwardPlan plan;
+    size_t bytes_qk, bytes_vy, bytes_state;
+    linfusion_status_t st;
+};
+
+// The plan for the descriptor's device and the checks every entry point makes first.
+Call begin(const linfusion_attn_desc_t* desc, const void* workspace, size_t workspace_bytes)
+{
+    Call c = {};
+    c.st = make_backward_plan(desc, 0, &c.plan);
+    if (c.st != LINFUSION_OK) return c;
+    if (workspace == nullptr || !is_aligned(workspace, 256)) {
+        c.st = LINFUSION_ERR_INVALID_ARG;
+        return c;
+    }
+    const int sms = device_sm_count(desc->device);
+    if (sms == -2) c.st = LINFUSION_ERR_UNSUPPORTED;
+    if (sms == -1) c.st = LINFUSION_ERR_CUDA;
+    if (sms < 0) return c;
+    c.st = make_backward_plan(desc, sms, &c.plan);
+    if (c.st != LINFUSION_OK) return c;
+    if (workspace_bytes < c.plan.total) c.st = LINFUSION_ERR_ALLOC;
+    const size_t rows = static_cast<size_t>(c.plan.slabs) * desc->N;
+    c.bytes_qk = rows * c.plan.dk * 2;
+    c.bytes_vy = rows * c.plan.dv * 2;
+    c.bytes_state = static_cast<size_t>(c.plan.slabs) * c.plan.floats * 4;
+    return c;
+}
+
+linfusion_status_t end(cudaError_t e)
+{
+    if (e == cudaSuccess) return LINFUSION_OK;
+    cudaGetLastError();
+    return LINFUSION_ERR_CUDA;
+}
+
+}  // namespace
+
+extern "C" {
+
+linfusion_status_t linfusion_attn_backward_workspace_bytes(const linfusion_attn_desc_t* desc, int sm_count, size_t* bytes)
+{
+    if (bytes == nullptr) return LINFUSION_ERR_INVALID_ARG;
+    BackwardPlan p;
+    const linfusion_status_t st = make_backward_plan(desc, sm_count, &p);
+    if (st != LINFUSION_OK) return st;
+    *bytes = p.total;
+    return LINFUSION_OK;
+}
+
+linfusion_status_t linfusion_attn_save_state(linfusion_attn_t* h, float* state, void* cuda_stream)
+{
+    if (h == nullptr || state == nullptr || !is_aligned(state, 16)) return LINFUSION_ERR_INVALID_ARG;
+    float* from = nullptr;
+    size_t floats = 0;
+    const linfusion_status_t st = linfusion_attn_state_buffer(h, &from, &floats);
+    if (st != LINFUSION_OK) return st;
+    if (overlaps(from, floats * 4, state, floats * 4)) return LINFUSION_ERR_INVALID_ARG;
+    cudaPointerAttributes where;
+    if (cudaPointerGetAttributes(&where, from) != cudaSuccess) {
+        cudaGetLastError();
+        return LINFUSION_ERR_CUDA;
+    }
+    CurrentDevice guard(where.device);
+    if (!guard.ok) return LINFUSION_ERR_CUDA;
+    return end(cudaMemcpyAsync(state, from, floats * 4, cudaMemcpyDeviceToDevice, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+linfusion_status_t linfusion_attn_backward(const linfusion_attn_desc_t* desc, const void* q, const void* k, const void* v,
+                                           const void* dy, const float* state, void* dq, void* dk, void* dv, void* workspace,
+                                           size_t workspace_bytes, void* cuda_stream)
+{
+    const Call c = begin(desc, workspace, workspace_bytes);
+    if (c.st != LINFUSION_OK) return c.st;
+    const Span spans[] = {{q, c.bytes_qk, false}, {k, c.bytes_qk, false}, {v, c.bytes_vy, false}, {dy, c.bytes_vy, false},
+                          {dq, c.bytes_qk, true}, {dk, c.bytes_qk, true}, {dv, c.bytes_vy, true},
+                          {workspace, c.plan.total, true}, {state, c.bytes_state, false}};
+    if (!spans_ok(spans, state != nullptr ? 9 : 8)) return LINFUSION_ERR_INVALID_ARG;
+    CurrentDevice guard(desc->device);
+    if (!guard.ok) return LINFUSION_ERR_CUDA;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    unsigned char* ws = static_cast<unsigned char*>(workspace);
+    float* partials = reinterpret_cast<float*>(ws + c.plan.partials_off);
+    float* own_state = reinterpret_cast<float*>(ws + c.plan.state_off);
+    float* grad = reinterpret_cast<float*>(ws + c.plan.grad_off);
+    cudaError_t e = cudaSuccess;
+    if (state == nullptr) e = run_state<false>(*desc, c.plan, k, v, nullptr, nullptr, partials, own_state, s);
+    if (e == cudaSuccess)
+        e = run_state<true>(*desc, c.plan, q, dy, state != nullptr ? state : own_state, dq, partials, grad, s);
+    if (e == cudaSuccess) e = run_kv(*desc, c.plan, k, v, grad, dk, dv, s);
+    return end(e);
+}
+
+linfusion_status_t linfusion_attn_backward_state(const linfusion_attn_desc_t* desc, const void* k, const void* v, float* state,
+                                                 void* workspace, size_t workspace_bytes, void* cuda_stream)
+{
+    const Call c = begin(desc, workspace, workspace_bytes);
+    if (c.st != LINFUSION_OK) return c.st;
+    const Span spans[] = {{k, c.bytes_qk, false}, {v, c.bytes_vy, false}, {state, c.bytes_state, true}, {workspace, c.plan.total, true}};
+    if (!spans_ok(spans, 4)) return LINFUSION_ERR_INVALID_ARG;
+    CurrentDevice guard(desc->device);
+    if (!guard.ok) return LINFUSION_ERR_CUDA;
+    float* partials = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + c.plan.partials_off);
+    return end(run_state<false>(*desc, c.plan, k, v, nullptr, nullptr, partials, state, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+linfusion_status_t linfusion_attn_backward_q(const linfusion_attn_desc_t* desc, const void* q, const void* dy, const float* state,
+                                             void* dq, float* grad_state, void* workspace, size_t workspace_bytes,
+                                             void* cuda_stream)
+{
+    const Call c = begin(desc, workspace, workspace_bytes);
+    if (c.st != LINFUSION_OK) return c.st;
+    const Span spans[] = {{q, c.bytes_qk, false}, {dy, c.bytes_vy, false}, {state, c.bytes_state, false},
+                          {dq, c.bytes_qk, true}, {grad_state, c.bytes_state, true}, {workspace, c.plan.total, true}};
+    if (!spans_ok(spans, 6)) return LINFUSION_ERR_INVALID_ARG;
+    CurrentDevice guard(desc->device);
+    if (!guard.ok) return LINFUSION_ERR_CUDA;
+    float* partials = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + c.plan.partials_off);
+    return end(run_state<true>(*desc, c.plan, q, dy, state, dq, partials, grad_state, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+linfusion_status_t linfusion_attn_backward_kv(const linfusion_attn_desc_t* desc, const void* k, const void* v,
+                                              const float* grad_state, void* dk, void* dv, void* workspace,
+                                              size_t workspace_bytes, void* cuda_stream)
+{
+    const Call c = begin(desc, workspace, workspace_bytes);
+    if (c.st != LINFUSION_OK) return c.st;
+    const Span spans[] = {{k, c.bytes_qk, false}, {v, c.bytes_vy, false}, {grad_state, c.bytes_state, false},
+                          {dk, c.bytes_qk, true}, {dv, c.bytes_vy, true}, {workspace, c.plan.total, true}};
+    if (!spans_ok(spans, 6)) return LINFUSION_ERR_INVALID_ARG;
+    CurrentDevice guard(desc->device);
+    if (!guard.ok) return LINFUSION_ERR_CUDA;
+    return end(run_kv(*desc, c.plan, k, v, grad_state, dk, dv, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+}  // extern "C"

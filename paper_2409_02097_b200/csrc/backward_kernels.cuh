@@ -1,0 +1,544 @@
+// Backward pass of the normalized linear attention (include/linfusion_attn.h), for every supported pair of widths.
+//
+// With f = phi(q_i), g = dY_i, the state S | z of the forward pass and den = f . z + eps:
+//
+//     t = S g        w = 1 / den        c = w (f . t)  (= Y_i . g, so Y is not needed)
+//     dq_i = phi'(q_i) * w (t - c z)
+//     dS  += (w f)^T g        dz -= (w f) c
+//
+// and then, with f = phi(k_j):
+//
+//     dk_j = phi'(k_j) * (dS v_j + dz)        dv_j = dS^T f
+//
+// (without the normalizer: w = 1, c = 0, dz = 0).  phi'(x) = min(1, exp(x)) for elu + 1, 1 for the identity.  So the
+// backward pass is two streams over the tokens, as the forward is: Q, dY -> dQ with the state gradient dS | dz summed
+// on the way, then K, V -> dK, dV.  Nothing of size N x N, and nothing of size N but the gradients, is written.
+//
+// Precision.  t - c z is a difference: with values that have a mean, S is that mean times z plus a remainder about
+// sqrt(N) times smaller, and only the remainder is left.  A state rounded to 16 bits (as the forward's apply operand
+// is) would lose it, so every operand of the tensor-core products that is not an input tensor (S, w f, dS, phi(k)) is
+// carried as a head and a tail of the storage type, x = hi + lo with |x - hi - lo| <= 2^-17 |x| (bf16) or 2^-22 (fp16):
+// two products in place of one (three for dS^T f).  The results are then off by little more than the one rounding
+// of the 16-bit outputs.
+#pragma once
+
+#include "common.cuh"
+
+namespace lf {
+
+// Layout of S | z and of dS | dz per slab: dk x dv row-major, then dk.
+__host__ __device__ constexpr int grad_state_floats(int dk, int dv) { return dk * dv + dk; }
+
+__device__ __forceinline__ void stmatrix_x4_trans(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3)
+{
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(r0), "r"(r1), "r"(r2),
+                 "r"(r3)
+                 : "memory");
+}
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src, bool valid)
+{
+    const uint32_t bytes = valid ? 16u : 0u;  // 0: the destination is filled with zeros, the source not read
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
+
+// phi and its slope of one value.
+template <int KIND>
+__device__ __forceinline__ void phi_and_slope(float x, float* f, float* slope)
+{
+    if (kind_phi(KIND) == kPhiIdentity) {
+        *f = x;
+        *slope = 1.0f;
+        return;
+    }
+    const float e = ex2_approx(fminf(x, 0.0f) * 1.4426950408889634f);
+    *f = fmaxf(x, 0.0f) + e;
+    *slope = e;
+}
+
+// A pair of values as head and tail in the storage type.
+template <int KIND>
+__device__ __forceinline__ void split_pair(float a, float b, uint32_t* hi, uint32_t* lo)
+{
+    *hi = pack_pair<KIND>(a, b);
+    *lo = pack_pair<KIND>(a - pair_lo<KIND>(*hi), b - pair_hi<KIND>(*hi));
+}
+
+template <int DK, int DV>
+struct BackwardCfg {
+    static constexpr int KP = (DK + 15) / 16 * 16, VP = (DV + 15) / 16 * 16;  // widths padded to the products' step
+    static constexpr int WQ = KP / 16;                                       // warps: 16 features each
+    static constexpr int WKV = (KP > VP ? KP : VP) / 16;                     // ... or 16 channels of dV
+    static constexpr int TILE = KP + VP <= 160 ? 64 : 32;                    // tokens at a time
+    // A row takes an odd number of 16-byte units: eight rows of a matrix fragment fall into different banks.
+    static constexpr int PITCHK = ((KP / 8) | 1) * 16, PITCHV = ((VP / 8) | 1) * 16;
+    static constexpr int STAGE = TILE * (PITCHK + PITCHV);
+    static constexpr int SMEM_Q = 2 * STAGE + WQ * TILE * 8;
+    static constexpr int SMEM_KV = 2 * STAGE + 2 * TILE * PITCHK;  // head and tail of phi(k)
+};
+
+struct BackwardScales {
+    float eps;        // negative: without the normalizer
+    int scaled;       // fp16 operands: scale S, w f and dS by powers of two of their own sizes
+};
+
+// Power of two 2^-e with 2^e <= x < 2^(e+1), times 2^up; 1 for zero, infinite or NaN x.
+__device__ __forceinline__ float pow2_scale(float x, int up)
+{
+    if (!(x > 0.0f) || isinf(x)) return 1.0f;
+    int e = static_cast<int>((__float_as_uint(x) >> 23) & 0xffu) - 127;
+    e = min(max(up - e, -120), 120);
+    return __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
+}
+
+// Copy tile `row0` .. of a slab into shared memory, rows past N as zeros.
+template <int D, int PITCH, int TILE, int THREADS>
+__device__ __forceinline__ void load_tile(unsigned char* dst, const __nv_bfloat16* base, int row_stride, int row0, int N)
+{
+    constexpr int VECS = D / 8;
+    for (int i = threadIdx.x; i < TILE * VECS; i += THREADS) {
+        const int r = i / VECS, v = i - r * VECS;
+        const bool in = row0 + r < N;
+        const __nv_bfloat16* src = base + static_cast<long long>(in ? row0 + r : 0) * row_stride + v * 8;
+        cp_async_16(smem_u32(dst + r * PITCH + v * 16), src, in);
+    }
+}
+template <int D, int PITCH, int TILE, int THREADS>
+__device__ __forceinline__ void store_tile(const unsigned char* src, __nv_bfloat16* base, int row_stride, int row0, int N)
+{
+    constexpr int VECS = D / 8;
+    for (int i = threadIdx.x; i < TILE * VECS; i += THREADS) {
+        const int r = i / VECS, v = i - r * VECS;
+        if (row0 + r < N)
+            st_stream_16B(base + static_cast<long long>(row0 + r) * row_stride + v * 8,
+                          *reinterpret_cast<const uint4*>(src + r * PITCH + v * 16));
+    }
+}
+template <int D, int PITCH, int TILE, int THREADS>
+__device__ __forceinline__ void clear_padding(unsigned char* dst)
+{
+    constexpr int P = (D + 15) / 16 * 16;
+    if (P > D)
+        for (int r = threadIdx.x; r < TILE; r += THREADS)
+            for (int v = D / 8; v < P / 8; ++v) *reinterpret_cast<uint4*>(dst + r * PITCH + v * 16) = make_uint4(0u, 0u, 0u, 0u);
+}
+
+// The largest |x| over the block's threads; `scratch`: 33 floats.
+__device__ __forceinline__ float block_max(float v, float* scratch, int warps)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x / 32] = v;
+    __syncthreads();
+    for (int i = 0; i < warps; ++i) v = fmaxf(v, scratch[i]);
+    __syncthreads();
+    return v;
+}
+
+// Warp's A operand of a product with the rows of S (or dS): 16 features x DV channels, head and tail.
+template <int KIND, int DK, int DV>
+__device__ __forceinline__ void load_state_rows(const float* S, int m0, int lane, float scale,
+                                                uint32_t (&hi)[(DV + 15) / 16][4], uint32_t (&lo)[(DV + 15) / 16][4])
+{
+#pragma unroll
+    for (int s = 0; s < (DV + 15) / 16; ++s)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int row = m0 + lane / 4 + (r & 1) * 8, col = s * 16 + 2 * (lane & 3) + (r >> 1) * 8;
+            float2 x = make_float2(0.0f, 0.0f);
+            if (row < DK && col < DV) x = *reinterpret_cast<const float2*>(S + row * DV + col);
+            split_pair<KIND>(x.x * scale, x.y * scale, &hi[s][r], &lo[s][r]);
+        }
+}
+// The same of its transpose: 16 channels x DK features.
+template <int KIND, int DK, int DV>
+__device__ __forceinline__ void load_state_cols(const float* S, int m0, int lane, float scale,
+                                                uint32_t (&hi)[(DK + 15) / 16][4], uint32_t (&lo)[(DK + 15) / 16][4])
+{
+#pragma unroll
+    for (int s = 0; s < (DK + 15) / 16; ++s)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int ch = m0 + lane / 4 + (r & 1) * 8, f = s * 16 + 2 * (lane & 3) + (r >> 1) * 8;
+            float a = 0.0f, b = 0.0f;
+            if (ch < DV && f < DK) a = S[f * DV + ch], b = S[(f + 1) * DV + ch];
+            split_pair<KIND>(a * scale, b * scale, &hi[s][r], &lo[s][r]);
+        }
+}
+
+// B fragments of two groups of eight tokens, contraction over channels k0 .. k0 + 15 of rows [token][channel].
+__device__ __forceinline__ void tokens_b(const unsigned char* tile, int pitch, int n0, int k0, int lane, uint32_t (&b)[4])
+{
+    const int row = n0 + (lane & 7) + ((lane >> 4) & 1) * 8, col = k0 + ((lane >> 3) & 1) * 8;
+    ldmatrix_x4(smem_u32(tile + row * pitch + col * 2), b[0], b[1], b[2], b[3]);
+}
+// B fragments of two groups of eight channels, contraction over tokens k0 .. k0 + 15.
+__device__ __forceinline__ void channels_b(const unsigned char* tile, int pitch, int k0, int n0, int lane, uint32_t (&b)[4])
+{
+    const int row = k0 + (lane & 7) + ((lane >> 3) & 1) * 8, col = n0 + ((lane >> 4) & 1) * 8;
+    ldmatrix_x4_trans(smem_u32(tile + row * pitch + col * 2), b[0], b[1], b[2], b[3]);
+}
+// Where the transposed 16 x 16 block (features m0 .., tokens n0 ..) of rows [token][feature] lies for ldmatrix /
+// stmatrix .trans: registers 0, 1: the first eight tokens, rows lane/4 and lane/4 + 8; 2, 3: the next eight.
+__device__ __forceinline__ uint32_t transposed_at(const unsigned char* tile, int pitch, int n0, int m0, int lane)
+{
+    const int row = n0 + (lane & 7) + ((lane >> 4) & 1) * 8, col = m0 + ((lane >> 3) & 1) * 8;
+    return smem_u32(tile + row * pitch + col * 2);
+}
+
+// ---------------------------------------------------------------------------------------------
+// First stream.  GRAD: Q, dY -> dQ, partial dS | dz.  Without GRAD: K, V -> partial S | z (the state itself, for a
+// backward pass that was given none).  grid (chunks, slabs); a CTA works through its chunk's tiles.  A warp owns
+// 16 features: it holds its rows of S (head, tail) and of dS in registers, so the products of a tile are
+//     t^T [16 x TILE] = S [16 x dv] dY^T         and        dS [16 x dv] += (w f)^T [16 x TILE] dY
+// and the accumulators of the first have the layout of the second's left operand: phi, the quotient and the
+// difference are done where the numbers lie, and only the two sums per token (den and f . t) cross warps.
+// ---------------------------------------------------------------------------------------------
+template <int DK, int DV, int KIND, bool GRAD>
+__global__ void __launch_bounds__(32 * BackwardCfg<DK, DV>::WQ)
+backward_state_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* __restrict__ dy, const float* __restrict__ state,
+                      __nv_bfloat16* __restrict__ dq, float* __restrict__ partials, int N, int chunks, SlabLayout Lk,
+                      SlabLayout Lv, BackwardScales sc)
+{
+    using C = BackwardCfg<DK, DV>;
+    constexpr int TILE = C::TILE, THREADS = 32 * C::WQ, NT = TILE / 8;
+    extern __shared__ __align__(16) unsigned char smem[];
+    float2* sums = reinterpret_cast<float2*>(smem + 2 * C::STAGE);  // [WQ][TILE]
+    __shared__ float scratch[33];
+    const int slab = blockIdx.y, chunk = blockIdx.x, warp = threadIdx.x / 32, lane = threadIdx.x & 31, m0 = warp * 16;
+    const int tiles = (N + TILE - 1) / TILE;
+    const int t_begin = static_cast<int>(static_cast<long long>(chunk) * tiles / chunks);
+    const int t_end = static_cast<int>(static_cast<long long>(chunk + 1) * tiles / chunks);
+    q += slab_base(Lk, slab);
+    dy += slab_base(Lv, slab);
+    if (GRAD) dq += slab_base(Lk, slab);
+
+    for (int s = 0; s < 2; ++s) {
+        clear_padding<DK, C::PITCHK, TILE, THREADS>(smem + s * C::STAGE);
+        clear_padding<DV, C::PITCHV, TILE, THREADS>(smem + s * C::STAGE + TILE * C::PITCHK);
+    }
+    pdl_launch_dependents();
+    pdl_wait();
+    auto fetch = [&](int t) {
+        unsigned char* st = smem + (t & 1) * C::STAGE;
+        load_tile<DK, C::PITCHK, TILE, THREADS>(st, q, Lk.row_stride, t * TILE, N);
+        load_tile<DV, C::PITCHV, TILE, THREADS>(st + TILE * C::PITCHK, dy, Lv.row_stride, t * TILE, N);
+        cp_async_commit();
+    };
+    if (t_begin < t_end) fetch(t_begin);
+
+    uint32_t s_hi[C::VP / 16][4], s_lo[C::VP / 16][4];
+    float z[2] = {0.0f, 0.0f};
+    float unscale_t = 1.0f, scale_w = 1.0f;
+    if (GRAD) {
+        const float* S = state + static_cast<size_t>(slab) * grad_state_floats(DK, DV);
+        for (int r = 0; r < 2; ++r)
+            if (m0 + lane / 4 + 8 * r < DK) z[r] = S[DK * DV + m0 + lane / 4 + 8 * r];
+        float scale_s = 1.0f;
+        if (sc.scaled) {
+            // fp16: S and w f by powers of two that keep head and tail inside the format.  w f is at most 1 / min z
+            // where features are not negative, so 2^12 min z bounds it; a z of zero or less says nothing, and then
+            // (or where some z is far below the others) the largest z does.
+            float big = 0.0f, z_max = 0.0f, z_inv = 0.0f;
+            for (int i = threadIdx.x; i < DK * DV; i += THREADS) big = fmaxf(big, fabsf(S[i]));
+            for (int i = threadIdx.x; i < DK; i += THREADS) {
+                const float v = S[DK * DV + i];
+                z_max = fmaxf(z_max, v);
+                z_inv = fmaxf(z_inv, v > 0.0f ? 1.0f / v : 3.0e38f);
+            }
+            big = block_max(big, scratch, C::WQ);
+            z_max = block_max(z_max, scratch, C::WQ);
+            z_inv = block_max(z_inv, scratch, C::WQ);
+            scale_s = pow2_scale(big, 12);
+            unscale_t = 1.0f / scale_s;
+            if (sc.eps >= 0.0f) scale_w = fmaxf(pow2_scale(z_inv, 12), 1.0f / pow2_scale(z_max, 4));
+        }
+        load_state_rows<KIND, DK, DV>(S, m0, lane, scale_s, s_hi, s_lo);
+    }
+    float acc[C::VP / 8][4];
+#pragma unroll
+    for (int n = 0; n < C::VP / 8; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[n][i] = 0.0f;
+    float dz[2] = {0.0f, 0.0f};
+
+    for (int t = t_begin; t < t_end; ++t) {
+        cp_async_wait_all();
+        __syncthreads();  // the tile has landed, and everybody is done with the other stage
+        if (t + 1 < t_end) fetch(t + 1);
+        unsigned char* tq = smem + (t & 1) * C::STAGE;
+        unsigned char* tg = tq + TILE * C::PITCHK;
+
+        float tt[NT][4];
+        if (GRAD) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) tt[j][i] = 0.0f;
+#pragma unroll
+            for (int s = 0; s < C::VP / 16; ++s)
+#pragma unroll
+                for (int j = 0; j < NT; j += 2) {
+                    uint32_t b[4];
+                    tokens_b(tg, C::PITCHV, j * 8, s * 16, lane, b);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        mma_16816<KIND>(tt[j + h], s_lo[s][0], s_lo[s][1], s_lo[s][2], s_lo[s][3], b[2 * h], b[2 * h + 1]);
+                        mma_16816<KIND>(tt[j + h], s_hi[s][0], s_hi[s][1], s_hi[s][2], s_hi[s][3], b[2 * h], b[2 * h + 1]);
+                    }
+                }
+        }
+        uint32_t x[NT][2];  // the warp's features of the tile's tokens, transposed
+#pragma unroll
+        for (int j = 0; j < NT; j += 2)
+            ldmatrix_x4_trans(transposed_at(tq, C::PITCHK, j * 8, m0, lane), x[j][0], x[j][1], x[j + 1][0], x[j + 1][1]);
+
+        if (GRAD && sc.eps >= 0.0f) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {  // the thread's two tokens of the group
+                    float den = 0.0f, ft = 0.0f;
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const float v = e == 0 ? pair_lo<KIND>(x[j][r]) : pair_hi<KIND>(x[j][r]);
+                        const float f = phi<KIND>(v);
+                        den = fmaf(f, z[r], den);
+                        ft = fmaf(f, tt[j][2 * r + e], ft);
+                    }
+#pragma unroll
+                    for (int o = 4; o < 32; o <<= 1) {
+                        den += __shfl_xor_sync(0xffffffffu, den, o);
+                        ft += __shfl_xor_sync(0xffffffffu, ft, o);
+                    }
+                    if (lane < 4) sums[warp * TILE + j * 8 + 2 * lane + e] = make_float2(den, ft);
+                }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int j = 0; j < NT; j += 2) {
+            uint32_t a_hi[4], a_lo[4], out[4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float wf[2][2], d[2][2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int tok = (j + h) * 8 + 2 * (lane & 3) + e;
+                    const bool in = t * TILE + tok < N;
+                    float w = in ? 1.0f : 0.0f, c = 0.0f;
+                    if (GRAD && sc.eps >= 0.0f) {
+                        float den = 0.0f, ft = 0.0f;
+#pragma unroll
+                        for (int i = 0; i < C::WQ; ++i) {
+                            const float2 o = sums[i * TILE + tok];
+                            den += o.x;
+                            ft += o.y;
+                        }
+                        w = in ? 1.0f / (den + sc.eps) : 0.0f;
+                        c = in ? ft * w : 0.0f;  // scaled as S is
+                    }
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const float v = e == 0 ? pair_lo<KIND>(x[j + h][r]) : pair_hi<KIND>(x[j + h][r]);
+                        float f, slope;
+                        phi_and_slope<KIND>(v, &f, &slope);
+                        wf[r][e] = w * f;
+                        if (GRAD) {
+                            d[r][e] = slope * (w * ((tt[j + h][2 * r + e] - c * z[r]) * unscale_t));
+                            dz[r] = fmaf(-wf[r][e], c * unscale_t, dz[r]);
+                        } else {
+                            dz[r] += wf[r][e];
+                        }
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    split_pair<KIND>(wf[r][0] * scale_w, wf[r][1] * scale_w, &a_hi[2 * h + r], &a_lo[2 * h + r]);
+                    if (GRAD) out[2 * h + r] = pack_pair<KIND>(d[r][0], d[r][1]);
+                }
+            }
+            if (GRAD) stmatrix_x4_trans(transposed_at(tq, C::PITCHK, j * 8, m0, lane), out[0], out[1], out[2], out[3]);
+#pragma unroll
+            for (int n = 0; n < C::VP / 16; ++n) {
+                uint32_t b[4];
+                channels_b(tg, C::PITCHV, j * 8, n * 16, lane, b);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    mma_16816<KIND>(acc[2 * n + h], a_lo[0], a_lo[1], a_lo[2], a_lo[3], b[2 * h], b[2 * h + 1]);
+                    mma_16816<KIND>(acc[2 * n + h], a_hi[0], a_hi[1], a_hi[2], a_hi[3], b[2 * h], b[2 * h + 1]);
+                }
+            }
+        }
+        if (GRAD) {
+            __syncthreads();  // dQ of all features is in place of Q
+            store_tile<DK, C::PITCHK, TILE, THREADS>(tq, dq, Lk.row_stride, t * TILE, N);
+        }
+    }
+    float* out = partials + (static_cast<size_t>(slab) * chunks + chunk) * grad_state_floats(DK, DV);
+    const float unscale_w = 1.0f / scale_w;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int row = m0 + lane / 4 + 8 * r;
+#pragma unroll
+        for (int n = 0; n < C::VP / 8; ++n) {
+            const int col = n * 8 + 2 * (lane & 3);
+            if (row < DK && col < DV)
+                *reinterpret_cast<float2*>(out + row * DV + col) = make_float2(acc[n][2 * r] * unscale_w, acc[n][2 * r + 1] * unscale_w);
+        }
+        dz[r] += __shfl_xor_sync(0xffffffffu, dz[r], 1);
+        dz[r] += __shfl_xor_sync(0xffffffffu, dz[r], 2);
+        if ((lane & 3) == 0 && row < DK) out[DK * DV + row] = dz[r];
+    }
+}
+
+// Sum of a slab's partials in the order of its chunks.
+static __global__ void __launch_bounds__(256)
+backward_reduce_kernel(const float* __restrict__ partials, float* __restrict__ out, int floats, int chunks)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= floats) return;
+    const float* p = partials + static_cast<size_t>(blockIdx.y) * chunks * floats + i;
+    float s = 0.0f;
+#pragma unroll 8
+    for (int c = 0; c < chunks; ++c) s += p[static_cast<size_t>(c) * floats];
+    out[static_cast<size_t>(blockIdx.y) * floats + i] = s;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Second stream: K, V -> dK, dV with dS | dz at hand.  A warp owns 16 features of dK and 16 channels of dV:
+//     dK^T [16 x TILE] = dS [16 x dv] V^T + dz          dV^T [16 x TILE] = dS^T [16 x dk] phi(K)^T
+// phi(K) crosses warps through shared memory as head and tail.
+// ---------------------------------------------------------------------------------------------
+template <int DK, int DV, int KIND>
+__global__ void __launch_bounds__(32 * BackwardCfg<DK, DV>::WKV)
+backward_kv_kernel(const __nv_bfloat16* __restrict__ k, const __nv_bfloat16* __restrict__ v, const float* __restrict__ grad_state,
+                   __nv_bfloat16* __restrict__ dk, __nv_bfloat16* __restrict__ dv, int N, int chunks, SlabLayout Lk,
+                   SlabLayout Lv, BackwardScales sc)
+{
+    using C = BackwardCfg<DK, DV>;
+    constexpr int TILE = C::TILE, THREADS = 32 * C::WKV, NT = TILE / 8;
+    extern __shared__ __align__(16) unsigned char smem[];
+    unsigned char* f_hi = smem + 2 * C::STAGE;
+    unsigned char* f_lo = f_hi + TILE * C::PITCHK;
+    __shared__ float scratch[33];
+    const int slab = blockIdx.y, chunk = blockIdx.x, warp = threadIdx.x / 32, lane = threadIdx.x & 31, m0 = warp * 16;
+    const int tiles = (N + TILE - 1) / TILE;
+    const int t_begin = static_cast<int>(static_cast<long long>(chunk) * tiles / chunks);
+    const int t_end = static_cast<int>(static_cast<long long>(chunk + 1) * tiles / chunks);
+    k += slab_base(Lk, slab);
+    dk += slab_base(Lk, slab);
+    v += slab_base(Lv, slab);
+    dv += slab_base(Lv, slab);
+    for (int s = 0; s < 2; ++s) {
+        clear_padding<DK, C::PITCHK, TILE, THREADS>(smem + s * C::STAGE);
+        clear_padding<DV, C::PITCHV, TILE, THREADS>(smem + s * C::STAGE + TILE * C::PITCHK);
+    }
+    pdl_launch_dependents();
+    pdl_wait();
+    auto fetch = [&](int t) {
+        unsigned char* st = smem + (t & 1) * C::STAGE;
+        load_tile<DK, C::PITCHK, TILE, THREADS>(st, k, Lk.row_stride, t * TILE, N);
+        load_tile<DV, C::PITCHV, TILE, THREADS>(st + TILE * C::PITCHK, v, Lv.row_stride, t * TILE, N);
+        cp_async_commit();
+    };
+    if (t_begin < t_end) fetch(t_begin);
+
+    const float* S = grad_state + static_cast<size_t>(slab) * grad_state_floats(DK, DV);
+    float scale = 1.0f;
+    if (sc.scaled) {
+        float big = 0.0f;
+        for (int i = threadIdx.x; i < DK * DV; i += THREADS) big = fmaxf(big, fabsf(S[i]));
+        scale = pow2_scale(block_max(big, scratch, C::WKV), 12);
+    }
+    const float unscale = 1.0f / scale;
+    uint32_t r_hi[C::VP / 16][4], r_lo[C::VP / 16][4], c_hi[C::KP / 16][4], c_lo[C::KP / 16][4];
+    load_state_rows<KIND, DK, DV>(S, m0, lane, scale, r_hi, r_lo);
+    load_state_cols<KIND, DK, DV>(S, m0, lane, scale, c_hi, c_lo);
+    float dz[2] = {0.0f, 0.0f};
+    for (int r = 0; r < 2; ++r)
+        if (m0 + lane / 4 + 8 * r < DK) dz[r] = S[DK * DV + m0 + lane / 4 + 8 * r];
+
+    for (int t = t_begin; t < t_end; ++t) {
+        cp_async_wait_all();
+        __syncthreads();
+        if (t + 1 < t_end) fetch(t + 1);
+        unsigned char* tk = smem + (t & 1) * C::STAGE;
+        unsigned char* tv = tk + TILE * C::PITCHK;
+        if (m0 < C::KP) {
+            float acc[NT][4];
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[j][i] = 0.0f;
+#pragma unroll
+            for (int s = 0; s < C::VP / 16; ++s)
+#pragma unroll
+                for (int j = 0; j < NT; j += 2) {
+                    uint32_t b[4];
+                    tokens_b(tv, C::PITCHV, j * 8, s * 16, lane, b);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        mma_16816<KIND>(acc[j + h], r_lo[s][0], r_lo[s][1], r_lo[s][2], r_lo[s][3], b[2 * h], b[2 * h + 1]);
+                        mma_16816<KIND>(acc[j + h], r_hi[s][0], r_hi[s][1], r_hi[s][2], r_hi[s][3], b[2 * h], b[2 * h + 1]);
+                    }
+                }
+#pragma unroll
+            for (int j = 0; j < NT; j += 2) {
+                uint32_t x[4], hi[4], lo[4], out[4];
+                const uint32_t at = transposed_at(tk, C::PITCHK, j * 8, m0, lane);
+                ldmatrix_x4_trans(at, x[0], x[1], x[2], x[3]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {  // i = 2 * (group of eight tokens) + (row of the fragment)
+                    const int r = i & 1;
+                    float f0, f1, s0, s1;
+                    phi_and_slope<KIND>(pair_lo<KIND>(x[i]), &f0, &s0);
+                    phi_and_slope<KIND>(pair_hi<KIND>(x[i]), &f1, &s1);
+                    split_pair<KIND>(f0, f1, &hi[i], &lo[i]);
+                    out[i] = pack_pair<KIND>(s0 * fmaf(acc[j + i / 2][2 * r], unscale, dz[r]),
+                                             s1 * fmaf(acc[j + i / 2][2 * r + 1], unscale, dz[r]));
+                }
+                stmatrix_x4_trans(transposed_at(f_hi, C::PITCHK, j * 8, m0, lane), hi[0], hi[1], hi[2], hi[3]);
+                stmatrix_x4_trans(transposed_at(f_lo, C::PITCHK, j * 8, m0, lane), lo[0], lo[1], lo[2], lo[3]);
+                stmatrix_x4_trans(at, out[0], out[1], out[2], out[3]);
+            }
+        }
+        __syncthreads();  // phi(K) and dK are in place; V has been read
+        if (m0 < C::VP) {
+            float acc[NT][4];
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[j][i] = 0.0f;
+#pragma unroll
+            for (int s = 0; s < C::KP / 16; ++s)
+#pragma unroll
+                for (int j = 0; j < NT; j += 2) {
+                    uint32_t b[4], bl[4];
+                    tokens_b(f_hi, C::PITCHK, j * 8, s * 16, lane, b);
+                    tokens_b(f_lo, C::PITCHK, j * 8, s * 16, lane, bl);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        mma_16816<KIND>(acc[j + h], c_lo[s][0], c_lo[s][1], c_lo[s][2], c_lo[s][3], b[2 * h], b[2 * h + 1]);
+                        mma_16816<KIND>(acc[j + h], c_hi[s][0], c_hi[s][1], c_hi[s][2], c_hi[s][3], bl[2 * h], bl[2 * h + 1]);
+                        mma_16816<KIND>(acc[j + h], c_hi[s][0], c_hi[s][1], c_hi[s][2], c_hi[s][3], b[2 * h], b[2 * h + 1]);
+                    }
+                }
+#pragma unroll
+            for (int j = 0; j < NT; j += 2) {
+                uint32_t out[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    out[i] = pack_pair<KIND>(acc[j + i / 2][2 * (i & 1)] * unscale, acc[j + i / 2][2 * (i & 1) + 1] * unscale);
+                stmatrix_x4_trans(transposed_at(tv, C::PITCHV, j * 8, m0, lane), out[0], out[1], out[2], out[3]);
+            }
+        }
+        __syncthreads();
+        store_tile<DK, C::PITCHK, TILE, THREADS>(tk, dk, Lk.row_stride, t * TILE, N);
+        store_tile<DV, C::PITCHV, TILE, THREADS>(tv, dv, Lv.row_stride, t * TILE, N);
+    }
+}
+
+}  // namespace lf

@@ -1,0 +1,525 @@
+// Host side of include/linfusion_block.h: argument checks and launches of the rotary positions and of the norms
+// around a block.
+#include "../../include/linfusion_block.h"
+
+#include <algorithm>
+#include <cmath>
+#include <initializer_list>
+
+#include "block_kernels.cuh"
+#include "host_util.h"
+
+using namespace lf;
+
+namespace {
+
+// The current device and its SM count.
+struct Here {
+    int device, sms;
+    linfusion_status_t st;
+};
+Here here()
+{
+    Here h = {0, 0, LINFUSION_OK};
+    if (cudaGetDevice(&h.device) != cudaSuccess) {
+        cudaGetLastError();
+        h.st = LINFUSION_ERR_CUDA;
+        return h;
+    }
+    h.sms = device_sm_count(h.device);
+    if (h.sms == -2) h.st = LINFUSION_ERR_UNSUPPORTED;
+    else if (h.sms < 0) h.st = LINFUSION_ERR_CUDA;
+    return h;
+}
+
+linfusion_status_t end(cudaError_t e)
+{
+    if (e == cudaSuccess) return LINFUSION_OK;
+    cudaGetLastError();
+    return LINFUSION_ERR_CUDA;
+}
+
+bool good_stride(int64_t s) { return s >= 0 && s % 8 == 0 && s < (int64_t(1) << 56); }
+
+// The bytes from the first to behind the last element that strides reach, as a half-open range.
+struct Extent {
+    const char* p;
+    size_t bytes;
+};
+Extent extent(const void* p, int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t n2, int64_t s2, int64_t row)
+{
+    const int64_t last = (n0 - 1) * s0 + (n1 - 1) * s1 + (n2 - 1) * s2 + row;
+    return {static_cast<const char*>(p), static_cast<size_t>(last) * 2};
+}
+bool meet(const Extent& a, const Extent& b) { return overlaps(a.p, a.bytes, b.p, b.bytes); }
+
+// Rows of `row` elements over axes of length n and stride s: no two of them share an element when, taken from the
+// smallest stride to the largest, each stride steps over everything below it.  Axes of length one do not count.
+struct Axis {
+    int64_t n, s;
+};
+bool rows_disjoint(std::initializer_list<Axis> axes, int64_t row)
+{
+    Axis a[4];
+    int count = 0;
+    for (const Axis& x : axes)
+        if (x.n > 1) a[count++] = x;
+    std::sort(a, a + count, [](const Axis& x, const Axis& y) { return x.s < y.s; });
+    int64_t reach = row;
+    for (int i = 0; i < count; ++i) {
+        if (a[i].s < reach) return false;
+        reach += (a[i].n - 1) * a[i].s;
+    }
+    return true;
+}
+
+// ------------------------------------------------------------------------------------------ rope
+linfusion_status_t check_rope(const linfusion_rope_desc_t* d, int* pairs)
+{
+    if (d == nullptr) return LINFUSION_ERR_INVALID_ARG;
+    if (d->B <= 0 || d->N <= 0 || d->d <= 0 || d->d % 8 != 0) return LINFUSION_ERR_INVALID_ARG;
+    if (d->n_axes < 1 || d->n_axes > LINFUSION_ROPE_MAX_AXES) return LINFUSION_ERR_INVALID_ARG;
+    if (!std::isfinite(d->theta) || d->theta <= 0.0) return LINFUSION_ERR_INVALID_ARG;
+    if ((d->interleaved & ~1) != 0 || (d->backward & ~1) != 0) return LINFUSION_ERR_INVALID_ARG;
+    if (d->d > LINFUSION_ROPE_MAX_WIDTH || d->B > 65535) return LINFUSION_ERR_UNSUPPORTED;
+    if ((d->flags & ~LINFUSION_DTYPE_FP16) != 0u) return LINFUSION_ERR_UNSUPPORTED;
+    int64_t sum = 0;
+    for (int a = 0; a < d->n_axes; ++a) {
+        if (d->pairs[a] < 0) return LINFUSION_ERR_INVALID_ARG;
+        sum += d->pairs[a];
+    }
+    if (sum < 1 || 2 * sum > d->d) return LINFUSION_ERR_INVALID_ARG;
+    *pairs = static_cast<int>(sum);
+    return LINFUSION_OK;
+}
+
+linfusion_status_t check_rope_tensor(const linfusion_rope_desc_t& d, const linfusion_rope_tensor_t& t)
+{
+    if (t.in == nullptr || t.out == nullptr || !is_aligned(t.in, 16) || !is_aligned(t.out, 16)) return LINFUSION_ERR_INVALID_ARG;
+    for (const int64_t s : {t.in_batch, t.in_token, t.in_head, t.out_batch, t.out_token, t.out_head})
+        if (!good_stride(s)) return LINFUSION_ERR_INVALID_ARG;
+    // no two output rows on top of one another
+    if (!rows_disjoint({{d.B, t.out_batch}, {d.N, t.out_token}, {t.heads, t.out_head}}, d.d)) return LINFUSION_ERR_INVALID_ARG;
+    const Extent in = extent(t.in, d.B, t.in_batch, d.N, t.in_token, t.heads, t.in_head, d.d);
+    const Extent out = extent(t.out, d.B, t.out_batch, d.N, t.out_token, t.heads, t.out_head, d.d);
+    const bool in_place = t.in == t.out && (d.B == 1 || t.in_batch == t.out_batch) && (d.N == 1 || t.in_token == t.out_token) &&
+                          (t.heads == 1 || t.in_head == t.out_head);
+    return in_place || !meet(in, out) ? LINFUSION_OK : LINFUSION_ERR_INVALID_ARG;
+}
+
+struct RopeView {
+    const char* p;
+    int64_t heads, batch, token, head;
+};
+RopeView rope_view(const linfusion_rope_tensor_t& t, bool out)
+{
+    return out ? RopeView{static_cast<const char*>(t.out), t.heads, t.out_batch, t.out_token, t.out_head}
+               : RopeView{static_cast<const char*>(t.in), t.heads, t.in_batch, t.in_token, t.in_head};
+}
+// Two views share no element: they lie apart, or they are interlaced views of one tensor with the same strides (Q and K
+// side by side in each token, or one behind the other in each batch entry).  What neither test can tell is refused.
+bool views_apart(const linfusion_rope_desc_t& d, RopeView a, RopeView b)
+{
+    const Extent ea = extent(a.p, d.B, a.batch, d.N, a.token, a.heads, a.head, d.d);
+    const Extent eb = extent(b.p, d.B, b.batch, d.N, b.token, b.heads, b.head, d.d);
+    if (!meet(ea, eb)) return true;
+    if ((d.B > 1 && a.batch != b.batch) || (d.N > 1 && a.token != b.token)) return false;
+    if (b.p < a.p) std::swap(a, b);
+    const int64_t bytes = b.p - a.p;
+    if (bytes % 16 != 0) return false;
+    const int64_t apart = bytes / 2, heads_a = (a.heads - 1) * a.head + d.d, heads_b = (b.heads - 1) * b.head + d.d;
+    if (apart >= heads_a && rows_disjoint({{d.B, a.batch}, {d.N, a.token}}, apart + heads_b)) return true;
+    if (a.heads > 1 && b.heads > 1 && a.head != b.head) return false;
+    const RopeView& more = a.heads >= b.heads ? a : b;
+    return rows_disjoint({{d.B, a.batch}, {d.N, a.token}, {more.heads, more.head}, {2, apart}}, d.d);
+}
+
+template <int KIND>
+cudaError_t launch_rope(const RopeParams& p, bool interleaved, dim3 grid, cudaStream_t s)
+{
+    if (interleaved) rope_kernel<KIND, true, 8><<<grid, kRopeThreads, 0, s>>>(p);
+    else if (p.P % 8 == 0) rope_kernel<KIND, false, 8><<<grid, kRopeThreads, 0, s>>>(p);
+    else if (p.P % 4 == 0) rope_kernel<KIND, false, 4><<<grid, kRopeThreads, 0, s>>>(p);
+    else if (p.P % 2 == 0) rope_kernel<KIND, false, 2><<<grid, kRopeThreads, 0, s>>>(p);
+    else rope_kernel<KIND, false, 1><<<grid, kRopeThreads, 0, s>>>(p);
+    return cudaGetLastError();
+}
+
+// ------------------------------------------------------------------------------------------ norms
+linfusion_status_t check_norm(const linfusion_block_norm_desc_t* d)
+{
+    if (d == nullptr) return LINFUSION_ERR_INVALID_ARG;
+    if (d->B <= 0 || d->N <= 0 || d->C <= 0) return LINFUSION_ERR_INVALID_ARG;
+    if (!std::isfinite(d->eps) || d->eps < 0.0f || !std::isfinite(d->residual_scale)) return LINFUSION_ERR_INVALID_ARG;
+    if (d->C % 8 != 0 || d->C > LINFUSION_BLOCK_NORM_MAX_C || d->B > 65535) return LINFUSION_ERR_UNSUPPORTED;
+    if ((d->flags & ~LINFUSION_DTYPE_FP16) != 0u) return LINFUSION_ERR_UNSUPPORTED;
+    for (const int32_t n : {d->pre, d->post})
+        if (n < LINFUSION_NORM_NONE || n > LINFUSION_NORM_RMS) return LINFUSION_ERR_UNSUPPORTED;
+    return LINFUSION_OK;
+}
+
+bool rows_given(const linfusion_rows_t* r) { return r != nullptr && r->p != nullptr; }
+bool rows_ok(const linfusion_rows_t* r)
+{
+    return rows_given(r) && is_aligned(r->p, 16) && good_stride(r->batch) && good_stride(r->row);
+}
+Rows to_rows(const linfusion_rows_t* r)
+{
+    Rows o = {nullptr, 0, 0};
+    if (rows_given(r)) o = {static_cast<char*>(r->p), r->batch * 2, r->row * 2};
+    return o;
+}
+bool channels_ok(const linfusion_channels_t& c) { return c.p == nullptr || (is_aligned(c.p, 16) && good_stride(c.batch)); }
+Channels to_channels(const linfusion_channels_t& c) { return {static_cast<const char*>(c.p), c.batch * 2}; }
+
+// What the forward and the backward pass ask of the vectors.
+bool vectors_ok(const linfusion_block_norm_desc_t& d, const linfusion_block_norm_vectors_t& v, bool branch)
+{
+    if (!channels_ok(v.gate) || !channels_ok(v.scale) || !channels_ok(v.shift)) return false;
+    for (const void* p : {v.pre_weight, v.pre_bias, v.post_weight, v.post_bias})
+        if (p != nullptr && !is_aligned(p, 16)) return false;
+    if ((v.scale.p == nullptr) != (v.shift.p == nullptr)) return false;
+    if (d.pre == LINFUSION_NORM_NONE && (v.scale.p != nullptr || v.pre_weight != nullptr || v.pre_bias != nullptr)) return false;
+    if (d.post == LINFUSION_NORM_NONE && (v.post_weight != nullptr || v.post_bias != nullptr)) return false;
+    if (!branch && (d.post != LINFUSION_NORM_NONE || v.gate.p != nullptr)) return false;
+    return branch || d.pre != LINFUSION_NORM_NONE;
+}
+
+Extent rows_extent(const linfusion_block_norm_desc_t& d, const linfusion_rows_t* r)
+{
+    return extent(r->p, d.B, r->batch, d.N, r->row, 1, 0, d.C);
+}
+bool out_ok(const linfusion_block_norm_desc_t& d, const linfusion_rows_t* r)
+{
+    return rows_ok(r) && rows_disjoint({{d.B, r->batch}, {d.N, r->row}}, d.C);
+}
+// `out` shares no memory with `in`, or lies exactly over it and may.
+bool apart(const linfusion_block_norm_desc_t& d, const linfusion_rows_t* out, const linfusion_rows_t* in, bool may_lie_over)
+{
+    if (!rows_given(in) || !meet(rows_extent(d, out), rows_extent(d, in))) return true;
+    return may_lie_over && out->p == in->p && (d.B == 1 || out->batch == in->batch) && (d.N == 1 || out->row == in->row);
+}
+// `out` shares no memory with a vector.
+bool apart(const linfusion_block_norm_desc_t& d, const linfusion_rows_t* out, const linfusion_block_norm_vectors_t& v)
+{
+    const Extent o = rows_extent(d, out);
+    for (const linfusion_channels_t& c : {v.gate, v.scale, v.shift})
+        if (c.p != nullptr && meet(o, extent(c.p, d.B, c.batch, 1, 0, 1, 0, d.C))) return false;
+    for (const void* p : {v.pre_weight, v.pre_bias, v.post_weight, v.post_bias})
+        if (p != nullptr && meet(o, extent(p, 1, 0, 1, 0, 1, 0, d.C))) return false;
+    return true;
+}
+
+// How rows are dealt out: groups of `warps` warps, `per_cta` of them in a block, `chunks` for each batch entry.
+struct NormPlan {
+    int warps, per_cta, chunks, groups, ctas;
+};
+// `rows_at_once`: rows a group loads together; `warps_per_sm`: warps that an SM is to hold.
+NormPlan norm_plan(const linfusion_block_norm_desc_t& d, int sms, int rows_at_once, int warps_per_sm)
+{
+    NormPlan p;
+    p.warps = (d.C + 255) / 256;
+    p.per_cta = p.warps >= 4 ? 1 : 4 / p.warps;
+    long long target = static_cast<long long>(sms) * (warps_per_sm / p.warps > 0 ? warps_per_sm / p.warps : 1);
+    long long chunks = (target + d.B - 1) / d.B;
+    const long long most = (d.N + rows_at_once - 1) / rows_at_once;
+    if (chunks > most) chunks = most;
+    if (chunks < 1) chunks = 1;
+    p.chunks = static_cast<int>(chunks);
+    p.groups = p.chunks * d.B;
+    p.ctas = (p.groups + p.per_cta - 1) / p.per_cta;
+    return p;
+}
+constexpr int kForwardRows = 4, kBackwardRows = 2;
+constexpr int kForwardWarpsPerSm = 32, kBackwardWarpsPerSm = 16;
+
+void fill(NormParams* p, const linfusion_block_norm_desc_t& d, const linfusion_block_norm_vectors_t& v, const NormPlan& plan, bool branch)
+{
+    p->gate = to_channels(v.gate);
+    p->scale = to_channels(v.scale);
+    p->shift = to_channels(v.shift);
+    p->pre_w = static_cast<const char*>(v.pre_weight);
+    p->pre_b = static_cast<const char*>(v.pre_bias);
+    p->post_w = static_cast<const char*>(v.post_weight);
+    p->post_b = static_cast<const char*>(v.post_bias);
+    p->N = d.N;
+    p->C = d.C;
+    p->warps = plan.warps;
+    p->chunks = plan.chunks;
+    p->groups = plan.groups;
+    p->eps = d.eps;
+    p->rs = branch ? d.residual_scale : 1.0f;  // without a branch y is x itself
+    p->inv_c = 1.0f / static_cast<float>(d.C);
+}
+
+template <int KIND, int R, int T, bool BACKWARD>
+cudaError_t launch_norm(const NormParams& p, const NormPlan& plan, int post, int pre, bool branch, cudaStream_t s)
+{
+    const dim3 grid(plan.ctas), block(32 * plan.warps * plan.per_cta);
+    const size_t smem = plan.warps > 1 ? static_cast<size_t>(plan.per_cta) * 2 * R * kNormMaxWarps * sizeof(float2) : 0;
+#define LF_NORM(POST, PRE, A)                                                                 \
+    if (BACKWARD) block_norm_backward_kernel<KIND, POST, PRE, A, R, T><<<grid, block, smem, s>>>(p); \
+    else block_norm_kernel<KIND, POST, PRE, A, R, T><<<grid, block, smem, s>>>(p)
+    if (!branch) {
+        if (pre == LINFUSION_NORM_LAYER) { LF_NORM(kNormNone, kNormLayer, false); }
+        else { LF_NORM(kNormNone, kNormRms, false); }
+        return cudaGetLastError();
+    }
+    switch (post * 3 + pre) {
+        case 0: LF_NORM(kNormNone, kNormNone, true); break;
+        case 1: LF_NORM(kNormNone, kNormLayer, true); break;
+        case 2: LF_NORM(kNormNone, kNormRms, true); break;
+        case 3: LF_NORM(kNormLayer, kNormNone, true); break;
+        case 4: LF_NORM(kNormLayer, kNormLayer, true); break;
+        case 5: LF_NORM(kNormLayer, kNormRms, true); break;
+        case 6: LF_NORM(kNormRms, kNormNone, true); break;
+        case 7: LF_NORM(kNormRms, kNormLayer, true); break;
+        default: LF_NORM(kNormRms, kNormRms, true); break;
+    }
+#undef LF_NORM
+    return cudaGetLastError();
+}
+
+template <bool BACKWARD>
+cudaError_t launch_norm_kind(const linfusion_block_norm_desc_t& d, const NormParams& p, const NormPlan& plan, bool branch,
+                             int rows_at_once, cudaStream_t s)
+{
+    const bool half = (d.flags & LINFUSION_DTYPE_FP16) != 0u;
+    constexpr int bf = make_kind(kPhiIdentity, kDtypeBf16), hf = make_kind(kPhiIdentity, kDtypeFp16);
+    constexpr int R = BACKWARD ? kBackwardRows : kForwardRows;
+    // Threads of a block: 256 up to C = 2048 (and then several rows at once), 512 or 1024 beyond, where fewer registers
+    // a thread are left and the many warps of a row bring enough loads by themselves.
+#define LF_SIZED(ROWS, T) \
+    return half ? launch_norm<hf, ROWS, T, BACKWARD>(p, plan, d.post, d.pre, branch, s) \
+                : launch_norm<bf, ROWS, T, BACKWARD>(p, plan, d.post, d.pre, branch, s)
+    if (plan.warps > 16) LF_SIZED(1, 1024);
+    if (plan.warps > 8) LF_SIZED(1, 512);
+    if (rows_at_once == 1) LF_SIZED(1, 256);
+    LF_SIZED(R, 256);
+#undef LF_SIZED
+}
+
+// Several rows at a time where there are enough of them to occupy every SM all the same.
+int rows_at_once(const linfusion_block_norm_desc_t& d, int sms, int rows, int warps_per_sm)
+{
+    const long long total = static_cast<long long>(d.B) * d.N, warps = (d.C + 255) / 256;
+    if (warps > 8) return 1;
+    return total * warps >= static_cast<long long>(sms) * warps_per_sm * rows ? rows : 1;
+}
+
+NormPlan backward_plan(const linfusion_block_norm_desc_t& d, int sms, int* rows)
+{
+    *rows = rows_at_once(d, sms, kBackwardRows, kBackwardWarpsPerSm);
+    return norm_plan(d, sms, *rows, kBackwardWarpsPerSm);
+}
+
+}  // namespace
+
+extern "C" {
+
+linfusion_status_t linfusion_rope(const linfusion_rope_desc_t* desc, const linfusion_rope_tensor_t* q,
+                                  const linfusion_rope_tensor_t* k, const float* positions, int64_t pos_batch_stride,
+                                  void* cuda_stream)
+{
+    int P = 0;
+    linfusion_status_t st = check_rope(desc, &P);
+    if (st != LINFUSION_OK) return st;
+    const linfusion_rope_tensor_t* given[2] = {q != nullptr && q->heads != 0 ? q : nullptr,
+                                               k != nullptr && k->heads != 0 ? k : nullptr};
+    if (given[0] == nullptr && given[1] == nullptr) return LINFUSION_ERR_INVALID_ARG;
+    if (positions == nullptr || !is_aligned(positions, 4) || pos_batch_stride < 0) return LINFUSION_ERR_INVALID_ARG;
+    const Extent pos = {reinterpret_cast<const char*>(positions),
+                        4 * (static_cast<size_t>(desc->B - 1) * pos_batch_stride + static_cast<size_t>(desc->N) * desc->n_axes)};
+    for (const linfusion_rope_tensor_t* t : given)
+        if (t != nullptr) {
+            if (t->heads < 0) return LINFUSION_ERR_INVALID_ARG;
+            st = check_rope_tensor(*desc, *t);
+            if (st != LINFUSION_OK) return st;
+            if (meet(pos, extent(t->out, desc->B, t->out_batch, desc->N, t->out_token, t->heads, t->out_head, desc->d)))
+                return LINFUSION_ERR_INVALID_ARG;
+        }
+    if (given[0] != nullptr && given[1] != nullptr) {
+        const linfusion_rope_tensor_t &a = *given[0], &b = *given[1];
+        const RopeView ai = rope_view(a, false), ao = rope_view(a, true), bi = rope_view(b, false), bo = rope_view(b, true);
+        if (!views_apart(*desc, ao, bo) || !views_apart(*desc, ao, bi) || !views_apart(*desc, bo, ai)) return LINFUSION_ERR_INVALID_ARG;
+    }
+    const Here at = here();
+    if (at.st != LINFUSION_OK) return at.st;
+
+    RopeParams p = {};
+    int heads = 0;
+    for (int w = 0; w < 2; ++w) {
+        if (given[w] == nullptr) continue;
+        const linfusion_rope_tensor_t& t = *given[w];
+        p.t[w] = {static_cast<const char*>(t.in), static_cast<char*>(t.out), t.heads, t.in_batch * 2, t.in_token * 2,
+                  t.in_head * 2, t.out_batch * 2, t.out_token * 2, t.out_head * 2};
+        heads += t.heads;
+    }
+    p.pos = positions;
+    p.pos_b = pos_batch_stride;
+    p.N = desc->N;
+    p.d = desc->d;
+    p.P = P;
+    p.n_axes = desc->n_axes;
+    p.sign = desc->backward ? -1.0f : 1.0f;
+    const bool interleaved = desc->interleaved != 0;
+    p.pair_items = interleaved ? desc->d / 8 : (P + 7) / 8;
+    p.items = interleaved ? desc->d / 8 : p.pair_items + (desc->d - 2 * P + 7) / 8;
+    for (int a = 0, i = 0; a < desc->n_axes; ++a)
+        for (int j = 0; j < desc->pairs[a]; ++j, ++i) {
+            const double turns = std::pow(desc->theta, -static_cast<double>(j) / desc->pairs[a]) / 6.283185307179586476925;
+            p.axis[i] = static_cast<unsigned char>(a);
+            p.f_hi[i] = static_cast<float>(turns);
+            p.f_lo[i] = static_cast<float>(turns - static_cast<double>(p.f_hi[i]));
+        }
+    // Threads of one head group, and head groups enough to give every SM four blocks where there are few tokens: a
+    // group forms its sines and cosines again, which costs less than idle SMs.
+    const long long threads = static_cast<long long>(desc->N) * p.items;
+    const long long blocks = (threads + kRopeThreads - 1) / kRopeThreads;
+    if (threads + kRopeThreads > 0xffffffffll) return LINFUSION_ERR_UNSUPPORTED;
+    long long groups = (4ll * at.sms + blocks * desc->B - 1) / (blocks * desc->B);
+    if (groups > heads) groups = heads;
+    p.heads_per_group = static_cast<int>((heads + groups - 1) / groups);
+    const long long grid_y = (heads + p.heads_per_group - 1) / p.heads_per_group;
+    if (grid_y > 65535) return LINFUSION_ERR_UNSUPPORTED;
+    const dim3 grid(static_cast<unsigned int>(blocks), static_cast<unsigned int>(grid_y), desc->B);
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    return end((desc->flags & LINFUSION_DTYPE_FP16) != 0u
+                   ? launch_rope<make_kind(kPhiIdentity, kDtypeFp16)>(p, interleaved, grid, s)
+                   : launch_rope<make_kind(kPhiIdentity, kDtypeBf16)>(p, interleaved, grid, s));
+}
+
+linfusion_status_t linfusion_block_norm(const linfusion_block_norm_desc_t* desc, const linfusion_rows_t* x,
+                                        const linfusion_rows_t* a, const linfusion_block_norm_vectors_t* v,
+                                        const linfusion_rows_t* y, const linfusion_rows_t* n, void* cuda_stream)
+{
+    linfusion_status_t st = check_norm(desc);
+    if (st != LINFUSION_OK) return st;
+    const linfusion_block_norm_vectors_t none = {};
+    if (v == nullptr) v = &none;
+    const bool branch = rows_given(a), pre = desc->pre != LINFUSION_NORM_NONE;
+    if (!vectors_ok(*desc, *v, branch) || !rows_ok(x) || (branch && !rows_ok(a))) return LINFUSION_ERR_INVALID_ARG;
+    if (rows_given(y) != branch || rows_given(n) != pre) return LINFUSION_ERR_INVALID_ARG;
+    if (branch && (!out_ok(*desc, y) || !apart(*desc, y, x, true) || !apart(*desc, y, a, true) || !apart(*desc, y, *v)))
+        return LINFUSION_ERR_INVALID_ARG;
+    if (pre && (!out_ok(*desc, n) || !apart(*desc, n, x, false) || !apart(*desc, n, a, false) || !apart(*desc, n, y, false) ||
+                !apart(*desc, n, *v)))
+        return LINFUSION_ERR_INVALID_ARG;
+    const Here at = here();
+    if (at.st != LINFUSION_OK) return at.st;
+    const int rows = rows_at_once(*desc, at.sms, kForwardRows, kForwardWarpsPerSm);
+    const NormPlan plan = norm_plan(*desc, at.sms, rows, kForwardWarpsPerSm);
+    NormParams p = {};
+    fill(&p, *desc, *v, plan, branch);
+    p.x = to_rows(x);
+    p.a = to_rows(a);
+    p.y = to_rows(y);
+    p.n = to_rows(n);
+    return end(launch_norm_kind<false>(*desc, p, plan, branch, rows, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+linfusion_status_t linfusion_block_norm_workspace_bytes(const linfusion_block_norm_desc_t* desc, int32_t sm_count, size_t* bytes)
+{
+    if (bytes == nullptr) return LINFUSION_ERR_INVALID_ARG;
+    const linfusion_status_t st = check_norm(desc);
+    if (st != LINFUSION_OK) return st;
+    int rows = 1;
+    const NormPlan plan = backward_plan(*desc, sm_count > 0 ? sm_count : 148, &rows);
+    *bytes = align_up_256(static_cast<size_t>(4) * plan.groups * desc->C * sizeof(float));
+    return LINFUSION_OK;
+}
+
+linfusion_status_t linfusion_block_norm_backward(const linfusion_block_norm_desc_t* desc, const linfusion_rows_t* y,
+                                                 const linfusion_rows_t* a, const linfusion_block_norm_vectors_t* v,
+                                                 const linfusion_rows_t* dy, const linfusion_rows_t* dn,
+                                                 const linfusion_rows_t* dx, const linfusion_rows_t* da,
+                                                 const linfusion_block_norm_grads_t* grads, void* workspace,
+                                                 size_t workspace_bytes, void* cuda_stream)
+{
+    linfusion_status_t st = check_norm(desc);
+    if (st != LINFUSION_OK) return st;
+    const linfusion_block_norm_vectors_t none = {};
+    const linfusion_block_norm_grads_t no_grads = {};
+    if (v == nullptr) v = &none;
+    if (grads == nullptr) grads = &no_grads;
+    const bool branch = rows_given(a), pre = desc->pre != LINFUSION_NORM_NONE;
+    if (!vectors_ok(*desc, *v, branch) || (branch && !rows_ok(a))) return LINFUSION_ERR_INVALID_ARG;
+    if (pre && (!rows_ok(y) || !rows_ok(dn))) return LINFUSION_ERR_INVALID_ARG;
+    if (!pre && (rows_given(dn) || !rows_ok(dy))) return LINFUSION_ERR_INVALID_ARG;
+    if (rows_given(dy) && !rows_ok(dy)) return LINFUSION_ERR_INVALID_ARG;
+    if (!out_ok(*desc, dx) || rows_given(da) != branch || (branch && !out_ok(*desc, da))) return LINFUSION_ERR_INVALID_ARG;
+    const linfusion_rows_t* y_read = pre ? y : nullptr;
+    if (!apart(*desc, dx, y_read, false) || !apart(*desc, dx, a, false) || !apart(*desc, dx, dy, true) ||
+        !apart(*desc, dx, dn, false) || !apart(*desc, dx, *v))
+        return LINFUSION_ERR_INVALID_ARG;
+    if (branch && (!apart(*desc, da, y_read, false) || !apart(*desc, da, a, true) || !apart(*desc, da, dy, false) ||
+                   !apart(*desc, da, dn, false) || !apart(*desc, da, dx, false) || !apart(*desc, da, *v)))
+        return LINFUSION_ERR_INVALID_ARG;
+    // a gradient of a vector that is not there
+    if ((grads->gate != nullptr && v->gate.p == nullptr) || (grads->scale != nullptr && v->scale.p == nullptr) ||
+        (grads->shift != nullptr && v->shift.p == nullptr) || (grads->pre_weight != nullptr && v->pre_weight == nullptr) ||
+        (grads->pre_bias != nullptr && v->pre_bias == nullptr) || (grads->post_weight != nullptr && v->post_weight == nullptr) ||
+        (grads->post_bias != nullptr && v->post_bias == nullptr))
+        return LINFUSION_ERR_INVALID_ARG;
+    for (const float* g : {grads->gate, grads->scale, grads->shift, grads->pre_weight, grads->pre_bias, grads->post_weight,
+                           grads->post_bias})
+        if (g != nullptr && !is_aligned(g, 4)) return LINFUSION_ERR_INVALID_ARG;
+    int want = 0;
+    if (grads->shift || grads->scale || grads->pre_bias) want |= 1;  // a bias' share of the scale's gradient needs sum dn
+    if (grads->scale || grads->pre_weight) want |= 2;
+    if (grads->gate || grads->post_weight) want |= 4;
+    if (grads->post_bias || (grads->gate && v->post_bias)) want |= 8;
+
+    const Here at = here();
+    if (at.st != LINFUSION_OK) return at.st;
+    int rows = 1;
+    const NormPlan plan = backward_plan(*desc, at.sms, &rows);
+    if (want != 0) {
+        if (workspace == nullptr || !is_aligned(workspace, 256)) return LINFUSION_ERR_INVALID_ARG;
+        if (workspace_bytes < align_up_256(static_cast<size_t>(4) * plan.groups * desc->C * sizeof(float))) return LINFUSION_ERR_ALLOC;
+    }
+    NormParams p = {};
+    fill(&p, *desc, *v, plan, branch);
+    p.x = to_rows(y);
+    p.a = to_rows(a);
+    p.dy = to_rows(dy);
+    p.dn = to_rows(dn);
+    p.dx = to_rows(dx);
+    p.da = to_rows(da);
+    p.partials = static_cast<float*>(workspace);
+    p.want = want;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    cudaError_t e = launch_norm_kind<true>(*desc, p, plan, branch, rows, s);
+    if (e != cudaSuccess || want == 0) return end(e);
+
+    NormGradParams g = {};
+    g.partials = p.partials;
+    g.B = desc->B;
+    g.C = desc->C;
+    g.chunks = plan.chunks;
+    g.groups = plan.groups;
+    g.want = want;
+    g.gate = p.gate;
+    g.scale = p.scale;
+    g.pre_w = p.pre_w;
+    g.pre_b = p.pre_b;
+    g.post_w = p.post_w;
+    g.post_b = p.post_b;
+    g.gate_per_batch = v->gate.batch != 0;
+    g.scale_per_batch = v->scale.batch != 0;
+    g.shift_per_batch = v->shift.batch != 0;
+    g.d_gate = grads->gate;
+    g.d_scale = grads->scale;
+    g.d_shift = grads->shift;
+    g.d_pre_w = grads->pre_weight;
+    g.d_pre_b = grads->pre_bias;
+    g.d_post_w = grads->post_weight;
+    g.d_post_b = grads->post_bias;
+    const dim3 grid((desc->C + 31) / 32), block(32 * kNormGradSlices);
+    e = (desc->flags & LINFUSION_DTYPE_FP16) != 0u
+            ? launch_pdl(block_norm_grads_kernel<make_kind(kPhiIdentity, kDtypeFp16)>, grid, block, 0, s, g)
+            : launch_pdl(block_norm_grads_kernel<make_kind(kPhiIdentity, kDtypeBf16)>, grid, block, 0, s, g);
+    return end(e);
+}
+
+}  // extern "C"

@@ -1,0 +1,298 @@
+"""The attention's backward pass against its 64-bit formulas: every pair of widths, both layouts, types, phi, with and
+without the normalizer, ragged lengths, a saved and a recomputed state, the halves of token-sharded use, and a block's
+operators one after the other, forward and back."""
+import math
+
+import pytest
+import torch
+
+from paper_2409_02097_b200 import attn, block, sharding
+
+import _block_ref as ref
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "fp16": torch.float16}
+EPS = 1e-6
+
+# Before its rounding an element of a gradient is off by what the operands' tails leave (2^-16 of the terms' sizes) and by
+# fp32 sums over tokens: in chunks and tiles, off by about sqrt(terms) 2^-24 of their sizes, far below.  2^-13 leaves room
+# for the products' own truncated fp32 accumulation.
+SLACK = 2.0 ** -13
+
+
+def _rms_limit(dtype):
+    """A value rounded to nearest is off by an error that is uniform in half a step: half / sqrt 3 of it in the mean square at
+    most (where mantissas are near one); and 2^-14 for everything before the rounding."""
+    return ref.HALF_STEP[DT[dtype]] / math.sqrt(3) + 2.0 ** -14
+
+
+def _inputs(B, H, N, dk, dv, dtype, seed=21, mean=0.0, grad_scale=None, kind=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    r = lambda w: torch.randn((B, H, N, w), generator=g, device="cuda")  # noqa: E731
+    q, k, v, dy = r(dk), r(dk), r(dv) + mean, r(dv) * (grad_scale or (64.0 if dtype == "fp16" else 1.0))
+    if kind == 1:
+        q, k = q.abs(), k.abs()
+    return [t.to(DT[dtype]) for t in (q, k, v, dy)]
+
+
+def _check(got, tensors, dtype, what, eps=EPS, kind=0, normalize=True, slack=SLACK, rms=True):
+    want, sizes = ref.attention_backward(*tensors, eps, kind, normalize)
+    for name, x, w, size in zip(("dq", "dk", "dv"), got, want, sizes):
+        ref.assert_rounded(x, w, slack * size, f"{what} {name}")
+        if rms and dtype == "bf16" or rms and w.abs().mean() > 1e-3:  # (fp16 gradients near the subnormal numbers round more coarsely)
+            rel = ((x.double() - w).norm() / w.norm()).item()
+            assert rel <= _rms_limit(dtype), f"{what} {name}: {rel:.3e}"
+
+
+def _major(t, layout):
+    return t if layout == "head_major" else t.transpose(1, 2).contiguous()
+
+
+PAIRS = [(32, 32), (40, 40), (64, 64), (80, 80), (128, 128), (160, 160), (128, 64), (80, 40), (32, 64)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("layout", ["head_major", "token_major"])
+@pytest.mark.parametrize("dk,dv", PAIRS)
+def test_every_pair_of_widths(dk, dv, layout, dtype):
+    for (B, H, N) in ((2, 3, 77), (1, 2, 1030)):
+        tensors = _inputs(B, H, N, dk, dv, dtype)
+        op = attn.LinFusionAttention(B, H, N, dv, eps=EPS, variant="split", layout=layout, dtype=dtype, d_qk=dk if dk != dv else 0)
+        got = op.backward(*[_major(t, layout) for t in tensors])
+        torch.cuda.synchronize()
+        _check([_major(g, layout) for g in got], tensors, dtype, f"{B}x{H}x{N} {dk}x{dv} {layout} {dtype}")
+        op.close()
+
+
+@pytest.mark.parametrize("N", [2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 257, 4097])
+@pytest.mark.parametrize("d", [40, 64, 160])
+def test_ragged_lengths(d, N):
+    tensors = _inputs(2, 2, N, d, d, "bf16", seed=N)
+    op = attn.LinFusionAttention(2, 2, N, d, eps=EPS)
+    _check(op.backward(*tensors), tensors, "bf16", f"N={N} d={d}", rms=N > 8)
+    op.close()
+
+
+@pytest.mark.parametrize("d", [40, 64, 160])
+def test_one_token(d):
+    # Y is V times den / (den + eps): dQ and dK are differences of equal terms, zero up to fp32 rounding of the terms
+    for dtype in ("bf16", "fp16"):
+        tensors = _inputs(3, 2, 1, d, d, dtype)
+        op = attn.LinFusionAttention(3, 2, 1, d, eps=EPS, dtype=dtype)
+        _check(op.backward(*tensors), tensors, dtype, f"one token {d}", rms=False)
+        op.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("kind,normalize,eps", [(1, True, 1e-6), (1, True, 0.5), (0, True, 0.0), (0, True, 10.0), (0, False, 1e-6), (1, False, 1e-6)])
+def test_phi_eps_and_normalizer(kind, normalize, eps, dtype):
+    B, H, N, d = 1, 3, 333, 64
+    scale = 1.0 if dtype == "bf16" or normalize else 2.0 ** -4
+    tensors = _inputs(B, H, N, d, d, dtype, kind=kind, grad_scale=scale)
+    op = attn.LinFusionAttention(B, H, N, d, phi=kind, eps=eps, normalize=normalize, dtype=dtype)
+    _check(op.backward(*tensors), tensors, dtype, f"phi {kind} eps {eps} normalize {normalize}", eps=eps, kind=kind, normalize=normalize)
+    op.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("d", [64, 80])
+def test_values_with_a_mean_and_features_of_unequal_size(d, dtype):
+    B, H, N = 2, 2, 3000
+    q, k, v, dy = _inputs(B, H, N, d, d, dtype, mean=3.0)
+    k[..., 0] -= 6.0      # z of very different sizes
+    k[..., 1] += 5.0
+    q[..., 2] -= 8.0
+    tensors = [q, k, v, dy]
+    op = attn.LinFusionAttention(B, H, N, d, eps=EPS, dtype=dtype)
+    _check(op.backward(*tensors), tensors, dtype, "mean", rms=False)
+    op.close()
+
+
+def test_tiny_and_large_gradients_bf16():
+    for scale in (2.0 ** -60, 2.0 ** 60):
+        tensors = _inputs(1, 2, 300, 64, 64, "bf16", grad_scale=scale)
+        op = attn.LinFusionAttention(1, 2, 300, 64, eps=EPS)
+        _check(op.backward(*tensors), tensors, "bf16", f"scale {scale}")
+        op.close()
+
+
+@pytest.mark.parametrize("variant,shape", [("split", (2, 4, 500, 64)), ("stream", (1, 4, 5000, 64)), ("fused", (2, 8, 1024, 80)),
+                                           ("cluster", (2, 8, 150, 160)), ("fused", (2, 20, 576, 64)), ("auto", (2, 8, 4096, 40))])
+def test_state_saved_by_the_forward_pass(variant, shape):
+    B, H, N, d = shape
+    tensors = _inputs(B, H, N, d, d, "bf16")
+    op = attn.LinFusionAttention(B, H, N, d, eps=EPS, variant=variant)
+    op.forward(*tensors[:3])
+    state = op.save_state()
+    S, z = op.read_state()
+    assert torch.equal(state.cpu()[:, :d * d].reshape(B, H, d, d), torch.from_numpy(S))
+    assert torch.equal(state.cpu()[:, d * d:].reshape(B, H, d), torch.from_numpy(z))
+    want, sizes = ref.attention_backward(*tensors, EPS)
+    for name, x, w in zip(("dq", "dk", "dv"), op.backward(*tensors, state=state), want):
+        # the forward's state carries phi(K) rounded to 16 bits: half a step on every term of S and z, and for phi itself as much again
+        rel = ((x.double() - w).norm() / w.norm()).item()
+        assert rel <= 4 * 2.0 ** -8 / math.sqrt(3), f"{variant} {name}: {rel:.3e}"
+    # a state of its own, exact to fp32: as good as recomputed, whichever call makes it
+    again = op.backward_state(*tensors[1:3])
+    _check(op.backward(*tensors, state=again), tensors, "bf16", "state of its own")
+    assert all(torch.equal(a, b) for a, b in zip(op.backward(*tensors), op.backward(*tensors, state=again)))
+    op.close()
+
+
+def test_token_shards_give_the_whole():
+    B, H, N, d = 1, 4, 1500, 64
+    tensors = _inputs(B, H, N, d, d, "bf16")
+    cuts = [sharding.token_shard(N, r, 3) for r in range(3)]
+    ops = [attn.LinFusionAttention(B, H, e - b, d, eps=EPS, variant="split") for b, e in cuts]
+    parts = [[t[:, :, b:e].contiguous() for t in tensors] for b, e in cuts]
+    state = sum(op.backward_state(p[1], p[2]) for op, p in zip(ops, parts))
+    firsts = [op.backward_q(p[0], p[3], state) for op, p in zip(ops, parts)]
+    grad = sum(g for _, g in firsts)
+    seconds = [op.backward_kv(p[1], p[2], grad) for op, p in zip(ops, parts)]
+    got = [torch.cat(ts, dim=2) for ts in ([f[0] for f in firsts], [s[0] for s in seconds], [s[1] for s in seconds])]
+    _check(got, tensors, "bf16", "shards")
+    for op in ops:
+        op.close()
+
+
+def test_outputs_stay_inside_their_buffers_and_inputs_are_kept():
+    for (B, H, N, d, layout) in ((1, 3, 77, 40, "head_major"), (2, 2, 129, 64, "token_major"), (1, 1, 33, 160, "head_major")):
+        tensors = [_major(t, layout) for t in _inputs(B, H, N, d, d, "bf16")]
+        kept = [t.clone() for t in tensors]
+        op = attn.LinFusionAttention(B, H, N, d, eps=EPS, variant="split", layout=layout)
+        n = tensors[0].numel()
+        bands = [torch.full((n + 1024,), 5.0, device="cuda", dtype=torch.bfloat16) for _ in range(3)]
+        ws = torch.full((op.backward_workspace_bytes() + 4096,), 77, device="cuda", dtype=torch.uint8)
+        outs = [b[512:512 + n].view(tensors[0].shape) for b in bands]
+        off = (-ws.data_ptr()) % 256 + 256
+        op.backward(*tensors, dq=outs[0], dk=outs[1], dv=outs[2], workspace=ws[off:off + op.backward_workspace_bytes()])
+        torch.cuda.synchronize()
+        for b in bands:
+            assert (b[:512] == 5).all() and (b[512 + n:] == 5).all()
+        assert (ws[:off] == 77).all() and (ws[off + op.backward_workspace_bytes():] == 77).all()
+        assert all(torch.equal(a, b) for a, b in zip(tensors, kept))
+        # without a word in a workspace read before it is written: the same bits from another filling
+        again = op.backward(*tensors)
+        assert all(torch.equal(a, b) for a, b in zip(outs, again))
+        op.close()
+
+
+def test_refusals_of_tensors():
+    op = attn.LinFusionAttention(1, 2, 64, 64)
+    q, k, v, dy = _inputs(1, 2, 64, 64, 64, "bf16")
+    for bad in (q.half(), q[:, :1], q.cpu(), q.transpose(1, 2)):
+        with pytest.raises(ValueError):
+            op.backward(bad, k, v, dy)
+    with pytest.raises(ValueError):
+        op.backward(q, k, v, dy, state=torch.zeros(2, 64 * 64, device="cuda"))
+    for kw in (dict(dq=q), dict(dk=v), dict(dv=dy), dict(workspace=torch.empty(1024, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises(attn.LinFusionError):
+            op.backward(q, k, v, dy, **kw)
+    out = torch.empty_like(q)
+    with pytest.raises(attn.LinFusionError):
+        op.backward(q, k, v, dy, dq=out, dk=out)
+    op.close()
+
+
+def test_streams_graphs_and_same_bits():
+    shapes = [(2, 8, 64, 160), (2, 10, 900, 64), (1, 8, 2000, 40)]
+    cases = []
+    for B, H, N, d in shapes:
+        op = attn.LinFusionAttention(B, H, N, d, eps=EPS)
+        tensors = _inputs(B, H, N, d, d, "bf16")
+        cases.append((op, tensors, op.backward(*tensors)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    outs = []
+    for _ in range(20):  # the same objects on three streams at once, forwards among them
+        for s in streams:
+            with torch.cuda.stream(s):
+                for op, tensors, first in cases:
+                    outs.append((op.backward(*tensors), first))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for got, first in outs for a, b in zip(got, first))
+    graphs = []
+    for s in streams[:2]:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            held = [op.backward(*tensors) for op, tensors, _ in cases]
+        graphs.append((g, held, s))
+    for _, held, _ in graphs:
+        for h in held:
+            for x in h:
+                x.zero_()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for g, _, s in graphs:
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    for _, held, _ in graphs:
+        for h, (_, _, first) in zip(held, cases):
+            assert all(torch.equal(a, b) for a, b in zip(h, first))
+    for op, _, _ in cases:
+        op.close()
+
+
+def test_a_block_forward_and_back():
+    """Norm before, projections, rotary positions, attention, gated residual and the next norm; then the gradients of the
+    input and of every vector, against differentiation in 64 bits of the same chain."""
+    B, N, H, d = 2, 300, 5, 64
+    C = H * d
+    g = torch.Generator(device="cuda").manual_seed(31)
+    r = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    x, w = r(B, N, C).bfloat16(), [(r(C, C) / math.sqrt(C)).bfloat16() for _ in range(3)]
+    mod = (0.3 * r(B, 3 * C)).bfloat16()
+    scale, shift, gate = mod[:, :C], mod[:, C:2 * C], mod[:, 2 * C:]
+    weight = (1 + 0.1 * r(C)).bfloat16()
+    pos = torch.stack([torch.arange(N, device="cuda") // 20, torch.arange(N, device="cuda") % 20], -1).float()
+    up_y, up_n = r(B, N, C).bfloat16(), r(B, N, C).bfloat16()
+
+    before = block.BlockNorm(C, pre="layer")
+    after = block.BlockNorm(C, pre="layer", post="rms")
+    rope = block.AxialRope(d, (16, 16), layout="token_major")
+    op = attn.LinFusionAttention(B, H, N, d, eps=EPS, variant="split", layout="token_major")
+    heads = lambda t: t.view(B, N, H, d)  # noqa: E731
+    _, n = before.forward(x, scale=scale, shift=shift)
+    q0, k0, v = (heads(n @ m) for m in w)
+    q, k = rope.forward(q0, k0, pos)
+    a = op.forward(q, k, v)
+    state = op.save_state()
+    y, n2 = after.forward(x, a.view(B, N, C), gate=gate, post_weight=weight)
+    back = after.backward(y, a.view(B, N, C), gate=gate, post_weight=weight, dy=up_y, dn=up_n)
+    dq, dk, dv = op.backward(q, k, v, heads(back["a"]), state=state)
+    dq, dk = rope.backward(dq, dk, pos)
+    dn = sum(t.view(B, N, C) @ m.t() for t, m in zip((dq, dk, dv), w))
+    first = before.backward(x, scale=scale, shift=shift, dy=back["x"], dn=dn)
+    torch.cuda.synchronize()
+    assert op.status() == attn.OK
+
+    leaf = {n_: t.double().requires_grad_(True) for n_, t in dict(x=x, scale=scale, shift=shift, gate=gate, weight=weight).items()}
+    lw = [m.double() for m in w]
+    vec = dict(scale=leaf["scale"], shift=leaf["shift"])
+    nn = ref.norm_before(leaf["x"], vec, "layer", 1e-6)
+    qq, kk, vv = ((nn @ m).view(B, N, H, d) for m in lw)
+    turn = lambda t: _rope_differentiable(t, pos)  # noqa: E731
+    yy = ref.attention(turn(qq).transpose(1, 2), turn(kk).transpose(1, 2), vv.transpose(1, 2), EPS).transpose(1, 2).reshape(B, N, C)
+    stream = ref.norm_after(leaf["x"], yy, dict(gate=leaf["gate"], post_weight=leaf["weight"]), "rms", 1e-6, 1.0)
+    out = ref.norm_before(stream, {}, "layer", 1e-6)
+    loss = (stream * up_y.double()).sum() + (out * up_n.double()).sum()
+    want = torch.autograd.grad(loss, list(leaf.values()))
+    got = (first["x"], first["scale"], first["shift"], back["gate"], back["post_weight"])
+    for name, a_, b_ in zip(leaf, got, want):
+        # about a dozen 16-bit roundings in a row, the phi(K) and S of the forward among them; the RMS norm divides by the small
+        # size of the attention's output, whose own relative error it passes on
+        rel = ((a_.double() - b_).norm() / b_.norm()).item()
+        assert rel <= 12 * 2.0 ** -8, f"{name}: {rel:.3e}"
+    ref_y = ((y.double() - stream).norm() / stream.norm()).item()
+    assert ref_y <= 12 * 2.0 ** -8 and ((n2.double() - out).norm() / out.norm()).item() <= 12 * 2.0 ** -8
+    op.close()
+
+
+def _rope_differentiable(x, pos):
+    freq = torch.tensor([10000.0 ** (-i / 16) for i in range(16)], dtype=torch.float64, device=x.device)
+    angle = torch.cat([pos[:, :1].double() * freq, pos[:, 1:].double() * freq], -1)[None, :, None]
+    u, w = x[..., 0::2], x[..., 1::2]
+    return torch.stack([u * angle.cos() - w * angle.sin(), u * angle.sin() + w * angle.cos()], -1).flatten(-2)
