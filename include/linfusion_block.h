@@ -94,7 +94,7 @@ linfusion_status_t linfusion_rope(const linfusion_rope_desc_t* desc, const linfu
 typedef enum { LINFUSION_NORM_NONE = 0, LINFUSION_NORM_LAYER = 1, LINFUSION_NORM_RMS = 2 } linfusion_norm_t;
 #define LINFUSION_BLOCK_NORM_MAX_C 8192
 typedef struct {
-    int32_t B;             /* 1 .. 65535                                   */
+    int32_t B;             /* 1 .. 65534                                   */
     int32_t N;             /* rows of a batch entry, >= 1                  */
     int32_t C;             /* channels, a multiple of 8, <= 8192           */
     int32_t pre, post;     /* linfusion_norm_t                             */

@@ -224,15 +224,23 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
 }
 
 // ---------------------------------------------------------------------------------------------
-// The norms around a block.  A group of W = ceil(C / 256) warps works on whole rows, each thread on the same
-// eight channels of every row (its gate, scale, shift, weights and column sums stay in registers), kRows rows
-// at a time so that their loads are in flight together and one barrier serves them all.  A row's mean and
-// variance: each warp takes its sum by shuffles, then the sum of squares about its own mean, and the warps'
-// (sum, squares) pairs are joined exactly:  M2 = sum_w [M2_w + n_w (mean_w - mean)^2].  Nothing cancels, whatever
-// the row's mean.
+// The norms around a block.  A group of W = ceil(C / (256 V)) warps works on whole rows, one at a time; each thread keeps
+// to the same 8 V channels of every row, so its gate, scale, shift, weights and column sums stay in registers (V = 1
+// up to C = 4096).  Rows are fetched three (two) ahead into the thread's own slots of shared memory (16-byte
+// asynchronous copies that only the thread itself waits for), so DRAM latency is hidden without registers.
+//
+// A row's mean and variance: each warp takes its sum by shuffles, then the sum of squares about its own mean, and the
+// warps' (sum, squares) pairs are joined exactly:  M2 = sum_w [M2_w + n_w (mean_w - mean)^2].  Nothing cancels,
+// whatever the row's mean.  Two quantities (the two norms of a row, or two sums) travel together, one in each half of the
+// warp: halving the values while the lanes are halved costs five shuffles instead of ten.
+//
+// What bounds them: DRAM at large C x rows; behind it the issue slots (about 300 instructions per 8 channels of a
+// warp in the backward pass before packed fp32x2 arithmetic, which halves the multiply-adds).
 // ---------------------------------------------------------------------------------------------
 constexpr int kNormNone = 0, kNormLayer = 1, kNormRms = 2;
-constexpr int kNormMaxWarps = 32;
+constexpr int kNormMaxWarps = 16;  // of a group: a half warp holds one value of each
+constexpr int kNormMaxThreads = 32 * kNormMaxWarps;  // which leaves a thread 128 registers: three blocks of five warps on an SM
+__host__ __device__ constexpr int norm_stages(int V) { return V == 1 ? 4 : 3; }
 
 struct Rows {
     char* p;
@@ -252,135 +260,186 @@ struct NormParams {
     int chunks;              // groups of a batch entry
     int groups;              // all
     float eps, rs, inv_c;
+    float inv_last, last;    // channels of a group's last warp, and 1 / them
     float* partials;         // backward: [sums][group][C]
     int want;                // backward: bit k set where column sum k is wanted
 };
 
-__device__ __forceinline__ float warp_sum(float v)
+// Two fp32 values handled by one instruction (sm_100's packed fp32 arithmetic; each half is rounded as the scalar is).
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float a, float b)
 {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
+    f32x2 d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
+    return d;
 }
+__device__ __forceinline__ f32x2 both(float a) { return pack2(a, a); }
+__device__ __forceinline__ float2 unpack2(f32x2 v)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
+{
+    f32x2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
+{
+    f32x2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b)
+{
+    f32x2 d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float sum2(f32x2 v)
+{
+    const float2 r = unpack2(v);
+    return r.x + r.y;
+}
+
+// Eight channels as four pairs.
+struct P8 {
+    f32x2 v[4];
+};
+template <int KIND>
+__device__ __forceinline__ P8 unpack_pairs(const uint4& p)
+{
+    P8 f;
+    f.v[0] = pack2(pair_lo<KIND>(p.x), pair_hi<KIND>(p.x));
+    f.v[1] = pack2(pair_lo<KIND>(p.y), pair_hi<KIND>(p.y));
+    f.v[2] = pack2(pair_lo<KIND>(p.z), pair_hi<KIND>(p.z));
+    f.v[3] = pack2(pair_lo<KIND>(p.w), pair_hi<KIND>(p.w));
+    return f;
+}
+template <int KIND>
+__device__ __forceinline__ uint4 pack_pairs(const P8& f)
+{
+    const float2 a = unpack2(f.v[0]), b = unpack2(f.v[1]), c = unpack2(f.v[2]), d = unpack2(f.v[3]);
+    return make_uint4(pack_pair<KIND>(a.x, a.y), pack_pair<KIND>(b.x, b.y), pack_pair<KIND>(c.x, c.y), pack_pair<KIND>(d.x, d.y));
+}
+template <int KIND>
+__device__ __forceinline__ P8 load_vector(const char* p, int c, bool active, float absent)
+{
+    P8 f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f.v[i] = both(active ? absent : 0.0f);
+    if (p != nullptr && active) f = unpack_pairs<KIND>(load16(p + 2 * c));
+    return f;
+}
+
 __device__ __forceinline__ void group_sync(int group_in_cta, int warps)
 {
     if (warps > 1) asm volatile("bar.sync %0, %1;" ::"r"(group_in_cta + 1), "r"(warps * 32) : "memory");
 }
-template <int KIND>
-__device__ __forceinline__ F8 load_vector(const char* p, int c, bool active, float absent)
+// Sums over the warp of two values: lanes 0 - 15 end with the first's, 16 - 31 with the second's.
+__device__ __forceinline__ float fold(float a, float b, int lane)
 {
-    F8 f;
+    const bool second = lane >= 16;
+    float k = second ? b : a;
+    k += __shfl_xor_sync(0xffffffffu, second ? a : b, 16);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f.v[i] = absent;
-    if (p != nullptr && active) f = unpack8<KIND>(load16(p + 2 * c));
-    return f;
+    for (int o = 8; o > 0; o >>= 1) k += __shfl_xor_sync(0xffffffffu, k, o);
+    return k;
 }
+__device__ __forceinline__ float from_first(float v) { return __shfl_sync(0xffffffffu, v, 0); }
+__device__ __forceinline__ float from_second(float v) { return __shfl_sync(0xffffffffu, v, 16); }
 
-// Exchange of one pair of sums per row between the warps of a group.  The two buffers take turns: a buffer is
-// written again only behind the barrier of the exchange in between, which every warp reaches after it has read.
-template <int R>
-struct GroupExchange {
-    float2* buf;  // [2][R][kNormMaxWarps] of this group
-    int turn;
-    __device__ __forceinline__ float2* next()
+// What a thread is in its group, and the group's exchange of one pair of numbers per warp and half.  The two buffers
+// take turns: a buffer is written again only behind the barrier of the exchange in between, which every warp
+// reaches after it has read.  J: steps that join the warps' values, 2^J >= W (0: the group is one warp).
+template <int J>
+struct Group {
+    float2* buf;  // [2][32]
+    int turn, warp, lane, g;
+    __device__ __forceinline__ float2 swap(float2 mine, const NormParams& p)
     {
-        float2* b = buf + turn * R * kNormMaxWarps;
-        turn ^= 1;
-        return b;
+        float2* b = buf + turn;
+        turn ^= 32;
+        if ((lane & 15) == 0) b[lane + warp] = mine;
+        group_sync(g, p.warps);
+        return (lane & 15) < p.warps ? b[lane] : make_float2(0.0f, 0.0f);
+    }
+    __device__ __forceinline__ float join(float v) const
+    {
+#pragma unroll
+        for (int o = 1 << J >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        return v;
     }
 };
+struct Stats {
+    float mean, rstd;
+};
 
-// mean (0 for RMS) and 1 / sqrt(var + eps) of R rows at once; NORM: kNormLayer or kNormRms.
-template <int NORM, int R>
-__device__ __forceinline__ void row_stats(const F8 (&v)[R], bool active, const NormParams& p, int warp, int lane, int g,
-                                          GroupExchange<R>& ex, float (&mean)[R], float (&rstd)[R])
+// Mean (0 for RMS) and 1 / sqrt(var + eps) of one row of `a` and one of `b`, each of its norm (kNormNone: not wanted).
+// Lanes without channels hold zeros, and take a mean of zero when deviations are formed.
+template <int NA, int NB, int V, int J>
+__device__ __forceinline__ void two_stats(const P8 (&a)[V], const P8 (&b)[V], const bool (&active)[V], const NormParams& p,
+                                          Group<J>& g, Stats* sa, Stats* sb)
 {
-    // channels of this warp: 256, fewer in the last one
-    const float cnt = static_cast<float>(min(256, p.C - warp * 256));
-    float sum[R], sq[R];
+    float m = 0.0f, sum = 0.0f;
+    if (NA == kNormLayer || NB == kNormLayer) {
+        f32x2 ta = both(0.0f), tb = both(0.0f);
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        float s = 0.0f;
-        if (NORM == kNormLayer) {
-            if (active) {
+        for (int v = 0; v < V; ++v)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s += v[r].v[i];
+            for (int i = 0; i < 4; ++i) {
+                if (NA == kNormLayer) ta = i + v == 0 ? a[v].v[i] : add2(ta, a[v].v[i]);
+                if (NB == kNormLayer) tb = i + v == 0 ? b[v].v[i] : add2(tb, b[v].v[i]);
             }
-            s = warp_sum(s);
-        }
-        sum[r] = s;
-        const float m = NORM == kNormLayer ? s / cnt : 0.0f;
-        float q = 0.0f;
-        if (active) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float d = v[r].v[i] - m;
-                q = fmaf(d, d, q);
-            }
-        }
-        sq[r] = warp_sum(q);
+        sum = fold(NA == kNormLayer ? sum2(ta) : 0.0f, NB == kNormLayer ? sum2(tb) : 0.0f, g.lane);
+        m = sum * (J == 0 ? p.inv_c : g.warp == p.warps - 1 ? p.inv_last : 1.0f / (256 * V));
     }
-    if (p.warps > 1) {
-        float2* b = ex.next();
-        if (lane == 0) {
+    const float ma = NA == kNormLayer ? -from_first(m) : 0.0f, mb = NB == kNormLayer ? -from_second(m) : 0.0f;
+    f32x2 qa = both(0.0f), qb = both(0.0f);
 #pragma unroll
-            for (int r = 0; r < R; ++r) b[r * kNormMaxWarps + warp] = make_float2(sum[r], sq[r]);
-        }
-        group_sync(g, p.warps);
+    for (int v = 0; v < V; ++v) {
+        const f32x2 va = both(active[v] ? ma : 0.0f), vb = both(active[v] ? mb : 0.0f);
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            float s = 0.0f, q = 0.0f;
-            if (NORM == kNormLayer) {
-                for (int w = 0; w < p.warps; ++w) s += b[r * kNormMaxWarps + w].x;
+        for (int i = 0; i < 4; ++i) {
+            if (NA != kNormNone) {
+                const f32x2 d = NA == kNormLayer ? add2(a[v].v[i], va) : a[v].v[i];
+                qa = i + v == 0 ? mul2(d, d) : fma2(d, d, qa);
             }
-            const float m = s * p.inv_c;
-            for (int w = 0; w < p.warps; ++w) {
-                const float2 o = b[r * kNormMaxWarps + w];
-                q += o.y;
-                if (NORM == kNormLayer) {
-                    const float n = static_cast<float>(min(256, p.C - w * 256));
-                    const float d = o.x / n - m;
-                    q = fmaf(n * d, d, q);
-                }
+            if (NB != kNormNone) {
+                const f32x2 d = NB == kNormLayer ? add2(b[v].v[i], vb) : b[v].v[i];
+                qb = i + v == 0 ? mul2(d, d) : fma2(d, d, qb);
             }
-            mean[r] = m;
-            rstd[r] = rsqrtf(q * p.inv_c + p.eps);
-        }
-    } else {
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            mean[r] = sum[r] * p.inv_c;
-            rstd[r] = rsqrtf(sq[r] * p.inv_c + p.eps);
         }
     }
+    float sq = fold(NA != kNormNone ? sum2(qa) : 0.0f, NB != kNormNone ? sum2(qb) : 0.0f, g.lane);
+    if (J > 0) {
+        const float2 o = g.swap(make_float2(sum, sq), p);
+        sq = o.y;
+        if (NA == kNormLayer || NB == kNormLayer) {
+            // a half whose norm is RMS has sums of zero: its mean stays zero and nothing is added
+            m = g.join(o.x) * p.inv_c;
+            const int w = g.lane & 15;
+            const bool full = w < p.warps - 1;
+            const float d = o.x * (full ? 1.0f / (256 * V) : p.inv_last) - m;
+            if (w < p.warps) sq = fmaf((full ? 256.0f * V : p.last) * d, d, sq);
+        }
+        sq = g.join(sq);
+    }
+    const float rs = rsqrtf(fmaf(sq, p.inv_c, p.eps));
+    if (NA != kNormNone) sa->mean = NA == kNormLayer ? from_first(m) : 0.0f, sa->rstd = from_first(rs);
+    if (NB != kNormNone) sb->mean = NB == kNormLayer ? from_second(m) : 0.0f, sb->rstd = from_second(rs);
 }
 
-// Sums over the row of two values per row.
-template <int R>
-__device__ __forceinline__ void row_sums(float (&u)[R], float (&w)[R], const NormParams& p, int warp, int lane, int g,
-                                         GroupExchange<R>& ex)
+// Means over the row of two values.
+template <int J>
+__device__ __forceinline__ float2 two_means(f32x2 u, f32x2 w, const NormParams& p, Group<J>& g)
 {
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        u[r] = warp_sum(u[r]);
-        w[r] = warp_sum(w[r]);
-    }
-    if (p.warps <= 1) return;
-    float2* b = ex.next();
-    if (lane == 0) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) b[r * kNormMaxWarps + warp] = make_float2(u[r], w[r]);
-    }
-    group_sync(g, p.warps);
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        u[r] = w[r] = 0.0f;
-        for (int i = 0; i < p.warps; ++i) {
-            const float2 o = b[r * kNormMaxWarps + i];
-            u[r] += o.x;
-            w[r] += o.y;
-        }
-    }
+    float v = fold(sum2(u), sum2(w), g.lane);
+    if (J > 0) v = g.join(g.swap(make_float2(v, 0.0f), p).x);
+    v *= p.inv_c;
+    return make_float2(from_first(v), from_second(v));
 }
 
 // Which rows of which batch entry a group works on: contiguous runs of near-equal length.
@@ -397,85 +456,157 @@ __device__ __forceinline__ GroupRows group_rows(const NormParams& p, int group)
     return r;
 }
 
-template <int KIND, int POST, int PRE, bool A, int R, int T>
-__global__ void __launch_bounds__(T) block_norm_kernel(const __grid_constant__ NormParams p)
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+// The thread's slots of S streams x V vectors x STAGES rows: [stage][warp][stream][vector][lane], so that a slot is the
+// stage's address plus a constant.  Slots of lanes without channels, and of streams that are absent, hold zeros.
+template <int S, int V>
+struct RowRing {
+    static constexpr int STAGES = norm_stages(V), SLOT = 512;
+    uint32_t first, pitch, read_at, fill_at;
+    __device__ __forceinline__ void begin(uint32_t base)
+    {
+        pitch = blockDim.x * (16 * S * V);
+        first = base + (threadIdx.x / 32) * (S * V * SLOT) + (threadIdx.x & 31) * 16;
+        read_at = fill_at = first;
+        for (int i = 0; i < STAGES; ++i)
+#pragma unroll
+            for (int s = 0; s < S * V; ++s)
+                asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(first + i * pitch + s * SLOT), "r"(0u) : "memory");
+    }
+    __device__ __forceinline__ uint32_t next(uint32_t at) const
+    {
+        const uint32_t n = at + pitch;
+        return n == first + STAGES * pitch ? first : n;
+    }
+    __device__ __forceinline__ void fill(int s, int v, const char* src) const
+    {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(fill_at + (s * V + v) * SLOT), "l"(src) : "memory");
+    }
+    __device__ __forceinline__ uint4 read(int s, int v) const
+    {
+        uint4 r;
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(read_at + (s * V + v) * SLOT) : "memory");
+        return r;
+    }
+};
+__host__ __device__ constexpr int norm_smem_bytes(int streams, int V, int threads, int groups) { return groups * 64 * 8 + norm_stages(V) * streams * V * threads * 16; }
+
+// Rows handed from one to the next by their stride.
+struct Walk {
+    char* p;
+    long long r;
+    __device__ __forceinline__ Walk(const Rows& t, const GroupRows& rows, int c)
+        : p(t.p == nullptr ? nullptr : t.p + rows.b * t.b + rows.begin * t.r + 2 * c), r(t.r) {}
+    __device__ __forceinline__ void step() { p += r; }
+};
+
+template <int KIND, int POST, int PRE, bool A, int V, int J>
+__global__ void __launch_bounds__(kNormMaxThreads) block_norm_kernel(const __grid_constant__ NormParams p)
 {
-    extern __shared__ float2 norm_smem[];
-    const int g = threadIdx.x / (32 * p.warps);
-    const int group = blockIdx.x * (blockDim.x / (32 * p.warps)) + g;
+    extern __shared__ __align__(16) unsigned char norm_smem[];
+    constexpr int S = A ? 2 : 1;
+    const int per_cta = J == 0 ? blockDim.x / 32 : blockDim.x / (32 * p.warps), g = J == 0 ? threadIdx.x / 32 : threadIdx.x / (32 * p.warps);
+    const int group = blockIdx.x * per_cta + g;
     if (group >= p.groups) return;
-    const int t = threadIdx.x - g * 32 * p.warps, warp = t / 32, lane = t & 31, c = 8 * t;
-    const bool active = c < p.C;
+    Group<J> me = {reinterpret_cast<float2*>(norm_smem) + g * 64, 0, static_cast<int>(threadIdx.x / 32) - g * (J == 0 ? 1 : p.warps),
+                   static_cast<int>(threadIdx.x & 31), g};
+    RowRing<S, V> ring;
+    ring.begin(smem_u32(norm_smem) + per_cta * 64 * 8);
+    // vector v of the thread: channels 256 (V warp + v) + 8 lane ..
+    const int c0 = 256 * V * me.warp + 8 * me.lane;
+    bool active[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) active[v] = c0 + 256 * v < p.C;
     const GroupRows rows = group_rows(p, group);
-    GroupExchange<R> ex = {norm_smem + g * 2 * R * kNormMaxWarps, 0};
+
+    Walk x(p.x, rows, c0), a(p.a, rows, c0), y(p.y, rows, c0), n(p.n, rows, c0);
+    int to_fetch = rows.end - rows.begin;
+    auto fetch = [&]() {
+        if (to_fetch > 0) {
+            --to_fetch;
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (active[v]) {
+                    ring.fill(0, v, x.p + 512 * v);
+                    if (A) ring.fill(S - 1, v, a.p + 512 * v);
+                }
+            ring.fill_at = ring.next(ring.fill_at);
+            x.step();
+            if (A) a.step();
+        }
+        copies_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < norm_stages(V) - 1; ++i) fetch();
 
     // y = rs x + (h Ap + Bp);  n = h An + Bn
-    F8 Ap, Bp, An, Bn;
-    if (A) {
-        const F8 gate = load_vector<KIND>(p.gate.p == nullptr ? nullptr : p.gate.p + rows.b * p.gate.b, c, active, 1.0f);
-        Ap = load_vector<KIND>(p.post_w, c, active, 1.0f);
-        Bp = load_vector<KIND>(p.post_b, c, active, 0.0f);
+    P8 Ap[V], Bp[V], An[V], Bn[V];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) Ap.v[i] *= gate.v[i], Bp.v[i] *= gate.v[i];
-    }
-    if (PRE != kNormNone) {
-        const F8 scale = load_vector<KIND>(p.scale.p == nullptr ? nullptr : p.scale.p + rows.b * p.scale.b, c, active, 0.0f);
-        const F8 shift = load_vector<KIND>(p.shift.p == nullptr ? nullptr : p.shift.p + rows.b * p.shift.b, c, active, 0.0f);
-        An = load_vector<KIND>(p.pre_w, c, active, 1.0f);
-        Bn = load_vector<KIND>(p.pre_b, c, active, 0.0f);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            An.v[i] *= 1.0f + scale.v[i];
-            Bn.v[i] = fmaf(Bn.v[i], 1.0f + scale.v[i], shift.v[i]);
-        }
-    }
-    const char* x0 = p.x.p + rows.b * p.x.b + 2 * c;
-    const char* a0 = A ? p.a.p + rows.b * p.a.b + 2 * c : nullptr;
-    char* y0 = A ? p.y.p + rows.b * p.y.b + 2 * c : nullptr;
-    char* n0 = PRE != kNormNone ? p.n.p + rows.b * p.n.b + 2 * c : nullptr;
-    for (int i0 = rows.begin; i0 < rows.end; i0 += R) {
-        uint4 xr[R], ar[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            xr[r] = ar[r] = make_uint4(0u, 0u, 0u, 0u);
-            if (active && i0 + r < rows.end) {
-                xr[r] = load16(x0 + (i0 + r) * p.x.r);
-                if (A) ar[r] = load16(a0 + (i0 + r) * p.a.r);
-            }
-        }
-        F8 y[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) y[r] = unpack8<KIND>(xr[r]);
-        float mean[R], rstd[R];
+    for (int v = 0; v < V; ++v) {
+        const int c = c0 + 256 * v;
         if (A) {
-            F8 h[R];
+            const P8 gate = load_vector<KIND>(p.gate.p == nullptr ? nullptr : p.gate.p + rows.b * p.gate.b, c, active[v], 1.0f);
+            Ap[v] = load_vector<KIND>(p.post_w, c, active[v], 1.0f);
+            Bp[v] = load_vector<KIND>(p.post_b, c, active[v], 0.0f);
 #pragma unroll
-            for (int r = 0; r < R; ++r) h[r] = unpack8<KIND>(ar[r]);
-            if (POST != kNormNone) {
-                row_stats<POST == kNormNone ? kNormRms : POST, R>(h, active, p, warp, lane, g, ex, mean, rstd);
-#pragma unroll
-                for (int r = 0; r < R; ++r)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) h[r].v[i] = (h[r].v[i] - mean[r]) * rstd[r];
-            }
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[r].v[i] = fmaf(p.rs, y[r].v[i], fmaf(h[r].v[i], Ap.v[i], Bp.v[i]));
-                const uint4 stored = pack8<KIND>(y[r]);
-                if (active && i0 + r < rows.end) store16(y0 + (i0 + r) * p.y.r, stored);
-                y[r] = unpack8<KIND>(stored);  // the norm below is that of the stored stream
-            }
+            for (int i = 0; i < 4; ++i) Ap[v].v[i] = mul2(Ap[v].v[i], gate.v[i]), Bp[v].v[i] = mul2(Bp[v].v[i], gate.v[i]);
         }
         if (PRE != kNormNone) {
-            row_stats<PRE == kNormNone ? kNormRms : PRE, R>(y, active, p, warp, lane, g, ex, mean, rstd);
+            const P8 scale = load_vector<KIND>(p.scale.p == nullptr ? nullptr : p.scale.p + rows.b * p.scale.b, c, active[v], 0.0f);
+            const P8 shift = load_vector<KIND>(p.shift.p == nullptr ? nullptr : p.shift.p + rows.b * p.shift.b, c, active[v], 0.0f);
+            An[v] = load_vector<KIND>(p.pre_w, c, active[v], 1.0f);
+            Bn[v] = load_vector<KIND>(p.pre_b, c, active[v], 0.0f);
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                F8 o;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) o.v[i] = fmaf((y[r].v[i] - mean[r]) * rstd[r], An.v[i], Bn.v[i]);
-                if (active && i0 + r < rows.end) store16(n0 + (i0 + r) * p.n.r, pack8<KIND>(o));
+            for (int i = 0; i < 4; ++i) {
+                const f32x2 s = add2(scale.v[i], both(1.0f));
+                An[v].v[i] = mul2(An[v].v[i], s);
+                Bn[v].v[i] = fma2(Bn[v].v[i], s, shift.v[i]);
             }
+        }
+    }
+    const f32x2 rs = both(p.rs);
+    for (int left = rows.end - rows.begin; left > 0; --left) {
+        copies_wait<norm_stages(V) - 2>();
+        P8 s[V], h[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            s[v] = unpack_pairs<KIND>(ring.read(0, v));
+            if (A) h[v] = unpack_pairs<KIND>(ring.read(S - 1, v));
+        }
+        ring.read_at = ring.next(ring.read_at);
+        fetch();  // into the slots of the row before, which has been read
+        Stats st = {0.0f, 1.0f};
+        if (A) {
+            if (POST != kNormNone) two_stats<POST, kNormNone, V, J>(h, h, active, p, me, &st, nullptr);
+            const f32x2 r = both(st.rstd), m = both(-st.mean * st.rstd);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x2 e = POST == kNormNone ? h[v].v[i] : POST == kNormRms ? mul2(h[v].v[i], r) : fma2(h[v].v[i], r, m);
+                    s[v].v[i] = fma2(rs, s[v].v[i], fma2(e, Ap[v].v[i], Bp[v].v[i]));
+                }
+                const uint4 stored = pack_pairs<KIND>(s[v]);
+                if (active[v]) store16(y.p + 512 * v, stored);
+                if (PRE != kNormNone) s[v] = unpack_pairs<KIND>(stored);  // the norm below is that of the stored stream
+            }
+            y.step();
+        }
+        if (PRE != kNormNone) {
+            two_stats<PRE, kNormNone, V, J>(s, s, active, p, me, &st, nullptr);
+            const f32x2 r = both(st.rstd), m = both(-st.mean * st.rstd);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                P8 o;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    o.v[i] = fma2(PRE == kNormRms ? mul2(s[v].v[i], r) : fma2(s[v].v[i], r, m), An[v].v[i], Bn[v].v[i]);
+                if (active[v]) store16(n.p + 512 * v, pack_pairs<KIND>(o));
+            }
+            n.step();
         }
     }
 }
@@ -486,145 +617,175 @@ __global__ void __launch_bounds__(T) block_norm_kernel(const __grid_constant__ N
 // and every vector's gradient follows from four column sums over a batch entry's rows:
 //     [0] sum dn   [1] sum dn h   [2] sum u e   [3] sum u
 // which the group keeps in registers over its rows and leaves as partials for block_norm_grads_kernel.
-template <int KIND, int POST, int PRE, bool A, int R, int T>
-__global__ void __launch_bounds__(T) block_norm_backward_kernel(const __grid_constant__ NormParams p)
+template <int KIND, int POST, int PRE, bool A, int V, int J>
+__global__ void __launch_bounds__(kNormMaxThreads) block_norm_backward_kernel(const __grid_constant__ NormParams p)
 {
-    extern __shared__ float2 norm_smem[];
-    const int g = threadIdx.x / (32 * p.warps);
-    const int group = blockIdx.x * (blockDim.x / (32 * p.warps)) + g;
+    extern __shared__ __align__(16) unsigned char norm_smem[];
+    constexpr int S = (PRE != kNormNone ? 2 : 0) + (A ? 2 : 1);
+    constexpr int kY = 0, kDn = 1, kDy = PRE != kNormNone ? 2 : 0, kA = S - 1;
+    const int per_cta = J == 0 ? blockDim.x / 32 : blockDim.x / (32 * p.warps), g = J == 0 ? threadIdx.x / 32 : threadIdx.x / (32 * p.warps);
+    const int group = blockIdx.x * per_cta + g;
     if (group >= p.groups) return;
-    const int t = threadIdx.x - g * 32 * p.warps, warp = t / 32, lane = t & 31, c = 8 * t;
-    const bool active = c < p.C;
+    Group<J> me = {reinterpret_cast<float2*>(norm_smem) + g * 64, 0, static_cast<int>(threadIdx.x / 32) - g * (J == 0 ? 1 : p.warps),
+                   static_cast<int>(threadIdx.x & 31), g};
+    RowRing<S, V> ring;
+    ring.begin(smem_u32(norm_smem) + per_cta * 64 * 8);
+    const int c0 = 256 * V * me.warp + 8 * me.lane;
+    bool active[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) active[v] = c0 + 256 * v < p.C;
     const GroupRows rows = group_rows(p, group);
-    GroupExchange<R> ex = {norm_smem + g * 2 * R * kNormMaxWarps, 0};
-
-    F8 Ap, An;
-    if (A) {
-        const F8 gate = load_vector<KIND>(p.gate.p == nullptr ? nullptr : p.gate.p + rows.b * p.gate.b, c, active, 1.0f);
-        Ap = load_vector<KIND>(p.post_w, c, active, 1.0f);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) Ap.v[i] *= gate.v[i];
-    }
-    if (PRE != kNormNone) {
-        const F8 scale = load_vector<KIND>(p.scale.p == nullptr ? nullptr : p.scale.p + rows.b * p.scale.b, c, active, 0.0f);
-        An = load_vector<KIND>(p.pre_w, c, active, 1.0f);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) An.v[i] *= 1.0f + scale.v[i];
-    }
-    F8 sum[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum[k].v[i] = 0.0f;
-
     const bool has_dy = p.dy.p != nullptr;
-    const char* y0 = PRE != kNormNone ? p.x.p + rows.b * p.x.b + 2 * c : nullptr;
-    const char* a0 = A ? p.a.p + rows.b * p.a.b + 2 * c : nullptr;
-    const char* dy0 = has_dy ? p.dy.p + rows.b * p.dy.b + 2 * c : nullptr;
-    const char* dn0 = PRE != kNormNone ? p.dn.p + rows.b * p.dn.b + 2 * c : nullptr;
-    char* dx0 = p.dx.p + rows.b * p.dx.b + 2 * c;
-    char* da0 = A ? p.da.p + rows.b * p.da.b + 2 * c : nullptr;
-    for (int i0 = rows.begin; i0 < rows.end; i0 += R) {
-        uint4 yr[R], ar[R], ur[R], gr[R];
+    Walk y(p.x, rows, c0), a(p.a, rows, c0), dy(p.dy, rows, c0), dnw(p.dn, rows, c0), dx(p.dx, rows, c0), da(p.da, rows, c0);
+    int to_fetch = rows.end - rows.begin;
+    auto fetch = [&]() {
+        if (to_fetch > 0) {
+            --to_fetch;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            yr[r] = ar[r] = ur[r] = gr[r] = make_uint4(0u, 0u, 0u, 0u);
-            if (active && i0 + r < rows.end) {
-                if (PRE != kNormNone) yr[r] = load16(y0 + (i0 + r) * p.x.r);
-                if (PRE != kNormNone) gr[r] = load16(dn0 + (i0 + r) * p.dn.r);
-                if (has_dy) ur[r] = load16(dy0 + (i0 + r) * p.dy.r);
-                if (A) ar[r] = load16(a0 + (i0 + r) * p.a.r);
-            }
-        }
-        F8 u[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) u[r] = unpack8<KIND>(ur[r]);
-        float mean[R], rstd[R], m1[R], m2[R];
-        if (PRE != kNormNone) {
-            F8 h[R];
-#pragma unroll
-            for (int r = 0; r < R; ++r) h[r] = unpack8<KIND>(yr[r]);
-            row_stats<PRE == kNormNone ? kNormRms : PRE, R>(h, active, p, warp, lane, g, ex, mean, rstd);
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const F8 dn = unpack8<KIND>(gr[r]);
-                m1[r] = m2[r] = 0.0f;
-                if (active && i0 + r < rows.end) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        h[r].v[i] = (h[r].v[i] - mean[r]) * rstd[r];
-                        sum[0].v[i] += dn.v[i];
-                        sum[1].v[i] = fmaf(dn.v[i], h[r].v[i], sum[1].v[i]);
-                        const float w = dn.v[i] * An.v[i];
-                        m1[r] += w;
-                        m2[r] = fmaf(w, h[r].v[i], m2[r]);
-                    }
+            for (int v = 0; v < V; ++v)
+                if (active[v]) {
+                    if (PRE != kNormNone) ring.fill(kY, v, y.p + 512 * v);
+                    if (PRE != kNormNone) ring.fill(kDn, v, dnw.p + 512 * v);
+                    if (has_dy) ring.fill(kDy, v, dy.p + 512 * v);
+                    if (A) ring.fill(kA, v, a.p + 512 * v);
                 }
-            }
-            row_sums<R>(m1, m2, p, warp, lane, g, ex);
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const F8 dn = unpack8<KIND>(gr[r]);
-                const float b1 = PRE == kNormLayer ? m1[r] * p.inv_c : 0.0f, b2 = m2[r] * p.inv_c;
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    u[r].v[i] = fmaf(rstd[r], dn.v[i] * An.v[i] - b1 - h[r].v[i] * b2, u[r].v[i]);
-            }
+            ring.fill_at = ring.next(ring.fill_at);
+            if (PRE != kNormNone) y.step(), dnw.step();
+            if (has_dy) dy.step();
+            if (A) a.step();
         }
+        copies_commit();
+    };
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (active && i0 + r < rows.end) {
-                F8 o;
+    for (int i = 0; i < norm_stages(V) - 1; ++i) fetch();
+
+    P8 Ap[V], An[V], sum[4][V];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) o.v[i] = p.rs * u[r].v[i];
-                store16(dx0 + (i0 + r) * p.dx.r, pack8<KIND>(o));
-            }
+    for (int v = 0; v < V; ++v) {
+        const int c = c0 + 256 * v;
         if (A) {
-            F8 e[R];
+            const P8 gate = load_vector<KIND>(p.gate.p == nullptr ? nullptr : p.gate.p + rows.b * p.gate.b, c, active[v], 1.0f);
+            Ap[v] = load_vector<KIND>(p.post_w, c, active[v], 1.0f);
 #pragma unroll
-            for (int r = 0; r < R; ++r) e[r] = unpack8<KIND>(ar[r]);
-            if (POST != kNormNone) row_stats<POST == kNormNone ? kNormRms : POST, R>(e, active, p, warp, lane, g, ex, mean, rstd);
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                m1[r] = m2[r] = 0.0f;
-                if (active && i0 + r < rows.end) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        if (POST != kNormNone) e[r].v[i] = (e[r].v[i] - mean[r]) * rstd[r];
-                        sum[2].v[i] = fmaf(u[r].v[i], e[r].v[i], sum[2].v[i]);
-                        sum[3].v[i] += u[r].v[i];
-                        u[r].v[i] *= Ap.v[i];
-                        m1[r] += u[r].v[i];
-                        m2[r] = fmaf(u[r].v[i], e[r].v[i], m2[r]);
-                    }
-                }
-            }
-            if (POST != kNormNone) row_sums<R>(m1, m2, p, warp, lane, g, ex);
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-                if (active && i0 + r < rows.end) {
-                    if (POST != kNormNone) {
-                        const float b1 = POST == kNormLayer ? m1[r] * p.inv_c : 0.0f, b2 = m2[r] * p.inv_c;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) u[r].v[i] = rstd[r] * (u[r].v[i] - b1 - e[r].v[i] * b2);
-                    }
-                    store16(da0 + (i0 + r) * p.da.r, pack8<KIND>(u[r]));
-                }
+            for (int i = 0; i < 4; ++i) Ap[v].v[i] = mul2(Ap[v].v[i], gate.v[i]);
         }
-    }
-    if (active) {
+        if (PRE != kNormNone) {
+            const P8 scale = load_vector<KIND>(p.scale.p == nullptr ? nullptr : p.scale.p + rows.b * p.scale.b, c, active[v], 0.0f);
+            An[v] = load_vector<KIND>(p.pre_w, c, active[v], 1.0f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) An[v].v[i] = mul2(An[v].v[i], add2(scale.v[i], both(1.0f)));
+        }
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-            if ((p.want >> k) & 1) {
-                float4* to = reinterpret_cast<float4*>(p.partials + (static_cast<size_t>(k) * p.groups + group) * p.C + c);
-                to[0] = make_float4(sum[k].v[0], sum[k].v[1], sum[k].v[2], sum[k].v[3]);
-                to[1] = make_float4(sum[k].v[4], sum[k].v[5], sum[k].v[6], sum[k].v[7]);
-            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[k][v].v[i] = both(0.0f);
     }
+    const f32x2 rs = both(p.rs), zero = both(0.0f);
+    for (int left = rows.end - rows.begin; left > 0; --left) {
+        copies_wait<norm_stages(V) - 2>();
+        P8 h[V], dn[V], u[V], e[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (PRE != kNormNone) h[v] = unpack_pairs<KIND>(ring.read(kY, v));
+            if (A) e[v] = unpack_pairs<KIND>(ring.read(kA, v));
+        }
+        Stats sy = {0.0f, 1.0f}, sa = {0.0f, 1.0f};
+        if (PRE != kNormNone || (A && POST != kNormNone)) two_stats<PRE, A ? POST : kNormNone, V, J>(h, e, active, p, me, &sy, &sa);
+        if (PRE != kNormNone) {
+            const f32x2 r = both(sy.rstd);
+            f32x2 m1 = zero, m2 = zero;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const f32x2 m = both(active[v] ? -sy.mean * sy.rstd : 0.0f);
+                dn[v] = unpack_pairs<KIND>(ring.read(kDn, v));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    h[v].v[i] = PRE == kNormRms ? mul2(h[v].v[i], r) : fma2(h[v].v[i], r, m);
+                    sum[0][v].v[i] = add2(sum[0][v].v[i], dn[v].v[i]);
+                    sum[1][v].v[i] = fma2(dn[v].v[i], h[v].v[i], sum[1][v].v[i]);
+                    dn[v].v[i] = mul2(dn[v].v[i], An[v].v[i]);
+                    if (PRE == kNormLayer) m1 = i + v == 0 ? dn[v].v[i] : add2(m1, dn[v].v[i]);
+                    m2 = i + v == 0 ? mul2(dn[v].v[i], h[v].v[i]) : fma2(dn[v].v[i], h[v].v[i], m2);
+                }
+            }
+            const float2 b = two_means<J>(m1, m2, p, me);
+            const f32x2 b1 = both(-sy.rstd * b.x), b2 = both(-sy.rstd * b.y);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                u[v] = unpack_pairs<KIND>(ring.read(kDy, v));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x2 k = PRE == kNormLayer ? fma2(h[v].v[i], b2, b1) : mul2(h[v].v[i], b2);
+                    u[v].v[i] = add2(u[v].v[i], fma2(r, dn[v].v[i], k));
+                }
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) u[v] = unpack_pairs<KIND>(ring.read(kDy, v));
+        }
+        ring.read_at = ring.next(ring.read_at);
+        fetch();  // into the slots of the row before
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            P8 o;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o.v[i] = mul2(rs, u[v].v[i]);
+            if (active[v]) store16(dx.p + 512 * v, pack_pairs<KIND>(o));
+        }
+        dx.step();
+        if (A) {
+            const f32x2 r = both(sa.rstd);
+            f32x2 m1 = zero, m2 = zero;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const f32x2 m = both(-sa.mean * sa.rstd);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (POST != kNormNone) e[v].v[i] = POST == kNormRms ? mul2(e[v].v[i], r) : fma2(e[v].v[i], r, m);
+                    sum[2][v].v[i] = fma2(u[v].v[i], e[v].v[i], sum[2][v].v[i]);
+                    sum[3][v].v[i] = add2(sum[3][v].v[i], u[v].v[i]);
+                    u[v].v[i] = mul2(u[v].v[i], Ap[v].v[i]);  // zero where the lane has no channels
+                    if (POST == kNormLayer) m1 = i + v == 0 ? u[v].v[i] : add2(m1, u[v].v[i]);
+                    if (POST != kNormNone) m2 = i + v == 0 ? mul2(u[v].v[i], e[v].v[i]) : fma2(u[v].v[i], e[v].v[i], m2);
+                }
+            }
+            f32x2 b1 = zero, b2 = zero;
+            if (POST != kNormNone) {
+                const float2 b = two_means<J>(m1, m2, p, me);
+                b1 = both(-sa.rstd * b.x);
+                b2 = both(-sa.rstd * b.y);
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (POST != kNormNone) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        u[v].v[i] = fma2(r, u[v].v[i], POST == kNormLayer ? fma2(e[v].v[i], b2, b1) : mul2(e[v].v[i], b2));
+                }
+                if (active[v]) store16(da.p + 512 * v, pack_pairs<KIND>(u[v]));
+            }
+            da.step();
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if ((p.want >> k) & 1)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (active[v]) {
+                    float4* to = reinterpret_cast<float4*>(p.partials + (static_cast<size_t>(k) * p.groups + group) * p.C + c0 + 256 * v);
+                    const float2 q0 = unpack2(sum[k][v].v[0]), q1 = unpack2(sum[k][v].v[1]), q2 = unpack2(sum[k][v].v[2]),
+                                 q3 = unpack2(sum[k][v].v[3]);
+                    to[0] = make_float4(q0.x, q0.y, q1.x, q1.y);
+                    to[1] = make_float4(q2.x, q2.y, q3.x, q3.y);
+                }
     pdl_launch_dependents();
 }
 
-// Second stage: the column sums of each batch entry in a fixed order, and from them the vectors' gradients.
+// Second stage: the column sums in a fixed order, and from them the vectors' gradients.  grid.y = 0 sums over all batch
+// entries (gradients of weights, biases and shared vectors), grid.y = 1 + b over entry b (vectors of its own).  A block takes
+// 32 channels: eight threads of four channels each, 64 slices of the groups; a slice adds its groups in order, the
+// slices are added in a fixed tree.
 struct NormGradParams {
     const float* partials;
     int B, C, chunks, groups, want;
@@ -633,7 +794,7 @@ struct NormGradParams {
     int gate_per_batch, scale_per_batch, shift_per_batch;
     float *d_gate, *d_scale, *d_shift, *d_pre_w, *d_pre_b, *d_post_w, *d_post_b;
 };
-constexpr int kNormGradSlices = 32;
+constexpr int kNormGradThreads = 512;
 
 template <int KIND>
 __device__ __forceinline__ float channel(const char* p, int c, float absent)
@@ -643,60 +804,77 @@ __device__ __forceinline__ float channel(const char* p, int c, float absent)
     return pair_lo<KIND>(h);
 }
 
-// 32 channels x 32 slices of the groups; the slices are joined through shared memory.
 template <int KIND>
-__global__ void __launch_bounds__(32 * kNormGradSlices) block_norm_grads_kernel(const __grid_constant__ NormGradParams p)
+__global__ void __launch_bounds__(kNormGradThreads) block_norm_grads_kernel(const __grid_constant__ NormGradParams p)
 {
-    __shared__ float s[4][kNormGradSlices][33];
-    const int lane = threadIdx.x & 31, slice = threadIdx.x / 32, c = blockIdx.x * 32 + lane;
+    constexpr int WARPS = kNormGradThreads / 32, SLICES = kNormGradThreads / 8;
+    __shared__ float s[8][WARPS][32];
+    const int column = threadIdx.x & 7, slice = threadIdx.x / 8, warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    const int c = blockIdx.x * 32 + column * 4;
+    const bool all = blockIdx.y == 0;
+    const int first = all ? 0 : (blockIdx.y - 1) * p.chunks, last = all ? p.groups : first + p.chunks;
+    // [0 .. 3]: the column sums; [4 .. 7], over all entries: weighted by 1 + scale (dn, dn h) and by the gate (u e, u)
+    float acc[8][4] = {};
     pdl_wait();
-    float all[7] = {};  // over the batch: shift, scale, pre_b, pre_w, gate, post_w, post_b (slice 0)
-    for (int b = 0; b < p.B; ++b) {
+    if (c < p.C) {
+        const bool weighted = all && (p.scale.p != nullptr || p.gate.p != nullptr);
+        for (int i = first + slice; i < last; i += SLICES) {
+            float4 v[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            float v = 0.0f;
-            if (((p.want >> k) & 1) && c < p.C)
-                for (int i = slice; i < p.chunks; i += kNormGradSlices)
-                    v += p.partials[(static_cast<size_t>(k) * p.groups + static_cast<size_t>(b) * p.chunks + i) * p.C + c];
-            s[k][slice][lane] = v;
+            for (int k = 0; k < 4; ++k)
+                v[k] = ((p.want >> k) & 1) ? *reinterpret_cast<const float4*>(p.partials + (static_cast<size_t>(k) * p.groups + i) * p.C + c)
+                                           : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            float sc[4] = {1.0f, 1.0f, 1.0f, 1.0f}, gt[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+            if (weighted) {
+                const int b = i / p.chunks;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    sc[j] = 1.0f + channel<KIND>(p.scale.p == nullptr ? nullptr : p.scale.p + b * p.scale.b, c + j, 0.0f);
+                    gt[j] = channel<KIND>(p.gate.p == nullptr ? nullptr : p.gate.p + b * p.gate.b, c + j, 1.0f);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float x[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    acc[k][j] += x[j];
+                    acc[k + 4][j] = fmaf(k < 2 ? sc[j] : gt[j], x[j], acc[k + 4][j]);
+                }
+            }
         }
-        __syncthreads();
-        // warp k joins column sum k: lane l over the slices of channel c
-        if (slice < 4) {
-            float v = 0.0f;
-            for (int i = 0; i < kNormGradSlices; ++i) v += s[slice][i][lane];
-            s[slice][0][lane] = v;
-        }
-        __syncthreads();
-        if (slice == 0 && c < p.C) {
-            const float dn = s[0][0][lane], dnh = s[1][0][lane], ue = s[2][0][lane], u = s[3][0][lane];
-            const size_t at = static_cast<size_t>(b) * p.C + c;
-            const float w = channel<KIND>(p.pre_w, c, 1.0f), wb = channel<KIND>(p.pre_b, c, 0.0f);
-            const float sc = 1.0f + channel<KIND>(p.scale.p == nullptr ? nullptr : p.scale.p + b * p.scale.b, c, 0.0f);
-            const float d_scale = w * dnh + wb * dn;
-            const float gate = channel<KIND>(p.gate.p == nullptr ? nullptr : p.gate.p + b * p.gate.b, c, 1.0f);
-            const float d_gate = channel<KIND>(p.post_w, c, 1.0f) * ue + channel<KIND>(p.post_b, c, 0.0f) * u;
-            if (p.d_shift != nullptr && p.shift_per_batch) p.d_shift[at] = dn;
-            if (p.d_scale != nullptr && p.scale_per_batch) p.d_scale[at] = d_scale;
-            if (p.d_gate != nullptr && p.gate_per_batch) p.d_gate[at] = d_gate;
-            all[0] += dn;
-            all[1] += d_scale;
-            all[2] += sc * dn;
-            all[3] += sc * dnh;
-            all[4] += d_gate;
-            all[5] += gate * ue;
-            all[6] += gate * u;
-        }
-        __syncthreads();
     }
-    if (slice != 0 || c >= p.C) return;
-    if (p.d_shift != nullptr && !p.shift_per_batch) p.d_shift[c] = all[0];
-    if (p.d_scale != nullptr && !p.scale_per_batch) p.d_scale[c] = all[1];
-    if (p.d_pre_b != nullptr) p.d_pre_b[c] = all[2];
-    if (p.d_pre_w != nullptr) p.d_pre_w[c] = all[3];
-    if (p.d_gate != nullptr && !p.gate_per_batch) p.d_gate[c] = all[4];
-    if (p.d_post_w != nullptr) p.d_post_w[c] = all[5];
-    if (p.d_post_b != nullptr) p.d_post_b[c] = all[6];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            acc[k][j] += __shfl_xor_sync(0xffffffffu, acc[k][j], 8);
+            acc[k][j] += __shfl_xor_sync(0xffffffffu, acc[k][j], 16);
+            if (lane < 8) s[k][warp][column * 4 + j] = acc[k][j];
+        }
+    __syncthreads();
+    if (threadIdx.x < 256) {
+        const int k = threadIdx.x / 32;
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) v += s[k][w][lane];
+        s[k][0][lane] = v;
+    }
+    __syncthreads();
+    const int ch = blockIdx.x * 32 + threadIdx.x;
+    if (threadIdx.x >= 32 || ch >= p.C) return;
+    const float dn = s[0][0][lane], dnh = s[1][0][lane], ue = s[2][0][lane], u = s[3][0][lane];
+    const float d_scale = channel<KIND>(p.pre_w, ch, 1.0f) * dnh + channel<KIND>(p.pre_b, ch, 0.0f) * dn;
+    const float d_gate = channel<KIND>(p.post_w, ch, 1.0f) * ue + channel<KIND>(p.post_b, ch, 0.0f) * u;
+    const size_t at = (all ? 0 : static_cast<size_t>(blockIdx.y - 1) * p.C) + ch;
+    if (p.d_shift != nullptr && all != (p.shift_per_batch != 0)) p.d_shift[at] = dn;
+    if (p.d_scale != nullptr && all != (p.scale_per_batch != 0)) p.d_scale[at] = d_scale;
+    if (p.d_gate != nullptr && all != (p.gate_per_batch != 0)) p.d_gate[at] = d_gate;
+    if (!all) return;
+    if (p.d_pre_b != nullptr) p.d_pre_b[ch] = s[4][0][lane];
+    if (p.d_pre_w != nullptr) p.d_pre_w[ch] = s[5][0][lane];
+    if (p.d_post_w != nullptr) p.d_post_w[ch] = s[6][0][lane];
+    if (p.d_post_b != nullptr) p.d_post_b[ch] = s[7][0][lane];
 }
 
 }  // namespace lf

@@ -151,7 +151,7 @@ linfusion_status_t check_norm(const linfusion_block_norm_desc_t* d)
     if (d == nullptr) return LINFUSION_ERR_INVALID_ARG;
     if (d->B <= 0 || d->N <= 0 || d->C <= 0) return LINFUSION_ERR_INVALID_ARG;
     if (!std::isfinite(d->eps) || d->eps < 0.0f || !std::isfinite(d->residual_scale)) return LINFUSION_ERR_INVALID_ARG;
-    if (d->C % 8 != 0 || d->C > LINFUSION_BLOCK_NORM_MAX_C || d->B > 65535) return LINFUSION_ERR_UNSUPPORTED;
+    if (d->C % 8 != 0 || d->C > LINFUSION_BLOCK_NORM_MAX_C || d->B > 65534) return LINFUSION_ERR_UNSUPPORTED;
     if ((d->flags & ~LINFUSION_DTYPE_FP16) != 0u) return LINFUSION_ERR_UNSUPPORTED;
     for (const int32_t n : {d->pre, d->post})
         if (n < LINFUSION_NORM_NONE || n > LINFUSION_NORM_RMS) return LINFUSION_ERR_UNSUPPORTED;
@@ -210,28 +210,29 @@ bool apart(const linfusion_block_norm_desc_t& d, const linfusion_rows_t* out, co
     return true;
 }
 
-// How rows are dealt out: groups of `warps` warps, `per_cta` of them in a block, `chunks` for each batch entry.
+// How rows are dealt out: groups of `warps` warps, each thread with `vectors` pieces of eight channels, `per_cta` groups in
+// a block, `chunks` groups for each batch entry.
 struct NormPlan {
-    int warps, per_cta, chunks, groups, ctas;
+    int vectors, warps, per_cta, chunks, groups, ctas;
 };
-// `rows_at_once`: rows a group loads together; `warps_per_sm`: warps that an SM is to hold.
-NormPlan norm_plan(const linfusion_block_norm_desc_t& d, int sms, int rows_at_once, int warps_per_sm)
+// `warps_per_sm`: warps that an SM holds at once.
+NormPlan norm_plan(const linfusion_block_norm_desc_t& d, int sms, int warps_per_sm)
 {
     NormPlan p;
-    p.warps = (d.C + 255) / 256;
+    p.vectors = d.C > 256 * kNormMaxWarps ? 2 : 1;
+    p.warps = (d.C + 256 * p.vectors - 1) / (256 * p.vectors);
     p.per_cta = p.warps >= 4 ? 1 : 4 / p.warps;
-    long long target = static_cast<long long>(sms) * (warps_per_sm / p.warps > 0 ? warps_per_sm / p.warps : 1);
-    long long chunks = (target + d.B - 1) / d.B;
-    const long long most = (d.N + rows_at_once - 1) / rows_at_once;
-    if (chunks > most) chunks = most;
+    // As many groups as run at once, so that none waits for another to end; fewer where there are fewer rows.
+    long long target = static_cast<long long>(sms) * (warps_per_sm / (p.warps * p.per_cta) > 0 ? warps_per_sm / (p.warps * p.per_cta) : 1) * p.per_cta;
+    long long chunks = target / d.B;
+    if (chunks > d.N) chunks = d.N;
     if (chunks < 1) chunks = 1;
     p.chunks = static_cast<int>(chunks);
     p.groups = p.chunks * d.B;
     p.ctas = (p.groups + p.per_cta - 1) / p.per_cta;
     return p;
 }
-constexpr int kForwardRows = 4, kBackwardRows = 2;
-constexpr int kForwardWarpsPerSm = 32, kBackwardWarpsPerSm = 16;
+constexpr int kForwardWarpsPerSm = 24, kBackwardWarpsPerSm = 16;
 
 void fill(NormParams* p, const linfusion_block_norm_desc_t& d, const linfusion_block_norm_vectors_t& v, const NormPlan& plan, bool branch)
 {
@@ -250,67 +251,64 @@ void fill(NormParams* p, const linfusion_block_norm_desc_t& d, const linfusion_b
     p->eps = d.eps;
     p->rs = branch ? d.residual_scale : 1.0f;  // without a branch y is x itself
     p->inv_c = 1.0f / static_cast<float>(d.C);
+    p->last = static_cast<float>(d.C - 256 * plan.vectors * (plan.warps - 1));
+    p->inv_last = 1.0f / p->last;
 }
 
-template <int KIND, int R, int T, bool BACKWARD>
-cudaError_t launch_norm(const NormParams& p, const NormPlan& plan, int post, int pre, bool branch, cudaStream_t s)
+template <int KIND, int POST, int PRE, bool A, int V, int J, bool BACKWARD>
+cudaError_t launch_norm_one(const NormParams& p, const NormPlan& plan, int device, cudaStream_t s)
 {
-    const dim3 grid(plan.ctas), block(32 * plan.warps * plan.per_cta);
-    const size_t smem = plan.warps > 1 ? static_cast<size_t>(plan.per_cta) * 2 * R * kNormMaxWarps * sizeof(float2) : 0;
-#define LF_NORM(POST, PRE, A)                                                                 \
-    if (BACKWARD) block_norm_backward_kernel<KIND, POST, PRE, A, R, T><<<grid, block, smem, s>>>(p); \
-    else block_norm_kernel<KIND, POST, PRE, A, R, T><<<grid, block, smem, s>>>(p)
+    static std::atomic<uint64_t> done{0};
+    const int threads = 32 * plan.warps * plan.per_cta;
+    const int streams = BACKWARD ? (PRE != kNormNone ? 2 : 0) + (A ? 2 : 1) : (A ? 2 : 1);
+    const size_t smem = norm_smem_bytes(streams, V, threads, plan.per_cta), most = norm_smem_bytes(streams, V, kNormMaxThreads, 4);
+    cudaError_t e;
+    if constexpr (BACKWARD) {
+        e = allow_smem(block_norm_backward_kernel<KIND, POST, PRE, A, V, J>, most, device, &done);
+        if (e == cudaSuccess) block_norm_backward_kernel<KIND, POST, PRE, A, V, J><<<plan.ctas, threads, smem, s>>>(p);
+    } else {
+        e = allow_smem(block_norm_kernel<KIND, POST, PRE, A, V, J>, most, device, &done);
+        if (e == cudaSuccess) block_norm_kernel<KIND, POST, PRE, A, V, J><<<plan.ctas, threads, smem, s>>>(p);
+    }
+    return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+template <int KIND, int V, int J, bool BACKWARD>
+cudaError_t launch_norm(const NormParams& p, const NormPlan& plan, int post, int pre, bool branch, int device, cudaStream_t s)
+{
+#define LF_NORM(POST, PRE, A) return launch_norm_one<KIND, POST, PRE, A, V, J, BACKWARD>(p, plan, device, s)
     if (!branch) {
-        if (pre == LINFUSION_NORM_LAYER) { LF_NORM(kNormNone, kNormLayer, false); }
-        else { LF_NORM(kNormNone, kNormRms, false); }
-        return cudaGetLastError();
+        if (pre == LINFUSION_NORM_LAYER) LF_NORM(kNormNone, kNormLayer, false);
+        LF_NORM(kNormNone, kNormRms, false);
     }
     switch (post * 3 + pre) {
-        case 0: LF_NORM(kNormNone, kNormNone, true); break;
-        case 1: LF_NORM(kNormNone, kNormLayer, true); break;
-        case 2: LF_NORM(kNormNone, kNormRms, true); break;
-        case 3: LF_NORM(kNormLayer, kNormNone, true); break;
-        case 4: LF_NORM(kNormLayer, kNormLayer, true); break;
-        case 5: LF_NORM(kNormLayer, kNormRms, true); break;
-        case 6: LF_NORM(kNormRms, kNormNone, true); break;
-        case 7: LF_NORM(kNormRms, kNormLayer, true); break;
-        default: LF_NORM(kNormRms, kNormRms, true); break;
+        case 0: LF_NORM(kNormNone, kNormNone, true);
+        case 1: LF_NORM(kNormNone, kNormLayer, true);
+        case 2: LF_NORM(kNormNone, kNormRms, true);
+        case 3: LF_NORM(kNormLayer, kNormNone, true);
+        case 4: LF_NORM(kNormLayer, kNormLayer, true);
+        case 5: LF_NORM(kNormLayer, kNormRms, true);
+        case 6: LF_NORM(kNormRms, kNormNone, true);
+        case 7: LF_NORM(kNormRms, kNormLayer, true);
+        default: LF_NORM(kNormRms, kNormRms, true);
     }
 #undef LF_NORM
-    return cudaGetLastError();
 }
 
 template <bool BACKWARD>
-cudaError_t launch_norm_kind(const linfusion_block_norm_desc_t& d, const NormParams& p, const NormPlan& plan, bool branch,
-                             int rows_at_once, cudaStream_t s)
+cudaError_t launch_norm_kind(const linfusion_block_norm_desc_t& d, const NormParams& p, const NormPlan& plan, bool branch, int device,
+                             cudaStream_t s)
 {
     const bool half = (d.flags & LINFUSION_DTYPE_FP16) != 0u;
     constexpr int bf = make_kind(kPhiIdentity, kDtypeBf16), hf = make_kind(kPhiIdentity, kDtypeFp16);
-    constexpr int R = BACKWARD ? kBackwardRows : kForwardRows;
-    // Threads of a block: 256 up to C = 2048 (and then several rows at once), 512 or 1024 beyond, where fewer registers
-    // a thread are left and the many warps of a row bring enough loads by themselves.
-#define LF_SIZED(ROWS, T) \
-    return half ? launch_norm<hf, ROWS, T, BACKWARD>(p, plan, d.post, d.pre, branch, s) \
-                : launch_norm<bf, ROWS, T, BACKWARD>(p, plan, d.post, d.pre, branch, s)
-    if (plan.warps > 16) LF_SIZED(1, 1024);
-    if (plan.warps > 8) LF_SIZED(1, 512);
-    if (rows_at_once == 1) LF_SIZED(1, 256);
-    LF_SIZED(R, 256);
+#define LF_SIZED(V, J)                                                                            \
+    return half ? launch_norm<hf, V, J, BACKWARD>(p, plan, d.post, d.pre, branch, device, s)       \
+                : launch_norm<bf, V, J, BACKWARD>(p, plan, d.post, d.pre, branch, device, s)
+    if (plan.vectors > 1) LF_SIZED(2, 4);
+    if (plan.warps > 8) LF_SIZED(1, 4);
+    if (plan.warps > 1) LF_SIZED(1, 3);
+    LF_SIZED(1, 0);
 #undef LF_SIZED
-}
-
-// Several rows at a time where there are enough of them to occupy every SM all the same.
-int rows_at_once(const linfusion_block_norm_desc_t& d, int sms, int rows, int warps_per_sm)
-{
-    const long long total = static_cast<long long>(d.B) * d.N, warps = (d.C + 255) / 256;
-    if (warps > 8) return 1;
-    return total * warps >= static_cast<long long>(sms) * warps_per_sm * rows ? rows : 1;
-}
-
-NormPlan backward_plan(const linfusion_block_norm_desc_t& d, int sms, int* rows)
-{
-    *rows = rows_at_once(d, sms, kBackwardRows, kBackwardWarpsPerSm);
-    return norm_plan(d, sms, *rows, kBackwardWarpsPerSm);
 }
 
 }  // namespace
@@ -407,15 +405,14 @@ linfusion_status_t linfusion_block_norm(const linfusion_block_norm_desc_t* desc,
         return LINFUSION_ERR_INVALID_ARG;
     const Here at = here();
     if (at.st != LINFUSION_OK) return at.st;
-    const int rows = rows_at_once(*desc, at.sms, kForwardRows, kForwardWarpsPerSm);
-    const NormPlan plan = norm_plan(*desc, at.sms, rows, kForwardWarpsPerSm);
+    const NormPlan plan = norm_plan(*desc, at.sms, kForwardWarpsPerSm);
     NormParams p = {};
     fill(&p, *desc, *v, plan, branch);
     p.x = to_rows(x);
     p.a = to_rows(a);
     p.y = to_rows(y);
     p.n = to_rows(n);
-    return end(launch_norm_kind<false>(*desc, p, plan, branch, rows, static_cast<cudaStream_t>(cuda_stream)));
+    return end(launch_norm_kind<false>(*desc, p, plan, branch, at.device, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 linfusion_status_t linfusion_block_norm_workspace_bytes(const linfusion_block_norm_desc_t* desc, int32_t sm_count, size_t* bytes)
@@ -423,8 +420,7 @@ linfusion_status_t linfusion_block_norm_workspace_bytes(const linfusion_block_no
     if (bytes == nullptr) return LINFUSION_ERR_INVALID_ARG;
     const linfusion_status_t st = check_norm(desc);
     if (st != LINFUSION_OK) return st;
-    int rows = 1;
-    const NormPlan plan = backward_plan(*desc, sm_count > 0 ? sm_count : 148, &rows);
+    const NormPlan plan = norm_plan(*desc, sm_count > 0 ? sm_count : 148, kBackwardWarpsPerSm);
     *bytes = align_up_256(static_cast<size_t>(4) * plan.groups * desc->C * sizeof(float));
     return LINFUSION_OK;
 }
@@ -472,8 +468,7 @@ linfusion_status_t linfusion_block_norm_backward(const linfusion_block_norm_desc
 
     const Here at = here();
     if (at.st != LINFUSION_OK) return at.st;
-    int rows = 1;
-    const NormPlan plan = backward_plan(*desc, at.sms, &rows);
+    const NormPlan plan = norm_plan(*desc, at.sms, kBackwardWarpsPerSm);
     if (want != 0) {
         if (workspace == nullptr || !is_aligned(workspace, 256)) return LINFUSION_ERR_INVALID_ARG;
         if (workspace_bytes < align_up_256(static_cast<size_t>(4) * plan.groups * desc->C * sizeof(float))) return LINFUSION_ERR_ALLOC;
@@ -489,7 +484,7 @@ linfusion_status_t linfusion_block_norm_backward(const linfusion_block_norm_desc
     p.partials = static_cast<float*>(workspace);
     p.want = want;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    cudaError_t e = launch_norm_kind<true>(*desc, p, plan, branch, rows, s);
+    cudaError_t e = launch_norm_kind<true>(*desc, p, plan, branch, at.device, s);
     if (e != cudaSuccess || want == 0) return end(e);
 
     NormGradParams g = {};
@@ -515,7 +510,9 @@ linfusion_status_t linfusion_block_norm_backward(const linfusion_block_norm_desc
     g.d_pre_b = grads->pre_bias;
     g.d_post_w = grads->post_weight;
     g.d_post_b = grads->post_bias;
-    const dim3 grid((desc->C + 31) / 32), block(32 * kNormGradSlices);
+    const bool own = (g.d_gate != nullptr && g.gate_per_batch) || (g.d_scale != nullptr && g.scale_per_batch) ||
+                     (g.d_shift != nullptr && g.shift_per_batch);
+    const dim3 grid((desc->C + 31) / 32, own ? 1 + desc->B : 1), block(kNormGradThreads);
     e = (desc->flags & LINFUSION_DTYPE_FP16) != 0u
             ? launch_pdl(block_norm_grads_kernel<make_kind(kPhiIdentity, kDtypeFp16)>, grid, block, 0, s, g)
             : launch_pdl(block_norm_grads_kernel<make_kind(kPhiIdentity, kDtypeBf16)>, grid, block, 0, s, g);
