@@ -312,7 +312,7 @@ class LinFusionAttention:
         import torch
         want = torch.float16 if self.dtype == "fp16" else torch.bfloat16
         shape = self.shape_qk if name in ("q", "k") else self.shape
-        if tuple(t.shape) != shape or t.dtype != want or not t.is_contiguous():
+        if t.shape != shape or t.dtype != want or not t.is_contiguous():
             raise ValueError(f"{name}: expected contiguous {self.dtype} tensor of shape {shape}")
 
     def _new_y(self, like):
@@ -502,7 +502,7 @@ class LinFusionAttention:
 
     def _check_state(self, t, name, device):
         import torch
-        if tuple(t.shape) != self.state_floats() or t.dtype != torch.float32 or not t.is_contiguous() or t.device != device:
+        if t.shape != self.state_floats() or t.dtype != torch.float32 or not t.is_contiguous() or t.device != device:
             raise ValueError(f"{name}: expected a contiguous fp32 tensor of shape {self.state_floats()} on {device}")
 
     def backward_workspace_bytes(self) -> int:
@@ -520,7 +520,8 @@ class LinFusionAttention:
     def _backward_args(self, tensors, states, outs, workspace, stream):
         """Checks; the outputs and the workspace that were not given; the stream."""
         import torch
-        device = torch.device("cuda", self.desc.device)
+        index = self.desc.device
+        device = torch.device("cuda", index)
         for t, name, like in tensors:
             self._check(t, like)
             if t.device != device:
@@ -529,24 +530,28 @@ class LinFusionAttention:
             self._check_state(t, name, device)
         made = []
         for t, name, like in outs:
-            if like == "state":
-                if t is None:
+            if t is None:
+                if like == "state":
                     t = torch.empty(self.state_floats(), dtype=torch.float32, device=device)
+                else:
+                    t = torch.empty(self.shape_qk if like in ("q", "k") else self.shape, dtype=tensors[0][0].dtype, device=device)
+            elif like == "state":
                 self._check_state(t, name, device)
             else:
-                if t is None:
-                    t = torch.empty(self.shape_qk if like in ("q", "k") else self.shape, dtype=tensors[0][0].dtype, device=device)
                 self._check(t, like)
                 if t.device != device:
                     raise ValueError(f"{name}: expected a tensor on {device}")
             made.append(t)
+        nbytes = self.backward_workspace_bytes()
         if workspace is None:
-            workspace = torch.empty(self.backward_workspace_bytes(), dtype=torch.uint8, device=device)
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
         elif workspace.device != device or not workspace.is_contiguous():
             raise ValueError(f"workspace: expected a contiguous tensor on {device}")
+        else:
+            nbytes = workspace.numel() * workspace.element_size()
         if stream is None:
-            stream = torch.cuda.current_stream(device).cuda_stream
-        return made, (workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream)
+            stream = torch._C._cuda_getCurrentRawStream(index)
+        return made, (workspace.data_ptr(), nbytes, stream)
 
     def backward(self, q, k, v, dy, state=None, dq=None, dk=None, dv=None, workspace=None, stream: Optional[int] = None):
         """(dq, dk, dv) from the gradient dy of the output.  ``state``: what ``save_state`` returned after the

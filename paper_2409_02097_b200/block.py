@@ -108,25 +108,49 @@ def _check_tensor(t, name, dtype, device=None):
         raise ValueError(f"{name}: the channels of a row must be contiguous")
 
 
-class _on:
-    """The device of the call's tensors made current for its length, where it is not."""
+_sms: Dict[int, int] = {}
 
-    def __init__(self, device):
+
+def _sm_count(index: int) -> int:
+    n = _sms.get(index)
+    if n is None:
         import torch
-        self._guard = torch.cuda.device(device) if torch.cuda.current_device() != device.index else None
-
-    def __enter__(self):
-        if self._guard is not None:
-            self._guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self._guard is not None:
-            self._guard.__exit__(*exc)
+        n = _sms[index] = torch.cuda.get_device_properties(index).multi_processor_count
+    return n
 
 
-def _stream(device, stream):
+def _look(t):
+    """What the checks of a tensor depend on; its address is no part of it."""
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device() if t.is_cuda else -1)
+
+
+class _Checked(dict):
+    """Argument checks by what they depend on (shapes, strides, types, devices): made once for each combination, not on
+    every call.  Holds descriptors only, no tensor and no address."""
+
+    MOST = 256
+
+    def keep(self, key, value):
+        if len(self) >= self.MOST:
+            self.clear()
+        self[key] = value
+        return value
+
+
+def _copy(struct):
+    """A structure of the caller's own (calls of several threads share the checked one)."""
+    return type(struct).from_buffer_copy(struct)
+
+
+def _call(index, stream, function, *args):
+    """`function(*args, stream)` with the tensors' device current."""
     import torch
-    return torch.cuda.current_stream(device).cuda_stream if stream is None else stream
+    if stream is None:
+        stream = torch._C._cuda_getCurrentRawStream(index)
+    if torch._C._cuda_getDevice() == index:
+        return function(*args, stream)
+    with torch.cuda.device(index):
+        return function(*args, stream)
 
 
 class AxialRope:
@@ -155,6 +179,7 @@ class AxialRope:
         self._padded = (_i32 * MAX_AXES)(*pairs)
         self._flags = DTYPE_FP16 if dtype == "fp16" else 0
         self._lib = load_library()
+        self._checked = _Checked()
 
     def _axes(self, t):
         """(batch, tokens, heads) axes' sizes and strides."""
@@ -162,31 +187,23 @@ class AxialRope:
         return ((s[0], s[2], s[1]), (st[0], st[2], st[1])) if self.layout == "head_major" else ((s[0], s[1], s[2]), st[:3])
 
     def _tensor(self, t, out, name, B, N, device):
-        import torch
         if t.dim() != 4 or t.shape[-1] != self.d:
             raise ValueError(f"{name}: expected four axes, the last of {self.d} channels, got {tuple(t.shape)}")
         _check_tensor(t, name, self._torch_dtype, device)
         (b, n, h), strides = self._axes(t)
         if (b, n) != (B, N):
             raise ValueError(f"{name}: expected {B} x {N} tokens, got {b} x {n}")
-        if out is None:
-            out = torch.empty(t.shape, dtype=t.dtype, device=t.device)
-        else:
-            if out.shape != t.shape:
-                raise ValueError(f"{name}: the output's shape is {tuple(out.shape)}, the input's {tuple(t.shape)}")
-            _check_tensor(out, name + " output", self._torch_dtype, device)
-        return out, RopeTensor(t.data_ptr(), out.data_ptr(), h, *strides, *self._axes(out)[1])
+        if out.shape != t.shape:
+            raise ValueError(f"{name}: the output's shape is {tuple(out.shape)}, the input's {tuple(t.shape)}")
+        _check_tensor(out, name + " output", self._torch_dtype, device)
+        return RopeTensor(None, None, h, *strides, *self._axes(out)[1])
 
-    def _run(self, q, k, positions, q_out, k_out, backward, stream):
+    def _check(self, q, k, positions, q_out, k_out, backward):
         import torch
         some = q if q is not None else k
-        if some is None:
-            raise ValueError("neither q nor k is given")
-        if some.dim() != 4:
-            raise ValueError(f"expected four axes, got {tuple(some.shape)}")
         (B, N, _), _s = self._axes(some)
-        device = some.device
         axes = len(self.pairs)
+        device = some.device
         if positions.dtype != torch.float32 or not positions.is_cuda or not positions.is_contiguous() or positions.device != device:
             raise ValueError("positions: expected a contiguous fp32 CUDA tensor on the device of q and k")
         if tuple(positions.shape) == (N, axes):
@@ -197,18 +214,40 @@ class AxialRope:
             raise ValueError(f"positions: expected {(N, axes)} or {(B, N, axes)}, got {tuple(positions.shape)}")
         if B == 0 or N == 0:
             raise ValueError("no tokens")
-        tq = tk = None
-        if q is not None:
-            q_out, tq = self._tensor(q, q_out, "q", B, N, device)
-        if k is not None:
-            k_out, tk = self._tensor(k, k_out, "k", B, N, device)
-        desc = RopeDesc(B, N, self.d, axes, self._padded, self.interleaved, backward, self.theta, self._flags)
-        with _on(device):
-            rc = self._lib.linfusion_rope(ctypes.byref(desc), None if tq is None else ctypes.byref(tq),
-                                          None if tk is None else ctypes.byref(tk), positions.data_ptr(), pos_batch,
-                                          _stream(device, stream))
-        _check_rc(rc, "linfusion_rope")
-        return (q_out if q is not None else None), (k_out if k is not None else None)
+        tq = None if q is None else self._tensor(q, q_out, "q", B, N, device)
+        tk = None if k is None else self._tensor(k, k_out, "k", B, N, device)
+        return RopeDesc(B, N, self.d, axes, self._padded, self.interleaved, backward, self.theta, self._flags), tq, tk, pos_batch
+
+    def _run(self, q, k, positions, q_out, k_out, backward, stream):
+        import torch
+        some = q if q is not None else k
+        if some is None:
+            raise ValueError("neither q nor k is given")
+        if some.dim() != 4:
+            raise ValueError(f"expected four axes, got {tuple(some.shape)}")
+        if q is None:
+            q_out = None
+        elif q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if k is None:
+            k_out = None
+        elif k_out is None:
+            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        key = (_look(q), _look(k), _look(positions), _look(q_out), _look(k_out), backward)
+        found = self._checked.get(key)
+        if found is None:
+            found = self._checked.keep(key, self._check(q, k, positions, q_out, k_out, backward))
+        desc, tq, tk, pos_batch = found
+        if tq is not None:
+            tq = _copy(tq)
+            tq.in_, tq.out = q.data_ptr(), q_out.data_ptr()
+        if tk is not None:
+            tk = _copy(tk)
+            tk.in_, tk.out = k.data_ptr(), k_out.data_ptr()
+        rc = _call(some.get_device(), stream, self._lib.linfusion_rope, desc, tq, tk, positions.data_ptr(), pos_batch)
+        if rc != OK:
+            raise LinFusionError(rc, "linfusion_rope")
+        return q_out, k_out
 
     def forward(self, q, k, positions, q_out=None, k_out=None, stream: Optional[int] = None):
         """(rotated q, rotated k), None where none was given."""
@@ -240,6 +279,7 @@ class BlockNorm:
         self._torch_dtype = _torch_dtype(dtype)
         self._flags = DTYPE_FP16 if dtype == "fp16" else 0
         self._lib = load_library()
+        self._checked = _Checked()
 
     def _desc(self, B, N):
         return NormDesc(B, N, self.C, self.pre, self.post, self.eps, self.residual_scale, self._flags)
@@ -257,57 +297,76 @@ class BlockNorm:
         if tuple(t.shape) != shape:
             raise ValueError(f"{name}: expected {shape}, got {tuple(t.shape)}")
         _check_tensor(t, name, self._torch_dtype, device)
-        return Rows(t.data_ptr(), t.stride(0), t.stride(1))
+        return Rows(None, t.stride(0), t.stride(1))
 
-    def _channels(self, t, name, B, device):
-        if t is None:
-            return (None, 0)
+    def _vector(self, t, name, B, device, per_entry):
+        """Stride of a vector's batch axis."""
         _check_tensor(t, name, self._torch_dtype, device)
         if tuple(t.shape) == (self.C,):
-            return (t.data_ptr(), 0)
-        if tuple(t.shape) == (B, self.C):
+            return 0
+        if per_entry and tuple(t.shape) == (B, self.C):
             # a stride of zero means one vector for all entries; a batch of one needs none of its own
-            return (t.data_ptr(), t.stride(0) if B > 1 else self.C)
-        raise ValueError(f"{name}: expected {(B, self.C)} or {(self.C,)}, got {tuple(t.shape)}")
+            return t.stride(0) if B > 1 else self.C
+        raise ValueError(f"{name}: expected {(B, self.C)} or {(self.C,)}, got {tuple(t.shape)}" if per_entry else
+                         f"{name}: expected {(self.C,)}, got {tuple(t.shape)}")
 
-    def _weight(self, t, name, device):
-        if t is None:
-            return None
-        if tuple(t.shape) != (self.C,):
-            raise ValueError(f"{name}: expected {(self.C,)}, got {tuple(t.shape)}")
-        _check_tensor(t, name, self._torch_dtype, device)
-        return t.data_ptr()
-
-    def _vectors(self, B, device, gate, scale, shift, pre_weight, pre_bias, post_weight, post_bias):
-        return NormVectors(self._channels(gate, "gate", B, device), self._channels(scale, "scale", B, device),
-                           self._channels(shift, "shift", B, device), self._weight(pre_weight, "pre_weight", device),
-                           self._weight(pre_bias, "pre_bias", device), self._weight(post_weight, "post_weight", device),
-                           self._weight(post_bias, "post_bias", device))
+    def _check(self, rows, vectors, shape, device):
+        """Descriptor, row structures and vector strides for tensors whose addresses come with each call."""
+        if len(shape) != 3 or shape[0] == 0 or shape[1] == 0:
+            raise ValueError(f"expected [B, N, C] with at least one row, got {shape}")
+        B = shape[0]
+        out = [self._rows(t, name, shape, device) for name, t in rows]
+        vec = NormVectors()
+        for name, t in vectors:
+            if t is not None:
+                per_entry = name in ("gate", "scale", "shift")
+                stride = self._vector(t, name, B, device, per_entry)
+                if per_entry:
+                    getattr(vec, name).batch = stride
+        return self._desc(B, shape[1]), out, vec
 
     @staticmethod
-    def _shape(t):
-        if t.dim() != 3 or t.shape[0] == 0 or t.shape[1] == 0:
-            raise ValueError(f"expected [B, N, C] with at least one row, got {tuple(t.shape)}")
-        return tuple(t.shape)
+    def _addresses(vec, vectors):
+        vec = _copy(vec)
+        for name, t in vectors:
+            if t is not None:
+                if name in ("gate", "scale", "shift"):
+                    getattr(vec, name).p = t.data_ptr()
+                else:
+                    setattr(vec, name, t.data_ptr())
+        return vec
+
+    @staticmethod
+    def _row_addresses(structs, rows):
+        out = []
+        for struct, (_, t) in zip(structs, rows):
+            if struct is not None:
+                struct = _copy(struct)
+                struct.p = t.data_ptr()
+            out.append(struct)
+        return out
 
     def forward(self, x, a=None, gate=None, scale=None, shift=None, pre_weight=None, pre_bias=None, post_weight=None,
                 post_bias=None, y=None, n=None, stream: Optional[int] = None) -> Tuple:
         """(y, n): the stream after the block (``x`` itself without ``a``) and the next block's input (None
         without ``pre``).  ``y`` may be given as ``x`` or ``a`` (in place)."""
         import torch
-        shape, device = self._shape(x), x.device
-        ref = ctypes.byref
-        vec = self._vectors(shape[0], device, gate, scale, shift, pre_weight, pre_bias, post_weight, post_bias)
         if a is not None and y is None:
-            y = torch.empty(shape, dtype=x.dtype, device=device)
+            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         if self.pre != NORM_NONE and n is None:
-            n = torch.empty(shape, dtype=x.dtype, device=device)
-        rows = [self._rows(t, name, shape, device) for t, name in ((x, "x"), (a, "a"), (y, "y"), (n, "n"))]
-        rx, ra, ry, rn = (None if r is None else ref(r) for r in rows)
-        with _on(device):
-            rc = self._lib.linfusion_block_norm(ref(self._desc(shape[0], shape[1])), rx, ra, ref(vec), ry, rn,
-                                                _stream(device, stream))
-        _check_rc(rc, "linfusion_block_norm")
+            n = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        rows = (("x", x), ("a", a), ("y", y), ("n", n))
+        vectors = (("gate", gate), ("scale", scale), ("shift", shift), ("pre_weight", pre_weight), ("pre_bias", pre_bias),
+                   ("post_weight", post_weight), ("post_bias", post_bias))
+        key = tuple([_look(t) for _, t in rows + vectors])
+        found = self._checked.get(key)
+        if found is None:
+            found = self._checked.keep(key, self._check(rows, vectors, tuple(x.shape), x.device))
+        desc, structs, vec = found
+        rx, ra, ry, rn = self._row_addresses(structs, rows)
+        rc = _call(x.get_device(), stream, self._lib.linfusion_block_norm, desc, rx, ra, self._addresses(vec, vectors), ry, rn)
+        if rc != OK:
+            raise LinFusionError(rc, "linfusion_block_norm")
         return (y if a is not None else x), n
 
     def backward(self, y, a=None, gate=None, scale=None, shift=None, pre_weight=None, pre_bias=None, post_weight=None,
@@ -322,36 +381,41 @@ class BlockNorm:
         some = dn if dn is not None else dy
         if some is None:
             raise ValueError("neither dy nor dn is given")
-        shape, device = self._shape(some), some.device
-        B, ref = shape[0], ctypes.byref
-        vec = self._vectors(B, device, gate, scale, shift, pre_weight, pre_bias, post_weight, post_bias)
+        device = some.device
         if dx is None:
-            dx = torch.empty(shape, dtype=some.dtype, device=device)
+            dx = torch.empty(some.shape, dtype=some.dtype, device=device)
         if a is not None and da is None:
-            da = torch.empty(shape, dtype=some.dtype, device=device)
-        out, grads, ws, ws_bytes = {"x": dx}, None, None, 0
+            da = torch.empty(some.shape, dtype=some.dtype, device=device)
+        rows = (("y", y), ("a", a), ("dy", dy), ("dn", dn), ("dx", dx), ("da", da))
+        vectors = (("gate", gate), ("scale", scale), ("shift", shift), ("pre_weight", pre_weight), ("pre_bias", pre_bias),
+                   ("post_weight", post_weight), ("post_bias", post_bias))
+        key = tuple([_look(t) for _, t in rows + vectors])
+        found = self._checked.get(key)
+        if found is None:
+            desc, structs, vec = self._check(rows, vectors, tuple(some.shape), device)
+            found = self._checked.keep(key, (desc, structs, vec, self.workspace_bytes(some.shape[0], some.shape[1], _sm_count(device.index))))
+        desc, structs, vec, ws_bytes = found
+        out, grads, ws = {"x": dx}, None, None
         if a is not None:
             out["a"] = da
         if need_vectors:
-            given = [(name, t) for name, t in (("gate", gate), ("scale", scale), ("shift", shift), ("pre_weight", pre_weight),
-                                               ("pre_bias", pre_bias), ("post_weight", post_weight), ("post_bias", post_bias))
-                     if t is not None]
-            if given:
-                grads = NormGrads()
-                for name, t in given:
-                    out[name] = torch.empty(t.shape, dtype=torch.float32, device=device)
-                    setattr(grads, name, out[name].data_ptr())
-                if workspace is None:
-                    sms = torch.cuda.get_device_properties(device).multi_processor_count
-                    workspace = torch.empty(self.workspace_bytes(B, shape[1], sms), dtype=torch.uint8, device=device)
-                elif not workspace.is_cuda or workspace.device != device or not workspace.is_contiguous():
-                    raise ValueError("workspace: expected a contiguous CUDA tensor on the device of the others")
-                ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-        rows = [self._rows(t, name, shape, device) for t, name in ((y, "y"), (a, "a"), (dy, "dy"), (dn, "dn"), (dx, "dx"), (da, "da"))]
-        ry, ra, rdy, rdn, rdx, rda = (None if r is None else ref(r) for r in rows)
-        with _on(device):
-            rc = self._lib.linfusion_block_norm_backward(ref(self._desc(B, shape[1])), ry, ra, ref(vec), rdy, rdn, rdx, rda,
-                                                         None if grads is None else ref(grads), ws, ws_bytes,
-                                                         _stream(device, stream))
-        _check_rc(rc, "linfusion_block_norm_backward")
+            # one allocation for the gradients of [C] vectors, one for those of [B, C]
+            grads = NormGrads()
+            for dims in (1, 2):
+                names = [name for name, t in vectors if t is not None and t.dim() == dims]
+                if names:
+                    shape = (len(names), self.C) if dims == 1 else (len(names), some.shape[0], self.C)
+                    for name, t in zip(names, torch.empty(shape, dtype=torch.float32, device=device).unbind(0)):
+                        out[name] = t
+                        setattr(grads, name, t.data_ptr())
+            if workspace is None:
+                workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=device)
+            elif not workspace.is_cuda or workspace.device != device or not workspace.is_contiguous():
+                raise ValueError("workspace: expected a contiguous CUDA tensor on the device of the others")
+            ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        ry, ra, rdy, rdn, rdx, rda = self._row_addresses(structs, rows)
+        rc = _call(some.get_device(), stream, self._lib.linfusion_block_norm_backward, desc, ry, ra, self._addresses(vec, vectors), rdy,
+                   rdn, rdx, rda, grads, ws, ws_bytes if need_vectors else 0)
+        if rc != OK:
+            raise LinFusionError(rc, "linfusion_block_norm_backward")
         return out

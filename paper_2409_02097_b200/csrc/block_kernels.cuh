@@ -784,8 +784,8 @@ __global__ void __launch_bounds__(kNormMaxThreads) block_norm_backward_kernel(co
 
 // Second stage: the column sums in a fixed order, and from them the vectors' gradients.  grid.y = 0 sums over all batch
 // entries (gradients of weights, biases and shared vectors), grid.y = 1 + b over entry b (vectors of its own).  A block takes
-// 32 channels: eight threads of four channels each, 64 slices of the groups; a slice adds its groups in order, the
-// slices are added in a fixed tree.
+// eight channels (one 32-byte sector of each partial: enough blocks for the narrow rows too): two threads of four channels,
+// 128 slices of the groups; a slice adds its groups in order, the slices are added in a fixed tree.
 struct NormGradParams {
     const float* partials;
     int B, C, chunks, groups, want;
@@ -794,7 +794,7 @@ struct NormGradParams {
     int gate_per_batch, scale_per_batch, shift_per_batch;
     float *d_gate, *d_scale, *d_shift, *d_pre_w, *d_pre_b, *d_post_w, *d_post_b;
 };
-constexpr int kNormGradThreads = 512;
+constexpr int kNormGradThreads = 256, kNormGradChannels = 8;
 
 template <int KIND>
 __device__ __forceinline__ float channel(const char* p, int c, float absent)
@@ -807,16 +807,16 @@ __device__ __forceinline__ float channel(const char* p, int c, float absent)
 template <int KIND>
 __global__ void __launch_bounds__(kNormGradThreads) block_norm_grads_kernel(const __grid_constant__ NormGradParams p)
 {
-    constexpr int WARPS = kNormGradThreads / 32, SLICES = kNormGradThreads / 8;
-    __shared__ float s[8][WARPS][32];
-    const int column = threadIdx.x & 7, slice = threadIdx.x / 8, warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-    const int c = blockIdx.x * 32 + column * 4;
+    constexpr int WARPS = kNormGradThreads / 32, SLICES = kNormGradThreads / 2, CH = kNormGradChannels;
+    __shared__ float s[8][WARPS][CH];
+    const int column = threadIdx.x & 1, slice = threadIdx.x / 2, warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    const int c = blockIdx.x * CH + column * 4;
     const bool all = blockIdx.y == 0;
     const int first = all ? 0 : (blockIdx.y - 1) * p.chunks, last = all ? p.groups : first + p.chunks;
     // [0 .. 3]: the column sums; [4 .. 7], over all entries: weighted by 1 + scale (dn, dn h) and by the gate (u e, u)
     float acc[8][4] = {};
     pdl_wait();
-    if (c < p.C) {
+    {
         const bool weighted = all && (p.scale.p != nullptr || p.gate.p != nullptr);
         for (int i = first + slice; i < last; i += SLICES) {
             float4 v[4];
@@ -848,21 +848,21 @@ __global__ void __launch_bounds__(kNormGradThreads) block_norm_grads_kernel(cons
     for (int k = 0; k < 8; ++k)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            acc[k][j] += __shfl_xor_sync(0xffffffffu, acc[k][j], 8);
-            acc[k][j] += __shfl_xor_sync(0xffffffffu, acc[k][j], 16);
-            if (lane < 8) s[k][warp][column * 4 + j] = acc[k][j];
+#pragma unroll
+            for (int o = 2; o < 32; o <<= 1) acc[k][j] += __shfl_xor_sync(0xffffffffu, acc[k][j], o);
+            if (lane < 2) s[k][warp][column * 4 + j] = acc[k][j];
         }
     __syncthreads();
-    if (threadIdx.x < 256) {
-        const int k = threadIdx.x / 32;
+    if (threadIdx.x < 8 * CH) {
+        const int k = threadIdx.x / CH, j = threadIdx.x % CH;
         float v = 0.0f;
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) v += s[k][w][lane];
-        s[k][0][lane] = v;
+        for (int w = 0; w < WARPS; ++w) v += s[k][w][j];
+        s[k][0][j] = v;
     }
     __syncthreads();
-    const int ch = blockIdx.x * 32 + threadIdx.x;
-    if (threadIdx.x >= 32 || ch >= p.C) return;
+    const int ch = blockIdx.x * CH + threadIdx.x;
+    if (threadIdx.x >= CH) return;
     const float dn = s[0][0][lane], dnh = s[1][0][lane], ue = s[2][0][lane], u = s[3][0][lane];
     const float d_scale = channel<KIND>(p.pre_w, ch, 1.0f) * dnh + channel<KIND>(p.pre_b, ch, 0.0f) * dn;
     const float d_gate = channel<KIND>(p.post_w, ch, 1.0f) * ue + channel<KIND>(p.post_b, ch, 0.0f) * u;

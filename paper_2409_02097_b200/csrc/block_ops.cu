@@ -512,7 +512,7 @@ linfusion_status_t linfusion_block_norm_backward(const linfusion_block_norm_desc
     g.d_post_b = grads->post_bias;
     const bool own = (g.d_gate != nullptr && g.gate_per_batch) || (g.d_scale != nullptr && g.scale_per_batch) ||
                      (g.d_shift != nullptr && g.shift_per_batch);
-    const dim3 grid((desc->C + 31) / 32, own ? 1 + desc->B : 1), block(kNormGradThreads);
+    const dim3 grid(desc->C / kNormGradChannels, own ? 1 + desc->B : 1), block(kNormGradThreads);
     e = (desc->flags & LINFUSION_DTYPE_FP16) != 0u
             ? launch_pdl(block_norm_grads_kernel<make_kind(kPhiIdentity, kDtypeFp16)>, grid, block, 0, s, g)
             : launch_pdl(block_norm_grads_kernel<make_kind(kPhiIdentity, kDtypeBf16)>, grid, block, 0, s, g);
