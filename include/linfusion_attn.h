@@ -505,6 +505,11 @@ linfusion_status_t linfusion_attn_backward_kv(const linfusion_attn_desc_t* desc,
  * pass needs of the forward pass.  Errors: INVALID_ARG, CUDA.
  */
 linfusion_status_t linfusion_attn_save_state(linfusion_attn_t* h, float* state, void* cuda_stream);
+/*
+ * Synchronize `cuda_stream` and read the status word of the last backward call that used `workspace`: OK, TIMEOUT if a kernel
+ * gave up on a bounded wait (its outputs are then undefined), or CUDA.
+ */
+linfusion_status_t linfusion_attn_backward_status(const linfusion_attn_desc_t* desc, const void* workspace, void* cuda_stream);
 /* Bytes of workspace for `desc` on a device with `sm_count` SMs (<= 0: 148).  Pure host computation. */
 linfusion_status_t linfusion_attn_backward_workspace_bytes(const linfusion_attn_desc_t* desc, int sm_count, size_t* bytes);
 

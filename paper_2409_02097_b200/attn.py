@@ -32,7 +32,7 @@ EXPORTED = [
     "linfusion_attn_apply_peers", "linfusion_attn_selftest_wait", "linfusion_attn_selftest_counter_wait",
     "linfusion_attn_state_x", "linfusion_attn_apply_x", "linfusion_attn_branch_x", "linfusion_attn_forward_x",
     "linfusion_attn_save_state", "linfusion_attn_backward", "linfusion_attn_backward_state", "linfusion_attn_backward_q",
-    "linfusion_attn_backward_kv", "linfusion_attn_backward_workspace_bytes",
+    "linfusion_attn_backward_kv", "linfusion_attn_backward_status", "linfusion_attn_backward_workspace_bytes",
     "linfusion_attn_checked_build", "linfusion_attn_checked_violations", "linfusion_attn_checked_shrink_y",
 ]
 
@@ -146,6 +146,8 @@ def load_library() -> ctypes.CDLL:
     lib.linfusion_attn_backward_q.argtypes = [ctypes.POINTER(Desc)] + [vp] * 6 + [sz, vp]
     lib.linfusion_attn_backward_kv.restype = st
     lib.linfusion_attn_backward_kv.argtypes = [ctypes.POINTER(Desc)] + [vp] * 6 + [sz, vp]
+    lib.linfusion_attn_backward_status.restype = st
+    lib.linfusion_attn_backward_status.argtypes = [ctypes.POINTER(Desc), vp, vp]
     lib.linfusion_attn_backward_workspace_bytes.restype = st
     lib.linfusion_attn_backward_workspace_bytes.argtypes = [ctypes.POINTER(Desc), st, ctypes.POINTER(sz)]
     lib.linfusion_attn_checked_build.restype = ctypes.c_int32
@@ -568,6 +570,13 @@ class LinFusionAttention:
         if rc != OK:
             raise LinFusionError(rc, "linfusion_attn_backward")
         return dq, dk, dv
+
+    def backward_status(self, workspace, stream: Optional[int] = None) -> int:
+        """Status of the last backward call that was given `workspace`: OK, or ERR_TIMEOUT (synchronizes the stream)."""
+        import torch
+        if stream is None:
+            stream = torch.cuda.current_stream(self.desc.device).cuda_stream
+        return int(self._lib.linfusion_attn_backward_status(ctypes.byref(self.desc), workspace.data_ptr(), stream))
 
     def backward_state(self, k, v, state=None, workspace=None, stream: Optional[int] = None):
         """S | z of the local tokens, for a backward pass that kept none (``sharding``: sum it over devices)."""

@@ -2,7 +2,10 @@
 // the tokens, workspace layout and launches.
 #include "../../include/linfusion_attn.h"
 
+#include <cstdlib>
+
 #include "backward_kernels.cuh"
+#include "backward_tc_kernels.cuh"
 #include "host_util.h"
 
 using namespace lf;
@@ -37,7 +40,10 @@ SlabLayout slab_layout(const linfusion_attn_desc_t& d, int width)
 struct BackwardPlan {
     int slabs, dk, dv, floats;  // floats of S | z of a slab
     int chunks_q, chunks_kv;    // CTAs per slab of the two streams
-    size_t partials_off, state_off, grad_off, total;
+    bool tc;                    // the tcgen05 kernels
+    int tiles_per_slab, ctas, spans;  // ... their tiles of a slab, CTAs, and slabs that a CTA meets at most
+    long long tiles;
+    size_t partials_off, state_off, grad_off, total;  // behind a status word
 };
 
 template <int DK, int DV>
@@ -66,6 +72,23 @@ void plan_chunks(const linfusion_attn_desc_t& d, int sm_count, BackwardPlan* p)
         default: break;                    \
     }
 
+// Where the tcgen05 kernels take over.
+void plan_tc(const linfusion_attn_desc_t& d, int sm_count, BackwardPlan* p)
+{
+    p->tiles_per_slab = (d.N + kTcTile - 1) / kTcTile;
+    p->tiles = static_cast<long long>(p->slabs) * p->tiles_per_slab;
+    p->tc = p->dk <= 64 && p->dv <= 64 && p->tiles_per_slab >= 4 && p->tiles >= 2ll * sm_count;
+    if (const char* force = std::getenv("LF_TC")) p->tc = p->dk <= 64 && p->dv <= 64 && std::atoi(force) != 0;
+    if (!p->tc) return;
+    p->ctas = static_cast<int>(p->tiles < sm_count ? p->tiles : sm_count);
+    p->spans = 1;
+    for (long long g = 0; g < p->ctas; ++g) {
+        const long long b = tc_first_tile(g, p->tiles, p->ctas), e = tc_first_tile(g + 1, p->tiles, p->ctas);
+        const int n = static_cast<int>((e - 1) / p->tiles_per_slab - b / p->tiles_per_slab) + 1;
+        if (n > p->spans) p->spans = n;
+    }
+}
+
 linfusion_status_t make_backward_plan(const linfusion_attn_desc_t* desc, int sm_count, BackwardPlan* p)
 {
     if (desc == nullptr) return LINFUSION_ERR_INVALID_ARG;
@@ -84,17 +107,19 @@ linfusion_status_t make_backward_plan(const linfusion_attn_desc_t* desc, int sm_
 #define LF_CALL(DK, DV) plan_chunks<DK, DV>(d, sm_count, p)
     LF_DISPATCH_WIDTHS(p->dk, p->dv, LF_CALL)
 #undef LF_CALL
-    const size_t state = align_up_256(static_cast<size_t>(p->slabs) * p->floats * sizeof(float));
-    p->state_off = 0;
-    p->grad_off = state;
-    p->partials_off = 2 * state;
-    p->total = 2 * state + state * static_cast<size_t>(p->chunks_q);
+    plan_tc(d, sm_count, p);
+    const size_t slab_state = static_cast<size_t>(p->slabs) * p->floats * sizeof(float), state = align_up_256(slab_state);
+    p->state_off = 256;
+    p->grad_off = p->state_off + state;
+    p->partials_off = p->grad_off + state;
+    p->total = p->partials_off + align_up_256(p->tc ? static_cast<size_t>(p->ctas) * p->spans * BackwardTc::PARTIAL_FLOATS * sizeof(float)
+                                                    : slab_state * static_cast<size_t>(p->chunks_q));
     return LINFUSION_OK;
 }
 
 template <int DK, int DV, int KIND, bool GRAD>
 cudaError_t launch_state(const linfusion_attn_desc_t& d, const BackwardPlan& p, const void* q, const void* dy, const float* state,
-                         void* dq, float* partials, float* out, cudaStream_t s)
+                         void* dq, float* partials, float* out, uint32_t* clear, cudaStream_t s)
 {
     using C = BackwardCfg<DK, DV>;
     static std::atomic<uint64_t> done{0};
@@ -106,7 +131,7 @@ cudaError_t launch_state(const linfusion_attn_desc_t& d, const BackwardPlan& p, 
     e = launch_pdl(backward_state_kernel<DK, DV, KIND, GRAD>, dim3(p.chunks_q, p.slabs), dim3(32 * C::WQ), C::SMEM_Q, s,
                    static_cast<const __nv_bfloat16*>(q), static_cast<const __nv_bfloat16*>(dy), state,
                    static_cast<__nv_bfloat16*>(dq), p.chunks_q == 1 ? out : partials, d.N, p.chunks_q, slab_layout(d, DK),
-                   slab_layout(d, DV), sc);
+                   slab_layout(d, DV), sc, clear);
     if (e != cudaSuccess || p.chunks_q == 1) return e;
     return launch_pdl(backward_reduce_kernel, dim3((p.floats + 255) / 256, p.slabs), dim3(256), 0, s, partials, out, p.floats,
                       p.chunks_q);
@@ -114,7 +139,7 @@ cudaError_t launch_state(const linfusion_attn_desc_t& d, const BackwardPlan& p, 
 
 template <int DK, int DV, int KIND>
 cudaError_t launch_kv(const linfusion_attn_desc_t& d, const BackwardPlan& p, const void* k, const void* v, const float* grad_state,
-                      void* dk, void* dv, cudaStream_t s)
+                      void* dk, void* dv, uint32_t* clear, cudaStream_t s)
 {
     using C = BackwardCfg<DK, DV>;
     static std::atomic<uint64_t> done{0};
@@ -126,7 +151,77 @@ cudaError_t launch_kv(const linfusion_attn_desc_t& d, const BackwardPlan& p, con
     return launch_pdl(backward_kv_kernel<DK, DV, KIND>, dim3(p.chunks_kv, p.slabs), dim3(32 * C::WKV), C::SMEM_KV, s,
                       static_cast<const __nv_bfloat16*>(k), static_cast<const __nv_bfloat16*>(v), grad_state,
                       static_cast<__nv_bfloat16*>(dk), static_cast<__nv_bfloat16*>(dv), d.N, p.chunks_kv, slab_layout(d, DK),
-                      slab_layout(d, DV), sc);
+                      slab_layout(d, DV), sc, clear);
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// A dense tensor of `width` channels as (channel, token, head, batch) -> boxes of 64 channels x `rows` tokens of one
+// slab in the 128-byte swizzle.  What lies past the width or past N is read as zero and not written.
+bool encode_map(CUtensorMap* map, const void* base, const linfusion_attn_desc_t& d, int width, int rows)
+{
+    static std::atomic<EncodeTiledFn> known{nullptr};
+    EncodeTiledFn fn = known.load(std::memory_order_acquire);
+    if (fn == nullptr) {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            return false;
+        fn = reinterpret_cast<EncodeTiledFn>(p);
+        known.store(fn, std::memory_order_release);
+    }
+    const SlabLayout L = slab_layout(d, width);
+    const cuuint64_t dims[4] = {static_cast<cuuint64_t>(width), static_cast<cuuint64_t>(d.N), static_cast<cuuint64_t>(d.H),
+                                static_cast<cuuint64_t>(d.B)};
+    const cuuint64_t strides[3] = {static_cast<cuuint64_t>(L.row_stride) * 2, static_cast<cuuint64_t>(L.head_stride) * 2,
+                                   static_cast<cuuint64_t>(L.batch_stride) * 2};
+    const cuuint32_t box[4] = {64u, static_cast<cuuint32_t>(rows), 1u, 1u}, step[4] = {1u, 1u, 1u, 1u};
+    // Rows of a slab that follow one another: 256 bytes per miss.  Rows between other heads' rows: what the box needs.
+    const CUtensorMapL2promotion promo = (d.flags & LINFUSION_LAYOUT_TOKEN_MAJOR) != 0u ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B
+                                                                                        : CU_TENSOR_MAP_L2_PROMOTION_L2_256B;
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, step,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, promo, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int KIND, bool GRAD>
+cudaError_t launch_tc_state(const linfusion_attn_desc_t& d, const BackwardPlan& p, const void* q, const void* dy, const float* state,
+                            void* dq, float* partials, float* out, uint32_t* status, bool clear, cudaStream_t s)
+{
+    static std::atomic<uint64_t> done{0};
+    cudaError_t e = allow_smem(backward_tc_state_kernel<KIND, GRAD>, BackwardTc::SMEM_BYTES, d.device, &done);
+    if (e != cudaSuccess) return e;
+    CUtensorMap mq, mg, mdq;
+    if (!encode_map(&mq, q, d, p.dk, kTcTile) || !encode_map(&mg, dy, d, p.dv, kTcTile) || !encode_map(&mdq, GRAD ? dq : q, d, p.dk, 32))
+        return cudaErrorInvalidValue;
+    BackwardScales sc;
+    sc.eps = (d.flags & LINFUSION_FLAG_UNNORMALIZED) != 0u ? kEpsUnnormalized : d.eps;
+    sc.scaled = kind_dtype(KIND) == kDtypeFp16 ? 1 : 0;
+    e = launch_pdl(backward_tc_state_kernel<KIND, GRAD>, dim3(p.ctas), dim3(BackwardTc::THREADS), BackwardTc::SMEM_BYTES, s, mq, mg, mdq,
+                   state, partials, status, d.N, p.dk, p.dv, p.tiles_per_slab, p.tiles, p.spans, d.H, sc, clear ? 1 : 0);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(backward_tc_reduce_kernel, dim3((p.floats + 255) / 256, p.slabs), dim3(256), 0, s, partials, out, p.dk, p.dv,
+                      p.tiles_per_slab, p.tiles, p.ctas, p.spans);
+}
+
+template <int KIND>
+cudaError_t launch_tc_kv(const linfusion_attn_desc_t& d, const BackwardPlan& p, const void* k, const void* v, const float* grad_state,
+                         void* dk, void* dv, uint32_t* status, bool clear, cudaStream_t s)
+{
+    static std::atomic<uint64_t> done{0};
+    cudaError_t e = allow_smem(backward_tc_kv_kernel<KIND>, BackwardTc::SMEM_BYTES, d.device, &done);
+    if (e != cudaSuccess) return e;
+    CUtensorMap mk, mv, mdk, mdv;
+    if (!encode_map(&mk, k, d, p.dk, kTcTile) || !encode_map(&mv, v, d, p.dv, kTcTile) || !encode_map(&mdk, dk, d, p.dk, 32) ||
+        !encode_map(&mdv, dv, d, p.dv, 32))
+        return cudaErrorInvalidValue;
+    BackwardScales sc;
+    sc.eps = d.eps;
+    sc.scaled = kind_dtype(KIND) == kDtypeFp16 ? 1 : 0;
+    return launch_pdl(backward_tc_kv_kernel<KIND>, dim3(p.ctas), dim3(BackwardTc::THREADS), BackwardTc::SMEM_BYTES, s, mk, mv, mdk, mdv,
+                      grad_state, status, d.N, p.dk, p.dv, p.tiles_per_slab, p.tiles, d.H, sc, clear ? 1 : 0);
 }
 
 #define LF_DISPATCH_KINDS(kind, CALL) \
@@ -138,13 +233,21 @@ cudaError_t launch_kv(const linfusion_attn_desc_t& d, const BackwardPlan& p, con
         default: break;               \
     }
 
-// grad: Q, dY -> dQ and dS | dz.  Otherwise K, V -> S | z.
+// grad: Q, dY -> dQ and dS | dz.  Otherwise K, V -> S | z.  `first`: of the call's kernels (it clears the status word).
 template <bool GRAD>
 cudaError_t run_state(const linfusion_attn_desc_t& d, const BackwardPlan& p, const void* q, const void* dy, const float* state,
-                      void* dq, float* partials, float* out, cudaStream_t s)
+                      void* dq, unsigned char* ws, float* out, bool first, cudaStream_t s)
 {
     cudaError_t e = cudaErrorInvalidValue;
-#define LF_KIND(KV) e = launch_state<kDK, kDV, KV, GRAD>(d, p, q, dy, state, dq, partials, out, s)
+    uint32_t* status = reinterpret_cast<uint32_t*>(ws);
+    float* partials = reinterpret_cast<float*>(ws + p.partials_off);
+    if (p.tc) {
+#define LF_KIND(KV) e = launch_tc_state<KV, GRAD>(d, p, q, dy, state, dq, partials, out, status, first, s)
+        LF_DISPATCH_KINDS(kernel_kind(d), LF_KIND)
+#undef LF_KIND
+        return e;
+    }
+#define LF_KIND(KV) e = launch_state<kDK, kDV, KV, GRAD>(d, p, q, dy, state, dq, partials, out, first ? status : nullptr, s)
 #define LF_CALL(DKV, DVV)                          \
     {                                              \
         constexpr int kDK = DKV, kDV = DVV;        \
@@ -157,10 +260,17 @@ cudaError_t run_state(const linfusion_attn_desc_t& d, const BackwardPlan& p, con
 }
 
 cudaError_t run_kv(const linfusion_attn_desc_t& d, const BackwardPlan& p, const void* k, const void* v, const float* grad_state,
-                   void* dk, void* dv, cudaStream_t s)
+                   void* dk, void* dv, unsigned char* ws, bool first, cudaStream_t s)
 {
     cudaError_t e = cudaErrorInvalidValue;
-#define LF_KIND(KV) e = launch_kv<kDK, kDV, KV>(d, p, k, v, grad_state, dk, dv, s)
+    uint32_t* status = reinterpret_cast<uint32_t*>(ws);
+    if (p.tc) {
+#define LF_KIND(KV) e = launch_tc_kv<KV>(d, p, k, v, grad_state, dk, dv, status, first, s)
+        LF_DISPATCH_KINDS(kernel_kind(d), LF_KIND)
+#undef LF_KIND
+        return e;
+    }
+#define LF_KIND(KV) e = launch_kv<kDK, kDV, KV>(d, p, k, v, grad_state, dk, dv, first ? status : nullptr, s)
 #define LF_CALL(DKV, DVV)                          \
     {                                              \
         constexpr int kDK = DKV, kDV = DVV;        \
@@ -231,6 +341,23 @@ linfusion_status_t end(cudaError_t e)
 
 extern "C" {
 
+linfusion_status_t linfusion_attn_backward_status(const linfusion_attn_desc_t* desc, const void* workspace, void* cuda_stream)
+{
+    BackwardPlan p;
+    const linfusion_status_t st = make_backward_plan(desc, 0, &p);
+    if (st != LINFUSION_OK) return st;
+    if (workspace == nullptr || !is_aligned(workspace, 256)) return LINFUSION_ERR_INVALID_ARG;
+    CurrentDevice guard(desc->device);
+    if (!guard.ok) return LINFUSION_ERR_CUDA;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    uint32_t word = 0;
+    if (cudaMemcpyAsync(&word, workspace, sizeof(word), cudaMemcpyDeviceToHost, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {
+        cudaGetLastError();
+        return LINFUSION_ERR_CUDA;
+    }
+    return word == kStatusOk ? LINFUSION_OK : LINFUSION_ERR_TIMEOUT;
+}
+
 linfusion_status_t linfusion_attn_backward_workspace_bytes(const linfusion_attn_desc_t* desc, int sm_count, size_t* bytes)
 {
     if (bytes == nullptr) return LINFUSION_ERR_INVALID_ARG;
@@ -273,14 +400,13 @@ linfusion_status_t linfusion_attn_backward(const linfusion_attn_desc_t* desc, co
     if (!guard.ok) return LINFUSION_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     unsigned char* ws = static_cast<unsigned char*>(workspace);
-    float* partials = reinterpret_cast<float*>(ws + c.plan.partials_off);
     float* own_state = reinterpret_cast<float*>(ws + c.plan.state_off);
     float* grad = reinterpret_cast<float*>(ws + c.plan.grad_off);
     cudaError_t e = cudaSuccess;
-    if (state == nullptr) e = run_state<false>(*desc, c.plan, k, v, nullptr, nullptr, partials, own_state, s);
+    if (state == nullptr) e = run_state<false>(*desc, c.plan, k, v, nullptr, nullptr, ws, own_state, true, s);
     if (e == cudaSuccess)
-        e = run_state<true>(*desc, c.plan, q, dy, state != nullptr ? state : own_state, dq, partials, grad, s);
-    if (e == cudaSuccess) e = run_kv(*desc, c.plan, k, v, grad, dk, dv, s);
+        e = run_state<true>(*desc, c.plan, q, dy, state != nullptr ? state : own_state, dq, ws, grad, state != nullptr, s);
+    if (e == cudaSuccess) e = run_kv(*desc, c.plan, k, v, grad, dk, dv, ws, false, s);
     return end(e);
 }
 
@@ -293,8 +419,8 @@ linfusion_status_t linfusion_attn_backward_state(const linfusion_attn_desc_t* de
     if (!spans_ok(spans, 4)) return LINFUSION_ERR_INVALID_ARG;
     CurrentDevice guard(desc->device);
     if (!guard.ok) return LINFUSION_ERR_CUDA;
-    float* partials = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + c.plan.partials_off);
-    return end(run_state<false>(*desc, c.plan, k, v, nullptr, nullptr, partials, state, static_cast<cudaStream_t>(cuda_stream)));
+    unsigned char* ws = static_cast<unsigned char*>(workspace);
+    return end(run_state<false>(*desc, c.plan, k, v, nullptr, nullptr, ws, state, true, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 linfusion_status_t linfusion_attn_backward_q(const linfusion_attn_desc_t* desc, const void* q, const void* dy, const float* state,
@@ -308,8 +434,8 @@ linfusion_status_t linfusion_attn_backward_q(const linfusion_attn_desc_t* desc, 
     if (!spans_ok(spans, 6)) return LINFUSION_ERR_INVALID_ARG;
     CurrentDevice guard(desc->device);
     if (!guard.ok) return LINFUSION_ERR_CUDA;
-    float* partials = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + c.plan.partials_off);
-    return end(run_state<true>(*desc, c.plan, q, dy, state, dq, partials, grad_state, static_cast<cudaStream_t>(cuda_stream)));
+    unsigned char* ws = static_cast<unsigned char*>(workspace);
+    return end(run_state<true>(*desc, c.plan, q, dy, state, dq, ws, grad_state, true, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 linfusion_status_t linfusion_attn_backward_kv(const linfusion_attn_desc_t* desc, const void* k, const void* v,
@@ -323,7 +449,8 @@ linfusion_status_t linfusion_attn_backward_kv(const linfusion_attn_desc_t* desc,
     if (!spans_ok(spans, 6)) return LINFUSION_ERR_INVALID_ARG;
     CurrentDevice guard(desc->device);
     if (!guard.ok) return LINFUSION_ERR_CUDA;
-    return end(run_kv(*desc, c.plan, k, v, grad_state, dk, dv, static_cast<cudaStream_t>(cuda_stream)));
+    return end(run_kv(*desc, c.plan, k, v, grad_state, dk, dv, static_cast<unsigned char*>(workspace), true,
+                      static_cast<cudaStream_t>(cuda_stream)));
 }
 
 }  // extern "C"

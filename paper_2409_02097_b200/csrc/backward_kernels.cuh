@@ -199,7 +199,7 @@ template <int DK, int DV, int KIND, bool GRAD>
 __global__ void __launch_bounds__(32 * BackwardCfg<DK, DV>::WQ)
 backward_state_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* __restrict__ dy, const float* __restrict__ state,
                       __nv_bfloat16* __restrict__ dq, float* __restrict__ partials, int N, int chunks, SlabLayout Lk,
-                      SlabLayout Lv, BackwardScales sc)
+                      SlabLayout Lv, BackwardScales sc, uint32_t* __restrict__ clear_status)
 {
     using C = BackwardCfg<DK, DV>;
     constexpr int TILE = C::TILE, THREADS = 32 * C::WQ, NT = TILE / 8;
@@ -220,6 +220,7 @@ backward_state_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* 
     }
     pdl_launch_dependents();
     pdl_wait();
+    if (clear_status != nullptr && blockIdx.x + blockIdx.y + threadIdx.x == 0) *clear_status = kStatusOk;
     auto fetch = [&](int t) {
         unsigned char* st = smem + (t & 1) * C::STAGE;
         load_tile<DK, C::PITCHK, TILE, THREADS>(st, q, Lk.row_stride, t * TILE, N);
@@ -416,7 +417,7 @@ template <int DK, int DV, int KIND>
 __global__ void __launch_bounds__(32 * BackwardCfg<DK, DV>::WKV)
 backward_kv_kernel(const __nv_bfloat16* __restrict__ k, const __nv_bfloat16* __restrict__ v, const float* __restrict__ grad_state,
                    __nv_bfloat16* __restrict__ dk, __nv_bfloat16* __restrict__ dv, int N, int chunks, SlabLayout Lk,
-                   SlabLayout Lv, BackwardScales sc)
+                   SlabLayout Lv, BackwardScales sc, uint32_t* __restrict__ clear_status)
 {
     using C = BackwardCfg<DK, DV>;
     constexpr int TILE = C::TILE, THREADS = 32 * C::WKV, NT = TILE / 8;
@@ -438,6 +439,7 @@ backward_kv_kernel(const __nv_bfloat16* __restrict__ k, const __nv_bfloat16* __r
     }
     pdl_launch_dependents();
     pdl_wait();
+    if (clear_status != nullptr && blockIdx.x + blockIdx.y + threadIdx.x == 0) *clear_status = kStatusOk;
     auto fetch = [&](int t) {
         unsigned char* st = smem + (t & 1) * C::STAGE;
         load_tile<DK, C::PITCHK, TILE, THREADS>(st, k, Lk.row_stride, t * TILE, N);

@@ -4,6 +4,7 @@
 #pragma once
 
 #include "common.cuh"
+#include "packed_math.cuh"
 
 namespace lf {
 
@@ -264,45 +265,6 @@ struct NormParams {
     float* partials;         // backward: [sums][group][C]
     int want;                // backward: bit k set where column sum k is wanted
 };
-
-// Two fp32 values handled by one instruction (sm_100's packed fp32 arithmetic; each half is rounded as the scalar is).
-typedef unsigned long long f32x2;
-__device__ __forceinline__ f32x2 pack2(float a, float b)
-{
-    f32x2 d;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
-    return d;
-}
-__device__ __forceinline__ f32x2 both(float a) { return pack2(a, a); }
-__device__ __forceinline__ float2 unpack2(f32x2 v)
-{
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-    return r;
-}
-__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
-{
-    f32x2 d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
-{
-    f32x2 d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b)
-{
-    f32x2 d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ float sum2(f32x2 v)
-{
-    const float2 r = unpack2(v);
-    return r.x + r.y;
-}
 
 // Eight channels as four pairs.
 struct P8 {
