@@ -158,9 +158,9 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// A dense tensor of `width` channels as (channel, token, head, batch) -> boxes of 64 channels x `rows` tokens of one
+// A dense tensor of `width` channels as (channel, token, head, batch) -> boxes of 64 channels x a tile's tokens of one
 // slab in the 128-byte swizzle.  What lies past the width or past N is read as zero and not written.
-bool encode_map(CUtensorMap* map, const void* base, const linfusion_attn_desc_t& d, int width, int rows)
+bool encode_map(CUtensorMap* map, const void* base, const linfusion_attn_desc_t& d, int width)
 {
     static std::atomic<EncodeTiledFn> known{nullptr};
     EncodeTiledFn fn = known.load(std::memory_order_acquire);
@@ -178,7 +178,7 @@ bool encode_map(CUtensorMap* map, const void* base, const linfusion_attn_desc_t&
                                 static_cast<cuuint64_t>(d.B)};
     const cuuint64_t strides[3] = {static_cast<cuuint64_t>(L.row_stride) * 2, static_cast<cuuint64_t>(L.head_stride) * 2,
                                    static_cast<cuuint64_t>(L.batch_stride) * 2};
-    const cuuint32_t box[4] = {64u, static_cast<cuuint32_t>(rows), 1u, 1u}, step[4] = {1u, 1u, 1u, 1u};
+    const cuuint32_t box[4] = {64u, kTcTile, 1u, 1u}, step[4] = {1u, 1u, 1u, 1u};
     // Rows of a slab that follow one another: 256 bytes per miss.  Rows between other heads' rows: what the box needs.
     const CUtensorMapL2promotion promo = (d.flags & LINFUSION_LAYOUT_TOKEN_MAJOR) != 0u ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B
                                                                                         : CU_TENSOR_MAP_L2_PROMOTION_L2_256B;
@@ -191,15 +191,15 @@ cudaError_t launch_tc_state(const linfusion_attn_desc_t& d, const BackwardPlan& 
                             void* dq, float* partials, float* out, uint32_t* status, bool clear, cudaStream_t s)
 {
     static std::atomic<uint64_t> done{0};
-    cudaError_t e = allow_smem(backward_tc_state_kernel<KIND, GRAD>, BackwardTc::SMEM_BYTES, d.device, &done);
+    cudaError_t e = allow_smem(backward_tc_state_kernel<KIND, GRAD>, BackwardTc::STATE_SMEM, d.device, &done);
     if (e != cudaSuccess) return e;
     CUtensorMap mq, mg, mdq;
-    if (!encode_map(&mq, q, d, p.dk, kTcTile) || !encode_map(&mg, dy, d, p.dv, kTcTile) || !encode_map(&mdq, GRAD ? dq : q, d, p.dk, 32))
+    if (!encode_map(&mq, q, d, p.dk) || !encode_map(&mg, dy, d, p.dv) || !encode_map(&mdq, GRAD ? dq : q, d, p.dk))
         return cudaErrorInvalidValue;
     BackwardScales sc;
     sc.eps = (d.flags & LINFUSION_FLAG_UNNORMALIZED) != 0u ? kEpsUnnormalized : d.eps;
     sc.scaled = kind_dtype(KIND) == kDtypeFp16 ? 1 : 0;
-    e = launch_pdl(backward_tc_state_kernel<KIND, GRAD>, dim3(p.ctas), dim3(BackwardTc::THREADS), BackwardTc::SMEM_BYTES, s, mq, mg, mdq,
+    e = launch_pdl(backward_tc_state_kernel<KIND, GRAD>, dim3(p.ctas), dim3(BackwardTc::STATE_THREADS), BackwardTc::STATE_SMEM, s, mq, mg, mdq,
                    state, partials, status, d.N, p.dk, p.dv, p.tiles_per_slab, p.tiles, p.spans, d.H, sc, clear ? 1 : 0);
     if (e != cudaSuccess) return e;
     return launch_pdl(backward_tc_reduce_kernel, dim3((p.floats + 255) / 256, p.slabs), dim3(256), 0, s, partials, out, p.dk, p.dv,
@@ -211,16 +211,16 @@ cudaError_t launch_tc_kv(const linfusion_attn_desc_t& d, const BackwardPlan& p, 
                          void* dk, void* dv, uint32_t* status, bool clear, cudaStream_t s)
 {
     static std::atomic<uint64_t> done{0};
-    cudaError_t e = allow_smem(backward_tc_kv_kernel<KIND>, BackwardTc::SMEM_BYTES, d.device, &done);
+    cudaError_t e = allow_smem(backward_tc_kv_kernel<KIND>, BackwardTc::KV_SMEM, d.device, &done);
     if (e != cudaSuccess) return e;
     CUtensorMap mk, mv, mdk, mdv;
-    if (!encode_map(&mk, k, d, p.dk, kTcTile) || !encode_map(&mv, v, d, p.dv, kTcTile) || !encode_map(&mdk, dk, d, p.dk, 32) ||
-        !encode_map(&mdv, dv, d, p.dv, 32))
+    if (!encode_map(&mk, k, d, p.dk) || !encode_map(&mv, v, d, p.dv) || !encode_map(&mdk, dk, d, p.dk) ||
+        !encode_map(&mdv, dv, d, p.dv))
         return cudaErrorInvalidValue;
     BackwardScales sc;
     sc.eps = d.eps;
     sc.scaled = kind_dtype(KIND) == kDtypeFp16 ? 1 : 0;
-    return launch_pdl(backward_tc_kv_kernel<KIND>, dim3(p.ctas), dim3(BackwardTc::THREADS), BackwardTc::SMEM_BYTES, s, mk, mv, mdk, mdv,
+    return launch_pdl(backward_tc_kv_kernel<KIND>, dim3(p.ctas), dim3(BackwardTc::KV_THREADS), BackwardTc::KV_SMEM, s, mk, mv, mdk, mdv,
                       grad_state, status, d.N, p.dk, p.dv, p.tiles_per_slab, p.tiles, d.H, sc, clear ? 1 : 0);
 }
 

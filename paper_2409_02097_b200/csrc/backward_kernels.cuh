@@ -23,6 +23,7 @@
 #pragma once
 
 #include "common.cuh"
+#include "packed_math.cuh"
 
 namespace lf {
 
@@ -62,7 +63,8 @@ template <int KIND>
 __device__ __forceinline__ void split_pair(float a, float b, uint32_t* hi, uint32_t* lo)
 {
     *hi = pack_pair<KIND>(a, b);
-    *lo = pack_pair<KIND>(a - pair_lo<KIND>(*hi), b - pair_hi<KIND>(*hi));
+    const float2 rest = unpack2(fma2(pack2(pair_lo<KIND>(*hi), pair_hi<KIND>(*hi)), both(-1.0f), pack2(a, b)));
+    *lo = pack_pair<KIND>(rest.x, rest.y);
 }
 
 template <int DK, int DV>

@@ -12,13 +12,14 @@
 //
 // A tile is one MMA tile: thread r of a warpgroup owns token r.  It reads its row from the swizzled stage, applies phi, and
 // needs nothing from other threads but the products' rows in tensor memory (its own lane): no shuffles for den, f . t or c.
-// Two warpgroups take turns at the tiles, a warp loads by TMA five tiles ahead (32 KB each), a warp issues the MMAs:
+// Two (pairs of) warpgroups take turns at the tiles, a warp loads by TMA into a ring of five
+// tiles (32 KB each), a warp issues the MMAs, a warp sends gradients out:
 //
 //   state:  T[128 x 64]  = dY S^T             (hi, then lo: 8 steps of K = 16, dY straight from the stage)
 //           D[128 x 64] += [F_hi | F_lo]^T dY (F = w phi(q); head and tail are the two halves of M = 128: 8 steps)
 //   kv:     T[128 x 64]  = V dS^T  (8 steps)   and   T'[128 x 64] = F dS = F_hi dS_hi + F_hi dS_lo + F_lo dS_hi (12)
 //
-// Gradients are written over Q (K, V) in the stage and leave by TMA, 32 rows per warp.  D is added to the fp32 partial
+// Gradients are written over Q (K, V) in the stage and leave by TMA.  D is added to the fp32 partial
 // in global memory every 32 tiles (the tensor core truncates its running sums: chains stay short, and two accumulators
 // take turns).  Each thread keeps the dz of its tokens in 64 columns of its own tensor-memory lane for a slab's run (in
 // registers, beside phi of the row, it made the kernel spill), and the lanes are summed at the end.
@@ -35,18 +36,23 @@ namespace lf {
 
 constexpr int kTcTile = 128, kTcTileBytes = kTcTile * 128;  // one tensor's tile: 16 KB
 struct BackwardTc {
-    static constexpr int GROUPS = 2, CONSUMERS = 128 * GROUPS;
-    static constexpr int PRODUCER_WARP = 4 * GROUPS, MMA_WARP = 4 * GROUPS + 1, THREADS = 32 * (4 * GROUPS + 2);
-    static constexpr int STAGES = 5, STAGE_BYTES = 2 * kTcTileBytes;
+    // kv: two warpgroups, a thread has a token's whole row.  state: two pairs of warpgroups, a thread has half a row (its
+    // chain of phi, two sums and the difference is the longer one: with 8 consumer warps it ran at a third of an instruction
+    // per clock and scheduler and took 511 us where 16 take 3xx, at 40 slabs x 131072).
+    static constexpr int KV_WARPS = 8, KV_THREADS = 32 * (KV_WARPS + 3);
+    static constexpr int STATE_WARPS = 8, STATE_THREADS = 32 * (STATE_WARPS + 3);
+    static constexpr int STAGE_BYTES = 2 * kTcTileBytes;
     static constexpr int F_BYTES = 2 * kTcTileBytes;         // head, tail
+    static constexpr int STATE_F = 1, STATE_STAGES = 5, KV_F = 1, KV_STAGES = 5;
     static constexpr int S_BYTES = 2 * 64 * 128;             // 64 rows of 64 channels: head, tail
     static constexpr int T_BUFFERS = 4, SEGMENT_TILES = 32;
     static constexpr int TMEM_COLS = 512;                    // T: 4 x 64, D: 2 x 64, dz: 2 x 64 (kv: 4 x 128)
     static constexpr int LEAD = 2;                           // tiles by which the first product runs ahead of the second
-    static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + F_BYTES + S_BYTES + 1024 /*align*/ + 2048 /*z, barriers*/;
+    static constexpr int STATE_SMEM = STATE_STAGES * STAGE_BYTES + STATE_F * F_BYTES + S_BYTES + 1024 /*align*/ + 1024 /*z, barriers*/;
+    static constexpr int KV_SMEM = KV_STAGES * STAGE_BYTES + KV_F * F_BYTES + S_BYTES + 1024 /*align*/ + 1024 /*z, barriers*/;
     static constexpr int PARTIAL_FLOATS = 128 * 64 + 8 * 64; // D (head rows, tail rows), then dz of each consumer warp
 };
-static_assert(BackwardTc::SMEM_BYTES <= 227 * 1024, "shared memory");
+static_assert(BackwardTc::STATE_SMEM <= 227 * 1024 && BackwardTc::KV_SMEM <= 227 * 1024, "shared memory");
 
 __host__ __device__ __forceinline__ long long tc_first_tile(long long g, long long W, long long G) { return g * W / G; }
 
@@ -57,7 +63,8 @@ __device__ __forceinline__ uint64_t policy_evict_normal()
     asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
     return p;
 }
-__device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, %0;" ::"n"(BackwardTc::CONSUMERS) : "memory"); }
+template <int WARPS>
+__device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory"); }
 __device__ __forceinline__ uint4 lds16(uint32_t a)
 {
     uint4 v;
@@ -96,13 +103,13 @@ __device__ __forceinline__ void tmem_store_16cols(uint32_t a, const uint32_t (&x
 }
 __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// phi of 64 packed values of a row.
-template <int KIND>
-__device__ __forceinline__ void phi_row(uint32_t tile, int r, float (&f)[64])
+// phi of 8 PIECES packed values of a row, from 16-byte piece `first` on.
+template <int KIND, int PIECES>
+__device__ __forceinline__ void phi_row(uint32_t tile, int r, int first, float (&f)[8 * PIECES])
 {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint4 x = lds16(tile + swizzled(r, j));
+    for (int j = 0; j < PIECES; ++j) {
+        const uint4 x = lds16(tile + swizzled(r, first + j));
         const uint32_t p[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -115,56 +122,55 @@ __device__ __forceinline__ void phi_row(uint32_t tile, int r, float (&f)[64])
 template <int KIND>
 __device__ __forceinline__ float slope_of(float f) { return kind_phi(KIND) == kPhiIdentity ? 1.0f : fminf(f, 1.0f); }
 
-// Largest values over the consumers; `scratch`: 8 floats of shared memory.
+// Largest value over the consumers; `scratch`: a float of shared memory for each warp.
+template <int WARPS>
 __device__ __forceinline__ float consumer_max(float v, float* scratch, int warp, int lane)
 {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
     if (lane == 0) scratch[warp] = v;
-    consumer_sync();
-    for (int i = 0; i < 8; ++i) v = fmaxf(v, scratch[i]);
-    consumer_sync();
+    consumer_sync<WARPS>();
+    for (int i = 0; i < WARPS; ++i) v = fmaxf(v, scratch[i]);
+    consumer_sync<WARPS>();
     return v;
 }
 
 // The consumers lay S (dS) of a slab out as 64 K-major rows of 64 channels, head and tail, and z (dz) as 64 floats; zeros
 // where the widths end.  Returns with the scales of fp16 operands.
-template <int KIND>
+template <int KIND, int WARPS>
 __device__ __forceinline__ void tc_load_state(const float* S, int dk, int dv, uint32_t operand, float* z, float* scratch, int tid,
                                               bool scaled, float eps, float* scale_s, float* scale_w)
 {
-    const int warp = tid / 32, lane = tid & 31, row = tid / 4;
-    float x[16];
+    constexpr int EACH = 4096 / (32 * WARPS), PER_ROW = 64 / EACH;  // floats of a thread, threads of a row
+    const int warp = tid / 32, lane = tid & 31, row = tid / PER_ROW, col0 = (tid % PER_ROW) * EACH;
+    float x[EACH];
 #pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-        const int col = (tid & 3) * 16 + i;
+    for (int i = 0; i < EACH; i += 2) {
         float2 v = make_float2(0.0f, 0.0f);
-        if (row < dk && col < dv) v = *reinterpret_cast<const float2*>(S + row * dv + col);
+        if (row < dk && col0 + i < dv) v = *reinterpret_cast<const float2*>(S + row * dv + col0 + i);
         x[i] = v.x;
         x[i + 1] = v.y;
     }
-    if (tid < 64) z[tid] = tid < dk ? S[dk * dv + tid] : 0.0f;
+    const float zv = tid < dk ? S[dk * dv + tid] : 0.0f;
+    if (tid < 64) z[tid] = zv;
     *scale_s = *scale_w = 1.0f;
     if (scaled) {
-        float big = 0.0f, z_max = 0.0f, z_inv = 0.0f;
+        float big = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) big = fmaxf(big, fabsf(x[i]));
-        if (tid < dk) {
-            const float v = S[dk * dv + tid];
-            z_max = v;
-            z_inv = v > 0.0f ? 1.0f / v : 3.0e38f;
+        for (int i = 0; i < EACH; ++i) big = fmaxf(big, fabsf(x[i]));
+        *scale_s = pow2_scale(consumer_max<WARPS>(big, scratch, warp, lane), 12);
+        if (eps >= 0.0f) {
+            const float z_max = consumer_max<WARPS>(zv, scratch, warp, lane);
+            const float z_inv = consumer_max<WARPS>(tid >= dk ? 0.0f : zv > 0.0f ? 1.0f / zv : 3.0e38f, scratch, warp, lane);
+            *scale_w = fmaxf(pow2_scale(z_inv, 12), 1.0f / pow2_scale(z_max, 4));
         }
-        *scale_s = pow2_scale(consumer_max(big, scratch, warp, lane), 12);
-        z_max = consumer_max(z_max, scratch, warp, lane);
-        z_inv = consumer_max(z_inv, scratch, warp, lane);
-        if (eps >= 0.0f) *scale_w = fmaxf(pow2_scale(z_inv, 12), 1.0f / pow2_scale(z_max, 4));
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < EACH / 8; ++h) {
         uint32_t hi[4], lo[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) split_pair<KIND>(x[8 * h + 2 * i] * *scale_s, x[8 * h + 2 * i + 1] * *scale_s, &hi[i], &lo[i]);
-        const uint32_t at = operand + swizzled(row, (tid & 3) * 2 + h);
+        const uint32_t at = operand + swizzled(row, col0 / 8 + h);
         sts16(at, hi[0], hi[1], hi[2], hi[3]);
         sts16(at + 64 * 128, lo[0], lo[1], lo[2], lo[3]);
     }
@@ -184,34 +190,57 @@ struct TcRun {
 };
 
 // The producer: tiles of two tensors into the ring.
-template <typename C>
+template <int STAGES>
 __device__ __forceinline__ void tc_produce(const CUtensorMap* a, const CUtensorMap* b, unsigned char* ring, uint64_t* full,
                                            uint64_t* empty, const TcRun& run, int H, uint64_t policy, uint32_t* status)
 {
     int issued = 0;
     for (int it = 0; it < run.n; ++it) {
-        const int s = it % C::STAGES;
-        if (it >= C::STAGES && !mbar_wait(&empty[s], ((it / C::STAGES) & 1) ^ 1)) {
+        const int s = it % STAGES;
+        if (it >= STAGES && !mbar_wait(&empty[s], ((it / STAGES) & 1) ^ 1)) {
             tc_expired(status);
             break;
         }
         const int slab = run.slab(it), row = static_cast<int>((run.u0 + it) % run.tiles_per_slab) * kTcTile;
-        unsigned char* dst = ring + s * C::STAGE_BYTES;
-        mbar_expect_tx(&full[s], C::STAGE_BYTES);
+        unsigned char* dst = ring + s * BackwardTc::STAGE_BYTES;
+        mbar_expect_tx(&full[s], BackwardTc::STAGE_BYTES);
         tma_load_4d(dst, a, 0, row, slab % H, slab / H, &full[s], policy);
         tma_load_4d(dst + kTcTileBytes, b, 0, row, slab % H, slab / H, &full[s], policy);
         ++issued;
     }
     // no copy may land in shared memory after the CTA has gone
-    for (int it = issued > C::STAGES ? issued - C::STAGES : 0; it < issued; ++it)
-        if (!mbar_wait(&full[it % C::STAGES], (it / C::STAGES) & 1)) {
+    for (int it = issued > STAGES ? issued - STAGES : 0; it < issued; ++it)
+        if (!mbar_wait(&full[it % STAGES], (it / STAGES) & 1)) {
             tc_expired(status);
             return;
         }
 }
 
+// The storing warp's thread: tiles of gradients leave the ring in order; a stage is handed back as soon as its store has
+// been read (the consumers come back to it only a tile later: too late for the loads to keep DRAM busy).
+template <int STAGES, int TENSORS>
+__device__ __forceinline__ void tc_store(const CUtensorMap* a, const CUtensorMap* b, unsigned char* ring, uint64_t* written, uint64_t* empty,
+                                         const TcRun& run, int H, uint32_t* status)
+{
+    const uint64_t policy = policy_evict_first();
+    for (int it = 0; it < run.n; ++it) {
+        const int s = it % STAGES;
+        if (!mbar_wait(&written[s], (it / STAGES) & 1)) {
+            tc_expired(status);
+            break;
+        }
+        const int slab = run.slab(it), row = static_cast<int>((run.u0 + it) % run.tiles_per_slab) * kTcTile;
+        unsigned char* src = ring + s * BackwardTc::STAGE_BYTES;
+        tma_store_4d(a, src, 0, row, slab % H, slab / H, policy);
+        if (TENSORS == 2) tma_store_4d(b, src + kTcTileBytes, 0, row, slab % H, slab / H, policy);
+        tma_store_wait_read();
+        mbar_arrive(&empty[s]);
+    }
+    tma_store_wait_all();
+}
+
 template <int KIND, bool GRAD>
-__global__ void __launch_bounds__(BackwardTc::THREADS, 1)
+__global__ void __launch_bounds__(BackwardTc::STATE_THREADS, 1)
 backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_g,
                          const __grid_constant__ CUtensorMap tmap_dq, const float* __restrict__ state, float* __restrict__ partials,
                          uint32_t* __restrict__ status, int N, int dk, int dv, int tiles_per_slab, long long W, int spans, int H,
@@ -220,21 +249,22 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
     using C = BackwardTc;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-    unsigned char* F = smem + C::STAGES * C::STAGE_BYTES;
-    unsigned char* So = F + C::F_BYTES;
+    unsigned char* F = smem + C::STATE_STAGES * C::STAGE_BYTES;
+    unsigned char* So = F + C::STATE_F * C::F_BYTES;
     float* z = reinterpret_cast<float*>(So + C::S_BYTES);
     float* scratch = z + 64;
-    uint64_t* full = reinterpret_cast<uint64_t*>(scratch + 8);
-    uint64_t* empty = full + C::STAGES;
-    uint64_t* t_full = empty + C::STAGES;      // [T_BUFFERS]
-    uint64_t* f_full = t_full + C::T_BUFFERS;  // F of a tile is written (4 warps)
-    // [2] ... and has been read (commit), odd and even tiles apart: with one barrier the group that waits for the tile before
+    uint64_t* full = reinterpret_cast<uint64_t*>(scratch + 16);
+    uint64_t* empty = full + C::STATE_STAGES;
+    uint64_t* t_full = empty + C::STATE_STAGES;      // [T_BUFFERS]
+    uint64_t* f_full = t_full + C::T_BUFFERS;  // F of a tile is written
+    // [2] ... and has been read (commit), odd and even tiles apart: with one barrier the pair that waits for the tile before
     // its own could find the phase it wants two behind, which a parity cannot tell from one not yet reached
     uint64_t* f_free = f_full + 1;
     uint64_t* s_ready = f_free + 2;            // a slab's operand is in place (8 warps)
     uint64_t* d_done = s_ready + 1;            // [2] an accumulator is complete (commit)
     uint64_t* d_free = d_done + 2;             // [2] ... and has been read (8 warps)
-    uint64_t* drained = d_free + 2;
+    uint64_t* written = d_free + 2;            // [STATE_STAGES] dQ is in place of Q
+    uint64_t* drained = written + C::STATE_STAGES;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -243,15 +273,16 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
     run.n = static_cast<int>(tc_first_tile(blockIdx.x + 1ll, W, gridDim.x) - run.u0);
     run.tiles_per_slab = tiles_per_slab;
     if (tid == 0) {
-        for (int s = 0; s < C::STAGES; ++s) {
+        for (int s = 0; s < C::STATE_STAGES; ++s) {
             mbar_init(&full[s], 1);
-            mbar_init(&empty[s], GRAD ? 5 : 1);  // the second product's commit; with dQ, its four warps' stores
+            mbar_init(&empty[s], GRAD ? 2 : 1);  // the second product's commit; with dQ, its store
+            mbar_init(&written[s], 4);
         }
         for (int b = 0; b < C::T_BUFFERS; ++b) mbar_init(&t_full[b], 1);
         mbar_init(f_full, 4);
         mbar_init(&f_free[0], 1), mbar_init(&f_free[1], 1);
-        mbar_init(s_ready, 8);
-        for (int b = 0; b < 2; ++b) mbar_init(&d_done[b], 1), mbar_init(&d_free[b], 8);
+        mbar_init(s_ready, C::STATE_WARPS);
+        for (int b = 0; b < 2; ++b) mbar_init(&d_done[b], 1), mbar_init(&d_free[b], C::STATE_WARPS);
         mbar_init(drained, 1);
         mbar_fence_init();
     }
@@ -260,7 +291,7 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = *tmem_slot, tmem_d = tmem + C::T_BUFFERS * 64;
-    if (warp == C::PRODUCER_WARP && lane == 0) {
+    if (warp == C::STATE_WARPS && lane == 0) {
         prefetch_tmap(&tmap_q);
         prefetch_tmap(&tmap_g);
     }
@@ -268,11 +299,13 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
     pdl_wait();
     if (clear_status != 0 && blockIdx.x == 0 && tid == 0) *status = kStatusOk;
 
-    if (warp == C::PRODUCER_WARP) {
+    if (warp == C::STATE_WARPS) {
         // Q and dY are not read again; K and V are, by the kernel after next.
         if (lane == 0)
-            tc_produce<C>(&tmap_q, &tmap_g, smem, full, empty, run, H, GRAD ? policy_evict_first() : policy_evict_normal(), status);
-    } else if (warp == C::MMA_WARP) {
+            tc_produce<C::STATE_STAGES>(&tmap_q, &tmap_g, smem, full, empty, run, H, GRAD ? policy_evict_first() : policy_evict_normal(), status);
+    } else if (warp == C::STATE_WARPS + 2) {
+        if (GRAD && lane == 0) tc_store<C::STATE_STAGES, 1>(&tmap_dq, nullptr, smem, written, empty, run, H, status);
+    } else if (warp == C::STATE_WARPS + 1) {
         if (lane == 0) {
             const uint32_t idesc_t = umma_idesc_f32acc(kind_dtype(KIND), 128, 64);
             const uint32_t idesc_d = umma_idesc_f32acc(kind_dtype(KIND), 128, 64, kUmmaAMnMajor | kUmmaBMnMajor);
@@ -284,13 +317,13 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                 ok = ok && mbar_wait(f_full, j & 1);
                 if (ok) {
                     tc_fence_after_sync();
-                    const uint32_t g_addr = smem_u32(smem + (j % C::STAGES) * C::STAGE_BYTES + kTcTileBytes);
+                    const uint32_t g_addr = smem_u32(smem + (j % C::STATE_STAGES) * C::STAGE_BYTES + kTcTileBytes);
 #pragma unroll
                     for (int k = 0; k < kTcTile / 16; ++k)
                         umma_ss(tmem_d + (seg & 1) * 64, umma_desc_mnmajor_sw128(f_addr + k * 2048, kTcTileBytes, 1024),
                                 umma_desc_mnmajor_sw128(g_addr + k * 2048, 0, 1024), idesc_d, in_seg == 0 && k == 0 ? 0u : 1u);
                     umma_commit(&f_free[j & 1]);
-                    umma_commit(&empty[j % C::STAGES]);
+                    umma_commit(&empty[j % C::STATE_STAGES]);
                 }
                 ++in_seg;
                 if (in_seg == C::SEGMENT_TILES || j + 1 == run.unit_end(j)) {
@@ -308,10 +341,10 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                         ok = ok && mbar_wait(s_ready, unit & 1);
                         ++unit;
                     }
-                    ok = ok && mbar_wait(&full[it % C::STAGES], (it / C::STAGES) & 1);
+                    ok = ok && mbar_wait(&full[it % C::STATE_STAGES], (it / C::STATE_STAGES) & 1);
                     if (!ok) break;
                     tc_fence_after_sync();
-                    const uint32_t g_addr = smem_u32(smem + (it % C::STAGES) * C::STAGE_BYTES + kTcTileBytes);
+                    const uint32_t g_addr = smem_u32(smem + (it % C::STATE_STAGES) * C::STAGE_BYTES + kTcTileBytes);
                     const uint32_t t_at = tmem + (it % C::T_BUFFERS) * 64;
                     // the buffer's last tile is it - 4, whose F the loop below has waited for: its T has been read
 #pragma unroll
@@ -338,25 +371,17 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
         const uint32_t f_at = smem_u32(F), dz_at = tmem_d + 128 + group * 64 + t_lane;
         bool ok = true;  // alike in a warp; a warp that gave up still goes through every barrier of the consumers
         auto wait = [&](uint64_t* bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity)); };
-        int pending = -1;  // stage whose dQ is on its way out
-        auto release = [&]() {
-            if (pending >= 0 && lane == 0) {
-                tma_store_wait_read();
-                mbar_arrive(&empty[pending]);
-            }
-            pending = -1;
-        };
         int seg0 = 0, span = 0;  // segments before this unit
         for (int a = 0; a < run.n;) {
             const int slab = run.slab(a), b = run.unit_end(a);
             float scale_s = 1.0f, scale_w = 1.0f;
             float* partial = partials + (static_cast<size_t>(blockIdx.x) * spans + span) * C::PARTIAL_FLOATS;
             if (GRAD) {
-                consumer_sync();  // everybody is through with the slab before
-                tc_load_state<KIND>(state + static_cast<size_t>(slab) * grad_state_floats(dk, dv), dk, dv, smem_u32(So), z, scratch, tid,
+                consumer_sync<C::STATE_WARPS>();  // everybody is through with the slab before
+                tc_load_state<KIND, C::STATE_WARPS>(state + static_cast<size_t>(slab) * grad_state_floats(dk, dv), dk, dv, smem_u32(So), z, scratch, tid,
                                     sc.scaled != 0, sc.eps, &scale_s, &scale_w);
                 fence_proxy_async_smem();
-                consumer_sync();  // z is there
+                consumer_sync<C::STATE_WARPS>();  // z is there
                 if (lane == 0) mbar_arrive(s_ready);
             }
             const float unscale_t = 1.0f / scale_s, unscale_w = 1.0f / scale_w;
@@ -402,18 +427,17 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
             for (int it = a; it < b; ++it) {
                 if ((it & 1) != group) continue;
                 flush_until((it - a) / C::SEGMENT_TILES);
-                const int s = it % C::STAGES;
+                const int s = it % C::STATE_STAGES;
                 unsigned char* stage = smem + s * C::STAGE_BYTES;
                 const uint32_t q_at = smem_u32(stage);
                 const bool in = static_cast<int>((run.u0 + it) % tiles_per_slab) * kTcTile + r < N;
-                wait(&full[s], (it / C::STAGES) & 1);
+                wait(&full[s], (it / C::STATE_STAGES) & 1);
                 float f[64];
                 float w = in ? 1.0f : 0.0f, c = 0.0f;
                 const uint32_t t_at = tmem + (it % C::T_BUFFERS) * 64 + t_lane;
-                if (ok) phi_row<KIND>(q_at, r, f);
+                if (ok) phi_row<KIND, 8>(q_at, r, 0, f);
                 if (GRAD) {
                     wait(&t_full[it % C::T_BUFFERS], (it / C::T_BUFFERS) & 1);
-                    release();
                     if (ok) {
                         tc_fence_after_sync();
                         if (sc.eps >= 0.0f) {
@@ -434,15 +458,28 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                         }
                     }
                 }
-                if (it > 0) wait(&f_free[(it - 1) & 1], ((it - 1) >> 1) & 1);  // the tile before has left F
+                const f32x2 ws = both(w * scale_w);
+                auto write_f = [&](int j) {  // piece j of the row of F, head and tail
+                    uint32_t hi[4], lo[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 wf = unpack2(mul2(pack2(f[8 * j + 2 * i], f[8 * j + 2 * i + 1]), ws));
+                        split_pair<KIND>(wf.x, wf.y, &hi[i], &lo[i]);
+                    }
+                    sts16(f_at + swizzled(r, j), hi[0], hi[1], hi[2], hi[3]);
+                    sts16(f_at + kTcTileBytes + swizzled(r, j), lo[0], lo[1], lo[2], lo[3]);
+                };
+                // F belongs to one tile at a time, from its first store to the end of the product that reads it.  Writing it in
+                // the pass that writes dQ was the faster with dQ (517 against 537 us), after dz the faster without (304 against 327).
+                if (GRAD && it > 0) wait(&f_free[(it - 1) & 1], ((it - 1) >> 1) & 1);
                 if (ok) {
-                    const f32x2 mc = both(-c), wu = both(w * unscale_t), cz = both(GRAD ? -c * unscale_t * w : w), ws = both(w * scale_w);
+                    const f32x2 mc = both(-c), wu = both(w * unscale_t), cz = both(GRAD ? -c * unscale_t * w : w);
 #pragma unroll
                     for (int h = 0; h < 4; ++h) {
                         uint32_t t[16], dz[16];
                         if (GRAD) tmem_load_2x16cols(t_at + 16 * h, t, dz_at + 16 * h, dz);
                         else tmem_load_16cols(dz_at + 16 * h, dz);
-                        uint32_t hi[8], lo[8], d[8];
+                        uint32_t d[8];
 #pragma unroll
                         for (int i = 0; i < 16; i += 2) {
                             const int ch = 16 * h + i;
@@ -450,8 +487,6 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                             const float2 sum = unpack2(fma2(fp, cz, pack2(__uint_as_float(dz[i]), __uint_as_float(dz[i + 1]))));
                             dz[i] = __float_as_uint(sum.x);
                             dz[i + 1] = __float_as_uint(sum.y);
-                            const float2 wf = unpack2(mul2(fp, ws));
-                            split_pair<KIND>(wf.x, wf.y, &hi[i / 2], &lo[i / 2]);
                             if (GRAD) {
                                 const f32x2 tp = pack2(__uint_as_float(t[i]), __uint_as_float(t[i + 1]));
                                 const f32x2 x = mul2(fma2(*reinterpret_cast<const f32x2*>(z + ch), mc, tp), wu);
@@ -460,30 +495,30 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                             }
                         }
                         tmem_store_16cols(dz_at + 16 * h, dz);
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const uint32_t at = swizzled(r, 2 * h + e);
-                            sts16(f_at + at, hi[4 * e], hi[4 * e + 1], hi[4 * e + 2], hi[4 * e + 3]);
-                            sts16(f_at + kTcTileBytes + at, lo[4 * e], lo[4 * e + 1], lo[4 * e + 2], lo[4 * e + 3]);
-                            if (GRAD) sts16(q_at + at, d[4 * e], d[4 * e + 1], d[4 * e + 2], d[4 * e + 3]);
+                        if (GRAD) {
+                            sts16(q_at + swizzled(r, 2 * h), d[0], d[1], d[2], d[3]);
+                            sts16(q_at + swizzled(r, 2 * h + 1), d[4], d[5], d[6], d[7]);
+                            write_f(2 * h);
+                            write_f(2 * h + 1);
                         }
                     }
                     tmem_store_wait();
+                }
+                if (!GRAD) {
+                    if (it > 0) wait(&f_free[(it - 1) & 1], ((it - 1) >> 1) & 1);
+                    if (ok) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) write_f(j);
+                    }
                 }
                 tc_fence_before_sync();
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
                     mbar_arrive(f_full);
-                    if (GRAD && ok) {
-                        const int row = static_cast<int>((run.u0 + it) % tiles_per_slab) * kTcTile + (warp & 3) * 32;
-                        if (row < N)
-                            tma_store_4d(&tmap_dq, stage + (warp & 3) * 32 * 128, 0, row, slab % H, slab / H, policy_evict_first());
-                    }
+                    if (GRAD) mbar_arrive(&written[s]);
                 }
-                if (GRAD) pending = s;
             }
-            release();
             flush_until(segs);
             seg0 += segs;
             // dz of the thread's tokens -> sums over the warp: 64 values are halved with the lanes, two are left in each
@@ -512,44 +547,59 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
             a = b;
         }
         if (!ok && lane == 0) tc_expired(status);
-        if (lane == 0) tma_store_wait_all();
     }
     __syncthreads();
     if (warp == 0) tmem_dealloc(tmem, C::TMEM_COLS);
 }
 
 // Sum of a slab's partials, in the order of the CTAs that worked on it: out[slab] = S | z (dS | dz).
+constexpr int kTcReduceAtOnce = 32;
 static __global__ void __launch_bounds__(256)
 backward_tc_reduce_kernel(const float* __restrict__ partials, float* __restrict__ out, int dk, int dv, int tiles_per_slab, long long W,
                           int G, int spans)
 {
+    __shared__ long long where[kTcReduceAtOnce];  // of a contributing CTA's partial; -1: none
+    const int slab = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x, floats = grad_state_floats(dk, dv);
+    const long long first = static_cast<long long>(slab) * tiles_per_slab, last = first + tiles_per_slab;
+    // the CTA that holds the slab's first tile: the largest g with g W / G <= first
+    const int g0 = static_cast<int>(((first + 1) * G - 1) / W), g1 = static_cast<int>((last * G - 1) / W);
+    const int row = i / dv, col = i - row * dv;
+    const bool of_z = i >= dk * dv;
     pdl_launch_dependents();
     pdl_wait();
-    const int slab = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x, floats = grad_state_floats(dk, dv);
-    if (i >= floats) return;
-    const long long first = static_cast<long long>(slab) * tiles_per_slab, last = first + tiles_per_slab;
-    // the CTA that holds tile t: the largest g with g W / G <= t
-    int g = static_cast<int>(((first + 1) * G - 1) / W);
     float sum = 0.0f;
-    for (; g < G && tc_first_tile(g, W, G) < last; ++g) {
-        const long long u0 = tc_first_tile(g, W, G);
-        if (tc_first_tile(g + 1, W, G) <= first || tc_first_tile(g + 1, W, G) == u0) continue;
-        const float* p = partials + (static_cast<size_t>(g) * spans + (slab - static_cast<int>(u0 / tiles_per_slab))) * BackwardTc::PARTIAL_FLOATS;
-        if (i < dk * dv) {
-            const int row = i / dv, col = i - row * dv;
-            sum += p[row * 64 + col] + p[(64 + row) * 64 + col];
-        } else {
-            float s = 0.0f;
+    for (int at = g0; at <= g1; at += kTcReduceAtOnce) {
+        const int n = min(kTcReduceAtOnce, g1 + 1 - at);
+        __syncthreads();
+        if (threadIdx.x < n) {
+            const int g = at + threadIdx.x;
+            const long long u0 = tc_first_tile(g, W, G), u1 = tc_first_tile(g + 1, W, G);
+            where[threadIdx.x] = u1 > u0 && u1 > first && u0 < last
+                                     ? (static_cast<long long>(g) * spans + (slab - static_cast<int>(u0 / tiles_per_slab))) * BackwardTc::PARTIAL_FLOATS
+                                     : -1;
+        }
+        __syncthreads();
+        if (i < floats) {
+#pragma unroll 4
+            for (int k = 0; k < n; ++k) {
+                if (where[k] < 0) continue;
+                const float* p = partials + where[k];
+                if (!of_z) {
+                    sum += p[row * 64 + col] + p[(64 + row) * 64 + col];
+                } else {
+                    float x[8];
 #pragma unroll
-            for (int w = 0; w < 8; ++w) s += p[128 * 64 + w * 64 + i - dk * dv];
-            sum += s;
+                    for (int w = 0; w < 8; ++w) x[w] = p[128 * 64 + w * 64 + i - dk * dv];
+                    sum += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+                }
+            }
         }
     }
-    out[static_cast<size_t>(slab) * floats + i] = sum;
+    if (i < floats) out[static_cast<size_t>(slab) * floats + i] = sum;
 }
 
 template <int KIND>
-__global__ void __launch_bounds__(BackwardTc::THREADS, 1)
+__global__ void __launch_bounds__(BackwardTc::KV_THREADS, 1)
 backward_tc_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                       const __grid_constant__ CUtensorMap tmap_dk, const __grid_constant__ CUtensorMap tmap_dv,
                       const float* __restrict__ grad_state, uint32_t* __restrict__ status, int N, int dk, int dv, int tiles_per_slab,
@@ -558,18 +608,21 @@ backward_tc_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
     using C = BackwardTc;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-    unsigned char* F = smem + C::STAGES * C::STAGE_BYTES;
+    unsigned char* F = smem + C::KV_STAGES * C::STAGE_BYTES;
     unsigned char* So = F + C::F_BYTES;
     float* z = reinterpret_cast<float*>(So + C::S_BYTES);
     float* scratch = z + 64;
-    uint64_t* full = reinterpret_cast<uint64_t*>(scratch + 8);
-    uint64_t* empty = full + C::STAGES;
-    uint64_t* t_full = empty + C::STAGES;      // [T_BUFFERS] both products of a tile are complete (commit)
+    uint64_t* full = reinterpret_cast<uint64_t*>(scratch + 16);
+    uint64_t* empty = full + C::KV_STAGES;
+    uint64_t* t_full = empty + C::KV_STAGES;      // [T_BUFFERS] both products of a tile are complete (commit)
     uint64_t* t_free = t_full + C::T_BUFFERS;  // [T_BUFFERS] ... and have been read (4 warps)
     uint64_t* f_full = t_free + C::T_BUFFERS;
-    uint64_t* f_free = f_full + 1;  // [2]
+    // [2] for odd and even tiles: with one barrier the group that waits for the tile before its own could find the phase it
+    // wants two behind, which a parity cannot tell from one not yet reached
+    uint64_t* f_free = f_full + 1;
     uint64_t* s_ready = f_free + 2;
-    uint64_t* drained = s_ready + 1;
+    uint64_t* written = s_ready + 1;  // [KV_STAGES] dK and dV are in place of K and V (4 warps)
+    uint64_t* drained = written + C::KV_STAGES;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -578,14 +631,15 @@ backward_tc_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
     run.n = static_cast<int>(tc_first_tile(blockIdx.x + 1ll, W, gridDim.x) - run.u0);
     run.tiles_per_slab = tiles_per_slab;
     if (tid == 0) {
-        for (int s = 0; s < C::STAGES; ++s) {
+        for (int s = 0; s < C::KV_STAGES; ++s) {
             mbar_init(&full[s], 1);
-            mbar_init(&empty[s], 4);  // the stores of the tile's four warps
+            mbar_init(&empty[s], 1);  // the tile's stores
+            mbar_init(&written[s], 4);
         }
         for (int b = 0; b < C::T_BUFFERS; ++b) mbar_init(&t_full[b], 1), mbar_init(&t_free[b], 4);
         mbar_init(f_full, 4);
         mbar_init(&f_free[0], 1), mbar_init(&f_free[1], 1);
-        mbar_init(s_ready, 8);
+        mbar_init(s_ready, C::KV_WARPS);
         mbar_init(drained, 1);
         mbar_fence_init();
     }
@@ -594,7 +648,7 @@ backward_tc_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = *tmem_slot;
-    if (warp == C::PRODUCER_WARP && lane == 0) {
+    if (warp == C::KV_WARPS && lane == 0) {
         prefetch_tmap(&tmap_k);
         prefetch_tmap(&tmap_v);
     }
@@ -602,9 +656,11 @@ backward_tc_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
     pdl_wait();
     if (clear_status != 0 && blockIdx.x == 0 && tid == 0) *status = kStatusOk;
 
-    if (warp == C::PRODUCER_WARP) {
-        if (lane == 0) tc_produce<C>(&tmap_k, &tmap_v, smem, full, empty, run, H, policy_evict_first(), status);
-    } else if (warp == C::MMA_WARP) {
+    if (warp == C::KV_WARPS) {
+        if (lane == 0) tc_produce<C::KV_STAGES>(&tmap_k, &tmap_v, smem, full, empty, run, H, policy_evict_first(), status);
+    } else if (warp == C::KV_WARPS + 2) {
+        if (lane == 0) tc_store<C::KV_STAGES, 2>(&tmap_dk, &tmap_dv, smem, written, empty, run, H, status);
+    } else if (warp == C::KV_WARPS + 1) {
         if (lane == 0) {
             const uint32_t idesc_k = umma_idesc_f32acc(kind_dtype(KIND), 128, 64);
             const uint32_t idesc_v = umma_idesc_f32acc(kind_dtype(KIND), 128, 64, kUmmaBMnMajor);
@@ -635,10 +691,10 @@ backward_tc_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
                     ++unit;
                 }
                 if (it >= C::T_BUFFERS) ok = ok && mbar_wait(&t_free[it % C::T_BUFFERS], ((it / C::T_BUFFERS) & 1) ^ 1);
-                ok = ok && mbar_wait(&full[it % C::STAGES], (it / C::STAGES) & 1);
+                ok = ok && mbar_wait(&full[it % C::KV_STAGES], (it / C::KV_STAGES) & 1);
                 if (!ok) break;
                 tc_fence_after_sync();
-                const uint32_t v_addr = smem_u32(smem + (it % C::STAGES) * C::STAGE_BYTES + kTcTileBytes);
+                const uint32_t v_addr = smem_u32(smem + (it % C::KV_STAGES) * C::STAGE_BYTES + kTcTileBytes);
 #pragma unroll
                 for (int h = 1; h >= 0; --h)
 #pragma unroll
@@ -658,33 +714,24 @@ backward_tc_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
         const uint32_t f_at = smem_u32(F);
         bool ok = true;
         auto wait = [&](uint64_t* bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity)); };
-        int pending = -1;
-        auto release = [&]() {
-            if (pending >= 0 && lane == 0) {
-                tma_store_wait_read();
-                mbar_arrive(&empty[pending]);
-            }
-            pending = -1;
-        };
         for (int a = 0; a < run.n;) {
             const int slab = run.slab(a), b = run.unit_end(a);
             float scale_s, unused;
-            consumer_sync();
-            tc_load_state<KIND>(grad_state + static_cast<size_t>(slab) * grad_state_floats(dk, dv), dk, dv, smem_u32(So), z, scratch, tid,
+            consumer_sync<C::KV_WARPS>();
+            tc_load_state<KIND, C::KV_WARPS>(grad_state + static_cast<size_t>(slab) * grad_state_floats(dk, dv), dk, dv, smem_u32(So), z, scratch, tid,
                                 sc.scaled != 0, -1.0f, &scale_s, &unused);
             fence_proxy_async_smem();
-            consumer_sync();
+            consumer_sync<C::KV_WARPS>();
             if (lane == 0) mbar_arrive(s_ready);
             const f32x2 unscale = both(1.0f / scale_s);
             for (int it = a; it < b; ++it) {
                 if ((it & 1) != group) continue;
-                const int s = it % C::STAGES;
+                const int s = it % C::KV_STAGES;
                 unsigned char* stage = smem + s * C::STAGE_BYTES;
                 const uint32_t k_at = smem_u32(stage), v_at = k_at + kTcTileBytes;
-                wait(&full[s], (it / C::STAGES) & 1);
+                wait(&full[s], (it / C::KV_STAGES) & 1);
                 float f[64];
-                if (ok) phi_row<KIND>(k_at, r, f);
-                release();
+                if (ok) phi_row<KIND, 8>(k_at, r, 0, f);
                 if (it > 0) wait(&f_free[(it - 1) & 1], ((it - 1) >> 1) & 1);
                 if (ok) {
 #pragma unroll
@@ -730,19 +777,12 @@ backward_tc_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
                 __syncwarp();
                 if (lane == 0) {
                     mbar_arrive(&t_free[it % C::T_BUFFERS]);
-                    const int row = static_cast<int>((run.u0 + it) % tiles_per_slab) * kTcTile + (warp & 3) * 32;
-                    if (ok && row < N) {
-                        tma_store_4d(&tmap_dk, stage + (warp & 3) * 32 * 128, 0, row, slab % H, slab / H, policy_evict_first());
-                        tma_store_4d(&tmap_dv, stage + kTcTileBytes + (warp & 3) * 32 * 128, 0, row, slab % H, slab / H, policy_evict_first());
-                    }
+                    mbar_arrive(&written[s]);
                 }
-                pending = s;
             }
-            release();
             a = b;
         }
         if (!ok && lane == 0) tc_expired(status);
-        if (lane == 0) tma_store_wait_all();
     }
     __syncthreads();
     if (warp == 0) tmem_dealloc(tmem, C::TMEM_COLS);
