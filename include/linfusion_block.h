@@ -70,7 +70,7 @@ typedef struct {
  * coordinates of token n of batch b at positions + b * pos_batch_stride + n * n_axes;
  * pos_batch_stride 0 shares them over the batch.  Coordinates need not be whole (interpolated
  * positions).  The angle is formed from a frequency held in two fp32 parts and reduced to one turn
- * before the sine and cosine, so it is good to about 3e-7 wherever the position itself is exact.
+ * before the sine and cosine, so it is good to about 3e-7 for coordinates below 2^24 in size.
  * Errors: INVALID_ARG (null / misaligned pointers, bad sizes or strides, both tensors absent),
  * UNSUPPORTED (unknown flags, d > 256), CUDA.
  */

@@ -536,7 +536,7 @@ class LinFusionAttention:
                 if like == "state":
                     t = torch.empty(self.state_floats(), dtype=torch.float32, device=device)
                 else:
-                    t = torch.empty(self.shape_qk if like in ("q", "k") else self.shape, dtype=tensors[0][0].dtype, device=device)
+                    t = torch.empty_like(next(x for x, _, kind in tensors if (kind == "v") == (like == "v")))
             elif like == "state":
                 self._check_state(t, name, device)
             else:

@@ -137,6 +137,12 @@ class _Checked(dict):
         return value
 
 
+def _like(t):
+    """An uninitialised contiguous tensor of t's shape, type and device."""
+    import torch
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 def _copy(struct):
     """A structure of the caller's own (calls of several threads share the checked one)."""
     return type(struct).from_buffer_copy(struct)
@@ -219,7 +225,6 @@ class AxialRope:
         return RopeDesc(B, N, self.d, axes, self._padded, self.interleaved, backward, self.theta, self._flags), tq, tk, pos_batch
 
     def _run(self, q, k, positions, q_out, k_out, backward, stream):
-        import torch
         some = q if q is not None else k
         if some is None:
             raise ValueError("neither q nor k is given")
@@ -228,11 +233,11 @@ class AxialRope:
         if q is None:
             q_out = None
         elif q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out = _like(q)
         if k is None:
             k_out = None
         elif k_out is None:
-            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+            k_out = _like(k)
         key = (_look(q), _look(k), _look(positions), _look(q_out), _look(k_out), backward)
         found = self._checked.get(key)
         if found is None:
@@ -350,11 +355,10 @@ class BlockNorm:
                 post_bias=None, y=None, n=None, stream: Optional[int] = None) -> Tuple:
         """(y, n): the stream after the block (``x`` itself without ``a``) and the next block's input (None
         without ``pre``).  ``y`` may be given as ``x`` or ``a`` (in place)."""
-        import torch
         if a is not None and y is None:
-            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            y = _like(x)
         if self.pre != NORM_NONE and n is None:
-            n = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            n = _like(x)
         rows = (("x", x), ("a", a), ("y", y), ("n", n))
         vectors = (("gate", gate), ("scale", scale), ("shift", shift), ("pre_weight", pre_weight), ("pre_bias", pre_bias),
                    ("post_weight", post_weight), ("post_bias", post_bias))
@@ -383,9 +387,9 @@ class BlockNorm:
             raise ValueError("neither dy nor dn is given")
         device = some.device
         if dx is None:
-            dx = torch.empty(some.shape, dtype=some.dtype, device=device)
+            dx = _like(some)
         if a is not None and da is None:
-            da = torch.empty(some.shape, dtype=some.dtype, device=device)
+            da = _like(some)
         rows = (("y", y), ("a", a), ("dy", dy), ("dn", dn), ("dx", dx), ("da", da))
         vectors = (("gate", gate), ("scale", scale), ("shift", shift), ("pre_weight", pre_weight), ("pre_bias", pre_bias),
                    ("post_weight", post_weight), ("post_bias", post_bias))

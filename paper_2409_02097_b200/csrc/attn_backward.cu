@@ -36,6 +36,8 @@ SlabLayout slab_layout(const linfusion_attn_desc_t& d, int width)
     return L;
 }
 
+constexpr int kPlanSms = 148;  // a B200's, where no count is given
+
 // What follows from (descriptor, SM count) alone.
 struct BackwardPlan {
     int slabs, dk, dv, floats;  // floats of S | z of a slab
@@ -81,12 +83,9 @@ void plan_tc(const linfusion_attn_desc_t& d, int sm_count, BackwardPlan* p)
     if (const char* force = std::getenv("LF_TC")) p->tc = p->dk <= 64 && p->dv <= 64 && std::atoi(force) != 0;
     if (!p->tc) return;
     p->ctas = static_cast<int>(p->tiles < sm_count ? p->tiles : sm_count);
-    p->spans = 1;
-    for (long long g = 0; g < p->ctas; ++g) {
-        const long long b = tc_first_tile(g, p->tiles, p->ctas), e = tc_first_tile(g + 1, p->tiles, p->ctas);
-        const int n = static_cast<int>((e - 1) / p->tiles_per_slab - b / p->tiles_per_slab) + 1;
-        if (n > p->spans) p->spans = n;
-    }
+    // a run of L tiles meets at most this many slabs
+    const long long L = (p->tiles + p->ctas - 1) / p->ctas;
+    p->spans = static_cast<int>((L + p->tiles_per_slab - 2) / p->tiles_per_slab) + 1;
 }
 
 linfusion_status_t make_backward_plan(const linfusion_attn_desc_t* desc, int sm_count, BackwardPlan* p)
@@ -99,7 +98,7 @@ linfusion_status_t make_backward_plan(const linfusion_attn_desc_t* desc, int sm_
     size_t unused = 0;
     const linfusion_status_t st = linfusion_attn_workspace_bytes(&d, sm_count, &unused);
     if (st != LINFUSION_OK) return st;
-    if (sm_count <= 0) sm_count = 148;
+    if (sm_count <= 0) sm_count = kPlanSms;
     p->slabs = d.B * d.H;
     p->dk = feature_width(d);
     p->dv = d.d;
@@ -320,7 +319,7 @@ Call begin(const linfusion_attn_desc_t* desc, const void* workspace, size_t work
     if (sms == -2) c.st = LINFUSION_ERR_UNSUPPORTED;
     if (sms == -1) c.st = LINFUSION_ERR_CUDA;
     if (sms < 0) return c;
-    c.st = make_backward_plan(desc, sms, &c.plan);
+    if (sms != kPlanSms) c.st = make_backward_plan(desc, sms, &c.plan);
     if (c.st != LINFUSION_OK) return c;
     if (workspace_bytes < c.plan.total) c.st = LINFUSION_ERR_ALLOC;
     const size_t rows = static_cast<size_t>(c.plan.slabs) * desc->N;

@@ -73,87 +73,105 @@ struct RopeParams {
     unsigned char axis[kRopeMaxPairs];
 };
 
+// Sine and cosine of r turns: the nearest quarter turn q is taken off exactly, the rest is at most 1/8 turn (pi / 4), where
+// the Taylor series to x^9 and x^10 are off by 2e-9 and 1e-10; then q swaps and signs them.  About thirty instructions,
+// where sincospif, inlined for every channel, was most of the kernel's work (21 against 10 us where each is used for eight
+// heads).
 __device__ __forceinline__ void rope_sincos(float pos, float hi, float lo, float sign, float* s, float* c)
 {
     const float p = pos * hi;
     const float e = fmaf(pos, hi, -p);
     const float r = (p - rintf(p)) + fmaf(pos, lo, e);
-    sincospif(2.0f * r, s, c);
-    *s *= sign;
+    const float q = rintf(4.0f * r);
+    const float x = 6.2831853071795865f * fmaf(-0.25f, q, r), x2 = x * x;
+    float u = fmaf(x2, 1.0f / 362880.0f, -1.0f / 5040.0f);
+    u = fmaf(x2, u, 1.0f / 120.0f);
+    u = fmaf(x2, u, -1.0f / 6.0f);
+    u = fmaf(x2 * x, u, x);
+    float v = fmaf(x2, -1.0f / 3628800.0f, 1.0f / 40320.0f);
+    v = fmaf(x2, v, -1.0f / 720.0f);
+    v = fmaf(x2, v, 1.0f / 24.0f);
+    v = fmaf(x2, v, -0.5f);
+    v = fmaf(x2, v, 1.0f);
+    const int k = static_cast<int>(q);
+    const float a = k & 1 ? v : u, b = k & 1 ? u : v;
+    *s = (k & 2 ? -a : a) * sign;
+    *c = (k + 1) & 2 ? -b : b;
 }
 
-// Eight 16-bit values at an address that is aligned to W elements only: pieces of W, those that begin before
-// element `end` (counted from the address).
+constexpr int kRopeUnroll = 4;
+
+// Eight channels in pieces of W, each at its own address.
 template <int W>
-__device__ __forceinline__ uint4 load_pieces(const char* p, int end)
+__device__ __forceinline__ uint4 gather_pieces(const char* const (&p)[8 / W], long long ahead)
 {
-    if (W == 8) return load16(p);
     uint32_t r[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int i = 0; i < 8; i += W) {
-        if (i >= end) break;
-        if (W == 4) asm volatile("ld.global.v2.u32 {%0,%1}, [%2];" : "=r"(r[i / 2]), "=r"(r[i / 2 + 1]) : "l"(p + 2 * i) : "memory");
-        if (W == 2) asm volatile("ld.global.u32 %0, [%1];" : "=r"(r[i / 2]) : "l"(p + 2 * i) : "memory");
+    for (int i = 0; i < 8 / W; ++i) {
+        if (W == 4) asm volatile("ld.global.v2.u32 {%0,%1}, [%2];" : "=r"(r[2 * i % 4]), "=r"(r[(2 * i + 1) % 4]) : "l"(p[i] + ahead) : "memory");
+        if (W == 2) asm volatile("ld.global.u32 %0, [%1];" : "=r"(r[i % 4]) : "l"(p[i] + ahead) : "memory");
         if (W == 1) {
             unsigned short h;
-            asm volatile("ld.global.u16 %0, [%1];" : "=h"(h) : "l"(p + 2 * i) : "memory");
+            asm volatile("ld.global.u16 %0, [%1];" : "=h"(h) : "l"(p[i] + ahead) : "memory");
             r[i / 2] |= static_cast<uint32_t>(h) << (16 * (i & 1));
         }
     }
     return make_uint4(r[0], r[1], r[2], r[3]);
 }
-template <int W>
-__device__ __forceinline__ void store_pieces(char* p, const uint4& v, int end)
-{
-    if (W == 8) {
-        store16(p, v);
-        return;
-    }
-    const uint32_t r[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 8; i += W) {
-        if (i >= end) break;
-        if (W == 4) asm volatile("st.global.v2.u32 [%0], {%1,%2};" ::"l"(p + 2 * i), "r"(r[i / 2]), "r"(r[i / 2 + 1]) : "memory");
-        if (W == 2) asm volatile("st.global.u32 [%0], %1;" ::"l"(p + 2 * i), "r"(r[i / 2]) : "memory");
-        if (W == 1)
-            asm volatile("st.global.u16 [%0], %1;" ::"l"(p + 2 * i), "h"(static_cast<unsigned short>(r[i / 2] >> (16 * (i & 1)))) : "memory");
-    }
-}
 
-constexpr int kRopeUnroll = 4;
+// PAIRS:
+//   kRopeInterleaved   a thread turns the four pairs of its eight channels
+//   kRopeHalves        P is a multiple of 8: a thread turns eight pairs, both sides in whole 16-byte pieces
+//   W = 4, 2, 1        P is a multiple of W only: a thread makes one 16-byte piece of the output, whatever roles its
+//                      channels have, from its own channels and their partners, P further or P back, which it gathers in pieces
+//                      of W elements (they lie in lines that its neighbours fetch).  Stores stay whole; no warp splits into
+//                      first, second and copied channels, which cost 26 us where this takes xx (B = 3, N = 2531, 16 heads of 80,
+//                      P = 30).  In place, the block's threads load before any of them stores: it holds whole rows.
+constexpr int kRopeInterleaved = 16, kRopeHalves = 8;
 
-// W: alignment in elements of channel P, where the second halves of the pairs begin (8 where P is a multiple of
-// 8: whole 16-byte pieces); INTERLEAVED needs none.  Pieces of 4, 2 or 1 keep the same sectors in use and
-// cost load and store instructions only.
-template <int KIND, bool INTERLEAVED, int W>
-__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constant__ RopeParams p)
+template <int KIND, int PAIRS>
+__global__ void __launch_bounds__(kRopeThreads, 4) rope_kernel(const __grid_constant__ RopeParams p)
 {
     // The frequencies are indexed per thread: from shared memory, where lanes with different pairs do not take turns.
     __shared__ float s_hi[kRopeMaxPairs], s_lo[kRopeMaxPairs];
     __shared__ unsigned char s_axis[kRopeMaxPairs];
-    if (threadIdx.x < kRopeMaxPairs) {
-        s_hi[threadIdx.x] = p.f_hi[threadIdx.x];
-        s_lo[threadIdx.x] = p.f_lo[threadIdx.x];
-        s_axis[threadIdx.x] = p.axis[threadIdx.x];
+    for (int i = threadIdx.x; i < p.P; i += blockDim.x) {
+        s_hi[i] = p.f_hi[i];
+        s_lo[i] = p.f_lo[i];
+        s_axis[i] = p.axis[i];
     }
     __syncthreads();
-    const unsigned int idx = blockIdx.x * kRopeThreads + threadIdx.x;
-    const unsigned int n = idx / p.items;
+    constexpr bool GATHER = PAIRS < kRopeHalves;
+    const unsigned int idx = blockIdx.x * blockDim.x + threadIdx.x;
+    unsigned int n = idx / p.items;
     const int item = static_cast<int>(idx - n * p.items);
-    if (n >= static_cast<unsigned int>(p.N)) return;
+    const bool in_range = n < static_cast<unsigned int>(p.N);
+    if (!GATHER && !in_range) return;
+    if (!in_range) n = p.N - 1;  // takes part in the barriers only
     const int b = blockIdx.z;
 
-    constexpr int NP = INTERLEAVED ? 4 : 8;
+    constexpr int NP = PAIRS == kRopeInterleaved ? 4 : 8;
     float sn[NP], cs[NP];
-    const bool rotates = INTERLEAVED || item < p.pair_items;
+    const bool rotates = PAIRS != kRopeHalves || item < p.pair_items;
+    constexpr int W = GATHER ? PAIRS : 1;
+    int partner[8 / W];        // byte offsets in the row
+    unsigned int copied = 0u;  // channels that pass
     if (rotates) {
         const float* pos = p.pos + static_cast<long long>(b) * p.pos_b + static_cast<long long>(n) * p.n_axes;
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            const int pair = item * NP + i;
+            int pair = item * NP + i;
+            float sign = p.sign;
+            if (GATHER) {
+                if (pair >= 2 * p.P) copied |= 1u << i;
+                // (u, w) -> (u cos - w sin, w cos + u sin): a first channel takes its partner times -sin
+                if (pair < p.P) sign = -sign;
+                if (i % W == 0) partner[i / W] = 2 * (pair < p.P ? pair + p.P : pair < 2 * p.P ? pair - p.P : pair);
+                if (pair >= p.P) pair = pair < 2 * p.P ? pair - p.P : p.P;
+            }
             sn[i] = 0.0f;
             cs[i] = 1.0f;
-            if (pair < p.P) rope_sincos(pos[s_axis[pair]], s_hi[pair], s_lo[pair], p.sign, &sn[i], &cs[i]);
+            if (pair < p.P) rope_sincos(pos[s_axis[pair]], s_hi[pair], s_lo[pair], sign, &sn[i], &cs[i]);
         }
     }
     const int first = blockIdx.y * p.heads_per_group;
@@ -164,10 +182,47 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
         const int h0 = max(first - (w == 0 ? 0 : p.t[0].heads), 0);
         const int h1 = min(last - (w == 0 ? 0 : p.t[0].heads), t.heads);
         const char* in = t.in + b * t.in_b + n * t.in_t;
-        char* out = t.out + b * t.out_b + n * t.out_t;
-        if (INTERLEAVED) {
+        char* out = t.out + b * t.out_b + n * t.out_t + 16 * item;
+        if (GATHER) {
+            constexpr int AT_ONCE = 2;  // heads; four took 128 registers and half of the occupancy
+            const char* own = in + h0 * t.in_h + 16 * item;
+            const char* of[8 / W];
+#pragma unroll
+            for (int i = 0; i < 8 / W; ++i) of[i] = in + h0 * t.in_h + partner[i];
+            out += h0 * t.out_h;
+            for (int h = h0; h < h1; h += AT_ONCE) {
+                const bool two = h + 1 < h1;
+                uint4 x[AT_ONCE], y[AT_ONCE];
+                asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0].x), "=r"(x[0].y), "=r"(x[0].z), "=r"(x[0].w) : "l"(own) : "memory");
+                y[0] = gather_pieces<W>(of, 0);
+                if (two) {
+                    asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];"
+                                 : "=r"(x[1].x), "=r"(x[1].y), "=r"(x[1].z), "=r"(x[1].w) : "l"(own + t.in_h) : "memory");
+                    y[1] = gather_pieces<W>(of, t.in_h);
+                }
+                if (t.in == t.out) __syncthreads();
+#pragma unroll
+                for (int j = 0; j < AT_ONCE; ++j)
+                    if ((j == 0 || two) && in_range) {
+                        const F8 f = unpack8<KIND>(x[j]), g = unpack8<KIND>(y[j]);
+                        F8 r;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) r.v[i] = fmaf(f.v[i], cs[i % NP], g.v[i] * sn[i % NP]);
+                        if (copied != 0u) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                if ((copied >> i) & 1u) r.v[i] = f.v[i];
+                        }
+                        store16(out + j * t.out_h, pack8<KIND>(r));
+                    }
+                if (t.in == t.out) __syncthreads();
+                own += 2 * t.in_h;
+#pragma unroll
+                for (int i = 0; i < 8 / W; ++i) of[i] += 2 * t.in_h;
+                out += 2 * t.out_h;
+            }
+        } else if (PAIRS == kRopeInterleaved) {
             in += 16 * item;
-            out += 16 * item;
             for (int h = h0; h < h1; h += kRopeUnroll) {
                 uint4 x[kRopeUnroll];
 #pragma unroll
@@ -180,25 +235,23 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
                         F8 r;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            r.v[2 * i] = f.v[2 * i] * cs[i] - f.v[2 * i + 1] * sn[i];
-                            r.v[2 * i + 1] = f.v[2 * i] * sn[i] + f.v[2 * i + 1] * cs[i];
+                            const bool turns = item * 4 + i < p.P;
+                            r.v[2 * i] = turns ? f.v[2 * i] * cs[i] - f.v[2 * i + 1] * sn[i] : f.v[2 * i];
+                            r.v[2 * i + 1] = turns ? f.v[2 * i] * sn[i] + f.v[2 * i + 1] * cs[i] : f.v[2 * i + 1];
                         }
                         store16(out + (h + j) * t.out_h, pack8<KIND>(r));
                     }
             }
         } else if (rotates) {
-            const int end = p.P - 8 * item;  // pairs left from this item's first on
             const long long second = 2ll * p.P;
             in += 16 * item;
-            out += 16 * item;
             for (int h = h0; h < h1; h += kRopeUnroll / 2) {
                 uint4 x[kRopeUnroll / 2], y[kRopeUnroll / 2];
 #pragma unroll
                 for (int j = 0; j < kRopeUnroll / 2; ++j)
                     if (h + j < h1) {
-                        const char* at = in + (h + j) * t.in_h;
-                        x[j] = (W == 8 || end >= 8) ? load16(at) : load_pieces<W>(at, end);
-                        y[j] = load_pieces<W>(at + second, end);
+                        x[j] = load16(in + (h + j) * t.in_h);
+                        y[j] = load16(in + (h + j) * t.in_h + second);
                     }
 #pragma unroll
                 for (int j = 0; j < kRopeUnroll / 2; ++j)
@@ -210,16 +263,14 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
                             r.v[i] = f.v[i] * cs[i % NP] - g.v[i] * sn[i % NP];
                             q.v[i] = f.v[i] * sn[i % NP] + g.v[i] * cs[i % NP];
                         }
-                        char* to = out + (h + j) * t.out_h;
-                        if (W == 8 || end >= 8) store16(to, pack8<KIND>(r));
-                        else store_pieces<W>(to, pack8<KIND>(r), end);
-                        store_pieces<W>(to + second, pack8<KIND>(q), end);
+                        store16(out + (h + j) * t.out_h, pack8<KIND>(r));
+                        store16(out + (h + j) * t.out_h + second, pack8<KIND>(q));
                     }
             }
-        } else {  // channels behind the rotated ones
-            const int at = 2 * p.P + 8 * (item - p.pair_items);
+        } else {  // channels behind the rotated ones: item counts eight-channel pieces from 2P on
+            const long long at = 4ll * p.P - 16ll * p.pair_items;
             for (int h = h0; h < h1; ++h)
-                store_pieces<W>(out + h * t.out_h + 2 * at, load_pieces<W>(in + h * t.in_h + 2 * at, p.d - at), p.d - at);
+                store16(out + h * t.out_h + at, load16(in + h * t.in_h + at + 16 * item));
         }
     }
 }

@@ -135,13 +135,15 @@ bool views_apart(const linfusion_rope_desc_t& d, RopeView a, RopeView b)
 }
 
 template <int KIND>
-cudaError_t launch_rope(const RopeParams& p, bool interleaved, dim3 grid, cudaStream_t s)
+cudaError_t launch_rope(const RopeParams& p, int pairs, dim3 grid, int threads, cudaStream_t s)
 {
-    if (interleaved) rope_kernel<KIND, true, 8><<<grid, kRopeThreads, 0, s>>>(p);
-    else if (p.P % 8 == 0) rope_kernel<KIND, false, 8><<<grid, kRopeThreads, 0, s>>>(p);
-    else if (p.P % 4 == 0) rope_kernel<KIND, false, 4><<<grid, kRopeThreads, 0, s>>>(p);
-    else if (p.P % 2 == 0) rope_kernel<KIND, false, 2><<<grid, kRopeThreads, 0, s>>>(p);
-    else rope_kernel<KIND, false, 1><<<grid, kRopeThreads, 0, s>>>(p);
+    switch (pairs) {
+        case kRopeInterleaved: rope_kernel<KIND, kRopeInterleaved><<<grid, threads, 0, s>>>(p); break;
+        case kRopeHalves: rope_kernel<KIND, kRopeHalves><<<grid, threads, 0, s>>>(p); break;
+        case 4: rope_kernel<KIND, 4><<<grid, threads, 0, s>>>(p); break;
+        case 2: rope_kernel<KIND, 2><<<grid, threads, 0, s>>>(p); break;
+        default: rope_kernel<KIND, 1><<<grid, threads, 0, s>>>(p); break;
+    }
     return cudaGetLastError();
 }
 
@@ -360,9 +362,9 @@ linfusion_status_t linfusion_rope(const linfusion_rope_desc_t* desc, const linfu
     p.P = P;
     p.n_axes = desc->n_axes;
     p.sign = desc->backward ? -1.0f : 1.0f;
-    const bool interleaved = desc->interleaved != 0;
-    p.pair_items = interleaved ? desc->d / 8 : (P + 7) / 8;
-    p.items = interleaved ? desc->d / 8 : p.pair_items + (desc->d - 2 * P + 7) / 8;
+    const int pairs = desc->interleaved != 0 ? kRopeInterleaved : P % 8 == 0 ? kRopeHalves : P % 4 == 0 ? 4 : P % 2 == 0 ? 2 : 1;
+    p.pair_items = P / 8;                                                                         // halves only
+    p.items = pairs == kRopeHalves ? p.pair_items + (desc->d - 2 * P) / 8 : desc->d / 8;
     for (int a = 0, i = 0; a < desc->n_axes; ++a)
         for (int j = 0; j < desc->pairs[a]; ++j, ++i) {
             const double turns = std::pow(desc->theta, -static_cast<double>(j) / desc->pairs[a]) / 6.283185307179586476925;
@@ -370,21 +372,28 @@ linfusion_status_t linfusion_rope(const linfusion_rope_desc_t* desc, const linfu
             p.f_hi[i] = static_cast<float>(turns);
             p.f_lo[i] = static_cast<float>(turns - static_cast<double>(p.f_hi[i]));
         }
-    // Threads of one head group, and head groups enough to give every SM four blocks where there are few tokens: a
-    // group forms its sines and cosines again, which costs less than idle SMs.
+    // Head groups: a block goes through its group's heads and forms its sines and cosines once, at the price of about three
+    // heads.  What counts is how many rounds of blocks the machine goes through (four blocks on an SM) times what one does.
     const long long threads = static_cast<long long>(desc->N) * p.items;
-    const long long blocks = (threads + kRopeThreads - 1) / kRopeThreads;
+    // (where partners are gathered a block holds whole rows)
+    const int block = pairs < kRopeHalves ? kRopeThreads / p.items * p.items : kRopeThreads;
+    const long long blocks = (threads + block - 1) / block;
     if (threads + kRopeThreads > 0xffffffffll) return LINFUSION_ERR_UNSUPPORTED;
-    long long groups = (4ll * at.sms + blocks * desc->B - 1) / (blocks * desc->B);
-    if (groups > heads) groups = heads;
-    p.heads_per_group = static_cast<int>((heads + groups - 1) / groups);
+    p.heads_per_group = heads;
+    double best = 1e300;
+    for (int g = 1; g <= heads && g <= 64; ++g) {
+        const int per_group = (heads + g - 1) / g;
+        const long long all = blocks * desc->B * ((heads + per_group - 1) / per_group), rounds = (all + 4 * at.sms - 1) / (4 * at.sms);
+        const double cost = static_cast<double>(rounds) * (3 + per_group);
+        if (cost < best) best = cost, p.heads_per_group = per_group;
+    }
     const long long grid_y = (heads + p.heads_per_group - 1) / p.heads_per_group;
     if (grid_y > 65535) return LINFUSION_ERR_UNSUPPORTED;
     const dim3 grid(static_cast<unsigned int>(blocks), static_cast<unsigned int>(grid_y), desc->B);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     return end((desc->flags & LINFUSION_DTYPE_FP16) != 0u
-                   ? launch_rope<make_kind(kPhiIdentity, kDtypeFp16)>(p, interleaved, grid, s)
-                   : launch_rope<make_kind(kPhiIdentity, kDtypeBf16)>(p, interleaved, grid, s));
+                   ? launch_rope<make_kind(kPhiIdentity, kDtypeFp16)>(p, pairs, grid, block, s)
+                   : launch_rope<make_kind(kPhiIdentity, kDtypeBf16)>(p, pairs, grid, block, s));
 }
 
 linfusion_status_t linfusion_block_norm(const linfusion_block_norm_desc_t* desc, const linfusion_rows_t* x,
