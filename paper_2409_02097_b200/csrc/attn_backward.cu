@@ -83,6 +83,10 @@ void plan_tc(const linfusion_attn_desc_t& d, int sm_count, BackwardPlan* p)
     if (const char* force = std::getenv("LF_TC")) p->tc = p->dk <= 64 && p->dv <= 64 && std::atoi(force) != 0;
     if (!p->tc) return;
     p->ctas = static_cast<int>(p->tiles < sm_count ? p->tiles : sm_count);
+    // The same number of CTAs on every slab where that keeps four fifths of the SMs busy and runs are short: a CTA that
+    // meets a second slab fetches another state and hands back another partial, 4 us of a run of a few tiles.
+    const int aligned = sm_count / p->slabs * p->slabs;
+    if (5 * aligned >= 4 * sm_count && aligned <= p->ctas && p->tiles < 64ll * sm_count) p->ctas = aligned;
     // a run of L tiles meets at most this many slabs
     const long long L = (p->tiles + p->ctas - 1) / p->ctas;
     p->spans = static_cast<int>((L + p->tiles_per_slab - 2) / p->tiles_per_slab) + 1;

@@ -122,16 +122,24 @@ __device__ __forceinline__ void phi_row(uint32_t tile, int r, int first, float (
 template <int KIND>
 __device__ __forceinline__ float slope_of(float f) { return kind_phi(KIND) == kPhiIdentity ? 1.0f : fminf(f, 1.0f); }
 
-// Largest value over the consumers; `scratch`: a float of shared memory for each warp.
+// Largest of three values over the consumers; `scratch`: three floats of shared memory for each warp.
 template <int WARPS>
-__device__ __forceinline__ float consumer_max(float v, float* scratch, int warp, int lane)
+__device__ __forceinline__ float3 consumer_max(float3 v, float* scratch, int warp, int lane)
 {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-    if (lane == 0) scratch[warp] = v;
+    for (int o = 16; o > 0; o >>= 1) {
+        v.x = fmaxf(v.x, __shfl_xor_sync(0xffffffffu, v.x, o));
+        v.y = fmaxf(v.y, __shfl_xor_sync(0xffffffffu, v.y, o));
+        v.z = fmaxf(v.z, __shfl_xor_sync(0xffffffffu, v.z, o));
+    }
+    if (lane == 0) scratch[3 * warp] = v.x, scratch[3 * warp + 1] = v.y, scratch[3 * warp + 2] = v.z;
     consumer_sync<WARPS>();
-    for (int i = 0; i < WARPS; ++i) v = fmaxf(v, scratch[i]);
-    consumer_sync<WARPS>();
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) {
+        v.x = fmaxf(v.x, scratch[3 * i]);
+        v.y = fmaxf(v.y, scratch[3 * i + 1]);
+        v.z = fmaxf(v.z, scratch[3 * i + 2]);
+    }
     return v;
 }
 
@@ -158,12 +166,9 @@ __device__ __forceinline__ void tc_load_state(const float* S, int dk, int dv, ui
         float big = 0.0f;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) big = fmaxf(big, fabsf(x[i]));
-        *scale_s = pow2_scale(consumer_max<WARPS>(big, scratch, warp, lane), 12);
-        if (eps >= 0.0f) {
-            const float z_max = consumer_max<WARPS>(zv, scratch, warp, lane);
-            const float z_inv = consumer_max<WARPS>(tid >= dk ? 0.0f : zv > 0.0f ? 1.0f / zv : 3.0e38f, scratch, warp, lane);
-            *scale_w = fmaxf(pow2_scale(z_inv, 12), 1.0f / pow2_scale(z_max, 4));
-        }
+        const float3 m = consumer_max<WARPS>(make_float3(big, zv, tid >= dk ? 0.0f : zv > 0.0f ? 1.0f / zv : 3.0e38f), scratch, warp, lane);
+        *scale_s = pow2_scale(m.x, 12);
+        if (eps >= 0.0f) *scale_w = fmaxf(pow2_scale(m.z, 12), 1.0f / pow2_scale(m.y, 4));
     }
 #pragma unroll
     for (int h = 0; h < EACH / 8; ++h) {
@@ -253,7 +258,7 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
     unsigned char* So = F + C::STATE_F * C::F_BYTES;
     float* z = reinterpret_cast<float*>(So + C::S_BYTES);
     float* scratch = z + 64;
-    uint64_t* full = reinterpret_cast<uint64_t*>(scratch + 16);
+    uint64_t* full = reinterpret_cast<uint64_t*>(scratch + 32);
     uint64_t* empty = full + C::STATE_STAGES;
     uint64_t* t_full = empty + C::STATE_STAGES;      // [T_BUFFERS]
     uint64_t* f_full = t_full + C::T_BUFFERS;  // F of a tile is written
@@ -612,7 +617,7 @@ backward_tc_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
     unsigned char* So = F + C::F_BYTES;
     float* z = reinterpret_cast<float*>(So + C::S_BYTES);
     float* scratch = z + 64;
-    uint64_t* full = reinterpret_cast<uint64_t*>(scratch + 16);
+    uint64_t* full = reinterpret_cast<uint64_t*>(scratch + 32);
     uint64_t* empty = full + C::KV_STAGES;
     uint64_t* t_full = empty + C::KV_STAGES;      // [T_BUFFERS] both products of a tile are complete (commit)
     uint64_t* t_free = t_full + C::T_BUFFERS;  // [T_BUFFERS] ... and have been read (4 warps)
