@@ -13,7 +13,8 @@ LIB_PATH = os.path.join(_PKG, "liblinfusion_attn.so")
 _SOURCES = {
     "linfusion_attn.cu": ["common.cuh", "split_kernels.cuh", "stream_kernels.cuh", "fused_kernels.cuh", "producer_kernels.cuh",
                           "padded_kernels.cuh", "linfusion_attn.h"],
-    "attn_backward.cu": ["common.cuh", "backward_kernels.cuh", "backward_tc_kernels.cuh", "packed_math.cuh", "host_util.h",
+    "attn_backward.cu": ["common.cuh", "backward_kernels.cuh", "backward_tc_kernels.cuh",
+                         "backward_tc_wide_kernels.cuh", "packed_math.cuh", "host_util.h",
                          "linfusion_attn.h"],
     "block_ops.cu": ["common.cuh", "block_kernels.cuh", "packed_math.cuh", "host_util.h", "linfusion_attn.h", "linfusion_block.h"],
 }

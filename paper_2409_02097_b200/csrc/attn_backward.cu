@@ -2,10 +2,9 @@
 // the tokens, workspace layout and launches.
 #include "../../include/linfusion_attn.h"
 
-#include <cstdlib>
-
 #include "backward_kernels.cuh"
 #include "backward_tc_kernels.cuh"
+#include "backward_tc_wide_kernels.cuh"
 #include "host_util.h"
 
 using namespace lf;
@@ -42,7 +41,8 @@ constexpr int kPlanSms = 148;  // a B200's, where no count is given
 struct BackwardPlan {
     int slabs, dk, dv, floats;  // floats of S | z of a slab
     int chunks_q, chunks_kv;    // CTAs per slab of the two streams
-    bool tc;                    // the tcgen05 kernels
+    int tc;                     // the tcgen05 kernels: 0 (not), 1 (widths up to 64), 2 (features up to 128)
+    size_t tc_partial;          // ... floats of a partial
     int tiles_per_slab, ctas, spans;  // ... their tiles of a slab, CTAs, and slabs that a CTA meets at most
     long long tiles;
     size_t partials_off, state_off, grad_off, total;  // behind a status word
@@ -74,13 +74,24 @@ void plan_chunks(const linfusion_attn_desc_t& d, int sm_count, BackwardPlan* p)
         default: break;                    \
     }
 
-// Where the tcgen05 kernels take over.
+// Where the tcgen05 kernels take over from the warp-level ones (whole backward pass, us, tcgen05 / warp-level):
+//   widths up to 64, from 1.75 tiles of 128 tokens per SM on: 41 / 53 at 128 slabs x 256 x 64, 38 / 36 at 16 x 2048 x 40,
+//   39 / 30 at 20 x 1024 x 64, 43 / 51 at 20 x 2048 x 64, 53 / 72 at 20 x 4096 x 64
+//   features up to 128, by the work, which the warp-level kernels feel more: 76 / 82 at 16 x 1024 x 128, 70 / 55 at 16 x 512 x
+//   128, 68 / 60 at 16 x 2048 x 80, 353 / 658 at 16 x 32768 x 80, 244 / 746 at 16 x 16384 x 128
+// and not where slabs are so short that a CTA changes its state every tile or two.
 void plan_tc(const linfusion_attn_desc_t& d, int sm_count, BackwardPlan* p)
 {
     p->tiles_per_slab = (d.N + kTcTile - 1) / kTcTile;
     p->tiles = static_cast<long long>(p->slabs) * p->tiles_per_slab;
-    p->tc = p->dk <= 64 && p->dv <= 64 && p->tiles_per_slab >= 4 && p->tiles >= 2ll * sm_count;
-    if (const char* force = std::getenv("LF_TC")) p->tc = p->dk <= 64 && p->dv <= 64 && std::atoi(force) != 0;
+    p->tc = 0;
+    if (p->dk <= 64 && p->dv <= 64) {
+        if (p->tiles_per_slab >= 2 && 4 * p->tiles >= 7ll * sm_count) p->tc = 1;
+    } else if (p->dk <= 128 && p->dv <= 128) {
+        const long long work = static_cast<long long>(p->slabs) * d.N * p->dk * p->dv;
+        if (p->tiles_per_slab >= 4 && work >= 1800000ll * sm_count) p->tc = 2;
+    }
+    p->tc_partial = p->tc == 1 ? BackwardTc::PARTIAL_FLOATS : p->dv > 64 ? BackwardTcWide<2>::PARTIAL_FLOATS : BackwardTcWide<1>::PARTIAL_FLOATS;
     if (!p->tc) return;
     p->ctas = static_cast<int>(p->tiles < sm_count ? p->tiles : sm_count);
     // The same number of CTAs on every slab where that keeps four fifths of the SMs busy and runs are short: a CTA that
@@ -115,7 +126,7 @@ linfusion_status_t make_backward_plan(const linfusion_attn_desc_t* desc, int sm_
     p->state_off = 256;
     p->grad_off = p->state_off + state;
     p->partials_off = p->grad_off + state;
-    p->total = p->partials_off + align_up_256(p->tc ? static_cast<size_t>(p->ctas) * p->spans * BackwardTc::PARTIAL_FLOATS * sizeof(float)
+    p->total = p->partials_off + align_up_256(p->tc ? static_cast<size_t>(p->ctas) * p->spans * p->tc_partial * sizeof(float)
                                                     : slab_state * static_cast<size_t>(p->chunks_q));
     return LINFUSION_OK;
 }
@@ -136,8 +147,12 @@ cudaError_t launch_state(const linfusion_attn_desc_t& d, const BackwardPlan& p, 
                    static_cast<__nv_bfloat16*>(dq), p.chunks_q == 1 ? out : partials, d.N, p.chunks_q, slab_layout(d, DK),
                    slab_layout(d, DV), sc, clear);
     if (e != cudaSuccess || p.chunks_q == 1) return e;
-    return launch_pdl(backward_reduce_kernel, dim3((p.floats + 255) / 256, p.slabs), dim3(256), 0, s, partials, out, p.floats,
-                      p.chunks_q);
+#define LF_REDUCE(S)                                                                                                               \
+    launch_pdl(backward_reduce_kernel<S>, dim3((p.floats + kReduceThreads / S - 1) / (kReduceThreads / S), p.slabs), dim3(kReduceThreads), 0, \
+               s, partials, out, p.floats, p.chunks_q)
+    const int slices = reduce_slices_for(p.chunks_q);
+    return slices == 1 ? LF_REDUCE(1) : slices == 4 ? LF_REDUCE(4) : LF_REDUCE(8);
+#undef LF_REDUCE
 }
 
 template <int DK, int DV, int KIND>
@@ -189,42 +204,64 @@ bool encode_map(CUtensorMap* map, const void* base, const linfusion_attn_desc_t&
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, promo, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The kernel of one of the three cuts: widths up to 64, or two feature atoms with one or two value atoms.
+template <typename K, typename... Args>
+cudaError_t launch_tc(K* kernel, int smem, int threads, std::atomic<uint64_t>* done, const linfusion_attn_desc_t& d, const BackwardPlan& p,
+                      cudaStream_t s, Args... args)
+{
+    const cudaError_t e = allow_smem(kernel, smem, d.device, done);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(kernel, dim3(p.ctas), dim3(threads), smem, s, args...);
+}
+
 template <int KIND, bool GRAD>
 cudaError_t launch_tc_state(const linfusion_attn_desc_t& d, const BackwardPlan& p, const void* q, const void* dy, const float* state,
                             void* dq, float* partials, float* out, uint32_t* status, bool clear, cudaStream_t s)
 {
-    static std::atomic<uint64_t> done{0};
-    cudaError_t e = allow_smem(backward_tc_state_kernel<KIND, GRAD>, BackwardTc::STATE_SMEM, d.device, &done);
-    if (e != cudaSuccess) return e;
+    static std::atomic<uint64_t> done[3];
     CUtensorMap mq, mg, mdq;
     if (!encode_map(&mq, q, d, p.dk) || !encode_map(&mg, dy, d, p.dv) || !encode_map(&mdq, GRAD ? dq : q, d, p.dk))
         return cudaErrorInvalidValue;
     BackwardScales sc;
     sc.eps = (d.flags & LINFUSION_FLAG_UNNORMALIZED) != 0u ? kEpsUnnormalized : d.eps;
     sc.scaled = kind_dtype(KIND) == kDtypeFp16 ? 1 : 0;
-    e = launch_pdl(backward_tc_state_kernel<KIND, GRAD>, dim3(p.ctas), dim3(BackwardTc::STATE_THREADS), BackwardTc::STATE_SMEM, s, mq, mg, mdq,
-                   state, partials, status, d.N, p.dk, p.dv, p.tiles_per_slab, p.tiles, p.spans, d.H, sc, clear ? 1 : 0);
+    const int first = clear ? 1 : 0;
+#define LF_STATE(KERNEL, SMEM, THREADS, I)                                                                                             \
+    launch_tc(KERNEL, SMEM, THREADS, &done[I], d, p, s, mq, mg, mdq, state, partials, status, d.N, p.dk, p.dv, p.tiles_per_slab, p.tiles, \
+              p.spans, d.H, sc, first)
+    const cudaError_t e =
+        p.tc == 1     ? LF_STATE((backward_tc_state_kernel<KIND, GRAD>), BackwardTc::STATE_SMEM, BackwardTc::STATE_THREADS, 0)
+        : p.dv <= 64 ? LF_STATE((backward_tc_wide_state_kernel<KIND, 1, GRAD>), BackwardTcWide<1>::SMEM, BackwardTcWide<1>::THREADS, 1)
+                     : LF_STATE((backward_tc_wide_state_kernel<KIND, 2, GRAD>), BackwardTcWide<2>::SMEM, BackwardTcWide<2>::THREADS, 2);
+#undef LF_STATE
     if (e != cudaSuccess) return e;
-    return launch_pdl(backward_tc_reduce_kernel, dim3((p.floats + 255) / 256, p.slabs), dim3(256), 0, s, partials, out, p.dk, p.dv,
-                      p.tiles_per_slab, p.tiles, p.ctas, p.spans);
+#define LF_REDUCE(S)                                                                                                                  \
+    launch_pdl(backward_tc_reduce_kernel<S>, dim3((p.floats + kReduceThreads / S - 1) / (kReduceThreads / S), p.slabs), dim3(kReduceThreads), 0, \
+               s, partials, out, p.dk, p.dv, p.tiles_per_slab, p.tiles, p.ctas, p.spans, p.dv <= 64 ? 64 : 128, p.tc)
+    const int slices = reduce_slices_for(p.ctas / p.slabs + 1);
+    return slices == 1 ? LF_REDUCE(1) : slices == 4 ? LF_REDUCE(4) : LF_REDUCE(8);
+#undef LF_REDUCE
 }
 
 template <int KIND>
 cudaError_t launch_tc_kv(const linfusion_attn_desc_t& d, const BackwardPlan& p, const void* k, const void* v, const float* grad_state,
                          void* dk, void* dv, uint32_t* status, bool clear, cudaStream_t s)
 {
-    static std::atomic<uint64_t> done{0};
-    cudaError_t e = allow_smem(backward_tc_kv_kernel<KIND>, BackwardTc::KV_SMEM, d.device, &done);
-    if (e != cudaSuccess) return e;
+    static std::atomic<uint64_t> done[3];
     CUtensorMap mk, mv, mdk, mdv;
-    if (!encode_map(&mk, k, d, p.dk) || !encode_map(&mv, v, d, p.dv) || !encode_map(&mdk, dk, d, p.dk) ||
-        !encode_map(&mdv, dv, d, p.dv))
+    if (!encode_map(&mk, k, d, p.dk) || !encode_map(&mv, v, d, p.dv) || !encode_map(&mdk, dk, d, p.dk) || !encode_map(&mdv, dv, d, p.dv))
         return cudaErrorInvalidValue;
     BackwardScales sc;
     sc.eps = d.eps;
     sc.scaled = kind_dtype(KIND) == kDtypeFp16 ? 1 : 0;
-    return launch_pdl(backward_tc_kv_kernel<KIND>, dim3(p.ctas), dim3(BackwardTc::KV_THREADS), BackwardTc::KV_SMEM, s, mk, mv, mdk, mdv,
-                      grad_state, status, d.N, p.dk, p.dv, p.tiles_per_slab, p.tiles, d.H, sc, clear ? 1 : 0);
+    const int first = clear ? 1 : 0;
+#define LF_KV(KERNEL, SMEM, THREADS, I)                                                                                                   \
+    launch_tc(KERNEL, SMEM, THREADS, &done[I], d, p, s, mk, mv, mdk, mdv, grad_state, status, d.N, p.dk, p.dv, p.tiles_per_slab, p.tiles, d.H, \
+              sc, first)
+    return p.tc == 1     ? LF_KV((backward_tc_kv_kernel<KIND>), BackwardTc::KV_SMEM, BackwardTc::KV_THREADS, 0)
+           : p.dv <= 64 ? LF_KV((backward_tc_wide_kv_kernel<KIND, 1>), BackwardTcWide<1>::SMEM, BackwardTcWide<1>::THREADS, 1)
+                        : LF_KV((backward_tc_wide_kv_kernel<KIND, 2>), BackwardTcWide<2>::SMEM, BackwardTcWide<2>::THREADS, 2);
+#undef LF_KV
 }
 
 #define LF_DISPATCH_KINDS(kind, CALL) \

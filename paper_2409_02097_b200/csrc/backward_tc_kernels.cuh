@@ -557,50 +557,58 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
     if (warp == 0) tmem_dealloc(tmem, C::TMEM_COLS);
 }
 
-// Sum of a slab's partials, in the order of the CTAs that worked on it: out[slab] = S | z (dS | dz).
-constexpr int kTcReduceAtOnce = 32;
-static __global__ void __launch_bounds__(256)
+// Sum of a slab's partials over the CTAs that worked on it, in a fixed order: out[slab] = S | z (dS | dz).  A partial holds, for each
+// 64-feature atom, 64 rows of heads and 64 of tails, vw floats each, and then 64 floats of z from each of the eight warps,
+// the warps of an atom next to one another.
+template <int SLICES>
+static __global__ void __launch_bounds__(kReduceThreads)
 backward_tc_reduce_kernel(const float* __restrict__ partials, float* __restrict__ out, int dk, int dv, int tiles_per_slab, long long W,
-                          int G, int spans)
+                          int G, int spans, int vw, int atoms)
 {
-    __shared__ long long where[kTcReduceAtOnce];  // of a contributing CTA's partial; -1: none
-    const int slab = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x, floats = grad_state_floats(dk, dv);
+    constexpr int AT_ONCE = kReduceThreads, OUT = kReduceThreads / SLICES;
+    __shared__ long long where[AT_ONCE];  // of a contributing CTA's partial; -1: none
+    __shared__ float scratch[kReduceThreads];
+    const int slab = blockIdx.y, slice = threadIdx.x / OUT, i = blockIdx.x * OUT + threadIdx.x % OUT;
+    const int floats = grad_state_floats(dk, dv);
     const long long first = static_cast<long long>(slab) * tiles_per_slab, last = first + tiles_per_slab;
     // the CTA that holds the slab's first tile: the largest g with g W / G <= first
     const int g0 = static_cast<int>(((first + 1) * G - 1) / W), g1 = static_cast<int>((last * G - 1) / W);
-    const int row = i / dv, col = i - row * dv;
     const bool of_z = i >= dk * dv;
-    pdl_launch_dependents();
-    pdl_wait();
+    const int row = of_z ? i - dk * dv : i / dv, col = of_z ? 0 : i - row * dv, a = row >> 6, ar = row & 63;
+    const long long partial_floats = static_cast<long long>(atoms) * 128 * vw + 512;
     float sum = 0.0f;
-    for (int at = g0; at <= g1; at += kTcReduceAtOnce) {
-        const int n = min(kTcReduceAtOnce, g1 + 1 - at);
+    bool waited = false;
+    pdl_launch_dependents();
+    for (int at = g0; at <= g1; at += AT_ONCE) {
+        const int n = min(AT_ONCE, g1 + 1 - at);
         __syncthreads();
         if (threadIdx.x < n) {
             const int g = at + threadIdx.x;
             const long long u0 = tc_first_tile(g, W, G), u1 = tc_first_tile(g + 1, W, G);
             where[threadIdx.x] = u1 > u0 && u1 > first && u0 < last
-                                     ? (static_cast<long long>(g) * spans + (slab - static_cast<int>(u0 / tiles_per_slab))) * BackwardTc::PARTIAL_FLOATS
+                                     ? (static_cast<long long>(g) * spans + (slab - static_cast<int>(u0 / tiles_per_slab))) * partial_floats
                                      : -1;
         }
+        if (!waited) pdl_wait();  // the table needs nothing of the kernel before
+        waited = true;
         __syncthreads();
         if (i < floats) {
 #pragma unroll 4
-            for (int k = 0; k < n; ++k) {
+            for (int k = slice; k < n; k += SLICES) {
                 if (where[k] < 0) continue;
                 const float* p = partials + where[k];
                 if (!of_z) {
-                    sum += p[row * 64 + col] + p[(64 + row) * 64 + col];
+                    sum += p[(a * 128 + ar) * vw + col] + p[(a * 128 + 64 + ar) * vw + col];
                 } else {
-                    float x[8];
-#pragma unroll
-                    for (int w = 0; w < 8; ++w) x[w] = p[128 * 64 + w * 64 + i - dk * dv];
-                    sum += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+                    const float* z = p + atoms * 128 * vw + ar;
+                    for (int w = a * 8 / atoms; w < (a + 1) * 8 / atoms; w += 4)
+                        sum += (z[w * 64] + z[(w + 1) * 64]) + (z[(w + 2) * 64] + z[(w + 3) * 64]);
                 }
             }
         }
     }
-    if (i < floats) out[static_cast<size_t>(slab) * floats + i] = sum;
+    sum = reduce_slices<SLICES>(sum, scratch);
+    if (slice == 0 && i < floats) out[static_cast<size_t>(slab) * floats + i] = sum;
 }
 
 template <int KIND>
