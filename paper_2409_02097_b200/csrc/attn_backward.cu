@@ -137,12 +137,13 @@ cudaError_t launch_state(const linfusion_attn_desc_t& d, const BackwardPlan& p, 
 {
     using C = BackwardCfg<DK, DV>;
     static std::atomic<uint64_t> done{0};
-    cudaError_t e = allow_smem(backward_state_kernel<DK, DV, KIND, GRAD>, C::SMEM_Q, d.device, &done);
+    cudaError_t e = allow_smem(backward_state_kernel<DK, DV, KIND, GRAD>, GRAD ? C::SMEM_Q : C::SMEM_STATE, d.device, &done);
     if (e != cudaSuccess) return e;
     BackwardScales sc;
     sc.eps = (d.flags & LINFUSION_FLAG_UNNORMALIZED) != 0u ? kEpsUnnormalized : d.eps;
     sc.scaled = kind_dtype(KIND) == kDtypeFp16 ? 1 : 0;
-    e = launch_pdl(backward_state_kernel<DK, DV, KIND, GRAD>, dim3(p.chunks_q, p.slabs), dim3(32 * C::WQ), C::SMEM_Q, s,
+    e = launch_pdl(backward_state_kernel<DK, DV, KIND, GRAD>, dim3(p.chunks_q, p.slabs), dim3(32 * C::WQ),
+                   GRAD ? C::SMEM_Q : C::SMEM_STATE, s,
                    static_cast<const __nv_bfloat16*>(q), static_cast<const __nv_bfloat16*>(dy), state,
                    static_cast<__nv_bfloat16*>(dq), p.chunks_q == 1 ? out : partials, d.N, p.chunks_q, slab_layout(d, DK),
                    slab_layout(d, DV), sc, clear);

@@ -76,8 +76,10 @@ struct BackwardCfg {
     // A row takes an odd number of 16-byte units: eight rows of a matrix fragment fall into different banks.
     static constexpr int PITCHK = ((KP / 8) | 1) * 16, PITCHV = ((VP / 8) | 1) * 16;
     static constexpr int STAGE = TILE * (PITCHK + PITCHV);
-    static constexpr int SMEM_Q = 2 * STAGE + WQ * TILE * 8;
-    static constexpr int SMEM_KV = 2 * STAGE + 2 * TILE * PITCHK;  // head and tail of phi(k)
+    static constexpr int S_HALF = KP * PITCHV;  // the state's head, or its tail
+    static constexpr int SMEM_STATE = 2 * STAGE;
+    static constexpr int SMEM_Q = 2 * STAGE + 2 * S_HALF + KP * 4 + WQ * TILE * 8 + TILE * 8 + WQ * 16 * TILE * 4;
+    static constexpr int SMEM_KV = 2 * STAGE + 2 * S_HALF + KP * 4 + 2 * TILE * PITCHK;  // head and tail of phi(k)
 };
 
 struct BackwardScales {
@@ -113,8 +115,8 @@ __device__ __forceinline__ void store_tile(const unsigned char* src, __nv_bfloat
     for (int i = threadIdx.x; i < TILE * VECS; i += THREADS) {
         const int r = i / VECS, v = i - r * VECS;
         if (row0 + r < N)
-            st_stream_16B(base + static_cast<long long>(row0 + r) * row_stride + v * 8,
-                          *reinterpret_cast<const uint4*>(src + r * PITCH + v * 16));
+            *reinterpret_cast<uint4*>(base + static_cast<long long>(row0 + r) * row_stride + v * 8) =
+                *reinterpret_cast<const uint4*>(src + r * PITCH + v * 16);
     }
 }
 template <int D, int PITCH, int TILE, int THREADS>
@@ -138,35 +140,41 @@ __device__ __forceinline__ float block_max(float v, float* scratch, int warps)
     return v;
 }
 
-// Warp's A operand of a product with the rows of S (or dS): 16 features x DV channels, head and tail.
-template <int KIND, int DK, int DV>
-__device__ __forceinline__ void load_state_rows(const float* S, int m0, int lane, float scale,
-                                                uint32_t (&hi)[(DV + 15) / 16][4], uint32_t (&lo)[(DV + 15) / 16][4])
+// The block lays S (dS) out in shared memory as rows of features, head and tail, zeros where the widths end, and z (dz)
+// as floats.
+template <int KIND, int DK, int DV, int THREADS>
+__device__ __forceinline__ void load_state(const float* S, unsigned char* hi_rows, float* z, float scale)
 {
-#pragma unroll
-    for (int s = 0; s < (DV + 15) / 16; ++s)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int row = m0 + lane / 4 + (r & 1) * 8, col = s * 16 + 2 * (lane & 3) + (r >> 1) * 8;
-            float2 x = make_float2(0.0f, 0.0f);
-            if (row < DK && col < DV) x = *reinterpret_cast<const float2*>(S + row * DV + col);
-            split_pair<KIND>(x.x * scale, x.y * scale, &hi[s][r], &lo[s][r]);
+    using C = BackwardCfg<DK, DV>;
+    for (int i = threadIdx.x; i < C::KP * (C::VP / 8); i += THREADS) {
+        const int row = i / (C::VP / 8), piece = i - row * (C::VP / 8);
+        float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f), y = x;
+        if (row < DK && piece < DV / 8) {
+            const float4* p = reinterpret_cast<const float4*>(S + row * DV + 8 * piece);
+            x = p[0];
+            y = p[1];
         }
+        uint4 hi, lo;
+        split_pair<KIND>(x.x * scale, x.y * scale, &hi.x, &lo.x);
+        split_pair<KIND>(x.z * scale, x.w * scale, &hi.y, &lo.y);
+        split_pair<KIND>(y.x * scale, y.y * scale, &hi.z, &lo.z);
+        split_pair<KIND>(y.z * scale, y.w * scale, &hi.w, &lo.w);
+        unsigned char* at = hi_rows + row * C::PITCHV + 16 * piece;
+        *reinterpret_cast<uint4*>(at) = hi;
+        *reinterpret_cast<uint4*>(at + C::S_HALF) = lo;
+    }
+    for (int i = threadIdx.x; i < C::KP; i += THREADS) z[i] = i < DK ? S[DK * DV + i] : 0.0f;
 }
-// The same of its transpose: 16 channels x DK features.
-template <int KIND, int DK, int DV>
-__device__ __forceinline__ void load_state_cols(const float* S, int m0, int lane, float scale,
-                                                uint32_t (&hi)[(DK + 15) / 16][4], uint32_t (&lo)[(DK + 15) / 16][4])
+// A fragment of 16 features (rows m0 ..) x 16 channels (k0 ..) of those rows; and of its transpose: 16 channels (m0 ..) x 16
+// features (k0 ..).
+__device__ __forceinline__ void state_a(const unsigned char* rows, int pitch, int m0, int k0, int lane, uint32_t (&r)[4])
 {
-#pragma unroll
-    for (int s = 0; s < (DK + 15) / 16; ++s)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int ch = m0 + lane / 4 + (r & 1) * 8, f = s * 16 + 2 * (lane & 3) + (r >> 1) * 8;
-            float a = 0.0f, b = 0.0f;
-            if (ch < DV && f < DK) a = S[f * DV + ch], b = S[(f + 1) * DV + ch];
-            split_pair<KIND>(a * scale, b * scale, &hi[s][r], &lo[s][r]);
-        }
+    ldmatrix_x4(smem_u32(rows + (m0 + (lane & 15)) * pitch + (k0 + (lane >> 4) * 8) * 2), r[0], r[1], r[2], r[3]);
+}
+__device__ __forceinline__ void state_a_transposed(const unsigned char* rows, int pitch, int m0, int k0, int lane, uint32_t (&r)[4])
+{
+    const int row = k0 + (lane & 7) + ((lane >> 4) & 1) * 8, col = m0 + ((lane >> 3) & 1) * 8;
+    ldmatrix_x4_trans(smem_u32(rows + row * pitch + col * 2), r[0], r[1], r[2], r[3]);
 }
 
 // B fragments of two groups of eight tokens, contraction over channels k0 .. k0 + 15 of rows [token][channel].
@@ -192,10 +200,12 @@ __device__ __forceinline__ uint32_t transposed_at(const unsigned char* tile, int
 // ---------------------------------------------------------------------------------------------
 // First stream.  GRAD: Q, dY -> dQ, partial dS | dz.  Without GRAD: K, V -> partial S | z (the state itself, for a
 // backward pass that was given none).  grid (chunks, slabs); a CTA works through its chunk's tiles.  A warp owns
-// 16 features: it holds its rows of S (head, tail) and of dS in registers, so the products of a tile are
+// 16 features, whose rows of dS stay in its registers:
 //     t^T [16 x TILE] = S [16 x dv] dY^T         and        dS [16 x dv] += (w f)^T [16 x TILE] dY
-// and the accumulators of the first have the layout of the second's left operand: phi, the quotient and the
-// difference are done where the numbers lie, and only the two sums per token (den and f . t) cross warps.
+// The accumulators of the first have the layout of the second's left operand: phi, the quotient and the
+// difference are done where the numbers lie, and only the two sums per token (den and f . t) cross warps, between two
+// passes over the tile's groups of 16 tokens.  S stays in shared memory and the loops over groups and k steps stay loops:
+// unrolled, with S in registers, the code was some 90 KB, which a call of one tile per CTA spent its time fetching.
 // ---------------------------------------------------------------------------------------------
 template <int DK, int DV, int KIND, bool GRAD>
 __global__ void __launch_bounds__(32 * BackwardCfg<DK, DV>::WQ)
@@ -204,9 +214,13 @@ backward_state_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* 
                       SlabLayout Lv, BackwardScales sc, uint32_t* __restrict__ clear_status)
 {
     using C = BackwardCfg<DK, DV>;
-    constexpr int TILE = C::TILE, THREADS = 32 * C::WQ, NT = TILE / 8;
+    constexpr int TILE = C::TILE, THREADS = 32 * C::WQ;
     extern __shared__ __align__(16) unsigned char smem[];
-    float2* sums = reinterpret_cast<float2*>(smem + 2 * C::STAGE);  // [WQ][TILE]
+    unsigned char* s_rows = smem + 2 * C::STAGE;
+    float* z = reinterpret_cast<float*>(s_rows + 2 * C::S_HALF);
+    float2* sums = reinterpret_cast<float2*>(z + C::KP);        // [WQ][TILE]: den and f . t of a warp's features
+    float2* wc = sums + C::WQ * TILE;                           // [TILE]: w and c
+    float4* kept = reinterpret_cast<float4*>(wc + TILE);        // t, as the threads hold it: [WQ][TILE / 8][lane]
     __shared__ float scratch[33];
     const int slab = blockIdx.y, chunk = blockIdx.x, warp = threadIdx.x / 32, lane = threadIdx.x & 31, m0 = warp * 16;
     const int tiles = (N + TILE - 1) / TILE;
@@ -231,13 +245,9 @@ backward_state_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* 
     };
     if (t_begin < t_end) fetch(t_begin);
 
-    uint32_t s_hi[C::VP / 16][4], s_lo[C::VP / 16][4];
-    float z[2] = {0.0f, 0.0f};
     float unscale_t = 1.0f, scale_w = 1.0f;
     if (GRAD) {
         const float* S = state + static_cast<size_t>(slab) * grad_state_floats(DK, DV);
-        for (int r = 0; r < 2; ++r)
-            if (m0 + lane / 4 + 8 * r < DK) z[r] = S[DK * DV + m0 + lane / 4 + 8 * r];
         float scale_s = 1.0f;
         if (sc.scaled) {
             // fp16: S and w f by powers of two that keep head and tail inside the format.  w f is at most 1 / min z
@@ -257,7 +267,7 @@ backward_state_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* 
             unscale_t = 1.0f / scale_s;
             if (sc.eps >= 0.0f) scale_w = fmaxf(pow2_scale(z_inv, 12), 1.0f / pow2_scale(z_max, 4));
         }
-        load_state_rows<KIND, DK, DV>(S, m0, lane, scale_s, s_hi, s_lo);
+        load_state<KIND, DK, DV, THREADS>(S, s_rows, z, scale_s);
     }
     float acc[C::VP / 8][4];
 #pragma unroll
@@ -268,87 +278,110 @@ backward_state_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* 
 
     for (int t = t_begin; t < t_end; ++t) {
         cp_async_wait_all();
-        __syncthreads();  // the tile has landed, and everybody is done with the other stage
+        __syncthreads();  // the tile has landed (and S is in place), and everybody is done with the other stage
         if (t + 1 < t_end) fetch(t + 1);
         unsigned char* tq = smem + (t & 1) * C::STAGE;
         unsigned char* tg = tq + TILE * C::PITCHK;
-
-        float tt[NT][4];
+        float zr[2] = {0.0f, 0.0f};
         if (GRAD) {
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) tt[j][i] = 0.0f;
-#pragma unroll
-            for (int s = 0; s < C::VP / 16; ++s)
-#pragma unroll
-                for (int j = 0; j < NT; j += 2) {
-                    uint32_t b[4];
+            zr[0] = z[m0 + lane / 4];
+            zr[1] = z[m0 + lane / 4 + 8];
+#pragma unroll 1
+            for (int j = 0; j < TILE / 8; j += 2) {  // 16 tokens
+                float tt[2][4] = {};
+#pragma unroll 2
+                for (int s = 0; s < C::VP / 16; ++s) {
+                    uint32_t hi[4], lo[4], b[4];
+                    state_a(s_rows, C::PITCHV, m0, s * 16, lane, hi);
+                    state_a(s_rows + C::S_HALF, C::PITCHV, m0, s * 16, lane, lo);
                     tokens_b(tg, C::PITCHV, j * 8, s * 16, lane, b);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        mma_16816<KIND>(tt[j + h], s_lo[s][0], s_lo[s][1], s_lo[s][2], s_lo[s][3], b[2 * h], b[2 * h + 1]);
-                        mma_16816<KIND>(tt[j + h], s_hi[s][0], s_hi[s][1], s_hi[s][2], s_hi[s][3], b[2 * h], b[2 * h + 1]);
+                        mma_16816<KIND>(tt[h], lo[0], lo[1], lo[2], lo[3], b[2 * h], b[2 * h + 1]);
+                        mma_16816<KIND>(tt[h], hi[0], hi[1], hi[2], hi[3], b[2 * h], b[2 * h + 1]);
                     }
                 }
-        }
-        uint32_t x[NT][2];  // the warp's features of the tile's tokens, transposed
 #pragma unroll
-        for (int j = 0; j < NT; j += 2)
-            ldmatrix_x4_trans(transposed_at(tq, C::PITCHK, j * 8, m0, lane), x[j][0], x[j][1], x[j + 1][0], x[j + 1][1]);
-
-        if (GRAD && sc.eps >= 0.0f) {
+                for (int h = 0; h < 2; ++h)
+                    kept[(warp * (TILE / 8) + j + h) * 32 + lane] = make_float4(tt[h][0], tt[h][1], tt[h][2], tt[h][3]);
+                if (sc.eps >= 0.0f) {
+                    uint32_t x[4];
+                    ldmatrix_x4_trans(transposed_at(tq, C::PITCHK, j * 8, m0, lane), x[0], x[1], x[2], x[3]);
+                    float part[8];  // den and f . t of the thread's four tokens
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
+                    for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {  // the thread's two tokens of the group
+                        for (int e = 0; e < 2; ++e) {
+                            float den = 0.0f, ft = 0.0f;
+#pragma unroll
+                            for (int r = 0; r < 2; ++r) {
+                                const float f = phi<KIND>(e == 0 ? pair_lo<KIND>(x[2 * h + r]) : pair_hi<KIND>(x[2 * h + r]));
+                                den = fmaf(f, zr[r], den);
+                                ft = fmaf(f, tt[h][2 * r + e], ft);
+                            }
+                            part[4 * h + 2 * e] = den;
+                            part[4 * h + 2 * e + 1] = ft;
+                        }
+                    // over the eight lanes of a column: the eight numbers are halved with the lanes, one is left in each
+#pragma unroll
+                    for (int o = 16, n = 4; o >= 4; o >>= 1, n >>= 1) {
+                        const bool up = (lane & o) != 0;
+#pragma unroll
+                        for (int i = 0; i < n; ++i) {
+                            const float keep = up ? part[i + n] : part[i], send = up ? part[i] : part[i + n];
+                            part[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+                        }
+                    }
+                    // lane bits 4, 3, 2: group of eight tokens, odd token, f . t
+                    const int tok = (j + (lane >> 4)) * 8 + 2 * (lane & 3) + ((lane >> 3) & 1);
+                    reinterpret_cast<float*>(sums + warp * TILE + tok)[(lane >> 2) & 1] = part[0];
+                }
+            }
+            if (sc.eps >= 0.0f) {
+                __syncthreads();
+                for (int i = threadIdx.x; i < TILE; i += THREADS) {
                     float den = 0.0f, ft = 0.0f;
 #pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const float v = e == 0 ? pair_lo<KIND>(x[j][r]) : pair_hi<KIND>(x[j][r]);
-                        const float f = phi<KIND>(v);
-                        den = fmaf(f, z[r], den);
-                        ft = fmaf(f, tt[j][2 * r + e], ft);
+                    for (int k = 0; k < C::WQ; ++k) {
+                        const float2 o = sums[k * TILE + i];
+                        den += o.x;
+                        ft += o.y;
                     }
-#pragma unroll
-                    for (int o = 4; o < 32; o <<= 1) {
-                        den += __shfl_xor_sync(0xffffffffu, den, o);
-                        ft += __shfl_xor_sync(0xffffffffu, ft, o);
-                    }
-                    if (lane < 4) sums[warp * TILE + j * 8 + 2 * lane + e] = make_float2(den, ft);
+                    const bool in = t * TILE + i < N;
+                    const float w = in ? 1.0f / (den + sc.eps) : 0.0f;
+                    wc[i] = make_float2(w, in ? ft * w : 0.0f);  // c scaled as S is
                 }
-            __syncthreads();
+                __syncthreads();
+            }
         }
-#pragma unroll
-        for (int j = 0; j < NT; j += 2) {
-            uint32_t a_hi[4], a_lo[4], out[4];
+#pragma unroll 1
+        for (int j = 0; j < TILE / 8; j += 2) {
+            uint32_t x[4], a_hi[4], a_lo[4], out[4];
+            const uint32_t at = transposed_at(tq, C::PITCHK, j * 8, m0, lane);
+            ldmatrix_x4_trans(at, x[0], x[1], x[2], x[3]);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
+                float4 tt = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (GRAD) tt = kept[(warp * (TILE / 8) + j + h) * 32 + lane];
+                const float tv[4] = {tt.x, tt.y, tt.z, tt.w};
                 float wf[2][2], d[2][2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int tok = (j + h) * 8 + 2 * (lane & 3) + e;
-                    const bool in = t * TILE + tok < N;
-                    float w = in ? 1.0f : 0.0f, c = 0.0f;
+                    float w = t * TILE + tok < N ? 1.0f : 0.0f, c = 0.0f;
                     if (GRAD && sc.eps >= 0.0f) {
-                        float den = 0.0f, ft = 0.0f;
-#pragma unroll
-                        for (int i = 0; i < C::WQ; ++i) {
-                            const float2 o = sums[i * TILE + tok];
-                            den += o.x;
-                            ft += o.y;
-                        }
-                        w = in ? 1.0f / (den + sc.eps) : 0.0f;
-                        c = in ? ft * w : 0.0f;  // scaled as S is
+                        const float2 o = wc[tok];
+                        w = o.x;
+                        c = o.y;
                     }
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        const float v = e == 0 ? pair_lo<KIND>(x[j + h][r]) : pair_hi<KIND>(x[j + h][r]);
+                        const float v = e == 0 ? pair_lo<KIND>(x[2 * h + r]) : pair_hi<KIND>(x[2 * h + r]);
                         float f, slope;
                         phi_and_slope<KIND>(v, &f, &slope);
                         wf[r][e] = w * f;
                         if (GRAD) {
-                            d[r][e] = slope * (w * ((tt[j + h][2 * r + e] - c * z[r]) * unscale_t));
+                            d[r][e] = slope * (w * ((tv[2 * r + e] - c * zr[r]) * unscale_t));
                             dz[r] = fmaf(-wf[r][e], c * unscale_t, dz[r]);
                         } else {
                             dz[r] += wf[r][e];
@@ -361,7 +394,7 @@ backward_state_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* 
                     if (GRAD) out[2 * h + r] = pack_pair<KIND>(d[r][0], d[r][1]);
                 }
             }
-            if (GRAD) stmatrix_x4_trans(transposed_at(tq, C::PITCHK, j * 8, m0, lane), out[0], out[1], out[2], out[3]);
+            if (GRAD) stmatrix_x4_trans(at, out[0], out[1], out[2], out[3]);
 #pragma unroll
             for (int n = 0; n < C::VP / 16; ++n) {
                 uint32_t b[4];
@@ -443,10 +476,12 @@ backward_kv_kernel(const __nv_bfloat16* __restrict__ k, const __nv_bfloat16* __r
                    SlabLayout Lv, BackwardScales sc, uint32_t* __restrict__ clear_status)
 {
     using C = BackwardCfg<DK, DV>;
-    constexpr int TILE = C::TILE, THREADS = 32 * C::WKV, NT = TILE / 8;
+    constexpr int TILE = C::TILE, THREADS = 32 * C::WKV;
     extern __shared__ __align__(16) unsigned char smem[];
-    unsigned char* f_hi = smem + 2 * C::STAGE;
+    unsigned char* s_rows = smem + 2 * C::STAGE;
+    unsigned char* f_hi = s_rows + 2 * C::S_HALF;
     unsigned char* f_lo = f_hi + TILE * C::PITCHK;
+    float* z = reinterpret_cast<float*>(f_lo + TILE * C::PITCHK);
     __shared__ float scratch[33];
     const int slab = blockIdx.y, chunk = blockIdx.x, warp = threadIdx.x / 32, lane = threadIdx.x & 31, m0 = warp * 16;
     const int tiles = (N + TILE - 1) / TILE;
@@ -479,12 +514,7 @@ backward_kv_kernel(const __nv_bfloat16* __restrict__ k, const __nv_bfloat16* __r
         scale = pow2_scale(block_max(big, scratch, C::WKV), 12);
     }
     const float unscale = 1.0f / scale;
-    uint32_t r_hi[C::VP / 16][4], r_lo[C::VP / 16][4], c_hi[C::KP / 16][4], c_lo[C::KP / 16][4];
-    load_state_rows<KIND, DK, DV>(S, m0, lane, scale, r_hi, r_lo);
-    load_state_cols<KIND, DK, DV>(S, m0, lane, scale, c_hi, c_lo);
-    float dz[2] = {0.0f, 0.0f};
-    for (int r = 0; r < 2; ++r)
-        if (m0 + lane / 4 + 8 * r < DK) dz[r] = S[DK * DV + m0 + lane / 4 + 8 * r];
+    load_state<KIND, DK, DV, THREADS>(S, s_rows, z, scale);
 
     for (int t = t_begin; t < t_end; ++t) {
         cp_async_wait_all();
@@ -493,25 +523,22 @@ backward_kv_kernel(const __nv_bfloat16* __restrict__ k, const __nv_bfloat16* __r
         unsigned char* tk = smem + (t & 1) * C::STAGE;
         unsigned char* tv = tk + TILE * C::PITCHK;
         if (m0 < C::KP) {
-            float acc[NT][4];
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[j][i] = 0.0f;
-#pragma unroll
-            for (int s = 0; s < C::VP / 16; ++s)
-#pragma unroll
-                for (int j = 0; j < NT; j += 2) {
-                    uint32_t b[4];
+            const float dz[2] = {z[m0 + lane / 4], z[m0 + lane / 4 + 8]};
+#pragma unroll 1
+            for (int j = 0; j < TILE / 8; j += 2) {
+                float acc[2][4] = {};
+#pragma unroll 2
+                for (int s = 0; s < C::VP / 16; ++s) {
+                    uint32_t a_hi[4], a_lo[4], b[4];
+                    state_a(s_rows, C::PITCHV, m0, s * 16, lane, a_hi);
+                    state_a(s_rows + C::S_HALF, C::PITCHV, m0, s * 16, lane, a_lo);
                     tokens_b(tv, C::PITCHV, j * 8, s * 16, lane, b);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        mma_16816<KIND>(acc[j + h], r_lo[s][0], r_lo[s][1], r_lo[s][2], r_lo[s][3], b[2 * h], b[2 * h + 1]);
-                        mma_16816<KIND>(acc[j + h], r_hi[s][0], r_hi[s][1], r_hi[s][2], r_hi[s][3], b[2 * h], b[2 * h + 1]);
+                        mma_16816<KIND>(acc[h], a_lo[0], a_lo[1], a_lo[2], a_lo[3], b[2 * h], b[2 * h + 1]);
+                        mma_16816<KIND>(acc[h], a_hi[0], a_hi[1], a_hi[2], a_hi[3], b[2 * h], b[2 * h + 1]);
                     }
                 }
-#pragma unroll
-            for (int j = 0; j < NT; j += 2) {
                 uint32_t x[4], hi[4], lo[4], out[4];
                 const uint32_t at = transposed_at(tk, C::PITCHK, j * 8, m0, lane);
                 ldmatrix_x4_trans(at, x[0], x[1], x[2], x[3]);
@@ -522,8 +549,8 @@ backward_kv_kernel(const __nv_bfloat16* __restrict__ k, const __nv_bfloat16* __r
                     phi_and_slope<KIND>(pair_lo<KIND>(x[i]), &f0, &s0);
                     phi_and_slope<KIND>(pair_hi<KIND>(x[i]), &f1, &s1);
                     split_pair<KIND>(f0, f1, &hi[i], &lo[i]);
-                    out[i] = pack_pair<KIND>(s0 * fmaf(acc[j + i / 2][2 * r], unscale, dz[r]),
-                                             s1 * fmaf(acc[j + i / 2][2 * r + 1], unscale, dz[r]));
+                    out[i] = pack_pair<KIND>(s0 * fmaf(acc[i / 2][2 * r], unscale, dz[r]),
+                                             s1 * fmaf(acc[i / 2][2 * r + 1], unscale, dz[r]));
                 }
                 stmatrix_x4_trans(transposed_at(f_hi, C::PITCHK, j * 8, m0, lane), hi[0], hi[1], hi[2], hi[3]);
                 stmatrix_x4_trans(transposed_at(f_lo, C::PITCHK, j * 8, m0, lane), lo[0], lo[1], lo[2], lo[3]);
@@ -532,31 +559,27 @@ backward_kv_kernel(const __nv_bfloat16* __restrict__ k, const __nv_bfloat16* __r
         }
         __syncthreads();  // phi(K) and dK are in place; V has been read
         if (m0 < C::VP) {
-            float acc[NT][4];
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[j][i] = 0.0f;
-#pragma unroll
-            for (int s = 0; s < C::KP / 16; ++s)
-#pragma unroll
-                for (int j = 0; j < NT; j += 2) {
-                    uint32_t b[4], bl[4];
+#pragma unroll 1
+            for (int j = 0; j < TILE / 8; j += 2) {
+                float acc[2][4] = {};
+#pragma unroll 2
+                for (int s = 0; s < C::KP / 16; ++s) {
+                    uint32_t a_hi[4], a_lo[4], b[4], bl[4];
+                    state_a_transposed(s_rows, C::PITCHV, m0, s * 16, lane, a_hi);
+                    state_a_transposed(s_rows + C::S_HALF, C::PITCHV, m0, s * 16, lane, a_lo);
                     tokens_b(f_hi, C::PITCHK, j * 8, s * 16, lane, b);
                     tokens_b(f_lo, C::PITCHK, j * 8, s * 16, lane, bl);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        mma_16816<KIND>(acc[j + h], c_lo[s][0], c_lo[s][1], c_lo[s][2], c_lo[s][3], b[2 * h], b[2 * h + 1]);
-                        mma_16816<KIND>(acc[j + h], c_hi[s][0], c_hi[s][1], c_hi[s][2], c_hi[s][3], bl[2 * h], bl[2 * h + 1]);
-                        mma_16816<KIND>(acc[j + h], c_hi[s][0], c_hi[s][1], c_hi[s][2], c_hi[s][3], b[2 * h], b[2 * h + 1]);
+                        mma_16816<KIND>(acc[h], a_lo[0], a_lo[1], a_lo[2], a_lo[3], b[2 * h], b[2 * h + 1]);
+                        mma_16816<KIND>(acc[h], a_hi[0], a_hi[1], a_hi[2], a_hi[3], bl[2 * h], bl[2 * h + 1]);
+                        mma_16816<KIND>(acc[h], a_hi[0], a_hi[1], a_hi[2], a_hi[3], b[2 * h], b[2 * h + 1]);
                     }
                 }
-#pragma unroll
-            for (int j = 0; j < NT; j += 2) {
                 uint32_t out[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    out[i] = pack_pair<KIND>(acc[j + i / 2][2 * (i & 1)] * unscale, acc[j + i / 2][2 * (i & 1) + 1] * unscale);
+                    out[i] = pack_pair<KIND>(acc[i / 2][2 * (i & 1)] * unscale, acc[i / 2][2 * (i & 1) + 1] * unscale);
                 stmatrix_x4_trans(transposed_at(tv, C::PITCHV, j * 8, m0, lane), out[0], out[1], out[2], out[3]);
             }
         }

@@ -12,8 +12,8 @@
 //
 // A tile is one MMA tile: thread r of a warpgroup owns token r.  It reads its row from the swizzled stage, applies phi, and
 // needs nothing from other threads but the products' rows in tensor memory (its own lane): no shuffles for den, f . t or c.
-// Two (pairs of) warpgroups take turns at the tiles, a warp loads by TMA into a ring of five
-// tiles (32 KB each), a warp issues the MMAs, a warp sends gradients out:
+// Two warpgroups take turns at the tiles, a warp loads by TMA into a ring of five tiles (32 KB each), a warp issues the
+// MMAs, a warp sends gradients out:
 //
 //   state:  T[128 x 64]  = dY S^T             (hi, then lo: 8 steps of K = 16, dY straight from the stage)
 //           D[128 x 64] += [F_hi | F_lo]^T dY (F = w phi(q); head and tail are the two halves of M = 128: 8 steps)
@@ -36,9 +36,8 @@ namespace lf {
 
 constexpr int kTcTile = 128, kTcTileBytes = kTcTile * 128;  // one tensor's tile: 16 KB
 struct BackwardTc {
-    // kv: two warpgroups, a thread has a token's whole row.  state: two pairs of warpgroups, a thread has half a row (its
-    // chain of phi, two sums and the difference is the longer one: with 8 consumer warps it ran at a third of an instruction
-    // per clock and scheduler and took 511 us where 16 take 3xx, at 40 slabs x 131072).
+    // Two warpgroups, a thread has a token's whole row.  (Four in the state kernel, two threads a row: 562 us where this takes
+    // 517, at 40 slabs x 131072: the threads' chains are shorter, but half of each crosses a shuffle or shared memory.)
     static constexpr int KV_WARPS = 8, KV_THREADS = 32 * (KV_WARPS + 3);
     static constexpr int STATE_WARPS = 8, STATE_THREADS = 32 * (STATE_WARPS + 3);
     static constexpr int STAGE_BYTES = 2 * kTcTileBytes;

@@ -75,8 +75,8 @@ struct RopeParams {
 
 // Sine and cosine of r turns: the nearest quarter turn q is taken off exactly, the rest is at most 1/8 turn (pi / 4), where
 // the Taylor series to x^9 and x^10 are off by 2e-9 and 1e-10; then q swaps and signs them.  About thirty instructions,
-// where sincospif, inlined for every channel, was most of the kernel's work (21 against 10 us where each is used for eight
-// heads).
+// fewer than sincospif takes with its own reduction (18.8 against 19.2 us for B = 3, N = 2531, 16 heads of 80, while each value
+// was computed once for eight heads).
 __device__ __forceinline__ void rope_sincos(float pos, float hi, float lo, float sign, float* s, float* c)
 {
     const float p = pos * hi;
@@ -125,7 +125,7 @@ __device__ __forceinline__ uint4 gather_pieces(const char* const (&p)[8 / W], lo
 //   W = 4, 2, 1        P is a multiple of W only: a thread makes one 16-byte piece of the output, whatever roles its
 //                      channels have, from its own channels and their partners, P further or P back, which it gathers in pieces
 //                      of W elements (they lie in lines that its neighbours fetch).  Stores stay whole; no warp splits into
-//                      first, second and copied channels, which cost 26 us where this takes xx (B = 3, N = 2531, 16 heads of 80,
+//                      first, second and copied channels, which cost 27 us where this takes 16.5 (B = 3, N = 2531, 16 heads of 80,
 //                      P = 30).  In place, the block's threads load before any of them stores: it holds whole rows.
 constexpr int kRopeInterleaved = 16, kRopeHalves = 8;
 
@@ -286,8 +286,8 @@ __global__ void __launch_bounds__(kRopeThreads, 4) rope_kernel(const __grid_cons
 // whatever the row's mean.  Two quantities (the two norms of a row, or two sums) travel together, one in each half of the
 // warp: halving the values while the lanes are halved costs five shuffles instead of ten.
 //
-// What bounds them: DRAM at large C x rows; behind it the issue slots (about 300 instructions per 8 channels of a
-// warp in the backward pass before packed fp32x2 arithmetic, which halves the multiply-adds).
+// What bounds them: DRAM at large C x rows; behind it the issue slots (365 instructions per row and
+// warp in the backward pass of both norms; 560 before packed fp32x2 arithmetic, which halves the multiply-adds).
 // ---------------------------------------------------------------------------------------------
 constexpr int kNormNone = 0, kNormLayer = 1, kNormRms = 2;
 constexpr int kNormMaxWarps = 16;  // of a group: a half warp holds one value of each
