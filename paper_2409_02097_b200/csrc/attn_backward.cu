@@ -41,23 +41,32 @@ constexpr int kPlanSms = 148;  // a B200's, where no count is given
 struct BackwardPlan {
     int slabs, dk, dv, floats;  // floats of S | z of a slab
     int chunks_q, chunks_kv;    // CTAs per slab of the two streams
-    int tc;                     // the tcgen05 kernels: 0 (not), 1 (widths up to 64), 2 (features up to 128)
+    int tc;                     // the tcgen05 kernels' cut: 0 (none for these widths), 1 (40 or 64 channels), 2 (features up to 128)
+    bool tc_state, tc_q, tc_kv; // the streams that they take
     size_t tc_partial;          // ... floats of a partial
     int tiles_per_slab, ctas, spans;  // ... their tiles of a slab, CTAs, and slabs that a CTA meets at most
     long long tiles;
     size_t partials_off, state_off, grad_off, total;  // behind a status word
 };
 
+// CTAs per slab of the warp-level kernels: the fewest whose longest run of tiles ends first, with as many CTAs at a time
+// as shared memory admits and a tile's time for laying out the state.  (Filling the SMs regardless of where tiles and waves
+// end cost 41 us where this takes 31 at 20 slabs x 1024 x 64, 57 where this takes 40 at 128 x 256 x 64.)
 template <int DK, int DV>
 void plan_chunks(const linfusion_attn_desc_t& d, int sm_count, BackwardPlan* p)
 {
     using C = BackwardCfg<DK, DV>;
-    // CTAs that an SM holds: two at most of the wide ones by registers, three of the narrow ones.
-    const int per_sm = C::WQ <= 4 ? 3 : C::WQ <= 6 ? 2 : 1;
-    const int tiles = (d.N + C::TILE - 1) / C::TILE;
-    int chunks = (per_sm * sm_count + p->slabs - 1) / p->slabs;
-    chunks = chunks > tiles ? tiles : chunks;
-    p->chunks_q = p->chunks_kv = chunks < 1 ? 1 : chunks;
+    constexpr int kSmem = C::SMEM_Q > C::SMEM_KV ? C::SMEM_Q : C::SMEM_KV, kPerSm = 228 * 1024 / (kSmem + 1024);
+    const long long tiles = (d.N + C::TILE - 1) / C::TILE, at_once = static_cast<long long>(kPerSm) * sm_count;
+    long long best = 0;
+    p->chunks_q = p->chunks_kv = 1;
+    for (long long c = 1; c <= tiles && (c == 1 || p->slabs * (c - 1) < at_once); ++c) {
+        const long long longest = (tiles + c - 1) / c, cost = (p->slabs * c + at_once - 1) / at_once * (longest + 1);
+        if (c == 1 || cost < best) {
+            best = cost;
+            p->chunks_q = p->chunks_kv = static_cast<int>(c);
+        }
+    }
 }
 
 #define LF_DISPATCH_WIDTHS(dk, dv, CALL)  \
@@ -74,25 +83,34 @@ void plan_chunks(const linfusion_attn_desc_t& d, int sm_count, BackwardPlan* p)
         default: break;                    \
     }
 
-// Where the tcgen05 kernels take over from the warp-level ones (whole backward pass, us, tcgen05 / warp-level):
-//   widths up to 64, from 1.75 tiles of 128 tokens per SM on: 41 / 53 at 128 slabs x 256 x 64, 38 / 36 at 16 x 2048 x 40,
-//   39 / 30 at 20 x 1024 x 64, 43 / 51 at 20 x 2048 x 64, 53 / 72 at 20 x 4096 x 64
-//   features up to 128, by the work, which the warp-level kernels feel more: 76 / 82 at 16 x 1024 x 128, 70 / 55 at 16 x 512 x
-//   128, 68 / 60 at 16 x 2048 x 80, 353 / 658 at 16 x 32768 x 80, 244 / 746 at 16 x 16384 x 128
-// and not where slabs are so short that a CTA changes its state every tile or two.
+// Which streams the tcgen05 kernels take (us, tcgen05 / warp-level, slabs x N x widths; a replayed graph of the stream alone):
+//   state   15 / 16 at 20 x 4096 x 64, 13 / 10 at 20 x 2048 x 64, 67 / 149 at 16 x 65536 x 64; 58 / 67 at 16 x 16384 x 128,
+//           41 / 39 at 16 x 8192 x 128; 79 / 84 at 16 x 32768 x 80, 50 / 46 at 16 x 16384 x 80
+//   q       16.4 / 17.1 at 20 x 2048 x 64, 14.7 / 11.4 at 20 x 1024 x 64, 111 / 222 at 16 x 65536 x 64; 72 / 86 at 16 x 8192 x 128,
+//           51 / 48 at 16 x 4096 x 128; 72 / 80 at 16 x 16384 x 80/40, but 164 / 156 at 16 x 32768 x 80, whose 80 are padded to 128 twice
+//   kv      12.6 / 19.6 at 20 x 4096 x 64, 6.3 / 7.4 at 128 x 64 x 64; 12.9 / 14.9 at 16 x 1024 x 128, 12.3 / 9.3 at 16 x 512 x 128
+// Widths of 32, padded to 64: 123 / 105, 211 / 168, 181 / 146 at 32 x 65536.  Short slabs: where a CTA changes its state every
+// tile, state and q take 73 / 15 and 91 / 41 at 1024 x 128 x 64, 245 / 44 and 327 / 115 at 1024 x 128 x 128, kv still 27 / 40 and
+// 82 / 113, but 25 / 21 at 1024 x 16 x 64.
 void plan_tc(const linfusion_attn_desc_t& d, int sm_count, BackwardPlan* p)
 {
     p->tiles_per_slab = (d.N + kTcTile - 1) / kTcTile;
     p->tiles = static_cast<long long>(p->slabs) * p->tiles_per_slab;
-    p->tc = 0;
-    if (p->dk <= 64 && p->dv <= 64) {
-        if (p->tiles_per_slab >= 2 && 4 * p->tiles >= 7ll * sm_count) p->tc = 1;
-    } else if (p->dk <= 128 && p->dv <= 128) {
-        const long long work = static_cast<long long>(p->slabs) * d.N * p->dk * p->dv;
-        if (p->tiles_per_slab >= 4 && work >= 1800000ll * sm_count) p->tc = 2;
+    p->tc = p->dk <= 32 && p->dv <= 32 ? 0 : p->dk <= 64 && p->dv <= 64 ? 1 : p->dk <= 128 && p->dv <= 128 ? 2 : 0;
+    p->tc_state = p->tc_q = p->tc_kv = false;
+    const double work = static_cast<double>(p->slabs) * d.N * p->dk * p->dv / sm_count, tiles = static_cast<double>(p->tiles) / sm_count;
+    if (p->tc == 1) {
+        p->tc_state = p->tiles_per_slab >= 16 && work >= 2.2e6;
+        p->tc_q = p->tiles_per_slab >= 4 && work >= 1e6;
+        p->tc_kv = d.N >= 64;
+    } else if (p->tc == 2) {
+        const bool padded = p->dk < 128;
+        p->tc_state = p->tiles_per_slab >= 16 && tiles >= (p->dv <= 64 ? 4.0 : padded ? 16.0 : 8.0);
+        p->tc_q = p->tiles_per_slab >= 8 && tiles >= (padded ? 12.0 : p->dv <= 64 ? 3.0 : 4.0) && !(padded && p->dv > 64);
+        p->tc_kv = d.N >= 64 && tiles >= 0.75;
     }
     p->tc_partial = p->tc == 1 ? BackwardTc::PARTIAL_FLOATS : p->dv > 64 ? BackwardTcWide<2>::PARTIAL_FLOATS : BackwardTcWide<1>::PARTIAL_FLOATS;
-    if (!p->tc) return;
+    if (!(p->tc_state || p->tc_q || p->tc_kv)) return;
     p->ctas = static_cast<int>(p->tiles < sm_count ? p->tiles : sm_count);
     // The same number of CTAs on every slab where that keeps four fifths of the SMs busy and runs are short: a CTA that
     // meets a second slab fetches another state and hands back another partial, 4 us of a run of a few tiles.
@@ -126,8 +144,9 @@ linfusion_status_t make_backward_plan(const linfusion_attn_desc_t* desc, int sm_
     p->state_off = 256;
     p->grad_off = p->state_off + state;
     p->partials_off = p->grad_off + state;
-    p->total = p->partials_off + align_up_256(p->tc ? static_cast<size_t>(p->ctas) * p->spans * p->tc_partial * sizeof(float)
-                                                    : slab_state * static_cast<size_t>(p->chunks_q));
+    const size_t warp_level = slab_state * static_cast<size_t>(p->chunks_q);
+    const size_t tc = p->tc_state || p->tc_q ? static_cast<size_t>(p->ctas) * p->spans * p->tc_partial * sizeof(float) : 0;
+    p->total = p->partials_off + align_up_256(p->tc_state && p->tc_q || tc > warp_level ? tc : warp_level);
     return LINFUSION_OK;
 }
 
@@ -282,7 +301,7 @@ cudaError_t run_state(const linfusion_attn_desc_t& d, const BackwardPlan& p, con
     cudaError_t e = cudaErrorInvalidValue;
     uint32_t* status = reinterpret_cast<uint32_t*>(ws);
     float* partials = reinterpret_cast<float*>(ws + p.partials_off);
-    if (p.tc) {
+    if (GRAD ? p.tc_q : p.tc_state) {
 #define LF_KIND(KV) e = launch_tc_state<KV, GRAD>(d, p, q, dy, state, dq, partials, out, status, first, s)
         LF_DISPATCH_KINDS(kernel_kind(d), LF_KIND)
 #undef LF_KIND
@@ -305,7 +324,7 @@ cudaError_t run_kv(const linfusion_attn_desc_t& d, const BackwardPlan& p, const 
 {
     cudaError_t e = cudaErrorInvalidValue;
     uint32_t* status = reinterpret_cast<uint32_t*>(ws);
-    if (p.tc) {
+    if (p.tc_kv) {
 #define LF_KIND(KV) e = launch_tc_kv<KV>(d, p, k, v, grad_state, dk, dv, status, first, s)
         LF_DISPATCH_KINDS(kernel_kind(d), LF_KIND)
 #undef LF_KIND

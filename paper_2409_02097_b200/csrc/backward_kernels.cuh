@@ -72,7 +72,9 @@ struct BackwardCfg {
     static constexpr int KP = (DK + 15) / 16 * 16, VP = (DV + 15) / 16 * 16;  // widths padded to the products' step
     static constexpr int WQ = KP / 16;                                       // warps: 16 features each
     static constexpr int WKV = (KP > VP ? KP : VP) / 16;                     // ... or 16 channels of dV
-    static constexpr int TILE = KP + VP <= 160 ? 64 : 32;                    // tokens at a time
+    // Tokens at a time, fewer where more CTAs then fit on an SM beside the state: 79 us with 16 against 96 with 32 at 16 slabs x
+    // 2048 x 128, 72 with 32 against 80 with 64 at 16 x 4096 x 80; 160 channels leave room for one CTA either way.
+    static constexpr int TILE = KP + VP <= 128 ? 64 : KP + VP <= 160 ? 32 : KP + VP <= 256 ? 16 : 32;
     // A row takes an odd number of 16-byte units: eight rows of a matrix fragment fall into different banks.
     static constexpr int PITCHK = ((KP / 8) | 1) * 16, PITCHV = ((VP / 8) | 1) * 16;
     static constexpr int STAGE = TILE * (PITCHK + PITCHV);

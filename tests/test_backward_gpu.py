@@ -96,6 +96,28 @@ def test_large_sizes(case, layout, dtype):
     op.close()
 
 
+# Sizes at which the tensor cores' kernels take the first stream (the state) too: runs of many tiles of one slab, and of a CTA
+# across slabs of 17 tiles each.
+LONG_CASES = [(2, 5, 8300, 64, 64), (5, 20, 2100, 64, 64), (1, 3, 70001, 40, 40), (2, 5, 16100, 32, 64), (1, 5, 15500, 128, 64),
+              (2, 7, 16300, 80, 40), (1, 5, 30400, 128, 128), (5, 20, 2100, 128, 128), (1, 7, 43400, 80, 80)]
+
+
+@pytest.mark.parametrize("dtype,layout", [("bf16", "head_major"), ("fp16", "token_major")])
+@pytest.mark.parametrize("case", LONG_CASES, ids=lambda c: "x".join(map(str, c)))
+def test_long_slabs(case, layout, dtype):
+    B, H, N, dk, dv = case
+    # gradients of a size that leaves dK and dV, sums of N terms of w dY, among fp16's normal numbers
+    tensors = _inputs(B, H, N, dk, dv, dtype, mean=0.5, grad_scale=64.0 if dtype == "fp16" else 1.0)
+    op = attn.LinFusionAttention(B, H, N, dv, eps=EPS, variant="split", layout=layout, dtype=dtype, d_qk=dk if dk != dv else 0)
+    given = [_major(t, layout) for t in tensors]
+    ws = torch.empty(op.backward_workspace_bytes(), dtype=torch.uint8, device="cuda")
+    got = op.backward(*given, workspace=ws)
+    assert op.backward_status(ws) == attn.OK
+    _check([_major(g, layout) for g in got], tensors, dtype, f"{case} {layout} {dtype}", rms=dtype == "bf16",
+           extra=_mean_term(dtype, N, 0.5))
+    op.close()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("d,N", [(64, 640_001), (128, 640_130)])
 def test_one_long_slab(d, N, dtype):
