@@ -168,7 +168,7 @@ cudaError_t launch_state(const linfusion_attn_desc_t& d, const BackwardPlan& p, 
                    slab_layout(d, DV), sc, clear);
     if (e != cudaSuccess || p.chunks_q == 1) return e;
 #define LF_REDUCE(S)                                                                                                               \
-    launch_pdl(backward_reduce_kernel<S>, dim3((p.floats + kReduceThreads / S - 1) / (kReduceThreads / S), p.slabs), dim3(kReduceThreads), 0, \
+    launch_pdl(backward_reduce_kernel<S>, dim3(reduce_blocks(p.floats, S), p.slabs), dim3(kReduceThreads), 0, \
                s, partials, out, p.floats, p.chunks_q)
     const int slices = reduce_slices_for(p.chunks_q);
     return slices == 1 ? LF_REDUCE(1) : slices == 4 ? LF_REDUCE(4) : LF_REDUCE(8);
@@ -256,7 +256,7 @@ cudaError_t launch_tc_state(const linfusion_attn_desc_t& d, const BackwardPlan& 
 #undef LF_STATE
     if (e != cudaSuccess) return e;
 #define LF_REDUCE(S)                                                                                                                  \
-    launch_pdl(backward_tc_reduce_kernel<S>, dim3((p.floats + kReduceThreads / S - 1) / (kReduceThreads / S), p.slabs), dim3(kReduceThreads), 0, \
+    launch_pdl(backward_tc_reduce_kernel<S>, dim3(reduce_blocks(p.floats, S), p.slabs), dim3(kReduceThreads), 0, \
                s, partials, out, p.dk, p.dv, p.tiles_per_slab, p.tiles, p.ctas, p.spans, p.dv <= 64 ? 64 : 128, p.tc)
     const int slices = reduce_slices_for(p.ctas / p.slabs + 1);
     return slices == 1 ? LF_REDUCE(1) : slices == 4 ? LF_REDUCE(4) : LF_REDUCE(8);

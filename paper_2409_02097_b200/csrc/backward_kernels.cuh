@@ -148,8 +148,12 @@ template <int KIND, int DK, int DV, int THREADS>
 __device__ __forceinline__ void load_state(const float* S, unsigned char* hi_rows, float* z, float scale)
 {
     using C = BackwardCfg<DK, DV>;
-    for (int i = threadIdx.x; i < C::KP * (C::VP / 8); i += THREADS) {
-        const int row = i / (C::VP / 8), piece = i - row * (C::VP / 8);
+    constexpr int PIECES = C::KP * (C::VP / 8);
+    // Unrolled, so that the loads are in flight together: one by one, ten of them were a third of a call of one tile.
+#pragma unroll
+    for (int n = 0; n < (PIECES + THREADS - 1) / THREADS; ++n) {
+        const int i = n * THREADS + threadIdx.x, row = i / (C::VP / 8), piece = i - row * (C::VP / 8);
+        if (PIECES % THREADS != 0 && i >= PIECES) break;
         float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f), y = x;
         if (row < DK && piece < DV / 8) {
             const float4* p = reinterpret_cast<const float4*>(S + row * DV + 8 * piece);
@@ -434,36 +438,39 @@ backward_state_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* 
 // SLICES-th chunk in order and are added in order.  Eight where a slab has many chunks (one thread for up to 444 of them took
 // 23 us), one where it has a few (eight made 66000 blocks of 128 slabs x 128 x 128: 307 against 94 us in all).
 constexpr int kReduceThreads = 256;
-__host__ __device__ constexpr int reduce_slices_for(int chunks) { return chunks <= 3 ? 1 : chunks <= 24 ? 4 : 8; }
+__host__ __device__ constexpr int reduce_slices_for(int chunks) { return chunks <= 3 ? 1 : chunks <= 6 ? 4 : 8; }
+__device__ __forceinline__ float4 add4(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
 template <int SLICES>
-__device__ __forceinline__ float reduce_slices(float sum, float* scratch)
+__device__ __forceinline__ float4 reduce_slices(float4 sum, float4* scratch)
 {
     if (SLICES == 1) return sum;
     constexpr int OUT = kReduceThreads / SLICES;
     scratch[threadIdx.x] = sum;
     __syncthreads();
-    sum = 0.0f;
+    sum = scratch[threadIdx.x % OUT];
 #pragma unroll
-    for (int i = 0; i < SLICES; ++i) sum += scratch[i * OUT + threadIdx.x % OUT];
+    for (int i = 1; i < SLICES; ++i) sum = add4(sum, scratch[i * OUT + threadIdx.x % OUT]);
     return sum;
 }
+// Blocks that write `floats` sums (a multiple of 8), four to a thread.
+__host__ __device__ constexpr int reduce_blocks(int floats, int slices) { return (floats / 4 + kReduceThreads / slices - 1) / (kReduceThreads / slices); }
 template <int SLICES>
 static __global__ void __launch_bounds__(kReduceThreads)
 backward_reduce_kernel(const float* __restrict__ partials, float* __restrict__ out, int floats, int chunks)
 {
     constexpr int OUT = kReduceThreads / SLICES;
-    __shared__ float scratch[kReduceThreads];
-    const int slice = threadIdx.x / OUT, i = blockIdx.x * OUT + threadIdx.x % OUT;
+    __shared__ float4 scratch[kReduceThreads];
+    const int slice = threadIdx.x / OUT, i = 4 * (blockIdx.x * OUT + threadIdx.x % OUT);
     pdl_launch_dependents();
     pdl_wait();
-    float s = 0.0f;
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (i < floats) {
         const float* p = partials + static_cast<size_t>(blockIdx.y) * chunks * floats + i;
 #pragma unroll 4
-        for (int c = slice; c < chunks; c += SLICES) s += p[static_cast<size_t>(c) * floats];
+        for (int c = slice; c < chunks; c += SLICES) s = add4(s, *reinterpret_cast<const float4*>(p + static_cast<size_t>(c) * floats));
     }
     s = reduce_slices<SLICES>(s, scratch);
-    if (slice == 0 && i < floats) out[static_cast<size_t>(blockIdx.y) * floats + i] = s;
+    if (slice == 0 && i < floats) *reinterpret_cast<float4*>(out + static_cast<size_t>(blockIdx.y) * floats + i) = s;
 }
 
 // ---------------------------------------------------------------------------------------------

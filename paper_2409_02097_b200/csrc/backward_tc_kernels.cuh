@@ -566,8 +566,8 @@ backward_tc_reduce_kernel(const float* __restrict__ partials, float* __restrict_
 {
     constexpr int AT_ONCE = kReduceThreads, OUT = kReduceThreads / SLICES;
     __shared__ long long where[AT_ONCE];  // of a contributing CTA's partial; -1: none
-    __shared__ float scratch[kReduceThreads];
-    const int slab = blockIdx.y, slice = threadIdx.x / OUT, i = blockIdx.x * OUT + threadIdx.x % OUT;
+    __shared__ float4 scratch[kReduceThreads];
+    const int slab = blockIdx.y, slice = threadIdx.x / OUT, i = 4 * (blockIdx.x * OUT + threadIdx.x % OUT);
     const int floats = grad_state_floats(dk, dv);
     const long long first = static_cast<long long>(slab) * tiles_per_slab, last = first + tiles_per_slab;
     // the CTA that holds the slab's first tile: the largest g with g W / G <= first
@@ -575,7 +575,8 @@ backward_tc_reduce_kernel(const float* __restrict__ partials, float* __restrict_
     const bool of_z = i >= dk * dv;
     const int row = of_z ? i - dk * dv : i / dv, col = of_z ? 0 : i - row * dv, a = row >> 6, ar = row & 63;
     const long long partial_floats = static_cast<long long>(atoms) * 128 * vw + 512;
-    float sum = 0.0f;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    auto at4 = [](const float* p) { return *reinterpret_cast<const float4*>(p); };
     bool waited = false;
     pdl_launch_dependents();
     for (int at = g0; at <= g1; at += AT_ONCE) {
@@ -597,17 +598,17 @@ backward_tc_reduce_kernel(const float* __restrict__ partials, float* __restrict_
                 if (where[k] < 0) continue;
                 const float* p = partials + where[k];
                 if (!of_z) {
-                    sum += p[(a * 128 + ar) * vw + col] + p[(a * 128 + 64 + ar) * vw + col];
+                    sum = add4(sum, add4(at4(p + (a * 128 + ar) * vw + col), at4(p + (a * 128 + 64 + ar) * vw + col)));
                 } else {
                     const float* z = p + atoms * 128 * vw + ar;
                     for (int w = a * 8 / atoms; w < (a + 1) * 8 / atoms; w += 4)
-                        sum += (z[w * 64] + z[(w + 1) * 64]) + (z[(w + 2) * 64] + z[(w + 3) * 64]);
+                        sum = add4(sum, add4(add4(at4(z + w * 64), at4(z + (w + 1) * 64)), add4(at4(z + (w + 2) * 64), at4(z + (w + 3) * 64))));
                 }
             }
         }
     }
     sum = reduce_slices<SLICES>(sum, scratch);
-    if (slice == 0 && i < floats) out[static_cast<size_t>(slab) * floats + i] = sum;
+    if (slice == 0 && i < floats) *reinterpret_cast<float4*>(out + static_cast<size_t>(slab) * floats + i) = sum;
 }
 
 template <int KIND>
