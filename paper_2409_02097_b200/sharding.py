@@ -1,9 +1,10 @@
-"""Token-sharded (sequence-parallel) forward across devices — the distributed inference of Sec. 4.3.
+"""Token-sharded (sequence-parallel) forward and backward across devices — the distributed inference of Sec. 4.3.
 
 Every rank owns a contiguous run of the N tokens of Q, K, V and Y.  Each rank builds the state
 S | z of its own K/V tokens, the ranks sum their states (one all-reduce of B*H*d*(d+1) floats,
 whatever N is — the "constant communication" the paper points out), and each rank applies the
-summed state to its own Q tokens.  The arithmetic is in the CUDA library (``attn``); this module
+summed state to its own Q tokens.  The backward pass has the same shape: a rank's Q and dY give its dQ and its
+part of the state's gradient, one all-reduce of as many floats, and its K and V give dK and dV.  The arithmetic is in the CUDA library (``attn``); this module
 only cuts the token range and calls the collective.
 """
 from __future__ import annotations
@@ -29,6 +30,15 @@ def sharded_forward(state_fn: Callable, apply_fn: Callable, allreduce_sum: Calla
     buf = state_fn(k, v)
     allreduce_sum(buf)
     return apply_fn(q)
+
+
+def sharded_backward(q_fn: Callable, kv_fn: Callable, allreduce_sum: Callable, q, k, v, dy):
+    """One layer's backward pass on one rank: ``q_fn(q, dy)`` returns dQ and this rank's part of the state's gradient,
+    ``allreduce_sum(buf)`` sums that over ranks in place, ``kv_fn(k, v, buf)`` returns (dK, dV) of the local tokens."""
+    dq, buf = q_fn(q, dy)
+    allreduce_sum(buf)
+    dk, dv = kv_fn(k, v, buf)
+    return dq, dk, dv
 
 
 class TokenShardedAttention:
@@ -118,6 +128,25 @@ class TokenShardedAttention:
             return out
 
         return sharded_forward(state_fn, apply_fn, allreduce_sum, q, k, v)
+
+    def save_state(self, out=None):
+        """A copy of the summed state that ``forward`` left, for ``backward``.  (``forward_peers`` and ``forward_symmetric``
+        sum while they apply and leave each rank its own part: after those call ``backward`` without a state.)"""
+        return self.op.save_state(out)
+
+    def backward(self, q, k, v, dy, state=None):
+        """(dq, dk, dv) of the local tokens.  ``state``: what ``save_state`` returned after this layer's ``forward``, on every
+        rank or on none; without it the state is recomputed from K and V and summed, which is a second exchange."""
+        import torch.distributed as dist
+
+        def allreduce_sum(buf):
+            if dist.is_available() and dist.is_initialized() and dist.get_world_size(self.group) > 1:
+                dist.all_reduce(buf, op=dist.ReduceOp.SUM, group=self.group)
+
+        if state is None:
+            state = self.op.backward_state(k, v)
+            allreduce_sum(state)
+        return sharded_backward(lambda q_, dy_: self.op.backward_q(q_, dy_, state), self.op.backward_kv, allreduce_sum, q, k, v, dy)
 
     def forward_peers(self, q, k, v, peer_state_ptrs, barrier: Callable[[], None], y=None, events=None):
         """The same layer with the cross-device sum done by the apply step itself instead of an

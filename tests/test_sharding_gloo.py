@@ -212,3 +212,87 @@ def test_forward_peers_keeps_its_two_barriers_around_the_peer_reads():
     np.testing.assert_allclose(y, oracle.linear(q, k, v, EPS), rtol=2e-5, atol=2e-6)
     with pytest.raises(RuntimeError):
         ranks[0][0].peer_state_ptrs()                    # needs the symmetric allocation
+
+
+class _BackwardOp(_StubOp):
+    """With the binding's backward members, in 64-bit formulas over fp32 state tensors."""
+
+    def save_state(self, out=None):
+        self.log.append("save_state")
+        return self._state_view().clone()
+
+    def backward_state(self, k, v):
+        self.log.append("backward_state")
+        S, z = oracle.state(k, v)
+        return torch.from_numpy(np.concatenate([S.reshape(self.slabs, -1), z], axis=1).astype(np.float32).reshape(-1))
+
+    def _split(self, state):
+        buf = state.numpy().astype(np.float64).reshape(self.slabs, -1)
+        return buf[:, :self.d * self.d].reshape(self.slabs, self.d, self.d), buf[:, self.d * self.d:]
+
+    def backward_q(self, q, dy, state):
+        self.log.append("backward_q")
+        S, z = self._split(state)
+        f = np.where(q > 0, q + 1, np.exp(q))
+        w = 1 / (np.einsum("sna,sa->sn", f, z) + EPS)
+        t = np.einsum("sne,sae->sna", dy, S)
+        c = np.einsum("sna,sna->sn", f, t) * w
+        dq = np.minimum(f, 1) * w[..., None] * (t - c[..., None] * z[:, None])
+        dS, dz = np.einsum("sna,sne->sae", w[..., None] * f, dy), -np.einsum("sna,sn->sa", f, w * c)
+        return dq, torch.from_numpy(np.concatenate([dS.reshape(self.slabs, -1), dz], axis=1).astype(np.float32).reshape(-1))
+
+    def backward_kv(self, k, v, grad_state):
+        self.log.append("backward_kv")
+        dS, dz = self._split(grad_state)
+        f = np.where(k > 0, k + 1, np.exp(k))
+        dk = np.minimum(f, 1) * (np.einsum("sne,sae->sna", v, dS) + dz[:, None])
+        return dk, np.einsum("sna,sae->sne", f, dS)
+
+
+def _backward_rank_main(rank, world, port, n, d, slabs, out_dir):
+    os.environ["MASTER_ADDR"] = "127.0.0.1"
+    os.environ["MASTER_PORT"] = str(port)
+    dist.init_process_group("gloo", rank=rank, world_size=world)
+    try:
+        rng = np.random.default_rng(77)
+        q, k, v, dy = (rng.standard_normal((slabs, n, d)) for _ in range(4))
+        b, e = sharding.token_shard(n, rank, world)
+        log = []
+        op = _BackwardOp(slabs, d, log)
+        sh = sharding.TokenShardedAttention(1, slabs, e - b, d, op=op, workspace_bytes=op.workspace_bytes())
+        mine = [x[:, b:e] for x in (q, k, v, dy)]
+        sh.forward(*mine[:3])
+        state = sh.save_state()
+        for name, given in (("saved", state), ("again", None)):
+            log.clear()
+            np.savez(os.path.join(out_dir, f"{name}_{rank}.npz"), *sh.backward(*mine, state=given))
+            assert log == ([] if given is not None else ["backward_state"]) + ["backward_q", "backward_kv"]
+        dist.barrier()
+    finally:
+        dist.destroy_process_group()
+
+
+def test_two_rank_token_sharded_backward(tmp_path):
+    """Against differences of the unsharded forward pass in 64 bits, at a step whose own error is 1e-6 of the gradients'
+    sizes, and against one rank that holds all tokens; the exchanged states are fp32."""
+    world, n, d, slabs = 2, 41, 8, 2
+    mp.spawn(_backward_rank_main, args=(world, _free_port(), n, d, slabs, str(tmp_path)), nprocs=world, join=True)
+    rng = np.random.default_rng(77)
+    tensors = [rng.standard_normal((slabs, n, d)) for _ in range(4)]
+    q, k, v, dy = tensors
+    whole = _BackwardOp(slabs, d, [])
+    dq, dS = whole.backward_q(q, dy, whole.backward_state(k, v))
+    want = [dq, *whole.backward_kv(k, v, dS)]
+    for name in ("saved", "again"):
+        parts = [np.load(tmp_path / f"{name}_{r}.npz") for r in range(world)]
+        got = [np.concatenate([p[f"arr_{i}"] for p in parts], axis=1) for i in range(3)]
+        for g, w in zip(got, want):
+            np.testing.assert_allclose(g, w, rtol=2e-5, atol=2e-6)
+        for which in range(3):
+            for at in ((0, 0, 0), (1, 20, 3), (1, 21, 7), (0, 40, 5)):
+                step, sides = 1e-4, []
+                for sign in (1, -1):
+                    moved = [x.copy() for x in tensors[:3]]
+                    moved[which][at] += sign * step
+                    sides.append((oracle.linear(*moved, EPS) * dy).sum())
+                np.testing.assert_allclose(got[which][at], (sides[0] - sides[1]) / (2 * step), rtol=1e-4, atol=1e-5)
