@@ -280,6 +280,16 @@ def linfusion_attn_destroy(handle) -> None:
         raise LinFusionError(rc, "linfusion_attn_destroy")
 
 
+def allocating_on(stream: Optional[int], index: int):
+    """A context with `stream` of device `index` as the current one (None: no change), for the tensors that a call allocates: memory
+    of another stream's pool could still be in use there, or be handed out again there, while the call's kernels run."""
+    import contextlib
+    import torch
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream, device=torch.device("cuda", index)))
+
+
 class LinFusionAttention:
     """One handle per shape.  ``forward`` takes bf16 CUDA tensors [B, H, N, d] (or [B, N, H, d]
     with ``layout="token_major"``).  With ``d_qk`` (Prop. 3's feature width d') Q and K are
@@ -492,7 +502,8 @@ class LinFusionAttention:
         import torch
         device = torch.device("cuda", self.desc.device)
         if out is None:
-            out = torch.empty(self.state_floats(), dtype=torch.float32, device=device)
+            with allocating_on(stream, self.desc.device):
+                out = torch.empty(self.state_floats(), dtype=torch.float32, device=device)
         else:
             self._check_state(out, "out", device)
         if stream is None:
@@ -530,27 +541,23 @@ class LinFusionAttention:
                 raise ValueError(f"{name}: expected a tensor on {device}")
         for t, name in states:
             self._check_state(t, name, device)
-        made = []
         for t, name, like in outs:
-            if t is None:
-                if like == "state":
-                    t = torch.empty(self.state_floats(), dtype=torch.float32, device=device)
-                else:
-                    t = torch.empty_like(next(x for x, _, kind in tensors if (kind == "v") == (like == "v")))
-            elif like == "state":
+            if t is not None and like == "state":
                 self._check_state(t, name, device)
-            else:
+            elif t is not None:
                 self._check(t, like)
                 if t.device != device:
                     raise ValueError(f"{name}: expected a tensor on {device}")
-            made.append(t)
         nbytes = self.backward_workspace_bytes()
-        if workspace is None:
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        elif workspace.device != device or not workspace.is_contiguous():
-            raise ValueError(f"workspace: expected a contiguous tensor on {device}")
-        else:
-            nbytes = workspace.numel() * workspace.element_size()
+        with allocating_on(stream, index):
+            made = [t if t is not None else torch.empty(self.state_floats(), dtype=torch.float32, device=device) if like == "state" else
+                    torch.empty_like(next(x for x, _, kind in tensors if (kind == "v") == (like == "v"))) for t, _, like in outs]
+            if workspace is None:
+                workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+            elif workspace.device != device or not workspace.is_contiguous():
+                raise ValueError(f"workspace: expected a contiguous tensor on {device}")
+            else:
+                nbytes = workspace.numel() * workspace.element_size()
         if stream is None:
             stream = torch._C._cuda_getCurrentRawStream(index)
         return made, (workspace.data_ptr(), nbytes, stream)

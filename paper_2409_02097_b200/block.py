@@ -14,7 +14,7 @@ import ctypes
 from typing import Dict, Optional, Sequence, Tuple
 
 from . import attn
-from .attn import DTYPE_FP16, LinFusionError, OK
+from .attn import DTYPE_FP16, LinFusionError, OK, allocating_on
 
 MAX_AXES = 4
 NORM_NONE, NORM_LAYER, NORM_RMS = 0, 1, 2
@@ -148,18 +148,26 @@ def _copy(struct):
     return type(struct).from_buffer_copy(struct)
 
 
-def _call(index, stream, function, *args):
-    """`function(*args, stream)` with the tensors' device current."""
+def _call(index, function, *args):
+    """`function(*args, stream)` on the current stream of the tensors' device, which is made current."""
     import torch
-    if stream is None:
-        stream = torch._C._cuda_getCurrentRawStream(index)
+    stream = torch._C._cuda_getCurrentRawStream(index)
     if torch._C._cuda_getDevice() == index:
         return function(*args, stream)
     with torch.cuda.device(index):
         return function(*args, stream)
 
 
-class AxialRope:
+class _Fixed:
+    """A configuration that stays as it was made: calls keep what they checked under it."""
+
+    def __setattr__(self, name, value):
+        if "_checked" in self.__dict__:
+            raise AttributeError(f"{type(self).__name__}.{name} is fixed: make another object")
+        object.__setattr__(self, name, value)
+
+
+class AxialRope(_Fixed):
     """Rotary positions with several axes for heads of width ``d``.
 
     ``pairs``: how many pairs of channels each axis turns, e.g. ``(16, 24, 24)`` for time, height and width
@@ -230,6 +238,9 @@ class AxialRope:
             raise ValueError("neither q nor k is given")
         if some.dim() != 4:
             raise ValueError(f"expected four axes, got {tuple(some.shape)}")
+        if stream is not None and some.is_cuda:
+            with allocating_on(stream, some.get_device()):
+                return self._run(q, k, positions, q_out, k_out, backward, None)
         if q is None:
             q_out = None
         elif q_out is None:
@@ -249,7 +260,7 @@ class AxialRope:
         if tk is not None:
             tk = _copy(tk)
             tk.in_, tk.out = k.data_ptr(), k_out.data_ptr()
-        rc = _call(some.get_device(), stream, self._lib.linfusion_rope, desc, tq, tk, positions.data_ptr(), pos_batch)
+        rc = _call(some.get_device(), self._lib.linfusion_rope, desc, tq, tk, positions.data_ptr(), pos_batch)
         if rc != OK:
             raise LinFusionError(rc, "linfusion_rope")
         return q_out, k_out
@@ -263,7 +274,7 @@ class AxialRope:
         return self._run(dq, dk, positions, dq_out, dk_out, 1, stream)
 
 
-class BlockNorm:
+class BlockNorm(_Fixed):
     """The norms before and after a block of a residual stream x [B, N, C], ``a`` the block's output:
 
         y = residual_scale * x + gate * (Post(a) * post_weight + post_bias)       (y = x without ``a``)
@@ -355,6 +366,9 @@ class BlockNorm:
                 post_bias=None, y=None, n=None, stream: Optional[int] = None) -> Tuple:
         """(y, n): the stream after the block (``x`` itself without ``a``) and the next block's input (None
         without ``pre``).  ``y`` may be given as ``x`` or ``a`` (in place)."""
+        if stream is not None and x.is_cuda:
+            with allocating_on(stream, x.get_device()):
+                return self.forward(x, a, gate, scale, shift, pre_weight, pre_bias, post_weight, post_bias, y, n)
         if a is not None and y is None:
             y = _like(x)
         if self.pre != NORM_NONE and n is None:
@@ -368,7 +382,7 @@ class BlockNorm:
             found = self._checked.keep(key, self._check(rows, vectors, tuple(x.shape), x.device))
         desc, structs, vec = found
         rx, ra, ry, rn = self._row_addresses(structs, rows)
-        rc = _call(x.get_device(), stream, self._lib.linfusion_block_norm, desc, rx, ra, self._addresses(vec, vectors), ry, rn)
+        rc = _call(x.get_device(), self._lib.linfusion_block_norm, desc, rx, ra, self._addresses(vec, vectors), ry, rn)
         if rc != OK:
             raise LinFusionError(rc, "linfusion_block_norm")
         return (y if a is not None else x), n
@@ -385,6 +399,10 @@ class BlockNorm:
         some = dn if dn is not None else dy
         if some is None:
             raise ValueError("neither dy nor dn is given")
+        if stream is not None and some.is_cuda:
+            with allocating_on(stream, some.get_device()):
+                return self.backward(y, a, gate, scale, shift, pre_weight, pre_bias, post_weight, post_bias, dy, dn, dx, da, need_vectors,
+                                     workspace)
         device = some.device
         if dx is None:
             dx = _like(some)
@@ -418,7 +436,7 @@ class BlockNorm:
                 raise ValueError("workspace: expected a contiguous CUDA tensor on the device of the others")
             ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
         ry, ra, rdy, rdn, rdx, rda = self._row_addresses(structs, rows)
-        rc = _call(some.get_device(), stream, self._lib.linfusion_block_norm_backward, desc, ry, ra, self._addresses(vec, vectors), rdy,
+        rc = _call(some.get_device(), self._lib.linfusion_block_norm_backward, desc, ry, ra, self._addresses(vec, vectors), rdy,
                    rdn, rdx, rda, grads, ws, ws_bytes if need_vectors else 0)
         if rc != OK:
             raise LinFusionError(rc, "linfusion_block_norm_backward")

@@ -39,7 +39,11 @@ linfusion_status_t end(cudaError_t e)
     return LINFUSION_ERR_CUDA;
 }
 
-bool good_stride(int64_t s) { return s >= 0 && s % 8 == 0 && s < (int64_t(1) << 56); }
+// An axis of n rows, s elements apart: whole 16-byte pieces, and within 2^46 elements, so that sums of such reaches are exact.
+bool good_stride(int64_t n, int64_t s)
+{
+    return s >= 0 && s % 8 == 0 && s < (int64_t(1) << 56) && (n <= 1 || s <= (int64_t(1) << 46) / (n - 1));
+}
 
 // The bytes from the first to behind the last element that strides reach, as a half-open range.
 struct Extent {
@@ -96,8 +100,9 @@ linfusion_status_t check_rope(const linfusion_rope_desc_t* d, int* pairs)
 linfusion_status_t check_rope_tensor(const linfusion_rope_desc_t& d, const linfusion_rope_tensor_t& t)
 {
     if (t.in == nullptr || t.out == nullptr || !is_aligned(t.in, 16) || !is_aligned(t.out, 16)) return LINFUSION_ERR_INVALID_ARG;
-    for (const int64_t s : {t.in_batch, t.in_token, t.in_head, t.out_batch, t.out_token, t.out_head})
-        if (!good_stride(s)) return LINFUSION_ERR_INVALID_ARG;
+    if (!good_stride(d.B, t.in_batch) || !good_stride(d.N, t.in_token) || !good_stride(t.heads, t.in_head) ||
+        !good_stride(d.B, t.out_batch) || !good_stride(d.N, t.out_token) || !good_stride(t.heads, t.out_head))
+        return LINFUSION_ERR_INVALID_ARG;
     // no two output rows on top of one another
     if (!rows_disjoint({{d.B, t.out_batch}, {d.N, t.out_token}, {t.heads, t.out_head}}, d.d)) return LINFUSION_ERR_INVALID_ARG;
     const Extent in = extent(t.in, d.B, t.in_batch, d.N, t.in_token, t.heads, t.in_head, d.d);
@@ -161,9 +166,9 @@ linfusion_status_t check_norm(const linfusion_block_norm_desc_t* d)
 }
 
 bool rows_given(const linfusion_rows_t* r) { return r != nullptr && r->p != nullptr; }
-bool rows_ok(const linfusion_rows_t* r)
+bool rows_ok(const linfusion_block_norm_desc_t& d, const linfusion_rows_t* r)
 {
-    return rows_given(r) && is_aligned(r->p, 16) && good_stride(r->batch) && good_stride(r->row);
+    return rows_given(r) && is_aligned(r->p, 16) && good_stride(d.B, r->batch) && good_stride(d.N, r->row);
 }
 Rows to_rows(const linfusion_rows_t* r)
 {
@@ -171,13 +176,13 @@ Rows to_rows(const linfusion_rows_t* r)
     if (rows_given(r)) o = {static_cast<char*>(r->p), r->batch * 2, r->row * 2};
     return o;
 }
-bool channels_ok(const linfusion_channels_t& c) { return c.p == nullptr || (is_aligned(c.p, 16) && good_stride(c.batch)); }
+bool channels_ok(int B, const linfusion_channels_t& c) { return c.p == nullptr || (is_aligned(c.p, 16) && good_stride(B, c.batch)); }
 Channels to_channels(const linfusion_channels_t& c) { return {static_cast<const char*>(c.p), c.batch * 2}; }
 
 // What the forward and the backward pass ask of the vectors.
 bool vectors_ok(const linfusion_block_norm_desc_t& d, const linfusion_block_norm_vectors_t& v, bool branch)
 {
-    if (!channels_ok(v.gate) || !channels_ok(v.scale) || !channels_ok(v.shift)) return false;
+    if (!channels_ok(d.B, v.gate) || !channels_ok(d.B, v.scale) || !channels_ok(d.B, v.shift)) return false;
     for (const void* p : {v.pre_weight, v.pre_bias, v.post_weight, v.post_bias})
         if (p != nullptr && !is_aligned(p, 16)) return false;
     if ((v.scale.p == nullptr) != (v.shift.p == nullptr)) return false;
@@ -193,7 +198,7 @@ Extent rows_extent(const linfusion_block_norm_desc_t& d, const linfusion_rows_t*
 }
 bool out_ok(const linfusion_block_norm_desc_t& d, const linfusion_rows_t* r)
 {
-    return rows_ok(r) && rows_disjoint({{d.B, r->batch}, {d.N, r->row}}, d.C);
+    return rows_ok(d, r) && rows_disjoint({{d.B, r->batch}, {d.N, r->row}}, d.C);
 }
 // `out` shares no memory with `in`, or lies exactly over it and may.
 bool apart(const linfusion_block_norm_desc_t& d, const linfusion_rows_t* out, const linfusion_rows_t* in, bool may_lie_over)
@@ -327,7 +332,7 @@ linfusion_status_t linfusion_rope(const linfusion_rope_desc_t* desc, const linfu
     const linfusion_rope_tensor_t* given[2] = {q != nullptr && q->heads != 0 ? q : nullptr,
                                                k != nullptr && k->heads != 0 ? k : nullptr};
     if (given[0] == nullptr && given[1] == nullptr) return LINFUSION_ERR_INVALID_ARG;
-    if (positions == nullptr || !is_aligned(positions, 4) || pos_batch_stride < 0) return LINFUSION_ERR_INVALID_ARG;
+    if (positions == nullptr || !is_aligned(positions, 4) || pos_batch_stride < 0 || pos_batch_stride >= (int64_t(1) << 40)) return LINFUSION_ERR_INVALID_ARG;
     const Extent pos = {reinterpret_cast<const char*>(positions),
                         4 * (static_cast<size_t>(desc->B - 1) * pos_batch_stride + static_cast<size_t>(desc->N) * desc->n_axes)};
     for (const linfusion_rope_tensor_t* t : given)
@@ -405,7 +410,7 @@ linfusion_status_t linfusion_block_norm(const linfusion_block_norm_desc_t* desc,
     const linfusion_block_norm_vectors_t none = {};
     if (v == nullptr) v = &none;
     const bool branch = rows_given(a), pre = desc->pre != LINFUSION_NORM_NONE;
-    if (!vectors_ok(*desc, *v, branch) || !rows_ok(x) || (branch && !rows_ok(a))) return LINFUSION_ERR_INVALID_ARG;
+    if (!vectors_ok(*desc, *v, branch) || !rows_ok(*desc, x) || (branch && !rows_ok(*desc, a))) return LINFUSION_ERR_INVALID_ARG;
     if (rows_given(y) != branch || rows_given(n) != pre) return LINFUSION_ERR_INVALID_ARG;
     if (branch && (!out_ok(*desc, y) || !apart(*desc, y, x, true) || !apart(*desc, y, a, true) || !apart(*desc, y, *v)))
         return LINFUSION_ERR_INVALID_ARG;
@@ -448,10 +453,10 @@ linfusion_status_t linfusion_block_norm_backward(const linfusion_block_norm_desc
     if (v == nullptr) v = &none;
     if (grads == nullptr) grads = &no_grads;
     const bool branch = rows_given(a), pre = desc->pre != LINFUSION_NORM_NONE;
-    if (!vectors_ok(*desc, *v, branch) || (branch && !rows_ok(a))) return LINFUSION_ERR_INVALID_ARG;
-    if (pre && (!rows_ok(y) || !rows_ok(dn))) return LINFUSION_ERR_INVALID_ARG;
-    if (!pre && (rows_given(dn) || !rows_ok(dy))) return LINFUSION_ERR_INVALID_ARG;
-    if (rows_given(dy) && !rows_ok(dy)) return LINFUSION_ERR_INVALID_ARG;
+    if (!vectors_ok(*desc, *v, branch) || (branch && !rows_ok(*desc, a))) return LINFUSION_ERR_INVALID_ARG;
+    if (pre && (!rows_ok(*desc, y) || !rows_ok(*desc, dn))) return LINFUSION_ERR_INVALID_ARG;
+    if (!pre && (rows_given(dn) || !rows_ok(*desc, dy))) return LINFUSION_ERR_INVALID_ARG;
+    if (rows_given(dy) && !rows_ok(*desc, dy)) return LINFUSION_ERR_INVALID_ARG;
     if (!out_ok(*desc, dx) || rows_given(da) != branch || (branch && !out_ok(*desc, da))) return LINFUSION_ERR_INVALID_ARG;
     const linfusion_rows_t* y_read = pre ? y : nullptr;
     if (!apart(*desc, dx, y_read, false) || !apart(*desc, dx, a, false) || !apart(*desc, dx, dy, true) ||

@@ -374,3 +374,22 @@ def _rope_differentiable(x, pos):
     angle = torch.cat([pos[:, :1].double() * freq, pos[:, 1:].double() * freq], -1)[None, :, None]
     u, w = x[..., 0::2], x[..., 1::2]
     return torch.stack([u * angle.cos() - w * angle.sin(), u * angle.sin() + w * angle.cos()], -1).flatten(-2)
+
+
+@pytest.mark.parametrize("layout,d", [("head_major", 64), ("token_major", 80)])
+def test_tensors_of_more_than_2_to_the_31_elements(layout, d):
+    # the last slab, whose offsets need more than 32 bits, against the formulas
+    if torch.cuda.mem_get_info()[0] < 90 << 30:
+        pytest.skip("needs 90 GB")
+    H = 2_200_000_000 // (d * 500_009) + 1
+    N = 500_009
+    shape = (1, H, N, d) if layout == "head_major" else (1, N, H, d)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    tensors = [torch.empty(shape, device="cuda", dtype=torch.bfloat16).normal_(generator=g) for _ in range(4)]
+    op = attn.LinFusionAttention(1, H, N, d, eps=EPS, variant="split", layout=layout)
+    ws = torch.empty(op.backward_workspace_bytes(), dtype=torch.uint8, device="cuda")
+    got = op.backward(*tensors, workspace=ws)
+    assert op.backward_status(ws) == attn.OK
+    last = lambda t: (t[:, -1:] if layout == "head_major" else t[:, :, -1:].transpose(1, 2)).contiguous()  # noqa: E731
+    _check([last(t) for t in got], [last(t) for t in tensors], "bf16", f"beyond 2^31 {layout} {d}")
+    op.close()

@@ -444,3 +444,57 @@ def test_streams_graphs_and_same_bits():
                 g.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for _, held, _ in graphs for a, b in zip(first, held))
+
+
+def test_given_streams_get_their_own_memory():
+    """What a call allocates for itself belongs to the stream that it was given: the current stream, which takes and overwrites
+    memory all the while, must not be handed the workspace or an output of work that still runs."""
+    from paper_2409_02097_b200 import attn
+    x, a = (torch.randn(2, 6000, 1280, device="cuda").bfloat16() for _ in range(2))
+    gate = torch.randn(2, 1280, device="cuda").bfloat16()
+    norm = block.BlockNorm(1280, "layer", "rms")
+    op = attn.LinFusionAttention(2, 8, 3000, 64)
+    q, k, v, dy = (torch.randn(2, 8, 3000, 64, device="cuda").bfloat16() for _ in range(4))
+    rope = block.AxialRope(64, (16, 16))
+    pos = torch.rand(3000, 2, device="cuda")
+    calls = lambda **kw: [*norm.backward(x, a, gate=gate, dn=a, **kw).values(), *norm.forward(x, a, gate=gate, **kw),  # noqa: E731
+                          *op.backward(q, k, v, dy, **kw), *rope.forward(q, k, pos, **kw)]
+    want = calls()
+    sizes = {norm.workspace_bytes(2, 6000), op.backward_workspace_bytes(), x.numel() * 2, q.numel() * 2, 1280 * 4, 2 * 1280 * 4}
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(10):
+        got = calls(stream=side.cuda_stream)
+        for n in sizes:
+            for _ in range(3):
+                torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        assert all(torch.equal(g, w) for g, w in zip(got, want))
+    op.close()
+
+
+def test_tensors_of_more_than_2_to_the_31_elements():
+    # the last rows, whose offsets need more than 32 bits, equal those of a small call on the same rows
+    free = torch.cuda.mem_get_info()[0]
+    if free < 40 << 30:
+        pytest.skip("needs 40 GB")
+    N, C = 1_700_001, 1280
+    x = torch.empty(1, N, C, device="cuda", dtype=torch.bfloat16).normal_()
+    norm = block.BlockNorm(C)
+    _, n = norm.forward(x)
+    _, few = norm.forward(x[:, -5:])
+    assert torch.equal(n[:, -5:], few)
+    dx = norm.backward(x, dn=n, dx=torch.empty_like(x), need_vectors=False)["x"]
+    assert torch.equal(dx[:, -5:], norm.backward(x[:, -5:], dn=few, need_vectors=False)["x"])
+    del n, dx
+    q = x.view(1, N, 20, 64)
+    rope = block.AxialRope(64, (16, 16), layout="token_major")
+    pos = torch.rand(N, 2, device="cuda") * 100
+    out, _ = rope.forward(q, None, pos)
+    assert torch.equal(out[:, -5:], rope.forward(q[:, -5:], None, pos[-5:].contiguous())[0])
+
+
+def test_configurations_are_fixed():
+    for op in (block.AxialRope(64, (16, 16)), block.BlockNorm(64)):
+        with pytest.raises(AttributeError):
+            op.dtype = "fp16"

@@ -259,3 +259,15 @@ def test_attention_backward_workspace_follows_the_split(lib):
     assert ws(2, 10, 1 << 19, 64) == ws(2, 10, 1 << 20, 64)  # bounded by the SMs
     assert ws(2, 10, 4096, 64) == ws(2, 10, 4096, 64, variant="stream")  # the forward's variant plays no part
     assert lib.linfusion_attn_backward_workspace_bytes(ctypes.byref(attn.make_desc(1, 1, 1, 64)), 0, None) == attn.ERR_INVALID_ARG
+
+
+def test_strides_whose_reach_has_no_sense_are_refused(lib):
+    # (n - 1) * stride would pass 64 bits: refused, not wrapped
+    far = 1 << 55
+    for kw in (dict(in_t=far), dict(out_t=far), dict(in_b=far), dict(out_h=far)):
+        _refused(_rope_call(lib, N=1 << 20, B=3, q=_rope_tensor(**kw)))
+    _refused(_rope_call(lib, pos_b=1 << 60))
+    for backward in (False, True):
+        _refused(_norm_call(lib, backward=backward, N=1 << 20, row=far))
+        _refused(_norm_call(lib, backward=backward, B=1 << 12, batch=far))
+        _refused(_norm_call(lib, backward=backward, B=1 << 12, gate=(A16 * 9, far)))
