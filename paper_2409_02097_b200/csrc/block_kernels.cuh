@@ -277,8 +277,7 @@ __global__ void __launch_bounds__(kRopeThreads, 4) rope_kernel(const __grid_cons
 
 // ---------------------------------------------------------------------------------------------
 // The norms around a block.  A group of W = ceil(C / (256 V)) warps works on whole rows, one at a time; each thread keeps
-// to the same 8 V channels of every row, so its gate, scale, shift, weights and column sums stay in registers (V = 1
-// up to C = 4096).  Rows are fetched three (two) ahead into the thread's own slots of shared memory (16-byte
+// to the same 8 V channels of every row, so its gate, scale, shift, weights and column sums stay in registers (V is 1 or 2).  Rows are fetched three (two) ahead into the thread's own slots of shared memory (16-byte
 // asynchronous copies that only the thread itself waits for), so DRAM latency is hidden without registers.
 //
 // A row's mean and variance: each warp takes its sum by shuffles, then the sum of squares about its own mean, and the
@@ -286,12 +285,17 @@ __global__ void __launch_bounds__(kRopeThreads, 4) rope_kernel(const __grid_cons
 // whatever the row's mean.  Two quantities (the two norms of a row, or two sums) travel together, one in each half of the
 // warp: halving the values while the lanes are halved costs five shuffles instead of ten.
 //
-// What bounds them: DRAM at large C x rows; behind it the issue slots (365 instructions per row and
-// warp in the backward pass of both norms; 560 before packed fp32x2 arithmetic, which halves the multiply-adds).
+// What bounds them: DRAM at large C x rows, 4.9 TB/s forward and 4.3 TB/s backward of the 6.5 of a copy (68.6 and 117 us at 2 x 16384 x
+// 1280, both norms with gate and modulation); behind it the latency of a row's exchanges, some 3000 clocks from its first sum to its
+// last store, and the issue slots (365 instructions per row and warp in the backward pass of both norms; 560 before packed fp32x2
+// arithmetic, which halves the multiply-adds).  More rows in flight would take registers: 96 of them for a fourth block
+// spilled (177 us where 128 take 117).
 // ---------------------------------------------------------------------------------------------
 constexpr int kNormNone = 0, kNormLayer = 1, kNormRms = 2;
 constexpr int kNormMaxWarps = 16;  // of a group: a half warp holds one value of each
 constexpr int kNormMaxThreads = 32 * kNormMaxWarps;  // which leaves a thread 128 registers: three blocks of five warps on an SM
+// Most threads of a block whose groups have one warp (J = 0) or more.
+__host__ __device__ constexpr int norm_threads(int V, int J) { return V > 1 && J == 0 ? 128 : kNormMaxThreads; }
 __host__ __device__ constexpr int norm_stages(int V) { return V == 1 ? 4 : 3; }
 
 struct Rows {
@@ -517,7 +521,7 @@ struct Walk {
 };
 
 template <int KIND, int POST, int PRE, bool A, int V, int J>
-__global__ void __launch_bounds__(kNormMaxThreads) block_norm_kernel(const __grid_constant__ NormParams p)
+__global__ void __launch_bounds__(norm_threads(V, J)) block_norm_kernel(const __grid_constant__ NormParams p)
 {
     extern __shared__ __align__(16) unsigned char norm_smem[];
     constexpr int S = A ? 2 : 1;
@@ -631,7 +635,7 @@ __global__ void __launch_bounds__(kNormMaxThreads) block_norm_kernel(const __gri
 //     [0] sum dn   [1] sum dn h   [2] sum u e   [3] sum u
 // which the group keeps in registers over its rows and leaves as partials for block_norm_grads_kernel.
 template <int KIND, int POST, int PRE, bool A, int V, int J>
-__global__ void __launch_bounds__(kNormMaxThreads) block_norm_backward_kernel(const __grid_constant__ NormParams p)
+__global__ void __launch_bounds__(norm_threads(V, J)) block_norm_backward_kernel(const __grid_constant__ NormParams p)
 {
     extern __shared__ __align__(16) unsigned char norm_smem[];
     constexpr int S = (PRE != kNormNone ? 2 : 0) + (A ? 2 : 1);

@@ -222,15 +222,22 @@ bool apart(const linfusion_block_norm_desc_t& d, const linfusion_rows_t* out, co
 struct NormPlan {
     int vectors, warps, per_cta, chunks, groups, ctas;
 };
-// `warps_per_sm`: warps that an SM holds at once.
-NormPlan norm_plan(const linfusion_block_norm_desc_t& d, int sms, int warps_per_sm)
+// Sixteen channels a thread in the forward pass wherever eight do not leave a row to one warp: half the warps to exchange a
+// row's sums, more rows in flight (us, sixteen / eight: 21 / 26 at 3 x 8192 x 320, 25 / 30 at 2 x 8192 x 640, 29 / 34 at 2 x 8192 x
+// 1024, 28 / 34 at 2 x 4096 x 2048; 68.6 / 69.1 at 2 x 16384 x 1280, 23 / 22 at 2 x 4096 x 1280, where the third warp is half empty).
+// The backward pass keeps four column sums of each channel and has no registers for that (162 / 117 at 2 x 16384 x 1280, 53 / 53
+// at 2 x 8192 x 1024), but where sixteen channels leave a row to one warp (43 / 50 at 2 x 16384 x 320, 20 / 21 at 2 x 4099 x 320;
+// 7.2 / 6.4 at 2 x 64 x 320).  Above 4096 channels eight would not do.
+NormPlan norm_plan(const linfusion_block_norm_desc_t& d, int sms, bool backward)
 {
     NormPlan p;
-    p.vectors = d.C > 256 * kNormMaxWarps ? 2 : 1;
+    p.vectors = d.C <= 256 ? 1 : !backward ? 2 : d.C > 256 * kNormMaxWarps || d.C <= 512 ? 2 : 1;
     p.warps = (d.C + 256 * p.vectors - 1) / (256 * p.vectors);
     p.per_cta = p.warps >= 4 ? 1 : 4 / p.warps;
-    // As many groups as run at once, so that none waits for another to end; fewer where there are fewer rows.
-    long long target = static_cast<long long>(sms) * (warps_per_sm / (p.warps * p.per_cta) > 0 ? warps_per_sm / (p.warps * p.per_cta) : 1) * p.per_cta;
+    // As many groups as run at once, so that none waits for another to end; fewer where there are fewer rows.  At 128
+    // registers a thread an SM holds sixteen warps (but four blocks of three); at the 212 of two vectors in one warp, eight.
+    const int block = p.warps * p.per_cta, per_sm = backward && p.vectors == 2 && p.warps == 1 ? 2 : block == 3 ? 4 : 16 / block;
+    const long long target = static_cast<long long>(sms) * per_sm * p.per_cta;
     long long chunks = target / d.B;
     if (chunks > d.N) chunks = d.N;
     if (chunks < 1) chunks = 1;
@@ -239,7 +246,6 @@ NormPlan norm_plan(const linfusion_block_norm_desc_t& d, int sms, int warps_per_
     p.ctas = (p.groups + p.per_cta - 1) / p.per_cta;
     return p;
 }
-constexpr int kForwardWarpsPerSm = 24, kBackwardWarpsPerSm = 16;
 
 void fill(NormParams* p, const linfusion_block_norm_desc_t& d, const linfusion_block_norm_vectors_t& v, const NormPlan& plan, bool branch)
 {
@@ -268,7 +274,7 @@ cudaError_t launch_norm_one(const NormParams& p, const NormPlan& plan, int devic
     static std::atomic<uint64_t> done{0};
     const int threads = 32 * plan.warps * plan.per_cta;
     const int streams = BACKWARD ? (PRE != kNormNone ? 2 : 0) + (A ? 2 : 1) : (A ? 2 : 1);
-    const size_t smem = norm_smem_bytes(streams, V, threads, plan.per_cta), most = norm_smem_bytes(streams, V, kNormMaxThreads, 4);
+    const size_t smem = norm_smem_bytes(streams, V, threads, plan.per_cta), most = norm_smem_bytes(streams, V, norm_threads(V, J), 4);
     cudaError_t e;
     if constexpr (BACKWARD) {
         e = allow_smem(block_norm_backward_kernel<KIND, POST, PRE, A, V, J>, most, device, &done);
@@ -311,10 +317,15 @@ cudaError_t launch_norm_kind(const linfusion_block_norm_desc_t& d, const NormPar
 #define LF_SIZED(V, J)                                                                            \
     return half ? launch_norm<hf, V, J, BACKWARD>(p, plan, d.post, d.pre, branch, device, s)       \
                 : launch_norm<bf, V, J, BACKWARD>(p, plan, d.post, d.pre, branch, device, s)
-    if (plan.vectors > 1) LF_SIZED(2, 4);
-    if (plan.warps > 8) LF_SIZED(1, 4);
-    if (plan.warps > 1) LF_SIZED(1, 3);
-    LF_SIZED(1, 0);
+    if (plan.vectors == 1 && plan.warps == 1) LF_SIZED(1, 0);
+    if (plan.warps == 1) LF_SIZED(2, 0);
+    if (plan.vectors == 2 && plan.warps > 8) LF_SIZED(2, 4);
+    if constexpr (BACKWARD) {
+        if (plan.warps > 8) LF_SIZED(1, 4);
+        LF_SIZED(1, 3);
+    } else {
+        LF_SIZED(2, 3);
+    }
 #undef LF_SIZED
 }
 
@@ -419,7 +430,7 @@ linfusion_status_t linfusion_block_norm(const linfusion_block_norm_desc_t* desc,
         return LINFUSION_ERR_INVALID_ARG;
     const Here at = here();
     if (at.st != LINFUSION_OK) return at.st;
-    const NormPlan plan = norm_plan(*desc, at.sms, kForwardWarpsPerSm);
+    const NormPlan plan = norm_plan(*desc, at.sms, false);
     NormParams p = {};
     fill(&p, *desc, *v, plan, branch);
     p.x = to_rows(x);
@@ -434,7 +445,7 @@ linfusion_status_t linfusion_block_norm_workspace_bytes(const linfusion_block_no
     if (bytes == nullptr) return LINFUSION_ERR_INVALID_ARG;
     const linfusion_status_t st = check_norm(desc);
     if (st != LINFUSION_OK) return st;
-    const NormPlan plan = norm_plan(*desc, sm_count > 0 ? sm_count : 148, kBackwardWarpsPerSm);
+    const NormPlan plan = norm_plan(*desc, sm_count > 0 ? sm_count : 148, true);
     *bytes = align_up_256(static_cast<size_t>(4) * plan.groups * desc->C * sizeof(float));
     return LINFUSION_OK;
 }
@@ -482,7 +493,7 @@ linfusion_status_t linfusion_block_norm_backward(const linfusion_block_norm_desc
 
     const Here at = here();
     if (at.st != LINFUSION_OK) return at.st;
-    const NormPlan plan = norm_plan(*desc, at.sms, kBackwardWarpsPerSm);
+    const NormPlan plan = norm_plan(*desc, at.sms, true);
     if (want != 0) {
         if (workspace == nullptr || !is_aligned(workspace, 256)) return LINFUSION_ERR_INVALID_ARG;
         if (workspace_bytes < align_up_256(static_cast<size_t>(4) * plan.groups * desc->C * sizeof(float))) return LINFUSION_ERR_ALLOC;
