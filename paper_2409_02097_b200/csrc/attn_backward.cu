@@ -112,10 +112,13 @@ void plan_tc(const linfusion_attn_desc_t& d, int sm_count, BackwardPlan* p)
     p->tc_partial = p->tc == 1 ? BackwardTc::PARTIAL_FLOATS : p->dv > 64 ? BackwardTcWide<2>::PARTIAL_FLOATS : BackwardTcWide<1>::PARTIAL_FLOATS;
     if (!(p->tc_state || p->tc_q || p->tc_kv)) return;
     p->ctas = static_cast<int>(p->tiles < sm_count ? p->tiles : sm_count);
-    // The same number of CTAs on every slab where that keeps four fifths of the SMs busy and runs are short: a CTA that
-    // meets a second slab fetches another state and hands back another partial, 4 us of a run of a few tiles.
-    const int aligned = sm_count / p->slabs * p->slabs;
-    if (5 * aligned >= 4 * sm_count && aligned <= p->ctas && p->tiles < 64ll * sm_count) p->ctas = aligned;
+    // The same number of CTAs on every slab where that lengthens the longest run by three tiles at most: a CTA that meets a
+    // second slab fetches another state and hands back another partial, some 4 us (44 / 38 us at 20 slabs x 4096 x 64; 193 / 216 at
+    // 40 x 16384 x 64, whose 128 tiles on three CTAs each would leave 28 SMs without any).
+    const int each = sm_count / p->slabs;
+    if (each > 0 && each * p->slabs <= p->ctas &&
+        (p->tiles_per_slab + each - 1) / each <= (p->tiles + p->ctas - 1) / p->ctas + 3)
+        p->ctas = each * p->slabs;
     // a run of L tiles meets at most this many slabs
     const long long L = (p->tiles + p->ctas - 1) / p->ctas;
     p->spans = static_cast<int>((L + p->tiles_per_slab - 2) / p->tiles_per_slab) + 1;
