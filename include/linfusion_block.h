@@ -14,8 +14,8 @@
  *
  * Tensors are 16-bit (bf16, or fp16 with LINFUSION_DTYPE_FP16) device memory.  Strides count
  * elements; the channels of a row are contiguous.  Every pointer is 16-byte aligned and every stride
- * a multiple of 8.  Arithmetic, row statistics and sums are fp32; each 16-bit output is rounded once,
- * to nearest even.
+ * a multiple of 8 (that of an axis of one is not looked at).  Arithmetic, row statistics and sums are
+ * fp32; each 16-bit output is rounded once, to nearest even.
  */
 #ifndef LINFUSION_BLOCK_H
 #define LINFUSION_BLOCK_H

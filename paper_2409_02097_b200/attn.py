@@ -287,7 +287,9 @@ def allocating_on(stream: Optional[int], index: int):
     import torch
     if stream is None:
         return contextlib.nullcontext()
-    return torch.cuda.stream(torch.cuda.ExternalStream(stream, device=torch.device("cuda", index)))
+    # an external stream of address 0 would be a new one, not the default stream
+    return torch.cuda.stream(torch.cuda.default_stream(index) if stream == 0 else
+                             torch.cuda.ExternalStream(stream, device=torch.device("cuda", index)))
 
 
 class LinFusionAttention:

@@ -40,10 +40,8 @@ linfusion_status_t end(cudaError_t e)
 }
 
 // An axis of n rows, s elements apart: whole 16-byte pieces, and within 2^46 elements, so that sums of such reaches are exact.
-bool good_stride(int64_t n, int64_t s)
-{
-    return s >= 0 && s % 8 == 0 && s < (int64_t(1) << 56) && (n <= 1 || s <= (int64_t(1) << 46) / (n - 1));
-}
+// The stride of an axis of one row says nothing.
+bool good_stride(int64_t n, int64_t s) { return n <= 1 || (s >= 0 && s % 8 == 0 && s <= (int64_t(1) << 46) / (n - 1)); }
 
 // The bytes from the first to behind the last element that strides reach, as a half-open range.
 struct Extent {

@@ -498,3 +498,27 @@ def test_configurations_are_fixed():
     for op in (block.AxialRope(64, (16, 16)), block.BlockNorm(64)):
         with pytest.raises(AttributeError):
             op.dtype = "fp16"
+
+
+def test_the_default_stream_can_be_named():
+    from paper_2409_02097_b200 import attn
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        with attn.allocating_on(0, side.device.index):
+            assert torch.cuda.current_stream().cuda_stream == 0
+        with attn.allocating_on(None, side.device.index):
+            assert torch.cuda.current_stream() == side
+        with attn.allocating_on(torch.cuda.Stream().cuda_stream, side.device.index):
+            assert torch.cuda.current_stream().cuda_stream not in (0, side.cuda_stream)
+
+
+def test_strides_of_axes_of_one_do_not_matter():
+    x = torch.randn(1, 33, 64, device="cuda").bfloat16()
+    odd = x.as_strided((1, 33, 64), (3, 64, 1))
+    norm = block.BlockNorm(64)
+    assert torch.equal(norm.forward(odd)[1], norm.forward(x)[1])
+    assert torch.equal(norm.backward(odd, dn=odd)["x"], norm.backward(x, dn=x)["x"])
+    rope = block.AxialRope(64, (32,), layout="token_major")
+    pos = torch.arange(33, device="cuda").float().unsqueeze(1)
+    q = x.as_strided((1, 33, 1, 64), (5, 64, 7, 1))
+    assert torch.equal(rope.forward(q, None, pos)[0], rope.forward(x.view(1, 33, 1, 64), None, pos)[0])

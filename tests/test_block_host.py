@@ -271,3 +271,6 @@ def test_strides_whose_reach_has_no_sense_are_refused(lib):
         _refused(_norm_call(lib, backward=backward, N=1 << 20, row=far))
         _refused(_norm_call(lib, backward=backward, B=1 << 12, batch=far))
         _refused(_norm_call(lib, backward=backward, B=1 << 12, gate=(A16 * 9, far)))
+    if not torch.cuda.is_available():  # an axis of one row: its stride is not looked at
+        _without_device(_norm_call(lib, B=1, batch=3, gate=(A16 * 9, 3)))
+        _without_device(_rope_call(lib, B=1, q=_rope_tensor(in_b=-5, out_b=5)))
