@@ -241,15 +241,20 @@ class AxialRope(_Fixed):
         if stream is not None and some.is_cuda:
             with allocating_on(stream, some.get_device()):
                 return self._run(q, k, positions, q_out, k_out, backward, None)
+        look_q = look_k = None  # of outputs that are given: those made here follow from the inputs
         if q is None:
             q_out = None
         elif q_out is None:
             q_out = _like(q)
+        else:
+            look_q = _look(q_out)
         if k is None:
             k_out = None
         elif k_out is None:
             k_out = _like(k)
-        key = (_look(q), _look(k), _look(positions), _look(q_out), _look(k_out), backward)
+        else:
+            look_k = _look(k_out)
+        key = (_look(q), _look(k), _look(positions), look_q, look_k, backward)
         found = self._checked.get(key)
         if found is None:
             found = self._checked.keep(key, self._check(q, k, positions, q_out, k_out, backward))

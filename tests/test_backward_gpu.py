@@ -393,3 +393,14 @@ def test_tensors_of_more_than_2_to_the_31_elements(layout, d):
     last = lambda t: (t[:, -1:] if layout == "head_major" else t[:, :, -1:].transpose(1, 2)).contiguous()  # noqa: E731
     _check([last(t) for t in got], [last(t) for t in tensors], "bf16", f"beyond 2^31 {layout} {d}")
     op.close()
+
+
+@pytest.mark.parametrize("N", [2, 130])
+def test_many_slabs(N):
+    B, H, d = 4095, 16, 64
+    tensors = _inputs(B, H, N, d, d, "bf16")
+    op = attn.LinFusionAttention(B, H, N, d, eps=EPS, variant="split")
+    got = op.backward(*tensors)
+    for part in (slice(0, 2), slice(B - 2, B)):
+        _check([g[part] for g in got], [t[part] for t in tensors], "bf16", f"{B * H} slabs of {N}", rms=N > 8)
+    op.close()
