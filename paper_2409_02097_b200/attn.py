@@ -537,32 +537,41 @@ class LinFusionAttention:
         import torch
         index = self.desc.device
         device = torch.device("cuda", index)
-        for t, name, like in tensors:
+        for t, name, like in tensors + [o for o in outs if o[0] is not None]:
+            if like == "state":
+                self._check_state(t, name, device)
+                continue
             self._check(t, like)
-            if t.device != device:
+            if not t.is_cuda or t.get_device() != index:
                 raise ValueError(f"{name}: expected a tensor on {device}")
         for t, name in states:
             self._check_state(t, name, device)
-        for t, name, like in outs:
-            if t is not None and like == "state":
-                self._check_state(t, name, device)
-            elif t is not None:
-                self._check(t, like)
-                if t.device != device:
-                    raise ValueError(f"{name}: expected a tensor on {device}")
-        nbytes = self.backward_workspace_bytes()
-        with allocating_on(stream, index):
-            made = [t if t is not None else torch.empty(self.state_floats(), dtype=torch.float32, device=device) if like == "state" else
-                    torch.empty_like(next(x for x, _, kind in tensors if (kind == "v") == (like == "v"))) for t, _, like in outs]
-            if workspace is None:
-                workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
-            elif workspace.device != device or not workspace.is_contiguous():
-                raise ValueError(f"workspace: expected a contiguous tensor on {device}")
-            else:
-                nbytes = workspace.numel() * workspace.element_size()
         if stream is None:
+            made, workspace, nbytes = self._backward_made(tensors, outs, workspace, device)
             stream = torch._C._cuda_getCurrentRawStream(index)
+        else:
+            with allocating_on(stream, index):
+                made, workspace, nbytes = self._backward_made(tensors, outs, workspace, device)
         return made, (workspace.data_ptr(), nbytes, stream)
+
+    def _backward_made(self, tensors, outs, workspace, device):
+        """The outputs and the workspace, made where they were not given."""
+        import torch
+        made = []
+        for t, _, like in outs:
+            if t is None:
+                # the first tensor of a call has the shape of q and k, the last that of v
+                t = (torch.empty(self.state_floats(), dtype=torch.float32, device=device) if like == "state" else
+                     torch.empty_like(tensors[-1 if like == "v" else 0][0]))
+            made.append(t)
+        nbytes = self.backward_workspace_bytes()
+        if workspace is None:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        elif workspace.device != device or not workspace.is_contiguous():
+            raise ValueError(f"workspace: expected a contiguous tensor on {device}")
+        else:
+            nbytes = workspace.numel() * workspace.element_size()
+        return made, workspace, nbytes
 
     def backward(self, q, k, v, dy, state=None, dq=None, dk=None, dv=None, workspace=None, stream: Optional[int] = None):
         """(dq, dk, dv) from the gradient dy of the output.  ``state``: what ``save_state`` returned after the

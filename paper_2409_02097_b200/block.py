@@ -121,7 +121,7 @@ def _sm_count(index: int) -> int:
 
 def _look(t):
     """What the checks of a tensor depend on; its address is no part of it."""
-    return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device() if t.is_cuda else -1)
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device())
 
 
 class _Checked(dict):
@@ -374,14 +374,15 @@ class BlockNorm(_Fixed):
         if stream is not None and x.is_cuda:
             with allocating_on(stream, x.get_device()):
                 return self.forward(x, a, gate, scale, shift, pre_weight, pre_bias, post_weight, post_bias, y, n)
+        vectors = (("gate", gate), ("scale", scale), ("shift", shift), ("pre_weight", pre_weight), ("pre_bias", pre_bias),
+                   ("post_weight", post_weight), ("post_bias", post_bias))
+        # outputs that are made here follow from the inputs
+        key = (_look(x), _look(a), _look(y), _look(n), *[_look(t) for _, t in vectors])
         if a is not None and y is None:
             y = _like(x)
         if self.pre != NORM_NONE and n is None:
             n = _like(x)
         rows = (("x", x), ("a", a), ("y", y), ("n", n))
-        vectors = (("gate", gate), ("scale", scale), ("shift", shift), ("pre_weight", pre_weight), ("pre_bias", pre_bias),
-                   ("post_weight", post_weight), ("post_bias", post_bias))
-        key = tuple([_look(t) for _, t in rows + vectors])
         found = self._checked.get(key)
         if found is None:
             found = self._checked.keep(key, self._check(rows, vectors, tuple(x.shape), x.device))
@@ -409,14 +410,15 @@ class BlockNorm(_Fixed):
                 return self.backward(y, a, gate, scale, shift, pre_weight, pre_bias, post_weight, post_bias, dy, dn, dx, da, need_vectors,
                                      workspace)
         device = some.device
+        vectors = (("gate", gate), ("scale", scale), ("shift", shift), ("pre_weight", pre_weight), ("pre_bias", pre_bias),
+                   ("post_weight", post_weight), ("post_bias", post_bias))
+        # outputs that are made here follow from the inputs
+        key = (_look(y), _look(a), _look(dy), _look(dn), _look(dx), _look(da), *[_look(t) for _, t in vectors])
         if dx is None:
             dx = _like(some)
         if a is not None and da is None:
             da = _like(some)
         rows = (("y", y), ("a", a), ("dy", dy), ("dn", dn), ("dx", dx), ("da", da))
-        vectors = (("gate", gate), ("scale", scale), ("shift", shift), ("pre_weight", pre_weight), ("pre_bias", pre_bias),
-                   ("post_weight", post_weight), ("post_bias", post_bias))
-        key = tuple([_look(t) for _, t in rows + vectors])
         found = self._checked.get(key)
         if found is None:
             desc, structs, vec = self._check(rows, vectors, tuple(some.shape), device)
