@@ -128,10 +128,15 @@ linfusion_status_t linfusion_block_norm(const linfusion_block_norm_desc_t* desc,
                                         const linfusion_rows_t* a, const linfusion_block_norm_vectors_t* v,
                                         const linfusion_rows_t* y, const linfusion_rows_t* n, void* cuda_stream);
 
-/* Gradients of the vectors, fp32, NULL where not wanted: [C], or [B, C] dense where the vector has a batch
- * stride (gate, scale, shift).  A shared vector's gradient is summed over the batch. */
+/* Gradients of the vectors, fp32, NULL where not wanted: [C], summed over the batch, or, of a gate, scale or shift that has a
+ * batch stride or its bit in `per_entry`, dense [B, C].  (The bit is for one vector seen by every entry through a stride of 0
+ * whose gradients are wanted entry by entry.) */
+#define LINFUSION_PER_ENTRY_GATE 1u
+#define LINFUSION_PER_ENTRY_SCALE 2u
+#define LINFUSION_PER_ENTRY_SHIFT 4u
 typedef struct {
     float *gate, *scale, *shift, *pre_weight, *pre_bias, *post_weight, *post_bias;
+    uint32_t per_entry;
 } linfusion_block_norm_grads_t;
 
 /*

@@ -62,9 +62,10 @@ class NormVectors(ctypes.Structure):
 class NormGrads(ctypes.Structure):
     """Mirror of ``linfusion_block_norm_grads_t``."""
     _fields_ = [("gate", _vp), ("scale", _vp), ("shift", _vp), ("pre_weight", _vp), ("pre_bias", _vp), ("post_weight", _vp),
-                ("post_bias", _vp)]
+                ("post_bias", _vp), ("per_entry", ctypes.c_uint32)]
 
 
+PER_ENTRY = {"gate": 1, "scale": 2, "shift": 4}  # bits of NormGrads.per_entry
 _lib = None
 
 
@@ -286,8 +287,9 @@ class BlockNorm(_Fixed):
         n = (Pre(y) * pre_weight + pre_bias) * (1 + scale) + shift
 
     ``pre`` / ``post``: "none", "layer" or "rms".  Tensors have any batch and row strides that are multiples of 8
-    elements.  gate, scale and shift are [B, C] (views of one projection are fine) or [C] for all batch entries,
-    the weights and biases [C]; all in the storage type, absent where None.  Gradients of vectors are fp32.
+    elements.  gate, scale and shift are [B, C] (views of one projection and expanded vectors are fine) or [C] for all batch
+    entries, the weights and biases [C]; all in the storage type, absent where None.  Gradients of vectors are fp32, of the
+    vector's shape.
     """
 
     def __init__(self, C: int, pre: Optional[str] = "layer", post: Optional[str] = "none", eps: float = 1e-6,
@@ -326,7 +328,7 @@ class BlockNorm(_Fixed):
         if tuple(t.shape) == (self.C,):
             return 0
         if per_entry and tuple(t.shape) == (B, self.C):
-            # a stride of zero means one vector for all entries; a batch of one needs none of its own
+            # an expanded vector has a stride of zero; a batch of one needs none of its own
             return t.stride(0) if B > 1 else self.C
         raise ValueError(f"{name}: expected {(B, self.C)} or {(self.C,)}, got {tuple(t.shape)}" if per_entry else
                          f"{name}: expected {(self.C,)}, got {tuple(t.shape)}")
@@ -437,6 +439,8 @@ class BlockNorm(_Fixed):
                     for name, t in zip(names, torch.empty(shape, dtype=torch.float32, device=device).unbind(0)):
                         out[name] = t
                         setattr(grads, name, t.data_ptr())
+                    if dims == 2:  # whatever the vectors' strides: an expanded one gets the gradient of each entry too
+                        grads.per_entry = sum(PER_ENTRY[name] for name in names)
             if workspace is None:
                 workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=device)
             elif not workspace.is_cuda or workspace.device != device or not workspace.is_contiguous():

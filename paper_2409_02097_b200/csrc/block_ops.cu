@@ -474,6 +474,8 @@ linfusion_status_t linfusion_block_norm_backward(const linfusion_block_norm_desc
     if (branch && (!apart(*desc, da, y_read, false) || !apart(*desc, da, a, true) || !apart(*desc, da, dy, false) ||
                    !apart(*desc, da, dn, false) || !apart(*desc, da, dx, false) || !apart(*desc, da, *v)))
         return LINFUSION_ERR_INVALID_ARG;
+    if ((grads->per_entry & ~(LINFUSION_PER_ENTRY_GATE | LINFUSION_PER_ENTRY_SCALE | LINFUSION_PER_ENTRY_SHIFT)) != 0u)
+        return LINFUSION_ERR_INVALID_ARG;
     // a gradient of a vector that is not there
     if ((grads->gate != nullptr && v->gate.p == nullptr) || (grads->scale != nullptr && v->scale.p == nullptr) ||
         (grads->shift != nullptr && v->shift.p == nullptr) || (grads->pre_weight != nullptr && v->pre_weight == nullptr) ||
@@ -523,9 +525,9 @@ linfusion_status_t linfusion_block_norm_backward(const linfusion_block_norm_desc
     g.pre_b = p.pre_b;
     g.post_w = p.post_w;
     g.post_b = p.post_b;
-    g.gate_per_batch = v->gate.batch != 0;
-    g.scale_per_batch = v->scale.batch != 0;
-    g.shift_per_batch = v->shift.batch != 0;
+    g.gate_per_batch = v->gate.batch != 0 || (grads->per_entry & LINFUSION_PER_ENTRY_GATE) != 0u;
+    g.scale_per_batch = v->scale.batch != 0 || (grads->per_entry & LINFUSION_PER_ENTRY_SCALE) != 0u;
+    g.shift_per_batch = v->shift.batch != 0 || (grads->per_entry & LINFUSION_PER_ENTRY_SHIFT) != 0u;
     g.d_gate = grads->gate;
     g.d_scale = grads->scale;
     g.d_shift = grads->shift;

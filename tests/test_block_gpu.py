@@ -385,6 +385,29 @@ def test_norm_batch_of_one_and_shared_vectors_agree():
         assert torch.equal(a[n].reshape(b[n].shape), b[n])
 
 
+@pytest.mark.parametrize("expanded", [("gate",), ("scale",), ("shift",), ("gate", "scale", "shift")])
+@pytest.mark.parametrize("case", [(2, 37, 320, "layer", "rms", True, True, "batch", True), (3, 130, 1280, "rms", "layer", True, True, "batch", False)],
+                         ids=lambda c: "-".join(map(str, c[:5])))
+def test_expanded_vectors_get_a_gradient_for_each_entry(case, expanded):
+    # one vector seen by all entries through a batch stride of zero: the same values made dense give the same gradients, and
+    # their sum over the entries is what the vector itself gets
+    B, N, C, *_ = case
+    t, vec = _norm_case(case, torch.bfloat16)
+    op = _norm_op(case, "bf16")
+    dy, dn = _grads_of(case, "bf16")
+    one = {n: vec[n][:1] for n in expanded}
+    wide = dict(vec, **{n: v.expand(B, C) for n, v in one.items()})
+    dense = dict(vec, **{n: v.repeat(B, 1) for n, v in one.items()})
+    y, n0 = op.forward(t["x"], t["a"], **dense)
+    y1, n1 = op.forward(t["x"], t["a"], **wide)
+    assert torch.equal(y, y1) and torch.equal(n0, n1)
+    want = op.backward(y, t["a"], dy=dy, dn=dn, **dense)
+    _check_norm_backward(case, t, dense, y, dy, dn, want)
+    torch.full((1 << 22,), float("nan"), device="cuda")  # what the next call's outputs may be made of
+    got = op.backward(y, t["a"], dy=dy, dn=dn, **wide)
+    assert set(got) == set(want) and all(got[n].shape == want[n].shape and torch.equal(got[n], want[n]) for n in want)
+
+
 def test_norm_refuses_tensors():
     op = block.BlockNorm(64, pre="layer", post="rms")
     x = _randn(_gen(1), 2, 4, 64)

@@ -274,3 +274,21 @@ def test_strides_whose_reach_has_no_sense_are_refused(lib):
     if not torch.cuda.is_available():  # an axis of one row: its stride is not looked at
         _without_device(_norm_call(lib, B=1, batch=3, gate=(A16 * 9, 3)))
         _without_device(_rope_call(lib, B=1, q=_rope_tensor(in_b=-5, out_b=5)))
+
+
+def test_gradients_per_entry_are_known_bits(lib):
+    text = open(os.path.join(ROOT, "include", "linfusion_block.h")).read()
+    for name, bit in block.PER_ENTRY.items():
+        assert re.search(rf"#define LINFUSION_PER_ENTRY_{name.upper()} {bit}u", text)
+
+    def call(per_entry):
+        desc = block.NormDesc(2, 8, 64, block.NORM_LAYER, block.NORM_RMS, 1e-6, 1.0, 0)
+        rows = [ctypes.byref(block.Rows(A16 * i, 512, 64)) for i in range(1, 7)]
+        shared = block.NormVectors((A16 * 9, 0), (A16 * 10, 0), (A16 * 11, 0))
+        grads = block.NormGrads(gate=A16 * 20, per_entry=per_entry)
+        return lib.linfusion_block_norm_backward(ctypes.byref(desc), rows[0], rows[1], ctypes.byref(shared), *rows[2:],
+                                                 ctypes.byref(grads), A16 * 16, 1 << 30, None)
+
+    _refused(call(8))
+    if not torch.cuda.is_available():
+        _without_device(call(7))
