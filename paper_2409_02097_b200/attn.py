@@ -533,7 +533,7 @@ class LinFusionAttention:
         return self._backward_bytes
 
     def _backward_args(self, tensors, states, outs, workspace, stream):
-        """Checks; the outputs and the workspace that were not given; the stream."""
+        """Checks; the outputs and the workspace that were not given; the call's last arguments."""
         import torch
         index = self.desc.device
         device = torch.device("cuda", index)
@@ -552,7 +552,9 @@ class LinFusionAttention:
         else:
             with allocating_on(stream, index):
                 made, workspace, nbytes = self._backward_made(tensors, outs, workspace, device)
-        return made, (workspace.data_ptr(), nbytes, stream)
+        # the workspace itself is the caller's to hold until its kernels are enqueued: a thread that runs in between could else be
+        # handed its memory
+        return made, workspace, (workspace.data_ptr(), nbytes, stream)
 
     def _backward_made(self, tensors, outs, workspace, device):
         """The outputs and the workspace, made where they were not given."""
@@ -579,7 +581,7 @@ class LinFusionAttention:
         calls may overlap each other and forwards; ``workspace`` (a CUDA tensor of ``backward_workspace_bytes``)
         is allocated for the call when not given."""
         states = [] if state is None else [(state, "state")]
-        (dq, dk, dv), tail = self._backward_args(
+        (dq, dk, dv), held, tail = self._backward_args(
             [(q, "q", "q"), (k, "k", "k"), (v, "v", "v"), (dy, "dy", "v")], states,
             [(dq, "dq", "q"), (dk, "dk", "k"), (dv, "dv", "v")], workspace, stream)
         rc = self._lib.linfusion_attn_backward(
@@ -598,7 +600,7 @@ class LinFusionAttention:
 
     def backward_state(self, k, v, state=None, workspace=None, stream: Optional[int] = None):
         """S | z of the local tokens, for a backward pass that kept none (``sharding``: sum it over devices)."""
-        (state,), tail = self._backward_args([(k, "k", "k"), (v, "v", "v")], [], [(state, "state", "state")], workspace, stream)
+        (state,), held, tail = self._backward_args([(k, "k", "k"), (v, "v", "v")], [], [(state, "state", "state")], workspace, stream)
         rc = self._lib.linfusion_attn_backward_state(ctypes.byref(self.desc), k.data_ptr(), v.data_ptr(), state.data_ptr(), *tail)
         if rc != OK:
             raise LinFusionError(rc, "linfusion_attn_backward_state")
@@ -606,8 +608,8 @@ class LinFusionAttention:
 
     def backward_q(self, q, dy, state, dq=None, grad_state=None, workspace=None, stream: Optional[int] = None):
         """(dq, dS | dz of the local tokens) given the state; the second is to be summed over devices."""
-        (dq, grad_state), tail = self._backward_args([(q, "q", "q"), (dy, "dy", "v")], [(state, "state")],
-                                                     [(dq, "dq", "q"), (grad_state, "grad_state", "state")], workspace, stream)
+        (dq, grad_state), held, tail = self._backward_args([(q, "q", "q"), (dy, "dy", "v")], [(state, "state")],
+                                                           [(dq, "dq", "q"), (grad_state, "grad_state", "state")], workspace, stream)
         rc = self._lib.linfusion_attn_backward_q(ctypes.byref(self.desc), q.data_ptr(), dy.data_ptr(), state.data_ptr(),
                                                  dq.data_ptr(), grad_state.data_ptr(), *tail)
         if rc != OK:
@@ -616,8 +618,8 @@ class LinFusionAttention:
 
     def backward_kv(self, k, v, grad_state, dk=None, dv=None, workspace=None, stream: Optional[int] = None):
         """(dk, dv) given the (summed) state gradient."""
-        (dk, dv), tail = self._backward_args([(k, "k", "k"), (v, "v", "v")], [(grad_state, "grad_state")],
-                                             [(dk, "dk", "k"), (dv, "dv", "v")], workspace, stream)
+        (dk, dv), held, tail = self._backward_args([(k, "k", "k"), (v, "v", "v")], [(grad_state, "grad_state")],
+                                                   [(dk, "dk", "k"), (dv, "dv", "v")], workspace, stream)
         rc = self._lib.linfusion_attn_backward_kv(ctypes.byref(self.desc), k.data_ptr(), v.data_ptr(), grad_state.data_ptr(),
                                                   dk.data_ptr(), dv.data_ptr(), *tail)
         if rc != OK:
