@@ -513,6 +513,17 @@ linfusion_status_t linfusion_attn_save_state(linfusion_attn_t* h, float* state, 
  * gave up on a bounded wait (its outputs are then undefined), or CUDA.
  */
 linfusion_status_t linfusion_attn_backward_status(const linfusion_attn_desc_t* desc, const void* workspace, void* cuda_stream);
+/*
+ * Synchronize `cuda_stream` and count the waits that kernels of backward calls gave up on on `device` since the library was
+ * loaded.  The count only grows, whatever became of the calls' workspaces: a caller that keeps none compares it with what it
+ * read before.  Errors: INVALID_ARG, UNSUPPORTED (not a device of this library), CUDA.
+ */
+linfusion_status_t linfusion_attn_backward_expired(int32_t device, uint32_t* count, void* cuda_stream);
+/*
+ * Self-test of both reports: enqueue a kernel that waits on a barrier nothing completes (a quarter of a second) and then
+ * reports as the backward kernels do, in `workspace` and in the count.
+ */
+linfusion_status_t linfusion_attn_selftest_backward_wait(const linfusion_attn_desc_t* desc, void* workspace, void* cuda_stream);
 /* Bytes of workspace for `desc` on a device with `sm_count` SMs (<= 0: 148).  Pure host computation. */
 linfusion_status_t linfusion_attn_backward_workspace_bytes(const linfusion_attn_desc_t* desc, int sm_count, size_t* bytes);
 

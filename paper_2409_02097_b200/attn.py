@@ -33,6 +33,7 @@ EXPORTED = [
     "linfusion_attn_state_x", "linfusion_attn_apply_x", "linfusion_attn_branch_x", "linfusion_attn_forward_x",
     "linfusion_attn_save_state", "linfusion_attn_backward", "linfusion_attn_backward_state", "linfusion_attn_backward_q",
     "linfusion_attn_backward_kv", "linfusion_attn_backward_status", "linfusion_attn_backward_workspace_bytes",
+    "linfusion_attn_backward_expired", "linfusion_attn_selftest_backward_wait",
     "linfusion_attn_checked_build", "linfusion_attn_checked_violations", "linfusion_attn_checked_shrink_y",
 ]
 
@@ -148,6 +149,10 @@ def load_library() -> ctypes.CDLL:
     lib.linfusion_attn_backward_kv.argtypes = [ctypes.POINTER(Desc)] + [vp] * 6 + [sz, vp]
     lib.linfusion_attn_backward_status.restype = st
     lib.linfusion_attn_backward_status.argtypes = [ctypes.POINTER(Desc), vp, vp]
+    lib.linfusion_attn_backward_expired.restype = st
+    lib.linfusion_attn_backward_expired.argtypes = [ctypes.c_int32, ctypes.POINTER(ctypes.c_uint32), vp]
+    lib.linfusion_attn_selftest_backward_wait.restype = st
+    lib.linfusion_attn_selftest_backward_wait.argtypes = [ctypes.POINTER(Desc), vp, vp]
     lib.linfusion_attn_backward_workspace_bytes.restype = st
     lib.linfusion_attn_backward_workspace_bytes.argtypes = [ctypes.POINTER(Desc), st, ctypes.POINTER(sz)]
     lib.linfusion_attn_checked_build.restype = ctypes.c_int32
@@ -292,6 +297,22 @@ def allocating_on(stream: Optional[int], index: int):
                              torch.cuda.ExternalStream(stream, device=torch.device("cuda", index)))
 
 
+_expired_known = {}  # device -> the count as it was last read
+
+
+def backward_expired(device: int = 0, stream: Optional[int] = None) -> int:
+    """How many waits of backward kernels expired on `device` since the library was loaded (synchronizes the stream)."""
+    import torch
+    if stream is None:
+        stream = torch.cuda.current_stream(device).cuda_stream
+    n = ctypes.c_uint32(0)
+    rc = load_library().linfusion_attn_backward_expired(int(device), ctypes.byref(n), stream)
+    if rc != OK:
+        raise LinFusionError(rc, "linfusion_attn_backward_expired")
+    _expired_known[int(device)] = int(n.value)
+    return int(n.value)
+
+
 class LinFusionAttention:
     """One handle per shape.  ``forward`` takes bf16 CUDA tensors [B, H, N, d] (or [B, N, H, d]
     with ``layout="token_major"``).  With ``d_qk`` (Prop. 3's feature width d') Q and K are
@@ -311,6 +332,7 @@ class LinFusionAttention:
         self._h = linfusion_attn_create(self.desc)
         self._lent_ws = None
         self._backward_bytes = None
+        self._expired_seen = _expired_known.get(int(device), 0)
 
     # -- properties -------------------------------------------------------------------------
     @property
@@ -579,7 +601,7 @@ class LinFusionAttention:
         """(dq, dk, dv) from the gradient dy of the output.  ``state``: what ``save_state`` returned after the
         forward pass, or None to have it recomputed from k and v.  Uses nothing of the handle but its shape, so
         calls may overlap each other and forwards; ``workspace`` (a CUDA tensor of ``backward_workspace_bytes``)
-        is allocated for the call when not given."""
+        is allocated for the call when not given.  ``backward_status`` tells whether a bounded wait on the device ran out."""
         states = [] if state is None else [(state, "state")]
         (dq, dk, dv), held, tail = self._backward_args(
             [(q, "q", "q"), (k, "k", "k"), (v, "v", "v"), (dy, "dy", "v")], states,
@@ -591,9 +613,15 @@ class LinFusionAttention:
             raise LinFusionError(rc, "linfusion_attn_backward")
         return dq, dk, dv
 
-    def backward_status(self, workspace, stream: Optional[int] = None) -> int:
-        """Status of the last backward call that was given `workspace`: OK, or ERR_TIMEOUT (synchronizes the stream)."""
+    def backward_status(self, workspace=None, stream: Optional[int] = None) -> int:
+        """OK, or ERR_TIMEOUT where kernels gave up on a wait and gradients are undefined (synchronizes the stream).  With a
+        `workspace`: of the last backward call that was given it.  Without: of every backward call on the device, of any object and
+        with any workspace, since this object was made or last asked."""
         import torch
+        if workspace is None:
+            count = backward_expired(self.desc.device, stream)
+            seen, self._expired_seen = self._expired_seen, count
+            return OK if count == seen else ERR_TIMEOUT
         if stream is None:
             stream = torch.cuda.current_stream(self.desc.device).cuda_stream
         return int(self._lib.linfusion_attn_backward_status(ctypes.byref(self.desc), workspace.data_ptr(), stream))

@@ -421,6 +421,35 @@ linfusion_status_t linfusion_attn_backward_status(const linfusion_attn_desc_t* d
     return word == kStatusOk ? LINFUSION_OK : LINFUSION_ERR_TIMEOUT;
 }
 
+linfusion_status_t linfusion_attn_backward_expired(int32_t device, uint32_t* count, void* cuda_stream)
+{
+    if (count == nullptr || device < 0) return LINFUSION_ERR_INVALID_ARG;
+    const int sms = device_sm_count(device);
+    if (sms < 0) return sms == -2 ? LINFUSION_ERR_UNSUPPORTED : LINFUSION_ERR_CUDA;
+    CurrentDevice guard(device);
+    if (!guard.ok) return LINFUSION_ERR_CUDA;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    unsigned int n = 0;
+    cudaError_t e = cudaMemcpyFromSymbolAsync(&n, backward_expired_waits, sizeof(n), 0, cudaMemcpyDeviceToHost, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    if (e == cudaSuccess) *count = n;
+    return end(e);
+}
+
+linfusion_status_t linfusion_attn_selftest_backward_wait(const linfusion_attn_desc_t* desc, void* workspace, void* cuda_stream)
+{
+    BackwardPlan p;
+    const linfusion_status_t st = make_backward_plan(desc, 0, &p);
+    if (st != LINFUSION_OK) return st;
+    if (workspace == nullptr || !is_aligned(workspace, 256)) return LINFUSION_ERR_INVALID_ARG;
+    const int sms = device_sm_count(desc->device);
+    if (sms < 0) return sms == -2 ? LINFUSION_ERR_UNSUPPORTED : LINFUSION_ERR_CUDA;
+    CurrentDevice guard(desc->device);
+    if (!guard.ok) return LINFUSION_ERR_CUDA;
+    backward_wait_selftest_kernel<<<1, 32, 0, static_cast<cudaStream_t>(cuda_stream)>>>(static_cast<uint32_t*>(workspace));
+    return end(cudaGetLastError());
+}
+
 linfusion_status_t linfusion_attn_backward_workspace_bytes(const linfusion_attn_desc_t* desc, int sm_count, size_t* bytes)
 {
     if (bytes == nullptr) return LINFUSION_ERR_INVALID_ARG;

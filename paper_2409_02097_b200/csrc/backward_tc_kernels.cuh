@@ -55,7 +55,14 @@ static_assert(BackwardTc::STATE_SMEM <= 227 * 1024 && BackwardTc::KV_SMEM <= 227
 
 __host__ __device__ __forceinline__ long long tc_first_tile(long long g, long long W, long long G) { return g * W / G; }
 
-__device__ __forceinline__ void tc_expired(uint32_t* status) { atomicExch(status, kStatusWaitExpired); }
+// How often kernels of the backward pass gave up on a wait on this device since the library was loaded: what is left of it when
+// a call's workspace, with the status word in it, has gone.
+static __device__ unsigned int backward_expired_waits;
+__device__ __forceinline__ void tc_expired(uint32_t* status)
+{
+    atomicExch(status, kStatusWaitExpired);
+    atomicAdd(&backward_expired_waits, 1u);
+}
 __device__ __forceinline__ uint64_t policy_evict_normal()
 {
     uint64_t p;
@@ -241,6 +248,17 @@ __device__ __forceinline__ void tc_store(const CUtensorMap* a, const CUtensorMap
         mbar_arrive(&empty[s]);
     }
     tma_store_wait_all();
+}
+
+// Waits on a barrier that nothing completes, as the kernels below wait, and reports it as they do.
+static __global__ void backward_wait_selftest_kernel(uint32_t* __restrict__ status)
+{
+    __shared__ uint64_t bar;
+    if (threadIdx.x == 0) {
+        mbar_init(&bar, 1);
+        mbar_fence_init();
+        if (!mbar_wait(&bar, 0)) tc_expired(status);
+    }
 }
 
 template <int KIND, bool GRAD>

@@ -148,6 +148,11 @@ class TokenShardedAttention:
             allreduce_sum(state)
         return sharded_backward(lambda q_, dy_: self.op.backward_q(q_, dy_, state), self.op.backward_kv, allreduce_sum, q, k, v, dy)
 
+    def backward_status(self) -> int:
+        """Whether a bounded wait of a backward call on this rank's device ran out since this was last asked: the binding's
+        ``backward_status``.  A rank whose kernels gave up has handed the others an undefined part of the state's gradient."""
+        return self.op.backward_status()
+
     def forward_peers(self, q, k, v, peer_state_ptrs, barrier: Callable[[], None], y=None, events=None):
         """The same layer with the cross-device sum done by the apply step itself instead of an
         all-reduce: ``peer_state_ptrs`` lists, in rank order, device addresses of every rank's

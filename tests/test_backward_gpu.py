@@ -404,3 +404,24 @@ def test_many_slabs(N):
     for part in (slice(0, 2), slice(B - 2, B)):
         _check([g[part] for g in got], [t[part] for t in tensors], "bf16", f"{B * H} slabs of {N}", rms=N > 8)
     op.close()
+
+
+def test_an_expired_wait_is_reported():
+    """A wait that nothing ends gives up after its time, in the workspace's status word and in the device's count, which
+    answers for calls whose workspace has gone."""
+    op, tensors = attn.LinFusionAttention(1, 2, 64, 64, eps=EPS), _inputs(1, 2, 64, 64, 64, "bf16")
+    other = attn.LinFusionAttention(1, 2, 64, 64, eps=EPS)
+    op.backward(*tensors)
+    assert op.backward_status() == attn.OK
+    ws = torch.empty(op.backward_workspace_bytes(), dtype=torch.uint8, device="cuda")
+    op.backward(*tensors, workspace=ws)
+    assert op.backward_status(ws) == attn.OK
+    stream = torch.cuda.current_stream().cuda_stream
+    assert op._lib.linfusion_attn_selftest_backward_wait(op.desc, ws.data_ptr(), stream) == attn.OK
+    assert op.backward_status(ws) == attn.ERR_TIMEOUT
+    assert op.backward_status() == attn.ERR_TIMEOUT and op.backward_status() == attn.OK
+    assert other.backward_status() == attn.ERR_TIMEOUT
+    assert attn.LinFusionAttention(1, 2, 64, 64).backward_status() == attn.OK  # made after it was read
+    again = op.backward(*tensors, workspace=ws)                                # the context goes on
+    assert op.backward_status(ws) == attn.OK and op.backward_status() == attn.OK
+    _check(again, tensors, "bf16", "after a wait that expired", rms=False)

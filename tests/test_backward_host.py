@@ -1,5 +1,6 @@
 """The binding of the attention's backward pass, as far as no GPU is needed: stand-ins for the library and for device memory."""
 import contextlib
+import ctypes
 import gc
 import weakref
 
@@ -88,3 +89,40 @@ def test_what_a_call_allocates_lives_until_its_kernels_are_enqueued(made, name):
     CALLS[name](op, *_inputs())
     assert op._lib.calls == [name]
     assert len(alive) == 1 and len(alive[0]) >= 2 and all(alive[0]), alive
+
+
+def test_an_expired_wait_is_reported_without_a_workspace(monkeypatch):
+    # the count of the device stands for the workspaces that calls made for themselves and dropped
+    count = [0]
+
+    def during(name, args):
+        assert name == "linfusion_attn_backward_expired" and args[0] == 0
+        args[1]._obj.value = count[0]
+
+    lib = _Library(during)
+    monkeypatch.setattr(attn, "load_library", lambda: lib)
+    monkeypatch.setattr(attn, "_expired_known", {})
+    op, other = _op(), _op()
+    for o in (op, other):
+        o._expired_seen = 0
+    assert op.backward_status(stream=1) == attn.OK
+    count[0] = 3
+    assert op.backward_status(stream=1) == attn.ERR_TIMEOUT  # once
+    assert op.backward_status(stream=1) == attn.OK
+    assert other.backward_status(stream=1) == attn.ERR_TIMEOUT
+    assert attn._expired_known == {0: 3}                      # where objects made from now on begin
+    from paper_2409_02097_b200 import sharding
+    shard = object.__new__(sharding.TokenShardedAttention)
+    shard.op = type("Op", (), {"backward_status": lambda self: attn.ERR_TIMEOUT})()
+    assert shard.backward_status() == attn.ERR_TIMEOUT
+
+
+def test_the_count_of_expired_waits_refuses_bad_arguments():
+    lib, n = attn.load_library(), ctypes.c_uint32(0)
+    assert lib.linfusion_attn_backward_expired(0, None, None) == attn.ERR_INVALID_ARG
+    assert lib.linfusion_attn_backward_expired(-1, ctypes.byref(n), None) == attn.ERR_INVALID_ARG
+    desc = attn.make_desc(B, H, N, D)
+    for ws in (0, 4096 + 16):
+        assert lib.linfusion_attn_selftest_backward_wait(ctypes.byref(desc), ws, None) == attn.ERR_INVALID_ARG
+    if not torch.cuda.is_available():
+        assert lib.linfusion_attn_backward_expired(0, ctypes.byref(n), None) == attn.ERR_CUDA
