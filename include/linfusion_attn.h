@@ -476,8 +476,9 @@ int32_t linfusion_attn_launches_per_forward(const linfusion_attn_t* h);
  * (17 significant bits in bf16, 22 in fp16) and fp32 sums.  dQ is a difference in which what the values have in common
  * cancels: with values of mean m and spread s its relative error before rounding is about 2^-18 sqrt(N) m / s in bf16.
  * With one token Y_1 = V_1 den / (den + eps) whatever Q and K are: dQ and dK are then differences of equal numbers,
- * zero up to rounding.  With fp16 operands w f and dS are scaled to the type's range by a power of two for each (b, h);
- * what lies below 2^-13 or so of the largest (a feature near zero of phi(x) = x) keeps fewer bits than that.
+ * zero up to rounding.  With fp16 operands dS is scaled to the type's range by a power of two for each (b, h), w f by one for
+ * each feature (phi(x) = x: for each (b, h)), and phi(K) is not: values below 2^-13 or so of the scaled range's middle, or
+ * features below 2^-13, keep fewer bits than that, each off by 2^-25 of the scale at most.
  * With fp16 storage gradients below 6e-8 are lost in dQ, dK, dV as in any fp16 tensor: scale the loss.
  * Errors: INVALID_ARG (null, misaligned or overlapping pointers, sizes, eps), UNSUPPORTED (as create()), ALLOC (workspace
  * too small), CUDA.

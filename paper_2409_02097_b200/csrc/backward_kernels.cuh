@@ -98,6 +98,18 @@ __device__ __forceinline__ float pow2_scale(float x, int up)
     return __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
 }
 
+// fp16: the power of two by which w f of feature a is multiplied to become an operand.  Features of elu + 1 are not negative, so
+// w f_a = f_a / (f . z + eps) is at most 1 / z_a, and at most 2^16 / eps: each feature's own bound goes to 2^12, whatever the
+// others' sizes (one scale for all let a token whose weight is on a feature of small z overflow; so did z = 0, keys that
+// are all masked).
+__device__ __forceinline__ float feature_scale(float z, float eps) { return pow2_scale(1.0f / fmaxf(z, eps * 1.52587890625e-5f), 12); }
+// ... for features of either sign (phi(x) = x): one scale for the slab, from its largest z and its largest 1 / z (3e38 for a z that is
+// not positive and so says nothing).
+__device__ __forceinline__ float slab_scale(float z_max, float z_inv, float eps)
+{
+    return fmaxf(pow2_scale(z_inv, 12), 1.0f / pow2_scale(fmaxf(z_max, eps), 4));
+}
+
 // Copy tile `row0` .. of a slab into shared memory, rows past N as zeros.
 template <int D, int PITCH, int TILE, int THREADS>
 __device__ __forceinline__ void load_tile(unsigned char* dst, const __nv_bfloat16* base, int row_stride, int row0, int N)
@@ -251,27 +263,34 @@ backward_state_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* 
     };
     if (t_begin < t_end) fetch(t_begin);
 
-    float unscale_t = 1.0f, scale_w = 1.0f;
+    float unscale_t = 1.0f, scale_w[2] = {1.0f, 1.0f};  // of the thread's two features
     if (GRAD) {
         const float* S = state + static_cast<size_t>(slab) * grad_state_floats(DK, DV);
         float scale_s = 1.0f;
         if (sc.scaled) {
-            // fp16: S and w f by powers of two that keep head and tail inside the format.  w f is at most 1 / min z
-            // where features are not negative, so 2^12 min z bounds it; a z of zero or less says nothing, and then
-            // (or where some z is far below the others) the largest z does.
-            float big = 0.0f, z_max = 0.0f, z_inv = 0.0f;
+            // fp16: S and w f by powers of two that keep head and tail inside the format.
+            float big = 0.0f;
             for (int i = threadIdx.x; i < DK * DV; i += THREADS) big = fmaxf(big, fabsf(S[i]));
-            for (int i = threadIdx.x; i < DK; i += THREADS) {
-                const float v = S[DK * DV + i];
-                z_max = fmaxf(z_max, v);
-                z_inv = fmaxf(z_inv, v > 0.0f ? 1.0f / v : 3.0e38f);
-            }
             big = block_max(big, scratch, C::WQ);
-            z_max = block_max(z_max, scratch, C::WQ);
-            z_inv = block_max(z_inv, scratch, C::WQ);
             scale_s = pow2_scale(big, 12);
             unscale_t = 1.0f / scale_s;
-            if (sc.eps >= 0.0f) scale_w = fmaxf(pow2_scale(z_inv, 12), 1.0f / pow2_scale(z_max, 4));
+            if (sc.eps >= 0.0f && kind_phi(KIND) == kPhiIdentity) {
+                float z_max = 0.0f, z_inv = 0.0f;
+                for (int i = threadIdx.x; i < DK; i += THREADS) {
+                    const float v = S[DK * DV + i];
+                    z_max = fmaxf(z_max, v);
+                    z_inv = fmaxf(z_inv, v > 0.0f ? 1.0f / v : 3.0e38f);
+                }
+                z_max = block_max(z_max, scratch, C::WQ);
+                z_inv = block_max(z_inv, scratch, C::WQ);
+                scale_w[0] = scale_w[1] = slab_scale(z_max, z_inv, sc.eps);
+            } else if (sc.eps >= 0.0f) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const int row = m0 + lane / 4 + 8 * r;
+                    scale_w[r] = feature_scale(row < DK ? S[DK * DV + row] : 0.0f, sc.eps);
+                }
+            }
         }
         load_state<KIND, DK, DV, THREADS>(S, s_rows, z, scale_s);
     }
@@ -396,7 +415,7 @@ backward_state_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* 
                 }
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    split_pair<KIND>(wf[r][0] * scale_w, wf[r][1] * scale_w, &a_hi[2 * h + r], &a_lo[2 * h + r]);
+                    split_pair<KIND>(wf[r][0] * scale_w[r], wf[r][1] * scale_w[r], &a_hi[2 * h + r], &a_lo[2 * h + r]);
                     if (GRAD) out[2 * h + r] = pack_pair<KIND>(d[r][0], d[r][1]);
                 }
             }
@@ -418,10 +437,10 @@ backward_state_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* 
         }
     }
     float* out = partials + (static_cast<size_t>(slab) * chunks + chunk) * grad_state_floats(DK, DV);
-    const float unscale_w = 1.0f / scale_w;
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         const int row = m0 + lane / 4 + 8 * r;
+        const float unscale_w = 1.0f / scale_w[r];
 #pragma unroll
         for (int n = 0; n < C::VP / 8; ++n) {
             const int col = n * 8 + 2 * (lane & 3);

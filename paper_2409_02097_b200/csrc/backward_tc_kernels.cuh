@@ -47,7 +47,7 @@ struct BackwardTc {
     static constexpr int T_BUFFERS = 4, SEGMENT_TILES = 32;
     static constexpr int TMEM_COLS = 512;                    // T: 4 x 64, D: 2 x 64, dz: 2 x 64 (kv: 4 x 128)
     static constexpr int LEAD = 2;                           // tiles by which the first product runs ahead of the second
-    static constexpr int STATE_SMEM = STATE_STAGES * STAGE_BYTES + STATE_F * F_BYTES + S_BYTES + 1024 /*align*/ + 1024 /*z, barriers*/;
+    static constexpr int STATE_SMEM = STATE_STAGES * STAGE_BYTES + STATE_F * F_BYTES + S_BYTES + 1024 /*align*/ + 1024 /*z, scales, barriers*/;
     static constexpr int KV_SMEM = KV_STAGES * STAGE_BYTES + KV_F * F_BYTES + S_BYTES + 1024 /*align*/ + 1024 /*z, barriers*/;
     static constexpr int PARTIAL_FLOATS = 128 * 64 + 8 * 64; // D (head rows, tail rows), then dz of each consumer warp
 };
@@ -150,10 +150,10 @@ __device__ __forceinline__ float3 consumer_max(float3 v, float* scratch, int war
 }
 
 // The consumers lay S (dS) of a slab out as 64 K-major rows of 64 channels, head and tail, and z (dz) as 64 floats; zeros
-// where the widths end.  Returns with the scales of fp16 operands.
+// where the widths end.  Returns with the scales of fp16 operands: of S, and in scale_w (NULL: not wanted) those of the features' w f.
 template <int KIND, int WARPS>
 __device__ __forceinline__ void tc_load_state(const float* S, int dk, int dv, uint32_t operand, float* z, float* scratch, int tid,
-                                              bool scaled, float eps, float* scale_s, float* scale_w)
+                                              float eps, float* scale_s, float* scale_w)
 {
     constexpr int EACH = 4096 / (32 * WARPS), PER_ROW = 64 / EACH;  // floats of a thread, threads of a row
     const int warp = tid / 32, lane = tid & 31, row = tid / PER_ROW, col0 = (tid % PER_ROW) * EACH;
@@ -167,14 +167,15 @@ __device__ __forceinline__ void tc_load_state(const float* S, int dk, int dv, ui
     }
     const float zv = tid < dk ? S[dk * dv + tid] : 0.0f;
     if (tid < 64) z[tid] = zv;
-    *scale_s = *scale_w = 1.0f;
-    if (scaled) {
+    *scale_s = 1.0f;
+    if (kind_dtype(KIND) == kDtypeFp16) {
         float big = 0.0f;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) big = fmaxf(big, fabsf(x[i]));
         const float3 m = consumer_max<WARPS>(make_float3(big, zv, tid >= dk ? 0.0f : zv > 0.0f ? 1.0f / zv : 3.0e38f), scratch, warp, lane);
         *scale_s = pow2_scale(m.x, 12);
-        if (eps >= 0.0f) *scale_w = fmaxf(pow2_scale(m.z, 12), 1.0f / pow2_scale(m.y, 4));
+        if (scale_w != nullptr && tid < 64)
+            scale_w[tid] = eps < 0.0f ? 1.0f : kind_phi(KIND) == kPhiIdentity ? slab_scale(m.y, m.z, eps) : feature_scale(zv, eps);
     }
 #pragma unroll
     for (int h = 0; h < EACH / 8; ++h) {
@@ -274,7 +275,8 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
     unsigned char* F = smem + C::STATE_STAGES * C::STAGE_BYTES;
     unsigned char* So = F + C::STATE_F * C::F_BYTES;
     float* z = reinterpret_cast<float*>(So + C::S_BYTES);
-    float* scratch = z + 64;
+    float* scale_w = z + 64;  // [64] fp16: of each feature's w f
+    float* scratch = scale_w + 64;
     uint64_t* full = reinterpret_cast<uint64_t*>(scratch + 32);
     uint64_t* empty = full + C::STATE_STAGES;
     uint64_t* t_full = empty + C::STATE_STAGES;      // [T_BUFFERS]
@@ -396,17 +398,18 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
         int seg0 = 0, span = 0;  // segments before this unit
         for (int a = 0; a < run.n;) {
             const int slab = run.slab(a), b = run.unit_end(a);
-            float scale_s = 1.0f, scale_w = 1.0f;
+            float scale_s = 1.0f;
             float* partial = partials + (static_cast<size_t>(blockIdx.x) * spans + span) * C::PARTIAL_FLOATS;
             if (GRAD) {
                 consumer_sync<C::STATE_WARPS>();  // everybody is through with the slab before
                 tc_load_state<KIND, C::STATE_WARPS>(state + static_cast<size_t>(slab) * grad_state_floats(dk, dv), dk, dv, smem_u32(So), z, scratch, tid,
-                                    sc.scaled != 0, sc.eps, &scale_s, &scale_w);
+                                    sc.eps, &scale_s, scale_w);
                 fence_proxy_async_smem();
                 consumer_sync<C::STATE_WARPS>();  // z is there
                 if (lane == 0) mbar_arrive(s_ready);
             }
-            const float unscale_t = 1.0f / scale_s, unscale_w = 1.0f / scale_w;
+            constexpr bool SCALED = GRAD && kind_dtype(KIND) == kDtypeFp16;
+            const float unscale_t = 1.0f / scale_s, unscale_w = SCALED ? 1.0f / scale_w[r & 63] : 1.0f;
             if (ok) {
                 uint32_t nothing[16];
 #pragma unroll
@@ -480,12 +483,14 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                         }
                     }
                 }
-                const f32x2 ws = both(w * scale_w);
+                const f32x2 ws = both(w);
                 auto write_f = [&](int j) {  // piece j of the row of F, head and tail
                     uint32_t hi[4], lo[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float2 wf = unpack2(mul2(pack2(f[8 * j + 2 * i], f[8 * j + 2 * i + 1]), ws));
+                        f32x2 x = mul2(pack2(f[8 * j + 2 * i], f[8 * j + 2 * i + 1]), ws);
+                        if (SCALED) x = mul2(x, *reinterpret_cast<const f32x2*>(scale_w + 8 * j + 2 * i));
+                        const float2 wf = unpack2(x);
                         split_pair<KIND>(wf.x, wf.y, &hi[i], &lo[i]);
                     }
                     sts16(f_at + swizzled(r, j), hi[0], hi[1], hi[2], hi[3]);
@@ -747,10 +752,10 @@ backward_tc_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
         auto wait = [&](uint64_t* bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity)); };
         for (int a = 0; a < run.n;) {
             const int slab = run.slab(a), b = run.unit_end(a);
-            float scale_s, unused;
+            float scale_s;
             consumer_sync<C::KV_WARPS>();
             tc_load_state<KIND, C::KV_WARPS>(grad_state + static_cast<size_t>(slab) * grad_state_floats(dk, dv), dk, dv, smem_u32(So), z, scratch, tid,
-                                sc.scaled != 0, -1.0f, &scale_s, &unused);
+                                -1.0f, &scale_s, nullptr);
             fence_proxy_async_smem();
             consumer_sync<C::KV_WARPS>();
             if (lane == 0) mbar_arrive(s_ready);

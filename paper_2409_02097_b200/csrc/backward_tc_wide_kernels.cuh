@@ -26,7 +26,7 @@ struct BackwardTcWide {
     static constexpr int FLO_BYTES = 2 * kTcTileBytes, S_HALF = VA * kTcTileBytes, S_BYTES = 2 * S_HALF;
     static constexpr int VW = 64 * VA, SEGMENT_TILES = 32;
     static constexpr int T_COL = 0, D_COL = 128, DZ_COL = 384;      // state: T, two D of VW columns, dz of each atom
-    static constexpr int SMEM = STAGES * STAGE_BYTES + FLO_BYTES + S_BYTES + 1024 /*align*/ + 1024 /*z, barriers*/;
+    static constexpr int SMEM = STAGES * STAGE_BYTES + FLO_BYTES + S_BYTES + 1024 /*align*/ + 2048 /*z, scales, barriers*/;
     static constexpr int PARTIAL_FLOATS = 2 * 128 * VW + WARPS * 64;
 };
 static_assert(BackwardTcWide<2>::SMEM <= 227 * 1024 && BackwardTcWide<1>::SMEM <= 227 * 1024, "shared memory");
@@ -34,14 +34,14 @@ static_assert(BackwardTcWide<2>::SMEM <= 227 * 1024 && BackwardTcWide<1>::SMEM <
 // S (dS) as 128 K-major rows (features) of VA atoms, head, then tail; z (dz) as 128 floats.
 template <int KIND, int VA>
 __device__ __forceinline__ void wide_load_state(const float* S, int dk, int dv, uint32_t operand, float* z, float* scratch, int tid,
-                                                bool scaled, float eps, float* scale_s, float* scale_w)
+                                                float eps, float* scale_s, float* scale_w)
 {
     using C = BackwardTcWide<VA>;
     const int warp = tid / 32, lane = tid & 31, row = tid / 2, col0 = (tid & 1) * (C::VW / 2);
     const float zv = tid < dk ? S[dk * dv + tid] : 0.0f;
     if (tid < 128) z[tid] = zv;
-    *scale_s = *scale_w = 1.0f;
-    if (scaled) {
+    *scale_s = 1.0f;
+    if (kind_dtype(KIND) == kDtypeFp16) {
         float big = 0.0f;
         if (row < dk)
             for (int i = 0; i < C::VW / 2; i += 2)
@@ -51,7 +51,8 @@ __device__ __forceinline__ void wide_load_state(const float* S, int dk, int dv, 
                 }
         const float3 m = consumer_max<C::WARPS>(make_float3(big, zv, tid >= dk ? 0.0f : zv > 0.0f ? 1.0f / zv : 3.0e38f), scratch, warp, lane);
         *scale_s = pow2_scale(m.x, 12);
-        if (eps >= 0.0f) *scale_w = fmaxf(pow2_scale(m.z, 12), 1.0f / pow2_scale(m.y, 4));
+        if (scale_w != nullptr && tid < 128)
+            scale_w[tid] = eps < 0.0f ? 1.0f : kind_phi(KIND) == kPhiIdentity ? slab_scale(m.y, m.z, eps) : feature_scale(zv, eps);
     }
 #pragma unroll
     for (int j = 0; j < C::VW / 16; ++j) {
@@ -131,7 +132,8 @@ backward_tc_wide_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const 
     unsigned char* Flo = smem + C::STAGES * C::STAGE_BYTES;
     unsigned char* So = Flo + C::FLO_BYTES;
     float* z = reinterpret_cast<float*>(So + C::S_BYTES);
-    float* scratch = z + 128;
+    float* scale_w = z + 128;  // [128] fp16: of each feature's w f
+    float* scratch = scale_w + 128;
     uint64_t* full = reinterpret_cast<uint64_t*>(scratch + 32);
     uint64_t* empty = full + C::STAGES;
     uint64_t* written = empty + C::STAGES;
@@ -261,17 +263,18 @@ backward_tc_wide_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const 
         int seg0 = 0, span = 0;
         for (int first = 0; first < run.n;) {
             const int slab = run.slab(first), last = run.unit_end(first);
-            float scale_s = 1.0f, scale_w = 1.0f;
+            float scale_s = 1.0f;
             float* partial = partials + (static_cast<size_t>(blockIdx.x) * spans + span) * C::PARTIAL_FLOATS;
             if (GRAD) {
                 consumer_sync<C::WARPS>();
                 wide_load_state<KIND, VA>(state + static_cast<size_t>(slab) * grad_state_floats(dk, dv), dk, dv, smem_u32(So), z, scratch,
-                                          tid, sc.scaled != 0, sc.eps, &scale_s, &scale_w);
+                                          tid, sc.eps, &scale_s, scale_w);
                 fence_proxy_async_smem();
                 consumer_sync<C::WARPS>();
                 if (lane == 0) mbar_arrive(s_ready);
             }
-            const float unscale_t = 1.0f / scale_s, unscale_w = 1.0f / scale_w;
+            constexpr bool SCALED = GRAD && kind_dtype(KIND) == kDtypeFp16;
+            const float unscale_t = 1.0f / scale_s, unscale_w = SCALED ? 1.0f / scale_w[a * 64 + (r & 63)] : 1.0f;
             if (ok) {
                 uint32_t nothing[16];
 #pragma unroll
@@ -353,7 +356,7 @@ backward_tc_wide_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const 
                     }
                 }
                 if (ok) {
-                    const f32x2 mc = both(-c), wu = both(w * unscale_t), cz = both(GRAD ? -c * unscale_t * w : w), ws = both(w * scale_w);
+                    const f32x2 mc = both(-c), wu = both(w * unscale_t), cz = both(GRAD ? -c * unscale_t * w : w), ws = both(w);
 #pragma unroll
                     for (int h = 0; h < 4; ++h) {
                         uint32_t t[16], dz[16];
@@ -369,7 +372,9 @@ backward_tc_wide_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const 
                                 const float2 sum = unpack2(fma2(fp, cz, pack2(__uint_as_float(dz[k]), __uint_as_float(dz[k + 1]))));
                                 dz[k] = __float_as_uint(sum.x);
                                 dz[k + 1] = __float_as_uint(sum.y);
-                                const float2 wf = unpack2(mul2(fp, ws));
+                                f32x2 wfp = mul2(fp, ws);
+                                if (SCALED) wfp = mul2(wfp, *reinterpret_cast<const f32x2*>(scale_w + a * 64 + ch));
+                                const float2 wf = unpack2(wfp);
                                 split_pair<KIND>(wf.x, wf.y, &hi[i], &lo[i]);
                                 if (GRAD) {
                                     const f32x2 tp = pack2(__uint_as_float(t[k]), __uint_as_float(t[k + 1]));
@@ -530,10 +535,10 @@ backward_tc_wide_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
         auto wait = [&](uint64_t* bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity)); };
         for (int first = 0; first < run.n;) {
             const int slab = run.slab(first), last = run.unit_end(first);
-            float scale_s, unused;
+            float scale_s;
             consumer_sync<C::WARPS>();
             wide_load_state<KIND, VA>(grad_state + static_cast<size_t>(slab) * grad_state_floats(dk, dv), dk, dv, smem_u32(So), z, scratch,
-                                      tid, sc.scaled != 0, -1.0f, &scale_s, &unused);
+                                      tid, -1.0f, &scale_s, nullptr);
             fence_proxy_async_smem();
             consumer_sync<C::WARPS>();
             if (lane == 0) mbar_arrive(s_ready);

@@ -425,3 +425,56 @@ def test_an_expired_wait_is_reported():
     again = op.backward(*tensors, workspace=ws)                                # the context goes on
     assert op.backward_status(ws) == attn.OK and op.backward_status() == attn.OK
     _check(again, tensors, "bf16", "after a wait that expired", rms=False)
+
+
+MASKED = [(1, 2, 300, 64, 64), (2, 4, 4200, 64, 64), (1, 5, 4001, 128, 128), (1, 2, 200, 160, 160), (2, 4, 4353, 40, 40)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("case", MASKED, ids=lambda c: "x".join(map(str, c)))
+def test_masked_keys_and_queries(case, dtype):
+    # keys of -inf have phi = 0: they take no part and get no gradient; queries of -inf have no weight on anything
+    B, H, N, dk, dv = case
+    q, k, v, dy = _inputs(B, H, N, dk, dv, dtype)
+    k[:, :, N // 3:N // 2] = -math.inf
+    k[:, -1] = -math.inf       # the last head's keys, all of them: its state is zero, den is eps
+    q[:, :, 5:40] = -math.inf
+    op = attn.LinFusionAttention(B, H, N, dv, eps=EPS, variant="split", dtype=dtype)
+    got = op.backward(q, k, v, dy)
+    _check(got, (q, k, v, dy), dtype, f"masked {case} {dtype}", rms=False)
+    assert (got[1][:, :, N // 3:N // 2] == 0).all() and (got[0][:, :, 5:40] == 0).all()
+    assert all((g[:, -1] == 0).all() for g in got)
+    op.close()
+
+
+@pytest.mark.parametrize("case", MASKED, ids=lambda c: "x".join(map(str, c)))
+def test_a_query_on_a_feature_of_small_keys_fp16(case):
+    # z of one feature 2^-22 of the others', and queries with their weight on it: w f there is some 2^20 times the others'
+    B, H, N, dk, dv = case
+    tensors = _inputs(B, H, N, dk, dv, "fp16")
+    q, k, v, dy = tensors
+    k[..., 0] = -15.25
+    q[:, :, 1:9] = -20.0
+    q[:, :, 1:9, 0] = 3.0
+    op = attn.LinFusionAttention(B, H, N, dv, eps=0.0, variant="split", dtype="fp16")
+    got = op.backward(*tensors)
+    want, sizes = ref.attention_backward(*tensors, 0.0)
+    # phi(K) enters as two fp16 numbers of one grid where it is small: off by 2^-25 (half of its smallest number), times |dS|
+    fq, z = ref.phi(q.double()), ref.phi(k.double()).sum(-2)
+    dS = (fq / (fq @ z.unsqueeze(-1))).transpose(-1, -2) @ dy.double()
+    extra = (0.0, 0.0, 2.0 ** -25 * dS.abs().sum(-2, keepdim=True))
+    for name, x, w, size, e in zip(("dq", "dk", "dv"), got, want, sizes, extra):
+        ref.assert_rounded(x, w, SLACK * size + e, f"{case} {name}")
+    op.close()
+
+
+@pytest.mark.parametrize("N,d", [(200, 64), (4200, 64), (4001, 128), (200, 160)])
+def test_keys_of_zero_where_phi_is_the_identity_fp16(N, d):
+    # z = 0, den = eps: w f is a million times f, and dV = dS^T 0 is zero all the same
+    tensors = _inputs(1, 5, N, d, d, "fp16", kind=1, grad_scale=2.0 ** -10)
+    tensors[1][:, -1] = 0
+    op = attn.LinFusionAttention(1, 5, N, d, phi=1, eps=EPS, variant="split", dtype="fp16")
+    dq, dk, dv = op.backward(*tensors)
+    assert (dv[:, -1] == 0).all() and (dq[:, -1] == 0).all() and not torch.isnan(dk).any()
+    _check([t[:, :-1] for t in (dq, dk, dv)], [t[:, :-1] for t in tensors], "fp16", f"identity {N} {d}", kind=1, rms=False)
+    op.close()
