@@ -462,7 +462,8 @@ int32_t linfusion_attn_launches_per_forward(const linfusion_attn_t* h);
  *     dQ_i = phi'(Q_i) * w (t - c z)          dS = sum_i (w f)^T g,   dz = - sum_i c w f
  *     dK_j = phi'(K_j) * (dS V_j + dz)        dV_j = dS^T phi(K_j)
  *
- * phi'(x) of elu + 1 is 1 for x > 0, exp(x) otherwise.  Neither Y nor anything of size N x N is needed.
+ * phi'(x) of elu + 1 is 1 for x > 0, exp(x) otherwise.  Neither Y nor anything of size N x N is needed.  A NaN goes wherever
+ * these formulas take it (forward() takes phi of a NaN for 1); a key of -inf has phi = phi' = 0 and no part in anything.
  *
  * These calls take a descriptor and no handle (its variant bits play no part), allocate nothing, keep nothing
  * between calls, and may run at the same time on any streams as long as each has a workspace of its own; they

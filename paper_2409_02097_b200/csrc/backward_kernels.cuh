@@ -44,7 +44,14 @@ __device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src, bool 
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
 
-// phi and its slope of one value.
+// The smaller of two values, NaN where one is NaN (fminf drops it, and with it phi of a NaN would be 1).
+__device__ __forceinline__ float min_nan(float a, float b)
+{
+    float y;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+// phi and its slope of one value; both NaN for a NaN.
 template <int KIND>
 __device__ __forceinline__ void phi_and_slope(float x, float* f, float* slope)
 {
@@ -53,9 +60,16 @@ __device__ __forceinline__ void phi_and_slope(float x, float* f, float* slope)
         *slope = 1.0f;
         return;
     }
-    const float e = ex2_approx(fminf(x, 0.0f) * 1.4426950408889634f);
+    const float e = ex2_approx(min_nan(x, 0.0f) * 1.4426950408889634f);
     *f = fmaxf(x, 0.0f) + e;
     *slope = e;
+}
+template <int KIND>
+__device__ __forceinline__ float phi_or_nan(float x)
+{
+    float f, slope;
+    phi_and_slope<KIND>(x, &f, &slope);
+    return f;
 }
 
 // A pair of values as head and tail in the storage type.
@@ -340,7 +354,7 @@ backward_state_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* 
                             float den = 0.0f, ft = 0.0f;
 #pragma unroll
                             for (int r = 0; r < 2; ++r) {
-                                const float f = phi<KIND>(e == 0 ? pair_lo<KIND>(x[2 * h + r]) : pair_hi<KIND>(x[2 * h + r]));
+                                const float f = phi_or_nan<KIND>(e == 0 ? pair_lo<KIND>(x[2 * h + r]) : pair_hi<KIND>(x[2 * h + r]));
                                 den = fmaf(f, zr[r], den);
                                 ft = fmaf(f, tt[h][2 * r + e], ft);
                             }

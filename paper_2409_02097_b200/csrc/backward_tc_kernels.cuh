@@ -119,14 +119,14 @@ __device__ __forceinline__ void phi_row(uint32_t tile, int r, int first, float (
         const uint32_t p[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            f[8 * j + 2 * i] = phi<KIND>(pair_lo<KIND>(p[i]));
-            f[8 * j + 2 * i + 1] = phi<KIND>(pair_hi<KIND>(p[i]));
+            f[8 * j + 2 * i] = phi_or_nan<KIND>(pair_lo<KIND>(p[i]));
+            f[8 * j + 2 * i + 1] = phi_or_nan<KIND>(pair_hi<KIND>(p[i]));
         }
     }
 }
 // phi' from phi: above zero phi > 1 and the slope is 1, below the slope is phi itself.
 template <int KIND>
-__device__ __forceinline__ float slope_of(float f) { return kind_phi(KIND) == kPhiIdentity ? 1.0f : fminf(f, 1.0f); }
+__device__ __forceinline__ float slope_of(float f) { return kind_phi(KIND) == kPhiIdentity ? 1.0f : min_nan(f, 1.0f); }
 
 // Largest of three values over the consumers; `scratch`: three floats of shared memory for each warp.
 template <int WARPS>

@@ -478,3 +478,33 @@ def test_keys_of_zero_where_phi_is_the_identity_fp16(N, d):
     assert (dv[:, -1] == 0).all() and (dq[:, -1] == 0).all() and not torch.isnan(dk).any()
     _check([t[:, :-1] for t in (dq, dk, dv)], [t[:, :-1] for t in tensors], "fp16", f"identity {N} {d}", kind=1, rms=False)
     op.close()
+
+
+@pytest.mark.parametrize("normalize", [True, False])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("case", [(1, 3, 300, 64, 64), (2, 4, 4200, 64, 64), (1, 5, 4001, 128, 128), (1, 3, 70, 160, 160)], ids=lambda c: "x".join(map(str, c)))
+def test_a_nan_goes_where_the_formulas_take_it(case, dtype, normalize):
+    # one NaN in Q, K, V or dY of the first head, the state that of clean K and V; the other heads are as without it
+    B, H, N, dk, dv = case
+    clean = _inputs(B, H, N, dk, dv, dtype, grad_scale=2.0 ** -4)
+    op = attn.LinFusionAttention(B, H, N, dv, eps=EPS, variant="split", dtype=dtype, normalize=normalize)
+    state = op.backward_state(*clean[1:3])
+    before = op.backward(*clean, state=state)
+    q, k, v, dy = (t.double() for t in clean)
+    fk = ref.phi(k)
+    S, z = fk.transpose(-1, -2) @ v, fk.sum(-2)
+    for which in range(4):
+        bad = [t.clone() for t in clean]
+        bad[which][0, 0, N - 2, 5] = math.nan
+        got = op.backward(*bad, state=state)
+        q, k, v, dy = (t[0, 0].double() for t in bad)
+        f, t = ref.phi(q), dy @ S[0, 0].T
+        w = 1 / (f @ z[0, 0] + EPS)[:, None] if normalize else torch.ones_like(f[:, :1])
+        c = w * (f * t).sum(-1, keepdim=True) if normalize else torch.zeros_like(w)
+        dS, dz = (w * f).T @ dy, -(c * w * f).sum(0)
+        want = (ref.phi_slope(q) * w * (t - c * z[0, 0]), ref.phi_slope(k) * (v @ dS.T + (dz if normalize else 0.0)), ref.phi(k) @ dS)
+        for name, x, x0, y in zip(("dq", "dk", "dv"), got, before, want):
+            # where the formulas are clean nothing is NaN, and the other way round (a term of NaN is one whatever it is multiplied by)
+            assert torch.equal(torch.isnan(x[0, 0]), torch.isnan(y)), f"{'qkvg'[which]} {name}"
+            assert torch.equal(x[:, 1:], x0[:, 1:])
+    op.close()
