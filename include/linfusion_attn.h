@@ -475,7 +475,10 @@ int32_t linfusion_attn_launches_per_forward(const linfusion_attn_t* h);
  * call's kernels have run.
  * The products run on the tensor cores with every computed operand as head + tail of the storage type
  * (17 significant bits in bf16, 22 in fp16) and fp32 sums.  dQ is a difference in which what the values have in common
- * cancels: with values of mean m and spread s its relative error before rounding is about 2^-18 sqrt(N) m / s in bf16.
+ * cancels: that part of S, the nearest multiple z mu^T, is taken off in fp32 before the products.  What S itself is off by
+ * then counts sqrt(N) m / s times in dQ for values of mean m and spread s: 2^-25 of its elements where `state` is exact to
+ * fp32, some 2^-22 where it is recomputed (the tensor cores' running sums), and the forward pass's 16-bit phi(K), the
+ * same in S and z, where it was saved.
  * With one token Y_1 = V_1 den / (den + eps) whatever Q and K are: dQ and dK are then differences of equal numbers,
  * zero up to rounding.  With fp16 operands dS is scaled to the type's range by a power of two for each (b, h), w f by one for
  * each feature (phi(x) = x: for each (b, h)), and phi(K) is not: values below 2^-13 or so of the scaled range's middle, or

@@ -15,11 +15,16 @@
 // on the way, then K, V -> dK, dV.  Nothing of size N x N, and nothing of size N but the gradients, is written.
 //
 // Precision.  t - c z is a difference: with values that have a mean, S is that mean times z plus a remainder about
-// sqrt(N) times smaller, and only the remainder is left.  A state rounded to 16 bits (as the forward's apply operand
-// is) would lose it, so every operand of the tensor-core products that is not an input tensor (S, w f, dS, phi(k)) is
-// carried as a head and a tail of the storage type, x = hi + lo with |x - hi - lo| <= 2^-17 |x| (bf16) or 2^-22 (fp16):
-// two products in place of one (three for dS^T f).  The results are then off by little more than the one rounding
-// of the 16-bit outputs.
+// sqrt(N) times smaller, and only the remainder is left.  So the mean leaves before the products: with any fixed mu and
+// R = S - z mu^T, and c' = w (f . R g - eps mu . g),
+//
+//     t - c z = R g - c' z        c = c' + mu . g        dz = - sum (w f) c' - dS mu
+//
+// mu = S^T z / (z . z) leaves the smallest R.  (The term with eps is formed only for tokens where w eps is 2^-24 or more: below,
+// it is less than what the rounding of S to fp32 leaves.)  Every operand of the tensor-core products that is not an input
+// tensor (R, w f, dS, phi(k)) is carried as a head and a tail of the storage type, x = hi + lo with |x - hi - lo| <= 2^-17 |x|
+// (bf16) or 2^-22 (fp16): two products in place of one (three for dS^T f).  The results are then off by little more
+// than the one rounding of the 16-bit outputs.
 #pragma once
 
 #include "common.cuh"
@@ -94,7 +99,7 @@ struct BackwardCfg {
     static constexpr int STAGE = TILE * (PITCHK + PITCHV);
     static constexpr int S_HALF = KP * PITCHV;  // the state's head, or its tail
     static constexpr int SMEM_STATE = 2 * STAGE;
-    static constexpr int SMEM_Q = 2 * STAGE + 2 * S_HALF + KP * 4 + WQ * TILE * 8 + TILE * 8 + WQ * 16 * TILE * 4;
+    static constexpr int SMEM_Q = 2 * STAGE + 2 * S_HALF + KP * 4 + WQ * TILE * 8 + TILE * 8 + WQ * 16 * TILE * 4 + VP * 4;
     static constexpr int SMEM_KV = 2 * STAGE + 2 * S_HALF + KP * 4 + 2 * TILE * PITCHK;  // head and tail of phi(k)
 };
 
@@ -168,34 +173,113 @@ __device__ __forceinline__ float block_max(float v, float* scratch, int warps)
     return v;
 }
 
+// The term of c' with eps counts from this w eps on.
+constexpr float kEpsCounts = 5.9604645e-8f;  // 2^-24
+
+// A column of mu = S^T z / (z . z) from the two sums; zero where it is not finite (no keys at all, sums beyond fp32): any mu is right.
+__device__ __forceinline__ float mean_of(float sum, float squares)
+{
+    const float m = sum / squares;
+    return fabsf(m) < 3.0e38f ? m : 0.0f;
+}
+// mu . g of eight channels from one 16-byte piece of a row of dY.
+template <int KIND>
+__device__ __forceinline__ float mean_dot(const uint4& g, const float* mu, float sum)
+{
+    const uint32_t p[4] = {g.x, g.y, g.z, g.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum = fmaf(pair_lo<KIND>(p[i]), mu[2 * i], fmaf(pair_hi<KIND>(p[i]), mu[2 * i + 1], sum));
+    return sum;
+}
+
 // The block lays S (dS) out in shared memory as rows of features, head and tail, zeros where the widths end, and z (dz)
-// as floats.
-template <int KIND, int DK, int DV, int THREADS>
-__device__ __forceinline__ void load_state(const float* S, unsigned char* hi_rows, float* z, float scale)
+// as floats; CENTRED: R = S - z mu^T in place of S where eps is not negative, and mu as VP floats, zeros behind DV.  SCALED: by the
+// power of two that takes the largest value to 2^12, which is returned.  Each thread has one 16-byte piece of every ROWS-th row
+// (all loads in flight together: one by one, ten of them were a third of a call of one tile), kept in registers through the
+// sums of mu, which pass through the rows' place.
+template <int KIND, int DK, int DV, int THREADS, bool CENTRED>
+__device__ __forceinline__ float load_state(const float* S, float eps, bool scaled, unsigned char* hi_rows, float* z, float* mu,
+                                            float* scratch)
 {
     using C = BackwardCfg<DK, DV>;
-    constexpr int PIECES = C::KP * (C::VP / 8);
-    // Unrolled, so that the loads are in flight together: one by one, ten of them were a third of a call of one tile.
+    constexpr int PER_ROW = C::VP / 8, ROWS = THREADS / PER_ROW, STEPS = (C::KP + ROWS - 1) / ROWS;
+    static_assert(ROWS * (C::VP + 1) * 4 <= 2 * C::S_HALF && C::VP <= THREADS, "the sums of mu take the rows' place");
+    const int slice = threadIdx.x / PER_ROW, piece = threadIdx.x - slice * PER_ROW;
+    float x[STEPS][8];
 #pragma unroll
-    for (int n = 0; n < (PIECES + THREADS - 1) / THREADS; ++n) {
-        const int i = n * THREADS + threadIdx.x, row = i / (C::VP / 8), piece = i - row * (C::VP / 8);
-        if (PIECES % THREADS != 0 && i >= PIECES) break;
-        float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f), y = x;
-        if (row < DK && piece < DV / 8) {
+    for (int n = 0; n < STEPS; ++n) {
+        const int row = n * ROWS + slice;
+        float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f), b = a;
+        if (slice < ROWS && row < DK && piece < DV / 8) {
             const float4* p = reinterpret_cast<const float4*>(S + row * DV + 8 * piece);
-            x = p[0];
-            y = p[1];
+            a = p[0];
+            b = p[1];
         }
+        x[n][0] = a.x, x[n][1] = a.y, x[n][2] = a.z, x[n][3] = a.w, x[n][4] = b.x, x[n][5] = b.y, x[n][6] = b.z, x[n][7] = b.w;
+    }
+    for (int i = threadIdx.x; i < C::KP; i += THREADS) z[i] = i < DK ? S[DK * DV + i] : 0.0f;
+    if (CENTRED) {
+        float* sums = reinterpret_cast<float*>(hi_rows);  // [ROWS][VP], then [ROWS] of z . z
+        __syncthreads();
+        if (slice < ROWS && eps >= 0.0f) {
+            float s[8] = {}, zz = 0.0f;
+#pragma unroll
+            for (int n = 0; n < STEPS; ++n) {
+                const int row = n * ROWS + slice;
+                const float zr = row < C::KP ? z[row] : 0.0f;
+                zz = fmaf(zr, zr, zz);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[i] = fmaf(zr, x[n][i], s[i]);
+            }
+            float4* to = reinterpret_cast<float4*>(sums + slice * C::VP + 8 * piece);
+            to[0] = make_float4(s[0], s[1], s[2], s[3]);
+            to[1] = make_float4(s[4], s[5], s[6], s[7]);
+            if (piece == 0) sums[ROWS * C::VP + slice] = zz;
+        }
+        __syncthreads();
+        if (threadIdx.x < C::VP) {
+            float s = 0.0f, zz = 0.0f;
+            if (eps >= 0.0f) {
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i) {
+                    s += sums[i * C::VP + threadIdx.x];
+                    zz += sums[ROWS * C::VP + i];
+                }
+            }
+            mu[threadIdx.x] = eps >= 0.0f ? mean_of(s, zz) : 0.0f;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < STEPS; ++n) {
+            const int row = n * ROWS + slice;
+            const float zr = slice < ROWS && row < C::KP ? -z[row] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[n][i] = fmaf(zr, mu[8 * piece + i], x[n][i]);
+        }
+    }
+    float scale = 1.0f;
+    if (scaled) {
+        float big = 0.0f;
+#pragma unroll
+        for (int n = 0; n < STEPS; ++n)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) big = fmaxf(big, fabsf(x[n][i]));
+        scale = pow2_scale(block_max(big, scratch, THREADS / 32), 12);
+    }
+#pragma unroll
+    for (int n = 0; n < STEPS; ++n) {
+        const int row = n * ROWS + slice;
+        if (slice >= ROWS || row >= C::KP) continue;
         uint4 hi, lo;
-        split_pair<KIND>(x.x * scale, x.y * scale, &hi.x, &lo.x);
-        split_pair<KIND>(x.z * scale, x.w * scale, &hi.y, &lo.y);
-        split_pair<KIND>(y.x * scale, y.y * scale, &hi.z, &lo.z);
-        split_pair<KIND>(y.z * scale, y.w * scale, &hi.w, &lo.w);
+        split_pair<KIND>(x[n][0] * scale, x[n][1] * scale, &hi.x, &lo.x);
+        split_pair<KIND>(x[n][2] * scale, x[n][3] * scale, &hi.y, &lo.y);
+        split_pair<KIND>(x[n][4] * scale, x[n][5] * scale, &hi.z, &lo.z);
+        split_pair<KIND>(x[n][6] * scale, x[n][7] * scale, &hi.w, &lo.w);
         unsigned char* at = hi_rows + row * C::PITCHV + 16 * piece;
         *reinterpret_cast<uint4*>(at) = hi;
         *reinterpret_cast<uint4*>(at + C::S_HALF) = lo;
     }
-    for (int i = threadIdx.x; i < C::KP; i += THREADS) z[i] = i < DK ? S[DK * DV + i] : 0.0f;
+    return scale;
 }
 // A fragment of 16 features (rows m0 ..) x 16 channels (k0 ..) of those rows; and of its transpose: 16 channels (m0 ..) x 16
 // features (k0 ..).
@@ -253,6 +337,7 @@ backward_state_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* 
     float2* sums = reinterpret_cast<float2*>(z + C::KP);        // [WQ][TILE]: den and f . t of a warp's features
     float2* wc = sums + C::WQ * TILE;                           // [TILE]: w and c
     float4* kept = reinterpret_cast<float4*>(wc + TILE);        // t, as the threads hold it: [WQ][TILE / 8][lane]
+    float* mu = reinterpret_cast<float*>(kept + C::WQ * TILE * 4);  // [VP]
     __shared__ float scratch[33];
     const int slab = blockIdx.y, chunk = blockIdx.x, warp = threadIdx.x / 32, lane = threadIdx.x & 31, m0 = warp * 16;
     const int tiles = (N + TILE - 1) / TILE;
@@ -277,17 +362,13 @@ backward_state_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* 
     };
     if (t_begin < t_end) fetch(t_begin);
 
-    float unscale_t = 1.0f, scale_w[2] = {1.0f, 1.0f};  // of the thread's two features
+    float scale_s = 1.0f, unscale_t = 1.0f, scale_w[2] = {1.0f, 1.0f};  // of the thread's two features
     if (GRAD) {
         const float* S = state + static_cast<size_t>(slab) * grad_state_floats(DK, DV);
-        float scale_s = 1.0f;
+        // fp16: R and w f by powers of two that keep head and tail inside the format.
+        scale_s = load_state<KIND, DK, DV, THREADS, true>(S, sc.eps, sc.scaled != 0, s_rows, z, mu, scratch);
+        unscale_t = 1.0f / scale_s;
         if (sc.scaled) {
-            // fp16: S and w f by powers of two that keep head and tail inside the format.
-            float big = 0.0f;
-            for (int i = threadIdx.x; i < DK * DV; i += THREADS) big = fmaxf(big, fabsf(S[i]));
-            big = block_max(big, scratch, C::WQ);
-            scale_s = pow2_scale(big, 12);
-            unscale_t = 1.0f / scale_s;
             if (sc.eps >= 0.0f && kind_phi(KIND) == kPhiIdentity) {
                 float z_max = 0.0f, z_inv = 0.0f;
                 for (int i = threadIdx.x; i < DK; i += THREADS) {
@@ -306,7 +387,6 @@ backward_state_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* 
                 }
             }
         }
-        load_state<KIND, DK, DV, THREADS>(S, s_rows, z, scale_s);
     }
     float acc[C::VP / 8][4];
 #pragma unroll
@@ -388,6 +468,13 @@ backward_state_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* 
                     }
                     const bool in = t * TILE + i < N;
                     const float w = in ? 1.0f / (den + sc.eps) : 0.0f;
+                    if (w * sc.eps >= kEpsCounts) {
+                        float mg = 0.0f;
+#pragma unroll 1
+                        for (int j = 0; j < DV / 8; ++j)
+                            mg = mean_dot<KIND>(*reinterpret_cast<const uint4*>(tg + i * C::PITCHV + 16 * j), mu + 8 * j, mg);
+                        ft = fmaf(-sc.eps * scale_s, mg, ft);
+                    }
                     wc[i] = make_float2(w, in ? ft * w : 0.0f);  // c scaled as S is
                 }
                 __syncthreads();
@@ -458,6 +545,7 @@ backward_state_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* 
 #pragma unroll
         for (int n = 0; n < C::VP / 8; ++n) {
             const int col = n * 8 + 2 * (lane & 3);
+            if (GRAD && sc.eps >= 0.0f) dz[r] = fmaf(-unscale_w, fmaf(acc[n][2 * r], mu[col], acc[n][2 * r + 1] * mu[col + 1]), dz[r]);
             if (row < DK && col < DV)
                 *reinterpret_cast<float2*>(out + row * DV + col) = make_float2(acc[n][2 * r] * unscale_w, acc[n][2 * r + 1] * unscale_w);
         }
@@ -549,14 +637,7 @@ backward_kv_kernel(const __nv_bfloat16* __restrict__ k, const __nv_bfloat16* __r
     if (t_begin < t_end) fetch(t_begin);
 
     const float* S = grad_state + static_cast<size_t>(slab) * grad_state_floats(DK, DV);
-    float scale = 1.0f;
-    if (sc.scaled) {
-        float big = 0.0f;
-        for (int i = threadIdx.x; i < DK * DV; i += THREADS) big = fmaxf(big, fabsf(S[i]));
-        scale = pow2_scale(block_max(big, scratch, C::WKV), 12);
-    }
-    const float unscale = 1.0f / scale;
-    load_state<KIND, DK, DV, THREADS>(S, s_rows, z, scale);
+    const float unscale = 1.0f / load_state<KIND, DK, DV, THREADS, false>(S, -1.0f, sc.scaled != 0, s_rows, z, nullptr, scratch);
 
     for (int t = t_begin; t < t_end; ++t) {
         cp_async_wait_all();

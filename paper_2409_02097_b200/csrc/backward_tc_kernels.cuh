@@ -28,6 +28,8 @@
 // MMAs take about 800 or 1000 clocks, the threads' arithmetic about 900 issue slots of each scheduler.
 #pragma once
 
+#include <type_traits>
+
 #include "backward_kernels.cuh"
 #include "common.cuh"
 #include "packed_math.cuh"
@@ -47,7 +49,7 @@ struct BackwardTc {
     static constexpr int T_BUFFERS = 4, SEGMENT_TILES = 32;
     static constexpr int TMEM_COLS = 512;                    // T: 4 x 64, D: 2 x 64, dz: 2 x 64 (kv: 4 x 128)
     static constexpr int LEAD = 2;                           // tiles by which the first product runs ahead of the second
-    static constexpr int STATE_SMEM = STATE_STAGES * STAGE_BYTES + STATE_F * F_BYTES + S_BYTES + 1024 /*align*/ + 1024 /*z, scales, barriers*/;
+    static constexpr int STATE_SMEM = STATE_STAGES * STAGE_BYTES + STATE_F * F_BYTES + S_BYTES + 1024 /*align*/ + 2048 /*z, scales, mu, barriers*/;
     static constexpr int KV_SMEM = KV_STAGES * STAGE_BYTES + KV_F * F_BYTES + S_BYTES + 1024 /*align*/ + 1024 /*z, barriers*/;
     static constexpr int PARTIAL_FLOATS = 128 * 64 + 8 * 64; // D (head rows, tail rows), then dz of each consumer warp
 };
@@ -80,6 +82,10 @@ __device__ __forceinline__ uint4 lds16(uint32_t a)
 __device__ __forceinline__ void sts16(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w)
 {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ void sts8(uint32_t a, uint32_t x, uint32_t y)
+{
+    asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(a), "r"(x), "r"(y) : "memory");
 }
 // Byte offset of 16-byte piece j of row r in a tile of 128-byte rows with the 128-byte swizzle.
 __device__ __forceinline__ uint32_t swizzled(int r, int j) { return r * 128 + ((j ^ (r & 7)) << 4); }
@@ -128,6 +134,17 @@ __device__ __forceinline__ void phi_row(uint32_t tile, int r, int first, float (
 template <int KIND>
 __device__ __forceinline__ float slope_of(float f) { return kind_phi(KIND) == kPhiIdentity ? 1.0f : min_nan(f, 1.0f); }
 
+// mu . g of a token's row in ATOMS tiles of dY.  A call: in the loop over tiles, which hardly ever takes it, its registers made the
+// compiler spill the row of phi (1046 against 999 us at 40 slabs x 131072 x 64).
+template <int KIND, int ATOMS>
+__device__ __noinline__ float row_mean_dot(uint32_t tile, int r, const float* mu)
+{
+    float sum = 0.0f;
+#pragma unroll 1
+    for (int j = 0; j < 8 * ATOMS; ++j) sum = mean_dot<KIND>(lds16(tile + (j / 8) * kTcTileBytes + swizzled(r, j & 7)), mu + 8 * j, sum);
+    return sum;
+}
+
 // Largest of three values over the consumers; `scratch`: three floats of shared memory for each warp.
 template <int WARPS>
 __device__ __forceinline__ float3 consumer_max(float3 v, float* scratch, int warp, int lane)
@@ -149,42 +166,79 @@ __device__ __forceinline__ float3 consumer_max(float3 v, float* scratch, int war
     return v;
 }
 
-// The consumers lay S (dS) of a slab out as 64 K-major rows of 64 channels, head and tail, and z (dz) as 64 floats; zeros
-// where the widths end.  Returns with the scales of fp16 operands: of S, and in scale_w (NULL: not wanted) those of the features' w f.
-template <int KIND, int WARPS>
-__device__ __forceinline__ void tc_load_state(const float* S, int dk, int dv, uint32_t operand, float* z, float* scratch, int tid,
-                                              float eps, float* scale_s, float* scale_w)
+// The consumers lay S (dS) of a slab out as KROWS K-major rows (features) of VW channels in atoms of 64, head, then tail, and z (dz) as
+// KROWS floats; zeros where the widths end.  CENTRED: R = S - z mu^T in place of S where eps is not negative, with mu as VW floats; its
+// sums pass through the operand's place.  Returns with the scales of fp16 operands: of S (R), and, CENTRED, of each feature's
+// w f in scale_w.  A thread has four columns of every ROWS-th row, in registers from one read of S to the operand.
+template <int KIND, int WARPS, int KROWS, int VW, bool CENTRED>
+__device__ __forceinline__ void tc_load_state(const float* S, int dk, int dv, unsigned char* operand, float* z, float* mu, float* scale_w,
+                                              float* scratch, int tid, float eps, float* scale_s)
 {
-    constexpr int EACH = 4096 / (32 * WARPS), PER_ROW = 64 / EACH;  // floats of a thread, threads of a row
-    const int warp = tid / 32, lane = tid & 31, row = tid / PER_ROW, col0 = (tid % PER_ROW) * EACH;
-    float x[EACH];
+    constexpr int PER_ROW = VW / 4, ROWS = 32 * WARPS / PER_ROW, STEPS = KROWS / ROWS, HALF = VW / 64 * KROWS * 128;
+    static_assert(KROWS <= 32 * WARPS && ROWS * (VW + 1) * 4 <= 2 * HALF, "one thread for each feature; the sums of mu take the operand's place");
+    const int warp = tid / 32, lane = tid & 31, slice = tid / PER_ROW, col = 4 * (tid % PER_ROW);
+    float x[STEPS][4];
 #pragma unroll
-    for (int i = 0; i < EACH; i += 2) {
-        float2 v = make_float2(0.0f, 0.0f);
-        if (row < dk && col0 + i < dv) v = *reinterpret_cast<const float2*>(S + row * dv + col0 + i);
-        x[i] = v.x;
-        x[i + 1] = v.y;
+    for (int n = 0; n < STEPS; ++n) {
+        const int row = n * ROWS + slice;
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (row < dk && col < dv) v = *reinterpret_cast<const float4*>(S + row * dv + col);
+        x[n][0] = v.x, x[n][1] = v.y, x[n][2] = v.z, x[n][3] = v.w;
     }
     const float zv = tid < dk ? S[dk * dv + tid] : 0.0f;
-    if (tid < 64) z[tid] = zv;
+    if (tid < KROWS) z[tid] = zv;
+    if (CENTRED && eps >= 0.0f) {
+        float* sums = reinterpret_cast<float*>(operand);  // [ROWS][VW], then [ROWS] of z . z
+        consumer_sync<WARPS>();
+        float s[4] = {}, zz = 0.0f;
+#pragma unroll
+        for (int n = 0; n < STEPS; ++n) {
+            const float zr = z[n * ROWS + slice];
+            zz = fmaf(zr, zr, zz);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] = fmaf(zr, x[n][i], s[i]);
+        }
+        *reinterpret_cast<float4*>(sums + slice * VW + col) = make_float4(s[0], s[1], s[2], s[3]);
+        if (col == 0) sums[ROWS * VW + slice] = zz;
+        consumer_sync<WARPS>();
+        if (tid < VW) {
+            float sum = 0.0f, squares = 0.0f;
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) {
+                sum += sums[i * VW + tid];
+                squares += sums[ROWS * VW + i];
+            }
+            mu[tid] = mean_of(sum, squares);
+        }
+        consumer_sync<WARPS>();
+#pragma unroll
+        for (int n = 0; n < STEPS; ++n) {
+            const float zr = -z[n * ROWS + slice];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[n][i] = fmaf(zr, mu[col + i], x[n][i]);
+        }
+    }
     *scale_s = 1.0f;
     if (kind_dtype(KIND) == kDtypeFp16) {
         float big = 0.0f;
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) big = fmaxf(big, fabsf(x[i]));
+        for (int n = 0; n < STEPS; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) big = fmaxf(big, fabsf(x[n][i]));
         const float3 m = consumer_max<WARPS>(make_float3(big, zv, tid >= dk ? 0.0f : zv > 0.0f ? 1.0f / zv : 3.0e38f), scratch, warp, lane);
         *scale_s = pow2_scale(m.x, 12);
-        if (scale_w != nullptr && tid < 64)
+        if (CENTRED && tid < KROWS)
             scale_w[tid] = eps < 0.0f ? 1.0f : kind_phi(KIND) == kPhiIdentity ? slab_scale(m.y, m.z, eps) : feature_scale(zv, eps);
     }
+    const uint32_t to = smem_u32(operand) + (col / 64) * (KROWS * 128) + (col & 4) * 2;
 #pragma unroll
-    for (int h = 0; h < EACH / 8; ++h) {
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) split_pair<KIND>(x[8 * h + 2 * i] * *scale_s, x[8 * h + 2 * i + 1] * *scale_s, &hi[i], &lo[i]);
-        const uint32_t at = operand + swizzled(row, col0 / 8 + h);
-        sts16(at, hi[0], hi[1], hi[2], hi[3]);
-        sts16(at + 64 * 128, lo[0], lo[1], lo[2], lo[3]);
+    for (int n = 0; n < STEPS; ++n) {
+        uint32_t hi[2], lo[2];
+        split_pair<KIND>(x[n][0] * *scale_s, x[n][1] * *scale_s, &hi[0], &lo[0]);
+        split_pair<KIND>(x[n][2] * *scale_s, x[n][3] * *scale_s, &hi[1], &lo[1]);
+        const uint32_t at = to + swizzled(n * ROWS + slice, (col & 63) / 8);
+        sts8(at, hi[0], hi[1]);
+        sts8(at + HALF, lo[0], lo[1]);
     }
 }
 
@@ -276,7 +330,8 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
     unsigned char* So = F + C::STATE_F * C::F_BYTES;
     float* z = reinterpret_cast<float*>(So + C::S_BYTES);
     float* scale_w = z + 64;  // [64] fp16: of each feature's w f
-    float* scratch = scale_w + 64;
+    float* mu = scale_w + 64; // [64]
+    float* scratch = mu + 64;
     uint64_t* full = reinterpret_cast<uint64_t*>(scratch + 32);
     uint64_t* empty = full + C::STATE_STAGES;
     uint64_t* t_full = empty + C::STATE_STAGES;      // [T_BUFFERS]
@@ -401,9 +456,9 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
             float scale_s = 1.0f;
             float* partial = partials + (static_cast<size_t>(blockIdx.x) * spans + span) * C::PARTIAL_FLOATS;
             if (GRAD) {
+                const float* S = state + static_cast<size_t>(slab) * grad_state_floats(dk, dv);
                 consumer_sync<C::STATE_WARPS>();  // everybody is through with the slab before
-                tc_load_state<KIND, C::STATE_WARPS>(state + static_cast<size_t>(slab) * grad_state_floats(dk, dv), dk, dv, smem_u32(So), z, scratch, tid,
-                                    sc.eps, &scale_s, scale_w);
+                tc_load_state<KIND, C::STATE_WARPS, 64, 64, true>(S, dk, dv, So, z, mu, scale_w, scratch, tid, sc.eps, &scale_s);
                 fence_proxy_async_smem();
                 consumer_sync<C::STATE_WARPS>();  // z is there
                 if (lane == 0) mbar_arrive(s_ready);
@@ -420,13 +475,17 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
             }
             int flushed = 0;  // segments of this unit that have gone to the partial
             const int segs = (b - a + C::SEGMENT_TILES - 1) / C::SEGMENT_TILES;
-            auto flush_until = [&](int want) {  // this warp's 32 lanes x its group's 32 columns
+            // this warp's 32 lanes x its group's 32 columns; behind the unit's last tile also dS mu, whose code in the loop over
+            // tiles made the compiler spill
+            auto flush_until = [&](int want, auto behind) {
+                constexpr bool WITH_MU = GRAD && decltype(behind)::value;
                 for (; flushed < want; ++flushed) {
                     const int sg = seg0 + flushed;
                     wait(&d_done[sg & 1], (sg >> 1) & 1);
                     if (ok) {
                         tc_fence_after_sync();
-                        float* to = partial + ((warp & 3) * 32 + lane) * 64 + group * 32;
+                        float* to = partial + r * 64 + group * 32;
+                        float with_mu = 0.0f;  // the row's columns times mu
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             uint32_t d[16];
@@ -441,8 +500,14 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                                     v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
                                 }
                                 *at = v;
+                                if (WITH_MU) {
+                                    const float4 m = *reinterpret_cast<const float4*>(mu + group * 32 + h * 16 + 4 * i);
+                                    with_mu = fmaf(v.x, m.x, fmaf(v.y, m.y, fmaf(v.z, m.z, fmaf(v.w, m.w, with_mu))));
+                                }
                             }
                         }
+                        // F's place is free: the last product that read it is complete
+                        if (WITH_MU && flushed + 1 == segs) reinterpret_cast<float*>(F)[group * 128 + r] = with_mu;
                         tc_fence_before_sync();
                     }
                     __syncwarp();
@@ -451,7 +516,7 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
             };
             for (int it = a; it < b; ++it) {
                 if ((it & 1) != group) continue;
-                flush_until((it - a) / C::SEGMENT_TILES);
+                flush_until((it - a) / C::SEGMENT_TILES, std::false_type());
                 const int s = it % C::STATE_STAGES;
                 unsigned char* stage = smem + s * C::STAGE_BYTES;
                 const uint32_t q_at = smem_u32(stage);
@@ -480,6 +545,10 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                             }
                             w = in ? 1.0f / (sum2(den) + sc.eps) : 0.0f;
                             c = in ? sum2(ft) * w : 0.0f;  // scaled as S is
+                            if (__any_sync(0xffffffffu, w * sc.eps >= kEpsCounts)) {
+                                const float mg = row_mean_dot<KIND, 1>(q_at + kTcTileBytes, r, mu);
+                                c = fmaf(-sc.eps * scale_s * w, mg, c);
+                            }
                         }
                     }
                 }
@@ -546,8 +615,9 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                     if (GRAD) mbar_arrive(&written[s]);
                 }
             }
-            flush_until(segs);
+            flush_until(segs, std::true_type());
             seg0 += segs;
+            if (GRAD) consumer_sync<C::STATE_WARPS>();  // dS mu of all rows is there
             // dz of the thread's tokens -> sums over the warp: 64 values are halved with the lanes, two are left in each
             if (ok) {
                 float v[64];
@@ -568,6 +638,11 @@ backward_tc_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const __gri
                     }
                 }
                 // o = 16 kept values 32 * (lane bit 4) .., o = 8 then 16 * (bit 3) .., down to 2 * (bit 0)
+                if (GRAD && sc.eps >= 0.0f && warp == 0) {  // dz lacks -dS mu so far: heads and tails, either half of the columns
+                    const float2* m = reinterpret_cast<const float2*>(F) + lane;
+                    v[0] -= (m[0].x + m[32].x) + (m[64].x + m[96].x);
+                    v[1] -= (m[0].y + m[32].y) + (m[64].y + m[96].y);
+                }
                 *reinterpret_cast<float2*>(partial + 128 * 64 + warp * 64 + 2 * lane) = make_float2(v[0], v[1]);
             }
             ++span;
@@ -754,8 +829,8 @@ backward_tc_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
             const int slab = run.slab(a), b = run.unit_end(a);
             float scale_s;
             consumer_sync<C::KV_WARPS>();
-            tc_load_state<KIND, C::KV_WARPS>(grad_state + static_cast<size_t>(slab) * grad_state_floats(dk, dv), dk, dv, smem_u32(So), z, scratch, tid,
-                                -1.0f, &scale_s, nullptr);
+            tc_load_state<KIND, C::KV_WARPS, 64, 64, false>(grad_state + static_cast<size_t>(slab) * grad_state_floats(dk, dv), dk, dv, So, z,
+                                                            nullptr, nullptr, scratch, tid, -1.0f, &scale_s);
             fence_proxy_async_smem();
             consumer_sync<C::KV_WARPS>();
             if (lane == 0) mbar_arrive(s_ready);

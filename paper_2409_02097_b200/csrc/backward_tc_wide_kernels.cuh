@@ -26,49 +26,10 @@ struct BackwardTcWide {
     static constexpr int FLO_BYTES = 2 * kTcTileBytes, S_HALF = VA * kTcTileBytes, S_BYTES = 2 * S_HALF;
     static constexpr int VW = 64 * VA, SEGMENT_TILES = 32;
     static constexpr int T_COL = 0, D_COL = 128, DZ_COL = 384;      // state: T, two D of VW columns, dz of each atom
-    static constexpr int SMEM = STAGES * STAGE_BYTES + FLO_BYTES + S_BYTES + 1024 /*align*/ + 2048 /*z, scales, barriers*/;
+    static constexpr int SMEM = STAGES * STAGE_BYTES + FLO_BYTES + S_BYTES + 1024 /*align*/ + 2048 /*z, scales, mu, barriers*/;
     static constexpr int PARTIAL_FLOATS = 2 * 128 * VW + WARPS * 64;
 };
 static_assert(BackwardTcWide<2>::SMEM <= 227 * 1024 && BackwardTcWide<1>::SMEM <= 227 * 1024, "shared memory");
-
-// S (dS) as 128 K-major rows (features) of VA atoms, head, then tail; z (dz) as 128 floats.
-template <int KIND, int VA>
-__device__ __forceinline__ void wide_load_state(const float* S, int dk, int dv, uint32_t operand, float* z, float* scratch, int tid,
-                                                float eps, float* scale_s, float* scale_w)
-{
-    using C = BackwardTcWide<VA>;
-    const int warp = tid / 32, lane = tid & 31, row = tid / 2, col0 = (tid & 1) * (C::VW / 2);
-    const float zv = tid < dk ? S[dk * dv + tid] : 0.0f;
-    if (tid < 128) z[tid] = zv;
-    *scale_s = 1.0f;
-    if (kind_dtype(KIND) == kDtypeFp16) {
-        float big = 0.0f;
-        if (row < dk)
-            for (int i = 0; i < C::VW / 2; i += 2)
-                if (col0 + i < dv) {
-                    const float2 v = *reinterpret_cast<const float2*>(S + row * dv + col0 + i);
-                    big = fmaxf(big, fmaxf(fabsf(v.x), fabsf(v.y)));
-                }
-        const float3 m = consumer_max<C::WARPS>(make_float3(big, zv, tid >= dk ? 0.0f : zv > 0.0f ? 1.0f / zv : 3.0e38f), scratch, warp, lane);
-        *scale_s = pow2_scale(m.x, 12);
-        if (scale_w != nullptr && tid < 128)
-            scale_w[tid] = eps < 0.0f ? 1.0f : kind_phi(KIND) == kPhiIdentity ? slab_scale(m.y, m.z, eps) : feature_scale(zv, eps);
-    }
-#pragma unroll
-    for (int j = 0; j < C::VW / 16; ++j) {
-        const int col = col0 + 8 * j;
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float2 v = make_float2(0.0f, 0.0f);
-            if (row < dk && col + 2 * i < dv) v = *reinterpret_cast<const float2*>(S + row * dv + col + 2 * i);
-            split_pair<KIND>(v.x * *scale_s, v.y * *scale_s, &hi[i], &lo[i]);
-        }
-        const uint32_t at = operand + (col / 64) * kTcTileBytes + swizzled(row, (col & 63) / 8);
-        sts16(at, hi[0], hi[1], hi[2], hi[3]);
-        sts16(at + C::S_HALF, lo[0], lo[1], lo[2], lo[3]);
-    }
-}
 
 // The producer and the storing warp: like tc_produce / tc_store with the tensors' atoms one by one.
 template <int VA>
@@ -133,7 +94,8 @@ backward_tc_wide_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const 
     unsigned char* So = Flo + C::FLO_BYTES;
     float* z = reinterpret_cast<float*>(So + C::S_BYTES);
     float* scale_w = z + 128;  // [128] fp16: of each feature's w f
-    float* scratch = scale_w + 128;
+    float* mu = scale_w + 128; // [VW]
+    float* scratch = mu + 128;
     uint64_t* full = reinterpret_cast<uint64_t*>(scratch + 32);
     uint64_t* empty = full + C::STAGES;
     uint64_t* written = empty + C::STAGES;
@@ -266,9 +228,9 @@ backward_tc_wide_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const 
             float scale_s = 1.0f;
             float* partial = partials + (static_cast<size_t>(blockIdx.x) * spans + span) * C::PARTIAL_FLOATS;
             if (GRAD) {
+                const float* S = state + static_cast<size_t>(slab) * grad_state_floats(dk, dv);
                 consumer_sync<C::WARPS>();
-                wide_load_state<KIND, VA>(state + static_cast<size_t>(slab) * grad_state_floats(dk, dv), dk, dv, smem_u32(So), z, scratch,
-                                          tid, sc.eps, &scale_s, scale_w);
+                tc_load_state<KIND, C::WARPS, 128, C::VW, true>(S, dk, dv, So, z, mu, scale_w, scratch, tid, sc.eps, &scale_s);
                 fence_proxy_async_smem();
                 consumer_sync<C::WARPS>();
                 if (lane == 0) mbar_arrive(s_ready);
@@ -285,12 +247,14 @@ backward_tc_wide_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const 
             }
             int flushed = 0;
             const int segs = (last - first + C::SEGMENT_TILES - 1) / C::SEGMENT_TILES;
-            auto flush_until = [&](int want) {  // this warp's 32 rows of its atom's accumulator
+            auto flush_until = [&](int want, auto behind) {  // this warp's 32 rows of its atom's accumulator
+                constexpr bool WITH_MU = GRAD && decltype(behind)::value;
                 for (; flushed < want; ++flushed) {
                     wait(d_done, (seg0 + flushed) & 1);
                     if (ok) {
                         tc_fence_after_sync();
                         float* to = partial + (a * 128 + r) * C::VW;
+                        float with_mu = 0.0f;  // the row times mu
 #pragma unroll
                         for (int h = 0; h < C::VW / 16; ++h) {
                             uint32_t x[16];
@@ -305,8 +269,14 @@ backward_tc_wide_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const 
                                     v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
                                 }
                                 at[i] = v;
+                                if (WITH_MU) {
+                                    const float4 m = *reinterpret_cast<const float4*>(mu + 16 * h + 4 * i);
+                                    with_mu = fmaf(v.x, m.x, fmaf(v.y, m.y, fmaf(v.z, m.z, fmaf(v.w, m.w, with_mu))));
+                                }
                             }
                         }
+                        // the tail's place is free: the last product that read it is complete
+                        if (WITH_MU && flushed + 1 == segs) reinterpret_cast<float*>(Flo)[a * 128 + r] = with_mu;
                         tc_fence_before_sync();
                     }
                     __syncwarp();
@@ -322,7 +292,7 @@ backward_tc_wide_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const 
                 float w = in ? 1.0f : 0.0f, c = 0.0f;
                 if (ok) phi_row<KIND, 8>(q_at, r, 0, f);
                 finish();
-                flush_until((it - first) / C::SEGMENT_TILES);
+                flush_until((it - first) / C::SEGMENT_TILES, std::false_type());
                 if (GRAD) {
                     wait(t_full, it & 1);
                     tc_fence_after_sync();
@@ -353,6 +323,10 @@ backward_tc_wide_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const 
                         const float d0 = a == 0 ? my_den : o.x, d1 = a == 0 ? o.x : my_den, f0 = a == 0 ? my_ft : o.y, f1 = a == 0 ? o.y : my_ft;
                         w = in ? 1.0f / (d0 + d1 + sc.eps) : 0.0f;
                         c = in ? (f0 + f1) * w : 0.0f;  // scaled as S is
+                        if (__any_sync(0xffffffffu, w * sc.eps >= kEpsCounts)) {
+                            const float mg = row_mean_dot<KIND, VA>(smem_u32(smem + s * C::STAGE_BYTES) + 2 * kTcTileBytes, r, mu);
+                            c = fmaf(-sc.eps * scale_s * w, mg, c);
+                        }
                     }
                 }
                 if (ok) {
@@ -397,8 +371,9 @@ backward_tc_wide_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const 
                 pending = it;
             }
             finish();
-            flush_until(segs);
+            flush_until(segs, std::true_type());
             seg0 += segs;
+            if (GRAD) consumer_sync<C::WARPS>();  // dS mu of all rows is there
             if (ok) {  // dz of the thread's tokens -> sums over the warp, as in the narrow kernel
                 float v[64];
 #pragma unroll
@@ -416,6 +391,11 @@ backward_tc_wide_state_kernel(const __grid_constant__ CUtensorMap tmap_q, const 
                         const float keep = hi ? v[i + 2 * o] : v[i], send = hi ? v[i] : v[i + 2 * o];
                         v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
                     }
+                }
+                if (GRAD && sc.eps >= 0.0f && quarter == 0) {  // dz lacks -dS mu so far: heads and tails
+                    const float2* m = reinterpret_cast<const float2*>(Flo) + a * 64 + lane;
+                    v[0] -= m[0].x + m[32].x;
+                    v[1] -= m[0].y + m[32].y;
                 }
                 *reinterpret_cast<float2*>(partial + 2 * 128 * C::VW + warp * 64 + 2 * lane) = make_float2(v[0], v[1]);
             }
@@ -537,8 +517,8 @@ backward_tc_wide_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __g
             const int slab = run.slab(first), last = run.unit_end(first);
             float scale_s;
             consumer_sync<C::WARPS>();
-            wide_load_state<KIND, VA>(grad_state + static_cast<size_t>(slab) * grad_state_floats(dk, dv), dk, dv, smem_u32(So), z, scratch,
-                                      tid, -1.0f, &scale_s, nullptr);
+            tc_load_state<KIND, C::WARPS, 128, C::VW, false>(grad_state + static_cast<size_t>(slab) * grad_state_floats(dk, dv), dk, dv, So, z,
+                                                             nullptr, nullptr, scratch, tid, -1.0f, &scale_s);
             fence_proxy_async_smem();
             consumer_sync<C::WARPS>();
             if (lane == 0) mbar_arrive(s_ready);

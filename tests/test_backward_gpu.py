@@ -508,3 +508,60 @@ def test_a_nan_goes_where_the_formulas_take_it(case, dtype, normalize):
             assert torch.equal(torch.isnan(x[0, 0]), torch.isnan(y)), f"{'qkvg'[which]} {name}"
             assert torch.equal(x[:, 1:], x0[:, 1:])
     op.close()
+
+
+# Means some hundred times the spread over sqrt(N): before its rounding dQ would be off by 2^-18 sqrt(N) mean (bf16), more than
+# the rounding, were the mean carried through the products.
+MEAN_CASES = [((1, 2, 65600, 64, 64), 8.0), ((2, 20, 9000, 64, 64), 20.0), ((1, 2, 65600, 128, 128), 8.0), ((1, 3, 33000, 80, 80), 8.0),
+              ((1, 3, 33000, 128, 64), 8.0), ((2, 7, 16100, 80, 40), 16.0), ((1, 2, 5000, 160, 160), 24.0), ((1, 2, 20000, 32, 32), 12.0),
+              ((1, 2, 1000, 40, 40), 60.0)]
+
+
+@pytest.mark.parametrize("saved", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("case,mean", MEAN_CASES, ids=lambda c: "x".join(map(str, c)) if isinstance(c, tuple) else f"mean{c:g}")
+def test_the_mean_of_the_values_costs_no_bits_of_dq(case, mean, dtype, saved):
+    B, H, N, dk, dv = case
+    # (spread / mean) of the values as they are stored: a step of bf16 at the mean is some of the spread, the reference reads the same
+    tensors = _inputs(B, H, N, dk, dv, dtype, mean=mean, grad_scale=1024.0 if dtype == "fp16" else 1.0)
+    op = attn.LinFusionAttention(B, H, N, dv, eps=EPS, variant="split", dtype=dtype, d_qk=dk if dk != dv else 0)
+    state = None
+    if saved:  # what an exact forward pass would leave
+        f, v = ref.phi(tensors[1].double()), tensors[2].double()
+        state = torch.cat([(f.transpose(-1, -2) @ v).flatten(-2), f.sum(-2)], -1).float().view(B * H, -1).contiguous()
+    dq = op.backward(*tensors, state=state)[0]
+    want = ref.attention_backward(*tensors, EPS)[0][0]
+    rel = ((dq.double() - want).norm() / want.norm()).item()
+    # What S itself is off by, t - c z takes 0.85 sqrt(N) mean times as large.  fp32: 2^-25, uniformly.  A recomputed state is
+    # summed by the tensor core, which truncates the running sum after each of n <= 32 * 8 steps of 16 tokens: off by 0 to 2^-23 of it,
+    # that is by a common part, a multiple of z, which leaves with the mean, and a part of 2^-23 / sqrt 12 in the mean square;
+    # over n steps of a sum that grows evenly, 2^-23 sqrt(n / 36).
+    grown = 0.85 * math.sqrt(N) * mean
+    extra = grown * (2 * 2.0 ** -25 / math.sqrt(3) + (0.0 if saved else 2.0 ** -23 * math.sqrt(256 / 36)))
+    assert rel <= _rms_limit(dtype) + extra, f"{rel:.3e}"
+    op.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("case", [(1, 2, 300, 64, 64), (2, 4, 4200, 64, 64), (1, 5, 4001, 128, 128), (1, 5, 8100, 128, 64), (1, 2, 70, 160, 160)],
+                         ids=lambda c: "x".join(map(str, c)))
+def test_an_eps_that_counts_and_values_with_a_mean(case, dtype):
+    # eps from far below den to far above it, tokens of small den among others: the mean does not cancel there
+    B, H, N, dk, dv = case
+    tensors = _inputs(B, H, N, dk, dv, dtype, mean=3.0, grad_scale=16.0)
+    tensors[0][:, :, ::7] = -12.0
+    tensors[0][:, :, 1::7, 3:] = -20.0
+    for eps in (1e-3, 1.0, 2e4):
+        op = attn.LinFusionAttention(B, H, N, dv, eps=eps, variant="split", dtype=dtype, d_qk=dk if dk != dv else 0)
+        _check(op.backward(*tensors), tensors, dtype, f"{case} {dtype} eps {eps}", eps=eps, rms=False)
+        whole, grad_state = op.backward_q(tensors[0], tensors[3], op.backward_state(*tensors[1:3]))
+        f = ref.phi(tensors[0].double())
+        S = ref.phi(tensors[1].double()).transpose(-1, -2) @ tensors[2].double()
+        z = ref.phi(tensors[1].double()).sum(-2)
+        w = 1 / (f @ z.unsqueeze(-1) + eps)
+        t = tensors[3].double() @ S.transpose(-1, -2)
+        dz = -(w * f * (w * (f * t).sum(-1, keepdim=True))).sum(-2)
+        sizes = (w * f * (w * (f * (tensors[3].double().abs() @ S.abs().transpose(-1, -2))).sum(-1, keepdim=True))).sum(-2)
+        err = (grad_state[:, dk * dv:].view(B, H, dk).double() - dz).abs()
+        assert (err <= SLACK * sizes).all(), f"dz {case} eps {eps}: {(err / sizes).max().item():.3e}"
+        op.close()
