@@ -50,7 +50,7 @@ typedef struct {
     int32_t pairs[LINFUSION_ROPE_MAX_AXES];  /* pairs of each axis, >= 0; 2 <= 2 * sum <= d   */
     int32_t interleaved;                     /* pairs (2p, 2p + 1) (1) or (p, p + P) (0)      */
     int32_t backward;                        /* rotate by the negative angle                  */
-    double theta;                            /* finite, > 0                                   */
+    double theta;                            /* finite, > 0; below 1 frequencies pass 1       */
     uint32_t flags;                          /* 0 or LINFUSION_DTYPE_FP16                     */
 } linfusion_rope_desc_t;
 
@@ -70,8 +70,10 @@ typedef struct {
  * coordinates of token n of batch b at positions + b * pos_batch_stride + n * n_axes;
  * pos_batch_stride 0 shares them over the batch.  Coordinates need not be whole (interpolated
  * positions).  The angle is formed from a frequency held in two fp32 parts and reduced to one turn
- * before the sine and cosine, so it is good to about 3e-7 for coordinates below 2^24 in size.
- * Errors: INVALID_ARG (null / misaligned pointers, bad sizes or strides, both tensors absent),
+ * before the sine and cosine, so it is good to about 3e-7 for angles below 2^24 radians (coordinates below 2^24 where
+ * theta >= 1), and to 2^-46 of the angle beyond.
+ * Errors: INVALID_ARG (null / misaligned pointers, bad sizes or strides, both tensors absent, a theta so small that a
+ * frequency passes 1e30),
  * UNSUPPORTED (unknown flags, d > 256), CUDA.
  */
 linfusion_status_t linfusion_rope(const linfusion_rope_desc_t* desc, const linfusion_rope_tensor_t* q,

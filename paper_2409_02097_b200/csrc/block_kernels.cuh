@@ -50,7 +50,8 @@ __device__ __forceinline__ void store16(void* p, const uint4& v)
 // The angle of a far position loses its fraction of a turn in fp32 (position 10^4 x frequency 1: 10^-3
 // radians).  The frequency is therefore held in turns per position as hi + lo floats (48 bits); with
 // p = pos * hi rounded and e = fma(pos, hi, -p) its exact error, p - rint(p) is exact, and
-// r = (p - rint(p)) + (e + pos * lo) is the fraction of a turn to 2^-25.
+// r = (p - rint(p)) + (e + pos * lo) is the fraction of a turn to 2^-25 for angles below 2^24 radians; beyond, to 2^-48 or so of
+// the turns (the 48 bits, and the last sum, whose second term then passes a turn).
 // ---------------------------------------------------------------------------------------------
 constexpr int kRopeMaxPairs = 128;
 constexpr int kRopeThreads = 256;

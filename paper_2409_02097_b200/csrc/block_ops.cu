@@ -91,6 +91,9 @@ linfusion_status_t check_rope(const linfusion_rope_desc_t* d, int* pairs)
         sum += d->pairs[a];
     }
     if (sum < 1 || 2 * sum > d->d) return LINFUSION_ERR_INVALID_ARG;
+    // theta^(-j / n) of the last pair of an axis is its largest where theta is below 1
+    for (int a = 0; a < d->n_axes; ++a)
+        if (d->pairs[a] > 0 && !(std::pow(d->theta, -static_cast<double>(d->pairs[a] - 1) / d->pairs[a]) <= 1e30)) return LINFUSION_ERR_INVALID_ARG;
     *pairs = static_cast<int>(sum);
     return LINFUSION_OK;
 }

@@ -545,3 +545,24 @@ def test_strides_of_axes_of_one_do_not_matter():
     pos = torch.arange(33, device="cuda").float().unsqueeze(1)
     q = x.as_strided((1, 33, 1, 64), (5, 64, 7, 1))
     assert torch.equal(rope.forward(q, None, pos)[0], rope.forward(x.view(1, 33, 1, 64), None, pos)[0])
+
+
+@pytest.mark.parametrize("interleaved,pairs", [(True, (16, 16)), (False, (16, 16)), (False, (9, 6))])
+@pytest.mark.parametrize("theta", [1.0, 0.25, 1e-2, 1e-4, 1e-7])
+def test_rope_theta_below_one(theta, interleaved, pairs):
+    # angles up to 2^24 radians are good to what ROPE_SLACK counts; beyond, to 2^-46 of the angle, and still rotations
+    case = (1, 2, 1, 300, 64, pairs, interleaved, "head_major")
+    q, k, _ = _rope_case(case, torch.float16)
+    op = block.AxialRope(64, pairs, theta=theta, interleaved=interleaved, dtype="fp16")
+    top = max(theta ** (-(n - 1) / n) for n in pairs)  # the largest frequency
+    gen = _gen(8)
+    for reach in (2.0 ** 24, 2.0 ** 24 * top):          # of the angles: within the bound, and coordinates near 2^24 whatever theta is
+        pos = (torch.rand(300, 2, generator=gen, device="cuda") * 2 - 1) * (reach / top)
+        qr, kr = op.forward(q, k, pos)
+        slack = ROPE_SLACK + 2.0 ** -46 * reach if reach > 2.0 ** 24 else ROPE_SLACK
+        if slack < 0.5:
+            _check_rope(qr, q, pos, case, False, f"theta {theta} {reach}", theta=theta, slack=slack)
+            _check_rope(kr, k, pos, case, False, f"theta {theta} {reach}", theta=theta, slack=slack)
+        for got, x in ((qr, q), (kr, k)):
+            rel = (got.double().square().sum(-1) / x.double().square().sum(-1) - 1).abs().max().item()
+            assert rel <= 3 * 2.0 ** -11, f"not a rotation: {rel:.3e}"

@@ -292,3 +292,11 @@ def test_gradients_per_entry_are_known_bits(lib):
     _refused(call(8))
     if not torch.cuda.is_available():
         _without_device(call(7))
+
+
+def test_rope_refuses_a_theta_whose_frequencies_have_no_fp32(lib):
+    for theta, pairs in ((1e-40, (16, 16)), (5e-324, (4, 4)), (1e-300, (2, 0))):
+        _refused(_rope_call(lib, theta=theta, pairs=pairs))
+    if not torch.cuda.is_available():
+        _without_device(_rope_call(lib, theta=1e-300, pairs=(1, 1)))  # one pair an axis: its frequency is 1
+        _without_device(_rope_call(lib, theta=1e-4, pairs=(16, 16)))
