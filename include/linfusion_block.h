@@ -145,8 +145,9 @@ typedef struct {
  * Backward.  y: the stream as the forward pass stored it (x where there is no a; not read without pre).
  * dy: the gradient of y from everything but n (NULL: zero); dn: the gradient of n (with pre).
  * dx = residual_scale * (dy + gradient through Pre) (without a: no residual_scale), and with a the gradient da.  Row statistics are
- * computed again from y and a, so the forward pass keeps nothing.  Outputs may be written over dy and dn
- * (dx over dy, da over a, each with the same strides); they must not overlap inputs otherwise.
+ * computed again from y and a, so the forward pass keeps nothing.  dx may lie exactly over dy and da exactly over a, with the
+ * same strides; otherwise the address range of an output, a gradient of a vector among them, must not meet that of an input or of
+ * another output, nor the workspace any of them.
  * workspace: device memory, 256-byte aligned, of linfusion_block_norm_workspace_bytes(); used until the
  * call's kernels have run, and may then be used by anything else.
  * Two launches (one where no gradient of a vector is wanted).  Errors: as above, ALLOC (workspace too small).

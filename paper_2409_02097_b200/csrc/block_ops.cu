@@ -218,6 +218,35 @@ bool apart(const linfusion_block_norm_desc_t& d, const linfusion_rows_t* out, co
     return true;
 }
 
+// The vectors' gradients and the workspace (where `workspace_bytes` of one is used) share no memory with each other, with a tensor
+// of the call or with a vector.
+bool sums_apart(const linfusion_block_norm_desc_t& d, const linfusion_block_norm_vectors_t& v, const linfusion_block_norm_grads_t& g,
+                std::initializer_list<const linfusion_rows_t*> tensors, const void* workspace, size_t workspace_bytes)
+{
+    const size_t shared = static_cast<size_t>(d.C) * 4, each = shared * d.B;
+    const auto bytes = [&](const linfusion_channels_t& c, uint32_t bit) { return c.batch != 0 || (g.per_entry & bit) != 0u ? each : shared; };
+    const Extent sums[8] = {{reinterpret_cast<const char*>(g.gate), bytes(v.gate, LINFUSION_PER_ENTRY_GATE)},
+                            {reinterpret_cast<const char*>(g.scale), bytes(v.scale, LINFUSION_PER_ENTRY_SCALE)},
+                            {reinterpret_cast<const char*>(g.shift), bytes(v.shift, LINFUSION_PER_ENTRY_SHIFT)},
+                            {reinterpret_cast<const char*>(g.pre_weight), shared},
+                            {reinterpret_cast<const char*>(g.pre_bias), shared},
+                            {reinterpret_cast<const char*>(g.post_weight), shared},
+                            {reinterpret_cast<const char*>(g.post_bias), shared},
+                            {workspace_bytes != 0 ? static_cast<const char*>(workspace) : nullptr, workspace_bytes}};
+    for (int i = 0; i < 8; ++i) {
+        if (sums[i].p == nullptr) continue;
+        for (int j = 0; j < i; ++j)
+            if (sums[j].p != nullptr && meet(sums[i], sums[j])) return false;
+        for (const linfusion_rows_t* t : tensors)
+            if (rows_given(t) && meet(sums[i], rows_extent(d, t))) return false;
+        for (const linfusion_channels_t& c : {v.gate, v.scale, v.shift})
+            if (c.p != nullptr && meet(sums[i], extent(c.p, d.B, c.batch, 1, 0, 1, 0, d.C))) return false;
+        for (const void* p : {v.pre_weight, v.pre_bias, v.post_weight, v.post_bias})
+            if (p != nullptr && meet(sums[i], extent(p, 1, 0, 1, 0, 1, 0, d.C))) return false;
+    }
+    return true;
+}
+
 // How rows are dealt out: groups of `warps` warps, each thread with `vectors` pieces of eight channels, `per_cta` groups in
 // a block, `chunks` groups for each batch entry.
 struct NormPlan {
@@ -494,13 +523,21 @@ linfusion_status_t linfusion_block_norm_backward(const linfusion_block_norm_desc
     if (grads->gate || grads->post_weight) want |= 4;
     if (grads->post_bias || (grads->gate && v->post_bias)) want |= 8;
 
+    if (want != 0 && (workspace == nullptr || !is_aligned(workspace, 256))) return LINFUSION_ERR_INVALID_ARG;
+    // The check of the workspace's range: what the call uses of it on the device, or, before that is known, on a B200.
+    const auto needs = [&](const NormPlan& plan) {
+        return want == 0 ? 0 : align_up_256(static_cast<size_t>(4) * plan.groups * desc->C * sizeof(float));
+    };
+    const auto clear = [&](size_t bytes) {
+        return sums_apart(*desc, *v, *grads, {y_read, a, dy, dn, dx, da}, workspace, std::min(bytes, workspace_bytes));
+    };
+    constexpr int kSms = 148;
+    if (!clear(needs(norm_plan(*desc, kSms, true)))) return LINFUSION_ERR_INVALID_ARG;
     const Here at = here();
     if (at.st != LINFUSION_OK) return at.st;
     const NormPlan plan = norm_plan(*desc, at.sms, true);
-    if (want != 0) {
-        if (workspace == nullptr || !is_aligned(workspace, 256)) return LINFUSION_ERR_INVALID_ARG;
-        if (workspace_bytes < align_up_256(static_cast<size_t>(4) * plan.groups * desc->C * sizeof(float))) return LINFUSION_ERR_ALLOC;
-    }
+    if (want != 0 && workspace_bytes < needs(plan)) return LINFUSION_ERR_ALLOC;
+    if (at.sms != kSms && !clear(needs(plan))) return LINFUSION_ERR_INVALID_ARG;
     NormParams p = {};
     fill(&p, *desc, *v, plan, branch);
     p.x = to_rows(y);

@@ -300,3 +300,23 @@ def test_rope_refuses_a_theta_whose_frequencies_have_no_fp32(lib):
     if not torch.cuda.is_available():
         _without_device(_rope_call(lib, theta=1e-300, pairs=(1, 1)))  # one pair an axis: its frequency is 1
         _without_device(_rope_call(lib, theta=1e-4, pairs=(16, 16)))
+
+
+@pytest.mark.parametrize("name,at", [
+    ("ws", A16 * 5), ("ws", A16 * 8), ("ws", A16 * 20), ("ws", A16 * 9), ("ws", A16 * 3), ("ws", A16 * 7 - 4096),  # over dy, da, a gradient, the gate, y, into dx
+    ("gate", A16 * 7), ("gate", A16 * 2 + 64), ("gate", A16 * 6 + 2 * 15 * 64 + 124), ("gate", A16 * 10), ("gate", A16 * 16 + 256),  # dx, a, dn's last bytes, the scale, the workspace
+    ("scale", A16 * 20 + 508), ("shift", A16 * 20 - 256), ("shift", A16 * 12), ("post_weight", A16 * 20 + 256),      # another gradient, a weight
+])
+def test_norm_backward_refuses_sums_over_anything_else(lib, name, at):
+    # B = 2, N = 8, C = 64: a tensor has 2048 bytes, a gradient of two entries 512, the partials 16 KB
+    grads = dict(gate=A16 * 20)
+    if name != "ws":
+        grads[name] = at
+    _refused(_norm_call(lib, backward=True, post_weight=A16 * 12, grads=grads, **({"ws": at} if name == "ws" else {})))
+
+
+def test_norm_backward_takes_neighbouring_sums(lib):
+    if not torch.cuda.is_available():
+        near = dict(gate=A16 * 20, scale=A16 * 20 + 512, shift=A16 * 20 + 1024, post_weight=A16 * 20 + 1536)
+        _without_device(_norm_call(lib, backward=True, post_weight=A16 * 12, grads=near, ws=A16 * 20 + 2048))
+        _without_device(_norm_call(lib, backward=True, post_weight=A16 * 12, grads={}, ws=A16 * 5))  # nothing wanted, nothing used
