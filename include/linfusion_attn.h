@@ -508,7 +508,7 @@ linfusion_status_t linfusion_attn_backward_kv(const linfusion_attn_desc_t* desc,
                                               const float* grad_state, void* dk, void* dv, void* workspace,
                                               size_t workspace_bytes, void* cuda_stream);
 /*
- * Enqueue a copy of the handle's state buffer (S | z of its last forward() or state(), in every variant; summed over
+ * Enqueue a copy of the handle's state buffer (S | z of its last forward(), forward_host() or state(), in every variant; summed over
  * devices where the caller has summed it) to `state`, fp32 device memory of the state buffer's length: what a backward
  * pass needs of the forward pass.  Errors: INVALID_ARG, CUDA.
  */

@@ -1273,6 +1273,12 @@ linfusion_status_t linfusion_attn_forward_host(linfusion_attn_t* h, const void* 
         if (!ok) break;
         linfusion_status_t st = linfusion_attn_forward(p->sub, dev(0, i), dev(1, i), dev(2, i), dev(3, i), s);
         if (st != LINFUSION_OK) return st;
+        // the group's slabs of S | z into the handle's own buffer, before the next group takes the sub-handle's
+        const size_t gstate = static_cast<size_t>(h->plan.slabs / p->groups) * h->plan.state_floats;
+        if (cudaMemcpyAsync(h->state + i * gstate, p->sub->state, gstate * sizeof(float), cudaMemcpyDeviceToDevice, s) != cudaSuccess) {
+            ok = false;
+            break;
+        }
         ok = cudaEventRecord(p->done[i], s) == cudaSuccess &&
              cudaStreamWaitEvent(p->copy_out, p->done[i], 0) == cudaSuccess &&
              cudaMemcpyAsync(static_cast<unsigned char*>(y_host) + i * gbytes, dev(3, i), gbytes,

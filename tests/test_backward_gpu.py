@@ -565,3 +565,24 @@ def test_an_eps_that_counts_and_values_with_a_mean(case, dtype):
         err = (grad_state[:, dk * dv:].view(B, H, dk).double() - dz).abs()
         assert (err <= SLACK * sizes).all(), f"dz {case} eps {eps}: {(err / sizes).max().item():.3e}"
         op.close()
+
+
+def test_state_saved_after_a_forward_on_host_buffers():
+    # large enough for two groups of slabs, which one sub-handle works through in turn
+    B, H, N, d = 1, 2, 262144, 64
+    tensors = _inputs(B, H, N, d, d, "bf16")[:3]
+    op = attn.LinFusionAttention(B, H, N, d, eps=EPS)
+    op.forward(*tensors)
+    want = op.save_state()
+    op.forward(tensors[0], torch.zeros_like(tensors[1]), tensors[2])  # another state
+    host = [t.cpu().pin_memory() for t in tensors]
+    y = torch.empty_like(host[0]).pin_memory()
+    op.forward_host(*host, y)
+    got = op.save_state()
+    torch.cuda.synchronize()
+    # the same terms, added in the order of another split of the tokens
+    for slab in range(H):
+        assert ((got[slab] - want[slab]).norm() / want[slab].norm()).item() <= 1e-5
+    S, z = op.read_state()
+    assert torch.equal(got.cpu()[:, :d * d].reshape(B, H, d, d), torch.from_numpy(S))
+    op.close()
