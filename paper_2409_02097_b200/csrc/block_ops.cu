@@ -385,6 +385,7 @@ linfusion_status_t linfusion_rope(const linfusion_rope_desc_t* desc, const linfu
                 return LINFUSION_ERR_INVALID_ARG;
         }
     if (given[0] != nullptr && given[1] != nullptr) {
+        if (static_cast<int64_t>(given[0]->heads) + given[1]->heads > INT32_MAX) return LINFUSION_ERR_UNSUPPORTED;
         const linfusion_rope_tensor_t &a = *given[0], &b = *given[1];
         const RopeView ai = rope_view(a, false), ao = rope_view(a, true), bi = rope_view(b, false), bo = rope_view(b, true);
         if (!views_apart(*desc, ao, bo) || !views_apart(*desc, ao, bi) || !views_apart(*desc, bo, ai)) return LINFUSION_ERR_INVALID_ARG;

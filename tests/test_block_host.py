@@ -320,3 +320,12 @@ def test_norm_backward_takes_neighbouring_sums(lib):
         near = dict(gate=A16 * 20, scale=A16 * 20 + 512, shift=A16 * 20 + 1024, post_weight=A16 * 20 + 1536)
         _without_device(_norm_call(lib, backward=True, post_weight=A16 * 12, grads=near, ws=A16 * 20 + 2048))
         _without_device(_norm_call(lib, backward=True, post_weight=A16 * 12, grads={}, ws=A16 * 5))  # nothing wanted, nothing used
+
+
+def test_rope_refuses_heads_that_pass_32_bits_together(lib):
+    far = 1 << 40
+    many = [_rope_tensor(in_=far * (2 * i + 2), out=far * (2 * i + 3), heads=1 << 30, in_t=0, out_t=8, in_h=8, out_h=8) for i in (0, 1)]
+    _refused(_rope_call(lib, q=many[0], k=many[1], B=1, N=1, d=8, pairs=(2, 2)), (attn.ERR_UNSUPPORTED,))
+    if not torch.cuda.is_available():
+        many[1].heads = (1 << 30) - 1
+        _without_device(_rope_call(lib, q=many[0], k=many[1], B=1, N=1, d=8, pairs=(2, 2)))
