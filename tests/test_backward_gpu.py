@@ -586,3 +586,64 @@ def test_state_saved_after_a_forward_on_host_buffers():
     S, z = op.read_state()
     assert torch.equal(got.cpu()[:, :d * d].reshape(B, H, d, d), torch.from_numpy(S))
     op.close()
+
+
+def test_threads_that_share_a_stream():
+    """Calls of several threads on one stream, their workspaces and outputs from one pool: what a thread's call holds is not
+    handed to another before its kernels are enqueued."""
+    import threading
+    shapes = [(2, 4, 900, 64), (1, 8, 300, 40), (1, 3, 2000, 128), (2, 2, 64, 160)]
+    jobs = []
+    for B, H, N, d in shapes:
+        op, tensors = attn.LinFusionAttention(B, H, N, d, eps=EPS, variant="split"), _inputs(B, H, N, d, d, "bf16", seed=N)
+        jobs.append((op, tensors, op.backward(*tensors)))
+    stream, wrong = torch.cuda.Stream(), []
+    stream.wait_stream(torch.cuda.current_stream())
+
+    def work(op, tensors, want):
+        with torch.cuda.stream(stream):
+            for _ in range(50):
+                got = op.backward(*tensors)
+                state = op.backward_state(*tensors[1:3])
+                dq, grad = op.backward_q(tensors[0], tensors[3], state)
+                parts = (dq, *op.backward_kv(tensors[1], tensors[2], grad))
+                if not all(torch.equal(a, c) and torch.equal(b, c) for a, b, c in zip(got, parts, want)):
+                    wrong.append(op.shape)
+
+    threads = [threading.Thread(target=work, args=job) for job in jobs for _ in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not wrong
+    for op, _, _ in jobs:
+        assert op.backward_status() == attn.OK
+        op.close()
+
+
+@pytest.mark.parametrize("variant,shape", [("split", (2, 4, 500, 64)), ("stream", (1, 4, 5000, 64)), ("fused", (2, 8, 1024, 80)), ("cluster", (2, 8, 150, 160)),
+                                           ("fused", (2, 20, 576, 64)), ("split", (1, 4, 4100, 128)), ("auto", (2, 8, 4096, 40))])
+def test_state_saved_by_a_forward_pass_in_fp16(variant, shape):
+    # S and z of the forward carry phi(K) rounded to 16 bits, the same in both: half a step on every term, and for phi itself as
+    # much again; a mean of the values leaves with the multiple of z
+    B, H, N, d = shape
+    for mean in (0.0, 2.0):
+        tensors = _inputs(B, H, N, d, d, "fp16", mean=mean, grad_scale=256.0)
+        op = attn.LinFusionAttention(B, H, N, d, eps=EPS, variant=variant, dtype="fp16")
+        op.forward(*tensors[:3])
+        want, _ = ref.attention_backward(*tensors, EPS)
+        for name, x, w in zip(("dq", "dk", "dv"), op.backward(*tensors, state=op.save_state()), want):
+            rel = ((x.double() - w).norm() / w.norm()).item()
+            assert rel <= 4 * 2.0 ** -11 / math.sqrt(3), f"{variant} mean {mean} {name}: {rel:.3e}"
+        op.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("case", [(2, 8, 16400, 160, 160), (1, 3, 16391, 32, 32)], ids=lambda c: "x".join(map(str, c)))
+def test_long_slabs_of_the_widths_that_have_no_tcgen05_kernel(case, dtype):
+    B, H, N, dk, dv = case
+    tensors = _inputs(B, H, N, dk, dv, dtype, mean=0.5, grad_scale=256.0 if dtype == "fp16" else 1.0)
+    op = attn.LinFusionAttention(B, H, N, dv, eps=EPS, variant="split", dtype=dtype)
+    _check(op.backward(*tensors), tensors, dtype, f"{case} {dtype}", rms=dtype == "bf16", extra=_mean_term(dtype, N, 0.5))
+    op.close()

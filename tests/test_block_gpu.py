@@ -566,3 +566,38 @@ def test_rope_theta_below_one(theta, interleaved, pairs):
         for got, x in ((qr, q), (kr, k)):
             rel = (got.double().square().sum(-1) / x.double().square().sum(-1) - 1).abs().max().item()
             assert rel <= 3 * 2.0 ** -11, f"not a rotation: {rel:.3e}"
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("N,C", [(9, 72), (9, 320), (7, 1280), (5, 4104)])
+def test_a_row_of_nan_or_infinity_stays_one_row(N, C, kind, value):
+    case = (2, N, C, kind, kind, True, True, "batch", True)
+    t, vec = _norm_case(case, torch.bfloat16)
+    op = _norm_op(case, "bf16")
+    y0, n0 = op.forward(t["x"], t["a"], **vec)
+    dy, dn = _grads_of(case, "bf16")
+    clean = op.backward(y0, t["a"], dy=dy, dn=dn, **vec)
+    row, other = (1, N // 2), torch.ones(2, N, dtype=torch.bool, device="cuda")
+    other[row] = False
+    for which in ("x", "a"):
+        bad = dict(t, **{which: t[which].clone()})
+        bad[which][row][C - 1] = value
+        y, n = op.forward(bad["x"], bad["a"], **vec)
+        assert torch.equal(y[other], y0[other]) and torch.equal(n[other], n0[other])
+        v = _dbl(vec)
+        want_y = ref.norm_after(bad["x"].double(), bad["a"].double(), v, kind, 1e-5, 0.75)
+        assert torch.equal(torch.isnan(y), torch.isnan(want_y)) and torch.equal(torch.isinf(y), torch.isinf(want_y))
+        assert torch.equal(torch.isnan(n), torch.isnan(ref.norm_before(y.double(), v, kind, 1e-5)))
+    for which in ("y", "a", "dy", "dn"):
+        bad = dict(y=y0, a=t["a"], dy=dy, dn=dn)
+        bad[which] = bad[which].clone()
+        bad[which][row][C - 1] = value
+        got = op.backward(bad["y"], bad["a"], dy=bad["dy"], dn=bad["dn"], **vec)
+        assert torch.equal(got["x"][other], clean["x"][other]) and torch.equal(got["a"][other], clean["a"][other])
+        for name in ("gate", "scale", "shift"):  # the other entry's vectors
+            assert torch.equal(got[name][0], clean[name][0])
+        want, _ = _reference_backward(case, dict(t, a=bad["a"]), vec, bad["y"], bad["dy"], bad["dn"])
+        assert not torch.isfinite(got["x"][row]).all() or which == "a"
+        for name in ("x", "a"):
+            assert torch.equal(torch.isfinite(got[name][row]), torch.isfinite(want[name][row])), f"{which} {name}"
