@@ -474,7 +474,7 @@ int32_t linfusion_attn_launches_per_forward(const linfusion_attn_t* h);
  * workspace: device memory, 256-byte aligned, of backward_workspace_bytes(), free again when the
  * call's kernels have run.
  * The products run on the tensor cores with every computed operand as head + tail of the storage type
- * (17 significant bits in bf16, 22 in fp16) and fp32 sums.  dQ is a difference in which what the values have in common
+ * (17 significant bits in bf16, 23 in fp16) and fp32 sums.  dQ is a difference in which what the values have in common
  * cancels: that part of S, the nearest multiple z mu^T, is taken off in fp32 before the products.  What S itself is off by
  * then counts sqrt(N) m / s times in dQ for values of mean m and spread s: 2^-25 of its elements where `state` is exact to
  * fp32, some 2^-22 where it is recomputed (the tensor cores' running sums), and the forward pass's 16-bit phi(K), the

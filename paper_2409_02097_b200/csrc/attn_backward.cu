@@ -86,11 +86,11 @@ void plan_chunks(const linfusion_attn_desc_t& d, int sm_count, BackwardPlan* p)
 // Which streams the tcgen05 kernels take (us, tcgen05 / warp-level, slabs x N x widths; a replayed graph of the stream alone):
 //   state   15 / 16 at 20 x 4096 x 64, 13 / 10 at 20 x 2048 x 64, 67 / 149 at 16 x 65536 x 64; 58 / 67 at 16 x 16384 x 128,
 //           41 / 39 at 16 x 8192 x 128; 79 / 84 at 16 x 32768 x 80, 50 / 46 at 16 x 16384 x 80
-//   q       16.4 / 17.1 at 20 x 2048 x 64, 14.7 / 11.4 at 20 x 1024 x 64, 111 / 222 at 16 x 65536 x 64; 72 / 86 at 16 x 8192 x 128,
-//           51 / 48 at 16 x 4096 x 128; 72 / 80 at 16 x 16384 x 80/40, but 164 / 156 at 16 x 32768 x 80, whose 80 are padded to 128 twice
+//   q       14.4 / 17.2 at 20 x 2048 x 64, 12.6 / 11.8 at 20 x 1024 x 64, 113 / 214 at 16 x 65536 x 64; 65 / 84 at 16 x 8192 x 128,
+//           44 / 49 at 16 x 4096 x 128; 76 / 79 at 16 x 16384 x 80/40, but 161 / 160 at 16 x 32768 x 80, whose 80 are padded to 128 twice
 //   kv      12.6 / 19.6 at 20 x 4096 x 64, 6.3 / 7.4 at 128 x 64 x 64; 12.9 / 14.9 at 16 x 1024 x 128, 12.3 / 9.3 at 16 x 512 x 128
 // Widths of 32, padded to 64: 123 / 105, 211 / 168, 181 / 146 at 32 x 65536.  Short slabs: where a CTA changes its state every
-// tile, state and q take 73 / 15 and 91 / 41 at 1024 x 128 x 64, 245 / 44 and 327 / 115 at 1024 x 128 x 128, kv still 27 / 40 and
+// tile, state and q take 73 / 15 and 69 / 40 at 1024 x 128 x 64, 245 / 44 and 199 / 112 at 1024 x 128 x 128, kv still 27 / 40 and
 // 82 / 113, but 25 / 21 at 1024 x 16 x 64.
 void plan_tc(const linfusion_attn_desc_t& d, int sm_count, BackwardPlan* p)
 {
@@ -106,7 +106,7 @@ void plan_tc(const linfusion_attn_desc_t& d, int sm_count, BackwardPlan* p)
     } else if (p->tc == 2) {
         const bool padded = p->dk < 128;
         p->tc_state = p->tiles_per_slab >= 16 && tiles >= (p->dv <= 64 ? 4.0 : padded ? 16.0 : 8.0);
-        p->tc_q = p->tiles_per_slab >= 8 && tiles >= (padded ? 12.0 : p->dv <= 64 ? 3.0 : 4.0) && !(padded && p->dv > 64);
+        p->tc_q = p->tiles_per_slab >= 8 && tiles >= (padded ? 12.0 : 3.0) && !(padded && p->dv > 64);
         p->tc_kv = d.N >= 64 && tiles >= 0.75;
     }
     p->tc_partial = p->tc == 1 ? BackwardTc::PARTIAL_FLOATS : p->dv > 64 ? BackwardTcWide<2>::PARTIAL_FLOATS : BackwardTcWide<1>::PARTIAL_FLOATS;

@@ -23,7 +23,7 @@
 // mu = S^T z / (z . z) leaves the smallest R.  (The term with eps is formed only for tokens where w eps is 2^-24 or more: below,
 // it is less than what the rounding of S to fp32 leaves.)  Every operand of the tensor-core products that is not an input
 // tensor (R, w f, dS, phi(k)) is carried as a head and a tail of the storage type, x = hi + lo with |x - hi - lo| <= 2^-17 |x|
-// (bf16) or 2^-22 (fp16): two products in place of one (three for dS^T f).  The results are then off by little more
+// (bf16) or 2^-23 (fp16): two products in place of one (three for dS^T f).  The results are then off by little more
 // than the one rounding of the 16-bit outputs.
 #pragma once
 
@@ -105,7 +105,7 @@ struct BackwardCfg {
 
 struct BackwardScales {
     float eps;        // negative: without the normalizer
-    int scaled;       // fp16 operands: scale S, w f and dS by powers of two of their own sizes
+    int scaled;       // fp16 operands: scale R, w f and dS by powers of two of their own sizes
 };
 
 // Power of two 2^-e with 2^e <= x < 2^(e+1), times 2^up; 1 for zero, infinite or NaN x.

@@ -15,7 +15,7 @@
 // Two warpgroups take turns at the tiles, a warp loads by TMA into a ring of five tiles (32 KB each), a warp issues the
 // MMAs, a warp sends gradients out:
 //
-//   state:  T[128 x 64]  = dY S^T             (hi, then lo: 8 steps of K = 16, dY straight from the stage)
+//   state:  T[128 x 64]  = dY R^T             (hi, then lo: 8 steps of K = 16, dY straight from the stage)
 //           D[128 x 64] += [F_hi | F_lo]^T dY (F = w phi(q); head and tail are the two halves of M = 128: 8 steps)
 //   kv:     T[128 x 64]  = V dS^T  (8 steps)   and   T'[128 x 64] = F dS = F_hi dS_hi + F_hi dS_lo + F_lo dS_hi (12)
 //

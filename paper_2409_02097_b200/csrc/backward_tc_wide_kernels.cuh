@@ -7,7 +7,7 @@
 // and the gradients wait in registers until the product that reads F is done, then take F's place and leave by TMA while the
 // next tile is under way.
 //
-//   state:  T[128 x 128] = dY S^T      (16 MMAs of N = 128 for head and tail at dv = 128)
+//   state:  T[128 x 128] = dY R^T      (16 MMAs of N = 128 for head and tail at dv = 128)
 //           D_a[128 x dv] += [F_hi,a | F_lo,a]^T dY for each atom a (8 MMAs each)
 //   kv:     T[128 x 128] = V dS^T,  T'[128 x dv] = F_hi dS_hi + F_hi dS_lo + F_lo dS_hi  (24 MMAs)
 //

@@ -282,8 +282,9 @@ __global__ void __launch_bounds__(kRopeThreads, 4) rope_kernel(const __grid_cons
 // asynchronous copies that only the thread itself waits for), so DRAM latency is hidden without registers.
 //
 // A row's mean and variance: each warp takes its sum by shuffles, then the sum of squares about its own mean, and the
-// warps' (sum, squares) pairs are joined exactly:  M2 = sum_w [M2_w + n_w (mean_w - mean)^2].  Nothing cancels,
-// whatever the row's mean.  Two quantities (the two norms of a row, or two sums) travel together, one in each half of the
+// warps' (sum, squares) pairs are joined exactly:  M2 = sum_w [M2_w + n_w (mean_w - mean)^2].  Nothing cancels in them,
+// whatever the row's mean; the normed value is then x rstd - mean rstd in one fma, off by the rounding of its last term (2^-24 of
+// mean / deviation).  Two quantities (the two norms of a row, or two sums) travel together, one in each half of the
 // warp: halving the values while the lanes are halved costs five shuffles instead of ten.
 //
 // What bounds them: DRAM at large C x rows, 4.9 TB/s forward and 4.3 TB/s backward of the 6.5 of a copy (68.6 and 117 us at 2 x 16384 x
