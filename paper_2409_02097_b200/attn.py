@@ -344,10 +344,11 @@ class LinFusionAttention:
         return int(self._lib.linfusion_attn_launches_per_forward(self._h))
 
     # -- calls ------------------------------------------------------------------------------
-    def _check(self, t, name):
+    def _check(self, t, name, like=None):
         import torch
+        like = like or name  # the tensor whose shape it has
         want = torch.float16 if self.dtype == "fp16" else torch.bfloat16
-        shape = self.shape_qk if name in ("q", "k") else self.shape
+        shape = self.shape_qk if like in ("q", "k") else self.shape
         if t.shape != shape or t.dtype != want or not t.is_contiguous():
             raise ValueError(f"{name}: expected contiguous {self.dtype} tensor of shape {shape}")
 
@@ -563,7 +564,7 @@ class LinFusionAttention:
             if like == "state":
                 self._check_state(t, name, device)
                 continue
-            self._check(t, like)
+            self._check(t, name, like)
             if not t.is_cuda or t.get_device() != index:
                 raise ValueError(f"{name}: expected a tensor on {device}")
         for t, name in states:

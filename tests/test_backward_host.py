@@ -126,3 +126,12 @@ def test_the_count_of_expired_waits_refuses_bad_arguments():
         assert lib.linfusion_attn_selftest_backward_wait(ctypes.byref(desc), ws, None) == attn.ERR_INVALID_ARG
     if not torch.cuda.is_available():
         assert lib.linfusion_attn_backward_expired(0, ctypes.byref(n), None) == attn.ERR_CUDA
+
+
+def test_refusals_name_the_tensor(made):
+    op = _op()
+    q, k, v, dy = _inputs()
+    for name, call in (("dy", lambda bad: op.backward(q, k, v, bad, stream=1)), ("dq", lambda bad: op.backward(q, k, v, dy, dq=bad, stream=1)),
+                       ("dv", lambda bad: op.backward_kv(k, v, _state(), dv=bad, stream=1))):
+        with pytest.raises(ValueError, match=rf"^{name}: "):
+            call(q[:, :1])
