@@ -647,3 +647,15 @@ def test_long_slabs_of_the_widths_that_have_no_tcgen05_kernel(case, dtype):
     op = attn.LinFusionAttention(B, H, N, dv, eps=EPS, variant="split", dtype=dtype)
     _check(op.backward(*tensors), tensors, dtype, f"{case} {dtype}", rms=dtype == "bf16", extra=_mean_term(dtype, N, 0.5))
     op.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("case", [(1, 3, 300, 64, 64), (2, 4, 4200, 64, 64), (1, 5, 4001, 128, 128), (1, 2, 150, 160, 160)], ids=lambda c: "x".join(map(str, c)))
+def test_features_of_both_signs(case, dtype):
+    # phi(x) = x with an eps that keeps f . z + eps away from zero: z of either sign, and the eps term counts for every token
+    B, H, N, dk, dv = case
+    q, k, v, dy = _inputs(B, H, N, dk, dv, dtype, mean=2.0, grad_scale=16.0)
+    eps = 60.0 * math.sqrt(N * dk)  # |f . z| is some sqrt(N dk)
+    op = attn.LinFusionAttention(B, H, N, dv, phi=1, eps=eps, variant="split", dtype=dtype)
+    _check(op.backward(q, k, v, dy), (q, k, v, dy), dtype, f"{case} {dtype}", eps=eps, kind=1, rms=False)
+    op.close()
