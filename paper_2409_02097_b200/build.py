@@ -16,7 +16,12 @@ _SOURCES = {
     "attn_backward.cu": ["common.cuh", "backward_kernels.cuh", "backward_tc_kernels.cuh",
                          "backward_tc_wide_kernels.cuh", "packed_math.cuh", "host_util.h",
                          "linfusion_attn.h"],
-    "block_ops.cu": ["common.cuh", "block_kernels.cuh", "packed_math.cuh", "host_util.h", "linfusion_attn.h", "linfusion_block.h"],
+    "block_ops.cu": ["common.cuh", "block_kernels.cuh", "packed_math.cuh", "host_checks.h", "host_util.h", "linfusion_attn.h",
+                     "linfusion_block.h"],
+    "pack8.cu": ["common.cuh", "pack8.cuh", "block_kernels.cuh", "packed_math.cuh", "host_checks.h", "host_util.h", "linfusion_attn.h",
+                 "linfusion_block.h", "linfusion_layers.h"],
+    "recurrence.cu": ["common.cuh", "recurrence_kernels.cuh", "pack8.cuh", "host_checks.h", "host_util.h", "linfusion_attn.h",
+                      "linfusion_block.h", "linfusion_layers.h"],
 }
 CHECKED_LIB_PATH = os.path.join(_PKG, "liblinfusion_attn_checked.so")
 

@@ -1,0 +1,66 @@
+// The 8-bit checkpoint format of include/linfusion_layers.h on the device: 32 channels share a power of two.
+//
+// Why a power of two and whole numbers: x * 2^-e and code * 2^e are exact, so packing rounds once, reading not at all, and the
+// same codes come out whatever computes them.  A value is off by at most half a step, max|x| / 127 of its group; against a scale of
+// max|x| / 127 itself that costs half a bit on average.  (An 8-bit float of four significant bits is off by up to 1 / 16 of
+// each value: for the activations of a layer several times as much in the 2-norm.)
+#pragma once
+
+#include "common.cuh"
+
+namespace lf {
+
+// What a scale byte may be: e + 127 for e in -126 .. 121, or -24 .. 9 in fp16 (there the smallest step is the format's own, and
+// 127 * 2^10 would pass its largest number; in bf16 127 * 2^122 would).
+template <int KIND>
+__device__ __forceinline__ constexpr int pack8_scale_min() { return kind_dtype(KIND) == kDtypeFp16 ? 103 : 1; }
+template <int KIND>
+__device__ __forceinline__ constexpr int pack8_scale_max() { return kind_dtype(KIND) == kDtypeFp16 ? 136 : 248; }
+
+// The scale byte for the largest magnitude of a group (finite): with most = m * 2^E, 1 <= m < 2, the smallest e with
+// m * 2^E <= 127 * 2^e is E - 6 for m <= 127 / 64, else E - 5; m's fraction above 0x7E0000 carries into the exponent below.
+template <int KIND>
+__device__ __forceinline__ int pack8_scale(float most)
+{
+    const int s = static_cast<int>((__float_as_uint(most) + 0x1FFFFu) >> 23) - 6;
+    return min(max(s, pack8_scale_min<KIND>()), pack8_scale_max<KIND>());
+}
+__device__ __forceinline__ float pack8_step(int scale) { return __uint_as_float(static_cast<uint32_t>(scale) << 23); }
+__device__ __forceinline__ float pack8_inverse_step(int scale) { return __uint_as_float(static_cast<uint32_t>(254 - scale) << 23); }
+
+// |x|, or 0 where x is not finite.
+__device__ __forceinline__ float finite_abs(float x)
+{
+    const float a = fabsf(x);
+    return a < __uint_as_float(0x7f800000u) ? a : 0.0f;
+}
+
+// Four values -> four codes in a word.  Adding 1.5 * 2^23 leaves the nearest whole number (ties to even) in the low bits.
+__device__ __forceinline__ uint32_t pack8_codes4(const float* x, float inverse)
+{
+    uint32_t c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float r = fminf(fmaxf(x[i] * inverse, -127.0f), 127.0f);
+        c[i] = __float_as_uint(r + 12582912.0f);
+        if (!(fabsf(x[i]) < __uint_as_float(0x7f800000u))) c[i] = 0x80u;
+    }
+    return __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
+}
+
+// Four codes -> four values.  A code's byte with its top bit turned over, as the low byte of a float of 2^23, is 2^23 + 128 +
+// code; the difference and the product are exact.  (One fma for both would overflow for steps above 2^104.)
+__device__ __forceinline__ void unpack8_codes4(uint32_t word, float step, float* x)
+{
+    const uint32_t w = word ^ 0x80808080u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7540 + i)) - 8388736.0f) * step;
+    // a byte of w that is zero was the code -128
+    if (((w - 0x01010101u) & ~w & 0x80808080u) != 0u) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (((word >> (8 * i)) & 0xffu) == 0x80u) x[i] = __uint_as_float(0x7fffffffu);
+    }
+}
+
+}  // namespace lf

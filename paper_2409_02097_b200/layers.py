@@ -1,0 +1,363 @@
+"""ctypes binding over the C ABI in ``include/linfusion_layers.h``: a block's own layers.
+
+``pack8``            activation checkpoints in 8 bits (``Packed8``), which the backward passes below read as they are
+``GatedRecurrence``  a gated linear recurrence over the tokens, each channel for itself
+
+Argument marshalling only: the arithmetic is in the CUDA library, and there is no CPU fallback.  Objects hold a
+configuration and no device memory, so one may serve any streams and threads at once.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Dict, Optional, Tuple
+
+from . import block
+from .attn import DTYPE_FP16, LinFusionError, OK, allocating_on
+from .block import Rows, _Checked, _Fixed, _call, _check_rc, _check_tensor, _like, _look, _torch_dtype
+
+GROUP = 32          # channels that share a scale of a checkpoint
+STATE_EVERY = 64    # tokens from one kept state of the recurrence to the next
+
+EXPORTED = ["linfusion_pack8", "linfusion_unpack8", "linfusion_recurrence", "linfusion_recurrence_backward",
+            "linfusion_recurrence_workspace_bytes", "linfusion_layers_expired"]
+
+_i32, _i64, _vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
+
+
+class Pack8Desc(ctypes.Structure):
+    """Mirror of ``linfusion_pack8_desc_t``."""
+    _fields_ = [("B", _i32), ("N", _i32), ("C", _i32), ("flags", ctypes.c_uint32)]
+
+
+class Packed8Struct(ctypes.Structure):
+    """Mirror of ``linfusion_packed8_t``."""
+    _fields_ = [("codes", _vp), ("scales", _vp)]
+
+
+class RecurrenceDesc(ctypes.Structure):
+    """Mirror of ``linfusion_recurrence_desc_t``."""
+    _fields_ = [("B", _i32), ("N", _i32), ("C", _i32), ("reverse", _i32), ("flags", ctypes.c_uint32)]
+
+
+class RecurrenceInput(ctypes.Structure):
+    """Mirror of ``linfusion_recurrence_input_t``."""
+    _fields_ = [("rows", Rows), ("packed", Packed8Struct)]
+
+
+class RecurrenceGrads(ctypes.Structure):
+    """Mirror of ``linfusion_recurrence_grads_t``."""
+    _fields_ = [("x", Rows), ("decay", Rows), ("gate", Rows), ("rate", _vp), ("h0", _vp)]
+
+
+_lib = None
+
+
+def load_library() -> ctypes.CDLL:
+    global _lib
+    if _lib is None:
+        lib, P, size = block.load_library(), ctypes.POINTER, ctypes.c_size_t
+        rows, given = P(Rows), P(RecurrenceInput)
+        for name, args in {
+                "linfusion_pack8": [P(Pack8Desc), rows, P(Packed8Struct), _vp],
+                "linfusion_unpack8": [P(Pack8Desc), P(Packed8Struct), rows, _vp],
+                "linfusion_recurrence": [P(RecurrenceDesc), given, given, given, _vp, _vp, rows, _vp, _vp, _vp, size, _vp],
+                "linfusion_recurrence_backward": [P(RecurrenceDesc), given, given, given, _vp, _vp, _vp, rows, _vp, P(RecurrenceGrads), _vp,
+                                                  size, _vp],
+                "linfusion_recurrence_workspace_bytes": [P(RecurrenceDesc), _i32, P(size)],
+                "linfusion_layers_expired": [_i32, P(ctypes.c_uint32), _vp]}.items():
+            getattr(lib, name).restype = ctypes.c_int
+            getattr(lib, name).argtypes = args
+        _lib = lib
+    return _lib
+
+
+def expired(device: int = 0, stream: Optional[int] = None) -> int:
+    """How many waits of these layers' kernels expired on `device` since the library was loaded (synchronizes the stream); outputs
+    of a call whose wait expired are not to be used."""
+    import torch
+    n = ctypes.c_uint32(0)
+    if stream is None:
+        stream = torch.cuda.current_stream(device).cuda_stream
+    _check_rc(load_library().linfusion_layers_expired(int(device), ctypes.byref(n), stream), "linfusion_layers_expired")
+    return int(n.value)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+# -------------------------------------------------------------------------------------- checkpoints
+def _rows3(t, name):
+    """A tensor of two or more axes as [B, N, C] without a copy: the axes before the last two have to merge."""
+    if t.dim() < 2:
+        raise ValueError(f"{name}: expected two axes or more, got {tuple(t.shape)}")
+    if t.dim() == 3:
+        return t
+    if t.dim() == 2:
+        return t.unsqueeze(0)
+    try:
+        return t.view(-1, *t.shape[-2:])
+    except RuntimeError:
+        raise ValueError(f"{name}: the axes before the last two, of strides {t.stride()}, do not merge") from None
+
+
+def _pack8_desc(t, name, dtype):
+    _check_tensor(t, name, _torch_dtype(dtype))
+    if t.numel() == 0:
+        raise ValueError(f"{name}: no values")
+    r = _rows3(t, name)
+    B, N, C = r.shape
+    return Pack8Desc(B, N, C, DTYPE_FP16 if dtype == "fp16" else 0), Rows(t.data_ptr(), r.stride(0), r.stride(1))
+
+
+class Packed8:
+    """A tensor in 8 bits: ``codes`` int8 of its shape, ``scales`` uint8 [..., ceil(C / 32)], both contiguous CUDA tensors; a value is
+    ``codes * 2 ** (scales - 127)``, the scale that of its 32 channels.  ``dtype``: the storage type ("bf16" or "fp16") that it
+    was made from, in which those values are exact.  A code of -128 stands for NaN."""
+
+    __slots__ = ("codes", "scales", "dtype")
+
+    def __init__(self, codes, scales, dtype: str = "bf16"):
+        import torch
+        _torch_dtype(dtype)
+        if codes.dtype != torch.int8 or scales.dtype != torch.uint8:
+            raise ValueError(f"expected int8 codes and uint8 scales, got {codes.dtype} and {scales.dtype}")
+        if codes.dim() < 2 or tuple(scales.shape) != (*codes.shape[:-1], -(-codes.shape[-1] // GROUP)):
+            raise ValueError(f"codes {tuple(codes.shape)} and scales {tuple(scales.shape)} do not belong together")
+        if not codes.is_cuda or scales.device != codes.device:
+            raise ValueError("expected CUDA tensors on one device")
+        if not codes.is_contiguous() or not scales.is_contiguous():
+            raise ValueError("codes and scales must be contiguous")
+        self.codes, self.scales, self.dtype = codes, scales, dtype
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+    @property
+    def device(self):
+        return self.codes.device
+
+    def unpack(self, out=None, stream: Optional[int] = None):
+        """The values in the storage type (exact)."""
+        import torch
+        index = self.codes.get_device()
+        if stream is not None:
+            with allocating_on(stream, index):
+                return self.unpack(out)
+        if out is None:
+            out = torch.empty(self.codes.shape, dtype=_torch_dtype(self.dtype), device=self.codes.device)
+        elif out.shape != self.codes.shape or out.device != self.codes.device:
+            raise ValueError(f"out: expected {tuple(self.codes.shape)} on {self.codes.device}, got {tuple(out.shape)} on {out.device}")
+        desc, rows = _pack8_desc(out, "out", self.dtype)
+        _check_rc(_call(index, load_library().linfusion_unpack8, desc, Packed8Struct(self.codes.data_ptr(), self.scales.data_ptr()), rows),
+                  "linfusion_unpack8")
+        return out
+
+
+def _new_packed(shape, dtype, device):
+    import torch
+    return Packed8(torch.empty(shape, dtype=torch.int8, device=device),
+                   torch.empty((*shape[:-1], -(-shape[-1] // GROUP)), dtype=torch.uint8, device=device), dtype)
+
+
+def pack8(x, out: Optional[Packed8] = None, stream: Optional[int] = None) -> Packed8:
+    """A bf16 or fp16 CUDA tensor [..., C] in 8 bits (see ``Packed8``): 32 channels share a power of two, values are rounded to 255 steps.
+    Axes before the last two must merge; strides are multiples of 8."""
+    import torch
+    if x.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"x: expected bf16 or fp16, got {x.dtype}")
+    dtype = "fp16" if x.dtype == torch.float16 else "bf16"
+    if stream is not None and x.is_cuda:
+        with allocating_on(stream, x.get_device()):
+            return pack8(x, out)
+    desc, rows = _pack8_desc(x, "x", dtype)
+    if out is None:
+        out = _new_packed(x.shape, dtype, x.device)
+    elif out.shape != x.shape or out.dtype != dtype or out.device != x.device:
+        raise ValueError(f"out: expected a {dtype} checkpoint of {tuple(x.shape)} on {x.device}")
+    _check_rc(_call(x.get_device(), load_library().linfusion_pack8, desc, rows, Packed8Struct(out.codes.data_ptr(), out.scales.data_ptr())),
+              "linfusion_pack8")
+    return out
+
+
+# -------------------------------------------------------------------------------------- recurrence
+def _look8(t):
+    """_look() of a tensor or a checkpoint (whose tensors are contiguous)."""
+    return (t.codes.shape, t.dtype, t.codes.get_device()) if isinstance(t, Packed8) else _look(t)
+
+
+class GatedRecurrence(_Fixed):
+    """A gated linear recurrence over the tokens of x [B, N, C], each channel for itself, from the first token to the last or
+    with ``reverse`` from the last to the first:
+
+        a_t = exp(-rate * sigmoid(decay_t))        v_t = sigmoid(gate_t) * x_t    (x_t without ``gate``)
+        h_t = a_t h_(t-1) + (1 - a_t) v_t
+
+    x, decay, gate: 16-bit CUDA tensors [B, N, C] with any batch and row strides that are multiples of 8 elements (windows of
+    one projection are fine); rate: fp32 [C], not negative; h0: fp32 [B, C], the state before the first token (None: zero).
+    A token with decay = -inf leaves the state as it is, whatever its x and gate hold: padding.  One token at a time, with
+    h0 the state that the call before returned, gives what one call over all tokens gives (up to the rounding of fp32).
+    """
+
+    def __init__(self, C: int, reverse: bool = False, dtype: str = "bf16"):
+        if int(C) <= 0 or int(C) % 8 != 0:
+            raise ValueError(f"C: expected a multiple of 8, got {C}")
+        self.C, self.reverse, self.dtype = int(C), bool(reverse), dtype
+        self._torch_dtype = _torch_dtype(dtype)
+        self._flags = DTYPE_FP16 if dtype == "fp16" else 0
+        self._lib = load_library()
+        self._checked = _Checked()
+
+    def _desc(self, B, N):
+        return RecurrenceDesc(B, N, self.C, self.reverse, self._flags)
+
+    def workspace_bytes(self, B: int, N: int, backward: bool = False, state: bool = True) -> int:
+        """Bytes of workspace that ``forward`` takes for B x N tokens, or ``backward`` with or without the saved states."""
+        n = ctypes.c_size_t(0)
+        _check_rc(self._lib.linfusion_recurrence_workspace_bytes(ctypes.byref(self._desc(int(B), int(N))), (1 if state else 2) if backward else 0,
+                                                                 ctypes.byref(n)), "linfusion_recurrence_workspace_bytes")
+        return int(n.value)
+
+    def state_shape(self, B: int, N: int) -> Tuple[int, int, int]:
+        """Shape of the saved states, those before every 64th token in the order of the scan."""
+        return (B, -(-N // STATE_EVERY), self.C)
+
+    def _rows(self, t, name, shape, device):
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name}: expected {shape}, got {tuple(t.shape)}")
+        _check_tensor(t, name, self._torch_dtype, device)
+        return Rows(None, t.stride(0), t.stride(1))
+
+    def _input(self, t, name, shape, device, packed):
+        if isinstance(t, Packed8) != packed:
+            raise ValueError("x, decay and gate: either all in 8 bits or none")
+        if not packed:
+            return RecurrenceInput(self._rows(t, name, shape, device), Packed8Struct())
+        if tuple(t.shape) != shape or t.dtype != self.dtype or t.device != device:
+            raise ValueError(f"{name}: expected a {self.dtype} checkpoint of {shape} on {device}, got a {t.dtype} one of {tuple(t.shape)} on {t.device}")
+        return RecurrenceInput()
+
+    def _floats(self, t, name, shape, device):
+        import torch
+        if t is None:
+            return
+        if tuple(t.shape) != shape or t.dtype != torch.float32 or t.device != device or not t.is_contiguous():
+            raise ValueError(f"{name}: expected a contiguous fp32 tensor of {shape} on {device}")
+
+    def _check(self, x, decay, gate, rate, h0, others, floats, backward):
+        if len(x.shape) != 3 or x.shape[0] == 0 or x.shape[1] == 0 or x.shape[2] != self.C:
+            raise ValueError(f"x: expected [B, N, {self.C}] with at least one token, got {tuple(x.shape)}")
+        shape, device, packed = tuple(x.shape), x.device, isinstance(x, Packed8)
+        B, N, _ = shape
+        ins = [None if t is None else self._input(t, name, shape, device, packed) for name, t in (("x", x), ("decay", decay), ("gate", gate))]
+        ends = (B, self.C)
+        for name, t, want in (("rate", rate, (self.C,)), ("h0", h0, ends), *((n, t, self.state_shape(B, N) if n == "state" else (self.C,) if n == "rate gradient" else ends) for n, t in floats)):
+            self._floats(t, name, want, device)
+        outs = [None if t is None else self._rows(t, name, shape, device) for name, t in others]
+        state = any(n == "state" and t is not None for n, t in floats)
+        return self._desc(B, N), ins, outs, self.workspace_bytes(B, N, backward, state)
+
+    @staticmethod
+    def _inputs(structs, tensors):
+        out = []
+        for s, t in zip(structs, tensors):
+            if s is not None:
+                s = type(s).from_buffer_copy(s)
+                if isinstance(t, Packed8):
+                    s.packed.codes, s.packed.scales = t.codes.data_ptr(), t.scales.data_ptr()
+                else:
+                    s.rows.p = t.data_ptr()
+            out.append(s)
+        return out
+
+    @staticmethod
+    def _workspace(workspace, need, device):
+        import torch
+        if workspace is None:
+            return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+        if not workspace.is_cuda or workspace.device != device or not workspace.is_contiguous():
+            raise ValueError("workspace: expected a contiguous CUDA tensor on the device of the others")
+        return workspace
+
+    def forward(self, x, decay, rate, gate=None, h0=None, save: bool = False, h=None, last=None, state=None, workspace=None,
+                stream: Optional[int] = None) -> Tuple:
+        """(h, last, state): the states of all tokens in the storage type, the last of the scan in fp32 [B, C], and with ``save`` those
+        before every 64th token in fp32 (``state_shape``; else None), which ``backward`` recomputes h from.  ``h`` may be given as x,
+        decay or gate, ``last`` as h0 (in place).  ``workspace``: a CUDA tensor of at least ``workspace_bytes``, else one is
+        allocated."""
+        import torch
+        if isinstance(x, Packed8) or isinstance(decay, Packed8) or isinstance(gate, Packed8):
+            raise ValueError("the forward pass takes 16-bit inputs")
+        if stream is not None and x.is_cuda:
+            with allocating_on(stream, x.get_device()):
+                return self.forward(x, decay, rate, gate, h0, save, h, last, state, workspace)
+        if state is not None and not save:
+            raise ValueError("state is given, but not save")
+        key = (0, _look(x), _look(decay), _look(gate), _look(rate), _look(h0), _look(h), _look(last), _look(state))
+        found = self._checked.get(key)
+        if found is None:
+            found = self._checked.keep(key, self._check(x, decay, gate, rate, h0, (("h", h),), (("last", last), ("state", state)), False))
+        desc, ins, outs, need = found
+        B, N, C = x.shape
+        device = x.device
+        if h is None:
+            h, rows = _like(x), Rows(None, N * C, C)
+        else:
+            rows = type(outs[0]).from_buffer_copy(outs[0])
+        rows.p = h.data_ptr()
+        if last is None:
+            last = torch.empty((B, C), dtype=torch.float32, device=device)
+        if save and state is None:
+            state = torch.empty(self.state_shape(B, N), dtype=torch.float32, device=device)
+        ws = self._workspace(workspace, need, device)
+        ix, id_, ig = self._inputs(ins, (x, decay, gate))
+        rc = _call(x.get_device(), self._lib.linfusion_recurrence, desc, ix, id_, ig, rate.data_ptr(), _ptr(h0), rows, last.data_ptr(), _ptr(state),
+                   _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
+        if rc != OK:
+            raise LinFusionError(rc, "linfusion_recurrence")
+        return h, last, state
+
+    def backward(self, dh, x, decay, rate, gate=None, h0=None, state=None, dlast=None, dx=None, ddecay=None, dgate=None, workspace=None,
+                 stream: Optional[int] = None) -> Dict:
+        """Gradients by name: ``x``, ``decay``, ``gate`` where there is one, in the storage type, ``rate`` and, with h0, ``h0`` in fp32.
+
+        x, decay, gate as ``forward`` had them, or all as ``Packed8``; ``state`` as ``forward(save=True)`` returned it (None:
+        recomputed, from the inputs and h0); ``dlast`` the gradient of the last state.  dx, ddecay and dgate may be given as dh
+        or as their 16-bit inputs (in place), or as windows of one tensor."""
+        import torch
+        if stream is not None and dh.is_cuda:
+            with allocating_on(stream, dh.get_device()):
+                return self.backward(dh, x, decay, rate, gate, h0, state, dlast, dx, ddecay, dgate, workspace)
+        if dgate is not None and gate is None:
+            raise ValueError("dgate is given, but no gate")
+        key = (1, _look(dh), _look8(x), _look8(decay), _look8(gate), _look(rate), _look(h0), _look(state), _look(dlast), _look(dx), _look(ddecay),
+               _look(dgate))
+        found = self._checked.get(key)
+        if found is None:
+            others = (("dh", dh), ("dx", dx), ("ddecay", ddecay), ("dgate", dgate))
+            found = self._checked.keep(key, self._check(x, decay, gate, rate, h0, others, (("state", state), ("dlast", dlast)), True))
+        desc, ins, outs, need = found
+        B, N, C = x.shape
+        out, rows = {}, []
+        for name, t, struct, wanted in (("x", dx, outs[1], True), ("decay", ddecay, outs[2], True), ("gate", dgate, outs[3], gate is not None)):
+            if not wanted:
+                rows.append(Rows())
+                continue
+            if t is None:
+                t, struct = _like(dh), Rows(None, N * C, C)
+            out[name] = t
+            rows.append(Rows(t.data_ptr(), struct.batch, struct.row))
+        device = dh.device
+        out["rate"] = torch.empty(C, dtype=torch.float32, device=device)
+        if h0 is not None:
+            out["h0"] = torch.empty((B, C), dtype=torch.float32, device=device)
+        grads = RecurrenceGrads(*rows, out["rate"].data_ptr(), _ptr(out.get("h0")))
+        ws = self._workspace(workspace, need, device)
+        ix, id_, ig = self._inputs(ins, (x, decay, gate))
+        rdh = Rows(dh.data_ptr(), outs[0].batch, outs[0].row)
+        rc = _call(dh.get_device(), self._lib.linfusion_recurrence_backward, desc, ix, id_, ig, rate.data_ptr(), _ptr(h0), _ptr(state), rdh,
+                   _ptr(dlast), grads, ws.data_ptr(), ws.numel() * ws.element_size())
+        if rc != OK:
+            raise LinFusionError(rc, "linfusion_recurrence_backward")
+        return out
