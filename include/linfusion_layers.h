@@ -161,11 +161,14 @@ typedef struct {
 
 /*
  * One launch.  y may lie exactly over residual.  Otherwise the address range of an output must not meet that of an
- * input or another output.  Errors: INVALID_ARG, UNSUPPORTED (K or N no multiple of 8, unknown flags or act), CUDA.
+ * input or another output.  workspace: device memory, 256-byte aligned, of linfusion_linear_workspace_bytes() (0 for
+ * many sizes; NULL is fine then); used until the call's kernel has run, and may then be used by anything else.
+ * Errors: INVALID_ARG, UNSUPPORTED (K or N no multiple of 8, unknown flags or act), ALLOC (workspace too small), CUDA.
  */
 linfusion_status_t linfusion_linear(const linfusion_linear_desc_t* desc, const linfusion_matrix_t* x, const linfusion_matrix_t* w,
                                     const void* bias, const linfusion_matrix_t* residual, const linfusion_matrix_t* y,
-                                    const linfusion_matrix_t* u, const linfusion_packed8_t* u_packed, void* cuda_stream);
+                                    const linfusion_matrix_t* u, const linfusion_packed8_t* u_packed, void* workspace,
+                                    size_t workspace_bytes, void* cuda_stream);
 
 /* What the backward pass reads besides dy and w: x and u each in 16 bits or as a checkpoint (of M rows). */
 typedef struct {
@@ -183,8 +186,9 @@ linfusion_status_t linfusion_linear_backward(const linfusion_linear_desc_t* desc
                                              const linfusion_linear_saved_t* saved, const linfusion_matrix_t* w,
                                              const linfusion_matrix_t* dx, const linfusion_matrix_t* dw, float* dbias,
                                              void* workspace, size_t workspace_bytes, void* cuda_stream);
-/* Pure host computation: of a backward pass that reads x as a checkpoint or not. */
-linfusion_status_t linfusion_linear_workspace_bytes(const linfusion_linear_desc_t* desc, int32_t x_packed, size_t* bytes);
+/* Pure host computation: of a forward pass (backward = 0), of a backward pass with x in 16 bits (1), with x as a checkpoint
+ * (2).  `sm_count` <= 0 means 148.  Never less than the call needs on a device with that many SMs. */
+linfusion_status_t linfusion_linear_workspace_bytes(const linfusion_linear_desc_t* desc, int32_t backward, int32_t sm_count, size_t* bytes);
 
 /* How many waits of this header's kernels expired on `device` since the library was loaded (0 in health; outputs of a call whose
  * wait expired are not to be used).  Synchronizes the stream. */

@@ -2,6 +2,7 @@
 #include "../../include/linfusion_layers.h"
 
 #include "host_checks.h"
+#include "layers_internal.h"
 #include "recurrence_kernels.cuh"
 
 using namespace lf;
@@ -329,9 +330,9 @@ linfusion_status_t linfusion_recurrence_backward(const linfusion_recurrence_desc
     else launch_backward<kBf, false>(p, packed, grid, s);
     e = cudaGetLastError();
     if (e == cudaSuccess && grads->rate != nullptr) {
-        const int blocks = plan.slabs * kRecSlab / kRecSumChannels;
-        recurrence_rate_kernel<<<blocks, kRecSumThreads, 0, s>>>(p.rate_partials, grads->rate, static_cast<long long>(d.B) * plan.tiles,
-                                                                 plan.slabs * kRecSlab, d.C);
+        const int blocks = plan.slabs * kRecSlab / kSumChannels;
+        column_sums_kernel<<<blocks, kSumThreads, 0, s>>>(p.rate_partials, grads->rate, static_cast<long long>(d.B) * plan.tiles,
+                                                          plan.slabs * kRecSlab, d.C);
         e = cudaGetLastError();
     }
     return end(e);
@@ -345,10 +346,11 @@ linfusion_status_t linfusion_layers_expired(int32_t device, uint32_t* count, voi
     CurrentDevice guard(device);
     if (!guard.ok) return LINFUSION_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    unsigned int n = 0;
-    cudaError_t e = cudaMemcpyFromSymbolAsync(&n, recurrence_expired_waits, sizeof(n), 0, cudaMemcpyDeviceToHost, s);
+    unsigned int n[2] = {0, 0};
+    cudaError_t e = cudaMemcpyFromSymbolAsync(&n[0], recurrence_expired_waits, sizeof(n[0]), 0, cudaMemcpyDeviceToHost, s);
+    if (e == cudaSuccess) e = read_linear_expired(&n[1], s);
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);
-    if (e == cudaSuccess) *count = n;
+    if (e == cudaSuccess) *count = n[0] + n[1];
     return end(e);
 }
 

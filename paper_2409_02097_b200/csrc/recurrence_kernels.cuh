@@ -15,6 +15,7 @@
 // Bound by DRAM: forward 8 bytes a value with a gate (three inputs, h), backward 14, or 11.1 from checkpoints.
 #pragma once
 
+#include "column_sums.cuh"
 #include "pack8.cuh"
 
 namespace lf {
@@ -615,31 +616,6 @@ __global__ void __launch_bounds__(256, 2) recurrence_backward_kernel(const __gri
             p.rate_partials[(static_cast<long long>(t.b) * p.tiles + tile) * (p.slabs * kRecSlab) + t.slab * kRecSlab + tid] = sum;
         }
     }
-}
-
-// Sums over the tiles of a channel: 16 channels x 64 threads a block, each thread every 64th row, then the threads in order.
-constexpr int kRecSumChannels = 16, kRecSumThreads = 1024;
-static __global__ void __launch_bounds__(kRecSumThreads) recurrence_rate_kernel(const float* __restrict__ partials, float* __restrict__ out,
-                                                                                long long rows, int width, int C)
-{
-    constexpr int lanes = kRecSumThreads / kRecSumChannels;
-    __shared__ float sums[lanes][kRecSumChannels];
-    const int c = threadIdx.x % kRecSumChannels, l = threadIdx.x / kRecSumChannels, ch = blockIdx.x * kRecSumChannels + c;
-    float a[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) a[k] = 0.0f;
-    for (long long r = l; r < rows; r += 8 * lanes)
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (r + k * lanes < rows) a[k] += partials[(r + k * lanes) * width + ch];
-    sums[l][c] = ((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7]));
-    __syncthreads();
-#pragma unroll
-    for (int n = lanes / 2; n > 0; n /= 2) {
-        if (l < n) sums[l][c] += sums[l + n][c];
-        __syncthreads();
-    }
-    if (l == 0 && ch < C) out[ch] = sums[0][c];
 }
 
 }  // namespace lf

@@ -1,7 +1,8 @@
 """ctypes binding over the C ABI in ``include/linfusion_layers.h``: a block's own layers.
 
-``pack8``            activation checkpoints in 8 bits (``Packed8``), which the backward passes below read as they are
+``Linear``           a matrix product with bias, activation and residual in its epilogue
 ``GatedRecurrence``  a gated linear recurrence over the tokens, each channel for itself
+``pack8``            activation checkpoints in 8 bits (``Packed8``), which both backward passes read as they are
 
 Argument marshalling only: the arithmetic is in the CUDA library, and there is no CPU fallback.  Objects hold a
 configuration and no device memory, so one may serve any streams and threads at once.
@@ -18,8 +19,10 @@ from .block import Rows, _Checked, _Fixed, _call, _check_rc, _check_tensor, _lik
 GROUP = 32          # channels that share a scale of a checkpoint
 STATE_EVERY = 64    # tokens from one kept state of the recurrence to the next
 
-EXPORTED = ["linfusion_pack8", "linfusion_unpack8", "linfusion_recurrence", "linfusion_recurrence_backward",
-            "linfusion_recurrence_workspace_bytes", "linfusion_layers_expired"]
+ACTIVATIONS = {"none": 0, None: 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
+
+EXPORTED = ["linfusion_linear", "linfusion_linear_backward", "linfusion_linear_workspace_bytes", "linfusion_pack8", "linfusion_unpack8",
+            "linfusion_recurrence", "linfusion_recurrence_backward", "linfusion_recurrence_workspace_bytes", "linfusion_layers_expired"]
 
 _i32, _i64, _vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
 
@@ -49,6 +52,21 @@ class RecurrenceGrads(ctypes.Structure):
     _fields_ = [("x", Rows), ("decay", Rows), ("gate", Rows), ("rate", _vp), ("h0", _vp)]
 
 
+class LinearDesc(ctypes.Structure):
+    """Mirror of ``linfusion_linear_desc_t``."""
+    _fields_ = [("M", _i32), ("K", _i32), ("N", _i32), ("act", _i32), ("w_transposed", _i32), ("flags", ctypes.c_uint32)]
+
+
+class Matrix(ctypes.Structure):
+    """Mirror of ``linfusion_matrix_t``."""
+    _fields_ = [("p", _vp), ("row", _i64)]
+
+
+class LinearSaved(ctypes.Structure):
+    """Mirror of ``linfusion_linear_saved_t``."""
+    _fields_ = [("x", Matrix), ("u", Matrix), ("x_packed", Packed8Struct), ("u_packed", Packed8Struct)]
+
+
 _lib = None
 
 
@@ -56,8 +74,11 @@ def load_library() -> ctypes.CDLL:
     global _lib
     if _lib is None:
         lib, P, size = block.load_library(), ctypes.POINTER, ctypes.c_size_t
-        rows, given = P(Rows), P(RecurrenceInput)
+        rows, given, matrix, linear = P(Rows), P(RecurrenceInput), P(Matrix), P(LinearDesc)
         for name, args in {
+                "linfusion_linear": [linear, matrix, matrix, _vp, matrix, matrix, matrix, P(Packed8Struct), _vp, size, _vp],
+                "linfusion_linear_backward": [linear, matrix, P(LinearSaved), matrix, matrix, matrix, _vp, _vp, size, _vp],
+                "linfusion_linear_workspace_bytes": [linear, _i32, _i32, P(size)],
                 "linfusion_pack8": [P(Pack8Desc), rows, P(Packed8Struct), _vp],
                 "linfusion_unpack8": [P(Pack8Desc), P(Packed8Struct), rows, _vp],
                 "linfusion_recurrence": [P(RecurrenceDesc), given, given, given, _vp, _vp, rows, _vp, _vp, _vp, size, _vp],
@@ -360,4 +381,218 @@ class GatedRecurrence(_Fixed):
                    _ptr(dlast), grads, ws.data_ptr(), ws.numel() * ws.element_size())
         if rc != OK:
             raise LinFusionError(rc, "linfusion_recurrence_backward")
+        return out
+
+
+# -------------------------------------------------------------------------------------- matrix product
+def _as_matrix(t, name, C):
+    """(rows, stride of a row) of a tensor [..., C] whose leading axes are rows evenly spaced."""
+    if t.dim() < 1 or t.shape[-1] != C:
+        raise ValueError(f"{name}: expected [..., {C}], got {tuple(t.shape)}")
+    rows, step = 1, None
+    for n, s in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if n == 1:
+            continue
+        if step is not None and s != rows * step:
+            raise ValueError(f"{name}: the rows of strides {t.stride()} are not evenly spaced")
+        if step is None:
+            step = s
+        rows *= n
+    return rows, C if step is None else step
+
+
+class Linear(_Fixed):
+    """A matrix product with its epilogue, u = x w + bias, y = act(u) + residual, from ``K`` input to ``N`` output channels (multiples
+    of 8).
+
+    x [..., K], residual and y [..., N]: 16-bit CUDA tensors whose leading axes are evenly spaced rows, a multiple of 8
+    elements apart; w [K, N] with either axis contiguous (a torch.nn.Linear's weight is given as ``weight.t()``); bias [N].
+    ``activation``: "none", "relu", "silu", "gelu" or "gelu_tanh".
+    """
+
+    def __init__(self, K: int, N: int, activation: Optional[str] = "none", dtype: str = "bf16"):
+        if activation not in ACTIVATIONS:
+            raise ValueError("activation must be 'none', 'relu', 'silu', 'gelu' or 'gelu_tanh'")
+        for name, n in (("K", K), ("N", N)):
+            if int(n) <= 0 or int(n) % 8 != 0:
+                raise ValueError(f"{name}: expected a multiple of 8, got {n}")
+        self.K, self.N, self.act, self.dtype = int(K), int(N), ACTIVATIONS[activation], dtype
+        self._torch_dtype = _torch_dtype(dtype)
+        self._flags = DTYPE_FP16 if dtype == "fp16" else 0
+        self._lib = load_library()
+        self._checked = _Checked()
+
+    def _desc(self, M, transposed=False):
+        return LinearDesc(M, self.K, self.N, self.act, transposed, self._flags)
+
+    def workspace_bytes(self, rows: int, backward: bool = False, x_packed: bool = False, transposed: bool = False, sm_count: int = 0) -> int:
+        """Bytes of workspace that ``forward`` takes for that many rows, or ``backward``, with x in 16 or 8 bits and a weight as [K, N] or, seen
+        transposed, as [N, K]."""
+        n = ctypes.c_size_t(0)
+        _check_rc(self._lib.linfusion_linear_workspace_bytes(ctypes.byref(self._desc(int(rows), bool(transposed))),
+                                                             (2 if x_packed else 1) if backward else 0, int(sm_count), ctypes.byref(n)),
+                  "linfusion_linear_workspace_bytes")
+        return int(n.value)
+
+    def _matrix(self, t, name, C, rows, device):
+        if t is None:
+            return None
+        _check_tensor(t, name, self._torch_dtype, device)
+        n, step = _as_matrix(t, name, C)
+        if n != rows:
+            raise ValueError(f"{name}: expected {rows} rows, got {n}")
+        return Matrix(None, step)
+
+    def _weight(self, t, name, device):
+        """(structure, transposed)"""
+        if tuple(t.shape) != (self.K, self.N) or t.dtype != self._torch_dtype or t.device != device:
+            raise ValueError(f"{name}: expected {self._torch_dtype} {(self.K, self.N)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        if t.stride(1) == 1:
+            return Matrix(None, t.stride(0)), False
+        if t.stride(0) == 1:
+            return Matrix(None, t.stride(1)), True
+        raise ValueError(f"{name}: one of its axes must be contiguous, got strides {t.stride()}")
+
+    def _packed(self, t, name, C, rows, device):
+        if t.shape[-1] != C or t.codes.numel() != rows * C or t.dtype != self.dtype or t.device != device:
+            raise ValueError(f"{name}: expected a {self.dtype} checkpoint of {rows} x {C} on {device}, got a {t.dtype} one of {tuple(t.shape)} on {t.device}")
+
+    @staticmethod
+    def _at(struct, t):
+        if struct is None or t is None:
+            return None
+        return Matrix(t.data_ptr(), struct.row)
+
+    def _check_forward(self, x, w, bias, residual, y, u):
+        if not x.is_cuda:
+            raise ValueError("x: expected a CUDA tensor")
+        device = x.device
+        rows, _ = _as_matrix(x, "x", self.K)
+        if rows == 0 or x.numel() == 0:
+            raise ValueError("x: no rows")
+        mx = self._matrix(x, "x", self.K, rows, device)
+        mw, transposed = self._weight(w, "w", device)
+        if bias is not None and (tuple(bias.shape) != (self.N,) or bias.dtype != self._torch_dtype or bias.device != device or not bias.is_contiguous()):
+            raise ValueError(f"bias: expected a contiguous {self._torch_dtype} tensor of {(self.N,)} on {device}")
+        shape = (*x.shape[:-1], self.N)
+        for name, t in (("residual", residual), ("y", y), ("u", u)):
+            if t is not None and tuple(t.shape) != shape:
+                raise ValueError(f"{name}: expected {shape}, got {tuple(t.shape)}")
+        mr, my = self._matrix(residual, "residual", self.N, rows, device), self._matrix(y, "y", self.N, rows, device)
+        mu = None
+        if isinstance(u, Packed8):
+            self._packed(u, "u", self.N, rows, device)
+        else:
+            mu = self._matrix(u, "u", self.N, rows, device)
+        dense = Matrix(None, self.N)
+        return (self._desc(rows, transposed), mx, mw, mr, my or dense, mu or dense, shape,
+                self.workspace_bytes(rows, transposed=transposed, sm_count=block._sm_count(device.index)))
+
+    def forward(self, x, w, bias=None, residual=None, save: Optional[str] = None, y=None, u=None, workspace=None,
+                stream: Optional[int] = None) -> Tuple:
+        """(y, u).  ``save``: what is kept of the pre-activation for ``backward``: None (u is None; enough without an activation), "full"
+        (in the storage type) or "packed" (a ``Packed8``, made from the fp32 sums).  ``y`` may be given as ``residual`` (in place).
+        ``workspace``: a CUDA tensor of at least ``workspace_bytes``, else one is allocated."""
+        import torch
+        if save not in (None, "full", "packed"):
+            raise ValueError("save must be None, 'full' or 'packed'")
+        if u is not None and (save is None or (save == "packed") != isinstance(u, Packed8)):
+            raise ValueError("u: expected a tensor with save='full', a Packed8 with save='packed'")
+        if stream is not None and x.is_cuda:
+            with allocating_on(stream, x.get_device()):
+                return self.forward(x, w, bias, residual, save, y, u, workspace)
+        key = (0, _look(x), _look(w), _look(bias), _look(residual), _look(y), _look8(u))
+        found = self._checked.get(key)
+        if found is None:
+            found = self._checked.keep(key, self._check_forward(x, w, bias, residual, y, u))
+        desc, mx, mw, mr, my, mu, shape, need = found
+        device = x.device
+        if y is None:
+            y = torch.empty(shape, dtype=self._torch_dtype, device=device)
+        packed = None
+        if save == "packed":
+            if u is None:
+                u = _new_packed(shape, self.dtype, device)
+            packed = Packed8Struct(u.codes.data_ptr(), u.scales.data_ptr())
+        elif save == "full" and u is None:
+            u = torch.empty(shape, dtype=self._torch_dtype, device=device)
+        ws = GatedRecurrence._workspace(workspace, need, device)
+        rc = _call(x.get_device(), self._lib.linfusion_linear, desc, self._at(mx, x), self._at(mw, w), _ptr(bias), self._at(mr, residual),
+                   self._at(my, y), self._at(mu, u) if save == "full" else None, packed, _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
+        if rc != OK:
+            raise LinFusionError(rc, "linfusion_linear")
+        return y, u
+
+    def _check_backward(self, dy, x, w, u, dx, dw, need):
+        if not dy.is_cuda:
+            raise ValueError("dy: expected a CUDA tensor")
+        device = dy.device
+        rows, _ = _as_matrix(dy, "dy", self.N)
+        if rows == 0 or dy.numel() == 0:
+            raise ValueError("dy: no rows")
+        mdy = self._matrix(dy, "dy", self.N, rows, device)
+        ms = {}
+        for name, t, C, wanted in (("x", x, self.K, "w" in need), ("u", u, self.N, self.act != 0)):
+            if not wanted:
+                continue
+            if t is None:
+                raise ValueError(f"{name}: needed for this backward pass")
+            if isinstance(t, Packed8):
+                self._packed(t, name, C, rows, device)
+            else:
+                ms[name] = self._matrix(t, name, C, rows, device)
+        if w is None:
+            raise ValueError("w: needed for the layout of its gradient")
+        mw, transposed = self._weight(w, "w", device)
+        if dx is not None and tuple(dx.shape) != (*dy.shape[:-1], self.K):
+            raise ValueError(f"dx: expected {(*dy.shape[:-1], self.K)}, got {tuple(dx.shape)}")
+        mdx = self._matrix(dx, "dx", self.K, rows, device) or Matrix(None, self.K)
+        mdw = Matrix(None, self.K if transposed else self.N)
+        if dw is not None:
+            mdw, other = self._weight(dw, "dw", device)
+            if other != transposed:
+                raise ValueError("dw: expected the contiguous axis of w")
+        return (self._desc(rows, transposed), mdy, ms, mw, mdx, mdw, transposed,
+                self.workspace_bytes(rows, True, isinstance(x, Packed8) and "w" in need, transposed, block._sm_count(device.index)))
+
+    def backward(self, dy, x, w, u=None, need=("x", "w", "bias"), dx=None, dw=None, workspace=None, stream: Optional[int] = None) -> Dict:
+        """Gradients by name, those in ``need``: ``x`` and ``w`` in the storage type (w's laid out as w is), ``bias`` in fp32.  The residual's is dy.
+
+        x and, with an activation, u as ``forward`` had and returned them, each in 16 bits or as a ``Packed8``.  du = dy * act'(u)
+        is rounded to 16 bits before the two products; the bias' gradient sums it unrounded."""
+        import torch
+        need = tuple(need)
+        if not need or any(n not in ("x", "w", "bias") for n in need):
+            raise ValueError("need: some of 'x', 'w' and 'bias'")
+        if (dx is not None and "x" not in need) or (dw is not None and "w" not in need):
+            raise ValueError("dx and dw: only where they are needed")
+        if stream is not None and dy.is_cuda:
+            with allocating_on(stream, dy.get_device()):
+                return self.backward(dy, x, w, u, need, dx, dw, workspace)
+        key = (1, _look(dy), _look8(x), _look(w), _look8(u), _look(dx), _look(dw), need)
+        found = self._checked.get(key)
+        if found is None:
+            found = self._checked.keep(key, self._check_backward(dy, x, w, u, dx, dw, need))
+        desc, mdy, ms, mw, mdx, mdw, transposed, size = found
+        device, out = dy.device, {}
+        if "x" in need:
+            out["x"] = dx if dx is not None else torch.empty((*dy.shape[:-1], self.K), dtype=self._torch_dtype, device=device)
+        if "w" in need:
+            if dw is None:
+                dw = torch.empty((self.N, self.K) if transposed else (self.K, self.N), dtype=self._torch_dtype, device=device)
+                dw = dw.t() if transposed else dw
+            out["w"] = dw
+        if "bias" in need:
+            out["bias"] = torch.empty(self.N, dtype=torch.float32, device=device)
+        saved = LinearSaved()
+        for name, t, wanted in (("x", x, "w" in need), ("u", u, self.act != 0)):
+            if wanted and isinstance(t, Packed8):
+                setattr(saved, name + "_packed", Packed8Struct(t.codes.data_ptr(), t.scales.data_ptr()))
+            elif wanted:
+                setattr(saved, name, self._at(ms[name], t))
+        ws = GatedRecurrence._workspace(workspace, size, device)
+        rc = _call(dy.get_device(), self._lib.linfusion_linear_backward, desc, self._at(mdy, dy), saved, self._at(mw, w), self._at(mdx, out.get("x")),
+                   self._at(mdw, out.get("w")), _ptr(out.get("bias")), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
+        if rc != OK:
+            raise LinFusionError(rc, "linfusion_linear_backward")
         return out
