@@ -22,12 +22,16 @@ struct Product {
     size_t partials, flags;       // bytes of workspace
 };
 
-// Estimated cycles.  A chunk (64 of K) of a tile takes what its matrix instructions or their operands' way through shared memory
-// take; a tile's last epilogue, and the joining of cut tiles, come on top.
+// Estimated cycles.  A chunk (64 of K) of a tile takes what its matrix instructions or its operands' way into shared memory take; a
+// round of tiles comes with a gap of its own, and joining cut tiles with the way of their sums through memory.  From the times of
+// twenty sizes with each of the four shapes, whole and cut (us): 8192 x 5120 x 1280 (M x K x N) 86 whole and 76 cut with 256 x 256
+// tiles, 82 and 79 with 256 x 128, 95 with 128 x 128; 8192 x 1280 x 1280 30, 32, 28, 32, 31; 1024 x 1280 x 1280 11.5, 18.7, 8.1,
+// 12.1, 7.7 and 9.9 with 128 x 64; 128 x 1280 x 1280 11, 17, 7.3, 12, 7.2, 6.3; 640 x 32768 x 2560 152, 107, 104, 101, 133, 222.
 struct Shape {
-    int cg, bn, chunk, tail;
+    int cg, bn, chunk, join;
 };
-constexpr Shape kShapes[] = {{2, 256, 530, 3600}, {2, 128, 290, 2800}, {1, 128, 300, 2800}, {1, 64, 220, 2200}};
+constexpr Shape kShapes[] = {{2, 256, 560, 13000}, {2, 128, 350, 9000}, {1, 128, 370, 9000}, {1, 64, 330, 8000}};
+constexpr int kRoundGap = 900;
 
 Product plan_product(int M, int N, int K, int sms)
 {
@@ -46,15 +50,15 @@ Product plan_product(int M, int N, int K, int sms)
         const int most = sms / s.cg > 0 ? sms / s.cg : 1;
         // all tiles whole
         const long long rounds = (tiles + most - 1) / most;
-        double cost = static_cast<double>(rounds) * p.chunks * s.chunk + s.tail;
+        double cost = static_cast<double>(rounds) * (p.chunks * s.chunk + kRoundGap);
         p.pairs = static_cast<int>(tiles < most ? tiles : most);
         p.whole = p.tiles;
         // or the last rounds cut: at least four chunks for each pair, and at least one round (where there is one) goes with the rest
         const long long full = tiles / most > 1 ? (tiles / most - 1) * most : 0, units = (tiles - full) * p.chunks;
         const long long pairs = units / 4 < most ? (units / 4 > 0 ? units / 4 : 1) : most;
-        if (tiles % most != 0 && pairs > 1 && (full == 0 || pairs == most)) {
+        if (tiles % most != 0 && pairs > 1 && (full == 0 || pairs == most) && units <= INT32_MAX / 2) {
             const double per = static_cast<double>((units + pairs - 1) / pairs), helpers = p.chunks / (per < p.chunks ? per : p.chunks);
-            const double cut = (static_cast<double>(full / most) * p.chunks + per) * s.chunk + s.tail + 4000 + helpers * s.bn * 8;
+            const double cut = static_cast<double>(full / most) * (p.chunks * s.chunk + kRoundGap) + per * s.chunk + kRoundGap + s.join + helpers * s.bn * 8;
             if (cut < cost) {
                 cost = cut;
                 p.pairs = static_cast<int>(pairs);
@@ -63,7 +67,7 @@ Product plan_product(int M, int N, int K, int sms)
         }
         if (p.whole < p.tiles) {
             p.partials = static_cast<size_t>(p.pairs) * p.cg * (p.bn / 4) * kLinRows * sizeof(float4);
-            p.flags = align_up_256(static_cast<size_t>(p.pairs) * p.cg * sizeof(uint32_t));
+            p.flags = align_up_256(static_cast<size_t>(p.pairs) * p.cg * (p.bn / kLinColumns) * sizeof(unsigned long long));
         }
         if (cost < least) {
             least = cost;
@@ -91,17 +95,17 @@ Sums plan_sums(int M, int N, int sms)
     return s;
 }
 
-// The parts of a call's workspace.  Flags first: they are cleared in one go.
+// The parts of a call's workspace.
 struct Workspace {
     Product forward, dx, dw;
     Sums sums;
-    size_t flags_dw, partials, du, x, column_sums, zeroed, bytes;
+    size_t flags_dw, partials, du, x, column_sums, bytes;
 };
 Workspace plan_forward(const linfusion_linear_desc_t& d, int sms)
 {
     Workspace w = {};
     w.forward = plan_product(d.M, d.N, d.K, sms);
-    w.zeroed = w.partials = w.forward.flags;
+    w.partials = w.forward.flags;
     w.bytes = w.partials + w.forward.partials;
     return w;
 }
@@ -112,7 +116,7 @@ Workspace plan_backward(const linfusion_linear_desc_t& d, bool x_packed, int sms
     w.dw = d.w_transposed ? plan_product(d.N, d.K, d.M, sms) : plan_product(d.K, d.N, d.M, sms);
     w.sums = plan_sums(d.M, d.N, sms);
     w.flags_dw = w.dx.flags;
-    w.zeroed = w.partials = w.flags_dw + w.dw.flags;
+    w.partials = w.flags_dw + w.dw.flags;
     w.du = w.partials + std::max(w.dx.partials, w.dw.partials);  // one product after the other
     w.x = w.du + (d.act != LINFUSION_ACT_NONE ? align_up_256(static_cast<size_t>(d.M) * d.N * 2) : 0);
     w.column_sums = w.x + (x_packed ? align_up_256(static_cast<size_t>(d.M) * d.K * 2) : 0);
@@ -161,9 +165,9 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// Boxes of 64 values x `box_rows` of a matrix of 16-bit values, in the 128-byte swizzle.  What lies outside is read as zero and not
-// written.
-bool encode(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t row, int box_rows)
+// Boxes of 64 values x `box_rows` of a matrix of 16-bit values in the 128-byte swizzle, or of bytes in that of 64 bytes.  What lies
+// outside is read as zero and not written.
+bool encode(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t row, int box_rows, bool bytes = false)
 {
     static std::atomic<EncodeTiledFn> known{nullptr};
     EncodeTiledFn fn = known.load(std::memory_order_acquire);
@@ -174,10 +178,10 @@ bool encode(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int6
         fn = reinterpret_cast<EncodeTiledFn>(p);
         known.store(fn, std::memory_order_release);
     }
-    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)}, strides[1] = {static_cast<cuuint64_t>(row) * 2};
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)}, strides[1] = {static_cast<cuuint64_t>(row) * (bytes ? 1 : 2)};
     const cuuint32_t box[2] = {64u, static_cast<cuuint32_t>(box_rows)}, step[2] = {1u, 1u};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return fn(map, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, step,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, bytes ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // An operand: `mn` rows or columns of D by K values, contiguous along K or along mn.
@@ -209,28 +213,40 @@ cudaError_t launch(const CUtensorMap (&maps)[5], const LinParams& p, int pairs, 
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(pairs * CG);
-    cfg.blockDim = dim3(kLinThreads);
+    cfg.blockDim = dim3(C::THREADS);
     cfg.dynamicSmemBytes = C::SMEM;
     cfg.stream = s;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = CG;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, linear_kernel<KIND, CG, BN>, maps[0], maps[1], maps[2], maps[3], maps[4], p);
 }
 
-// D[M, N] = A B with its epilogue.  flags: cleared.
+// A mark for the flags of one call: a different one each time, and unlikely to be what memory holds by chance.
+unsigned long long next_mark()
+{
+    static std::atomic<unsigned long long> calls{0x9E3779B97F4A7C15ull};
+    return calls.fetch_add(0xD1342543DE82EF95ull, std::memory_order_relaxed) | 1ull;
+}
+
+// D[M, N] = A B with its epilogue.
 linfusion_status_t product(const Product& plan, int M, int N, int K, const Operand& a, const Operand& b, const linfusion_matrix_t& y,
                            const Epilogue& ep, bool half, void* flags, void* partials, int device, cudaStream_t s)
 {
     CUtensorMap maps[5];
-    bool ok = encode_operand(&maps[0], a, M, K, kLinRows) && encode_operand(&maps[1], b, N, K, plan.bn / plan.cg) &&
+    const int a_rows = M >= kLinRows ? kLinRows : (M + 7) / 8 * 8;
+    bool ok = encode_operand(&maps[0], a, M, K, a_rows) && encode_operand(&maps[1], b, N, K, plan.bn / plan.cg) &&
               encode(&maps[2], y.p, M, N, row_of(y, M, N), kLinRows);
     maps[3] = maps[4] = maps[2];
     if (ok && ep.residual != nullptr) ok = encode(&maps[3], ep.residual->p, M, N, row_of(*ep.residual, M, N), kLinRows);
     if (ok && ep.u != nullptr) ok = encode(&maps[4], ep.u->p, M, N, row_of(*ep.u, M, N), kLinRows);
+    const bool codes_map = ep.u_packed != nullptr && N % 16 == 0;
+    if (ok && codes_map) ok = encode(&maps[4], ep.u_packed->codes, M, N, N, kLinRows, true);
     if (!ok) return LINFUSION_ERR_CUDA;
     LinParams p = {};
     p.M = M;
@@ -249,9 +265,12 @@ linfusion_status_t product(const Product& plan, int M, int N, int K, const Opera
         p.codes = static_cast<signed char*>(ep.u_packed->codes);
         p.scales = static_cast<unsigned char*>(ep.u_packed->scales);
         p.scale_groups = scale_groups(N);
+        p.codes_map = codes_map;
     }
+    p.a_rows = a_rows;
     p.partials = static_cast<float4*>(partials);
-    p.flags = static_cast<uint32_t*>(flags);
+    p.flags = static_cast<unsigned long long*>(flags);
+    p.mark = next_mark();
     cudaError_t e = cudaErrorInvalidValue;
 #define LF_PRODUCT(CG, BN) \
     if (plan.cg == CG && plan.bn == BN) e = half ? launch<kHf, CG, BN>(maps, p, plan.pairs, device, s) : launch<kBf, CG, BN>(maps, p, plan.pairs, device, s)
@@ -350,10 +369,6 @@ linfusion_status_t linfusion_linear(const linfusion_linear_desc_t* desc, const l
     if (at.st != LINFUSION_OK) return at.st;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     char* ws = static_cast<char*>(workspace);
-    if (plan.zeroed != 0) {
-        const cudaError_t err = cudaMemsetAsync(ws, 0, plan.zeroed, s);
-        if (err != cudaSuccess) return end(err);
-    }
     Epilogue ep;
     ep.act = d.act;
     ep.bias = bias;
@@ -451,10 +466,6 @@ linfusion_status_t linfusion_linear_backward(const linfusion_linear_desc_t* desc
         }
         if (err != cudaSuccess) return end(err);
         if (act) du = {ws + plan.du, d.N};
-    }
-    if (plan.zeroed != 0) {
-        const cudaError_t err = cudaMemsetAsync(ws, 0, plan.zeroed, s);
-        if (err != cudaSuccess) return end(err);
     }
     const int64_t du_row = row_of(du, d.M, d.N);
     if (dx != nullptr) {

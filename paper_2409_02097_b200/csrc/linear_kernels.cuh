@@ -4,14 +4,20 @@
 //
 // A tile is 256 x BN and belongs to a pair of CTAs on two SMs (cta_group::2: each holds 128 rows of A and of D and half of B, so a
 // value of B is read from shared memory once for two SMs), or 128 x BN and one CTA.  Roles in a CTA: a TMA warp, an MMA warp (one
-// thread, in the first CTA of a pair), and two groups of four epilogue warps that share a tile's columns; the accumulator is
-// double-buffered in tensor memory, so a tile's epilogue runs under the next tile's products.
+// thread, in the first CTA of a pair), and a group of four epilogue warps for every 64 columns of a tile; the accumulator is
+// double-buffered in tensor memory, so a tile's epilogue runs under the next tile's products.  An epilogue has about 20 issue slots a value
+// (K = 640): its arithmetic runs on pairs of fp32 values, an instruction for two.
 //
 // Every SM is busy for the same time whatever the number of tiles: as many tiles as make whole rounds of the machine are dealt out whole,
 // the K axes of the others are laid end to end and cut into equal runs, one for each pair.  A run that ends inside a tile
 // leaves its fp32 sums in the workspace; the pair whose run has the tile's end adds them in the order of K (a fixed order)
-// before its epilogue.  A pair does that unfinished tile first and the tiles that it completes last, and waits only for pairs
-// before it, which were scheduled no later: waits are short, and bounded.
+// before its epilogue.  A pair does that unfinished tile first, then the tiles that it completes, then the whole ones (under whose
+// products the joining disappears), and waits only for pairs before it, which were scheduled no later: waits are short, and
+// bounded.
+//
+// What bounds it: an SM takes in about 64 bytes a cycle, 256 rows of 128 bytes a chunk in 512 cycles, which is also what the matrix
+// instructions of a 256 x 256 tile take.  Narrower tiles load nearly as much for half the products; they serve where there
+// are few tiles.
 #pragma once
 
 #include "block_kernels.cuh"
@@ -24,10 +30,7 @@ static __device__ unsigned int linear_expired_waits;
 
 constexpr int kLinKc = 64;           // K of a stage: 128 bytes of a row
 constexpr int kLinRows = 128;        // rows of A and D in a CTA
-constexpr int kLinEpilogueWarps = 8;
-constexpr int kLinTmaWarp = kLinEpilogueWarps, kLinMmaWarp = kLinTmaWarp + 1;
-constexpr int kLinThreads = 32 * (kLinEpilogueWarps + 2);
-constexpr int kLinChunk = 64;        // columns of D that are staged at a time: 128 bytes of a row
+constexpr int kLinColumns = 64;      // columns of D of an epilogue group: 128 bytes of a row
 constexpr int kLinStaging = kLinRows * 128;
 
 enum : int { kUNone = 0, kUFull = 1, kUPacked = 2 };
@@ -36,10 +39,16 @@ template <int CG, int BN>
 struct LinCfg {
     static constexpr int A_BYTES = kLinRows * 128;
     static constexpr int B_BYTES = BN / CG * 128;
+    static_assert(BN / CG == 64 || BN / CG == 128, "one or two blocks of 64 of B in a CTA");
     static constexpr int STAGE = A_BYTES + B_BYTES;
-    static constexpr int STAGES = (224 * 1024 - 4 * kLinStaging) / STAGE > 8 ? 8 : (224 * 1024 - 4 * kLinStaging) / STAGE;
+    static constexpr int GROUPS = BN / kLinColumns;
+    static constexpr int STAGES = (224 * 1024 - GROUPS * kLinStaging) / STAGE > 8 ? 8 : (224 * 1024 - GROUPS * kLinStaging) / STAGE;
     static constexpr int TMEM_COLS = 2 * BN;
-    static constexpr int SMEM = STAGES * STAGE + 4 * kLinStaging + 1024 + 512;
+    static constexpr int EPILOGUE_WARPS = 4 * GROUPS, TMA_WARP = EPILOGUE_WARPS, MMA_WARP = TMA_WARP + 1;
+    static constexpr int THREADS = 32 * (EPILOGUE_WARPS + 2);
+    static constexpr int BIAS = BN * 4;  // the tile's bias in fp32
+    static constexpr int SMEM = STAGES * STAGE + GROUPS * kLinStaging + BIAS + 1024 + 512;
+    static_assert(SMEM <= 227 * 1024 && 16 * STAGES + 8 * (4 + GROUPS) + 4 <= 512, "shared memory of a CTA; barriers");
 };
 
 struct LinParams {
@@ -49,11 +58,13 @@ struct LinParams {
     int a_mn, b_mn;              // an operand's contiguous axis is M / N, not K
     int act, u_mode, has_residual;
     const char* bias;            // 16-bit [N] or null
-    signed char* codes;          // u in 8 bits
+    signed char* codes;          // u in 8 bits; codes_map: through map_u (rows of whole 16-byte pieces)
     unsigned char* scales;
-    int scale_groups;
+    int scale_groups, codes_map;
+    int a_rows;                  // rows of A's boxes where K is contiguous: fewer than 128 where there are fewer
     float4* partials;            // [CTA][column / 4][row]
-    uint32_t* flags;             // [CTA], zero when the kernel starts
+    unsigned long long* flags;   // [CTA][group]: `mark` while the CTA's sums wait to be fetched, anything else before and after
+    unsigned long long mark;     // another for every call; replays of a captured one find their flags taken down again
 };
 
 __device__ __forceinline__ uint32_t cluster_rank()
@@ -155,7 +166,18 @@ __device__ __forceinline__ bool lin_all(int id, int threads, bool ok)
         : "memory");
     return r != 0u;
 }
+// True in one lane of a converged warp.  A branch on this, unlike one on the lane's number, tells the compiler that one thread is behind
+// it: the TMA loop took 420 cycles a chunk with `lane == 0`, and set the pace of everything.
+__device__ __forceinline__ bool lin_elect()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0u;
+}
 __device__ __forceinline__ void lin_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
+// How many blocks of 64 of an operand's `most` rows (or columns) begin inside, where `left` are left.
+__device__ __forceinline__ int lin_blocks(int left, int most) { return left <= 0 ? 0 : left >= most ? most / 64 : (left + 63) / 64; }
 
 // ------------------------------------------------------------------------------------------ the tiles of a pair
 struct LinItem {
@@ -164,58 +186,55 @@ struct LinItem {
     int helpers;          // pairs [helpers, own) have left sums of this tile; own: none have
 };
 struct LinSchedule {
-    int pair, pairs, chunks, whole, tiles;
-    long long units, u0, u1;   // of the tiles that are cut: all, and this pair's run
-    int at;                    // next whole tile; -1: the unfinished tile first
-    long long u;               // next unit of the tiles that this pair completes
+    int pair, pairs, chunks, whole;
+    int units, u0, u1;   // of the tiles that are cut: all (fewer than 2^31), and this pair's run
+    int at;              // next whole tile; -1: the unfinished tile first
+    int u;               // next unit of the tiles that this pair completes
 
-    __device__ __forceinline__ LinSchedule(const LinParams& p, int pair_, int pairs_)
-        : pair(pair_), pairs(pairs_), chunks(p.chunks), whole(p.whole), tiles(p.tiles)
+    __device__ __forceinline__ LinSchedule(const LinParams& p, int pair_, int pairs_) : pair(pair_), pairs(pairs_), chunks(p.chunks), whole(p.whole)
     {
-        units = static_cast<long long>(tiles - whole) * chunks;
-        u0 = units * pair / pairs;
-        u1 = units * (pair + 1) / pairs;
-        at = -1;
+        units = (p.tiles - whole) * chunks;
+        u0 = start(pair);
+        u1 = start(pair + 1);
+        at = units != 0 ? -1 : pair;
         u = u0;
     }
+    __device__ __forceinline__ int start(int pair_) const { return static_cast<int>(static_cast<long long>(units) * pair_ / pairs); }
     __device__ __forceinline__ bool next(LinItem* it)
     {
+        it->helpers = pair;
         if (at < 0) {
             at = pair;
-            const long long tile = u1 / chunks, first = tile * chunks;
+            const int tile = u1 / chunks, first = tile * chunks;
             if (u1 > first && u1 > u0) {
-                it->tile = whole + static_cast<int>(tile);
-                it->k0 = static_cast<int>((u0 > first ? u0 : first) - first);
-                it->k1 = static_cast<int>(u1 - first);
+                it->tile = whole + tile;
+                it->k0 = (u0 > first ? u0 : first) - first;
+                it->k1 = u1 - first;
                 it->partial = true;
-                it->helpers = pair;
                 return true;
             }
         }
-        if (at < whole) {
-            it->tile = at;
-            it->k0 = 0;
-            it->k1 = chunks;
-            it->partial = false;
-            it->helpers = pair;
-            at += pairs;
-            return true;
-        }
-        const long long tile = u / chunks, last = (tile + 1) * chunks;
-        if (u >= u1 || last > u1) return false;
-        it->tile = whole + static_cast<int>(tile);
-        it->k0 = static_cast<int>(u - tile * chunks);
-        it->k1 = chunks;
         it->partial = false;
-        it->helpers = pair;
-        if (it->k0 != 0) {
-            // the first pair whose run passes the tile's first unit
-            const long long first = tile * chunks;
-            long long q = first * pairs / units;
-            while (units * (q + 1) / pairs <= first) ++q;
-            it->helpers = static_cast<int>(q);
+        it->k1 = chunks;
+        if (u < u1) {
+            const int tile = u / chunks, first = tile * chunks;
+            if (first + chunks <= u1) {
+                it->tile = whole + tile;
+                it->k0 = u - first;
+                if (it->k0 != 0) {  // the first pair whose run passes the tile's first unit
+                    int q = static_cast<int>(static_cast<long long>(first) * pairs / units);
+                    while (start(q + 1) <= first) ++q;
+                    it->helpers = q;
+                }
+                u = first + chunks;
+                return true;
+            }
+            u = u1;
         }
-        u = last;
+        if (at >= whole) return false;
+        it->tile = at;
+        it->k0 = 0;
+        at += pairs;
         return true;
     }
 };
@@ -248,11 +267,6 @@ __device__ __forceinline__ float lin_act(float u)
 {
     if (ACT == 1) return u < 0.0f ? 0.0f : u;  // a NaN stays one
     if (ACT == 2) return u * lin_sigmoid(u);
-    if (ACT == 3) {
-        float bell;
-        const float tail = lin_normal_tail(u, &bell);
-        return u * (u < 0.0f ? tail : 1.0f - tail);
-    }
     if (ACT == 4) return u * lin_sigmoid(2.0f * kLinTanhScale * fmaf(kLinTanhCube * u * u, u, u));
     return u;
 }
@@ -275,16 +289,45 @@ __device__ __forceinline__ float lin_act_slope(float u)
     }
     return 1.0f;
 }
+// The activation of 32 values in place, two at a time.
 template <int ACT>
-__device__ __forceinline__ void lin_act_all(float (&v)[32])
+__device__ __forceinline__ void lin_act_all(f32x2 (&v)[16])
 {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = lin_act<ACT>(v[i]);
+    for (int i = 0; i < 16; ++i) {
+        const float2 u = unpack2(v[i]);
+        if constexpr (ACT == 3) {
+            // u Phi(u) = max(u, 0) - |u| Phi(-|u|), with formula 7.1.28 of Abramowitz and Stegun, Handbook of Mathematical
+            // Functions: erfc(x) = (1 + a1 x + ... + a6 x^6)^-16, off by at most 3e-7; x = |u| / sqrt 2 is in the coefficients.  One
+            // reciprocal a value and no exponential.  Beyond 30 the power is infinite and the tail zero.
+            constexpr float r = 0.70710678118654752f;
+            constexpr float b1 = 0.0705230784f * r, b2 = 0.0422820123f * r * r, b3 = 0.0092705272f * r * r * r, b4 = 0.0001520143f * r * r * r * r,
+                            b5 = 0.0002765672f * r * r * r * r * r, b6 = 0.0000430638f * r * r * r * r * r * r;
+            const f32x2 a = pack2(fminf(fabsf(u.x), 30.0f), fminf(fabsf(u.y), 30.0f));
+            f32x2 s = fma2(a, both(b6), both(b5));
+            s = fma2(a, s, both(b4));
+            s = fma2(a, s, both(b3));
+            s = fma2(a, s, both(b2));
+            s = fma2(a, s, both(b1));
+            s = fma2(a, s, both(1.0f));
+            s = mul2(s, s);
+            s = mul2(s, s);
+            s = mul2(s, s);
+            s = mul2(s, s);
+            const float2 q = unpack2(s);
+            float p0, p1;  // a NaN stays one
+            asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(p0) : "f"(u.x));
+            asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(p1) : "f"(u.y));
+            v[i] = fma2(mul2(a, both(-0.5f)), pack2(lin_rcp(q.x), lin_rcp(q.y)), pack2(p0, p1));
+        } else {
+            v[i] = pack2(lin_act<ACT>(u.x), lin_act<ACT>(u.y));
+        }
+    }
 }
 
 // ------------------------------------------------------------------------------------------ the product
 template <int KIND, int CG, int BN>
-__global__ void __launch_bounds__(kLinThreads, 1)
+__global__ void __launch_bounds__(LinCfg<CG, BN>::THREADS, 1)
 linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_y,
               const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_u, const __grid_constant__ LinParams p)
 {
@@ -292,11 +335,16 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
     extern __shared__ unsigned char smem_raw[];
     // the same place in both CTAs of a pair: descriptors and commits address both by one offset
     const uint32_t raw = smem_u32(smem_raw), stages = (raw + 1023u) & ~1023u, staging = stages + C::STAGES * C::STAGE;
-    const uint32_t bars = staging + 4 * kLinStaging;
+    const uint32_t bias_at = staging + C::GROUPS * kLinStaging, bars = bias_at + C::BIAS;
     const uint32_t full = bars, empty = full + 8 * C::STAGES, acc_full = empty + 8 * C::STAGES, acc_empty = acc_full + 16, res_full = acc_empty + 16;
     uint32_t* slot = reinterpret_cast<uint32_t*>(smem_raw + (res_full + 32 - raw));
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (warp == C::TMA_WARP && lane == 0) {
+        prefetch_tmap(&map_a);
+        prefetch_tmap(&map_b);
+        prefetch_tmap(&map_y);
+    }
     const int rank = CG == 2 ? static_cast<int>(cluster_rank()) : 0;
     const int pair = blockIdx.x / CG, pairs = gridDim.x / CG;
     if (tid == 0) {
@@ -307,9 +355,9 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
         }
         for (int b = 0; b < 2; ++b) {
             init(acc_full + 8 * b, 1);
-            init(acc_empty + 8 * b, CG * kLinEpilogueWarps);
+            init(acc_empty + 8 * b, CG * C::EPILOGUE_WARPS);
         }
-        for (int b = 0; b < 4; ++b) init(res_full + 8 * b, 1);
+        for (int b = 0; b < C::GROUPS; ++b) init(res_full + 8 * b, 1);
         mbar_fence_init();
     }
     if (warp == 0) lin_tmem_alloc<CG>(slot, C::TMEM_COLS);
@@ -319,12 +367,12 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
     tc_fence_after_sync();
     const uint32_t tmem = *slot;
     LinSchedule todo(p, pair, pairs);
+    pdl_launch_dependents();
+    pdl_wait();
     LinItem it;
 
-    if (warp == kLinTmaWarp) {
-        if (lane == 0) {
-            prefetch_tmap(&map_a);
-            prefetch_tmap(&map_b);
+    if (warp == C::TMA_WARP) {
+        if (lin_elect()) {
             const uint32_t lead = CG == 2 ? lin_map(full, 0) : full;
             int s = 0;
             uint32_t phase = 0;
@@ -332,24 +380,26 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
             bool ok = true;
             while (ok && todo.next(&it)) {
                 const int m0 = (it.tile / p.tiles_n) * (CG * kLinRows) + rank * kLinRows, n0 = (it.tile % p.tiles_n) * BN + rank * (BN / CG);
+                // blocks of 64 rows or columns that lie outside are not loaded: nothing of what they would give is kept
+                const int a_blocks = p.a_mn ? lin_blocks(p.M - m0, kLinRows) : 0, b_blocks = p.b_mn ? lin_blocks(p.N - n0, BN / CG) : 0;
+                uint32_t bytes = 0;  // of the pair
+                if (rank == 0)
+#pragma unroll
+                    for (int c = 0; c < CG; ++c)
+                        bytes += (p.a_mn ? lin_blocks(p.M - m0 - c * kLinRows, kLinRows) * 8192 : p.a_rows * 128) +
+                                 (p.b_mn ? lin_blocks(p.N - n0 - c * (BN / CG), BN / CG) * 8192 : C::B_BYTES);
                 for (int k = it.k0; k < it.k1; ++k) {
                     ok = lin_wait(empty + 8 * s, phase ^ 1u);
                     if (!ok) break;
                     // all bytes of the pair are counted on the first CTA's barrier
-                    if (rank == 0) lin_expect(full + 8 * s, CG * C::STAGE);
+                    if (rank == 0) lin_expect(full + 8 * s, bytes);
                     const uint32_t a = stages + s * C::STAGE, b = a + C::A_BYTES, bar = lead + 8 * s;
-                    if (p.a_mn) {
-#pragma unroll
-                        for (int i = 0; i < kLinRows / 64; ++i) lin_load<CG>(a + i * 8192, &map_a, m0 + 64 * i, k * kLinKc, bar);
-                    } else {
-                        lin_load<CG>(a, &map_a, k * kLinKc, m0, bar);
-                    }
-                    if (p.b_mn) {
-#pragma unroll
-                        for (int i = 0; i < BN / CG / 64; ++i) lin_load<CG>(b + i * 8192, &map_b, n0 + 64 * i, k * kLinKc, bar);
-                    } else {
-                        lin_load<CG>(b, &map_b, k * kLinKc, n0, bar);
-                    }
+                    if (!p.a_mn) lin_load<CG>(a, &map_a, k * kLinKc, m0, bar);
+                    if (a_blocks > 0) lin_load<CG>(a, &map_a, m0, k * kLinKc, bar);
+                    if (a_blocks > 1) lin_load<CG>(a + 8192, &map_a, m0 + 64, k * kLinKc, bar);
+                    if (!p.b_mn) lin_load<CG>(b, &map_b, k * kLinKc, n0, bar);
+                    if (b_blocks > 0) lin_load<CG>(b, &map_b, n0, k * kLinKc, bar);
+                    if (BN / CG > 64 && b_blocks > 1) lin_load<CG>(b + 8192, &map_b, n0 + 64, k * kLinKc, bar);
                     ++issued;
                     if (++s == C::STAGES) {
                         s = 0;
@@ -365,8 +415,8 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                         if (!lin_wait(full + 8 * static_cast<uint32_t>(i % C::STAGES), static_cast<uint32_t>(i / C::STAGES) & 1u)) break;
             }
         }
-    } else if (warp == kLinMmaWarp) {
-        if (lane == 0 && rank == 0) {
+    } else if (warp == C::MMA_WARP) {
+        if (rank == 0 && lin_elect()) {
             const uint32_t idesc = umma_idesc_f32acc(kind_dtype(KIND), CG * kLinRows, BN, (p.a_mn ? kUmmaAMnMajor : 0u) | (p.b_mn ? kUmmaBMnMajor : 0u));
             const uint64_t a0 = p.a_mn ? umma_desc_mnmajor_sw128(stages, 8192, 1024) : umma_desc_kmajor_sw128(stages);
             const uint64_t b0 = p.b_mn ? umma_desc_mnmajor_sw128(stages + C::A_BYTES, 8192, 1024) : umma_desc_kmajor_sw128(stages + C::A_BYTES);
@@ -384,10 +434,10 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                     ok = lin_wait(full + 8 * s, phase);
                     if (!ok) break;
                     tc_fence_after_sync();
-                    const uint64_t at = static_cast<uint64_t>(s * (C::STAGE >> 4));
+                    const uint64_t a = a0 + static_cast<uint64_t>(s * (C::STAGE >> 4)), b = b0 + static_cast<uint64_t>(s * (C::STAGE >> 4));
+                    lin_mma<CG>(d, a, b, idesc, k > it.k0 ? 1u : 0u);
 #pragma unroll
-                    for (int i = 0; i < kLinKc / 16; ++i)
-                        lin_mma<CG>(d, a0 + at + i * a_step, b0 + at + i * b_step, idesc, k > it.k0 || i > 0 ? 1u : 0u);
+                    for (int i = 1; i < kLinKc / 16; ++i) lin_mma<CG>(d, a + i * a_step, b + i * b_step, idesc, 1u);
                     lin_commit<CG>(empty + 8 * s);
                     if (++s == C::STAGES) {
                         s = 0;
@@ -399,176 +449,203 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
             if (!ok) atomicAdd(&linear_expired_waits, 1u);
         }
     } else {
-        const int group = warp >> 2, row = (warp & 3) * 32 + lane;
-        const bool chief = (tid & 127) == 0;
-        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-        const uint32_t stage0 = staging + group * 2 * kLinStaging, res0 = res_full + 16 * group;
+        const int group = warp >> 2, row = (warp & 3) * 32 + lane, in_group = tid & 127;
+        const bool chief = in_group == 0;
+        const uint32_t buffer = staging + group * kLinStaging, res_bar = res_full + 8 * group;
+        const uint32_t acc = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + group * kLinColumns;
         const uint32_t acc_free = CG == 2 ? lin_map(acc_empty, 0) : acc_empty;
-        constexpr int kChunks = BN / kLinChunk;   // of a tile, taken in turn by the groups
-        const bool one_buffer = p.u_mode == kUFull;  // the other is for u
-        uint32_t res_phase[2] = {0u, 0u};
-        int turn = 0;     // the buffer of the next chunk
+        uint32_t res_phase = 0u;
         // Once a wait has expired none is begun any more, but every barrier is met, so that all of the CTA's threads come to the end.
         bool good = true;
         for (int n = 0; todo.next(&it); ++n) {
             const int buf = n & 1;
-            const int m0 = (it.tile / p.tiles_n) * (CG * kLinRows) + rank * kLinRows, n0 = (it.tile % p.tiles_n) * BN;
-            const bool residual = p.has_residual && !it.partial;
-            // the residual comes into the buffers that y will leave from, while the products run
-            if (residual && chief) {
+            const int m0 = (it.tile / p.tiles_n) * (CG * kLinRows) + rank * kLinRows, col0 = (it.tile % p.tiles_n) * BN + group * kLinColumns;
+            const bool residual = p.has_residual && !it.partial, inside = m0 < p.M && col0 < p.N;
+            const uint32_t bias = bias_at + group * kLinColumns * 4;
+            // the buffer has to be free; the residual comes into it while the products run
+            if (chief) {
                 tma_store_wait_read();
-                for (int i = 0; i < (one_buffer ? 1 : 2); ++i) {
-                    const int c = group + 2 * i, b = one_buffer ? 0 : turn ^ i;
-                    if (c < kChunks) {
-                        lin_expect(res0 + 8 * b, kLinStaging);
-                        lin_load<1>(stage0 + b * kLinStaging, &map_r, n0 + c * kLinChunk, m0, res0 + 8 * b);
-                    }
+                if (residual) {
+                    lin_expect(res_bar, kLinStaging);
+                    lin_load<1>(buffer, &map_r, col0, m0, res_bar);
                 }
+            }
+            if (in_group < kLinColumns) {
+                const int col = col0 + in_group;
+                float b = 0.0f;
+                if (p.bias != nullptr && col < p.N) b = pair_lo<KIND>(__ldg(reinterpret_cast<const unsigned short*>(p.bias) + col));
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(bias + 4 * in_group), "f"(b) : "memory");
             }
             good = good && lin_wait(acc_full + 8 * buf, (n >> 1) & 1);
-            if (good && it.helpers < pair && tid == 0)
+            if (good && it.helpers < pair && chief)
                 for (int q = it.helpers; q < pair && good; ++q) {
-                    const uint32_t* flag = p.flags + q * CG + rank;
+                    unsigned long long* flag = p.flags + (q * CG + rank) * C::GROUPS + group;
                     const unsigned long long t0 = global_timer_ns();
-                    uint32_t there;
+                    unsigned long long there;
                     do {
-                        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(there) : "l"(flag) : "memory");
-                        good = there != 0u;
+                        asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(there) : "l"(flag) : "memory");
+                        good = there == p.mark;
                     } while (!good && global_timer_ns() - t0 < kMaxBarrierWaitNs);
+                    *flag = 0ull;  // this group alone looks at it
                 }
+            if (residual) {
+                good = good && lin_wait(res_bar, res_phase);
+                res_phase ^= 1u;
+            }
             __syncwarp();
-            good = lin_all(1, 32 * kLinEpilogueWarps, good);
+            good = lin_all(1 + group, 128, good);
             tc_fence_after_sync();
-            for (int c = group; c < kChunks; c += 2, turn ^= 1) {
-                const int b = one_buffer ? 0 : turn;
-                const int col0 = n0 + c * kLinChunk;
-                const uint32_t mine = stage0 + b * kLinStaging + row * 128;
-                if (!it.partial) {
-                    // the buffer is free, or holds the residual
-                    if (residual) {
-                        if (one_buffer && c != group && chief) {
-                            tma_store_wait_read();
-                            lin_expect(res0, kLinStaging);
-                            lin_load<1>(stage0, &map_r, col0, m0, res0);
-                        }
-                        good = good && lin_wait(res0 + 8 * b, res_phase[b]);
-                        res_phase[b] ^= 1u;
-                    } else if (chief) {
-                        if (one_buffer) tma_store_wait_read();
-                        else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-                    }
-                    __syncwarp();
-                    lin_sync(2 + group, 128);
-                }
+
+            // 32 columns of u: the accumulator, what other pairs have left of the tile, and the bias
+            constexpr long long slot_size = static_cast<long long>(BN / 4) * kLinRows;
+            const long long block = static_cast<long long>(group * (kLinColumns / 4)) * kLinRows + row;
+            const auto sums = [&](int half, f32x2 (&v)[16]) {
+                uint32_t d[32];
+                __syncwarp();
+                tmem_load_32cols(acc + buf * BN + 32 * half, d);
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    uint32_t d[32];
-                    float v[32];
-                    __syncwarp();
-                    tmem_load_32cols(tmem + lanes + buf * BN + c * kLinChunk + 32 * half, d);
+                for (int j = 0; j < 16; ++j) v[j] = pack2(__uint_as_float(d[2 * j]), __uint_as_float(d[2 * j + 1]));
+                for (int q = it.helpers; q < pair; ++q) {
+                    const float4* from = p.partials + (q * CG + rank) * slot_size + block + half * 8 * kLinRows;
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(d[j]);
-                    const long long block = static_cast<long long>((c * 2 + half) * 8) * kLinRows + row;
-                    constexpr long long slot_size = static_cast<long long>(BN / 4) * kLinRows;
-                    for (int q = it.helpers; q < pair; ++q) {
-                        const float4* from = p.partials + (q * CG + rank) * slot_size + block;
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            float4 f;
-                            asm volatile("ld.global.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w) : "l"(from + j * kLinRows) : "memory");
-                            v[4 * j] += f.x;
-                            v[4 * j + 1] += f.y;
-                            v[4 * j + 2] += f.z;
-                            v[4 * j + 3] += f.w;
-                        }
-                    }
-                    if (it.partial) {
-                        float4* to = p.partials + (pair * CG + rank) * slot_size + block;
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) to[j * kLinRows] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-                        continue;
-                    }
-                    const int col = col0 + 32 * half;
-                    if (p.bias != nullptr)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (col + 8 * j < p.N) {
-                                const uint4 w = __ldg(reinterpret_cast<const uint4*>(p.bias + 2ll * (col + 8 * j)));
-                                v[8 * j] += pair_lo<KIND>(w.x); v[8 * j + 1] += pair_hi<KIND>(w.x);
-                                v[8 * j + 2] += pair_lo<KIND>(w.y); v[8 * j + 3] += pair_hi<KIND>(w.y);
-                                v[8 * j + 4] += pair_lo<KIND>(w.z); v[8 * j + 5] += pair_hi<KIND>(w.z);
-                                v[8 * j + 6] += pair_lo<KIND>(w.w); v[8 * j + 7] += pair_hi<KIND>(w.w);
-                            }
-                    if (p.u_mode == kUFull) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(mine + kLinStaging + (((4 * half + j) ^ (row & 7)) << 4)),
-                                         "r"(pack_pair<KIND>(v[8 * j], v[8 * j + 1])), "r"(pack_pair<KIND>(v[8 * j + 2], v[8 * j + 3])),
-                                         "r"(pack_pair<KIND>(v[8 * j + 4], v[8 * j + 5])), "r"(pack_pair<KIND>(v[8 * j + 6], v[8 * j + 7]))
-                                         : "memory");
-                    } else if (p.u_mode == kUPacked && m0 + row < p.M && col < p.N) {
-                        // 32 columns are a group of the 8-bit format; columns behind the last are zero but for no bias: sums of zeros
-                        float most = 0.0f;
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) most = fmaxf(most, finite_abs(v[j]));
-                        const int scale = pack8_scale<KIND>(most);
-                        const float inverse = pack8_inverse_step(scale);
-                        const long long at = static_cast<long long>(m0 + row) * p.N + col;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (col + 8 * j < p.N)
-                                *reinterpret_cast<uint2*>(p.codes + at + 8 * j) = make_uint2(pack8_codes4(v + 8 * j, inverse), pack8_codes4(v + 8 * j + 4, inverse));
-                        p.scales[static_cast<long long>(m0 + row) * p.scale_groups + col / 32] = static_cast<unsigned char>(scale);
-                    }
-                    switch (p.act) {
-                        case 1: lin_act_all<1>(v); break;
-                        case 2: lin_act_all<2>(v); break;
-                        case 3: lin_act_all<3>(v); break;
-                        case 4: lin_act_all<4>(v); break;
-                        default: break;
-                    }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t at = mine + (((4 * half + j) ^ (row & 7)) << 4);
-                        if (residual) {
-                            uint4 w;
-                            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(at) : "memory");
-                            v[8 * j] += pair_lo<KIND>(w.x); v[8 * j + 1] += pair_hi<KIND>(w.x);
-                            v[8 * j + 2] += pair_lo<KIND>(w.y); v[8 * j + 3] += pair_hi<KIND>(w.y);
-                            v[8 * j + 4] += pair_lo<KIND>(w.z); v[8 * j + 5] += pair_hi<KIND>(w.z);
-                            v[8 * j + 6] += pair_lo<KIND>(w.w); v[8 * j + 7] += pair_hi<KIND>(w.w);
-                        }
-                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(pack_pair<KIND>(v[8 * j], v[8 * j + 1])),
-                                     "r"(pack_pair<KIND>(v[8 * j + 2], v[8 * j + 3])), "r"(pack_pair<KIND>(v[8 * j + 4], v[8 * j + 5])),
-                                     "r"(pack_pair<KIND>(v[8 * j + 6], v[8 * j + 7]))
-                                     : "memory");
+                    for (int j = 0; j < 8; ++j) {
+                        float4 f;
+                        asm volatile("ld.global.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w) : "l"(from + j * kLinRows) : "memory");
+                        v[2 * j] = add2(v[2 * j], pack2(f.x, f.y));
+                        v[2 * j + 1] = add2(v[2 * j + 1], pack2(f.z, f.w));
                     }
                 }
-                if (it.partial) continue;
+                if (p.bias != nullptr && !it.partial)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        float4 f;
+                        asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w) : "r"(bias + 128 * half + 16 * j));
+                        v[2 * j] = add2(v[2 * j], pack2(f.x, f.y));
+                        v[2 * j + 1] = add2(v[2 * j + 1], pack2(f.z, f.w));
+                    }
+            };
+            const auto release = [&] {  // the accumulator has been read
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) lin_arrive(acc_free + 8 * buf);
+            };
+            // eight values of this row in 16 bits into the staging buffer
+            const auto stage = [&](int piece, const f32x2* v) {
+                const float2 a = unpack2(v[0]), b = unpack2(v[1]), c = unpack2(v[2]), e = unpack2(v[3]);
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(buffer + row * 128 + ((piece ^ (row & 7)) << 4)), "r"(pack_pair<KIND>(a.x, a.y)),
+                             "r"(pack_pair<KIND>(b.x, b.y)), "r"(pack_pair<KIND>(c.x, c.y)), "r"(pack_pair<KIND>(e.x, e.y))
+                             : "memory");
+            };
+            const auto leave = [&](const void* map) {  // the buffer to its place in memory
                 fence_proxy_async_smem();
                 __syncwarp();
-                lin_sync(2 + group, 128);
+                lin_sync(1 + group, 128);
                 if (chief) {
-                    if (m0 < p.M && col0 < p.N) {
-                        lin_store(&map_y, stage0 + b * kLinStaging, col0, m0);
-                        if (p.u_mode == kUFull) lin_store(&map_u, stage0 + kLinStaging, col0, m0);
-                    }
+                    if (inside) lin_store(map, buffer, col0, m0);
                     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                 }
-            }
-            // the accumulator has been read
-            tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) lin_arrive(acc_free + 8 * buf);
+            };
+
             if (it.partial) {
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    f32x2 v[16];
+                    sums(half, v);
+                    float4* to = p.partials + (pair * CG + rank) * slot_size + block + half * 8 * kLinRows;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float2 a = unpack2(v[2 * j]), b = unpack2(v[2 * j + 1]);
+                        to[j * kLinRows] = make_float4(a.x, a.y, b.x, b.y);
+                    }
+                }
+                release();
                 __threadfence();
                 __syncwarp();
-                lin_sync(1, 32 * kLinEpilogueWarps);
-                if (tid == 0) asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(p.flags + pair * CG + rank), "r"(1u) : "memory");
+                lin_sync(1 + group, 128);
+                if (chief) asm volatile("st.release.gpu.global.u64 [%0], %1;" ::"l"(p.flags + (pair * CG + rank) * C::GROUPS + group), "l"(p.mark) : "memory");
+                continue;
+            }
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                f32x2 v[16];
+                sums(half, v);
+                switch (p.act) {
+                    case 1: lin_act_all<1>(v); break;
+                    case 2: lin_act_all<2>(v); break;
+                    case 3: lin_act_all<3>(v); break;
+                    case 4: lin_act_all<4>(v); break;
+                    default: break;
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (residual) {
+                        uint4 w;
+                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(buffer + row * 128 + (((4 * half + j) ^ (row & 7)) << 4)) : "memory");
+                        v[4 * j] = add2(v[4 * j], pack2(pair_lo<KIND>(w.x), pair_hi<KIND>(w.x)));
+                        v[4 * j + 1] = add2(v[4 * j + 1], pack2(pair_lo<KIND>(w.y), pair_hi<KIND>(w.y)));
+                        v[4 * j + 2] = add2(v[4 * j + 2], pack2(pair_lo<KIND>(w.z), pair_hi<KIND>(w.z)));
+                        v[4 * j + 3] = add2(v[4 * j + 3], pack2(pair_lo<KIND>(w.w), pair_hi<KIND>(w.w)));
+                    }
+                    stage(4 * half + j, v + 4 * j);
+                }
+            }
+            if (p.u_mode == kUNone) release();
+            leave(&map_y);
+            if (p.u_mode == kUNone) continue;
+            // u takes the same way, once y has left the buffer
+            if (chief) tma_store_wait_read();
+            __syncwarp();
+            lin_sync(1 + group, 128);
+            int scales[2];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                f32x2 v[16];
+                sums(half, v);
+                if (p.u_mode == kUFull) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) stage(4 * half + j, v + 4 * j);
+                    continue;
+                }
+                // 32 columns are a group of the 8-bit format; columns behind the last are sums of zeros, without a bias
+                float x[32];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float2 a = unpack2(v[j]);
+                    x[2 * j] = a.x;
+                    x[2 * j + 1] = a.y;
+                }
+                uint32_t w[8];
+                scales[half] = pack8_group<KIND>(x, w);
+                if (p.codes_map) {  // rows of 64 bytes in the 64-byte swizzle
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(buffer + row * 64 + (((2 * half + j) ^ ((row >> 1) & 3)) << 4)), "r"(w[4 * j]),
+                                     "r"(w[4 * j + 1]), "r"(w[4 * j + 2]), "r"(w[4 * j + 3])
+                                     : "memory");
+                } else if (m0 + row < p.M) {
+                    const int col = col0 + 32 * half;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (col + 8 * j < p.N)
+                            *reinterpret_cast<uint2*>(p.codes + static_cast<long long>(m0 + row) * p.N + col + 8 * j) = make_uint2(w[2 * j], w[2 * j + 1]);
+                }
+            }
+            release();
+            __syncwarp();
+            if (p.u_mode == kUFull || p.codes_map) leave(&map_u);
+            else lin_sync(1 + group, 128);  // everybody has read the bias
+            if (p.u_mode == kUPacked && m0 + row < p.M) {
+                unsigned char* to = p.scales + static_cast<long long>(m0 + row) * p.scale_groups + col0 / 32;
+                if (col0 + 32 < p.N && (reinterpret_cast<uintptr_t>(to) & 1) == 0) {
+                    *reinterpret_cast<unsigned short*>(to) = static_cast<unsigned short>(scales[0] | (scales[1] << 8));
+                } else {
+                    if (col0 < p.N) to[0] = static_cast<unsigned char>(scales[0]);
+                    if (col0 + 32 < p.N) to[1] = static_cast<unsigned char>(scales[1]);
+                }
             }
         }
         if (!good && lane == 0) atomicAdd(&linear_expired_waits, 1u);
-        if (chief) tma_store_wait_all();
+        if (chief) tma_store_wait_read();  // what has been read gets to memory by itself
     }
     // nobody leaves while the other CTA may still arrive on its barriers or read its shared memory
     __syncwarp();

@@ -7,6 +7,7 @@
 #pragma once
 
 #include "common.cuh"
+#include "packed_math.cuh"
 
 namespace lf {
 
@@ -46,6 +47,41 @@ __device__ __forceinline__ uint32_t pack8_codes4(const float* x, float inverse)
         if (!(fabsf(x[i]) < __uint_as_float(0x7f800000u))) c[i] = 0x80u;
     }
     return __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
+}
+
+// The 32 values of a group -> their codes and the scale byte.  Where all are finite and the scale is not held to its most, which is
+// nearly always, a code is the low byte of one fma: x * 2^-e is exact and the sum with 1.5 * 2^23 rounds once.
+template <int KIND>
+__device__ __forceinline__ int pack8_group(const float (&x)[32], uint32_t (&w)[8])
+{
+    float most = fabsf(x[0]);
+    f32x2 odd = both(0.0f);  // NaN where a value is not finite
+#pragma unroll
+    for (int i = 1; i < 32; ++i) most = fmaxf(most, fabsf(x[i]));
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) odd = fma2(pack2(x[i], x[i + 1]), both(0.0f), odd);
+    const bool plain = sum2(odd) == 0.0f;
+    if (!plain) {
+        most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) most = fmaxf(most, finite_abs(x[i]));
+    }
+    const int scale = pack8_scale<KIND>(most);
+    const float inverse = pack8_inverse_step(scale);
+    if (plain && most * inverse <= 127.0f) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const f32x2 k = both(12582912.0f), s = both(inverse);
+            const f32x2 a = fma2(pack2(x[4 * j], x[4 * j + 1]), s, k), b = fma2(pack2(x[4 * j + 2], x[4 * j + 3]), s, k);
+            const float2 fa = unpack2(a), fb = unpack2(b);
+            w[j] = __byte_perm(__byte_perm(__float_as_uint(fa.x), __float_as_uint(fa.y), 0x0040),
+                               __byte_perm(__float_as_uint(fb.x), __float_as_uint(fb.y), 0x0040), 0x5410);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = pack8_codes4(x + 4 * j, inverse);
+    }
+    return scale;
 }
 
 // Four codes -> four values.  A code's byte with its top bit turned over, as the low byte of a float of 2^23, is 2^23 + 128 +
