@@ -79,7 +79,7 @@ linfusion_status_t linfusion_unpack8(const linfusion_pack8_desc_t* desc, const l
  * ---------------------------------------------------------------------------------------------- */
 #define LINFUSION_RECURRENCE_EVERY 64
 typedef struct {
-    int32_t B;        /* batch, >= 1                              */
+    int32_t B;        /* batch, 1 .. 65535                        */
     int32_t N;        /* tokens, >= 1                             */
     int32_t C;        /* channels, a multiple of 8, >= 8          */
     int32_t reverse;  /* 1: from the last token to the first      */
@@ -97,8 +97,9 @@ typedef struct {
  * Forward, from 16-bit inputs.  Outputs: h (may lie exactly over x, decay or gate), and where given last and state (last may be
  * h0).  Otherwise the address range of an output must not meet that of an input or another output.
  * workspace: device memory, 256-byte aligned, of linfusion_recurrence_workspace_bytes(); used until the call's kernels
- * have run, and may then be used by anything else.  One token to eight: one launch and no workspace.
- * Errors: INVALID_ARG, UNSUPPORTED (unknown flags, packed inputs, 2^31 tiles or more), ALLOC (workspace too small), CUDA.
+ * have run, and may then be used by anything else.  Up to 64 tokens: one launch and no workspace; else three launches.
+ * Errors: INVALID_ARG, UNSUPPORTED (unknown flags, packed inputs, B above 65535, 2^31 tiles of 64 x 64 or more), ALLOC (workspace too
+ * small), CUDA.
  */
 linfusion_status_t linfusion_recurrence(const linfusion_recurrence_desc_t* desc, const linfusion_recurrence_input_t* x,
                                         const linfusion_recurrence_input_t* decay, const linfusion_recurrence_input_t* gate,

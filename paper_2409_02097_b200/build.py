@@ -21,9 +21,9 @@ _SOURCES = {
     "pack8.cu": ["common.cuh", "pack8.cuh", "block_kernels.cuh", "packed_math.cuh", "host_checks.h", "host_util.h", "linfusion_attn.h",
                  "linfusion_block.h", "linfusion_layers.h"],
     "recurrence.cu": ["common.cuh", "recurrence_kernels.cuh", "column_sums.cuh", "pack8.cuh", "packed_math.cuh", "host_checks.h", "host_util.h",
-                      "layers_internal.h", "linfusion_attn.h", "linfusion_block.h", "linfusion_layers.h"],
+                      "linfusion_attn.h", "linfusion_block.h", "linfusion_layers.h"],
     "linear.cu": ["common.cuh", "linear_kernels.cuh", "column_sums.cuh", "pack8.cuh", "block_kernels.cuh", "packed_math.cuh",
-                  "host_checks.h", "host_util.h", "layers_internal.h", "linfusion_attn.h", "linfusion_block.h", "linfusion_layers.h"],
+                  "host_checks.h", "host_util.h", "linfusion_attn.h", "linfusion_block.h", "linfusion_layers.h"],
 }
 CHECKED_LIB_PATH = os.path.join(_PKG, "liblinfusion_attn_checked.so")
 

@@ -4,7 +4,6 @@
 #include "../../include/linfusion_layers.h"
 
 #include "host_checks.h"
-#include "layers_internal.h"
 #include "linear_kernels.cuh"
 
 using namespace lf;
@@ -303,13 +302,6 @@ linfusion_status_t workspace_ok(const void* workspace, size_t given, size_t need
 
 }  // namespace
 
-namespace lf {
-cudaError_t read_linear_expired(unsigned int* n, cudaStream_t s)
-{
-    return cudaMemcpyFromSymbolAsync(n, linear_expired_waits, sizeof(*n), 0, cudaMemcpyDeviceToHost, s);
-}
-}  // namespace lf
-
 extern "C" {
 
 linfusion_status_t linfusion_linear_workspace_bytes(const linfusion_linear_desc_t* desc, int32_t backward, int32_t sm_count, size_t* bytes)
@@ -487,6 +479,21 @@ linfusion_status_t linfusion_linear_backward(const linfusion_linear_desc_t* desc
         else st = product(plan.dw, d.K, d.N, d.M, xo, duo, *dw, {}, half, ws + plan.flags_dw, ws + plan.partials, at.device, s);
     }
     return st;
+}
+
+linfusion_status_t linfusion_layers_expired(int32_t device, uint32_t* count, void* cuda_stream)
+{
+    if (count == nullptr || device < 0) return LINFUSION_ERR_INVALID_ARG;
+    const int sms = device_sm_count(device);
+    if (sms < 0) return sms == -2 ? LINFUSION_ERR_UNSUPPORTED : LINFUSION_ERR_CUDA;
+    CurrentDevice guard(device);
+    if (!guard.ok) return LINFUSION_ERR_CUDA;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    unsigned int n = 0;
+    cudaError_t e = cudaMemcpyFromSymbolAsync(&n, linear_expired_waits, sizeof(n), 0, cudaMemcpyDeviceToHost, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    if (e == cudaSuccess) *count = n;
+    return end(e);
 }
 
 }  // extern "C"

@@ -2,46 +2,42 @@
 #include "../../include/linfusion_layers.h"
 
 #include "host_checks.h"
-#include "layers_internal.h"
 #include "recurrence_kernels.cuh"
 
 using namespace lf;
 
 namespace {
 
-constexpr int kForwardTokens = 128, kBackwardTokens = kRecEvery;
-
 linfusion_status_t check(const linfusion_recurrence_desc_t* d)
 {
     if (d == nullptr || d->B <= 0 || d->N <= 0 || d->C <= 0 || d->C % 8 != 0 || (d->reverse & ~1) != 0) return LINFUSION_ERR_INVALID_ARG;
     if ((d->flags & ~LINFUSION_DTYPE_FP16) != 0u) return LINFUSION_ERR_UNSUPPORTED;
     // positions, tiles and rows are counted in 32 bits
-    const int64_t tiles = static_cast<int64_t>(d->B) * ((static_cast<int64_t>(d->C) + kRecSlab - 1) / kRecSlab) *
-                          ((static_cast<int64_t>(d->N) + kBackwardTokens - 1) / kBackwardTokens);
-    if (tiles > INT32_MAX || d->N > INT32_MAX - kForwardTokens || d->C > INT32_MAX - kRecSlab) return LINFUSION_ERR_UNSUPPORTED;
-    return LINFUSION_OK;
+    if (d->N > INT32_MAX - kRecEvery || d->C > INT32_MAX - kRecSlab) return LINFUSION_ERR_UNSUPPORTED;
+    const int64_t tiles = (d->N + kRecEvery - 1) / kRecEvery, slabs = (d->C + kRecSlab - 1) / kRecSlab;
+    // and the grid is slabs x 32768 tiles x the rest
+    if (d->B * ((tiles + kRecTilesY - 1) / kRecTilesY) > 65535) return LINFUSION_ERR_UNSUPPORTED;
+    return d->B * tiles <= INT32_MAX / slabs ? LINFUSION_OK : LINFUSION_ERR_UNSUPPORTED;
 }
 
-// How a pass is cut into tiles, and where its parts of the workspace are.
+// The tiles of a call, and where the parts of its workspace are.
 struct Plan {
-    int slabs, tiles, groups, states;
-    size_t maps, group_states, zeroed, rate, kept, bytes;  // offsets; the first `zeroed` bytes are cleared before the launch
+    int slabs, tiles, width;
+    size_t maps, enters, kept, rate, bytes;
 };
-// `kept`: room for the states that a backward pass recomputes.
-Plan make_plan(const linfusion_recurrence_desc_t& d, int tokens, bool rate, bool kept)
+// `backward`: with the rates' sums; `kept`: room for the states that a backward pass recomputes.
+Plan make_plan(const linfusion_recurrence_desc_t& d, bool backward, bool kept)
 {
-    Plan p;
+    Plan p = {};
     p.slabs = (d.C + kRecSlab - 1) / kRecSlab;
-    p.tiles = (d.N + tokens - 1) / tokens;
-    p.groups = (p.tiles + kRecGroup - 1) / kRecGroup;
-    p.states = (d.N + kRecEvery - 1) / kRecEvery;
-    const size_t lanes = static_cast<size_t>(d.B) * p.slabs * kRecSlab;
-    p.maps = 256;
-    p.group_states = p.maps + lanes * p.tiles * sizeof(ulonglong2);
-    p.zeroed = p.tiles > 1 ? p.group_states + lanes * p.groups * sizeof(unsigned long long) : 0;
-    p.rate = align_up_256(p.zeroed);
-    p.kept = p.rate + (rate ? align_up_256(lanes * p.tiles * sizeof(float)) : 0);
-    p.bytes = p.kept + (kept ? align_up_256(static_cast<size_t>(d.B) * p.states * d.C * sizeof(float)) : 0);
+    p.tiles = (d.N + kRecEvery - 1) / kRecEvery;
+    p.width = p.slabs * kRecSlab;
+    const size_t rows = static_cast<size_t>(d.B) * p.tiles;
+    const bool many = p.tiles > 1;
+    p.enters = many ? align_up_256(rows * p.width * sizeof(float2)) : 0;
+    p.kept = p.enters + (many ? align_up_256(rows * d.C * sizeof(float)) : 0);
+    p.rate = p.kept + (many && kept ? align_up_256(rows * d.C * sizeof(float)) : 0);
+    p.bytes = p.rate + (backward ? align_up_256(rows * p.width * sizeof(float)) : 0);
     return p;
 }
 
@@ -115,50 +111,55 @@ RecParams base(const linfusion_recurrence_desc_t& d, const Plan& plan, const lin
     p.gate = to_input(d, gate);
     p.rate = rate;
     p.h0 = h0;
-    char* ws = static_cast<char*>(workspace);
-    p.ticket = reinterpret_cast<unsigned int*>(ws);
-    p.maps = reinterpret_cast<ulonglong2*>(ws + plan.maps);
-    p.states = reinterpret_cast<unsigned long long*>(ws + plan.group_states);
+    p.maps = reinterpret_cast<float2*>(static_cast<char*>(workspace) + plan.maps);
     p.B = d.B;
     p.N = d.N;
     p.C = d.C;
     p.slabs = plan.slabs;
     p.tiles = plan.tiles;
-    p.groups = plan.groups;
+    p.stacks = (plan.tiles + kRecTilesY - 1) / kRecTilesY;
+    p.width = plan.width;
     p.scale_groups = scale_groups(d);
-    p.n_states = plan.states;
     p.reverse = d.reverse;
     return p;
 }
 
-cudaError_t clear(const Plan& plan, void* workspace, cudaStream_t s)
-{
-    return plan.zeroed != 0 ? cudaMemsetAsync(workspace, 0, plan.zeroed, s) : cudaSuccess;
-}
-
 constexpr int kBf = make_kind(kPhiIdentity, kDtypeBf16), kHf = make_kind(kPhiIdentity, kDtypeFp16);
 
-template <int KIND, bool GATE>
-void launch_forward(const RecParams& p, bool packed, bool store, unsigned int grid, cudaStream_t s)
+dim3 blocks(const RecParams& p) { return dim3(p.slabs, p.stacks > 1 ? kRecTilesY : p.tiles, p.B * p.stacks); }
+
+template <int KIND>
+cudaError_t launch_maps(const RecParams& p, bool gated, bool packed, bool grad, cudaStream_t s)
 {
-    if (store) recurrence_kernel<KIND, GATE, false, true><<<grid, 256, 0, s>>>(p);
-    else if (packed) recurrence_kernel<KIND, GATE, true, false><<<grid, 256, 0, s>>>(p);
-    else recurrence_kernel<KIND, GATE, false, false><<<grid, 256, 0, s>>>(p);
+    const dim3 grid = blocks(p), block(kRecMapsThreads);
+    if (grad)
+        return packed ? launch_pdl(recurrence_maps_kernel<KIND, false, true, true>, grid, block, 0, s, p)
+                      : launch_pdl(recurrence_maps_kernel<KIND, false, false, true>, grid, block, 0, s, p);
+    if (gated)
+        return packed ? launch_pdl(recurrence_maps_kernel<KIND, true, true, false>, grid, block, 0, s, p)
+                      : launch_pdl(recurrence_maps_kernel<KIND, true, false, false>, grid, block, 0, s, p);
+    return packed ? launch_pdl(recurrence_maps_kernel<KIND, false, true, false>, grid, block, 0, s, p)
+                  : launch_pdl(recurrence_maps_kernel<KIND, false, false, false>, grid, block, 0, s, p);
 }
-void launch_forward(const linfusion_recurrence_desc_t& d, const RecParams& p, bool gate, bool packed, bool store, cudaStream_t s)
+// What enters each tile: the maps, then the way from tile to tile.  GRAD: the gradient, else the state.
+template <bool GRAD>
+cudaError_t launch_enters(const linfusion_recurrence_desc_t& d, const RecParams& p, bool gated, bool packed, const float* first, float* enters, cudaStream_t s)
 {
-    const unsigned int grid = static_cast<unsigned int>(p.B) * p.slabs * p.tiles;
     const bool half = (d.flags & LINFUSION_DTYPE_FP16) != 0u;
-    if (half && gate) launch_forward<kHf, true>(p, packed, store, grid, s);
-    else if (half) launch_forward<kHf, false>(p, packed, store, grid, s);
-    else if (gate) launch_forward<kBf, true>(p, packed, store, grid, s);
-    else launch_forward<kBf, false>(p, packed, store, grid, s);
+    const cudaError_t e = half ? launch_maps<kHf>(p, gated, packed, GRAD, s) : launch_maps<kBf>(p, gated, packed, GRAD, s);
+    if (e != cudaSuccess) return e;
+    const dim3 grid(static_cast<unsigned int>(p.width / kRecScanChannels) * p.B), block(kRecScanChannels * kRecScanRuns);
+    return launch_pdl(recurrence_scan_kernel<GRAD>, grid, block, 0, s, p.maps, first, enters, p.tiles, p.width, p.C);
 }
-template <int KIND, bool GATE>
-void launch_backward(const RecParams& p, bool packed, unsigned int grid, cudaStream_t s)
+template <int KIND>
+cudaError_t launch_backward(const RecParams& p, bool gated, bool packed, cudaStream_t s)
 {
-    if (packed) recurrence_backward_kernel<KIND, GATE, true><<<grid, 256, 0, s>>>(p);
-    else recurrence_backward_kernel<KIND, GATE, false><<<grid, 256, 0, s>>>(p);
+    const dim3 grid = blocks(p), block(kRecThreads);
+    if (gated)
+        return packed ? launch_pdl(recurrence_backward_kernel<KIND, true, true>, grid, block, 0, s, p)
+                      : launch_pdl(recurrence_backward_kernel<KIND, true, false>, grid, block, 0, s, p);
+    return packed ? launch_pdl(recurrence_backward_kernel<KIND, false, true>, grid, block, 0, s, p)
+                  : launch_pdl(recurrence_backward_kernel<KIND, false, false>, grid, block, 0, s, p);
 }
 
 bool floats_ok(const float* p) { return p == nullptr || is_aligned(p, 16); }
@@ -173,9 +174,9 @@ linfusion_status_t linfusion_recurrence_workspace_bytes(const linfusion_recurren
     const linfusion_status_t st = check(desc);
     if (st != LINFUSION_OK) return st;
     if (backward == 0) {
-        *bytes = desc->N <= kRecShort ? 0 : make_plan(*desc, kForwardTokens, false, false).bytes;
+        *bytes = make_plan(*desc, false, false).bytes;
     } else {
-        *bytes = make_plan(*desc, kBackwardTokens, true, backward == 2).bytes;
+        *bytes = make_plan(*desc, true, backward == 2).bytes;
     }
     return LINFUSION_OK;
 }
@@ -195,9 +196,9 @@ linfusion_status_t linfusion_recurrence(const linfusion_recurrence_desc_t* desc,
     if (rate == nullptr || !floats_ok(rate) || !floats_ok(h0) || !floats_ok(last) || !floats_ok(state)) return LINFUSION_ERR_INVALID_ARG;
     if (h == nullptr || !output_ok(d, *h)) return LINFUSION_ERR_INVALID_ARG;
     const bool brief = d.N <= kRecShort;
-    const Plan plan = make_plan(d, kForwardTokens, false, false);
-    const size_t need = brief ? 0 : plan.bytes;
-    const size_t ends = static_cast<size_t>(d.B) * d.C * 4, kept = ends * plan.states;
+    const Plan plan = make_plan(d, false, false);
+    const size_t need = plan.bytes;
+    const size_t ends = static_cast<size_t>(d.B) * d.C * 4, kept = ends * plan.tiles;
     View in[8], out[3];
     int ni = 0, no = 0;
     for (const linfusion_recurrence_input_t* i : {x, decay, gate}) add_input(d, i, in, &ni);
@@ -233,7 +234,7 @@ linfusion_status_t linfusion_recurrence(const linfusion_recurrence_desc_t* desc,
     RecParams p = base(d, plan, x, decay, gate, rate, h0, workspace);
     p.h = to_output(*h);
     p.last = last;
-    p.state_out = state;
+    if (plan.tiles == 1) p.keep = state;
     if (brief) {
         const long long threads = static_cast<long long>(d.B) * (d.C / 2), grid = (threads + kRecShortThreads - 1) / kRecShortThreads;
         if (grid > INT32_MAX) return LINFUSION_ERR_UNSUPPORTED;
@@ -245,10 +246,19 @@ linfusion_status_t linfusion_recurrence(const linfusion_recurrence_desc_t* desc,
         else recurrence_short_kernel<kBf, false><<<g, kRecShortThreads, 0, s>>>(p);
         return end(cudaGetLastError());
     }
-    const cudaError_t e = clear(plan, workspace, s);
-    if (e != cudaSuccess) return end(e);
-    launch_forward(d, p, gated, false, true, s);
-    return end(cudaGetLastError());
+    cudaError_t e = cudaSuccess;
+    if (plan.tiles > 1) {
+        float* enters = state != nullptr ? state : reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.enters);
+        e = launch_enters<false>(d, p, gated, false, h0, enters, s);
+        if (e != cudaSuccess) return end(e);
+        p.states = enters;
+    }
+    const dim3 grid = blocks(p), block(kRecForwardThreads);
+    if ((d.flags & LINFUSION_DTYPE_FP16) != 0u)
+        e = gated ? launch_pdl(recurrence_kernel<kHf, true>, grid, block, 0, s, p) : launch_pdl(recurrence_kernel<kHf, false>, grid, block, 0, s, p);
+    else
+        e = gated ? launch_pdl(recurrence_kernel<kBf, true>, grid, block, 0, s, p) : launch_pdl(recurrence_kernel<kBf, false>, grid, block, 0, s, p);
+    return end(e);
 }
 
 linfusion_status_t linfusion_recurrence_backward(const linfusion_recurrence_desc_t* desc, const linfusion_recurrence_input_t* x,
@@ -269,8 +279,8 @@ linfusion_status_t linfusion_recurrence_backward(const linfusion_recurrence_desc
     if (!output_ok(d, grads->x) || !output_ok(d, grads->decay)) return LINFUSION_ERR_INVALID_ARG;
     if ((grads->gate.p != nullptr) != gated || (gated && !output_ok(d, grads->gate))) return LINFUSION_ERR_INVALID_ARG;
 
-    const Plan plan = make_plan(d, kBackwardTokens, true, state == nullptr);
-    const size_t ends = static_cast<size_t>(d.B) * d.C * 4, kept = ends * plan.states;
+    const Plan plan = make_plan(d, true, state == nullptr);
+    const size_t ends = static_cast<size_t>(d.B) * d.C * 4, kept = ends * plan.tiles;
     View in[12], out[6];
     int ni = 0, no = 0;
     for (const linfusion_recurrence_input_t* i : {x, decay, gate}) add_input(d, i, in, &ni);
@@ -297,22 +307,8 @@ linfusion_status_t linfusion_recurrence_backward(const linfusion_recurrence_desc
     if (at.st != LINFUSION_OK) return at.st;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     char* ws = static_cast<char*>(workspace);
-    cudaError_t e;
+    cudaError_t e = cudaSuccess;
     RecParams p = base(d, plan, x, decay, gate, rate, h0, workspace);
-    if (state == nullptr) {
-        // the forward pass' tiles are longer, so its part of the workspace is the smaller
-        const Plan forward = make_plan(d, kForwardTokens, false, false);
-        RecParams f = base(d, forward, x, decay, gate, rate, h0, workspace);
-        f.state_out = reinterpret_cast<float*>(ws + plan.kept);
-        e = clear(forward, workspace, s);
-        if (e != cudaSuccess) return end(e);
-        launch_forward(d, f, gated, packed, false, s);
-        e = cudaGetLastError();
-        if (e != cudaSuccess) return end(e);
-        p.state_in = f.state_out;
-    } else {
-        p.state_in = state;
-    }
     p.dh = {static_cast<const char*>(dh->p), nullptr, dh->batch * 2, dh->row * 2};
     p.dlast = dlast;
     p.dx = to_output(grads->x);
@@ -320,37 +316,26 @@ linfusion_status_t linfusion_recurrence_backward(const linfusion_recurrence_desc
     if (gated) p.dgate = to_output(grads->gate);
     p.dh0 = grads->h0;
     p.rate_partials = grads->rate != nullptr ? reinterpret_cast<float*>(ws + plan.rate) : nullptr;
-    e = clear(plan, workspace, s);
-    if (e != cudaSuccess) return end(e);
-    const unsigned int grid = static_cast<unsigned int>(d.B) * plan.slabs * plan.tiles;
+    p.states = state;
+    if (plan.tiles > 1) {
+        if (state == nullptr) {
+            float* kept_states = reinterpret_cast<float*>(ws + plan.kept);
+            e = launch_enters<false>(d, p, gated, packed, h0, kept_states, s);
+            if (e != cudaSuccess) return end(e);
+            p.states = kept_states;
+        }
+        float* enters = reinterpret_cast<float*>(ws + plan.enters);
+        e = launch_enters<true>(d, p, gated, packed, dlast, enters, s);
+        if (e != cudaSuccess) return end(e);
+        p.grads = enters;
+    }
     const bool half = (d.flags & LINFUSION_DTYPE_FP16) != 0u;
-    if (half && gated) launch_backward<kHf, true>(p, packed, grid, s);
-    else if (half) launch_backward<kHf, false>(p, packed, grid, s);
-    else if (gated) launch_backward<kBf, true>(p, packed, grid, s);
-    else launch_backward<kBf, false>(p, packed, grid, s);
-    e = cudaGetLastError();
+    e = half ? launch_backward<kHf>(p, gated, packed, s) : launch_backward<kBf>(p, gated, packed, s);
     if (e == cudaSuccess && grads->rate != nullptr) {
-        const int blocks = plan.slabs * kRecSlab / kSumChannels;
-        column_sums_kernel<<<blocks, kSumThreads, 0, s>>>(p.rate_partials, grads->rate, static_cast<long long>(d.B) * plan.tiles,
-                                                          plan.slabs * kRecSlab, d.C);
+        column_sums_kernel<<<plan.width / kSumChannels, kSumThreads, 0, s>>>(p.rate_partials, grads->rate, static_cast<long long>(d.B) * plan.tiles,
+                                                          plan.width, d.C);
         e = cudaGetLastError();
     }
-    return end(e);
-}
-
-linfusion_status_t linfusion_layers_expired(int32_t device, uint32_t* count, void* cuda_stream)
-{
-    if (count == nullptr || device < 0) return LINFUSION_ERR_INVALID_ARG;
-    const int sms = device_sm_count(device);
-    if (sms < 0) return sms == -2 ? LINFUSION_ERR_UNSUPPORTED : LINFUSION_ERR_CUDA;
-    CurrentDevice guard(device);
-    if (!guard.ok) return LINFUSION_ERR_CUDA;
-    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    unsigned int n[2] = {0, 0};
-    cudaError_t e = cudaMemcpyFromSymbolAsync(&n[0], recurrence_expired_waits, sizeof(n[0]), 0, cudaMemcpyDeviceToHost, s);
-    if (e == cudaSuccess) e = read_linear_expired(&n[1], s);
-    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
-    if (e == cudaSuccess) *count = n[0] + n[1];
     return end(e);
 }
 

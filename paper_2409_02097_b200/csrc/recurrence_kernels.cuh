@@ -1,18 +1,22 @@
 // The gated linear recurrence of include/linfusion_layers.h, forward and backward.
 //
 // Mathematics.  h_t = h_(t-1) + e_t (v_t - h_(t-1)) is the map h -> A h + H with A = 1 - e, H = e v, and maps compose:
-// (A1, H1) then (A2, H2) is (A1 A2, A2 H1 + H2).  A tile of tokens is read once, into registers; each thread forms the map of its
-// few tokens, threads and warps are joined by a scan, and tiles by the state that enters them, which a tile gets from those
-// before it while its own data stays where it is.  The update is kept in the form h + e (v - h) with e formed without
-// cancellation: near e = 0 (long memories) 1 - e has lost e's digits, and a product of thousands of such factors would show it.
+// (A1, H1) then (A2, H2) is (A1 A2, A2 H1 + H2).  So is the gradient's way back, G -> (1 - e)(dh + G).  The update is kept in the form
+// h + e (v - h) with e formed without cancellation: near e = 0 (long memories) 1 - e has lost e's digits, and a product of
+// thousands of such factors would show it.
 //
-// Between tiles.  Every tile publishes its map at once.  Tiles come in groups of kGroup; the last of a group also publishes the
-// state behind it.  A tile composes the maps of those before it in its group and applies them to the last group's state:
-// always the same products in the same order, so results do not depend on which tile was how far (a look-back that takes the
-// first state it finds would).  Tiles are dealt out by a counter in the order of the scan, so whatever a tile waits for
-// belongs to a tile that runs already.  Waits are bounded.
+// Three launches.  recurrence_maps_kernel forms the map of every tile of 64 tokens, recurrence_scan_kernel goes through the
+// tiles of each channel (a run of them a thread, then the runs' maps, then the run again with what enters it) and leaves the state that
+// enters each tile, which is what the backward pass keeps; recurrence_kernel and recurrence_backward_kernel then do every tile
+// by itself.  Sums and products have a fixed order, nothing waits for another block.  The price is that inputs are read
+// twice: 14 bytes a value instead of 8 forward, 18 instead of 14 backward (the maps need decay and dh alone; the states are kept), but the
+// second time from L2 where they fit.  The one-pass form, in which a tile waits for the maps of the tiles before it while its own inputs
+// stay in registers, was built first and was slower: 363 against 263 us forward for 131072 x 640, 49 against 42 for 2 x 4096 x 1280, and
+// 145 against 110 backward for 2 x 16384 x 640; its blocks spent two thirds of their time waiting or at barriers, and registers allow
+// but two on an SM.
 //
-// Bound by DRAM: forward 8 bytes a value with a gate (three inputs, h), backward 14, or 11.1 from checkpoints.
+// What bounds it now: issue slots, not DRAM (30 to 40 % of its rate).  A value takes 30 instructions in the maps, 42 in the forward pass
+// and 75 in the backward pass, of which the arithmetic proper is half; it runs on pairs of fp32 values.
 #pragma once
 
 #include "column_sums.cuh"
@@ -21,11 +25,8 @@
 namespace lf {
 
 constexpr int kRecSlab = 64;    // channels of a tile: rows of 128 bytes
-constexpr int kRecEvery = 64;   // tokens from one kept state to the next
-constexpr int kRecGroup = 16;   // tiles whose maps a tile composes at most, but one
+constexpr int kRecEvery = 64;   // tokens of a tile, and from one kept state to the next
 constexpr int kRecShort = 8;    // tokens up to which a thread goes through the sequence alone
-
-static __device__ unsigned int recurrence_expired_waits;
 
 struct RecInput {
     const char* p;                // 16-bit values, or codes
@@ -40,21 +41,12 @@ struct RecParams {
     RecInput x, decay, gate, dh;
     RecOutput h;                  // forward
     RecOutput dx, ddecay, dgate;  // backward
-    const float *rate, *h0, *state_in, *dlast;
-    float *last, *state_out, *dh0, *rate_partials;
-    unsigned int* ticket;         // these three are zero when the kernel starts; not used with one tile
-    ulonglong2* maps;             // [tile][channel]: a word for A and one for H, each with a flag above its 32 bits
-    unsigned long long* states;   // [group][channel]: the state behind the group, in the same way
-    int B, N, C, slabs, tiles, groups, scale_groups, n_states, reverse;
-};
-
-// Where lanes sit in a tile: V channels a thread, so kRecSlab / V lanes make a row of tokens, R tokens a thread.
-template <int V, int R, int WARPS>
-struct RecShape {
-    static constexpr int kLanes = kRecSlab / V;      // lanes across the channels
-    static constexpr int kSegs = 32 / kLanes;        // token segments in a warp
-    static constexpr int kTokens = WARPS * kSegs * R;
-    static constexpr int kThreads = 32 * WARPS;
+    const float *rate, *h0, *dlast;
+    const float* states;          // [B][tiles][C]: what enters each tile (null: one tile, h0 does)
+    const float* grads;           // [B][tiles][C]: the gradient that enters each tile from behind (null: one tile, dlast does)
+    float2* maps;                 // [B][tiles][width]
+    float *last, *dh0, *rate_partials, *keep;  // keep: where the state that enters the only tile is left
+    int B, N, C, slabs, tiles, stacks, width, scale_groups, reverse;  // width: channels in whole slabs; stacks: see RecPlace
 };
 
 __device__ __forceinline__ float rec_rcp(float x)
@@ -64,346 +56,445 @@ __device__ __forceinline__ float rec_rcp(float x)
     return y;
 }
 constexpr float kLog2e = 1.4426950408889634f;
-__device__ __forceinline__ float rec_sigmoid(float x) { return rec_rcp(1.0f + ex2_approx(-kLog2e * x)); }
-// 1 - exp(-L).  Below 1/4 by its series (the next term is below 2^-24 of the sum), above from the exponential.
-__device__ __forceinline__ float rec_one_minus_exp(float L)
+__device__ __forceinline__ f32x2 rec_sigmoid(f32x2 x)
 {
-    float s = fmaf(L, -1.0f / 720, 1.0f / 120);
-    s = fmaf(L, s, -1.0f / 24);
-    s = fmaf(L, s, 1.0f / 6);
-    s = fmaf(L, s, -0.5f);
-    s = fmaf(L * L, s, L);
-    const float direct = 1.0f - ex2_approx(-kLog2e * L);
-    return fabsf(L) < 0.25f ? s : direct;
+    const float2 t = unpack2(mul2(x, both(-kLog2e))), d = unpack2(add2(pack2(ex2_approx(t.x), ex2_approx(t.y)), both(1.0f)));
+    return pack2(rec_rcp(d.x), rec_rcp(d.y));
+}
+__device__ __forceinline__ f32x2 rec_exp_minus(f32x2 L)
+{
+    const float2 t = unpack2(mul2(L, both(-kLog2e)));
+    return pack2(ex2_approx(t.x), ex2_approx(t.y));
+}
+// 1 - exp(-L) for 0 <= L <= 1, where it is L times a polynomial of degree six: least-squares fit of (1 - exp(-L)) / L at 4000
+// Chebyshev nodes with the reciprocal of its value as the weight, off by at most 2.6e-9.  No cancellation, and none of the special
+// function unit's time, of which the sigmoids take most.
+__device__ __forceinline__ f32x2 rec_one_minus_exp_unit(f32x2 L)
+{
+    f32x2 s = fma2(L, both(0.00012827072f), both(-0.0012983276f));
+    s = fma2(L, s, both(0.008272708f));
+    s = fma2(L, s, both(-0.04164537f));
+    s = fma2(L, s, both(0.16666305f));
+    s = fma2(L, s, both(-0.49999976f));
+    s = fma2(L, s, both(1.0f));
+    return mul2(L, s);
+}
+// The same for any L: outside from the exponential.  (Rates are not negative in use; a little below zero the polynomial still holds.)
+__device__ __forceinline__ f32x2 rec_one_minus_exp(f32x2 L)
+{
+    const float2 a = unpack2(L), b = unpack2(rec_one_minus_exp_unit(L)), c = unpack2(fma2(rec_exp_minus(L), both(-1.0f), both(1.0f)));
+    return pack2(a.x > -0.0625f && a.x <= 1.0f ? b.x : c.x, a.y > -0.0625f && a.y <= 1.0f ? b.y : c.y);
+}
+template <bool WIDE>
+__device__ __forceinline__ f32x2 rec_decay(f32x2 L) { return WIDE ? rec_one_minus_exp(L) : rec_one_minus_exp_unit(L); }
+// Whether a lane's rates pass 1 or are negative (or NaN), for the whole warp.
+template <int P>
+__device__ __forceinline__ bool rec_wide(const f32x2 (&rate)[P])
+{
+    bool unit = true;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        const float2 r = unpack2(rate[i]);
+        unit = unit && r.x >= 0.0f && r.x <= 1.0f && r.y >= 0.0f && r.y <= 1.0f;
+    }
+    return !__all_sync(0xffffffffu, unit);
+}
+template <bool B>
+struct RecBool {
+    static constexpr bool value = B;
+};
+__device__ __forceinline__ float rec_least(float least, f32x2 s)
+{
+    const float2 f = unpack2(s);
+    return fminf(least, fminf(f.x, f.y));
+}
+// v where the token counts, 0 where its sigmoid(decay) (or 1 - exp(-L) of it) is 0: padding, whatever v holds.
+__device__ __forceinline__ f32x2 rec_unless_padding(f32x2 s, f32x2 v)
+{
+    const float2 a = unpack2(s), b = unpack2(v);
+    return pack2(a.x == 0.0f ? 0.0f : b.x, a.y == 0.0f ? 0.0f : b.y);
 }
 
-// V values of one token: 2 V bytes, or V bytes and the byte of their group's scale.
-template <int KIND, int V, bool PACKED>
-struct RecRaw {
-    uint32_t w[PACKED ? V / 4 : V / 2];
-    int scale;
-    __device__ __forceinline__ void load(const RecInput& in, long long at, long long scale_at)
+// ------------------------------------------------------------------------------------------ a thread's share of a tile
+// Four channels a thread, so sixteen lanes make a row; R tokens a thread: four, so that a tile is eight warps of two segments each, or
+// eight and four warps, where the registers allow it (what a thread does once, some 200 instructions, weighs half as much).
+constexpr int kRecV = 4, kRecP = kRecV / 2, kRecR = 4, kRecMapsR = 8, kRecForwardR = 8;
+constexpr int kRecLanes = kRecSlab / kRecV, kRecSegs = 32 / kRecLanes;
+__host__ __device__ constexpr int rec_warps(int R) { return kRecEvery / (kRecSegs * R); }
+constexpr int kRecWarps = rec_warps(kRecR), kRecThreads = 32 * kRecWarps, kRecMapsThreads = 32 * rec_warps(kRecMapsR),
+              kRecForwardThreads = 32 * rec_warps(kRecForwardR);
+static_assert(kRecWarps * kRecSegs * kRecR == kRecEvery, "a tile");
+
+// Blocks: slabs along x, so that neighbours read the same rows; tiles along y, and where there are more than kRecTilesY, on along z.
+constexpr int kRecTilesY = 32768;
+template <int R>
+struct RecPlace {
+    int b, tile, slab, lane, warp, cl, ch, pos0, left;  // cl: channel in the slab; left: tokens from pos0 on (none behind the last channel)
+    __device__ __forceinline__ explicit RecPlace(const RecParams& p)
     {
-        constexpr int words = PACKED ? V / 4 : V / 2;
-        const char* q = in.p + at;
-        if (words == 4) asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1 % words]), "=r"(w[2 % words]), "=r"(w[3 % words]) : "l"(q) : "memory");
-        else if (words == 2) asm volatile("ld.global.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1 % words]) : "l"(q) : "memory");
-        else asm volatile("ld.global.u32 %0, [%1];" : "=r"(w[0]) : "l"(q) : "memory");
-        if (PACKED) scale = in.scales[scale_at];
-    }
-    // What stands in for a token behind the end: `pair` in every pair of a 16-bit input, zeros in a packed one.
-    __device__ __forceinline__ void fill(uint32_t pair)
-    {
-#pragma unroll
-        for (int i = 0; i < (PACKED ? V / 4 : V / 2); ++i) w[i] = PACKED ? 0u : pair;
-        scale = 127;
-    }
-    __device__ __forceinline__ void values(float* v) const
-    {
-        if constexpr (PACKED) {
-#pragma unroll
-            for (int i = 0; i < V / 4; ++i) unpack8_codes4(w[i], pack8_step(scale), v + 4 * i);
-        } else {
-#pragma unroll
-            for (int i = 0; i < V / 2; ++i) {
-                v[2 * i] = pair_lo<KIND>(w[i]);
-                v[2 * i + 1] = pair_hi<KIND>(w[i]);
-            }
+        slab = blockIdx.x;
+        tile = blockIdx.y;
+        b = blockIdx.z;
+        if (p.stacks > 1) {
+            b = static_cast<int>(blockIdx.z) / p.stacks;
+            tile += (static_cast<int>(blockIdx.z) - b * p.stacks) * kRecTilesY;
         }
+        lane = threadIdx.x & 31;
+        warp = threadIdx.x >> 5;
+        cl = (lane % kRecLanes) * kRecV;
+        ch = slab * kRecSlab + cl;
+        pos0 = tile * kRecEvery + (warp * kRecSegs + lane / kRecLanes) * R;
+        left = ch < p.C && tile < p.tiles ? p.N - pos0 : 0;
     }
 };
+// A thread's tokens in a tensor: the first one's address, and the way to the next.
+struct RecRun {
+    char* p;
+    long long step;
+    template <int R>
+    __device__ __forceinline__ RecRun(const char* base, long long batch, long long row, const RecParams& q, const RecPlace<R>& at, long long channel_bytes)
+    {
+        step = q.reverse ? -row : row;
+        p = const_cast<char*>(base) + at.b * batch + (q.reverse ? q.N - 1 - at.pos0 : at.pos0) * row + channel_bytes;
+    }
+    __device__ __forceinline__ char* at(int r) const { return p + r * step; }
+};
+// A thread's tokens of an input as they are read: two words each, or a word of codes.  In packed ones the eight lanes of a scale load
+// one of their R tokens' scales each, and hand it on when it is needed.
+template <int R, bool PACKED>
+struct RecRaw {
+    uint32_t w[R][PACKED ? 1 : 2];
+    int scale;
+};
+template <int R, bool PACKED>
+__device__ __forceinline__ void rec_read(RecRaw<R, PACKED>& raw, const RecInput& in, const RecParams& p, const RecPlace<R>& at)
+{
+    const RecRun run(in.p, in.batch, in.row, p, at, PACKED ? at.ch : 2ll * at.ch);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        raw.w[r][0] = 0u;
+        if (!PACKED) raw.w[r][PACKED ? 0 : 1] = 0u;
+        if (r < at.left) {
+            // plain loads: an output may lie over this input, each element written by the thread that has read it
+            if constexpr (PACKED) asm volatile("ld.global.u32 %0, [%1];" : "=r"(raw.w[r][0]) : "l"(run.at(r)) : "memory");
+            else asm volatile("ld.global.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(raw.w[r][0]), "=r"(raw.w[r][1]) : "l"(run.at(r)) : "memory");
+        }
+    }
+    if constexpr (PACKED) {
+        const int pos = at.pos0 + (at.lane & 7), tok = p.reverse ? p.N - 1 - pos : pos;
+        raw.scale = 127;
+        if ((at.lane & 7) < R && at.tile < p.tiles && at.ch / 32 < p.scale_groups && pos < p.N)  // a lane past the last channel loads for its group too
+            raw.scale = in.scales[(static_cast<long long>(at.b) * p.N + tok) * p.scale_groups + at.ch / 32];
+    }
+}
+template <int KIND, int R, bool PACKED>
+__device__ __forceinline__ void rec_values(const RecRaw<R, PACKED>& raw, int r, int lane, f32x2 (&v)[kRecP])
+{
+    if constexpr (PACKED) {
+        float f[4];
+        unpack8_codes4(raw.w[r][0], pack8_step(__shfl_sync(0xffffffffu, raw.scale, (lane & 24) | r)), f);
+        v[0] = pack2(f[0], f[1]);
+        v[1] = pack2(f[2], f[3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kRecP; ++i) v[i] = pack2(pair_lo<KIND>(raw.w[r][i % (PACKED ? 1 : 2)]), pair_hi<KIND>(raw.w[r][i % (PACKED ? 1 : 2)]));
+    }
+}
 template <int KIND, int V>
-__device__ __forceinline__ void rec_store(char* at, const float* v)
+__device__ __forceinline__ void rec_store(char* at, const f32x2* v)
 {
     uint32_t w[V / 2];
 #pragma unroll
-    for (int i = 0; i < V / 2; ++i) w[i] = pack_pair<KIND>(v[2 * i], v[2 * i + 1]);
+    for (int i = 0; i < V / 2; ++i) {
+        const float2 a = unpack2(v[i]);
+        w[i] = pack_pair<KIND>(a.x, a.y);
+    }
     if constexpr (V == 8) asm volatile("st.global.cs.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
     else if constexpr (V == 4) asm volatile("st.global.cs.v2.u32 [%0], {%1,%2};" ::"l"(at), "r"(w[0]), "r"(w[1]) : "memory");
     else asm volatile("st.global.cs.u32 [%0], %1;" ::"l"(at), "r"(w[0]) : "memory");
 }
 template <int V>
-__device__ __forceinline__ void rec_load_floats(float* v, const float* p)  // 4 V bytes on a boundary of that
+__device__ __forceinline__ void rec_load_floats(f32x2* v, const float* p)  // 4 V bytes on a boundary of eight
 {
 #pragma unroll
     for (int i = 0; i < V / 2; ++i) {
         const float2 t = *reinterpret_cast<const float2*>(p + 2 * i);
-        v[2 * i] = t.x;
-        v[2 * i + 1] = t.y;
+        v[i] = pack2(t.x, t.y);
     }
 }
 template <int V>
-__device__ __forceinline__ void rec_store_floats(float* p, const float* v)
+__device__ __forceinline__ void rec_store_floats(float* p, const f32x2* v)
 {
 #pragma unroll
-    for (int i = 0; i < V / 2; ++i) *reinterpret_cast<float2*>(p + 2 * i) = make_float2(v[2 * i], v[2 * i + 1]);
+    for (int i = 0; i < V / 2; ++i) *reinterpret_cast<float2*>(p + 2 * i) = unpack2(v[i]);
 }
 
-// ------------------------------------------------------------------------------------------ between tiles
-__device__ __forceinline__ unsigned long long rec_word(float x) { return (1ull << 32) | __float_as_uint(x); }
-__device__ __forceinline__ void rec_publish(ulonglong2* p, float A, float H)
-{
-    asm volatile("st.relaxed.gpu.global.v2.b64 [%0], {%1, %2};" ::"l"(p), "l"(rec_word(A)), "l"(rec_word(H)) : "memory");
-}
-__device__ __forceinline__ void rec_publish(unsigned long long* p, float s)
-{
-    asm volatile("st.relaxed.gpu.global.b64 [%0], %1;" ::"l"(p), "l"(rec_word(s)) : "memory");
-}
-__device__ __forceinline__ ulonglong2 rec_peek(const ulonglong2* p)
-{
-    ulonglong2 v;
-    asm volatile("ld.relaxed.gpu.global.v2.b64 {%0, %1}, [%2];" : "=l"(v.x), "=l"(v.y) : "l"(p) : "memory");
-    return v;
-}
-__device__ __forceinline__ unsigned long long rec_peek(const unsigned long long* p)
-{
-    unsigned long long v;
-    asm volatile("ld.relaxed.gpu.global.b64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
-    return v;
-}
-__device__ __forceinline__ bool rec_there(ulonglong2 v) { return (v.x >> 32) != 0ull && (v.y >> 32) != 0ull; }
-__device__ __forceinline__ bool rec_there(unsigned long long v) { return (v >> 32) != 0ull; }
-// `v`, read from p before, again until it is there or the time is up.  A value that never came counts as NaN.
-template <typename W>
-__device__ __forceinline__ W rec_await(const W* p, W v, W never)
-{
-    if (rec_there(v)) return v;
-    const unsigned long long t0 = global_timer_ns();
-    do {
-        v = rec_peek(p);
-        if (rec_there(v)) return v;
-    } while (global_timer_ns() - t0 < kMaxBarrierWaitNs);
-    atomicAdd(&recurrence_expired_waits, 1u);
-    return never;
-}
-__device__ __forceinline__ float rec_low(unsigned long long w) { return __uint_as_float(static_cast<uint32_t>(w)); }
 
-// The state that enters tile k (in the order of the pass) of a slab.  All threads call it; those of channel tid % 64 share the
-// maps before it, four threads of up to four each.  `own` is this tile's map, `first` what enters tile 0 (both looked at in the
-// first 64 threads, and `first` in tile 0 alone: it publishes the state behind it as a map that forgets what enters.  So nobody reads h0
-// after tile 0 has, and the last state may be written over it).  Returns the state to the first 64 threads.  part: 4 x 64 maps in
-// shared memory.
-template <int THREADS>
-__device__ __forceinline__ float rec_enter(const RecParams& p, long long slab_index, int k, float2 own, float first, float2 (*part)[kRecSlab])
-{
-    static_assert(THREADS == 256 && kRecGroup == 16, "four threads a channel, four maps each");
-    const int ch = threadIdx.x & (kRecSlab - 1), quarter = threadIdx.x / kRecSlab;
-    const int g = k / kRecGroup, in_group = k - g * kRecGroup;
-    ulonglong2* maps = p.maps + slab_index * p.tiles * kRecSlab + ch;
-    unsigned long long* states = p.states + slab_index * p.groups * kRecSlab + ch;
-    if (quarter == 0) {
-        if (k == 0) own = make_float2(0.0f, fmaf(own.x, first, own.y));
-        rec_publish(maps + static_cast<long long>(k) * kRecSlab, own.x, own.y);
-    }
-    float A = 1.0f, H = 0.0f;
-    const int j0 = 4 * quarter, n = min(4, in_group - j0);
-    if (n > 0) {
-        const ulonglong2* q = maps + static_cast<long long>(g * kRecGroup + j0) * kRecSlab;
-        ulonglong2 v[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (j < n) v[j] = rec_peek(q + j * kRecSlab);
-        const unsigned long long nan = (1ull << 32) | 0x7fffffffull;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (j < n) {
-                const ulonglong2 w = rec_await(q + j * kRecSlab, v[j], make_ulonglong2(nan, nan));
-                H = fmaf(rec_low(w.x), H, rec_low(w.y));
-                A *= rec_low(w.x);
-            }
-    }
-    part[quarter][ch] = make_float2(A, H);
-    __syncthreads();
-    float s = 0.0f;
-    if (quarter == 0) {
-        s = first;
-        if (g > 0) {
-            const unsigned long long* q = states + static_cast<long long>(g - 1) * kRecSlab;
-            s = rec_low(rec_await(q, rec_peek(q), (1ull << 32) | 0x7fffffffull));
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 m = part[i][ch];
-            s = fmaf(m.x, s, m.y);
-        }
-        if (in_group == kRecGroup - 1) rec_publish(states + static_cast<long long>(g) * kRecSlab, fmaf(own.x, s, own.y));
-    }
-    return s;
-}
-
-// The tile that this block takes.
-struct RecTile {
-    int b, slab, k;           // k: its place in the order of the pass
-    long long slab_index;     // b * slabs + slab
-};
-__device__ __forceinline__ RecTile rec_take(const RecParams& p, unsigned int* box)
-{
-    unsigned int t = blockIdx.x;
-    if (p.tiles > 1) {
-        if (threadIdx.x == 0) *box = atomicAdd(p.ticket, 1u);
-        __syncthreads();
-        t = *box;
-    }
-    const unsigned int all = static_cast<unsigned int>(p.B) * p.slabs;
-    RecTile o;
-    o.k = static_cast<int>(t / all);
-    const unsigned int i = t - static_cast<unsigned int>(o.k) * all;
-    o.b = static_cast<int>(i / p.slabs);
-    o.slab = static_cast<int>(i - static_cast<unsigned int>(o.b) * p.slabs);
-    o.slab_index = i;
-    return o;
-}
-
-// Inclusive scan of maps over the token segments of a warp (lanes kLanes apart), forward or backward in the tokens; then the
+// Inclusive scan of maps over the token segments of a warp (lanes LANES apart), forward or backward in the tokens; then the
 // map of what lies before the own segment.
 template <int V, int LANES, bool UP>
-__device__ __forceinline__ void rec_warp_scan(float (&A)[V], float (&H)[V], float (&Ax)[V], float (&Hx)[V], int lane)
+__device__ __forceinline__ void rec_warp_scan(f32x2 (&A)[V / 2], f32x2 (&H)[V / 2], f32x2 (&Ax)[V / 2], f32x2 (&Hx)[V / 2], int lane)
 {
     const int seg = lane / LANES;
     constexpr int segs = 32 / LANES;
+    const auto from = [&](f32x2 x, int off) { return UP ? __shfl_up_sync(0xffffffffu, x, off) : __shfl_down_sync(0xffffffffu, x, off); };
 #pragma unroll
     for (int off = 1; off < segs; off *= 2) {
         const bool in = UP ? seg >= off : seg + off < segs;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float a = UP ? __shfl_up_sync(0xffffffffu, A[i], off * LANES) : __shfl_down_sync(0xffffffffu, A[i], off * LANES);
-            const float h = UP ? __shfl_up_sync(0xffffffffu, H[i], off * LANES) : __shfl_down_sync(0xffffffffu, H[i], off * LANES);
+        for (int i = 0; i < V / 2; ++i) {
+            const f32x2 a = from(A[i], off * LANES), h = from(H[i], off * LANES);
             if (in) {
-                H[i] = fmaf(A[i], h, H[i]);
-                A[i] *= a;
+                H[i] = fma2(A[i], h, H[i]);
+                A[i] = mul2(A[i], a);
             }
         }
     }
     const bool first = UP ? seg == 0 : seg == segs - 1;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        Ax[i] = UP ? __shfl_up_sync(0xffffffffu, A[i], LANES) : __shfl_down_sync(0xffffffffu, A[i], LANES);
-        Hx[i] = UP ? __shfl_up_sync(0xffffffffu, H[i], LANES) : __shfl_down_sync(0xffffffffu, H[i], LANES);
-        if (first) {
-            Ax[i] = 1.0f;
-            Hx[i] = 0.0f;
+    for (int i = 0; i < V / 2; ++i) {
+        const f32x2 a = from(A[i], LANES), h = from(H[i], LANES);
+        Ax[i] = first ? both(1.0f) : a;
+        Hx[i] = first ? both(0.0f) : h;
+    }
+}
+// Per channel, the map before each warp of a tile in the place of the warp's, and the tile's.  One thread a channel.
+template <bool UP, int WARPS>
+__device__ __forceinline__ float2 rec_join(float2 (&totals)[WARPS][kRecSlab], int c)
+{
+    float2 own = make_float2(1.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) {
+        const int w = UP ? i : WARPS - 1 - i;
+        const float2 m = totals[w][c];
+        totals[w][c] = own;
+        own = make_float2(own.x * m.x, fmaf(m.x, own.y, m.y));
+    }
+    return own;
+}
+__device__ __forceinline__ void rec_put(float2* to, const f32x2* A, const f32x2* H)
+{
+#pragma unroll
+    for (int i = 0; i < kRecP; ++i) {
+        const float2 a = unpack2(A[i]), h = unpack2(H[i]);
+        *reinterpret_cast<float4*>(to + 2 * i) = make_float4(a.x, h.x, a.y, h.y);
+    }
+}
+// What enters the thread's segment, from what enters the tile: through the warps before, then the segments before.
+__device__ __forceinline__ void rec_arrive(f32x2 (&h)[kRecP], const float2* before_warp, const float* enters, const f32x2* Ax, const f32x2* Hx)
+{
+#pragma unroll
+    for (int i = 0; i < kRecP; ++i) {
+        const float4 m = *reinterpret_cast<const float4*>(before_warp + 2 * i);
+        const float2 s = *reinterpret_cast<const float2*>(enters + 2 * i);
+        h[i] = fma2(Ax[i], pack2(fmaf(m.x, s.x, m.y), fmaf(m.z, s.y, m.w)), Hx[i]);
+    }
+}
+__device__ __forceinline__ f32x2 rec_minus(f32x2 a, f32x2 b) { return fma2(b, both(-1.0f), a); }
+
+// ------------------------------------------------------------------------------------------ maps of the tiles
+// GRAD: of the gradient (from decay and dh, backward in the tokens); else of the state (from x, decay and gate).
+template <int KIND, bool GATE, bool PACKED, bool GRAD>
+__global__ void __launch_bounds__(kRecMapsThreads, 6) recurrence_maps_kernel(const __grid_constant__ RecParams p)
+{
+    constexpr int R = kRecMapsR;
+    __shared__ __align__(16) float2 totals[rec_warps(R)][kRecSlab];
+    const RecPlace<R> at(p);
+    pdl_wait();
+    pdl_launch_dependents();
+    RecRaw<R, PACKED> d, x, g;
+    RecRaw<R, false> y;
+    rec_read(d, p.decay, p, at);
+    if constexpr (GRAD) rec_read(y, p.dh, p, at);
+    else rec_read(x, p.x, p, at);
+    if constexpr (GATE && !GRAD) rec_read(g, p.gate, p, at);
+    f32x2 rate[kRecP], A[kRecP], H[kRecP];
+#pragma unroll
+    for (int i = 0; i < kRecP; ++i) rate[i] = both(0.0f);
+    if (at.ch < p.C) rec_load_floats<kRecV>(rate, p.rate + at.ch);
+    const bool ragged = (at.tile + 1) * kRecEvery > p.N;
+    float least = 1.0f;
+    // PADDED: with regard to tokens whose other inputs must not count
+    const auto pass = [&](auto wide, auto padded) {
+#pragma unroll
+        for (int i = 0; i < kRecP; ++i) A[i] = H[i] = both(0.0f);
+#pragma unroll
+        for (int n = 0; n < R; ++n) {
+            const int r = GRAD ? R - 1 - n : n;
+            f32x2 s[kRecP], v[kRecP], q[kRecP];
+            rec_values<KIND>(d, r, at.lane, s);
+            if constexpr (GRAD) rec_values<KIND>(y, r, at.lane, v);
+            else rec_values<KIND>(x, r, at.lane, v);
+            if constexpr (GATE && !GRAD) rec_values<KIND>(g, r, at.lane, q);
+#pragma unroll
+            for (int i = 0; i < kRecP; ++i) {
+                s[i] = rec_sigmoid(s[i]);
+                if (ragged && r >= at.left) s[i] = both(0.0f);
+                const f32x2 L = mul2(rate[i], s[i]), e = rec_decay<decltype(wide)::value>(L);
+                A[i] = add2(A[i], L);
+                if constexpr (GRAD) {
+                    const f32x2 sum = add2(v[i], H[i]);
+                    H[i] = rec_minus(sum, mul2(e, sum));
+                } else {
+                    least = rec_least(least, s[i]);
+                    if constexpr (GATE) v[i] = mul2(v[i], rec_sigmoid(q[i]));
+                    if constexpr (decltype(padded)::value) v[i] = rec_unless_padding(s[i], v[i]);
+                    H[i] = fma2(e, rec_minus(v[i], H[i]), H[i]);
+                }
+            }
         }
+    };
+    if (rec_wide(rate)) pass(RecBool<true>(), RecBool<true>());
+    else pass(RecBool<false>(), RecBool<false>());
+    if (!GRAD && __any_sync(0xffffffffu, least == 0.0f)) pass(RecBool<true>(), RecBool<true>());
+#pragma unroll
+    for (int i = 0; i < kRecP; ++i) {
+        A[i] = rec_minus(both(1.0f), rec_one_minus_exp(A[i]));
+        // the segments of a warp, one after the other
+#pragma unroll
+        for (int off = 1; off < kRecSegs; off *= 2) {
+            const f32x2 a = __shfl_xor_sync(0xffffffffu, A[i], off * kRecLanes), h = __shfl_xor_sync(0xffffffffu, H[i], off * kRecLanes);
+            const bool second = ((at.lane / kRecLanes) & off) != 0;
+            H[i] = second != GRAD ? fma2(A[i], h, H[i]) : fma2(a, H[i], h);
+            A[i] = mul2(A[i], a);
+        }
+    }
+    if (at.lane < kRecLanes) rec_put(&totals[at.warp][at.cl], A, H);
+    __syncthreads();
+    if (threadIdx.x < kRecSlab && at.tile < p.tiles)
+        p.maps[(static_cast<long long>(at.b) * p.tiles + at.tile) * p.width + at.slab * kRecSlab + threadIdx.x] = rec_join<!GRAD>(totals, threadIdx.x);
+}
+
+// ------------------------------------------------------------------------------------------ from tile to tile
+// What enters each tile of a channel, in the order of the tiles or (GRAD) from the last to the first.  A block takes 16 channels, a thread a
+// run of tiles: its map, the runs' maps one after the other, then the run again.
+constexpr int kRecScanChannels = 16, kRecScanRuns = 64;
+template <bool GRAD>
+__global__ void __launch_bounds__(kRecScanChannels* kRecScanRuns) recurrence_scan_kernel(const float2* __restrict__ maps, const float* __restrict__ first,
+                                                                                        float* __restrict__ enters, int tiles, int width, int C)
+{
+    __shared__ float2 runs[kRecScanRuns][kRecScanChannels];
+    const int c = threadIdx.x % kRecScanChannels, run = threadIdx.x / kRecScanChannels, ch = static_cast<int>(blockIdx.x % (width / kRecScanChannels)) * kRecScanChannels + c,
+              b = static_cast<int>(blockIdx.x / (width / kRecScanChannels));
+    pdl_wait();
+    pdl_launch_dependents();
+    const int length = (tiles + kRecScanRuns - 1) / kRecScanRuns, k0 = run * length, k1 = min(tiles, k0 + length);
+    const auto tile = [&](int k) { return static_cast<long long>(b) * tiles + (GRAD ? tiles - 1 - k : k); };
+    constexpr int U = 8;
+    float2 m[U], own = make_float2(1.0f, 0.0f);
+    for (int k = k0; k < k1; k += U) {
+#pragma unroll
+        for (int j = 0; j < U; ++j)
+            if (k + j < k1) m[j] = maps[tile(k + j) * width + ch];
+#pragma unroll
+        for (int j = 0; j < U; ++j)
+            if (k + j < k1) own = make_float2(own.x * m[j].x, fmaf(m[j].x, own.y, m[j].y));
+    }
+    // the runs' maps, each with all before it, by doubling
+    for (int n = 1; n < kRecScanRuns; n *= 2) {
+        runs[run][c] = own;
+        __syncthreads();
+        const float2 before = runs[run >= n ? run - n : run][c];
+        if (run >= n) own = make_float2(before.x * own.x, fmaf(own.x, before.y, own.y));
+        __syncthreads();
+    }
+    runs[run][c] = own;
+    __syncthreads();
+    if (ch >= C) return;
+    float s = first != nullptr ? first[static_cast<long long>(b) * C + ch] : 0.0f;
+    if (run > 0) s = fmaf(runs[run - 1][c].x, s, runs[run - 1][c].y);
+    for (int k = k0; k < k1; k += U) {
+#pragma unroll
+        for (int j = 0; j < U; ++j)
+            if (k + j < k1) m[j] = maps[tile(k + j) * width + ch];
+#pragma unroll
+        for (int j = 0; j < U; ++j)
+            if (k + j < k1) {
+                enters[tile(k + j) * C + ch] = s;
+                s = fmaf(m[j].x, s, m[j].y);
+            }
     }
 }
 
-// Pairs that stand for tokens behind the end: -infinity as a decay, zeros otherwise.
-template <int KIND>
-__device__ __forceinline__ constexpr uint32_t rec_minus_infinity() { return kind_dtype(KIND) == kDtypeFp16 ? 0xFC00FC00u : 0xFF80FF80u; }
-
 // ------------------------------------------------------------------------------------------ forward
-// 128 tokens x 64 channels a block.  STORE: writes h and what else is asked for; without it only the kept states (the first half of a
-// backward pass that was given none).
-template <int KIND, bool GATE, bool PACKED, bool STORE>
-__global__ void __launch_bounds__(256, 2) recurrence_kernel(const __grid_constant__ RecParams p)
+template <int KIND, bool GATE>
+__global__ void __launch_bounds__(kRecForwardThreads, 4) recurrence_kernel(const __grid_constant__ RecParams p)
 {
-    constexpr int V = 8, R = 4, WARPS = 8;
-    using S = RecShape<V, R, WARPS>;
-    __shared__ unsigned int box;
-    __shared__ float2 totals[WARPS][kRecSlab];
-    __shared__ float2 part[4][kRecSlab];
-    __shared__ float enters[kRecSlab];
-
-    const RecTile t = rec_take(p, &box);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int seg = warp * S::kSegs + lane / S::kLanes, ch = t.slab * kRecSlab + (lane % S::kLanes) * V;
-    const bool live = ch < p.C;
-    const int pos0 = t.k * S::kTokens + seg * R;
-
-    RecRaw<KIND, V, PACKED> x[R], d[R], g[R];
+    constexpr int R = kRecForwardR, WARPS = rec_warps(R);
+    __shared__ __align__(16) float2 totals[WARPS][kRecSlab];
+    __shared__ __align__(16) float enters[kRecSlab];
+    const RecPlace<R> at(p);
+    // With more than one tile the kernels before, which have waited for what was before them, write none of the inputs.
+    if (p.tiles == 1) pdl_wait();
+    RecRaw<R, false> x, d, g;
+    rec_read(d, p.decay, p, at);
+    rec_read(x, p.x, p, at);
+    if constexpr (GATE) rec_read(g, p.gate, p, at);
+    f32x2 rate[kRecP], e[R][kRecP], v[R][kRecP], A[kRecP], H[kRecP], Ax[kRecP], Hx[kRecP];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int pos = pos0 + r, tok = p.reverse ? p.N - 1 - pos : pos;
-        if (live && pos < p.N) {
-            const long long width = PACKED ? ch : 2ll * ch, scale_at = (static_cast<long long>(t.b) * p.N + tok) * p.scale_groups + ch / 32;
-            x[r].load(p.x, t.b * p.x.batch + tok * p.x.row + width, scale_at);
-            d[r].load(p.decay, t.b * p.decay.batch + tok * p.decay.row + width, scale_at);
-            if (GATE) g[r].load(p.gate, t.b * p.gate.batch + tok * p.gate.row + width, scale_at);
-        } else {
-            x[r].fill(0u);
-            d[r].fill(rec_minus_infinity<KIND>());
-            if (GATE) g[r].fill(0u);
-        }
-    }
-    float rate[V];
-    if (live) rec_load_floats<V>(rate, p.rate + ch);
-    else
-#pragma unroll
-        for (int i = 0; i < V; ++i) rate[i] = 0.0f;
-
-    float e[R][V], v[R][V], A[V], H[V], Ax[V], Hx[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) A[i] = H[i] = 0.0f;
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        float f[V];
-        d[r].values(f);
-        x[r].values(v[r]);
-        const bool behind = PACKED && pos0 + r >= p.N;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float s = behind ? 0.0f : rec_sigmoid(f[i]), L = rate[i] * s;
-            A[i] += L;
-            e[r][i] = rec_one_minus_exp(L);
-            if (s == 0.0f) v[r][i] = 0.0f;  // padding: whatever it holds
-            f[i] = s;
-        }
-        if (GATE) {
-            float q[V];
-            g[r].values(q);
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (f[i] != 0.0f) v[r][i] *= rec_sigmoid(q[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) H[i] = fmaf(e[r][i], v[r][i] - H[i], H[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) A[i] = ex2_approx(-kLog2e * A[i]);
-
-    rec_warp_scan<V, S::kLanes, true>(A, H, Ax, Hx, lane);
-    if (lane / S::kLanes == S::kSegs - 1)
-#pragma unroll
-        for (int i = 0; i < V; ++i) totals[warp][(lane % S::kLanes) * V + i] = make_float2(A[i], H[i]);
-    __syncthreads();
-    // per channel: the map before each warp, and the tile's
-    float2 own = make_float2(1.0f, 0.0f);
-    float first = 0.0f;
-    if (tid < kRecSlab) {
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-            const float2 m = totals[w][tid];
-            totals[w][tid] = own;
-            own = make_float2(own.x * m.x, fmaf(m.x, own.y, m.y));
-        }
-        const int c = t.slab * kRecSlab + tid;
-        if (p.h0 != nullptr && c < p.C && t.k == 0) first = p.h0[static_cast<long long>(t.b) * p.C + c];
-    }
-    if (p.tiles > 1) first = rec_enter<S::kThreads>(p, t.slab_index, t.k, own, first, part);
-    if (tid < kRecSlab) enters[tid] = first;
-    __syncthreads();
-
-    float h[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int c = (lane % S::kLanes) * V + i;
-        const float2 m = totals[warp][c];
-        h[i] = fmaf(Ax[i], fmaf(m.x, enters[c], m.y), Hx[i]);
-    }
-    if (!live) return;
-    if (p.state_out != nullptr && pos0 % kRecEvery == 0 && pos0 < p.N)
-        rec_store_floats<V>(p.state_out + (static_cast<long long>(t.b) * p.n_states + pos0 / kRecEvery) * p.C + ch, h);
-    if constexpr (STORE) {
+    for (int i = 0; i < kRecP; ++i) rate[i] = A[i] = H[i] = both(0.0f);
+    if (at.ch < p.C) rec_load_floats<kRecV>(rate, p.rate + at.ch);
+    const bool ragged = (at.tile + 1) * kRecEvery > p.N;
+    float least = 1.0f;
+    const auto gates = [&](auto wide) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int pos = pos0 + r, tok = p.reverse ? p.N - 1 - pos : pos;
+            f32x2 s[kRecP], q[kRecP];
+            rec_values<KIND>(d, r, at.lane, s);
+            rec_values<KIND>(x, r, at.lane, v[r]);
+            if constexpr (GATE) rec_values<KIND>(g, r, at.lane, q);
 #pragma unroll
-            for (int i = 0; i < V; ++i) h[i] = fmaf(e[r][i], v[r][i] - h[i], h[i]);
-            if (pos < p.N) rec_store<KIND, V>(p.h.p + t.b * p.h.batch + tok * p.h.row + 2ll * ch, h);
+            for (int i = 0; i < kRecP; ++i) {
+                s[i] = rec_sigmoid(s[i]);
+                if (ragged && r >= at.left) s[i] = both(0.0f);
+                const f32x2 L = mul2(rate[i], s[i]);
+                A[i] = add2(A[i], L);
+                e[r][i] = rec_decay<decltype(wide)::value>(L);
+                least = rec_least(least, s[i]);
+                if constexpr (GATE) v[r][i] = mul2(v[r][i], rec_sigmoid(q[i]));
+            }
         }
-        // tokens behind the end have left the state as it was
-        if (p.last != nullptr && t.k == p.tiles - 1 && seg == WARPS * S::kSegs - 1)
-            rec_store_floats<V>(p.last + static_cast<long long>(t.b) * p.C + ch, h);
+    };
+    if (rec_wide(rate)) gates(RecBool<true>());
+    else gates(RecBool<false>());
+    if (least == 0.0f)  // what a padded token holds must not count
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < kRecP; ++i) v[r][i] = rec_unless_padding(e[r][i], v[r][i]);
+#pragma unroll
+    for (int i = 0; i < kRecP; ++i) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) H[i] = fma2(e[r][i], rec_minus(v[r][i], H[i]), H[i]);
+        A[i] = rec_minus(both(1.0f), rec_one_minus_exp(A[i]));
     }
+    rec_warp_scan<kRecV, kRecLanes, true>(A, H, Ax, Hx, at.lane);
+    if (at.lane / kRecLanes == kRecSegs - 1) rec_put(&totals[at.warp][at.cl], A, H);
+    if (p.tiles > 1) pdl_wait();
+    if (threadIdx.x >= kRecForwardThreads - kRecSlab) {
+        const int c = threadIdx.x - (kRecForwardThreads - kRecSlab), ch = at.slab * kRecSlab + c;
+        float s = 0.0f;
+        if (ch < p.C && at.tile < p.tiles && p.states != nullptr) s = p.states[(static_cast<long long>(at.b) * p.tiles + at.tile) * p.C + ch];
+        else if (ch < p.C && p.h0 != nullptr) s = p.h0[static_cast<long long>(at.b) * p.C + ch];
+        if (ch < p.C && p.keep != nullptr) p.keep[static_cast<long long>(at.b) * p.C + ch] = s;
+        enters[c] = s;
+    }
+    __syncthreads();
+    if (threadIdx.x < kRecSlab) rec_join<true>(totals, threadIdx.x);
+    __syncthreads();
+    f32x2 h[kRecP];
+    rec_arrive(h, &totals[at.warp][at.cl], &enters[at.cl], Ax, Hx);
+    if (at.ch >= p.C || at.tile >= p.tiles) return;
+    const RecRun run(p.h.p, p.h.batch, p.h.row, p, at, 2ll * at.ch);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+        for (int i = 0; i < kRecP; ++i) h[i] = fma2(e[r][i], rec_minus(v[r][i], h[i]), h[i]);
+        if (r < at.left) rec_store<KIND, kRecV>(run.at(r), h);
+    }
+    // tokens behind the end have left the state as it was
+    if (p.last != nullptr && at.tile == p.tiles - 1 && at.warp == WARPS - 1 && at.lane / kRecLanes == kRecSegs - 1)
+        rec_store_floats<kRecV>(p.last + static_cast<long long>(at.b) * p.C + at.ch, h);
 }
 
 // A few tokens (one, when a sequence is continued token by token): a thread takes two channels through all of them.  Latency.
@@ -414,206 +505,177 @@ __global__ void __launch_bounds__(kRecShortThreads) recurrence_short_kernel(cons
     const long long i = static_cast<long long>(blockIdx.x) * kRecShortThreads + threadIdx.x;
     const int pairs = p.C / 2, b = static_cast<int>(i / pairs), ch = 2 * static_cast<int>(i - static_cast<long long>(b) * pairs);
     if (b >= p.B) return;
-    float rate[2], h[2] = {0.0f, 0.0f};
-    rec_load_floats<2>(rate, p.rate + ch);
-    if (p.h0 != nullptr) rec_load_floats<2>(h, p.h0 + static_cast<long long>(b) * p.C + ch);
-    if (p.state_out != nullptr) rec_store_floats<2>(p.state_out + static_cast<long long>(b) * p.C + ch, h);
-    RecRaw<KIND, 2, false> x[kRecShort], d[kRecShort], g[kRecShort];
+    f32x2 rate, h = both(0.0f);
+    rec_load_floats<2>(&rate, p.rate + ch);
+    if (p.h0 != nullptr) rec_load_floats<2>(&h, p.h0 + static_cast<long long>(b) * p.C + ch);
+    if (p.keep != nullptr) rec_store_floats<2>(p.keep + static_cast<long long>(b) * p.C + ch, &h);
+    uint32_t x[kRecShort], d[kRecShort], g[kRecShort];
 #pragma unroll
     for (int r = 0; r < kRecShort; ++r)
         if (r < p.N) {
             const int tok = p.reverse ? p.N - 1 - r : r;
-            x[r].load(p.x, b * p.x.batch + tok * p.x.row + 2ll * ch, 0);
-            d[r].load(p.decay, b * p.decay.batch + tok * p.decay.row + 2ll * ch, 0);
-            if (GATE) g[r].load(p.gate, b * p.gate.batch + tok * p.gate.row + 2ll * ch, 0);
+            x[r] = *reinterpret_cast<const uint32_t*>(p.x.p + b * p.x.batch + tok * p.x.row + 2ll * ch);
+            d[r] = *reinterpret_cast<const uint32_t*>(p.decay.p + b * p.decay.batch + tok * p.decay.row + 2ll * ch);
+            if (GATE) g[r] = *reinterpret_cast<const uint32_t*>(p.gate.p + b * p.gate.batch + tok * p.gate.row + 2ll * ch);
         }
 #pragma unroll
     for (int r = 0; r < kRecShort; ++r)
         if (r < p.N) {
             const int tok = p.reverse ? p.N - 1 - r : r;
-            float v[2], f[2], q[2] = {0.0f, 0.0f};
-            x[r].values(v);
-            d[r].values(f);
-            if (GATE) g[r].values(q);
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const float s = rec_sigmoid(f[k]), e = rec_one_minus_exp(rate[k] * s);
-                if (GATE) v[k] *= rec_sigmoid(q[k]);
-                if (s == 0.0f) v[k] = 0.0f;
-                h[k] = fmaf(e, v[k] - h[k], h[k]);
-            }
-            rec_store<KIND, 2>(p.h.p + b * p.h.batch + tok * p.h.row + 2ll * ch, h);
+            f32x2 v = pack2(pair_lo<KIND>(x[r]), pair_hi<KIND>(x[r]));
+            if (GATE) v = mul2(v, rec_sigmoid(pack2(pair_lo<KIND>(g[r]), pair_hi<KIND>(g[r]))));
+            const f32x2 s = rec_sigmoid(pack2(pair_lo<KIND>(d[r]), pair_hi<KIND>(d[r])));
+            h = fma2(rec_one_minus_exp(mul2(rate, s)), fma2(h, both(-1.0f), rec_unless_padding(s, v)), h);
+            rec_store<KIND, 2>(p.h.p + b * p.h.batch + tok * p.h.row + 2ll * ch, &h);
         }
-    if (p.last != nullptr) rec_store_floats<2>(p.last + static_cast<long long>(b) * p.C + ch, h);
+    if (p.last != nullptr) rec_store_floats<2>(p.last + static_cast<long long>(b) * p.C + ch, &h);
 }
 
 // ------------------------------------------------------------------------------------------ backward
-// 64 tokens x 64 channels a block, tiles from the last to the first.  The states inside the tile come from the kept one, the gradient
-// G from the tiles behind; G's map over a token is G -> (1 - e)(dh + G), so its A is the forward pass' own.
+// The states inside the tile from the one that enters it, then the gradients from the last token to the first.
 template <int KIND, bool GATE, bool PACKED>
-__global__ void __launch_bounds__(256, 2) recurrence_backward_kernel(const __grid_constant__ RecParams p)
+__global__ void __launch_bounds__(kRecThreads, 2) recurrence_backward_kernel(const __grid_constant__ RecParams p)
 {
-    constexpr int V = 4, R = 4, WARPS = 8;
-    using S = RecShape<V, R, WARPS>;
-    static_assert(S::kTokens == kRecEvery, "a kept state for each tile");
-    __shared__ unsigned int box;
-    __shared__ float2 totals[2][WARPS][kRecSlab];
-    __shared__ float2 part[4][kRecSlab];
-    __shared__ float enters[2][kRecSlab];
-
-    const RecTile t = rec_take(p, &box);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int seg = warp * S::kSegs + lane / S::kLanes, cl = (lane % S::kLanes) * V, ch = t.slab * kRecSlab + cl;
-    const bool live = ch < p.C;
-    const int tile = p.tiles - 1 - t.k, pos0 = tile * S::kTokens + seg * R;
-
-    RecRaw<KIND, V, PACKED> x[R], d[R], g[R];
-    RecRaw<KIND, V, false> dh[R];
+    __shared__ __align__(16) float2 totals[2][kRecWarps][kRecSlab];
+    __shared__ __align__(16) float enters[2][kRecSlab];
+    const RecPlace<kRecR> at(p);
+    if (p.tiles == 1) pdl_wait();
+    RecRaw<kRecR, PACKED> x, d, g;
+    RecRaw<kRecR, false> dh;
+    rec_read(d, p.decay, p, at);
+    rec_read(x, p.x, p, at);
+    if constexpr (GATE) rec_read(g, p.gate, p, at);
+    rec_read(dh, p.dh, p, at);
+    f32x2 rate[kRecP];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int pos = pos0 + r, tok = p.reverse ? p.N - 1 - pos : pos;
-        if (live && pos < p.N) {
-            const long long width = PACKED ? ch : 2ll * ch, scale_at = (static_cast<long long>(t.b) * p.N + tok) * p.scale_groups + ch / 32;
-            x[r].load(p.x, t.b * p.x.batch + tok * p.x.row + width, scale_at);
-            d[r].load(p.decay, t.b * p.decay.batch + tok * p.decay.row + width, scale_at);
-            if (GATE) g[r].load(p.gate, t.b * p.gate.batch + tok * p.gate.row + width, scale_at);
-            dh[r].load(p.dh, t.b * p.dh.batch + tok * p.dh.row + 2ll * ch, 0);
-        } else {
-            x[r].fill(0u);
-            d[r].fill(rec_minus_infinity<KIND>());
-            if (GATE) g[r].fill(0u);
-            dh[r].fill(0u);
-        }
-    }
-    float rate[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) rate[i] = 0.0f;
-    if (live) rec_load_floats<V>(rate, p.rate + ch);
+    for (int i = 0; i < kRecP; ++i) rate[i] = both(0.0f);
+    if (at.ch < p.C) rec_load_floats<kRecV>(rate, p.rate + at.ch);
 
     // s = sigmoid(decay), q = sigmoid(gate), e, v = q x; a padded token's are zero
-    float s[R][V], e[R][V], q[R][V], v[R][V], A[V], H[V], G[V];
+    f32x2 s[kRecR][kRecP], e[kRecR][kRecP], q[kRecR][kRecP], v[kRecR][kRecP], A[kRecP], H[kRecP], G[kRecP];
 #pragma unroll
-    for (int i = 0; i < V; ++i) A[i] = H[i] = G[i] = 0.0f;
+    for (int i = 0; i < kRecP; ++i) A[i] = H[i] = G[i] = both(0.0f);
+    const bool ragged = (at.tile + 1) * kRecEvery > p.N;
+    float least = 1.0f;
+    const auto gates = [&](auto wide) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const bool behind = PACKED && pos0 + r >= p.N;
-        d[r].values(s[r]);
-        x[r].values(v[r]);
-        if (GATE) g[r].values(q[r]);
+        for (int r = 0; r < kRecR; ++r) {
+            rec_values<KIND>(d, r, at.lane, s[r]);
+            rec_values<KIND>(x, r, at.lane, v[r]);
+            if constexpr (GATE) rec_values<KIND>(g, r, at.lane, q[r]);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            s[r][i] = behind ? 0.0f : rec_sigmoid(s[r][i]);
-            const float L = rate[i] * s[r][i];
-            A[i] += L;
-            e[r][i] = rec_one_minus_exp(L);
-            if (GATE) {
-                q[r][i] = rec_sigmoid(q[r][i]);
-                v[r][i] *= q[r][i];
+            for (int i = 0; i < kRecP; ++i) {
+                s[r][i] = rec_sigmoid(s[r][i]);
+                if (ragged && r >= at.left) s[r][i] = both(0.0f);
+                const f32x2 L = mul2(rate[i], s[r][i]);
+                A[i] = add2(A[i], L);
+                e[r][i] = rec_decay<decltype(wide)::value>(L);
+                least = rec_least(least, s[r][i]);
+                if constexpr (GATE) {
+                    q[r][i] = rec_sigmoid(q[r][i]);
+                    v[r][i] = mul2(v[r][i], q[r][i]);
+                }
             }
-            if (s[r][i] == 0.0f) v[r][i] = q[r][i] = 0.0f;
-            H[i] = fmaf(e[r][i], v[r][i] - H[i], H[i]);
+        }
+    };
+    if (rec_wide(rate)) gates(RecBool<true>());
+    else gates(RecBool<false>());
+    if (least == 0.0f)  // what a padded token holds must not count
+#pragma unroll
+        for (int r = 0; r < kRecR; ++r)
+#pragma unroll
+            for (int i = 0; i < kRecP; ++i) {
+                if constexpr (GATE) q[r][i] = rec_unless_padding(s[r][i], q[r][i]);
+                v[r][i] = rec_unless_padding(s[r][i], v[r][i]);
+            }
+#pragma unroll
+    for (int r = 0; r < kRecR; ++r)
+#pragma unroll
+        for (int i = 0; i < kRecP; ++i) H[i] = fma2(e[r][i], rec_minus(v[r][i], H[i]), H[i]);
+#pragma unroll
+    for (int r = kRecR - 1; r >= 0; --r) {
+        f32x2 y[kRecP];
+        rec_values<KIND>(dh, r, at.lane, y);
+#pragma unroll
+        for (int i = 0; i < kRecP; ++i) {
+            const f32x2 sum = add2(y[i], G[i]);
+            G[i] = rec_minus(sum, mul2(e[r][i], sum));
         }
     }
+    f32x2 Ar[kRecP], Axr[kRecP], Gx[kRecP], Ax[kRecP], Hx[kRecP];
 #pragma unroll
-    for (int r = R - 1; r >= 0; --r) {
-        float y[V];
-        dh[r].values(y);
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float sum = y[i] + G[i];
-            G[i] = fmaf(-e[r][i], sum, sum);
-        }
+    for (int i = 0; i < kRecP; ++i) Ar[i] = A[i] = rec_minus(both(1.0f), rec_one_minus_exp(A[i]));
+    rec_warp_scan<kRecV, kRecLanes, true>(A, H, Ax, Hx, at.lane);
+    rec_warp_scan<kRecV, kRecLanes, false>(Ar, G, Axr, Gx, at.lane);
+    if (at.lane / kRecLanes == kRecSegs - 1) rec_put(&totals[0][at.warp][at.cl], A, H);
+    if (at.lane / kRecLanes == 0) rec_put(&totals[1][at.warp][at.cl], Ar, G);
+    if (p.tiles > 1) pdl_wait();
+    if (threadIdx.x >= kRecThreads - 2 * kRecSlab) {
+        const int i = threadIdx.x - (kRecThreads - 2 * kRecSlab), which = i / kRecSlab, c = i % kRecSlab, ch = at.slab * kRecSlab + c;
+        const float *many = which == 0 ? p.states : p.grads, *one = which == 0 ? p.h0 : p.dlast;
+        float t = 0.0f;
+        if (ch < p.C && at.tile < p.tiles && many != nullptr) t = many[(static_cast<long long>(at.b) * p.tiles + at.tile) * p.C + ch];
+        else if (ch < p.C && one != nullptr) t = one[static_cast<long long>(at.b) * p.C + ch];
+        enters[which][c] = t;
     }
-    float Ar[V], Axr[V], Gx[V], Ax[V], Hx[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) Ar[i] = A[i] = ex2_approx(-kLog2e * A[i]);
-    rec_warp_scan<V, S::kLanes, true>(A, H, Ax, Hx, lane);
-    rec_warp_scan<V, S::kLanes, false>(Ar, G, Axr, Gx, lane);
-    if (lane / S::kLanes == S::kSegs - 1)
-#pragma unroll
-        for (int i = 0; i < V; ++i) totals[0][warp][cl + i] = make_float2(A[i], H[i]);
-    if (lane / S::kLanes == 0)
-#pragma unroll
-        for (int i = 0; i < V; ++i) totals[1][warp][cl + i] = make_float2(Ar[i], G[i]);
     __syncthreads();
-    float2 own = make_float2(1.0f, 0.0f);
-    float first = 0.0f;
-    if (tid < kRecSlab) {  // the gradient, from the last warp to the first
-#pragma unroll
-        for (int w = WARPS - 1; w >= 0; --w) {
-            const float2 m = totals[1][w][tid];
-            totals[1][w][tid] = own;
-            own = make_float2(own.x * m.x, fmaf(m.x, own.y, m.y));
-        }
-        const int c = t.slab * kRecSlab + tid;
-        if (p.dlast != nullptr && c < p.C && t.k == 0) first = p.dlast[static_cast<long long>(t.b) * p.C + c];
-    } else if (tid < 2 * kRecSlab) {  // the state
-        const int cs = tid - kRecSlab, c = t.slab * kRecSlab + cs;
-        float h = c < p.C ? p.state_in[(static_cast<long long>(t.b) * p.n_states + tile) * p.C + c] : 0.0f;
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-            const float2 m = totals[0][w][cs];
-            totals[0][w][cs].x = h;  // what enters the warp
-            h = fmaf(m.x, h, m.y);
-        }
-    }
-    if (p.tiles > 1) first = rec_enter<S::kThreads>(p, t.slab_index, t.k, own, first, part);
-    if (tid < kRecSlab) enters[0][tid] = first;
+    if (threadIdx.x < kRecSlab) rec_join<true>(totals[0], threadIdx.x);
+    else if (threadIdx.x < 2 * kRecSlab) rec_join<false>(totals[1], threadIdx.x - kRecSlab);
     __syncthreads();
-
-    float h[V], drate[V];
+    f32x2 h[kRecP], drate[kRecP];
+    rec_arrive(h, &totals[0][at.warp][at.cl], &enters[0][at.cl], Ax, Hx);
+    rec_arrive(G, &totals[1][at.warp][at.cl], &enters[1][at.cl], Axr, Gx);
+    // v - h_(t-1); then from the last token to the first
+    f32x2 step[kRecR][kRecP];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const float2 m = totals[1][warp][cl + i];
-        G[i] = fmaf(Axr[i], fmaf(m.x, enters[0][cl + i], m.y), Gx[i]);
-        h[i] = fmaf(Ax[i], totals[0][warp][cl + i].x, Hx[i]);
-        drate[i] = 0.0f;
+    for (int r = 0; r < kRecR; ++r)
+#pragma unroll
+        for (int i = 0; i < kRecP; ++i) {
+            step[r][i] = rec_minus(v[r][i], h[i]);
+            h[i] = fma2(e[r][i], step[r][i], h[i]);
+            drate[i] = both(0.0f);
+        }
+    const RecRun run_x(p.dx.p, p.dx.batch, p.dx.row, p, at, 2ll * at.ch), run_d(p.ddecay.p, p.ddecay.batch, p.ddecay.row, p, at, 2ll * at.ch),
+        run_g(p.dgate.p, p.dgate.batch, p.dgate.row, p, at, 2ll * at.ch);
+#pragma unroll
+    for (int r = kRecR - 1; r >= 0; --r) {
+        f32x2 y[kRecP], ox[kRecP], od[kRecP], og[kRecP];
+        rec_values<KIND>(dh, r, at.lane, y);
+#pragma unroll
+        for (int i = 0; i < kRecP; ++i) {
+            const f32x2 sum = add2(y[i], G[i]), dv = mul2(e[r][i], sum);
+            G[i] = rec_minus(sum, dv);
+            const f32x2 dL = mul2(mul2(G[i], step[r][i]), s[r][i]);  // dL sigmoid(decay)
+            drate[i] = add2(drate[i], dL);
+            od[i] = mul2(mul2(dL, rate[i]), rec_minus(both(1.0f), s[r][i]));
+            if constexpr (GATE) {
+                ox[i] = mul2(dv, q[r][i]);
+                og[i] = mul2(mul2(dv, v[r][i]), rec_minus(both(1.0f), q[r][i]));
+            } else {
+                ox[i] = dv;
+            }
+        }
+        if (r < at.left) {
+            rec_store<KIND, kRecV>(run_x.at(r), ox);
+            rec_store<KIND, kRecV>(run_d.at(r), od);
+            if constexpr (GATE) rec_store<KIND, kRecV>(run_g.at(r), og);
+        }
     }
-    // v - h_(t-1), in v's place; then from the last token to the first
-    float step[R][V];
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            step[r][i] = v[r][i] - h[i];
-            h[i] = fmaf(e[r][i], step[r][i], h[i]);
-        }
-#pragma unroll
-    for (int r = R - 1; r >= 0; --r) {
-        const int pos = pos0 + r, tok = p.reverse ? p.N - 1 - pos : pos;
-        float y[V], ox[V], od[V], og[V];
-        dh[r].values(y);
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float sum = y[i] + G[i], dv = e[r][i] * sum;
-            G[i] = sum - dv;
-            const float dL = G[i] * step[r][i] * s[r][i];  // dL sigmoid(decay)
-            drate[i] += dL;
-            od[i] = dL * rate[i] * (1.0f - s[r][i]);
-            ox[i] = GATE ? dv * q[r][i] : dv;
-            if (GATE) og[i] = dv * v[r][i] * (1.0f - q[r][i]);
-        }
-        if (live && pos < p.N) {
-            rec_store<KIND, V>(p.dx.p + t.b * p.dx.batch + tok * p.dx.row + 2ll * ch, ox);
-            rec_store<KIND, V>(p.ddecay.p + t.b * p.ddecay.batch + tok * p.ddecay.row + 2ll * ch, od);
-            if (GATE) rec_store<KIND, V>(p.dgate.p + t.b * p.dgate.batch + tok * p.dgate.row + 2ll * ch, og);
-        }
-    }
-    if (live && p.dh0 != nullptr && tile == 0 && seg == 0) rec_store_floats<V>(p.dh0 + static_cast<long long>(t.b) * p.C + ch, G);
+    if (at.ch < p.C && p.dh0 != nullptr && at.tile == 0 && at.warp == 0 && at.lane < kRecLanes)
+        rec_store_floats<kRecV>(p.dh0 + static_cast<long long>(at.b) * p.C + at.ch, G);
     if (p.rate_partials != nullptr) {
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
+        for (int i = 0; i < kRecP; ++i)
 #pragma unroll
-            for (int off = S::kLanes; off < 32; off *= 2) drate[i] += __shfl_xor_sync(0xffffffffu, drate[i], off);
-            if (lane < S::kLanes) totals[0][warp][cl + i].x = drate[i];
-        }
+            for (int off = kRecLanes; off < 32; off *= 2) drate[i] = add2(drate[i], __shfl_xor_sync(0xffffffffu, drate[i], off));
+        if (at.lane < kRecLanes) rec_put(&totals[0][at.warp][at.cl], drate, drate);
         __syncthreads();
-        if (tid < kRecSlab) {
+        if (threadIdx.x < kRecSlab && at.tile < p.tiles) {
             float sum = 0.0f;
 #pragma unroll
-            for (int w = 0; w < WARPS; ++w) sum += totals[0][w][tid].x;
-            p.rate_partials[(static_cast<long long>(t.b) * p.tiles + tile) * (p.slabs * kRecSlab) + t.slab * kRecSlab + tid] = sum;
+            for (int w = 0; w < kRecWarps; ++w) sum += totals[0][w][threadIdx.x].x;
+            p.rate_partials[(static_cast<long long>(at.b) * p.tiles + at.tile) * p.width + at.slab * kRecSlab + threadIdx.x] = sum;
         }
     }
 }
