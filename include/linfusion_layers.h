@@ -67,7 +67,7 @@ linfusion_status_t linfusion_unpack8(const linfusion_pack8_desc_t* desc, const l
  *     L_t = rate * sigmoid(decay_t)       e_t = 1 - exp(-L_t)        v_t = sigmoid(gate_t) * x_t   (x_t without a gate)
  *     h_t = h_(t-1) + e_t (v_t - h_(t-1)) = exp(-L_t) h_(t-1) + (1 - exp(-L_t)) v_t,     h_(-1) = h0 (zero without one)
  *
- * x, decay, gate, h [B, N, C]; rate fp32 [C], >= 0 in use; h0, last fp32 [B, C].  A token with decay = -infinity leaves the state
+ * x, decay, gate, h [B, N, C]; rate fp32 [C], >= 0 (a negative one counts as NaN); h0, last fp32 [B, C].  A token with decay = -infinity leaves the state
  * as it is, whatever its x and gate hold (NaN too): padding.  `state` keeps the states before every 64th token of
  * the scan, fp32 [B, ceil(N / 64), C]; the backward pass recomputes h from them, 64 tokens at a time, and needs no h.
  *

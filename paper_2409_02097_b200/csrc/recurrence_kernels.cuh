@@ -79,15 +79,37 @@ __device__ __forceinline__ f32x2 rec_one_minus_exp_unit(f32x2 L)
     s = fma2(L, s, both(1.0f));
     return mul2(L, s);
 }
-// The same for any L: outside from the exponential.  (Rates are not negative in use; a little below zero the polynomial still holds.)
+// The same for any L >= 0: above 1 from the exponential.
 __device__ __forceinline__ f32x2 rec_one_minus_exp(f32x2 L)
 {
     const float2 a = unpack2(L), b = unpack2(rec_one_minus_exp_unit(L)), c = unpack2(fma2(rec_exp_minus(L), both(-1.0f), both(1.0f)));
-    return pack2(a.x > -0.0625f && a.x <= 1.0f ? b.x : c.x, a.y > -0.0625f && a.y <= 1.0f ? b.y : c.y);
+    return pack2(a.x <= 1.0f ? b.x : c.x, a.y <= 1.0f ? b.y : c.y);
+}
+// exp(-L), with all its digits whether it is next to 1 or to 0.
+__device__ __forceinline__ f32x2 rec_keep(f32x2 L)
+{
+    const float2 a = unpack2(L), b = unpack2(fma2(rec_one_minus_exp_unit(L), both(-1.0f), both(1.0f))), c = unpack2(rec_exp_minus(L));
+    return pack2(a.x < 0.25f ? b.x : c.x, a.y < 0.25f ? b.y : c.y);
+}
+// e = 1 - exp(-L) and exp(-L) in one number: e up to L = 0.7, beyond it -exp(-L) (with its sign, also where it is zero).
+__device__ __forceinline__ f32x2 rec_both(f32x2 L)
+{
+    const float2 a = unpack2(L), e = unpack2(rec_one_minus_exp(L)), k = unpack2(rec_exp_minus(L));
+    return pack2(a.x > 0.7f ? -k.x : e.x, a.y > 0.7f ? -k.y : e.y);
+}
+__device__ __forceinline__ f32x2 rec_both_e(f32x2 w)
+{
+    const float2 a = unpack2(w);
+    return pack2(__float_as_int(a.x) < 0 ? 1.0f + a.x : a.x, __float_as_int(a.y) < 0 ? 1.0f + a.y : a.y);
+}
+__device__ __forceinline__ f32x2 rec_both_keep(f32x2 w)
+{
+    const float2 a = unpack2(w);
+    return pack2(__float_as_int(a.x) < 0 ? -a.x : 1.0f - a.x, __float_as_int(a.y) < 0 ? -a.y : 1.0f - a.y);
 }
 template <bool WIDE>
 __device__ __forceinline__ f32x2 rec_decay(f32x2 L) { return WIDE ? rec_one_minus_exp(L) : rec_one_minus_exp_unit(L); }
-// Whether a lane's rates pass 1 or are negative (or NaN), for the whole warp.
+// Whether a lane's rates pass 1 (or are NaN), for the whole warp; all warps of a block have the same channels.
 template <int P>
 __device__ __forceinline__ bool rec_wide(const f32x2 (&rate)[P])
 {
@@ -95,7 +117,7 @@ __device__ __forceinline__ bool rec_wide(const f32x2 (&rate)[P])
 #pragma unroll
     for (int i = 0; i < P; ++i) {
         const float2 r = unpack2(rate[i]);
-        unit = unit && r.x >= 0.0f && r.x <= 1.0f && r.y >= 0.0f && r.y <= 1.0f;
+        unit = unit && r.x <= 1.0f && r.y <= 1.0f;
     }
     return !__all_sync(0xffffffffu, unit);
 }
@@ -222,6 +244,18 @@ __device__ __forceinline__ void rec_load_floats(f32x2* v, const float* p)  // 4 
         v[i] = pack2(t.x, t.y);
     }
 }
+// Rates; a negative one counts as NaN.
+template <int V>
+__device__ __forceinline__ void rec_load_rates(f32x2* v, const float* p)
+{
+    rec_load_floats<V>(v, p);
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+        const float2 t = unpack2(v[i]);
+        const float nan = __uint_as_float(0x7fffffffu);
+        v[i] = pack2(t.x >= 0.0f ? fabsf(t.x) : nan, t.y >= 0.0f ? fabsf(t.y) : nan);
+    }
+}
 template <int V>
 __device__ __forceinline__ void rec_store_floats(float* p, const f32x2* v)
 {
@@ -311,7 +345,7 @@ __global__ void __launch_bounds__(kRecMapsThreads, 6) recurrence_maps_kernel(con
     f32x2 rate[kRecP], A[kRecP], H[kRecP];
 #pragma unroll
     for (int i = 0; i < kRecP; ++i) rate[i] = both(0.0f);
-    if (at.ch < p.C) rec_load_floats<kRecV>(rate, p.rate + at.ch);
+    if (at.ch < p.C) rec_load_rates<kRecV>(rate, p.rate + at.ch);
     const bool ragged = (at.tile + 1) * kRecEvery > p.N;
     float least = 1.0f;
     // PADDED: with regard to tokens whose other inputs must not count
@@ -334,7 +368,7 @@ __global__ void __launch_bounds__(kRecMapsThreads, 6) recurrence_maps_kernel(con
                 A[i] = add2(A[i], L);
                 if constexpr (GRAD) {
                     const f32x2 sum = add2(v[i], H[i]);
-                    H[i] = rec_minus(sum, mul2(e, sum));
+                    H[i] = decltype(wide)::value ? mul2(rec_keep(L), sum) : rec_minus(sum, mul2(e, sum));
                 } else {
                     least = rec_least(least, s[i]);
                     if constexpr (GATE) v[i] = mul2(v[i], rec_sigmoid(q[i]));
@@ -349,7 +383,7 @@ __global__ void __launch_bounds__(kRecMapsThreads, 6) recurrence_maps_kernel(con
     if (!GRAD && __any_sync(0xffffffffu, least == 0.0f)) pass(RecBool<true>(), RecBool<true>());
 #pragma unroll
     for (int i = 0; i < kRecP; ++i) {
-        A[i] = rec_minus(both(1.0f), rec_one_minus_exp(A[i]));
+        A[i] = rec_keep(A[i]);
         // the segments of a warp, one after the other
 #pragma unroll
         for (int off = 1; off < kRecSegs; off *= 2) {
@@ -433,7 +467,7 @@ __global__ void __launch_bounds__(kRecForwardThreads, 4) recurrence_kernel(const
     f32x2 rate[kRecP], e[R][kRecP], v[R][kRecP], A[kRecP], H[kRecP], Ax[kRecP], Hx[kRecP];
 #pragma unroll
     for (int i = 0; i < kRecP; ++i) rate[i] = A[i] = H[i] = both(0.0f);
-    if (at.ch < p.C) rec_load_floats<kRecV>(rate, p.rate + at.ch);
+    if (at.ch < p.C) rec_load_rates<kRecV>(rate, p.rate + at.ch);
     const bool ragged = (at.tile + 1) * kRecEvery > p.N;
     float least = 1.0f;
     const auto gates = [&](auto wide) {
@@ -466,7 +500,7 @@ __global__ void __launch_bounds__(kRecForwardThreads, 4) recurrence_kernel(const
     for (int i = 0; i < kRecP; ++i) {
 #pragma unroll
         for (int r = 0; r < R; ++r) H[i] = fma2(e[r][i], rec_minus(v[r][i], H[i]), H[i]);
-        A[i] = rec_minus(both(1.0f), rec_one_minus_exp(A[i]));
+        A[i] = rec_keep(A[i]);
     }
     rec_warp_scan<kRecV, kRecLanes, true>(A, H, Ax, Hx, at.lane);
     if (at.lane / kRecLanes == kRecSegs - 1) rec_put(&totals[at.warp][at.cl], A, H);
@@ -506,7 +540,7 @@ __global__ void __launch_bounds__(kRecShortThreads) recurrence_short_kernel(cons
     const int pairs = p.C / 2, b = static_cast<int>(i / pairs), ch = 2 * static_cast<int>(i - static_cast<long long>(b) * pairs);
     if (b >= p.B) return;
     f32x2 rate, h = both(0.0f);
-    rec_load_floats<2>(&rate, p.rate + ch);
+    rec_load_rates<2>(&rate, p.rate + ch);
     if (p.h0 != nullptr) rec_load_floats<2>(&h, p.h0 + static_cast<long long>(b) * p.C + ch);
     if (p.keep != nullptr) rec_store_floats<2>(p.keep + static_cast<long long>(b) * p.C + ch, &h);
     uint32_t x[kRecShort], d[kRecShort], g[kRecShort];
@@ -549,7 +583,7 @@ __global__ void __launch_bounds__(kRecThreads, 2) recurrence_backward_kernel(con
     f32x2 rate[kRecP];
 #pragma unroll
     for (int i = 0; i < kRecP; ++i) rate[i] = both(0.0f);
-    if (at.ch < p.C) rec_load_floats<kRecV>(rate, p.rate + at.ch);
+    if (at.ch < p.C) rec_load_rates<kRecV>(rate, p.rate + at.ch);
 
     // s = sigmoid(decay), q = sigmoid(gate), e, v = q x; a padded token's are zero
     f32x2 s[kRecR][kRecP], e[kRecR][kRecP], q[kRecR][kRecP], v[kRecR][kRecP], A[kRecP], H[kRecP], G[kRecP];
@@ -569,7 +603,7 @@ __global__ void __launch_bounds__(kRecThreads, 2) recurrence_backward_kernel(con
                 if (ragged && r >= at.left) s[r][i] = both(0.0f);
                 const f32x2 L = mul2(rate[i], s[r][i]);
                 A[i] = add2(A[i], L);
-                e[r][i] = rec_decay<decltype(wide)::value>(L);
+                e[r][i] = decltype(wide)::value ? rec_both(L) : rec_decay<false>(L);
                 least = rec_least(least, s[r][i]);
                 if constexpr (GATE) {
                     q[r][i] = rec_sigmoid(q[r][i]);
@@ -578,7 +612,8 @@ __global__ void __launch_bounds__(kRecThreads, 2) recurrence_backward_kernel(con
             }
         }
     };
-    if (rec_wide(rate)) gates(RecBool<true>());
+    const bool wide = rec_wide(rate);
+    if (wide) gates(RecBool<true>());
     else gates(RecBool<false>());
     if (least == 0.0f)  // what a padded token holds must not count
 #pragma unroll
@@ -588,23 +623,28 @@ __global__ void __launch_bounds__(kRecThreads, 2) recurrence_backward_kernel(con
                 if constexpr (GATE) q[r][i] = rec_unless_padding(s[r][i], q[r][i]);
                 v[r][i] = rec_unless_padding(s[r][i], v[r][i]);
             }
+    const auto sums = [&](auto w) {
+        constexpr bool kWide = decltype(w)::value;
 #pragma unroll
-    for (int r = 0; r < kRecR; ++r)
+        for (int r = 0; r < kRecR; ++r)
 #pragma unroll
-        for (int i = 0; i < kRecP; ++i) H[i] = fma2(e[r][i], rec_minus(v[r][i], H[i]), H[i]);
+            for (int i = 0; i < kRecP; ++i) H[i] = fma2(kWide ? rec_both_e(e[r][i]) : e[r][i], rec_minus(v[r][i], H[i]), H[i]);
 #pragma unroll
-    for (int r = kRecR - 1; r >= 0; --r) {
-        f32x2 y[kRecP];
-        rec_values<KIND>(dh, r, at.lane, y);
+        for (int r = kRecR - 1; r >= 0; --r) {
+            f32x2 y[kRecP];
+            rec_values<KIND>(dh, r, at.lane, y);
 #pragma unroll
-        for (int i = 0; i < kRecP; ++i) {
-            const f32x2 sum = add2(y[i], G[i]);
-            G[i] = rec_minus(sum, mul2(e[r][i], sum));
+            for (int i = 0; i < kRecP; ++i) {
+                const f32x2 sum = add2(y[i], G[i]);
+                G[i] = kWide ? mul2(rec_both_keep(e[r][i]), sum) : rec_minus(sum, mul2(e[r][i], sum));
+            }
         }
-    }
+    };
+    if (wide) sums(RecBool<true>());
+    else sums(RecBool<false>());
     f32x2 Ar[kRecP], Axr[kRecP], Gx[kRecP], Ax[kRecP], Hx[kRecP];
 #pragma unroll
-    for (int i = 0; i < kRecP; ++i) Ar[i] = A[i] = rec_minus(both(1.0f), rec_one_minus_exp(A[i]));
+    for (int i = 0; i < kRecP; ++i) Ar[i] = A[i] = rec_keep(A[i]);
     rec_warp_scan<kRecV, kRecLanes, true>(A, H, Ax, Hx, at.lane);
     rec_warp_scan<kRecV, kRecLanes, false>(Ar, G, Axr, Gx, at.lane);
     if (at.lane / kRecLanes == kRecSegs - 1) rec_put(&totals[0][at.warp][at.cl], A, H);
@@ -627,40 +667,45 @@ __global__ void __launch_bounds__(kRecThreads, 2) recurrence_backward_kernel(con
     rec_arrive(G, &totals[1][at.warp][at.cl], &enters[1][at.cl], Axr, Gx);
     // v - h_(t-1); then from the last token to the first
     f32x2 step[kRecR][kRecP];
-#pragma unroll
-    for (int r = 0; r < kRecR; ++r)
-#pragma unroll
-        for (int i = 0; i < kRecP; ++i) {
-            step[r][i] = rec_minus(v[r][i], h[i]);
-            h[i] = fma2(e[r][i], step[r][i], h[i]);
-            drate[i] = both(0.0f);
-        }
     const RecRun run_x(p.dx.p, p.dx.batch, p.dx.row, p, at, 2ll * at.ch), run_d(p.ddecay.p, p.ddecay.batch, p.ddecay.row, p, at, 2ll * at.ch),
         run_g(p.dgate.p, p.dgate.batch, p.dgate.row, p, at, 2ll * at.ch);
+    const auto gradients = [&](auto w) {
+        constexpr bool kWide = decltype(w)::value;
 #pragma unroll
-    for (int r = kRecR - 1; r >= 0; --r) {
-        f32x2 y[kRecP], ox[kRecP], od[kRecP], og[kRecP];
-        rec_values<KIND>(dh, r, at.lane, y);
+        for (int r = 0; r < kRecR; ++r)
 #pragma unroll
-        for (int i = 0; i < kRecP; ++i) {
-            const f32x2 sum = add2(y[i], G[i]), dv = mul2(e[r][i], sum);
-            G[i] = rec_minus(sum, dv);
-            const f32x2 dL = mul2(mul2(G[i], step[r][i]), s[r][i]);  // dL sigmoid(decay)
-            drate[i] = add2(drate[i], dL);
-            od[i] = mul2(mul2(dL, rate[i]), rec_minus(both(1.0f), s[r][i]));
-            if constexpr (GATE) {
-                ox[i] = mul2(dv, q[r][i]);
-                og[i] = mul2(mul2(dv, v[r][i]), rec_minus(both(1.0f), q[r][i]));
-            } else {
-                ox[i] = dv;
+            for (int i = 0; i < kRecP; ++i) {
+                step[r][i] = rec_minus(v[r][i], h[i]);
+                h[i] = fma2(kWide ? rec_both_e(e[r][i]) : e[r][i], step[r][i], h[i]);
+                drate[i] = both(0.0f);
+            }
+#pragma unroll
+        for (int r = kRecR - 1; r >= 0; --r) {
+            f32x2 y[kRecP], ox[kRecP], od[kRecP], og[kRecP];
+            rec_values<KIND>(dh, r, at.lane, y);
+#pragma unroll
+            for (int i = 0; i < kRecP; ++i) {
+                const f32x2 sum = add2(y[i], G[i]), dv = mul2(kWide ? rec_both_e(e[r][i]) : e[r][i], sum);
+                G[i] = kWide ? mul2(rec_both_keep(e[r][i]), sum) : rec_minus(sum, dv);
+                const f32x2 dL = mul2(mul2(G[i], step[r][i]), s[r][i]);  // dL sigmoid(decay)
+                drate[i] = add2(drate[i], dL);
+                od[i] = mul2(mul2(dL, rate[i]), rec_minus(both(1.0f), s[r][i]));
+                if constexpr (GATE) {
+                    ox[i] = mul2(dv, q[r][i]);
+                    og[i] = mul2(mul2(dv, v[r][i]), rec_minus(both(1.0f), q[r][i]));
+                } else {
+                    ox[i] = dv;
+                }
+            }
+            if (r < at.left) {
+                rec_store<KIND, kRecV>(run_x.at(r), ox);
+                rec_store<KIND, kRecV>(run_d.at(r), od);
+                if constexpr (GATE) rec_store<KIND, kRecV>(run_g.at(r), og);
             }
         }
-        if (r < at.left) {
-            rec_store<KIND, kRecV>(run_x.at(r), ox);
-            rec_store<KIND, kRecV>(run_d.at(r), od);
-            if constexpr (GATE) rec_store<KIND, kRecV>(run_g.at(r), og);
-        }
-    }
+    };
+    if (wide) gradients(RecBool<true>());
+    else gradients(RecBool<false>());
     if (at.ch < p.C && p.dh0 != nullptr && at.tile == 0 && at.warp == 0 && at.lane < kRecLanes)
         rec_store_floats<kRecV>(p.dh0 + static_cast<long long>(at.b) * p.C + at.ch, G);
     if (p.rate_partials != nullptr) {

@@ -14,7 +14,7 @@ from typing import Dict, Optional, Tuple
 
 from . import block
 from .attn import DTYPE_FP16, LinFusionError, OK, allocating_on
-from .block import Rows, _Checked, _Fixed, _call, _check_rc, _check_tensor, _like, _look, _torch_dtype
+from .block import Rows, _Checked, _Fixed, _call, _check_rc, _check_tensor, _copy, _like, _look, _torch_dtype
 
 GROUP = 32          # channels that share a scale of a checkpoint
 STATE_EVERY = 64    # tokens from one kept state of the recurrence to the next
@@ -128,7 +128,21 @@ def _pack8_desc(t, name, dtype):
         raise ValueError(f"{name}: no values")
     r = _rows3(t, name)
     B, N, C = r.shape
-    return Pack8Desc(B, N, C, DTYPE_FP16 if dtype == "fp16" else 0), Rows(t.data_ptr(), r.stride(0), r.stride(1))
+    return Pack8Desc(B, N, C, DTYPE_FP16 if dtype == "fp16" else 0), Rows(None, r.stride(0), r.stride(1))
+
+
+_packings = _Checked()
+
+
+def _pack8_rows(t, name, dtype):
+    """Descriptor and rows of a tensor, the checks made once for each combination of what they depend on."""
+    key = (_look(t), dtype)
+    found = _packings.get(key)
+    if found is None:
+        found = _packings.keep(key, _pack8_desc(t, name, dtype))
+    rows = _copy(found[1])
+    rows.p = t.data_ptr()
+    return found[0], rows
 
 
 class Packed8:
@@ -136,7 +150,7 @@ class Packed8:
     ``codes * 2 ** (scales - 127)``, the scale that of its 32 channels.  ``dtype``: the storage type ("bf16" or "fp16") that it
     was made from, in which those values are exact.  A code of -128 stands for NaN."""
 
-    __slots__ = ("codes", "scales", "dtype")
+    __slots__ = ("_codes", "_scales", "_buffer", "_at", "shape", "dtype", "device")
 
     def __init__(self, codes, scales, dtype: str = "bf16"):
         import torch
@@ -149,37 +163,59 @@ class Packed8:
             raise ValueError("expected CUDA tensors on one device")
         if not codes.is_contiguous() or not scales.is_contiguous():
             raise ValueError("codes and scales must be contiguous")
-        self.codes, self.scales, self.dtype = codes, scales, dtype
+        self._codes, self._scales, self._buffer = codes, scales, None
+        self._at = (codes.data_ptr(), scales.data_ptr())
+        self.shape, self.dtype, self.device = codes.shape, dtype, codes.device
+
+    @classmethod
+    def _new(cls, shape, dtype, device):
+        """An uninitialised checkpoint; its two tensors lie in one allocation and are made when they are asked for."""
+        import torch
+        self = object.__new__(cls)
+        rows = 1
+        for n in shape[:-1]:
+            rows *= n
+        room = -(-rows * shape[-1] // 256) * 256
+        self._buffer = torch.empty(room + rows * -(-shape[-1] // GROUP), dtype=torch.uint8, device=device)
+        p = self._buffer.data_ptr()
+        self._codes = self._scales = None
+        self._at = (p, p + room)
+        self.shape, self.dtype, self.device = torch.Size(shape), dtype, self._buffer.device
+        return self
 
     @property
-    def shape(self):
-        return self.codes.shape
+    def codes(self):
+        import torch
+        if self._codes is None:
+            self._codes = self._buffer[:self.shape.numel()].view(torch.int8).view(self.shape)
+        return self._codes
 
     @property
-    def device(self):
-        return self.codes.device
+    def scales(self):
+        if self._scales is None:
+            groups = (*self.shape[:-1], -(-self.shape[-1] // GROUP))
+            self._scales = self._buffer[self._at[1] - self._at[0]:].view(groups)
+        return self._scales
+
+    def _struct(self):
+        return Packed8Struct(*self._at)
 
     def unpack(self, out=None, stream: Optional[int] = None):
         """The values in the storage type (exact)."""
         import torch
-        index = self.codes.get_device()
+        index = self.device.index
         if stream is not None:
             with allocating_on(stream, index):
                 return self.unpack(out)
         if out is None:
-            out = torch.empty(self.codes.shape, dtype=_torch_dtype(self.dtype), device=self.codes.device)
-        elif out.shape != self.codes.shape or out.device != self.codes.device:
-            raise ValueError(f"out: expected {tuple(self.codes.shape)} on {self.codes.device}, got {tuple(out.shape)} on {out.device}")
-        desc, rows = _pack8_desc(out, "out", self.dtype)
-        _check_rc(_call(index, load_library().linfusion_unpack8, desc, Packed8Struct(self.codes.data_ptr(), self.scales.data_ptr()), rows),
-                  "linfusion_unpack8")
+            out = torch.empty(self.shape, dtype=_torch_dtype(self.dtype), device=self.device)
+        elif out.shape != self.shape or out.device != self.device:
+            raise ValueError(f"out: expected {tuple(self.shape)} on {self.device}, got {tuple(out.shape)} on {out.device}")
+        desc, rows = _pack8_rows(out, "out", self.dtype)
+        rc = _call(index, load_library().linfusion_unpack8, desc, self._struct(), rows)
+        if rc != OK:
+            raise LinFusionError(rc, "linfusion_unpack8")
         return out
-
-
-def _new_packed(shape, dtype, device):
-    import torch
-    return Packed8(torch.empty(shape, dtype=torch.int8, device=device),
-                   torch.empty((*shape[:-1], -(-shape[-1] // GROUP)), dtype=torch.uint8, device=device), dtype)
 
 
 def pack8(x, out: Optional[Packed8] = None, stream: Optional[int] = None) -> Packed8:
@@ -192,20 +228,21 @@ def pack8(x, out: Optional[Packed8] = None, stream: Optional[int] = None) -> Pac
     if stream is not None and x.is_cuda:
         with allocating_on(stream, x.get_device()):
             return pack8(x, out)
-    desc, rows = _pack8_desc(x, "x", dtype)
+    desc, rows = _pack8_rows(x, "x", dtype)
     if out is None:
-        out = _new_packed(x.shape, dtype, x.device)
+        out = Packed8._new(x.shape, dtype, x.device)
     elif out.shape != x.shape or out.dtype != dtype or out.device != x.device:
         raise ValueError(f"out: expected a {dtype} checkpoint of {tuple(x.shape)} on {x.device}")
-    _check_rc(_call(x.get_device(), load_library().linfusion_pack8, desc, rows, Packed8Struct(out.codes.data_ptr(), out.scales.data_ptr())),
-              "linfusion_pack8")
+    rc = _call(x.get_device(), load_library().linfusion_pack8, desc, rows, out._struct())
+    if rc != OK:
+        raise LinFusionError(rc, "linfusion_pack8")
     return out
 
 
 # -------------------------------------------------------------------------------------- recurrence
 def _look8(t):
     """_look() of a tensor or a checkpoint (whose tensors are contiguous)."""
-    return (t.codes.shape, t.dtype, t.codes.get_device()) if isinstance(t, Packed8) else _look(t)
+    return (t.shape, t.dtype, t.device) if isinstance(t, Packed8) else _look(t)
 
 
 class GatedRecurrence(_Fixed):
@@ -216,7 +253,7 @@ class GatedRecurrence(_Fixed):
         h_t = a_t h_(t-1) + (1 - a_t) v_t
 
     x, decay, gate: 16-bit CUDA tensors [B, N, C] with any batch and row strides that are multiples of 8 elements (windows of
-    one projection are fine); rate: fp32 [C], not negative; h0: fp32 [B, C], the state before the first token (None: zero).
+    one projection are fine); rate: fp32 [C], a negative one counts as NaN; h0: fp32 [B, C], the state before the first token (None: zero).
     A token with decay = -inf leaves the state as it is, whatever its x and gate hold: padding.  One token at a time, with
     h0 the state that the call before returned, gives what one call over all tokens gives (up to the rounding of fp32).
     """
@@ -262,6 +299,8 @@ class GatedRecurrence(_Fixed):
     def _floats(self, t, name, shape, device):
         import torch
         if t is None:
+            if name == "rate":
+                raise ValueError("rate: needed")
             return
         if tuple(t.shape) != shape or t.dtype != torch.float32 or t.device != device or not t.is_contiguous():
             raise ValueError(f"{name}: expected a contiguous fp32 tensor of {shape} on {device}")
@@ -284,9 +323,9 @@ class GatedRecurrence(_Fixed):
         out = []
         for s, t in zip(structs, tensors):
             if s is not None:
-                s = type(s).from_buffer_copy(s)
+                s = _copy(s)
                 if isinstance(t, Packed8):
-                    s.packed.codes, s.packed.scales = t.codes.data_ptr(), t.scales.data_ptr()
+                    s.packed = t._struct()
                 else:
                     s.rows.p = t.data_ptr()
             out.append(s)
@@ -325,7 +364,7 @@ class GatedRecurrence(_Fixed):
         if h is None:
             h, rows = _like(x), Rows(None, N * C, C)
         else:
-            rows = type(outs[0]).from_buffer_copy(outs[0])
+            rows = _copy(outs[0])
         rows.p = h.data_ptr()
         if last is None:
             last = torch.empty((B, C), dtype=torch.float32, device=device)
@@ -454,7 +493,7 @@ class Linear(_Fixed):
         raise ValueError(f"{name}: one of its axes must be contiguous, got strides {t.stride()}")
 
     def _packed(self, t, name, C, rows, device):
-        if t.shape[-1] != C or t.codes.numel() != rows * C or t.dtype != self.dtype or t.device != device:
+        if t.shape[-1] != C or t.shape.numel() != rows * C or t.dtype != self.dtype or t.device != device:
             raise ValueError(f"{name}: expected a {self.dtype} checkpoint of {rows} x {C} on {device}, got a {t.dtype} one of {tuple(t.shape)} on {t.device}")
 
     @staticmethod
@@ -512,8 +551,8 @@ class Linear(_Fixed):
         packed = None
         if save == "packed":
             if u is None:
-                u = _new_packed(shape, self.dtype, device)
-            packed = Packed8Struct(u.codes.data_ptr(), u.scales.data_ptr())
+                u = Packed8._new(shape, self.dtype, device)
+            packed = u._struct()
         elif save == "full" and u is None:
             u = torch.empty(shape, dtype=self._torch_dtype, device=device)
         ws = GatedRecurrence._workspace(workspace, need, device)
@@ -587,7 +626,7 @@ class Linear(_Fixed):
         saved = LinearSaved()
         for name, t, wanted in (("x", x, "w" in need), ("u", u, self.act != 0)):
             if wanted and isinstance(t, Packed8):
-                setattr(saved, name + "_packed", Packed8Struct(t.codes.data_ptr(), t.scales.data_ptr()))
+                setattr(saved, name + "_packed", t._struct())
             elif wanted:
                 setattr(saved, name, self._at(ms[name], t))
         ws = GatedRecurrence._workspace(workspace, size, device)
