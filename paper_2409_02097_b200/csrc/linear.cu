@@ -76,7 +76,7 @@ Product plan_product(int M, int N, int K, int sms)
     return best;
 }
 
-// The sums over du's columns: blocks of rows, as many as keep the machine busy.
+// The sums over du's columns: blocks of rows, as many as run at once (three on an SM).
 struct Sums {
     int width, columns, blocks, rows;
 };
@@ -85,7 +85,7 @@ Sums plan_sums(int M, int N, int sms)
     Sums s;
     s.width = (N + kSumChannels - 1) / kSumChannels * kSumChannels;
     s.columns = (N + kDuColumns - 1) / kDuColumns;
-    int blocks = (4 * sms + s.columns - 1) / s.columns;
+    int blocks = 3 * sms / s.columns > 0 ? 3 * sms / s.columns : 1;
     const int step = kDuUnroll * kDuThreads / 32, most = (M + step - 1) / step;
     if (blocks > most) blocks = most;
     if (blocks > 65535) blocks = 65535;

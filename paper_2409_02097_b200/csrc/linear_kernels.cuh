@@ -248,17 +248,11 @@ __device__ __forceinline__ float lin_rcp(float x)
 }
 constexpr float kLinLog2e = 1.4426950408889634f;
 __device__ __forceinline__ float lin_sigmoid(float x) { return lin_rcp(1.0f + ex2_approx(-kLinLog2e * x)); }
-// Phi(-|u|), the tail of the normal distribution, and its density without 1 / sqrt(2 pi): formula 7.1.26 of Abramowitz and Stegun, Handbook
-// of Mathematical Functions, for erfc(|u| / sqrt 2); off by at most 7.5e-8, below what fp32 keeps of the other branch.
-__device__ __forceinline__ float lin_normal_tail(float u, float* bell)
+// 1 / (1 + exp(-x)) of two values.
+__device__ __forceinline__ f32x2 lin_sigmoid2(f32x2 x)
 {
-    const float a = fabsf(u), t = lin_rcp(fmaf(0.3275911f * 0.70710678f, a, 1.0f));
-    *bell = ex2_approx(-0.5f * kLinLog2e * u * u);
-    float s = fmaf(1.061405429f, t, -1.453152027f);
-    s = fmaf(s, t, 1.421413741f);
-    s = fmaf(s, t, -0.284496736f);
-    s = fmaf(s, t, 0.254829592f);
-    return 0.5f * s * t * *bell;
+    const float2 t = unpack2(mul2(x, both(-kLinLog2e))), d = unpack2(add2(pack2(ex2_approx(t.x), ex2_approx(t.y)), both(1.0f)));
+    return pack2(lin_rcp(d.x), lin_rcp(d.y));
 }
 constexpr float kLinTanhScale = 0.7978845608f, kLinTanhCube = 0.044715f;
 // ACT: linfusion_act_t.
@@ -270,24 +264,56 @@ __device__ __forceinline__ float lin_act(float u)
     if (ACT == 4) return u * lin_sigmoid(2.0f * kLinTanhScale * fmaf(kLinTanhCube * u * u, u, u));
     return u;
 }
-template <int ACT>
-__device__ __forceinline__ float lin_act_slope(float u)
+// Phi(-a) for 0 <= a <= 30: formula 7.1.28 of Abramowitz and Stegun, Handbook of Mathematical Functions,
+// erfc(x) = (1 + a1 x + ... + a6 x^6)^-16, off by at most 3e-7; x = a / sqrt 2 is in the coefficients.  One reciprocal a value and no
+// exponential.  Towards 30 the power passes fp32 and the tail is zero.
+__device__ __forceinline__ f32x2 lin_normal_tail(f32x2 a)
 {
-    if (ACT == 1) return u > 0.0f ? 1.0f : u <= 0.0f ? 0.0f : u;
-    if (ACT == 2) {
-        const float s = lin_sigmoid(u);
-        return s * fmaf(u, 1.0f - s, 1.0f);
+    constexpr float r = 0.70710678118654752f;
+    constexpr float b1 = 0.0705230784f * r, b2 = 0.0422820123f * r * r, b3 = 0.0092705272f * r * r * r, b4 = 0.0001520143f * r * r * r * r,
+                    b5 = 0.0002765672f * r * r * r * r * r, b6 = 0.0000430638f * r * r * r * r * r * r;
+    f32x2 s = fma2(a, both(b6), both(b5));
+    s = fma2(a, s, both(b4));
+    s = fma2(a, s, both(b3));
+    s = fma2(a, s, both(b2));
+    s = fma2(a, s, both(b1));
+    s = fma2(a, s, both(1.0f));
+    s = mul2(s, s);
+    s = mul2(s, s);
+    s = mul2(s, s);
+    s = mul2(s, s);
+    const float2 q = unpack2(s);
+    return mul2(pack2(lin_rcp(q.x), lin_rcp(q.y)), both(0.5f));
+}
+__device__ __forceinline__ f32x2 lin_magnitude(float2 u) { return pack2(fminf(fabsf(u.x), 30.0f), fminf(fabsf(u.y), 30.0f)); }
+
+// The activation's slope, two values at a time.
+template <int ACT>
+__device__ __forceinline__ f32x2 lin_act_slope(f32x2 v)
+{
+    const float2 u = unpack2(v);
+    if constexpr (ACT == 1) return pack2(u.x > 0.0f ? 1.0f : u.x <= 0.0f ? 0.0f : u.x, u.y > 0.0f ? 1.0f : u.y <= 0.0f ? 0.0f : u.y);
+    if constexpr (ACT == 2) {
+        const f32x2 s = lin_sigmoid2(v);
+        return mul2(s, fma2(v, fma2(s, both(-1.0f), both(1.0f)), both(1.0f)));
     }
-    if (ACT == 3) {
-        float bell;
-        const float tail = lin_normal_tail(u, &bell);
-        return fmaf(0.3989422804f * u, bell, u < 0.0f ? tail : 1.0f - tail);
+    if constexpr (ACT == 3) {
+        // Phi(u) + u phi(u); Phi = 1/2 + (1/2 - tail) with u's sign.  The density is cut off where it is zero anyway, so that infinities
+        // give the limits; a NaN stays one through u phi(u).
+        const f32x2 a = lin_magnitude(u);
+        const float2 d = unpack2(fma2(lin_normal_tail(a), both(-1.0f), both(0.5f)));
+        const f32x2 cdf = add2(pack2(copysignf(d.x, u.x), copysignf(d.y, u.y)), both(0.5f));
+        const float2 t = unpack2(mul2(mul2(a, a), both(-0.5f * kLinLog2e)));
+        const f32x2 bell = mul2(pack2(ex2_approx(t.x), ex2_approx(t.y)), both(0.3989422804f));
+        const f32x2 c = pack2(u.x > 30.0f ? 30.0f : u.x < -30.0f ? -30.0f : u.x, u.y > 30.0f ? 30.0f : u.y < -30.0f ? -30.0f : u.y);
+        return fma2(c, bell, cdf);
     }
-    if (ACT == 4) {
-        const float s = lin_sigmoid(2.0f * kLinTanhScale * fmaf(kLinTanhCube * u * u, u, u));
-        return fmaf(u * s * (1.0f - s), 2.0f * kLinTanhScale * fmaf(3.0f * kLinTanhCube * u, u, 1.0f), s);
+    if constexpr (ACT == 4) {
+        const f32x2 uu = mul2(v, v), s = lin_sigmoid2(mul2(v, fma2(uu, both(2.0f * kLinTanhScale * kLinTanhCube), both(2.0f * kLinTanhScale))));
+        const f32x2 w = fma2(uu, both(6.0f * kLinTanhScale * kLinTanhCube), both(2.0f * kLinTanhScale));
+        return fma2(mul2(mul2(v, s), fma2(s, both(-1.0f), both(1.0f))), w, s);
     }
-    return 1.0f;
+    return both(1.0f);
 }
 // The activation of 32 values in place, two at a time.
 template <int ACT>
@@ -297,28 +323,12 @@ __device__ __forceinline__ void lin_act_all(f32x2 (&v)[16])
     for (int i = 0; i < 16; ++i) {
         const float2 u = unpack2(v[i]);
         if constexpr (ACT == 3) {
-            // u Phi(u) = max(u, 0) - |u| Phi(-|u|), with formula 7.1.28 of Abramowitz and Stegun, Handbook of Mathematical
-            // Functions: erfc(x) = (1 + a1 x + ... + a6 x^6)^-16, off by at most 3e-7; x = |u| / sqrt 2 is in the coefficients.  One
-            // reciprocal a value and no exponential.  Beyond 30 the power is infinite and the tail zero.
-            constexpr float r = 0.70710678118654752f;
-            constexpr float b1 = 0.0705230784f * r, b2 = 0.0422820123f * r * r, b3 = 0.0092705272f * r * r * r, b4 = 0.0001520143f * r * r * r * r,
-                            b5 = 0.0002765672f * r * r * r * r * r, b6 = 0.0000430638f * r * r * r * r * r * r;
-            const f32x2 a = pack2(fminf(fabsf(u.x), 30.0f), fminf(fabsf(u.y), 30.0f));
-            f32x2 s = fma2(a, both(b6), both(b5));
-            s = fma2(a, s, both(b4));
-            s = fma2(a, s, both(b3));
-            s = fma2(a, s, both(b2));
-            s = fma2(a, s, both(b1));
-            s = fma2(a, s, both(1.0f));
-            s = mul2(s, s);
-            s = mul2(s, s);
-            s = mul2(s, s);
-            s = mul2(s, s);
-            const float2 q = unpack2(s);
+            // u Phi(u) = max(u, 0) - |u| Phi(-|u|)
+            const f32x2 a = lin_magnitude(u);
             float p0, p1;  // a NaN stays one
             asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(p0) : "f"(u.x));
             asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(p1) : "f"(u.y));
-            v[i] = fma2(mul2(a, both(-0.5f)), pack2(lin_rcp(q.x), lin_rcp(q.y)), pack2(p0, p1));
+            v[i] = fma2(mul2(a, both(-1.0f)), lin_normal_tail(a), pack2(p0, p1));
         } else {
             v[i] = pack2(lin_act<ACT>(u.x), lin_act<ACT>(u.y));
         }
@@ -607,15 +617,11 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                     continue;
                 }
                 // 32 columns are a group of the 8-bit format; columns behind the last are sums of zeros, without a bias
-                float x[32];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const float2 a = unpack2(v[j]);
-                    x[2 * j] = a.x;
-                    x[2 * j + 1] = a.y;
-                }
                 uint32_t w[8];
-                scales[half] = pack8_group<KIND>(x, w);
+                const bool plain = all_finite(v);
+                const float most = largest(v, plain);
+                scales[half] = pack8_scale<KIND>(most);
+                pack8_codes(v, most, pack8_inverse_step(scales[half]), plain, w);
                 if (p.codes_map) {  // rows of 64 bytes in the 64-byte swizzle
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
@@ -670,16 +676,16 @@ struct DuParams {
     int M, N, width, rows_per_block, scale_groups;
 };
 template <int KIND, int ACT, bool PACKED>
-__global__ void __launch_bounds__(kDuThreads) linear_du_kernel(const __grid_constant__ DuParams p)
+__global__ void __launch_bounds__(kDuThreads, 3) linear_du_kernel(const __grid_constant__ DuParams p)
 {
     __shared__ float joined[kDuThreads / 32][kDuColumns];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * kDuColumns + 8 * lane;
     const bool live = col < p.N;
     const long long first = static_cast<long long>(blockIdx.y) * p.rows_per_block;
     const long long end = first + p.rows_per_block < p.M ? first + p.rows_per_block : p.M;
-    float sum[8];
+    f32x2 sum[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+    for (int i = 0; i < 4; ++i) sum[i] = both(0.0f);
     if (live)
         for (long long r0 = first + warp; r0 < end; r0 += kDuUnroll * (kDuThreads / 32)) {
             uint4 dy[kDuUnroll], u[kDuUnroll];
@@ -689,12 +695,12 @@ __global__ void __launch_bounds__(kDuThreads) linear_du_kernel(const __grid_cons
                 const long long r = r0 + k * (kDuThreads / 32);
                 if (r < end) {
                     dy[k] = load16(p.dy + r * p.dy_row + 2ll * col);
-                    if (ACT != 0 && PACKED) {
+                    if constexpr (ACT != 0 && PACKED) {
                         const uint2 c = *reinterpret_cast<const uint2*>(p.u + r * p.u_row + col);
                         u[k].x = c.x;
                         u[k].y = c.y;
                         scale[k] = p.scales[r * p.scale_groups + col / 32];
-                    } else if (ACT != 0) {
+                    } else if constexpr (ACT != 0) {
                         u[k] = load16(p.u + r * p.u_row + 2ll * col);
                     }
                 }
@@ -703,28 +709,39 @@ __global__ void __launch_bounds__(kDuThreads) linear_du_kernel(const __grid_cons
             for (int k = 0; k < kDuUnroll; ++k) {
                 const long long r = r0 + k * (kDuThreads / 32);
                 if (r < end) {
-                    F8 g = unpack8<KIND>(dy[k]);
-                    if (ACT != 0) {
-                        F8 v;
-                        if (PACKED) {
-                            unpack8_codes4(u[k].x, pack8_step(scale[k]), v.v);
-                            unpack8_codes4(u[k].y, pack8_step(scale[k]), v.v + 4);
+                    f32x2 g[4], v[4];
+                    g[0] = pack2(pair_lo<KIND>(dy[k].x), pair_hi<KIND>(dy[k].x));
+                    g[1] = pack2(pair_lo<KIND>(dy[k].y), pair_hi<KIND>(dy[k].y));
+                    g[2] = pack2(pair_lo<KIND>(dy[k].z), pair_hi<KIND>(dy[k].z));
+                    g[3] = pack2(pair_lo<KIND>(dy[k].w), pair_hi<KIND>(dy[k].w));
+                    if constexpr (ACT != 0) {
+                        if constexpr (PACKED) {
+                            unpack8_codes4(u[k].x, pack8_step(scale[k]), v);
+                            unpack8_codes4(u[k].y, pack8_step(scale[k]), v + 2);
                         } else {
-                            v = unpack8<KIND>(u[k]);
+                            v[0] = pack2(pair_lo<KIND>(u[k].x), pair_hi<KIND>(u[k].x));
+                            v[1] = pack2(pair_lo<KIND>(u[k].y), pair_hi<KIND>(u[k].y));
+                            v[2] = pack2(pair_lo<KIND>(u[k].z), pair_hi<KIND>(u[k].z));
+                            v[3] = pack2(pair_lo<KIND>(u[k].w), pair_hi<KIND>(u[k].w));
                         }
+                        uint32_t w[4];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) g.v[i] *= lin_act_slope<ACT>(v.v[i]);
+                        for (int i = 0; i < 4; ++i) {
+                            g[i] = mul2(g[i], lin_act_slope<ACT>(v[i]));
+                            const float2 a = unpack2(g[i]);
+                            w[i] = pack_pair<KIND>(a.x, a.y);
+                        }
                         // read again by the two products that follow: no streaming store
-                        *reinterpret_cast<uint4*>(p.du + 2ll * (r * p.N + col)) = pack8<KIND>(g);
+                        *reinterpret_cast<uint4*>(p.du + 2ll * (r * p.N + col)) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) sum[i] += g.v[i];
+                    for (int i = 0; i < 4; ++i) sum[i] = add2(sum[i], g[i]);
                 }
             }
         }
     if (p.sums == nullptr) return;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) joined[warp][8 * lane + i] = sum[i];
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<float2*>(&joined[warp][8 * lane + 2 * i]) = unpack2(sum[i]);
     __syncthreads();
     const int c = blockIdx.x * kDuColumns + threadIdx.x;
     if (c < p.width) {

@@ -10,96 +10,123 @@ using namespace lf;
 namespace {
 
 // A thread takes eight channels (16 bytes there, 8 here) and the four threads of a group share its maximum.  Bound by DRAM: 3.03
-// bytes a value.  Two pieces a thread, half a grid apart, are in flight together.
-constexpr int kThreads = 256, kPieces = 2;
+// bytes a value.  A thread goes through pieces a grid apart, four of them in flight; only the first one's row is found by a division, and
+// the batch is one long column of rows wherever its stride says so.
+constexpr int kThreads = 256, kPieces = 4;
 
 struct Pack8Params {
     const char* x;
     char* codes;
     unsigned char* scales;
     long long batch, row;          // of x, bytes
-    int N, C, groups;              // groups of 32 in a row
+    int B, N, C, groups;           // groups of 32 in a row
     long long total;               // pieces of eight channels, four to each group, over all rows
 };
 
-struct Piece {
+// The pieces of a thread, one after the other.
+struct Pieces {
     long long row;   // of the dense tensor
-    long long at;    // of x, bytes
-    int piece;       // in the row
-    bool live;
+    int piece, per_row, step_piece;
+    long long step_row;
+    bool flat;       // B == 1
+    __device__ __forceinline__ explicit Pieces(const Pack8Params& p)
+    {
+        per_row = 4 * p.groups;
+        const long long first = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x, step = static_cast<long long>(gridDim.x) * kThreads;
+        row = first / per_row;
+        piece = static_cast<int>(first - row * per_row);
+        step_row = step / per_row;
+        step_piece = static_cast<int>(step - step_row * per_row);
+        flat = p.B == 1;
+    }
+    __device__ __forceinline__ void next()
+    {
+        row += step_row;
+        piece += step_piece;
+        if (piece >= per_row) {
+            piece -= per_row;
+            ++row;
+        }
+    }
+    __device__ __forceinline__ long long at(const Pack8Params& p) const
+    {
+        if (flat) return row * p.row + 16ll * piece;
+        const unsigned int r = static_cast<unsigned int>(row);  // rows are fewer than 2^31
+        return static_cast<long long>(r / p.N) * p.batch + static_cast<long long>(r % p.N) * p.row + 16ll * piece;
+    }
 };
-__device__ __forceinline__ Piece piece_of(const Pack8Params& p, long long i)
-{
-    Piece o;
-    const int per_row = 4 * p.groups;
-    // the totals of all but giant tensors fit 32 bits, where a division is much cheaper
-    if (p.total <= 0x7fffffffll) {
-        const unsigned int r = static_cast<unsigned int>(i) / per_row;
-        o.row = r;
-        o.piece = static_cast<int>(static_cast<unsigned int>(i) - r * per_row);
-        o.at = static_cast<long long>(r / p.N) * p.batch + static_cast<long long>(r % p.N) * p.row;
-    } else {
-        o.row = i / per_row;
-        o.piece = static_cast<int>(i - o.row * per_row);
-        o.at = o.row / p.N * p.batch + o.row % p.N * p.row;
-    }
-    o.at += 16ll * o.piece;
-    o.live = i < p.total && 8 * o.piece < p.C;
-    return o;
-}
 
 template <int KIND>
-__global__ void __launch_bounds__(kThreads) pack8_kernel(Pack8Params p)
+__global__ void __launch_bounds__(kThreads) pack8_kernel(const __grid_constant__ Pack8Params p)
 {
-    const long long step = static_cast<long long>(gridDim.x) * kThreads, first = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
-    Piece q[kPieces];
-    uint4 raw[kPieces];
+    const long long rows = static_cast<long long>(p.B) * p.N;
+    Pieces q(p);
+    while (__any_sync(0xffffffffu, q.row < rows)) {
+        uint4 raw[kPieces];
+        long long row[kPieces];
+        int piece[kPieces];
 #pragma unroll
-    for (int k = 0; k < kPieces; ++k) {
-        q[k] = piece_of(p, first + k * step);
-        raw[k] = q[k].live ? load16(p.x + q[k].at) : make_uint4(0u, 0u, 0u, 0u);
-    }
+        for (int k = 0; k < kPieces; ++k, q.next()) {
+            row[k] = q.row;
+            piece[k] = q.piece;
+            raw[k] = make_uint4(0u, 0u, 0u, 0u);
+            if (q.row < rows && 8 * q.piece < p.C) raw[k] = load16(p.x + q.at(p));
+        }
 #pragma unroll
-    for (int k = 0; k < kPieces; ++k) {
-        const F8 f = unpack8<KIND>(raw[k]);
-        float most = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) most = fmaxf(most, finite_abs(f.v[i]));
-        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-        const int scale = pack8_scale<KIND>(most);
-        if (q[k].live) {
-            const float inverse = pack8_inverse_step(scale);
-            const uint2 c = make_uint2(pack8_codes4(f.v, inverse), pack8_codes4(f.v + 4, inverse));
-            *reinterpret_cast<uint2*>(p.codes + q[k].row * p.C + 8ll * q[k].piece) = c;
-            if ((q[k].piece & 3) == 0) p.scales[q[k].row * p.groups + (q[k].piece >> 2)] = static_cast<unsigned char>(scale);
+        for (int k = 0; k < kPieces; ++k) {
+            f32x2 f[4];
+            f[0] = pack2(pair_lo<KIND>(raw[k].x), pair_hi<KIND>(raw[k].x));
+            f[1] = pack2(pair_lo<KIND>(raw[k].y), pair_hi<KIND>(raw[k].y));
+            f[2] = pack2(pair_lo<KIND>(raw[k].z), pair_hi<KIND>(raw[k].z));
+            f[3] = pack2(pair_lo<KIND>(raw[k].w), pair_hi<KIND>(raw[k].w));
+            const bool plain = all_finite(f);
+            float most = largest(f, plain);
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+            const int scale = pack8_scale<KIND>(most);
+            if (row[k] < rows && 8 * piece[k] < p.C) {
+                uint32_t w[2];
+                pack8_codes(f, most, pack8_inverse_step(scale), plain, w);
+                *reinterpret_cast<uint2*>(p.codes + row[k] * p.C + 8ll * piece[k]) = make_uint2(w[0], w[1]);
+                if ((piece[k] & 3) == 0) p.scales[row[k] * p.groups + (piece[k] >> 2)] = static_cast<unsigned char>(scale);
+            }
         }
     }
 }
 
 template <int KIND>
-__global__ void __launch_bounds__(kThreads) unpack8_kernel(Pack8Params p)
+__global__ void __launch_bounds__(kThreads) unpack8_kernel(const __grid_constant__ Pack8Params p)
 {
-    const long long step = static_cast<long long>(gridDim.x) * kThreads, first = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
-    Piece q[kPieces];
-    uint2 codes[kPieces];
-    int scale[kPieces];
+    const long long rows = static_cast<long long>(p.B) * p.N;
+    Pieces q(p);
+    while (q.row < rows) {
+        uint2 codes[kPieces];
+        int scale[kPieces];
+        long long at[kPieces];
 #pragma unroll
-    for (int k = 0; k < kPieces; ++k) {
-        q[k] = piece_of(p, first + k * step);
-        if (q[k].live) {
-            codes[k] = *reinterpret_cast<const uint2*>(p.codes + q[k].row * p.C + 8ll * q[k].piece);
-            scale[k] = p.scales[q[k].row * p.groups + (q[k].piece >> 2)];
+        for (int k = 0; k < kPieces; ++k, q.next()) {
+            at[k] = -1;
+            if (q.row < rows && 8 * q.piece < p.C) {
+                at[k] = q.at(p);
+                codes[k] = *reinterpret_cast<const uint2*>(p.codes + q.row * p.C + 8ll * q.piece);
+                scale[k] = p.scales[q.row * p.groups + (q.piece >> 2)];
+            }
         }
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k)
+            if (at[k] >= 0) {
+                f32x2 f[4];
+                unpack8_codes4(codes[k].x, pack8_step(scale[k]), f);
+                unpack8_codes4(codes[k].y, pack8_step(scale[k]), f + 2);
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 a = unpack2(f[i]);
+                    w[i] = pack_pair<KIND>(a.x, a.y);
+                }
+                store16(const_cast<char*>(p.x) + at[k], make_uint4(w[0], w[1], w[2], w[3]));
+            }
     }
-#pragma unroll
-    for (int k = 0; k < kPieces; ++k)
-        if (q[k].live) {
-            F8 f;
-            unpack8_codes4(codes[k].x, pack8_step(scale[k]), f.v);
-            unpack8_codes4(codes[k].y, pack8_step(scale[k]), f.v + 4);
-            store16(const_cast<char*>(p.x) + q[k].at, pack8<KIND>(f));
-        }
 }
 
 linfusion_status_t run(const linfusion_pack8_desc_t* d, const linfusion_rows_t* x, const linfusion_packed8_t* packed, bool pack, void* stream)
@@ -120,8 +147,15 @@ linfusion_status_t run(const linfusion_pack8_desc_t* d, const linfusion_rows_t* 
     const Here at = here();
     if (at.st != LINFUSION_OK) return at.st;
     Pack8Params p = {static_cast<const char*>(x->p), static_cast<char*>(packed->codes), static_cast<unsigned char*>(packed->scales),
-                     x->batch * 2, x->row * 2, d->N, d->C, groups, rows * groups * 4};
-    const unsigned int grid = static_cast<unsigned int>((p.total + kThreads * kPieces - 1) / (kThreads * kPieces));
+                     x->batch * 2, x->row * 2, d->B, d->N, d->C, groups, rows * groups * 4};
+    if (d->B > 1 && d->N == 1) p.row = p.batch;
+    if (d->N == 1 || d->B == 1 || x->batch == d->N * x->row) {  // one column of rows
+        p.B = 1;
+        p.N = static_cast<int>(rows);
+    }
+    // as many blocks as run at once, fewer where there is less to do
+    const long long most = (p.total + kThreads - 1) / kThreads;
+    const unsigned int grid = static_cast<unsigned int>(std::min<long long>(most, 8ll * at.sms));
     const bool half = (d->flags & LINFUSION_DTYPE_FP16) != 0u;
     constexpr int bf = make_kind(kPhiIdentity, kDtypeBf16), hf = make_kind(kPhiIdentity, kDtypeFp16);
     cudaStream_t s = static_cast<cudaStream_t>(stream);

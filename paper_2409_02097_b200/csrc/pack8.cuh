@@ -49,53 +49,77 @@ __device__ __forceinline__ uint32_t pack8_codes4(const float* x, float inverse)
     return __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
 }
 
-// The 32 values of a group -> their codes and the scale byte.  Where all are finite and the scale is not held to its most, which is
-// nearly always, a code is the low byte of one fma: x * 2^-e is exact and the sum with 1.5 * 2^23 rounds once.
-template <int KIND>
-__device__ __forceinline__ int pack8_group(const float (&x)[32], uint32_t (&w)[8])
+// Whether 2 * P values are all finite: 0 * x is NaN where one is not.
+template <int P>
+__device__ __forceinline__ bool all_finite(const f32x2 (&x)[P])
 {
-    float most = fabsf(x[0]);
-    f32x2 odd = both(0.0f);  // NaN where a value is not finite
+    f32x2 odd = both(0.0f);
 #pragma unroll
-    for (int i = 1; i < 32; ++i) most = fmaxf(most, fabsf(x[i]));
+    for (int i = 0; i < P; ++i) odd = fma2(x[i], both(0.0f), odd);
+    return sum2(odd) == 0.0f;
+}
+// Four values -> four codes where all are finite and none passes 127 steps, which is nearly always: a code is the low byte of one
+// fma, since x * 2^-e is exact and the sum with 1.5 * 2^23 rounds once.
+__device__ __forceinline__ uint32_t pack8_codes4_plain(f32x2 x, f32x2 y, float inverse)
+{
+    const float2 a = unpack2(fma2(x, both(inverse), both(12582912.0f))), b = unpack2(fma2(y, both(inverse), both(12582912.0f)));
+    return __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040), __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
+}
+// The largest magnitude of 2 * P values, of the finite ones where not all are.
+template <int P>
+__device__ __forceinline__ float largest(const f32x2 (&x)[P], bool plain)
+{
+    float most = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 32; i += 2) odd = fma2(pack2(x[i], x[i + 1]), both(0.0f), odd);
-    const bool plain = sum2(odd) == 0.0f;
+    for (int i = 0; i < P; ++i) {
+        const float2 a = unpack2(x[i]);
+        most = fmaxf(most, fmaxf(fabsf(a.x), fabsf(a.y)));
+    }
     if (!plain) {
         most = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) most = fmaxf(most, finite_abs(x[i]));
+        for (int i = 0; i < P; ++i) {
+            const float2 a = unpack2(x[i]);
+            most = fmaxf(most, fmaxf(finite_abs(a.x), finite_abs(a.y)));
+        }
     }
-    const int scale = pack8_scale<KIND>(most);
-    const float inverse = pack8_inverse_step(scale);
+    return most;
+}
+// 2 * P values -> codes, four in a word; plain: all finite.
+template <int P>
+__device__ __forceinline__ void pack8_codes(const f32x2 (&x)[P], float most, float inverse, bool plain, uint32_t (&w)[P / 2])
+{
     if (plain && most * inverse <= 127.0f) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const f32x2 k = both(12582912.0f), s = both(inverse);
-            const f32x2 a = fma2(pack2(x[4 * j], x[4 * j + 1]), s, k), b = fma2(pack2(x[4 * j + 2], x[4 * j + 3]), s, k);
-            const float2 fa = unpack2(a), fb = unpack2(b);
-            w[j] = __byte_perm(__byte_perm(__float_as_uint(fa.x), __float_as_uint(fa.y), 0x0040),
-                               __byte_perm(__float_as_uint(fb.x), __float_as_uint(fb.y), 0x0040), 0x5410);
-        }
+        for (int j = 0; j < P / 2; ++j) w[j] = pack8_codes4_plain(x[2 * j], x[2 * j + 1], inverse);
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = pack8_codes4(x + 4 * j, inverse);
+        for (int j = 0; j < P / 2; ++j) {
+            const float2 a = unpack2(x[2 * j]), b = unpack2(x[2 * j + 1]);
+            const float f[4] = {a.x, a.y, b.x, b.y};
+            w[j] = pack8_codes4(f, inverse);
+        }
     }
-    return scale;
 }
 
 // Four codes -> four values.  A code's byte with its top bit turned over, as the low byte of a float of 2^23, is 2^23 + 128 +
 // code; the difference and the product are exact.  (One fma for both would overflow for steps above 2^104.)
-__device__ __forceinline__ void unpack8_codes4(uint32_t word, float step, float* x)
+__device__ __forceinline__ void unpack8_codes4(uint32_t word, float step, f32x2* x)
 {
     const uint32_t w = word ^ 0x80808080u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = (__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7540 + i)) - 8388736.0f) * step;
+    const auto offset = [&](int i) { return __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7540 + i)); };
+    x[0] = mul2(add2(pack2(offset(0), offset(1)), both(-8388736.0f)), both(step));
+    x[1] = mul2(add2(pack2(offset(2), offset(3)), both(-8388736.0f)), both(step));
     // a byte of w that is zero was the code -128
     if (((w - 0x01010101u) & ~w & 0x80808080u) != 0u) {
+        float f[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (((word >> (8 * i)) & 0xffu) == 0x80u) x[i] = __uint_as_float(0x7fffffffu);
+        for (int i = 0; i < 4; ++i) {
+            const float2 a = unpack2(x[i / 2]);
+            f[i] = ((word >> (8 * i)) & 0xffu) == 0x80u ? __uint_as_float(0x7fffffffu) : i % 2 == 0 ? a.x : a.y;
+        }
+        x[0] = pack2(f[0], f[1]);
+        x[1] = pack2(f[2], f[3]);
     }
 }
 

@@ -213,10 +213,7 @@ template <int KIND, int R, bool PACKED>
 __device__ __forceinline__ void rec_values(const RecRaw<R, PACKED>& raw, int r, int lane, f32x2 (&v)[kRecP])
 {
     if constexpr (PACKED) {
-        float f[4];
-        unpack8_codes4(raw.w[r][0], pack8_step(__shfl_sync(0xffffffffu, raw.scale, (lane & 24) | r)), f);
-        v[0] = pack2(f[0], f[1]);
-        v[1] = pack2(f[2], f[3]);
+        unpack8_codes4(raw.w[r][0], pack8_step(__shfl_sync(0xffffffffu, raw.scale, (lane & 24) | r)), v);
     } else {
 #pragma unroll
         for (int i = 0; i < kRecP; ++i) v[i] = pack2(pair_lo<KIND>(raw.w[r][i % (PACKED ? 1 : 2)]), pair_hi<KIND>(raw.w[r][i % (PACKED ? 1 : 2)]));
