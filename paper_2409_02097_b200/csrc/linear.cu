@@ -282,14 +282,15 @@ linfusion_status_t product(const Product& plan, int M, int N, int K, const Opera
 }
 
 template <int KIND, bool PACKED>
-void launch_du(const DuParams& p, int act, dim3 grid, cudaStream_t s)
+cudaError_t launch_du(const DuParams& p, int act, dim3 grid, cudaStream_t s)
 {
+    const dim3 block(kDuThreads);
     switch (act) {
-        case LINFUSION_ACT_RELU: linear_du_kernel<KIND, 1, PACKED><<<grid, kDuThreads, 0, s>>>(p); break;
-        case LINFUSION_ACT_SILU: linear_du_kernel<KIND, 2, PACKED><<<grid, kDuThreads, 0, s>>>(p); break;
-        case LINFUSION_ACT_GELU: linear_du_kernel<KIND, 3, PACKED><<<grid, kDuThreads, 0, s>>>(p); break;
-        case LINFUSION_ACT_GELU_TANH: linear_du_kernel<KIND, 4, PACKED><<<grid, kDuThreads, 0, s>>>(p); break;
-        default: linear_du_kernel<KIND, 0, false><<<grid, kDuThreads, 0, s>>>(p); break;
+        case LINFUSION_ACT_RELU: return launch_pdl(linear_du_kernel<KIND, 1, PACKED>, grid, block, 0, s, p);
+        case LINFUSION_ACT_SILU: return launch_pdl(linear_du_kernel<KIND, 2, PACKED>, grid, block, 0, s, p);
+        case LINFUSION_ACT_GELU: return launch_pdl(linear_du_kernel<KIND, 3, PACKED>, grid, block, 0, s, p);
+        case LINFUSION_ACT_GELU_TANH: return launch_pdl(linear_du_kernel<KIND, 4, PACKED>, grid, block, 0, s, p);
+        default: return launch_pdl(linear_du_kernel<KIND, 0, false>, grid, block, 0, s, p);
     }
 }
 
@@ -447,15 +448,12 @@ linfusion_status_t linfusion_linear_backward(const linfusion_linear_desc_t* desc
         p.rows_per_block = plan.sums.rows;
         p.scale_groups = scale_groups(d.N);
         const dim3 grid(plan.sums.columns, plan.sums.blocks);
-        if (half && u_packed) launch_du<kHf, true>(p, d.act, grid, s);
-        else if (half) launch_du<kHf, false>(p, d.act, grid, s);
-        else if (u_packed) launch_du<kBf, true>(p, d.act, grid, s);
-        else launch_du<kBf, false>(p, d.act, grid, s);
-        cudaError_t err = cudaGetLastError();
-        if (err == cudaSuccess && dbias != nullptr) {
-            column_sums_kernel<<<plan.sums.width / kSumChannels, kSumThreads, 0, s>>>(p.sums, dbias, plan.sums.blocks, plan.sums.width, d.N);
-            err = cudaGetLastError();
-        }
+        cudaError_t err;
+        if (half) err = u_packed ? launch_du<kHf, true>(p, d.act, grid, s) : launch_du<kHf, false>(p, d.act, grid, s);
+        else err = u_packed ? launch_du<kBf, true>(p, d.act, grid, s) : launch_du<kBf, false>(p, d.act, grid, s);
+        if (err == cudaSuccess && dbias != nullptr)
+            err = launch_pdl(column_sums_kernel, dim3(plan.sums.width / kSumChannels), dim3(kSumThreads), 0, s, p.sums, dbias, plan.sums.blocks,
+                             plan.sums.width, d.N);
         if (err != cudaSuccess) return end(err);
         if (act) du = {ws + plan.du, d.N};
     }

@@ -686,6 +686,8 @@ __global__ void __launch_bounds__(kDuThreads, 3) linear_du_kernel(const __grid_c
     f32x2 sum[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) sum[i] = both(0.0f);
+    pdl_wait();
+    pdl_launch_dependents();
     if (live)
         for (long long r0 = first + warp; r0 < end; r0 += kDuUnroll * (kDuThreads / 32)) {
             uint4 dy[kDuUnroll], u[kDuUnroll];

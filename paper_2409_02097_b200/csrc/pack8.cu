@@ -61,6 +61,8 @@ __global__ void __launch_bounds__(kThreads) pack8_kernel(const __grid_constant__
 {
     const long long rows = static_cast<long long>(p.B) * p.N;
     Pieces q(p);
+    pdl_wait();
+    pdl_launch_dependents();
     while (__any_sync(0xffffffffu, q.row < rows)) {
         uint4 raw[kPieces];
         long long row[kPieces];
@@ -99,6 +101,8 @@ __global__ void __launch_bounds__(kThreads) unpack8_kernel(const __grid_constant
 {
     const long long rows = static_cast<long long>(p.B) * p.N;
     Pieces q(p);
+    pdl_wait();
+    pdl_launch_dependents();
     while (q.row < rows) {
         uint2 codes[kPieces];
         int scale[kPieces];
@@ -159,14 +163,10 @@ linfusion_status_t run(const linfusion_pack8_desc_t* d, const linfusion_rows_t* 
     const bool half = (d->flags & LINFUSION_DTYPE_FP16) != 0u;
     constexpr int bf = make_kind(kPhiIdentity, kDtypeBf16), hf = make_kind(kPhiIdentity, kDtypeFp16);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (pack) {
-        if (half) pack8_kernel<hf><<<grid, kThreads, 0, s>>>(p);
-        else pack8_kernel<bf><<<grid, kThreads, 0, s>>>(p);
-    } else {
-        if (half) unpack8_kernel<hf><<<grid, kThreads, 0, s>>>(p);
-        else unpack8_kernel<bf><<<grid, kThreads, 0, s>>>(p);
-    }
-    return end(cudaGetLastError());
+    cudaError_t e;
+    if (pack) e = half ? launch_pdl(pack8_kernel<hf>, dim3(grid), dim3(kThreads), 0, s, p) : launch_pdl(pack8_kernel<bf>, dim3(grid), dim3(kThreads), 0, s, p);
+    else e = half ? launch_pdl(unpack8_kernel<hf>, dim3(grid), dim3(kThreads), 0, s, p) : launch_pdl(unpack8_kernel<bf>, dim3(grid), dim3(kThreads), 0, s, p);
+    return end(e);
 }
 
 }  // namespace

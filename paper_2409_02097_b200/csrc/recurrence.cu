@@ -240,11 +240,9 @@ linfusion_status_t linfusion_recurrence(const linfusion_recurrence_desc_t* desc,
         if (grid > INT32_MAX) return LINFUSION_ERR_UNSUPPORTED;
         const unsigned int g = static_cast<unsigned int>(grid);
         const bool half = (d.flags & LINFUSION_DTYPE_FP16) != 0u;
-        if (half && gated) recurrence_short_kernel<kHf, true><<<g, kRecShortThreads, 0, s>>>(p);
-        else if (half) recurrence_short_kernel<kHf, false><<<g, kRecShortThreads, 0, s>>>(p);
-        else if (gated) recurrence_short_kernel<kBf, true><<<g, kRecShortThreads, 0, s>>>(p);
-        else recurrence_short_kernel<kBf, false><<<g, kRecShortThreads, 0, s>>>(p);
-        return end(cudaGetLastError());
+        const dim3 block(kRecShortThreads);
+        if (half) return end(gated ? launch_pdl(recurrence_short_kernel<kHf, true>, dim3(g), block, 0, s, p) : launch_pdl(recurrence_short_kernel<kHf, false>, dim3(g), block, 0, s, p));
+        return end(gated ? launch_pdl(recurrence_short_kernel<kBf, true>, dim3(g), block, 0, s, p) : launch_pdl(recurrence_short_kernel<kBf, false>, dim3(g), block, 0, s, p));
     }
     cudaError_t e = cudaSuccess;
     if (plan.tiles > 1) {
@@ -332,9 +330,8 @@ linfusion_status_t linfusion_recurrence_backward(const linfusion_recurrence_desc
     const bool half = (d.flags & LINFUSION_DTYPE_FP16) != 0u;
     e = half ? launch_backward<kHf>(p, gated, packed, s) : launch_backward<kBf>(p, gated, packed, s);
     if (e == cudaSuccess && grads->rate != nullptr) {
-        column_sums_kernel<<<plan.width / kSumChannels, kSumThreads, 0, s>>>(p.rate_partials, grads->rate, static_cast<long long>(d.B) * plan.tiles,
-                                                          plan.width, d.C);
-        e = cudaGetLastError();
+        e = launch_pdl(column_sums_kernel, dim3(plan.width / kSumChannels), dim3(kSumThreads), 0, s, p.rate_partials, grads->rate,
+                       static_cast<long long>(d.B) * plan.tiles, plan.width, d.C);
     }
     return end(e);
 }

@@ -535,6 +535,7 @@ __global__ void __launch_bounds__(kRecShortThreads) recurrence_short_kernel(cons
 {
     const long long i = static_cast<long long>(blockIdx.x) * kRecShortThreads + threadIdx.x;
     const int pairs = p.C / 2, b = static_cast<int>(i / pairs), ch = 2 * static_cast<int>(i - static_cast<long long>(b) * pairs);
+    pdl_wait();
     if (b >= p.B) return;
     f32x2 rate, h = both(0.0f);
     rec_load_rates<2>(&rate, p.rate + ch);

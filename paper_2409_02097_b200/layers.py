@@ -354,7 +354,8 @@ class GatedRecurrence(_Fixed):
                 return self.forward(x, decay, rate, gate, h0, save, h, last, state, workspace)
         if state is not None and not save:
             raise ValueError("state is given, but not save")
-        key = (0, _look(x), _look(decay), _look(gate), _look(rate), _look(h0), _look(h), _look(last), _look(state))
+        key = (x.shape, x.stride(), x.dtype, decay.shape, decay.stride(), decay.dtype, x.get_device(), decay.get_device(), _look(gate), _look(rate), _look(h0),
+               _look(h), _look(last), _look(state))
         found = self._checked.get(key)
         if found is None:
             found = self._checked.keep(key, self._check(x, decay, gate, rate, h0, (("h", h),), (("last", last), ("state", state)), False))
@@ -367,7 +368,7 @@ class GatedRecurrence(_Fixed):
             rows = _copy(outs[0])
         rows.p = h.data_ptr()
         if last is None:
-            last = torch.empty((B, C), dtype=torch.float32, device=device)
+            last = torch.empty((B, C), dtype=torch.float32, device=device) if h0 is None else torch.empty_like(h0)
         if save and state is None:
             state = torch.empty(self.state_shape(B, N), dtype=torch.float32, device=device)
         ws = self._workspace(workspace, need, device)
@@ -540,14 +541,14 @@ class Linear(_Fixed):
         if stream is not None and x.is_cuda:
             with allocating_on(stream, x.get_device()):
                 return self.forward(x, w, bias, residual, save, y, u, workspace)
-        key = (0, _look(x), _look(w), _look(bias), _look(residual), _look(y), _look8(u))
+        key = (x.shape, x.stride(), x.dtype, w.shape, w.stride(), w.dtype, x.get_device(), w.get_device(), _look(bias), _look(residual), _look(y), _look8(u))
         found = self._checked.get(key)
         if found is None:
             found = self._checked.keep(key, self._check_forward(x, w, bias, residual, y, u))
         desc, mx, mw, mr, my, mu, shape, need = found
         device = x.device
         if y is None:
-            y = torch.empty(shape, dtype=self._torch_dtype, device=device)
+            y = torch.empty(shape, dtype=self._torch_dtype, device=device) if residual is None else _like(residual)
         packed = None
         if save == "packed":
             if u is None:
