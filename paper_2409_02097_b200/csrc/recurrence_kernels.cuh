@@ -404,7 +404,7 @@ template <bool GRAD>
 __global__ void __launch_bounds__(kRecScanChannels* kRecScanRuns) recurrence_scan_kernel(const float2* __restrict__ maps, const float* __restrict__ first,
                                                                                         float* __restrict__ enters, int tiles, int width, int C)
 {
-    __shared__ float2 runs[kRecScanRuns][kRecScanChannels];
+    __shared__ float2 both_runs[2][kRecScanRuns][kRecScanChannels];
     const int c = threadIdx.x % kRecScanChannels, run = threadIdx.x / kRecScanChannels, ch = static_cast<int>(blockIdx.x % (width / kRecScanChannels)) * kRecScanChannels + c,
               b = static_cast<int>(blockIdx.x / (width / kRecScanChannels));
     pdl_wait();
@@ -422,13 +422,15 @@ __global__ void __launch_bounds__(kRecScanChannels* kRecScanRuns) recurrence_sca
             if (k + j < k1) own = make_float2(own.x * m[j].x, fmaf(m[j].x, own.y, m[j].y));
     }
     // the runs' maps, each with all before it, by doubling
-    for (int n = 1; n < kRecScanRuns; n *= 2) {
-        runs[run][c] = own;
+    int side = 0;
+#pragma unroll
+    for (int n = 1; n < kRecScanRuns; n *= 2, side ^= 1) {
+        both_runs[side][run][c] = own;
         __syncthreads();
-        const float2 before = runs[run >= n ? run - n : run][c];
+        const float2 before = both_runs[side][run >= n ? run - n : run][c];
         if (run >= n) own = make_float2(before.x * own.x, fmaf(own.x, before.y, own.y));
-        __syncthreads();
     }
+    float2 (&runs)[kRecScanRuns][kRecScanChannels] = both_runs[side];
     runs[run][c] = own;
     __syncthreads();
     if (ch >= C) return;
