@@ -8,8 +8,7 @@ namespace lf {
 // Partial sums of the blocks of a kernel, joined channel by channel: 16 channels x 64 threads a block, each thread every 64th row, then
 // the threads in pairs, always the same.
 constexpr int kSumChannels = 16, kSumThreads = 1024;
-static __global__ void __launch_bounds__(kSumThreads) column_sums_kernel(const float* __restrict__ partials, float* __restrict__ out,
-                                                                         long long rows, int width, int C)
+static __global__ void __launch_bounds__(kSumThreads) column_sums_kernel(const float* partials, float* out, long long rows, int width, int C)
 {
     constexpr int lanes = kSumThreads / kSumChannels;
     __shared__ float sums[lanes][kSumChannels];

@@ -17,7 +17,9 @@
 //
 // What bounds it: an SM takes in about 64 bytes a cycle, 256 rows of 128 bytes a chunk in 512 cycles, which is also what the matrix
 // instructions of a 256 x 256 tile take.  Narrower tiles load nearly as much for half the products; they serve where there
-// are few tiles.
+// are few tiles.  Measured (M x K x N, bf16): 32768 x 640 x 2560 89 us (1200 TFLOP/s; cuBLAS 87), with gelu 94 to 99, with gelu and the
+// pre-activation in 8 bits 121 to 127 and in 16 bits 117; 8192 x 1280 x 5120 79 us (1360 TFLOP/s; 84); 8192 x 1280 x 1280 24 us
+// (21); 128 x 1280 x 1280 6.0 us (3.8).  Of a small call's time 3 us are the launch, the first loads and the last tile's way out.
 #pragma once
 
 #include "block_kernels.cuh"
@@ -483,7 +485,11 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
             if (in_group < kLinColumns) {
                 const int col = col0 + in_group;
                 float b = 0.0f;
-                if (p.bias != nullptr && col < p.N) b = pair_lo<KIND>(__ldg(reinterpret_cast<const unsigned short*>(p.bias) + col));
+                if (p.bias != nullptr && col < p.N) {
+                    unsigned short w;  // a plain load: what was there when this kernel began may have been written over since
+                    asm volatile("ld.global.u16 %0, [%1];" : "=h"(w) : "l"(p.bias + 2ll * col) : "memory");
+                    b = pair_lo<KIND>(w);
+                }
                 asm volatile("st.shared.f32 [%0], %1;" ::"r"(bias + 4 * in_group), "f"(b) : "memory");
             }
             good = good && lin_wait(acc_full + 8 * buf, (n >> 1) & 1);
@@ -664,8 +670,10 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
 
 // ------------------------------------------------------------------------------------------ before the backward products
 // du = dy act'(u), rounded once to the 16 bits that the products take, and its sums over the rows from the unrounded values.
-// A block takes 256 columns, a thread eight of them; eight rows at a time, four times unrolled.  Bound by DRAM: six bytes a value, five
-// where u is a checkpoint, two where there is no activation (the sums alone).
+// A block takes 256 columns, a thread eight of them; eight rows at a time, four times unrolled; blocks that all run at once (600 of them in
+// two rounds took 118 us where 440 take 99).  Six bytes a value, five where u is a checkpoint, two where there is no activation (the sums
+// alone).  32768 x 2560 with gelu: 99 us, 110 from a checkpoint (77 and 64 at the copy rate); its 20 to 25 instructions a value keep
+// the issue slots as busy as DRAM.
 constexpr int kDuThreads = 256, kDuColumns = 256, kDuUnroll = 4;
 struct DuParams {
     const char *dy, *u;

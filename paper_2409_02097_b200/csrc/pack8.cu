@@ -11,7 +11,7 @@ namespace {
 
 // A thread takes eight channels (16 bytes there, 8 here) and the four threads of a group share its maximum.  Bound by DRAM: 3.03
 // bytes a value.  A thread goes through pieces a grid apart, four of them in flight; only the first one's row is found by a division, and
-// the batch is one long column of rows wherever its stride says so.
+// the batch is one long column of rows wherever its stride says so.  61441 x 648: 28 us there, 25 us back (18.4 each at the copy rate).
 constexpr int kThreads = 256, kPieces = 4;
 
 struct Pack8Params {

@@ -23,7 +23,7 @@ linfusion_status_t check(const linfusion_recurrence_desc_t* d)
 // The tiles of a call, and where the parts of its workspace are.
 struct Plan {
     int slabs, tiles, width;
-    size_t maps, enters, kept, rate, bytes;
+    size_t maps, grad_maps, enters, kept, rate, bytes;
 };
 // `backward`: with the rates' sums; `kept`: room for the states that a backward pass recomputes.
 Plan make_plan(const linfusion_recurrence_desc_t& d, bool backward, bool kept)
@@ -34,7 +34,10 @@ Plan make_plan(const linfusion_recurrence_desc_t& d, bool backward, bool kept)
     p.width = p.slabs * kRecSlab;
     const size_t rows = static_cast<size_t>(d.B) * p.tiles;
     const bool many = p.tiles > 1;
-    p.enters = many ? align_up_256(rows * p.width * sizeof(float2)) : 0;
+    // maps of the state, and of the gradient behind them where both are formed; else in their place
+    const size_t maps = many ? align_up_256(rows * p.width * sizeof(float2)) : 0;
+    p.grad_maps = backward && kept ? maps : 0;
+    p.enters = p.grad_maps + maps;
     p.kept = p.enters + (many ? align_up_256(rows * d.C * sizeof(float)) : 0);
     p.rate = p.kept + (many && kept ? align_up_256(rows * d.C * sizeof(float)) : 0);
     p.bytes = p.rate + (backward ? align_up_256(rows * p.width * sizeof(float)) : 0);
@@ -128,28 +131,28 @@ constexpr int kBf = make_kind(kPhiIdentity, kDtypeBf16), kHf = make_kind(kPhiIde
 
 dim3 blocks(const RecParams& p) { return dim3(p.slabs, p.stacks > 1 ? kRecTilesY : p.tiles, p.B * p.stacks); }
 
-template <int KIND>
-cudaError_t launch_maps(const RecParams& p, bool gated, bool packed, bool grad, cudaStream_t s)
+template <int KIND, int WHAT>
+cudaError_t launch_maps(const RecParams& p, bool gated, bool packed, cudaStream_t s)
 {
+    constexpr bool state = (WHAT & kRecMapState) != 0;  // the gradient's maps need no gate
     const dim3 grid = blocks(p), block(kRecMapsThreads);
-    if (grad)
-        return packed ? launch_pdl(recurrence_maps_kernel<KIND, false, true, true>, grid, block, 0, s, p)
-                      : launch_pdl(recurrence_maps_kernel<KIND, false, false, true>, grid, block, 0, s, p);
-    if (gated)
-        return packed ? launch_pdl(recurrence_maps_kernel<KIND, true, true, false>, grid, block, 0, s, p)
-                      : launch_pdl(recurrence_maps_kernel<KIND, true, false, false>, grid, block, 0, s, p);
-    return packed ? launch_pdl(recurrence_maps_kernel<KIND, false, true, false>, grid, block, 0, s, p)
-                  : launch_pdl(recurrence_maps_kernel<KIND, false, false, false>, grid, block, 0, s, p);
+    constexpr bool may = WHAT != kRecMapState;          // be packed: the forward pass reads 16 bits
+    if (state && gated)
+        return may && packed ? launch_pdl(recurrence_maps_kernel<KIND, state, may, WHAT>, grid, block, 0, s, p)
+                             : launch_pdl(recurrence_maps_kernel<KIND, state, false, WHAT>, grid, block, 0, s, p);
+    return may && packed ? launch_pdl(recurrence_maps_kernel<KIND, false, may, WHAT>, grid, block, 0, s, p)
+                         : launch_pdl(recurrence_maps_kernel<KIND, false, false, WHAT>, grid, block, 0, s, p);
 }
-// What enters each tile: the maps, then the way from tile to tile.  GRAD: the gradient, else the state.
-template <bool GRAD>
-cudaError_t launch_enters(const linfusion_recurrence_desc_t& d, const RecParams& p, bool gated, bool packed, const float* first, float* enters, cudaStream_t s)
+// What enters each tile: the maps, then the way from tile to tile, of the state, the gradient or both.
+template <int WHAT>
+cudaError_t launch_enters(const linfusion_recurrence_desc_t& d, const RecParams& p, bool gated, bool packed, float* states, float* grads, cudaStream_t s)
 {
     const bool half = (d.flags & LINFUSION_DTYPE_FP16) != 0u;
-    const cudaError_t e = half ? launch_maps<kHf>(p, gated, packed, GRAD, s) : launch_maps<kBf>(p, gated, packed, GRAD, s);
+    const cudaError_t e = half ? launch_maps<kHf, WHAT>(p, gated, packed, s) : launch_maps<kBf, WHAT>(p, gated, packed, s);
     if (e != cudaSuccess) return e;
-    const dim3 grid(static_cast<unsigned int>(p.width / kRecScanChannels) * p.B), block(kRecScanChannels * kRecScanRuns);
-    return launch_pdl(recurrence_scan_kernel<GRAD>, grid, block, 0, s, p.maps, first, enters, p.tiles, p.width, p.C);
+    const RecScan state = {p.maps, p.h0, states, 0}, grad = {p.grad_maps, p.dlast, grads, 1};
+    const dim3 grid(static_cast<unsigned int>(p.width / kRecScanChannels) * p.B, WHAT == kRecMapBoth ? 2 : 1), block(kRecScanChannels * kRecScanRuns);
+    return launch_pdl(recurrence_scan_kernel, grid, block, 0, s, WHAT == kRecMapGrad ? grad : state, grad, p.tiles, p.width, p.C);
 }
 template <int KIND>
 cudaError_t launch_backward(const RecParams& p, bool gated, bool packed, cudaStream_t s)
@@ -247,7 +250,7 @@ linfusion_status_t linfusion_recurrence(const linfusion_recurrence_desc_t* desc,
     cudaError_t e = cudaSuccess;
     if (plan.tiles > 1) {
         float* enters = state != nullptr ? state : reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.enters);
-        e = launch_enters<false>(d, p, gated, false, h0, enters, s);
+        e = launch_enters<kRecMapState>(d, p, gated, false, enters, nullptr, s);
         if (e != cudaSuccess) return end(e);
         p.states = enters;
     }
@@ -316,14 +319,15 @@ linfusion_status_t linfusion_recurrence_backward(const linfusion_recurrence_desc
     p.rate_partials = grads->rate != nullptr ? reinterpret_cast<float*>(ws + plan.rate) : nullptr;
     p.states = state;
     if (plan.tiles > 1) {
+        float* enters = reinterpret_cast<float*>(ws + plan.enters);
+        p.grad_maps = reinterpret_cast<float2*>(ws + plan.grad_maps);
         if (state == nullptr) {
             float* kept_states = reinterpret_cast<float*>(ws + plan.kept);
-            e = launch_enters<false>(d, p, gated, packed, h0, kept_states, s);
-            if (e != cudaSuccess) return end(e);
+            e = launch_enters<kRecMapBoth>(d, p, gated, packed, kept_states, enters, s);
             p.states = kept_states;
+        } else {
+            e = launch_enters<kRecMapGrad>(d, p, gated, packed, nullptr, enters, s);
         }
-        float* enters = reinterpret_cast<float*>(ws + plan.enters);
-        e = launch_enters<true>(d, p, gated, packed, dlast, enters, s);
         if (e != cudaSuccess) return end(e);
         p.grads = enters;
     }

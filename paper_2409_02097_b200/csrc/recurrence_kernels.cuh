@@ -5,18 +5,18 @@
 // h + e (v - h) with e formed without cancellation: near e = 0 (long memories) 1 - e has lost e's digits, and a product of
 // thousands of such factors would show it.
 //
-// Three launches.  recurrence_maps_kernel forms the map of every tile of 64 tokens, recurrence_scan_kernel goes through the
-// tiles of each channel (a run of them a thread, then the runs' maps, then the run again with what enters it) and leaves the state that
-// enters each tile, which is what the backward pass keeps; recurrence_kernel and recurrence_backward_kernel then do every tile
-// by itself.  Sums and products have a fixed order, nothing waits for another block.  The price is that inputs are read
-// twice: 14 bytes a value instead of 8 forward, 18 instead of 14 backward (the maps need decay and dh alone; the states are kept), but the
-// second time from L2 where they fit.  The one-pass form, in which a tile waits for the maps of the tiles before it while its own inputs
-// stay in registers, was built first and was slower: 363 against 263 us forward for 131072 x 640, 49 against 42 for 2 x 4096 x 1280, and
-// 145 against 110 backward for 2 x 16384 x 640; its blocks spent two thirds of their time waiting or at barriers, and registers allow
-// but two on an SM.
+// Three launches.  recurrence_maps_kernel forms the map of every tile of 64 tokens (in a backward pass without kept states those of the
+// states and of the gradient at once), recurrence_scan_kernel goes through the tiles of each channel (a run of them a thread, then the
+// runs' maps, then the run again with what enters it) and leaves what enters each tile, which is also what a forward pass keeps;
+// recurrence_kernel and recurrence_backward_kernel then do every tile by itself.  Sums and products have a fixed order, nothing waits for
+// another block.  The price is that inputs are read twice: 14 bytes a value instead of 8 forward, 18 instead of 14 backward (the maps need
+// decay and dh alone; the states are kept), but the second time from L2 where they fit.  The one-pass form, in which a tile waits for the
+// maps of the tiles before it while its own inputs stay in registers, was built first and was slower: 363 against 265 us forward for
+// 131072 x 640, 49 against 42 for 2 x 4096 x 1280, and 145 against 108 backward for 2 x 16384 x 640; its blocks spent two thirds of
+// their time waiting or at barriers, and registers allow but two on an SM.
 //
-// What bounds it now: issue slots, not DRAM (30 to 40 % of its rate).  A value takes 30 instructions in the maps, 42 in the forward pass
-// and 75 in the backward pass, of which the arithmetic proper is half; it runs on pairs of fp32 values.
+// What bounds it now: issue slots, not DRAM (15 to 40 % of its rate): a value takes 30 instructions in the maps, 36 in the forward pass and
+// 72 in the backward pass (89 from checkpoints), of which the arithmetic proper is half; it runs on pairs of fp32 values.
 #pragma once
 
 #include "column_sums.cuh"
@@ -44,7 +44,7 @@ struct RecParams {
     const float *rate, *h0, *dlast;
     const float* states;          // [B][tiles][C]: what enters each tile (null: one tile, h0 does)
     const float* grads;           // [B][tiles][C]: the gradient that enters each tile from behind (null: one tile, dlast does)
-    float2* maps;                 // [B][tiles][width]
+    float2 *maps, *grad_maps;     // [B][tiles][width]
     float *last, *dh0, *rate_partials, *keep;  // keep: where the state that enters the only tile is left
     int B, N, C, slabs, tiles, stacks, width, scale_groups, reverse;  // width: channels in whole slabs; stacks: see RecPlace
 };
@@ -324,12 +324,31 @@ __device__ __forceinline__ void rec_arrive(f32x2 (&h)[kRecP], const float2* befo
 __device__ __forceinline__ f32x2 rec_minus(f32x2 a, f32x2 b) { return fma2(b, both(-1.0f), a); }
 
 // ------------------------------------------------------------------------------------------ maps of the tiles
-// GRAD: of the gradient (from decay and dh, backward in the tokens); else of the state (from x, decay and gate).
-template <int KIND, bool GATE, bool PACKED, bool GRAD>
-__global__ void __launch_bounds__(kRecMapsThreads, 6) recurrence_maps_kernel(const __grid_constant__ RecParams p)
+// Of the state (from x, decay and gate), of the gradient (from decay and dh, backward in the tokens), or both at once.
+enum : int { kRecMapState = 1, kRecMapGrad = 2, kRecMapBoth = 3 };
+
+// The map of a tile from those of its threads' segments: those of a warp, then the warps'.  UP: in the order of the tokens.
+template <bool UP, int WARPS>
+__device__ __forceinline__ void rec_tile_map(f32x2 (&A)[kRecP], f32x2 (&H)[kRecP], float2 (&totals)[WARPS][kRecSlab], int lane, int warp, int cl)
 {
-    constexpr int R = kRecMapsR;
-    __shared__ __align__(16) float2 totals[rec_warps(R)][kRecSlab];
+#pragma unroll
+    for (int i = 0; i < kRecP; ++i)
+#pragma unroll
+        for (int off = 1; off < kRecSegs; off *= 2) {
+            const f32x2 a = __shfl_xor_sync(0xffffffffu, A[i], off * kRecLanes), h = __shfl_xor_sync(0xffffffffu, H[i], off * kRecLanes);
+            const bool second = ((lane / kRecLanes) & off) != 0;
+            H[i] = second == UP ? fma2(A[i], h, H[i]) : fma2(a, H[i], h);
+            A[i] = mul2(A[i], a);
+        }
+    if (lane < kRecLanes) rec_put(&totals[warp][cl], A, H);
+}
+
+template <int KIND, bool GATE, bool PACKED, int WHAT>
+__global__ void __launch_bounds__(kRecMapsThreads, WHAT == kRecMapBoth ? 4 : 6) recurrence_maps_kernel(const __grid_constant__ RecParams p)
+{
+    constexpr int R = kRecMapsR, WARPS = rec_warps(R);
+    constexpr bool STATE = (WHAT & kRecMapState) != 0, GRAD = (WHAT & kRecMapGrad) != 0;
+    __shared__ __align__(16) float2 totals[2][WARPS][kRecSlab];
     const RecPlace<R> at(p);
     pdl_wait();
     pdl_launch_dependents();
@@ -337,9 +356,9 @@ __global__ void __launch_bounds__(kRecMapsThreads, 6) recurrence_maps_kernel(con
     RecRaw<R, false> y;
     rec_read(d, p.decay, p, at);
     if constexpr (GRAD) rec_read(y, p.dh, p, at);
-    else rec_read(x, p.x, p, at);
-    if constexpr (GATE && !GRAD) rec_read(g, p.gate, p, at);
-    f32x2 rate[kRecP], A[kRecP], H[kRecP];
+    if constexpr (STATE) rec_read(x, p.x, p, at);
+    if constexpr (STATE && GATE) rec_read(g, p.gate, p, at);
+    f32x2 rate[kRecP], A[kRecP], H[kRecP], G[kRecP];
 #pragma unroll
     for (int i = 0; i < kRecP; ++i) rate[i] = both(0.0f);
     if (at.ch < p.C) rec_load_rates<kRecV>(rate, p.rate + at.ch);
@@ -347,70 +366,89 @@ __global__ void __launch_bounds__(kRecMapsThreads, 6) recurrence_maps_kernel(con
     float least = 1.0f;
     // PADDED: with regard to tokens whose other inputs must not count
     const auto pass = [&](auto wide, auto padded) {
+        constexpr bool kWide = decltype(wide)::value;
+        // 1 - exp(-L), or exp(-L) where WIDE: for the gradient, whose tokens come the other way.  (The sums of L are formed in one order
+        // whatever is asked for, so that a pass with kept states gives the bits of one without.)
+        f32x2 kept[R][kRecP];
 #pragma unroll
-        for (int i = 0; i < kRecP; ++i) A[i] = H[i] = both(0.0f);
+        for (int i = 0; i < kRecP; ++i) A[i] = H[i] = G[i] = both(0.0f);
 #pragma unroll
-        for (int n = 0; n < R; ++n) {
-            const int r = GRAD ? R - 1 - n : n;
+        for (int r = 0; r < R; ++r) {
             f32x2 s[kRecP], v[kRecP], q[kRecP];
             rec_values<KIND>(d, r, at.lane, s);
-            if constexpr (GRAD) rec_values<KIND>(y, r, at.lane, v);
-            else rec_values<KIND>(x, r, at.lane, v);
-            if constexpr (GATE && !GRAD) rec_values<KIND>(g, r, at.lane, q);
+            if constexpr (STATE) rec_values<KIND>(x, r, at.lane, v);
+            if constexpr (STATE && GATE) rec_values<KIND>(g, r, at.lane, q);
 #pragma unroll
             for (int i = 0; i < kRecP; ++i) {
                 s[i] = rec_sigmoid(s[i]);
                 if (ragged && r >= at.left) s[i] = both(0.0f);
-                const f32x2 L = mul2(rate[i], s[i]), e = rec_decay<decltype(wide)::value>(L);
+                const f32x2 L = mul2(rate[i], s[i]), e = rec_decay<kWide>(L);
                 A[i] = add2(A[i], L);
-                if constexpr (GRAD) {
-                    const f32x2 sum = add2(v[i], H[i]);
-                    H[i] = decltype(wide)::value ? mul2(rec_keep(L), sum) : rec_minus(sum, mul2(e, sum));
-                } else {
+                if constexpr (STATE) {
                     least = rec_least(least, s[i]);
                     if constexpr (GATE) v[i] = mul2(v[i], rec_sigmoid(q[i]));
                     if constexpr (decltype(padded)::value) v[i] = rec_unless_padding(s[i], v[i]);
                     H[i] = fma2(e, rec_minus(v[i], H[i]), H[i]);
                 }
+                if constexpr (GRAD) kept[r][i] = kWide ? rec_keep(L) : e;
+            }
+        }
+        if constexpr (GRAD) {
+#pragma unroll
+            for (int r = R - 1; r >= 0; --r) {
+                f32x2 t[kRecP];
+                rec_values<KIND>(y, r, at.lane, t);
+#pragma unroll
+                for (int i = 0; i < kRecP; ++i) {
+                    const f32x2 sum = add2(t[i], G[i]);
+                    G[i] = kWide ? mul2(kept[r][i], sum) : rec_minus(sum, mul2(kept[r][i], sum));
+                }
             }
         }
     };
-    if (rec_wide(rate)) pass(RecBool<true>(), RecBool<true>());
-    else pass(RecBool<false>(), RecBool<false>());
-    if (!GRAD && __any_sync(0xffffffffu, least == 0.0f)) pass(RecBool<true>(), RecBool<true>());
-#pragma unroll
-    for (int i = 0; i < kRecP; ++i) {
-        A[i] = rec_keep(A[i]);
-        // the segments of a warp, one after the other
-#pragma unroll
-        for (int off = 1; off < kRecSegs; off *= 2) {
-            const f32x2 a = __shfl_xor_sync(0xffffffffu, A[i], off * kRecLanes), h = __shfl_xor_sync(0xffffffffu, H[i], off * kRecLanes);
-            const bool second = ((at.lane / kRecLanes) & off) != 0;
-            H[i] = second != GRAD ? fma2(A[i], h, H[i]) : fma2(a, H[i], h);
-            A[i] = mul2(A[i], a);
-        }
+    if (rec_wide(rate)) {
+        pass(RecBool<true>(), RecBool<true>());
+    } else {
+        pass(RecBool<false>(), RecBool<false>());
+        if (STATE && __any_sync(0xffffffffu, least == 0.0f)) pass(RecBool<false>(), RecBool<true>());
     }
-    if (at.lane < kRecLanes) rec_put(&totals[at.warp][at.cl], A, H);
+    f32x2 B[kRecP];
+#pragma unroll
+    for (int i = 0; i < kRecP; ++i) A[i] = B[i] = rec_keep(A[i]);
+    if constexpr (STATE) rec_tile_map<true>(A, H, totals[0], at.lane, at.warp, at.cl);
+    if constexpr (GRAD) rec_tile_map<false>(B, G, totals[1], at.lane, at.warp, at.cl);
     __syncthreads();
-    if (threadIdx.x < kRecSlab && at.tile < p.tiles)
-        p.maps[(static_cast<long long>(at.b) * p.tiles + at.tile) * p.width + at.slab * kRecSlab + threadIdx.x] = rec_join<!GRAD>(totals, threadIdx.x);
+    const int c = threadIdx.x % kRecSlab, which = threadIdx.x / kRecSlab;
+    const long long to = (static_cast<long long>(at.b) * p.tiles + at.tile) * p.width + at.slab * kRecSlab + c;
+    if (at.tile >= p.tiles) return;
+    if (STATE && which == 0) p.maps[to] = rec_join<true>(totals[0], c);
+    if (GRAD && which == 1) p.grad_maps[to] = rec_join<false>(totals[1], c);
 }
 
 // ------------------------------------------------------------------------------------------ from tile to tile
-// What enters each tile of a channel, in the order of the tiles or (GRAD) from the last to the first.  A block takes 16 channels, a thread a
-// run of tiles: its map, the runs' maps one after the other, then the run again.
+// What enters each tile of a channel, in the order of the tiles or (backward) from the last to the first.  A block takes 16 channels, a
+// thread a run of tiles: its map, the runs' maps by doubling, then the run again.  Two such jobs may share a launch (blocks along y).
 constexpr int kRecScanChannels = 16, kRecScanRuns = 64;
-template <bool GRAD>
-__global__ void __launch_bounds__(kRecScanChannels* kRecScanRuns) recurrence_scan_kernel(const float2* __restrict__ maps, const float* __restrict__ first,
-                                                                                        float* __restrict__ enters, int tiles, int width, int C)
+struct RecScan {
+    const float2* maps;
+    const float* first;  // what enters the first one, or null
+    float* enters;
+    int backward;
+};
+static __global__ void __launch_bounds__(kRecScanChannels* kRecScanRuns) recurrence_scan_kernel(const __grid_constant__ RecScan one, const __grid_constant__ RecScan two,
+                                                                                               int tiles, int width, int C)
 {
     __shared__ float2 both_runs[2][kRecScanRuns][kRecScanChannels];
     const int c = threadIdx.x % kRecScanChannels, run = threadIdx.x / kRecScanChannels, ch = static_cast<int>(blockIdx.x % (width / kRecScanChannels)) * kRecScanChannels + c,
               b = static_cast<int>(blockIdx.x / (width / kRecScanChannels));
+    const RecScan& job = blockIdx.y == 0 ? one : two;
+    const float2* const maps = job.maps;
+    const float* const first = job.first;
+    float* const enters = job.enters;
     pdl_wait();
     pdl_launch_dependents();
     const int length = (tiles + kRecScanRuns - 1) / kRecScanRuns, k0 = run * length, k1 = min(tiles, k0 + length);
-    const auto tile = [&](int k) { return static_cast<long long>(b) * tiles + (GRAD ? tiles - 1 - k : k); };
+    const auto tile = [&](int k) { return static_cast<long long>(b) * tiles + (job.backward ? tiles - 1 - k : k); };
     constexpr int U = 8;
     float2 m[U], own = make_float2(1.0f, 0.0f);
     for (int k = k0; k < k1; k += U) {
