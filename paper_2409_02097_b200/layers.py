@@ -109,13 +109,13 @@ def _ptr(t):
 
 # -------------------------------------------------------------------------------------- checkpoints
 def _rows3(t, name):
-    """A tensor of two or more axes as [B, N, C] without a copy: the axes before the last two have to merge."""
-    if t.dim() < 2:
-        raise ValueError(f"{name}: expected two axes or more, got {tuple(t.shape)}")
+    """A tensor [..., C] as [B, N, C] without a copy: the axes before the last two have to merge."""
+    if t.dim() == 0:
+        raise ValueError(f"{name}: expected [..., C], got a number")
     if t.dim() == 3:
         return t
-    if t.dim() == 2:
-        return t.unsqueeze(0)
+    if t.dim() < 3:
+        return t.view((1,) * (3 - t.dim()) + tuple(t.shape)) if t.is_contiguous() else t.unsqueeze(0)
     try:
         return t.view(-1, *t.shape[-2:])
     except RuntimeError:
@@ -157,7 +157,7 @@ class Packed8:
         _torch_dtype(dtype)
         if codes.dtype != torch.int8 or scales.dtype != torch.uint8:
             raise ValueError(f"expected int8 codes and uint8 scales, got {codes.dtype} and {scales.dtype}")
-        if codes.dim() < 2 or tuple(scales.shape) != (*codes.shape[:-1], -(-codes.shape[-1] // GROUP)):
+        if codes.dim() < 1 or tuple(scales.shape) != (*codes.shape[:-1], -(-codes.shape[-1] // GROUP)):
             raise ValueError(f"codes {tuple(codes.shape)} and scales {tuple(scales.shape)} do not belong together")
         if not codes.is_cuda or scales.device != codes.device:
             raise ValueError("expected CUDA tensors on one device")

@@ -207,6 +207,17 @@ def test_linear_strides_and_places(layers):
         assert (t[:, :8] == 7).all() and (t[:, -8:] == 7).all()
 
 
+def test_a_single_row_without_leading_axes(layers):
+    x, w, bias, residual, dy = _linear_inputs(1, 64, 40, "bf16", False)
+    lin = layers.Linear(64, 40, "silu")
+    y, u = lin.forward(x, w, bias, residual, save="packed")
+    y1, u1 = lin.forward(x[0], w, bias, residual[0], save="packed")
+    assert y1.shape == (40,) and torch.equal(y1, y[0]) and torch.equal(u1.unpack(), u.unpack()[0]) and torch.equal(u1.scales, u.scales[0])
+    want = lin.backward(dy, layers.pack8(x), w, u=u)
+    got = lin.backward(dy[0], layers.pack8(x[0]), w, u=layers.Packed8(u1.codes, u1.scales))
+    assert torch.equal(got["x"], want["x"][0]) and torch.equal(got["w"], want["w"]) and torch.equal(got["bias"], want["bias"])
+
+
 def test_linear_what_is_not_finite_stays_in_its_row(layers):
     M, K, N = 140, 64, 72
     x, w, bias, _, _ = _linear_inputs(M, K, N, "fp16", True)
