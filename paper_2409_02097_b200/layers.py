@@ -349,6 +349,8 @@ class GatedRecurrence(_Fixed):
         import torch
         if isinstance(x, Packed8) or isinstance(decay, Packed8) or isinstance(gate, Packed8):
             raise ValueError("the forward pass takes 16-bit inputs")
+        if decay is None:
+            raise ValueError("decay: needed")
         if stream is not None and x.is_cuda:
             with allocating_on(stream, x.get_device()):
                 return self.forward(x, decay, rate, gate, h0, save, h, last, state, workspace)
@@ -392,6 +394,8 @@ class GatedRecurrence(_Fixed):
                 return self.backward(dh, x, decay, rate, gate, h0, state, dlast, dx, ddecay, dgate, workspace)
         if dgate is not None and gate is None:
             raise ValueError("dgate is given, but no gate")
+        if decay is None:
+            raise ValueError("decay: needed")
         key = (1, _look(dh), _look8(x), _look8(decay), _look8(gate), _look(rate), _look(h0), _look(state), _look(dlast), _look(dx), _look(ddecay),
                _look(dgate))
         found = self._checked.get(key)

@@ -286,3 +286,11 @@ def test_python_refuses_what_the_library_cannot_know():
         layers.pack8(torch.zeros(4, 8))
     with pytest.raises(ValueError):
         layers.Packed8(torch.zeros(4, 40, dtype=torch.int8), torch.zeros(4, 1, dtype=torch.uint8))
+
+
+def test_python_refuses_a_recurrence_without_decay():
+    rec, x, rate = layers.GatedRecurrence(8), torch.zeros(1, 4, 8, dtype=torch.bfloat16), torch.ones(8)
+    with pytest.raises(ValueError, match="decay: needed"):
+        rec.forward(x, None, rate)
+    with pytest.raises(ValueError, match="decay: needed"):
+        rec.backward(x, x, None, rate)
