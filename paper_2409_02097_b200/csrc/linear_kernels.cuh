@@ -419,6 +419,15 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                     }
                 }
             }
+            // The tensor core arrives on `empty` for the last chunks too, in both CTAs of a pair, and nothing else waits for that: as if every stage
+            // were filled once more, so that no arrival comes to the shared memory of a CTA that has left.
+            for (int i = 0; ok && i < C::STAGES; ++i) {
+                ok = lin_wait(empty + 8 * s, phase ^ 1u);
+                if (++s == C::STAGES) {
+                    s = 0;
+                    phase ^= 1u;
+                }
+            }
             if (!ok) {
                 atomicAdd(&linear_expired_waits, 1u);
                 // what is still in flight lands before the pair leaves (the first CTA's barriers count both CTAs' bytes)
