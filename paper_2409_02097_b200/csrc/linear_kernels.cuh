@@ -476,7 +476,8 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
         const uint32_t acc = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + group * kLinColumns;
         const uint32_t acc_free = CG == 2 ? lin_map(acc_empty, 0) : acc_empty;
         uint32_t res_phase = 0u;
-        // Once a wait has expired none is begun any more, but every barrier is met, so that all of the CTA's threads come to the end.
+        // Once a wait has expired none is begun any more but that for the residual on its way into the buffer, and every barrier is met,
+        // so that all of the CTA's threads come to the end.
         bool good = true;
         for (int n = 0; todo.next(&it); ++n) {
             const int buf = n & 1;
@@ -513,8 +514,9 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                     } while (!good && global_timer_ns() - t0 < kMaxBarrierWaitNs);
                     *flag = 0ull;  // this group alone looks at it
                 }
-            if (residual) {
-                good = good && lin_wait(res_bar, res_phase);
+            if (residual) {  // waited for in any case: its copy has been issued
+                const bool there = lin_wait(res_bar, res_phase);
+                good = good && there;
                 res_phase ^= 1u;
             }
             __syncwarp();
