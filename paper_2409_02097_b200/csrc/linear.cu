@@ -66,7 +66,7 @@ Product plan_product(int M, int N, int K, int sms)
         }
         if (p.whole < p.tiles) {
             p.partials = static_cast<size_t>(p.pairs) * p.cg * (p.bn / 4) * kLinRows * sizeof(float4);
-            p.flags = align_up_256(static_cast<size_t>(p.pairs) * p.cg * (p.bn / kLinColumns) * sizeof(unsigned long long));
+            p.flags = align_up_256(static_cast<size_t>(p.pairs) * p.cg * (p.bn / kLinColumns) * sizeof(Handover));
         }
         if (cost < least) {
             least = cost;
@@ -226,8 +226,8 @@ cudaError_t launch(const CUtensorMap (&maps)[5], const LinParams& p, int pairs, 
     return cudaLaunchKernelEx(&cfg, linear_kernel<KIND, CG, BN>, maps[0], maps[1], maps[2], maps[3], maps[4], p);
 }
 
-// A mark for the flags of one call: a different one each time, and unlikely to be what memory holds by chance.
-unsigned long long next_mark()
+// A mark for the flags of one call: a different one each time, odd, and unlikely to be what memory holds by chance.
+Handover next_mark()
 {
     static std::atomic<unsigned long long> calls{0x9E3779B97F4A7C15ull};
     return calls.fetch_add(0xD1342543DE82EF95ull, std::memory_order_relaxed) | 1ull;
@@ -268,7 +268,7 @@ linfusion_status_t product(const Product& plan, int M, int N, int K, const Opera
     }
     p.a_rows = a_rows;
     p.partials = static_cast<float4*>(partials);
-    p.flags = static_cast<unsigned long long*>(flags);
+    p.flags = static_cast<Handover*>(flags);
     p.mark = next_mark();
     cudaError_t e = cudaErrorInvalidValue;
 #define LF_PRODUCT(CG, BN) \

@@ -24,6 +24,7 @@
 
 #include "block_kernels.cuh"
 #include "column_sums.cuh"
+#include "handover.h"
 #include "pack8.cuh"
 
 namespace lf {
@@ -65,8 +66,8 @@ struct LinParams {
     int scale_groups, codes_map;
     int a_rows;                  // rows of A's boxes where K is contiguous: fewer than 128 where there are fewer
     float4* partials;            // [CTA][column / 4][row]
-    unsigned long long* flags;   // [CTA][group]: `mark` while the CTA's sums wait to be fetched, anything else before and after
-    unsigned long long mark;     // another for every call; replays of a captured one find their flags taken down again
+    Handover* flags;             // [CTA][group]: `mark` while the CTA's sums wait to be fetched, anything else before, 0 after
+    Handover mark;               // another for every call; replays of a captured one find their flags taken down again
 };
 
 __device__ __forceinline__ uint32_t cluster_rank()
@@ -176,6 +177,16 @@ __device__ __forceinline__ bool lin_elect()
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
     return r != 0u;
 }
+// A flag in global memory; what this thread's block has written before, and what is read after, goes with the exchange.
+struct LinFlag {
+    Handover* at;
+    __device__ __forceinline__ Handover operator()(Handover v) const
+    {
+        Handover was;
+        asm volatile("atom.acq_rel.gpu.global.exch.b64 %0, [%1], %2;" : "=l"(was) : "l"(at), "l"(v) : "memory");
+        return was;
+    }
+};
 __device__ __forceinline__ void lin_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 // How many blocks of 64 of an operand's `most` rows (or columns) begin inside, where `left` are left.
@@ -503,16 +514,19 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                 asm volatile("st.shared.f32 [%0], %1;" ::"r"(bias + 4 * in_group), "f"(b) : "memory");
             }
             good = good && lin_wait(acc_full + 8 * buf, (n >> 1) & 1);
-            if (good && it.helpers < pair && chief)
-                for (int q = it.helpers; q < pair && good; ++q) {
-                    unsigned long long* flag = p.flags + (q * CG + rank) * C::GROUPS + group;
-                    const unsigned long long t0 = global_timer_ns();
-                    unsigned long long there;
-                    do {
-                        asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(there) : "l"(flag) : "memory");
-                        good = there == p.mark;
-                    } while (!good && global_timer_ns() - t0 < kMaxBarrierWaitNs);
-                    *flag = 0ull;  // this group alone looks at it
+            if (it.helpers < pair && chief)
+                for (int q = it.helpers; q < pair; ++q) {
+                    Handover* flag = p.flags + (q * CG + rank) * C::GROUPS + group;
+                    if (good) {
+                        const unsigned long long t0 = global_timer_ns();
+                        Handover there;
+                        do {
+                            asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(there) : "l"(flag) : "memory");
+                            good = there == p.mark;
+                        } while (!good && global_timer_ns() - t0 < kMaxBarrierWaitNs);
+                    }
+                    if (good) *flag = 0ull;  // this group alone looks at it
+                    else handover_leave(LinFlag{flag}, p.mark);
                 }
             if (residual) {  // waited for in any case: its copy has been issued
                 const bool there = lin_wait(res_bar, res_phase);
@@ -589,7 +603,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                 __threadfence();
                 __syncwarp();
                 lin_sync(1 + group, 128);
-                if (chief) asm volatile("st.release.gpu.global.u64 [%0], %1;" ::"l"(p.flags + (pair * CG + rank) * C::GROUPS + group), "l"(p.mark) : "memory");
+                if (chief) handover_raise(LinFlag{p.flags + (pair * CG + rank) * C::GROUPS + group}, p.mark);
                 continue;
             }
 #pragma unroll

@@ -40,3 +40,19 @@ def test_calls_close_to_one_another(layers):
     for run in outs:
         assert all(torch.equal(y, want) for y, (_, _, _, want) in zip(run, calls))
     assert layers.expired() == 0
+
+
+def test_flags_are_down_after_a_call(layers):
+    """The workspace of a cut product begins with its flags: none is up when the call is over, whatever they held before."""
+    M, K, N = 512, 8192, 1280
+    lin = layers.Linear(K, N)
+    x, w = _randn(90, M, K).bfloat16(), (_randn(91, K, N) / math.sqrt(K)).bfloat16()
+    want = lin.forward(x, w)[0]
+    for fill in (0, 255, 1):
+        ws = torch.full((lin.workspace_bytes(M),), fill, dtype=torch.uint8, device="cuda")
+        assert ws.numel() > 0 and torch.equal(lin.forward(x, w, workspace=ws)[0], want)
+        flags = ws[:512].view(torch.int64)  # of the first blocks
+        assert (flags != -1).any() and all(f in (0, int.from_bytes(bytes([fill] * 8), "little", signed=True)) for f in flags.tolist())
+        if fill:
+            assert (flags == 0).any()
+    assert layers.expired() == 0
