@@ -37,8 +37,8 @@ extern "C" {
  * codes: int8 [rows, C]; scales: uint8 [rows, ceil(C / 32)], the byte e + 127; both dense.  A value is off by at most
  * max|x| / 127 of its group (half a step).  Because the scale is a power of two, code * 2^e has at most seven
  * significant bits and is a number of the storage type: reading a checkpoint rounds nothing, so a product on
- * 16-bit operands may read one as it is.  A value that is not finite has the code -128 and reads as NaN; the
- * maximum is that of the finite ones.
+ * 16-bit operands may read one as it is.  A value that is not finite has the code -128 and reads as NaN (the
+ * recurrence's decay: as -infinity); the maximum is that of the finite ones.
  * ---------------------------------------------------------------------------------------------- */
 #define LINFUSION_PACK8_GROUP 32
 typedef struct {
@@ -68,7 +68,9 @@ linfusion_status_t linfusion_unpack8(const linfusion_pack8_desc_t* desc, const l
  *     h_t = h_(t-1) + e_t (v_t - h_(t-1)) = exp(-L_t) h_(t-1) + (1 - exp(-L_t)) v_t,     h_(-1) = h0 (zero without one)
  *
  * x, decay, gate, h [B, N, C]; rate fp32 [C], >= 0 (a negative one counts as NaN); h0, last fp32 [B, C].  A token with decay = -infinity leaves the state
- * as it is, whatever its x and gate hold (NaN too): padding.  `state` keeps the states before every 64th token of
+ * as it is, whatever its x and gate hold (NaN too): padding.  In a checkpoint of decay the code -128 counts as -infinity, so that padding
+ * goes through one; a decay of +infinity or NaN cannot be told from it any more (from 17 on the sigmoid is 1: a finite decay does for
+ * +infinity).  `state` keeps the states before every 64th token of
  * the scan, fp32 [B, ceil(N / 64), C]; the backward pass recomputes h from them, 64 tokens at a time, and needs no h.
  *
  * Backward, G_t the gradient of everything that follows from h_t (dlast, the gradient of the last state, with it):

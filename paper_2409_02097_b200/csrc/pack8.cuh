@@ -102,9 +102,9 @@ __device__ __forceinline__ void pack8_codes(const f32x2 (&x)[P], float most, flo
     }
 }
 
-// Four codes -> four values.  A code's byte with its top bit turned over, as the low byte of a float of 2^23, is 2^23 + 128 +
+// Four codes -> four values; the code -128 -> the number of these bits (a NaN, or what a reader takes it for).  A code's byte with its top bit turned over, as the low byte of a float of 2^23, is 2^23 + 128 +
 // code; the difference and the product are exact.  (One fma for both would overflow for steps above 2^104.)
-__device__ __forceinline__ void unpack8_codes4(uint32_t word, float step, f32x2* x)
+__device__ __forceinline__ void unpack8_codes4(uint32_t word, float step, f32x2* x, uint32_t not_finite = 0x7fffffffu)
 {
     const uint32_t w = word ^ 0x80808080u;
     const auto offset = [&](int i) { return __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7540 + i)); };
@@ -116,7 +116,7 @@ __device__ __forceinline__ void unpack8_codes4(uint32_t word, float step, f32x2*
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float2 a = unpack2(x[i / 2]);
-            f[i] = ((word >> (8 * i)) & 0xffu) == 0x80u ? __uint_as_float(0x7fffffffu) : i % 2 == 0 ? a.x : a.y;
+            f[i] = ((word >> (8 * i)) & 0xffu) == 0x80u ? __uint_as_float(not_finite) : i % 2 == 0 ? a.x : a.y;
         }
         x[0] = pack2(f[0], f[1]);
         x[1] = pack2(f[2], f[3]);

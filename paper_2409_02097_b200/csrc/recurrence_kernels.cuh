@@ -209,11 +209,12 @@ __device__ __forceinline__ void rec_read(RecRaw<R, PACKED>& raw, const RecInput&
             raw.scale = in.scales[(static_cast<long long>(at.b) * p.N + tok) * p.scale_groups + at.ch / 32];
     }
 }
-template <int KIND, int R, bool PACKED>
+// DECAY: what was not finite reads as -infinity, a padded token.
+template <int KIND, bool DECAY = false, int R, bool PACKED>
 __device__ __forceinline__ void rec_values(const RecRaw<R, PACKED>& raw, int r, int lane, f32x2 (&v)[kRecP])
 {
     if constexpr (PACKED) {
-        unpack8_codes4(raw.w[r][0], pack8_step(__shfl_sync(0xffffffffu, raw.scale, (lane & 24) | r)), v);
+        unpack8_codes4(raw.w[r][0], pack8_step(__shfl_sync(0xffffffffu, raw.scale, (lane & 24) | r)), v, DECAY ? 0xff800000u : 0x7fffffffu);
     } else {
 #pragma unroll
         for (int i = 0; i < kRecP; ++i) v[i] = pack2(pair_lo<KIND>(raw.w[r][i % (PACKED ? 1 : 2)]), pair_hi<KIND>(raw.w[r][i % (PACKED ? 1 : 2)]));
@@ -375,7 +376,7 @@ __global__ void __launch_bounds__(kRecMapsThreads, WHAT == kRecMapBoth ? 4 : 6) 
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             f32x2 s[kRecP], v[kRecP], q[kRecP];
-            rec_values<KIND>(d, r, at.lane, s);
+            rec_values<KIND, true>(d, r, at.lane, s);
             if constexpr (STATE) rec_values<KIND>(x, r, at.lane, v);
             if constexpr (STATE && GATE) rec_values<KIND>(g, r, at.lane, q);
 #pragma unroll
@@ -511,7 +512,7 @@ __global__ void __launch_bounds__(kRecForwardThreads, 4) recurrence_kernel(const
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             f32x2 s[kRecP], q[kRecP];
-            rec_values<KIND>(d, r, at.lane, s);
+            rec_values<KIND, true>(d, r, at.lane, s);
             rec_values<KIND>(x, r, at.lane, v[r]);
             if constexpr (GATE) rec_values<KIND>(g, r, at.lane, q);
 #pragma unroll
@@ -632,7 +633,7 @@ __global__ void __launch_bounds__(kRecThreads, 2) recurrence_backward_kernel(con
     const auto gates = [&](auto wide) {
 #pragma unroll
         for (int r = 0; r < kRecR; ++r) {
-            rec_values<KIND>(d, r, at.lane, s[r]);
+            rec_values<KIND, true>(d, r, at.lane, s[r]);
             rec_values<KIND>(x, r, at.lane, v[r]);
             if constexpr (GATE) rec_values<KIND>(g, r, at.lane, q[r]);
 #pragma unroll

@@ -148,7 +148,8 @@ def _pack8_rows(t, name, dtype):
 class Packed8:
     """A tensor in 8 bits: ``codes`` int8 of its shape, ``scales`` uint8 [..., ceil(C / 32)], both contiguous CUDA tensors; a value is
     ``codes * 2 ** (scales - 127)``, the scale that of its 32 channels.  ``dtype``: the storage type ("bf16" or "fp16") that it
-    was made from, in which those values are exact.  A code of -128 stands for NaN."""
+    was made from, in which those values are exact.  A code of -128 stands for what was not finite and reads as NaN
+    (``GatedRecurrence``: as a padded token, where it is decay's)."""
 
     __slots__ = ("_codes", "_scales", "_buffer", "_at", "shape", "dtype", "device")
 
@@ -254,8 +255,9 @@ class GatedRecurrence(_Fixed):
 
     x, decay, gate: 16-bit CUDA tensors [B, N, C] with any batch and row strides that are multiples of 8 elements (windows of
     one projection are fine); rate: fp32 [C], a negative one counts as NaN; h0: fp32 [B, C], the state before the first token (None: zero).
-    A token with decay = -inf leaves the state as it is, whatever its x and gate hold: padding.  One token at a time, with
-    h0 the state that the call before returned, gives what one call over all tokens gives (up to the rounding of fp32).
+    A token with decay = -inf leaves the state as it is, whatever its x and gate hold: padding (in a checkpoint of decay, a token whose
+    decay was not finite: give a finite one of 17 or more for +inf).  One token at a time, with h0 the state that the call before
+    returned, gives what one call over all tokens gives (up to the rounding of fp32).
     """
 
     def __init__(self, C: int, reverse: bool = False, dtype: str = "bf16"):
