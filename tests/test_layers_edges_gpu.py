@@ -59,3 +59,48 @@ def test_padding_goes_through_a_checkpoint(layers, shape, case):
                 ref.assert_rounded(got[n], grads[n], slack.unsqueeze(1) * sizes[n], n)
         ref.assert_near(got["rate"], grads["rate"], slack.amax(0) * sizes["rate"], "rate")
         ref.assert_near(got["h0"], grads["h0"], slack * sizes["h0"] + 1e-30, "h0")
+
+
+def _all_values(dtype, low, high):
+    """Every number of the storage type between two bounds, in rows of 64."""
+    v = torch.arange(-32768, 32768, dtype=torch.int32, device="cuda").to(torch.int16).view(TYPES[dtype])
+    v = v[(v.float() >= low) & (v.float() <= high)]
+    return torch.cat([v, v.new_zeros(-v.numel() % 64)]).view(-1, 64)
+
+
+def _tail(a):
+    """Phi(-a) and the density, in 64 bits and without cancellation."""
+    return 0.5 * torch.special.erfcx(a / math.sqrt(2)) * torch.exp(-a * a / 2), torch.exp(-a * a / 2) / math.sqrt(2 * math.pi)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_gelu_of_every_value_is_rounded_once(layers, dtype):
+    """Far below zero too, where the tail of the distribution is all there is."""
+    x = _all_values(dtype, -13.0, 8.0)
+    y, _ = layers.Linear(64, 64, "gelu", dtype).forward(x, torch.eye(64, device="cuda", dtype=TYPES[dtype]))
+    u = x.double()
+    want = u.clamp(min=0) - u.abs() * _tail(u.abs())[0]
+    # the exponent of exp(-u^2 / 2) is rounded three times in fp32 (122 binary digits of it at u = -13: 122 * 3 * 2^-24 ln 2 = 1.5e-5), the rest is good
+    # to 1e-6
+    ref.assert_rounded(y, want, 2e-5 * (u.abs() * _tail(u.abs())[0]) + 2.0 ** -24 * u.clamp(min=0), "gelu")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_slope_of_gelu_has_its_digits(layers, dtype):
+    u = _all_values(dtype, -13.0, 13.0).view(1, -1)
+    N = u.numel()
+    lin = layers.Linear(8, N, "gelu", dtype)
+    # of a single row the bias' gradient is the slope itself, in fp32
+    got = lin.backward(torch.ones_like(u), None, torch.zeros(8, N, device="cuda", dtype=TYPES[dtype]), u=u, need=("bias",))["bias"]
+    a = u.double().abs()[0]
+    tail, density = _tail(a)
+    w = tail - a * density
+    want = torch.where(u[0] < 0, w, 1 - w)
+    ref.assert_near(got, want, 2e-5 * (tail + a * density) + 2.0 ** -23 * (u[0] >= 0).double() + 1e-36, "the slope")
+    special = torch.tensor([[math.inf, -math.inf, math.nan, 0.0, -0.0, 60000.0, -60000.0, 30.5]], device="cuda").to(TYPES[dtype])
+    lin = layers.Linear(8, 8, "gelu", dtype)
+    got = lin.backward(torch.ones_like(special), None, torch.zeros(8, 8, device="cuda", dtype=TYPES[dtype]), u=special, need=("bias",))["bias"]
+    assert got.tolist()[:2] == [1.0, 0.0] and got[2].isnan() and got.tolist()[5:] == [1.0, 0.0, 1.0]
+    assert (got[3:5] - 0.5).abs().max() <= 1e-6
+    y, _ = lin.forward(torch.eye(8, device="cuda", dtype=TYPES[dtype]), torch.diag(special[0].nan_to_num(0, 0, 0)), bias=special[0])
+    assert y[0, 0] == math.inf and (y[:, 1] == 0).all() and y[:, 2].isnan().all()
