@@ -304,7 +304,17 @@ __device__ __forceinline__ f32x2 lin_normal_ratio(f32x2 a, f32x2* bell)
     return fma2(t, s, both(-2.73163387e-05f));
 }
 
-// The activation's slope, two values at a time.
+// Two values held to -128 .. 128; a NaN stays one.
+__device__ __forceinline__ f32x2 lin_within(float2 u)
+{
+    float a, b;
+    asm("{\n\t.reg .f32 t;\n\tmax.NaN.f32 t, %1, 0fC3000000;\n\tmin.NaN.f32 %0, t, 0f43000000;\n\t}" : "=f"(a) : "f"(u.x));
+    asm("{\n\t.reg .f32 t;\n\tmax.NaN.f32 t, %1, 0fC3000000;\n\tmin.NaN.f32 %0, t, 0f43000000;\n\t}" : "=f"(b) : "f"(u.y));
+    return pack2(a, b);
+}
+
+// The activation's slope, two values at a time.  Where sigmoids are 0 or 1 in fp32 (from 128 on all of them), a factor that would pass fp32, or an
+// infinity (a pre-activation beyond fp16), must not meet the zero beside it.
 template <int ACT>
 __device__ __forceinline__ f32x2 lin_act_slope(f32x2 v)
 {
@@ -312,7 +322,7 @@ __device__ __forceinline__ f32x2 lin_act_slope(f32x2 v)
     if constexpr (ACT == 1) return pack2(u.x > 0.0f ? 1.0f : u.x <= 0.0f ? 0.0f : u.x, u.y > 0.0f ? 1.0f : u.y <= 0.0f ? 0.0f : u.y);
     if constexpr (ACT == 2) {
         const f32x2 s = lin_sigmoid2(v);
-        return mul2(s, fma2(v, fma2(s, both(-1.0f), both(1.0f)), both(1.0f)));
+        return mul2(s, fma2(lin_within(u), fma2(s, both(-1.0f), both(1.0f)), both(1.0f)));
     }
     if constexpr (ACT == 3) {
         // Phi(u) + u phi(u), which is w(|u|) = Phi(-|u|) - |u| phi(u) for a negative u and 1 - w for a positive one; both terms have the bell as a
@@ -325,9 +335,9 @@ __device__ __forceinline__ f32x2 lin_act_slope(f32x2 v)
         return fma2(s, w, fma2(s, both(-0.5f), both(0.5f)));
     }
     if constexpr (ACT == 4) {
-        const f32x2 uu = mul2(v, v), s = lin_sigmoid2(mul2(v, fma2(uu, both(2.0f * kLinTanhScale * kLinTanhCube), both(2.0f * kLinTanhScale))));
+        const f32x2 c = lin_within(u), uu = mul2(c, c), s = lin_sigmoid2(mul2(c, fma2(uu, both(2.0f * kLinTanhScale * kLinTanhCube), both(2.0f * kLinTanhScale))));
         const f32x2 w = fma2(uu, both(6.0f * kLinTanhScale * kLinTanhCube), both(2.0f * kLinTanhScale));
-        return fma2(mul2(mul2(v, s), fma2(s, both(-1.0f), both(1.0f))), w, s);
+        return fma2(mul2(mul2(c, s), fma2(s, both(-1.0f), both(1.0f))), w, s);
     }
     return both(1.0f);
 }

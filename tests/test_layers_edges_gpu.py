@@ -104,3 +104,25 @@ def test_slope_of_gelu_has_its_digits(layers, dtype):
     assert (got[3:5] - 0.5).abs().max() <= 1e-6
     y, _ = lin.forward(torch.eye(8, device="cuda", dtype=TYPES[dtype]), torch.diag(special[0].nan_to_num(0, 0, 0)), bias=special[0])
     assert y[0, 0] == math.inf and (y[:, 1] == 0).all() and y[:, 2].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+def test_slopes_of_large_values_are_their_limits(layers, act, dtype):
+    """Finite values up to the end of the type, and infinities (a kept pre-activation that has passed fp16): no infinity times zero."""
+    big = [65504.0, 200.0, 129.0, math.inf] + ([1e15, 2e19, 1e25, 3e38] if dtype == "bf16" else [1e3, 1e4, 3e4, 6e4])
+    u = torch.tensor([big + [-v for v in big]], device="cuda").to(TYPES[dtype])
+    lin, w = layers.Linear(8, 16, act, dtype), torch.zeros(8, 16, device="cuda", dtype=TYPES[dtype])
+    got = lin.backward(torch.ones_like(u), None, w, u=u, need=("bias",))["bias"]
+    assert got.tolist() == [1.0] * 8 + [0.0] * 8
+    u = torch.full_like(u, math.nan)
+    assert lin.backward(torch.ones_like(u), None, w, u=u, need=("bias",))["bias"].isnan().all()
+
+
+def test_slope_of_silu_far_below_zero(layers):
+    u = torch.linspace(-80, -20, 64, device="cuda").bfloat16().view(1, -1)
+    lin, w = layers.Linear(8, 64, "silu"), torch.zeros(8, 64, device="cuda", dtype=torch.bfloat16)
+    got = lin.backward(torch.ones_like(u), None, w, u=u, need=("bias",))["bias"]
+    want = ref.act_slope(u[0].double(), "silu")
+    # 116 binary digits of the exponent are rounded twice: 116 * 2 * 2^-24 ln 2 = 1e-5
+    ref.assert_near(got, want, 1.5e-5 * want.abs(), "the slope")
