@@ -61,6 +61,22 @@ __device__ __forceinline__ f32x2 rec_sigmoid(f32x2 x)
     const float2 t = unpack2(mul2(x, both(-kLog2e))), d = unpack2(add2(pack2(ex2_approx(t.x), ex2_approx(t.y)), both(1.0f)));
     return pack2(rec_rcp(d.x), rec_rcp(d.y));
 }
+// The sigmoid in a form from which 1 - sigmoid comes without a difference: k = exp(-x), the sigmoid 1 / (1 + k), the rest of it k / (1 + k).
+// k is held to 2^127, where the sigmoid is 0 (and so is the product: what it multiplies is 0 there).  A NaN stays one.
+constexpr float kRecClosed = 1.7014118346046923e38f;
+__device__ __forceinline__ f32x2 rec_odds(f32x2 x)
+{
+    const float2 t = unpack2(mul2(x, both(-kLog2e)));
+    float a, b;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(ex2_approx(t.x)), "f"(kRecClosed));
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(b) : "f"(ex2_approx(t.y)), "f"(kRecClosed));
+    return pack2(a, b);
+}
+__device__ __forceinline__ f32x2 rec_open(f32x2 k)
+{
+    const float2 d = unpack2(add2(k, both(1.0f)));
+    return pack2(rec_rcp(d.x), rec_rcp(d.y));
+}
 __device__ __forceinline__ f32x2 rec_exp_minus(f32x2 L)
 {
     const float2 t = unpack2(mul2(L, both(-kLog2e)));
@@ -624,8 +640,9 @@ __global__ void __launch_bounds__(kRecThreads, 2) recurrence_backward_kernel(con
     for (int i = 0; i < kRecP; ++i) rate[i] = both(0.0f);
     if (at.ch < p.C) rec_load_rates<kRecV>(rate, p.rate + at.ch);
 
-    // s = sigmoid(decay), q = sigmoid(gate), e, v = q x; a padded token's are zero
-    f32x2 s[kRecR][kRecP], e[kRecR][kRecP], q[kRecR][kRecP], v[kRecR][kRecP], A[kRecP], H[kRecP], G[kRecP];
+    // exp(-decay) and exp(-gate), from which the sigmoids s and q come (again, below: both they and 1 - s, 1 - q are needed, which have no digits left
+    // in the other where a gate is saturated), e, v = q x; a padded token's s, q, e and v are zero
+    f32x2 odds_s[kRecR][kRecP], e[kRecR][kRecP], odds_q[kRecR][kRecP], v[kRecR][kRecP], A[kRecP], H[kRecP], G[kRecP];
 #pragma unroll
     for (int i = 0; i < kRecP; ++i) A[i] = H[i] = G[i] = both(0.0f);
     const bool ragged = (at.tile + 1) * kRecEvery > p.N;
@@ -633,20 +650,21 @@ __global__ void __launch_bounds__(kRecThreads, 2) recurrence_backward_kernel(con
     const auto gates = [&](auto wide) {
 #pragma unroll
         for (int r = 0; r < kRecR; ++r) {
-            rec_values<KIND, true>(d, r, at.lane, s[r]);
+            f32x2 decay[kRecP], gate[kRecP];
+            rec_values<KIND, true>(d, r, at.lane, decay);
             rec_values<KIND>(x, r, at.lane, v[r]);
-            if constexpr (GATE) rec_values<KIND>(g, r, at.lane, q[r]);
+            if constexpr (GATE) rec_values<KIND>(g, r, at.lane, gate);
 #pragma unroll
             for (int i = 0; i < kRecP; ++i) {
-                s[r][i] = rec_sigmoid(s[r][i]);
-                if (ragged && r >= at.left) s[r][i] = both(0.0f);
-                const f32x2 L = mul2(rate[i], s[r][i]);
+                odds_s[r][i] = rec_odds(decay[i]);
+                if (ragged && r >= at.left) odds_s[r][i] = both(kRecClosed);
+                const f32x2 s = rec_open(odds_s[r][i]), L = mul2(rate[i], s);
                 A[i] = add2(A[i], L);
                 e[r][i] = decltype(wide)::value ? rec_both(L) : rec_decay<false>(L);
-                least = rec_least(least, s[r][i]);
+                least = rec_least(least, s);
                 if constexpr (GATE) {
-                    q[r][i] = rec_sigmoid(q[r][i]);
-                    v[r][i] = mul2(v[r][i], q[r][i]);
+                    odds_q[r][i] = rec_odds(gate[i]);
+                    v[r][i] = mul2(v[r][i], rec_open(odds_q[r][i]));
                 }
             }
         }
@@ -659,8 +677,12 @@ __global__ void __launch_bounds__(kRecThreads, 2) recurrence_backward_kernel(con
         for (int r = 0; r < kRecR; ++r)
 #pragma unroll
             for (int i = 0; i < kRecP; ++i) {
-                if constexpr (GATE) q[r][i] = rec_unless_padding(s[r][i], q[r][i]);
-                v[r][i] = rec_unless_padding(s[r][i], v[r][i]);
+                const f32x2 s = rec_open(odds_s[r][i]);
+                if constexpr (GATE) {
+                    const float2 a = unpack2(s), b = unpack2(odds_q[r][i]);
+                    odds_q[r][i] = pack2(a.x == 0.0f ? kRecClosed : b.x, a.y == 0.0f ? kRecClosed : b.y);
+                }
+                v[r][i] = rec_unless_padding(s, v[r][i]);
             }
     const auto sums = [&](auto w) {
         constexpr bool kWide = decltype(w)::value;
@@ -726,12 +748,13 @@ __global__ void __launch_bounds__(kRecThreads, 2) recurrence_backward_kernel(con
             for (int i = 0; i < kRecP; ++i) {
                 const f32x2 sum = add2(y[i], G[i]), dv = mul2(kWide ? rec_both_e(e[r][i]) : e[r][i], sum);
                 G[i] = kWide ? mul2(rec_both_keep(e[r][i]), sum) : rec_minus(sum, dv);
-                const f32x2 dL = mul2(mul2(G[i], step[r][i]), s[r][i]);  // dL sigmoid(decay)
+                const f32x2 s = rec_open(odds_s[r][i]), dL = mul2(mul2(G[i], step[r][i]), s);  // dL sigmoid(decay)
                 drate[i] = add2(drate[i], dL);
-                od[i] = mul2(mul2(dL, rate[i]), rec_minus(both(1.0f), s[r][i]));
+                od[i] = mul2(mul2(dL, rate[i]), mul2(odds_s[r][i], s));
                 if constexpr (GATE) {
-                    ox[i] = mul2(dv, q[r][i]);
-                    og[i] = mul2(mul2(dv, v[r][i]), rec_minus(both(1.0f), q[r][i]));
+                    const f32x2 q = rec_open(odds_q[r][i]);
+                    ox[i] = mul2(dv, q);
+                    og[i] = mul2(mul2(dv, v[r][i]), mul2(odds_q[r][i], q));
                 } else {
                     ox[i] = dv;
                 }

@@ -126,3 +126,32 @@ def test_slope_of_silu_far_below_zero(layers):
     want = ref.act_slope(u[0].double(), "silu")
     # 116 binary digits of the exponent are rounded twice: 116 * 2 * 2^-24 ln 2 = 1e-5
     ref.assert_near(got, want, 1.5e-5 * want.abs(), "the slope")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("wide", [False, True])
+def test_gradients_at_saturated_gates(layers, wide, packed, dtype):
+    """Gates and decays of 6 to 24 and of -6 to -24: their gradients carry the factor 1 - sigmoid, whose digits a difference would not have."""
+    B, N, C = 2, 130, 64
+    x, decay, gate, rate, h0, dlast, dh = _inputs(B, N, C, dtype, 65)
+    rate = rate * (3.0 if wide else 1.0)
+    # the gradients are below fp16's smallest numbers else
+    dh, dlast = (dh.float() * 2.0 ** 10).to(TYPES[dtype]), dlast * 2.0 ** 10
+    far = torch.linspace(6, 24, N, device="cuda").view(1, N, 1) * torch.where(torch.arange(C, device="cuda") % 2 == 0, 1.0, -1.0)
+    gate = (gate.float() + far).to(TYPES[dtype])
+    decay = (decay.float() + far.flip(1).roll(1, 2)).to(TYPES[dtype])
+    rec = layers.GatedRecurrence(C, dtype=dtype)
+    keep = layers.pack8 if packed else (lambda t: t)
+    kept = [keep(t) for t in (x, decay, gate)]
+    got = rec.backward(dh, kept[0], kept[1], rate, gate=kept[2], h0=h0, dlast=dlast)
+    x, decay, gate = (t.unpack() if packed else t for t in kept)
+    grads, sizes, f = ref.recurrence_backward(dh, x, decay, rate, gate, h0, dlast)
+    slack = (2.0 ** -17 + f["steps"] * 2.0 ** -20).unsqueeze(1)
+    # 1 - sigmoid is good to 2^-19 of itself, as the sigmoid is
+    ref.assert_rounded(got["decay"], grads["decay"], slack * sizes["decay"] * torch.sigmoid(-decay.double()), "decay")
+    ref.assert_rounded(got["gate"], grads["gate"], slack * sizes["gate"] * torch.sigmoid(-gate.double()), "gate")
+    ref.assert_rounded(got["x"], grads["x"], slack * sizes["x"], "x")
+    # in fp16 what is left of them there, rate e^-6 2^10 e^-17 or so, passes for zero
+    still = (gate > 17) & (grads["gate"].abs() > 4 * ref.SMALLEST[TYPES[dtype]])
+    assert (still.any() or dtype == "fp16") and (got["gate"][still] != 0).all()
