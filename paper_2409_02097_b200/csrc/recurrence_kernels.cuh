@@ -258,7 +258,7 @@ __device__ __forceinline__ void rec_load_floats(f32x2* v, const float* p)  // 4 
         v[i] = pack2(t.x, t.y);
     }
 }
-// Rates; a negative one counts as NaN.
+// Rates; a negative one counts as NaN, an infinite one as fp32's largest, so that a token that counts for nothing (rate * 0) still does.
 template <int V>
 __device__ __forceinline__ void rec_load_rates(f32x2* v, const float* p)
 {
@@ -266,8 +266,8 @@ __device__ __forceinline__ void rec_load_rates(f32x2* v, const float* p)
 #pragma unroll
     for (int i = 0; i < V / 2; ++i) {
         const float2 t = unpack2(v[i]);
-        const float nan = __uint_as_float(0x7fffffffu);
-        v[i] = pack2(t.x >= 0.0f ? fabsf(t.x) : nan, t.y >= 0.0f ? fabsf(t.y) : nan);
+        const float nan = __uint_as_float(0x7fffffffu), most = __uint_as_float(0x7f7fffffu);
+        v[i] = pack2(t.x >= 0.0f ? fminf(fabsf(t.x), most) : nan, t.y >= 0.0f ? fminf(fabsf(t.y), most) : nan);
     }
 }
 template <int V>

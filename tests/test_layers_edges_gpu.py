@@ -155,3 +155,32 @@ def test_gradients_at_saturated_gates(layers, wide, packed, dtype):
     # in fp16 what is left of them there, rate e^-6 2^10 e^-17 or so, passes for zero
     still = (gate > 17) & (grads["gate"].abs() > 4 * ref.SMALLEST[TYPES[dtype]])
     assert (still.any() or dtype == "fp16") and (got["gate"][still] != 0).all()
+
+
+@pytest.mark.parametrize("N", [3, 64, 70, 200])
+def test_an_infinite_rate(layers, N):
+    """The state is the token's value, and a padded token or the end of the sequence inside a tile leaves it (not infinity times zero)."""
+    B, C = 2, 40
+    x, decay, gate, rate, h0, dlast, dh = _inputs(B, N, C, "bf16", 66)
+    decay[:, 1], x[:, 1] = -math.inf, math.nan
+    rate[3::5] = math.inf
+    fast = torch.arange(C, device="cuda") % 5 == 3
+    rec = layers.GatedRecurrence(C)
+    h, last, state = rec.forward(x, decay, rate, gate=gate, h0=h0, save=True)
+    v = (torch.sigmoid(gate.double()) * x.double())[:, :, fast]
+    v[:, 1] = v[:, 0]
+    # the sigmoid is good to 2^-19; h + (v - h) is off by 2^-24 of |v - h| and by 2^-24 of the result: 3 * 2^-24 of the largest value at most, and on the
+    # way into a tile the same once more
+    slack = 2.0 ** -19 * v.abs() + 2.0 ** -21 * torch.maximum(v.abs().amax(), h0.abs().amax()).double()
+    ref.assert_rounded(h[:, :, fast], v, slack, "h")
+    ref.assert_near(last[:, fast], v[:, -1], slack[:, -1], "last")
+    for kept in (state, None):
+        got = rec.backward(dh, x, decay, rate, gate=gate, h0=h0, state=kept, dlast=dlast)
+        assert all(torch.isfinite(t.float()).all() for t in got.values())
+        assert (got["rate"][fast] == 0).all() and (got["h0"][:, fast] == 0).all() and (got["decay"][:, :, fast] == 0).all()
+        G = dh.double()[:, :, fast]
+        G[:, -1] += dlast[:, fast].double()
+        G[:, 0] += G[:, 1]
+        G[:, 1] = 0
+        want = torch.sigmoid(gate.double())[:, :, fast] * G
+        ref.assert_rounded(got["x"][:, :, fast], want, 2.0 ** -18 * want.abs(), "dx")
