@@ -146,7 +146,7 @@ __device__ __forceinline__ float rec_least(float least, f32x2 s)
     const float2 f = unpack2(s);
     return fminf(least, fminf(f.x, f.y));
 }
-// v where the token counts, 0 where its sigmoid(decay) (or 1 - exp(-L) of it) is 0: padding, whatever v holds.
+// v where the token counts, 0 where its sigmoid(decay) is 0: padding, whatever v holds.
 __device__ __forceinline__ f32x2 rec_unless_padding(f32x2 s, f32x2 v)
 {
     const float2 a = unpack2(s), b = unpack2(v);
@@ -545,11 +545,16 @@ __global__ void __launch_bounds__(kRecForwardThreads, 4) recurrence_kernel(const
     };
     if (rec_wide(rate)) gates(RecBool<true>());
     else gates(RecBool<false>());
-    if (least == 0.0f)  // what a padded token holds must not count
+    if (least == 0.0f) {  // what a padded token holds must not count; read again (nothing has been written yet): e may be zero by the rate alone
+        rec_read(d, p.decay, p, at);
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+        for (int r = 0; r < R; ++r) {
+            f32x2 s[kRecP];
+            rec_values<KIND, true>(d, r, at.lane, s);
 #pragma unroll
-            for (int i = 0; i < kRecP; ++i) v[r][i] = rec_unless_padding(e[r][i], v[r][i]);
+            for (int i = 0; i < kRecP; ++i) v[r][i] = rec_unless_padding(rec_sigmoid(s[i]), v[r][i]);
+        }
+    }
 #pragma unroll
     for (int i = 0; i < kRecP; ++i) {
 #pragma unroll

@@ -184,3 +184,20 @@ def test_an_infinite_rate(layers, N):
         G[:, 1] = 0
         want = torch.sigmoid(gate.double())[:, :, fast] * G
         ref.assert_rounded(got["x"][:, :, fast], want, 2.0 ** -18 * want.abs(), "dx")
+
+
+@pytest.mark.parametrize("N", [6, 60, 200])
+def test_a_rate_of_zero_hides_no_nan(layers, N):
+    """Only padding does: a token that counts gives 0 * NaN, also beside a padded one."""
+    B, C, at = 1, 40, 4
+    x, decay, gate, rate, h0, _, _ = _inputs(B, N, C, "bf16", 67)
+    rate[7] = rate[8] = 0
+    decay[:, at - 1], x[:, at - 1] = -math.inf, math.nan
+    rec = layers.GatedRecurrence(C)
+    clean = rec.forward(x, decay, rate, gate=gate, h0=h0)[0]
+    assert torch.isfinite(clean.float()).all() and (clean[..., 7:9] == h0[:, None, 7:9].bfloat16()).all()
+    x[:, at, 7] = math.nan
+    h, last, _ = rec.forward(x, decay, rate, gate=gate, h0=h0)
+    assert h[:, at:, 7].isnan().all() and last[:, 7].isnan().all() and torch.equal(h[:, :at], clean[:, :at])
+    others = [c for c in range(C) if c != 7]
+    assert torch.equal(h[..., others], clean[..., others])
