@@ -103,6 +103,13 @@ def expired(device: int = 0, stream: Optional[int] = None) -> int:
     return int(n.value)
 
 
+def _counted(**counts):
+    """Refuses what the descriptors' 32 bits do not hold (ctypes would cut it off)."""
+    for name, n in counts.items():
+        if n > 2 ** 31 - 1:
+            raise ValueError(f"{name}: {n} does not fit 32 bits")
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -128,6 +135,7 @@ def _pack8_desc(t, name, dtype):
         raise ValueError(f"{name}: no values")
     r = _rows3(t, name)
     B, N, C = r.shape
+    _counted(**{f"{name}: batch": B, f"{name}: rows": N, f"{name}: channels": C})
     return Pack8Desc(B, N, C, DTYPE_FP16 if dtype == "fp16" else 0), Rows(None, r.stride(0), r.stride(1))
 
 
@@ -263,6 +271,7 @@ class GatedRecurrence(_Fixed):
     def __init__(self, C: int, reverse: bool = False, dtype: str = "bf16"):
         if int(C) <= 0 or int(C) % 8 != 0:
             raise ValueError(f"C: expected a multiple of 8, got {C}")
+        _counted(C=int(C))
         self.C, self.reverse, self.dtype = int(C), bool(reverse), dtype
         self._torch_dtype = _torch_dtype(dtype)
         self._flags = DTYPE_FP16 if dtype == "fp16" else 0
@@ -270,6 +279,7 @@ class GatedRecurrence(_Fixed):
         self._checked = _Checked()
 
     def _desc(self, B, N):
+        _counted(B=B, N=N)
         return RecurrenceDesc(B, N, self.C, self.reverse, self._flags)
 
     def workspace_bytes(self, B: int, N: int, backward: bool = False, state: bool = True) -> int:
@@ -462,6 +472,7 @@ class Linear(_Fixed):
         for name, n in (("K", K), ("N", N)):
             if int(n) <= 0 or int(n) % 8 != 0:
                 raise ValueError(f"{name}: expected a multiple of 8, got {n}")
+            _counted(**{name: int(n)})
         self.K, self.N, self.act, self.dtype = int(K), int(N), ACTIVATIONS[activation], dtype
         self._torch_dtype = _torch_dtype(dtype)
         self._flags = DTYPE_FP16 if dtype == "fp16" else 0
@@ -469,6 +480,7 @@ class Linear(_Fixed):
         self._checked = _Checked()
 
     def _desc(self, M, transposed=False):
+        _counted(rows=M)
         return LinearDesc(M, self.K, self.N, self.act, transposed, self._flags)
 
     def workspace_bytes(self, rows: int, backward: bool = False, x_packed: bool = False, transposed: bool = False, sm_count: int = 0) -> int:
