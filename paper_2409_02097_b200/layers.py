@@ -599,9 +599,9 @@ class Linear(_Fixed):
                 self._packed(t, name, C, rows, device)
             else:
                 ms[name] = self._matrix(t, name, C, rows, device)
-        if w is None:
-            raise ValueError("w: needed for the layout of its gradient")
-        mw, transposed = self._weight(w, "w", device)
+        if w is None and ("x" in need or "w" in need):
+            raise ValueError("w: needed for x's gradient, and for the layout of its own")
+        mw, transposed = (None, False) if w is None else self._weight(w, "w", device)
         if dx is not None and tuple(dx.shape) != (*dy.shape[:-1], self.K):
             raise ValueError(f"dx: expected {(*dy.shape[:-1], self.K)}, got {tuple(dx.shape)}")
         mdx = self._matrix(dx, "dx", self.K, rows, device) or Matrix(None, self.K)
@@ -613,11 +613,12 @@ class Linear(_Fixed):
         return (self._desc(rows, transposed), mdy, ms, mw, mdx, mdw, transposed,
                 self.workspace_bytes(rows, True, isinstance(x, Packed8) and "w" in need, transposed, block._sm_count(device.index)))
 
-    def backward(self, dy, x, w, u=None, need=("x", "w", "bias"), dx=None, dw=None, workspace=None, stream: Optional[int] = None) -> Dict:
+    def backward(self, dy, x, w=None, u=None, need=("x", "w", "bias"), dx=None, dw=None, workspace=None, stream: Optional[int] = None) -> Dict:
         """Gradients by name, those in ``need``: ``x`` and ``w`` in the storage type (w's laid out as w is), ``bias`` in fp32.  The residual's is dy.
 
-        x and, with an activation, u as ``forward`` had and returned them, each in 16 bits or as a ``Packed8``.  du = dy * act'(u)
-        is rounded to 16 bits before the two products; the bias' gradient sums it unrounded."""
+        x and, with an activation, u as ``forward`` had and returned them, each in 16 bits or as a ``Packed8``; x may be None without
+        w's gradient, w where only the bias' is wanted.  du = dy * act'(u) is rounded to 16 bits before the two products; the
+        bias' gradient sums it unrounded."""
         import torch
         need = tuple(need)
         if not need or any(n not in ("x", "w", "bias") for n in need):

@@ -201,3 +201,16 @@ def test_a_rate_of_zero_hides_no_nan(layers, N):
     assert h[:, at:, 7].isnan().all() and last[:, 7].isnan().all() and torch.equal(h[:, :at], clean[:, :at])
     others = [c for c in range(C) if c != 7]
     assert torch.equal(h[..., others], clean[..., others])
+
+
+def test_the_bias_gradient_needs_no_weight(layers):
+    g = torch.Generator(device="cuda").manual_seed(68)
+    dy, u, w, x = (_randn(g, *s).bfloat16() for s in ((70, 40), (70, 40), (24, 40), (70, 24)))
+    for act in ("none", "silu"):
+        lin = layers.Linear(24, 40, act)
+        want = lin.backward(dy, x, w, u=u)["bias"]
+        assert torch.equal(lin.backward(dy, None, None, u=u, need=("bias",))["bias"], want)
+        assert torch.equal(lin.backward(dy, None, u=u, need=("bias",))["bias"], want)
+        for need in (("x",), ("w",), ("w", "bias")):
+            with pytest.raises(ValueError, match="w: needed"):
+                lin.backward(dy, x, None, u=u, need=need)
