@@ -156,7 +156,7 @@ typedef struct {
     uint32_t flags;        /* 0 or LINFUSION_DTYPE_FP16           */
 } linfusion_linear_desc_t;
 
-/* A [rows, channels] tensor: element stride of a row, a multiple of 8 and, but for inputs, at least the channels. */
+/* A [rows, channels] tensor: element stride of a row, a multiple of 8 and at least the channels, of inputs too (not looked at of a single row). */
 typedef struct {
     void* p;
     int64_t row;

@@ -134,13 +134,13 @@ linfusion_status_t check(const linfusion_linear_desc_t* d)
         if (n > INT32_MAX - 1024) return LINFUSION_ERR_UNSUPPORTED;
     return LINFUSION_OK;
 }
-// A matrix of `rows` x `cols`; tensor maps hold strides below 2^40 bytes.
+// A matrix of `rows` x `cols`, whose rows lie apart; tensor maps hold strides below 2^40 bytes.
 bool matrix_ok(const linfusion_matrix_t* m, int64_t rows, int64_t cols)
 {
     if (m == nullptr || m->p == nullptr || !is_aligned(m->p, 16)) return false;
     return rows == 1 || (m->row >= cols && m->row % 8 == 0 && m->row < (int64_t(1) << 38));
 }
-// An input may repeat a row (stride 0) as far as strides go, but a tensor map's are positive.
+// The stride of a single row says nothing.
 int64_t row_of(const linfusion_matrix_t& m, int64_t rows, int64_t cols) { return rows == 1 ? cols : m.row; }
 Extent extent_of(const linfusion_matrix_t& m, int64_t rows, int64_t cols)
 {

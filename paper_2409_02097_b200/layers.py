@@ -13,7 +13,7 @@ import ctypes
 from typing import Dict, Optional, Tuple
 
 from . import block
-from .attn import DTYPE_FP16, LinFusionError, OK, allocating_on
+from .attn import DTYPE_FP16, ERR_INVALID_ARG, LinFusionError, OK, allocating_on
 from .block import Rows, _Checked, _Fixed, _call, _check_rc, _check_tensor, _copy, _like, _look, _torch_dtype
 
 GROUP = 32          # channels that share a scale of a checkpoint
@@ -112,6 +112,29 @@ def _counted(**counts):
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
+
+
+def _refusal(rc, what, apart=(), **tensors):
+    """The error of a call that the library refused; of an invalid argument with the name of the first tensor whose place or strides are the
+    reason (the checks above it have seen to shapes and types).  ``apart``: those whose rows may not lie on top of one another."""
+    if rc == ERR_INVALID_ARG:
+        for name, t in tensors.items():
+            if t is None:
+                continue
+            if isinstance(t, Packed8):
+                p, axes = t._at[0], []
+            else:
+                p, axes = t.data_ptr(), sorted((s, n) for n, s in zip(t.shape, t.stride()) if n > 1 and s != 1)
+            reach = 1 if not axes else t.shape[-1] if t.stride(-1) == 1 or t.shape[-1] == 1 else t.shape[-2]
+            if p % 16 != 0 or (name == "workspace" and p % 256 != 0):
+                return LinFusionError(rc, f"{what}: {name}: not on a boundary of {256 if name == 'workspace' else 16} bytes")
+            for s, n in axes:
+                if s % 8 != 0:
+                    return LinFusionError(rc, f"{what}: {name}: a stride of {s} elements is no multiple of 8")
+                if name in apart and s < reach:
+                    return LinFusionError(rc, f"{what}: {name}: rows on top of one another ({s} elements apart)")
+                reach += (n - 1) * s
+    return LinFusionError(rc, what)
 
 
 # -------------------------------------------------------------------------------------- checkpoints
@@ -223,7 +246,7 @@ class Packed8:
         desc, rows = _pack8_rows(out, "out", self.dtype)
         rc = _call(index, load_library().linfusion_unpack8, desc, self._struct(), rows)
         if rc != OK:
-            raise LinFusionError(rc, "linfusion_unpack8")
+            raise _refusal(rc, "linfusion_unpack8", ("out",), codes=self, out=out)
         return out
 
 
@@ -244,7 +267,7 @@ def pack8(x, out: Optional[Packed8] = None, stream: Optional[int] = None) -> Pac
         raise ValueError(f"out: expected a {dtype} checkpoint of {tuple(x.shape)} on {x.device}")
     rc = _call(x.get_device(), load_library().linfusion_pack8, desc, rows, out._struct())
     if rc != OK:
-        raise LinFusionError(rc, "linfusion_pack8")
+        raise _refusal(rc, "linfusion_pack8", x=x, out=out)
     return out
 
 
@@ -390,7 +413,7 @@ class GatedRecurrence(_Fixed):
         rc = _call(x.get_device(), self._lib.linfusion_recurrence, desc, ix, id_, ig, rate.data_ptr(), _ptr(h0), rows, last.data_ptr(), _ptr(state),
                    _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
         if rc != OK:
-            raise LinFusionError(rc, "linfusion_recurrence")
+            raise _refusal(rc, "linfusion_recurrence", ("h",), x=x, decay=decay, gate=gate, rate=rate, h0=h0, h=h, last=last, state=state, workspace=ws)
         return h, last, state
 
     def backward(self, dh, x, decay, rate, gate=None, h0=None, state=None, dlast=None, dx=None, ddecay=None, dgate=None, workspace=None,
@@ -436,7 +459,8 @@ class GatedRecurrence(_Fixed):
         rc = _call(dh.get_device(), self._lib.linfusion_recurrence_backward, desc, ix, id_, ig, rate.data_ptr(), _ptr(h0), _ptr(state), rdh,
                    _ptr(dlast), grads, ws.data_ptr(), ws.numel() * ws.element_size())
         if rc != OK:
-            raise LinFusionError(rc, "linfusion_recurrence_backward")
+            raise _refusal(rc, "linfusion_recurrence_backward", ("dx", "ddecay", "dgate"), dh=dh, x=x, decay=decay, gate=gate, rate=rate, h0=h0, state=state,
+                           dlast=dlast, dx=dx, ddecay=ddecay, dgate=dgate, workspace=ws)
         return out
 
 
@@ -462,7 +486,7 @@ class Linear(_Fixed):
     of 8).
 
     x [..., K], residual and y [..., N]: 16-bit CUDA tensors whose leading axes are evenly spaced rows, a multiple of 8
-    elements apart; w [K, N] with either axis contiguous (a torch.nn.Linear's weight is given as ``weight.t()``); bias [N].
+    elements and at least their own length apart (an expanded tensor is made contiguous first); w [K, N] with either axis contiguous (a torch.nn.Linear's weight is given as ``weight.t()``); bias [N].
     ``activation``: "none", "relu", "silu", "gelu" or "gelu_tanh".
     """
 
@@ -578,7 +602,7 @@ class Linear(_Fixed):
         rc = _call(x.get_device(), self._lib.linfusion_linear, desc, self._at(mx, x), self._at(mw, w), _ptr(bias), self._at(mr, residual),
                    self._at(my, y), self._at(mu, u) if save == "full" else None, packed, _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
         if rc != OK:
-            raise LinFusionError(rc, "linfusion_linear")
+            raise _refusal(rc, "linfusion_linear", ("x", "w", "residual", "y", "u"), x=x, w=w, bias=bias, residual=residual, y=y, u=u, workspace=ws)
         return y, u
 
     def _check_backward(self, dy, x, w, u, dx, dw, need):
@@ -653,5 +677,5 @@ class Linear(_Fixed):
         rc = _call(dy.get_device(), self._lib.linfusion_linear_backward, desc, self._at(mdy, dy), saved, self._at(mw, w), self._at(mdx, out.get("x")),
                    self._at(mdw, out.get("w")), _ptr(out.get("bias")), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
         if rc != OK:
-            raise LinFusionError(rc, "linfusion_linear_backward")
+            raise _refusal(rc, "linfusion_linear_backward", ("dy", "x", "w", "u", "dx", "dw"), dy=dy, x=x, w=w, u=u, dx=dx, dw=dw, workspace=ws)
         return out

@@ -214,3 +214,26 @@ def test_the_bias_gradient_needs_no_weight(layers):
         for need in (("x",), ("w",), ("w", "bias")):
             with pytest.raises(ValueError, match="w: needed"):
                 lin.backward(dy, x, None, u=u, need=need)
+
+
+def test_refusals_name_the_tensor(layers):
+    from paper_2409_02097_b200.attn import LinFusionError
+    lin = layers.Linear(64, 32)
+    x, w, dy = (torch.zeros(*s, device="cuda", dtype=torch.bfloat16) for s in ((16, 64), (64, 32), (16, 32)))
+    with pytest.raises(LinFusionError, match="x: rows on top"):
+        lin.forward(x[:1].expand(16, 64), w)
+    with pytest.raises(LinFusionError, match="dy: rows on top"):
+        lin.backward(dy[:1].expand(16, 32), x, w)
+    with pytest.raises(LinFusionError, match="w: not on a boundary"):
+        lin.forward(x, torch.zeros(64 * 32 + 4, device="cuda", dtype=torch.bfloat16)[4:].view(64, 32))
+    wide = torch.zeros(2, 20, 68, device="cuda", dtype=torch.bfloat16)[..., :64]
+    rec, rate = layers.GatedRecurrence(64), torch.ones(64, device="cuda")
+    good = torch.zeros(2, 20, 64, device="cuda", dtype=torch.bfloat16)
+    with pytest.raises(LinFusionError, match="decay: a stride of 68"):
+        rec.forward(good, wide, rate)
+    with pytest.raises(LinFusionError, match="h: rows on top"):
+        rec.forward(good, good, rate, h=torch.zeros(1, 20, 64, device="cuda", dtype=torch.bfloat16).expand(2, 20, 64))
+    with pytest.raises(LinFusionError, match="x: a stride of 68"):
+        layers.pack8(wide)
+    with pytest.raises(LinFusionError, match="out: a stride of 68"):
+        layers.pack8(good).unpack(out=wide)

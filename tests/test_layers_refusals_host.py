@@ -28,3 +28,30 @@ def test_counts_beyond_32_bits_are_refused_not_cut_off(monkeypatch):
     for t in (big, big.unsqueeze(0), big.unsqueeze(1)):
         with pytest.raises(ValueError, match="32 bits"):
             layers._pack8_desc(t, "x", "bf16")
+
+
+class _Stand:
+    """A stand-in for a tensor of the given shape, strides and address."""
+
+    def __init__(self, shape, strides, p=A16):
+        self.shape, self._strides, self._p = torch.Size(shape), tuple(strides), p
+
+    def stride(self, i=None):
+        return self._strides if i is None else self._strides[i]
+
+    def data_ptr(self):
+        return self._p
+
+
+def test_refusals_name_the_tensor():
+    say = lambda apart=(), **t: str(layers._refusal(attn.ERR_INVALID_ARG, "linfusion_linear", apart, **t))  # noqa: E731
+    good = _Stand((4, 64), (64, 1))
+    assert "x: not on a boundary of 16" in say(w=good, x=_Stand((4, 64), (64, 1), A16 + 8))
+    assert "workspace: not on a boundary of 256" in say(x=good, workspace=_Stand((512,), (1,), A16 + 16))
+    assert "w: a stride of 60 elements" in say(x=good, w=_Stand((64, 60), (60, 1)))
+    assert "w: a stride of 60 elements" in say(x=good, w=_Stand((60, 64), (1, 60)))
+    assert "dy: rows on top of one another (0" in say(("dy",), x=good, dy=_Stand((4, 64), (0, 1)))
+    assert "dy: rows on top of one another (32" in say(("dy",), x=good, dy=_Stand((2, 4, 64), (64, 32, 1)))
+    nobody = say(("x", "w", "dy"), x=good, bias=None, w=_Stand((64, 40), (1, 64)), dy=_Stand((2, 4, 64), (512, 128, 1)), dh=_Stand((4, 64), (0, 1)))
+    assert nobody.startswith("linfusion_linear: ") and "apart" not in nobody and "stride of" not in nobody
+    assert layers._refusal(attn.ERR_ALLOC, "linfusion_linear", x=_Stand((4, 64), (60, 1))).code == attn.ERR_ALLOC
