@@ -138,7 +138,7 @@ linfusion_status_t check(const linfusion_linear_desc_t* d)
 bool matrix_ok(const linfusion_matrix_t* m, int64_t rows, int64_t cols)
 {
     if (m == nullptr || m->p == nullptr || !is_aligned(m->p, 16)) return false;
-    return rows == 1 || (m->row >= cols && m->row % 8 == 0 && m->row < (int64_t(1) << 38));
+    return rows == 1 || (m->row >= cols && good_stride(rows, m->row) && m->row < (int64_t(1) << 38));
 }
 // The stride of a single row says nothing.
 int64_t row_of(const linfusion_matrix_t& m, int64_t rows, int64_t cols) { return rows == 1 ? cols : m.row; }

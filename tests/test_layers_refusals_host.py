@@ -4,7 +4,7 @@ import ctypes
 import pytest
 import torch
 
-from paper_2409_02097_b200 import attn, block, build, layers
+from paper_2409_02097_b200 import attn, build, layers
 
 A16 = 1 << 24  # an aligned address that is never read: the calls below are refused, or find no device
 
@@ -55,3 +55,19 @@ def test_refusals_name_the_tensor():
     nobody = say(("x", "w", "dy"), x=good, bias=None, w=_Stand((64, 40), (1, 64)), dy=_Stand((2, 4, 64), (512, 128, 1)), dh=_Stand((4, 64), (0, 1)))
     assert nobody.startswith("linfusion_linear: ") and "apart" not in nobody and "stride of" not in nobody
     assert layers._refusal(attn.ERR_ALLOC, "linfusion_linear", x=_Stand((4, 64), (60, 1))).code == attn.ERR_ALLOC
+
+
+def test_strides_whose_reach_passes_every_address_are_refused(lib):
+    """The range of rows is computed in 64 bits: it may not wrap and come out next to nothing."""
+    M, n = 2 ** 30 + 1, ctypes.c_size_t(0)
+    desc = layers.LinearDesc(M, 64, 64, 0, 0, 0)
+    assert lib.linfusion_linear_workspace_bytes(ctypes.byref(desc), 0, 0, ctypes.byref(n)) == attn.OK
+    far = [layers.Matrix(A16 * (1 + i), 1 << 34) for i in range(2)]  # 2^64 elements
+    near = layers.Matrix(A16 * 4, 64)
+    rows = [layers.Matrix(2 ** 45 * (1 + i), 64) for i in range(2)]
+    for x, y in ((far[0], rows[1]), (rows[0], far[1])):
+        assert lib.linfusion_linear(ctypes.byref(desc), ctypes.byref(x), ctypes.byref(near), None, None, ctypes.byref(y), None, None, 2 ** 50, n.value,
+                                    None) == attn.ERR_INVALID_ARG
+    if not torch.cuda.is_available():
+        assert lib.linfusion_linear(ctypes.byref(desc), ctypes.byref(rows[0]), ctypes.byref(near), None, None, ctypes.byref(rows[1]), None, None, 2 ** 50, n.value,
+                                    None) == attn.ERR_CUDA
