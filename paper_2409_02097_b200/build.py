@@ -20,9 +20,9 @@ _SOURCES = {
                      "linfusion_block.h"],
     "pack8.cu": ["common.cuh", "pack8.cuh", "block_kernels.cuh", "packed_math.cuh", "host_checks.h", "host_util.h", "linfusion_attn.h",
                  "linfusion_block.h", "linfusion_layers.h"],
-    "recurrence.cu": ["common.cuh", "recurrence_kernels.cuh", "column_sums.cuh", "pack8.cuh", "packed_math.cuh", "host_checks.h", "host_util.h",
+    "recurrence.cu": ["common.cuh", "recurrence_kernels.cuh", "column_sums.cuh", "pack8.cuh", "packed_math.cuh", "sigmoid.cuh", "host_checks.h", "host_util.h",
                       "linfusion_attn.h", "linfusion_block.h", "linfusion_layers.h"],
-    "linear.cu": ["common.cuh", "linear_kernels.cuh", "column_sums.cuh", "handover.h", "pack8.cuh", "block_kernels.cuh", "packed_math.cuh",
+    "linear.cu": ["common.cuh", "linear_kernels.cuh", "column_sums.cuh", "handover.h", "pack8.cuh", "block_kernels.cuh", "packed_math.cuh", "sigmoid.cuh",
                   "host_checks.h", "host_util.h", "linfusion_attn.h", "linfusion_block.h", "linfusion_layers.h"],
 }
 CHECKED_LIB_PATH = os.path.join(_PKG, "liblinfusion_attn_checked.so")

@@ -26,6 +26,7 @@
 #include "column_sums.cuh"
 #include "handover.h"
 #include "pack8.cuh"
+#include "sigmoid.cuh"
 
 namespace lf {
 
@@ -253,28 +254,14 @@ struct LinSchedule {
 };
 
 // ------------------------------------------------------------------------------------------ activations
-__device__ __forceinline__ float lin_rcp(float x)
-{
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-constexpr float kLinLog2e = 1.4426950408889634f;
-__device__ __forceinline__ float lin_sigmoid(float x) { return lin_rcp(1.0f + ex2_approx(-kLinLog2e * x)); }
-// 1 / (1 + exp(-x)) of two values.
-__device__ __forceinline__ f32x2 lin_sigmoid2(f32x2 x)
-{
-    const float2 t = unpack2(mul2(x, both(-kLinLog2e))), d = unpack2(add2(pack2(ex2_approx(t.x), ex2_approx(t.y)), both(1.0f)));
-    return pack2(lin_rcp(d.x), lin_rcp(d.y));
-}
 constexpr float kLinTanhScale = 0.7978845608f, kLinTanhCube = 0.044715f;
 // ACT: linfusion_act_t.
 template <int ACT>
 __device__ __forceinline__ float lin_act(float u)
 {
     if (ACT == 1) return u < 0.0f ? 0.0f : u;  // a NaN stays one
-    if (ACT == 2) return u * lin_sigmoid(u);
-    if (ACT == 4) return u * lin_sigmoid(2.0f * kLinTanhScale * fmaf(kLinTanhCube * u * u, u, u));
+    if (ACT == 2) return u * sigmoid1(u);
+    if (ACT == 4) return u * sigmoid1(2.0f * kLinTanhScale * fmaf(kLinTanhCube * u * u, u, u));
     return u;
 }
 // |u|, at most 30 (where Phi(-a) is zero); a NaN stays one.
@@ -292,8 +279,8 @@ __device__ __forceinline__ f32x2 lin_magnitude(float2 u)
 // 13, where it reaches the end of the format (the exponent's rounding).  One reciprocal and one exponential a value.
 __device__ __forceinline__ f32x2 lin_normal_ratio(f32x2 a, f32x2* bell)
 {
-    const float2 d = unpack2(fma2(a, both(0.35f), both(1.0f))), e = unpack2(mul2(mul2(a, a), both(-0.5f * kLinLog2e)));
-    const f32x2 t = pack2(lin_rcp(d.x), lin_rcp(d.y));
+    const float2 e = unpack2(mul2(mul2(a, a), both(-0.5f * kLog2e)));
+    const f32x2 t = rcp2(fma2(a, both(0.35f), both(1.0f)));
     *bell = pack2(ex2_approx(e.x), ex2_approx(e.y));
     f32x2 s = fma2(t, both(0.0489425994f), both(-0.202119902f));
     s = fma2(t, s, both(0.240641817f));
@@ -321,7 +308,7 @@ __device__ __forceinline__ f32x2 lin_act_slope(f32x2 v)
     const float2 u = unpack2(v);
     if constexpr (ACT == 1) return pack2(u.x > 0.0f ? 1.0f : u.x <= 0.0f ? 0.0f : u.x, u.y > 0.0f ? 1.0f : u.y <= 0.0f ? 0.0f : u.y);
     if constexpr (ACT == 2) {
-        const f32x2 s = lin_sigmoid2(v);
+        const f32x2 s = sigmoid2(v);
         return mul2(s, fma2(lin_within(u), fma2(s, both(-1.0f), both(1.0f)), both(1.0f)));
     }
     if constexpr (ACT == 3) {
@@ -335,7 +322,7 @@ __device__ __forceinline__ f32x2 lin_act_slope(f32x2 v)
         return fma2(s, w, fma2(s, both(-0.5f), both(0.5f)));
     }
     if constexpr (ACT == 4) {
-        const f32x2 c = lin_within(u), uu = mul2(c, c), s = lin_sigmoid2(mul2(c, fma2(uu, both(2.0f * kLinTanhScale * kLinTanhCube), both(2.0f * kLinTanhScale))));
+        const f32x2 c = lin_within(u), uu = mul2(c, c), s = sigmoid2(mul2(c, fma2(uu, both(2.0f * kLinTanhScale * kLinTanhCube), both(2.0f * kLinTanhScale))));
         const f32x2 w = fma2(uu, both(6.0f * kLinTanhScale * kLinTanhCube), both(2.0f * kLinTanhScale));
         return fma2(mul2(mul2(c, s), fma2(s, both(-1.0f), both(1.0f))), w, s);
     }

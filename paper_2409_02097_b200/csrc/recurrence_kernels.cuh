@@ -21,6 +21,7 @@
 
 #include "column_sums.cuh"
 #include "pack8.cuh"
+#include "sigmoid.cuh"
 
 namespace lf {
 
@@ -49,42 +50,21 @@ struct RecParams {
     int B, N, C, slabs, tiles, stacks, width, scale_groups, reverse;  // width: channels in whole slabs; stacks: see RecPlace
 };
 
-__device__ __forceinline__ float rec_rcp(float x)
-{
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-constexpr float kLog2e = 1.4426950408889634f;
-__device__ __forceinline__ f32x2 rec_sigmoid(f32x2 x)
-{
-    const float2 t = unpack2(mul2(x, both(-kLog2e))), d = unpack2(add2(pack2(ex2_approx(t.x), ex2_approx(t.y)), both(1.0f)));
-    return pack2(rec_rcp(d.x), rec_rcp(d.y));
-}
 // The sigmoid in a form from which 1 - sigmoid comes without a difference: k = exp(-x), the sigmoid 1 / (1 + k), the rest of it k / (1 + k).
 // k is held to 2^127, where the sigmoid is 0 (and so is the product: what it multiplies is 0 there).  A NaN stays one.
 constexpr float kRecClosed = 1.7014118346046923e38f;
 __device__ __forceinline__ f32x2 rec_odds(f32x2 x)
 {
-    const float2 t = unpack2(mul2(x, both(-kLog2e)));
+    const float2 k = unpack2(exp_minus2(x));
     float a, b;
-    asm("min.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(ex2_approx(t.x)), "f"(kRecClosed));
-    asm("min.NaN.f32 %0, %1, %2;" : "=f"(b) : "f"(ex2_approx(t.y)), "f"(kRecClosed));
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(k.x), "f"(kRecClosed));
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(b) : "f"(k.y), "f"(kRecClosed));
     return pack2(a, b);
 }
-__device__ __forceinline__ f32x2 rec_open(f32x2 k)
-{
-    const float2 d = unpack2(add2(k, both(1.0f)));
-    return pack2(rec_rcp(d.x), rec_rcp(d.y));
-}
-__device__ __forceinline__ f32x2 rec_exp_minus(f32x2 L)
-{
-    const float2 t = unpack2(mul2(L, both(-kLog2e)));
-    return pack2(ex2_approx(t.x), ex2_approx(t.y));
-}
+__device__ __forceinline__ f32x2 rec_open(f32x2 k) { return rcp2(add2(k, both(1.0f))); }
 // 1 - exp(-L) for 0 <= L <= 1, where it is L times a polynomial of degree six: least-squares fit of (1 - exp(-L)) / L at 4000
-// Chebyshev nodes with the reciprocal of its value as the weight, off by at most 2.6e-9.  No cancellation, and none of the special
-// function unit's time, of which the sigmoids take most.
+// Chebyshev nodes with the reciprocal of its value as the weight, off by at most 2.6e-9 of itself, 1.8e-8 with the coefficients rounded to
+// fp32 and 1.4e-7 evaluated in it.  No cancellation, and none of the special function unit's time, of which the sigmoids take most.
 __device__ __forceinline__ f32x2 rec_one_minus_exp_unit(f32x2 L)
 {
     f32x2 s = fma2(L, both(0.00012827072f), both(-0.0012983276f));
@@ -98,19 +78,19 @@ __device__ __forceinline__ f32x2 rec_one_minus_exp_unit(f32x2 L)
 // The same for any L >= 0: above 1 from the exponential.
 __device__ __forceinline__ f32x2 rec_one_minus_exp(f32x2 L)
 {
-    const float2 a = unpack2(L), b = unpack2(rec_one_minus_exp_unit(L)), c = unpack2(fma2(rec_exp_minus(L), both(-1.0f), both(1.0f)));
+    const float2 a = unpack2(L), b = unpack2(rec_one_minus_exp_unit(L)), c = unpack2(fma2(exp_minus2(L), both(-1.0f), both(1.0f)));
     return pack2(a.x <= 1.0f ? b.x : c.x, a.y <= 1.0f ? b.y : c.y);
 }
 // exp(-L), with all its digits whether it is next to 1 or to 0.
 __device__ __forceinline__ f32x2 rec_keep(f32x2 L)
 {
-    const float2 a = unpack2(L), b = unpack2(fma2(rec_one_minus_exp_unit(L), both(-1.0f), both(1.0f))), c = unpack2(rec_exp_minus(L));
+    const float2 a = unpack2(L), b = unpack2(fma2(rec_one_minus_exp_unit(L), both(-1.0f), both(1.0f))), c = unpack2(exp_minus2(L));
     return pack2(a.x < 0.25f ? b.x : c.x, a.y < 0.25f ? b.y : c.y);
 }
 // e = 1 - exp(-L) and exp(-L) in one number: e up to L = 0.7, beyond it -exp(-L) (with its sign, also where it is zero).
 __device__ __forceinline__ f32x2 rec_both(f32x2 L)
 {
-    const float2 a = unpack2(L), e = unpack2(rec_one_minus_exp(L)), k = unpack2(rec_exp_minus(L));
+    const float2 a = unpack2(L), e = unpack2(rec_one_minus_exp(L)), k = unpack2(exp_minus2(L));
     return pack2(a.x > 0.7f ? -k.x : e.x, a.y > 0.7f ? -k.y : e.y);
 }
 __device__ __forceinline__ f32x2 rec_both_e(f32x2 w)
@@ -245,8 +225,7 @@ __device__ __forceinline__ void rec_store(char* at, const f32x2* v)
         const float2 a = unpack2(v[i]);
         w[i] = pack_pair<KIND>(a.x, a.y);
     }
-    if constexpr (V == 8) asm volatile("st.global.cs.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-    else if constexpr (V == 4) asm volatile("st.global.cs.v2.u32 [%0], {%1,%2};" ::"l"(at), "r"(w[0]), "r"(w[1]) : "memory");
+    if constexpr (V == 4) asm volatile("st.global.cs.v2.u32 [%0], {%1,%2};" ::"l"(at), "r"(w[0]), "r"(w[1]) : "memory");
     else asm volatile("st.global.cs.u32 [%0], %1;" ::"l"(at), "r"(w[0]) : "memory");
 }
 template <int V>
@@ -386,24 +365,24 @@ __global__ void __launch_bounds__(kRecMapsThreads, WHAT == kRecMapBoth ? 4 : 6) 
         constexpr bool kWide = decltype(wide)::value;
         // 1 - exp(-L), or exp(-L) where WIDE: for the gradient, whose tokens come the other way.  (The sums of L are formed in one order
         // whatever is asked for, so that a pass with kept states gives the bits of one without.)
-        f32x2 kept[R][kRecP];
+        [[maybe_unused]] f32x2 kept[R][kRecP];
 #pragma unroll
         for (int i = 0; i < kRecP; ++i) A[i] = H[i] = G[i] = both(0.0f);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            f32x2 s[kRecP], v[kRecP], q[kRecP];
+            [[maybe_unused]] f32x2 s[kRecP], v[kRecP], q[kRecP];
             rec_values<KIND, true>(d, r, at.lane, s);
             if constexpr (STATE) rec_values<KIND>(x, r, at.lane, v);
             if constexpr (STATE && GATE) rec_values<KIND>(g, r, at.lane, q);
 #pragma unroll
             for (int i = 0; i < kRecP; ++i) {
-                s[i] = rec_sigmoid(s[i]);
+                s[i] = sigmoid2(s[i]);
                 if (ragged && r >= at.left) s[i] = both(0.0f);
                 const f32x2 L = mul2(rate[i], s[i]), e = rec_decay<kWide>(L);
                 A[i] = add2(A[i], L);
                 if constexpr (STATE) {
                     least = rec_least(least, s[i]);
-                    if constexpr (GATE) v[i] = mul2(v[i], rec_sigmoid(q[i]));
+                    if constexpr (GATE) v[i] = mul2(v[i], sigmoid2(q[i]));
                     if constexpr (decltype(padded)::value) v[i] = rec_unless_padding(s[i], v[i]);
                     H[i] = fma2(e, rec_minus(v[i], H[i]), H[i]);
                 }
@@ -527,19 +506,19 @@ __global__ void __launch_bounds__(kRecForwardThreads, 4) recurrence_kernel(const
     const auto gates = [&](auto wide) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            f32x2 s[kRecP], q[kRecP];
+            [[maybe_unused]] f32x2 s[kRecP], q[kRecP];
             rec_values<KIND, true>(d, r, at.lane, s);
             rec_values<KIND>(x, r, at.lane, v[r]);
             if constexpr (GATE) rec_values<KIND>(g, r, at.lane, q);
 #pragma unroll
             for (int i = 0; i < kRecP; ++i) {
-                s[i] = rec_sigmoid(s[i]);
+                s[i] = sigmoid2(s[i]);
                 if (ragged && r >= at.left) s[i] = both(0.0f);
                 const f32x2 L = mul2(rate[i], s[i]);
                 A[i] = add2(A[i], L);
                 e[r][i] = rec_decay<decltype(wide)::value>(L);
                 least = rec_least(least, s[i]);
-                if constexpr (GATE) v[r][i] = mul2(v[r][i], rec_sigmoid(q[i]));
+                if constexpr (GATE) v[r][i] = mul2(v[r][i], sigmoid2(q[i]));
             }
         }
     };
@@ -552,7 +531,7 @@ __global__ void __launch_bounds__(kRecForwardThreads, 4) recurrence_kernel(const
             f32x2 s[kRecP];
             rec_values<KIND, true>(d, r, at.lane, s);
 #pragma unroll
-            for (int i = 0; i < kRecP; ++i) v[r][i] = rec_unless_padding(rec_sigmoid(s[i]), v[r][i]);
+            for (int i = 0; i < kRecP; ++i) v[r][i] = rec_unless_padding(sigmoid2(s[i]), v[r][i]);
         }
     }
 #pragma unroll
@@ -617,8 +596,8 @@ __global__ void __launch_bounds__(kRecShortThreads) recurrence_short_kernel(cons
         if (r < p.N) {
             const int tok = p.reverse ? p.N - 1 - r : r;
             f32x2 v = pack2(pair_lo<KIND>(x[r]), pair_hi<KIND>(x[r]));
-            if (GATE) v = mul2(v, rec_sigmoid(pack2(pair_lo<KIND>(g[r]), pair_hi<KIND>(g[r]))));
-            const f32x2 s = rec_sigmoid(pack2(pair_lo<KIND>(d[r]), pair_hi<KIND>(d[r])));
+            if (GATE) v = mul2(v, sigmoid2(pack2(pair_lo<KIND>(g[r]), pair_hi<KIND>(g[r]))));
+            const f32x2 s = sigmoid2(pack2(pair_lo<KIND>(d[r]), pair_hi<KIND>(d[r])));
             h = fma2(rec_one_minus_exp(mul2(rate, s)), fma2(h, both(-1.0f), rec_unless_padding(s, v)), h);
             rec_store<KIND, 2>(p.h.p + b * p.h.batch + tok * p.h.row + 2ll * ch, &h);
         }
@@ -655,7 +634,7 @@ __global__ void __launch_bounds__(kRecThreads, 2) recurrence_backward_kernel(con
     const auto gates = [&](auto wide) {
 #pragma unroll
         for (int r = 0; r < kRecR; ++r) {
-            f32x2 decay[kRecP], gate[kRecP];
+            [[maybe_unused]] f32x2 decay[kRecP], gate[kRecP];
             rec_values<KIND, true>(d, r, at.lane, decay);
             rec_values<KIND>(x, r, at.lane, v[r]);
             if constexpr (GATE) rec_values<KIND>(g, r, at.lane, gate);
@@ -747,7 +726,7 @@ __global__ void __launch_bounds__(kRecThreads, 2) recurrence_backward_kernel(con
             }
 #pragma unroll
         for (int r = kRecR - 1; r >= 0; --r) {
-            f32x2 y[kRecP], ox[kRecP], od[kRecP], og[kRecP];
+            [[maybe_unused]] f32x2 y[kRecP], ox[kRecP], od[kRecP], og[kRecP];
             rec_values<KIND>(dh, r, at.lane, y);
 #pragma unroll
             for (int i = 0; i < kRecP; ++i) {

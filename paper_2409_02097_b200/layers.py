@@ -347,7 +347,7 @@ class GatedRecurrence(_Fixed):
         B, N, _ = shape
         ins = [None if t is None else self._input(t, name, shape, device, packed) for name, t in (("x", x), ("decay", decay), ("gate", gate))]
         ends = (B, self.C)
-        for name, t, want in (("rate", rate, (self.C,)), ("h0", h0, ends), *((n, t, self.state_shape(B, N) if n == "state" else (self.C,) if n == "rate gradient" else ends) for n, t in floats)):
+        for name, t, want in (("rate", rate, (self.C,)), ("h0", h0, ends), *((n, t, self.state_shape(B, N) if n == "state" else ends) for n, t in floats)):
             self._floats(t, name, want, device)
         outs = [None if t is None else self._rows(t, name, shape, device) for name, t in others]
         state = any(n == "state" and t is not None for n, t in floats)
