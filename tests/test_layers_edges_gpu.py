@@ -237,3 +237,27 @@ def test_refusals_name_the_tensor(layers):
         layers.pack8(wide)
     with pytest.raises(LinFusionError, match="out: a stride of 68"):
         layers.pack8(good).unpack(out=wide)
+
+
+@pytest.mark.parametrize("case", range(4))
+def test_long_sums_keep_their_digits(layers, case):
+    """Last and kept states and the gradients that sum over all tokens, in the 2-norm, where states remember a thousand tokens and more."""
+    B, N, C = 2, 4099, 64
+    dtype, reverse, fast = ("bf16", "fp16")[case % 2], case in (1, 2), case == 3
+    x, decay, gate, rate, h0, dlast, dh = _inputs(B, N, C, dtype, 69)
+    g = torch.Generator(device="cuda").manual_seed(70)
+    rate = torch.exp((3 if fast else -7) * torch.rand(C, generator=g, device="cuda"))
+    rec = layers.GatedRecurrence(C, reverse, dtype)
+    h, last, state = rec.forward(x, decay, rate, gate=gate, h0=h0, save=True)
+    grads, _, f = ref.recurrence_backward(dh, x, decay, rate, gate, h0, dlast, reverse)
+    off = lambda got, want: ((got.double() - want).norm() / want.norm()).item()  # noqa: E731
+    # a sigmoid is off by 2^-20 at most (1e-6); a step rounds the state, 2^-25 of it in the mean, and up to 2 e^7 = 2200 steps are remembered:
+    # sqrt(2200 / 2) * 2^-25 = 1e-6.  Twice their sum for a state, once more for a gradient, which has those of G and of the state
+    assert off(last, f["last"]) <= 4e-6 and off(state, f["state"]) <= 4e-6
+    for kept in (state, None):
+        got = rec.backward(dh, x, decay, rate, gate=gate, h0=h0, state=kept, dlast=dlast)
+        assert off(got["rate"], grads["rate"]) <= 6e-6
+        # with fast decays nothing of the gradient arrives at the first state but products of thousands of factors
+        assert fast or off(got["h0"], grads["h0"]) <= 6e-6
+        for n in ("x", "decay", "gate"):
+            assert off(got[n], grads[n]) <= 0.7 * ref.HALF_STEP[TYPES[dtype]] + 6e-6  # and one rounding: half a step at most, 0.6 of that in the mean
