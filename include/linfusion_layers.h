@@ -1,8 +1,8 @@
 /*
  * linfusion_layers.h — C ABI of a block's own layers, beside the attention of linfusion_attn.h and the
  * operators around it in linfusion_block.h: matrix products with bias, activation and residual in
- * their epilogue, a gated linear recurrence over the tokens (Eq. 3 of the paper, with a
- * state of one value a channel), and activation checkpoints in 8 bits that both backward passes read.
+ * their epilogue, a gated linear recurrence over the tokens (of the kind that Eq. 3 of the paper gates, but each
+ * channel for itself: a state of one value, no B and no C), and activation checkpoints in 8 bits that both backward passes read.
  * Same library, status codes and conventions as linfusion_block.h:
  *
  * Every function returns a status code; nothing throws or aborts across this boundary.  Calls only
@@ -35,7 +35,8 @@ extern "C" {
  *     code = x * 2^-e rounded to the nearest whole number (ties to even), held to -127 .. 127
  *
  * codes: int8 [rows, C]; scales: uint8 [rows, ceil(C / 32)], the byte e + 127; both dense.  A value is off by at most
- * max|x| / 127 of its group (half a step).  Because the scale is a power of two, code * 2^e has at most seven
+ * max|x| / 127 of its group (half a step; one at the top of the range), or by 2^-127 where that is more (bf16).  An fp32 value beyond the
+ * range (a pre-activation above 65024 in fp16) is kept as 127 of the largest steps.  Because the scale is a power of two, code * 2^e has at most seven
  * significant bits and is a number of the storage type: reading a checkpoint rounds nothing, so a product on
  * 16-bit operands may read one as it is.  A value that is not finite has the code -128 and reads as NaN (the
  * recurrence's decay: as -infinity); the maximum is that of the finite ones.
@@ -67,7 +68,7 @@ linfusion_status_t linfusion_unpack8(const linfusion_pack8_desc_t* desc, const l
  *     L_t = rate * sigmoid(decay_t)       e_t = 1 - exp(-L_t)        v_t = sigmoid(gate_t) * x_t   (x_t without a gate)
  *     h_t = h_(t-1) + e_t (v_t - h_(t-1)) = exp(-L_t) h_(t-1) + (1 - exp(-L_t)) v_t,     h_(-1) = h0 (zero without one)
  *
- * x, decay, gate, h [B, N, C]; rate fp32 [C], >= 0 (a negative one counts as NaN); h0, last fp32 [B, C].  A token with decay = -infinity leaves the state
+ * x, decay, gate, h [B, N, C]; rate fp32 [C], >= 0 (a negative one counts as NaN, an infinite one as fp32's largest number); h0, last fp32 [B, C].  A token with decay = -infinity leaves the state
  * as it is, whatever its x and gate hold (NaN too): padding.  In a checkpoint of decay the code -128 counts as -infinity, so that padding
  * goes through one; a decay of +infinity or NaN cannot be told from it any more (from 17 on the sigmoid is 1: a finite decay does for
  * +infinity).  `state` keeps the states before every 64th token of
@@ -138,6 +139,8 @@ linfusion_status_t linfusion_recurrence_workspace_bytes(const linfusion_recurren
  * Backward:  du = dy * act'(u)      dx = du w^T      dw = x^T du      dbias = sum of du over the rows (fp32)
  *
  * du is rounded to 16 bits before the two products (they run on 16-bit operands); dbias sums it unrounded.  The gradient of the residual is dy.
+ * The activations are good to 2e-5 of themselves before their rounding (1e-6 near zero), their slopes to as much of the terms that they are
+ * the sum of.
  * ---------------------------------------------------------------------------------------------- */
 typedef enum {
     LINFUSION_ACT_NONE = 0,

@@ -6,7 +6,7 @@
 // value of B is read from shared memory once for two SMs), or 128 x BN and one CTA.  Roles in a CTA: a TMA warp, an MMA warp (one
 // thread, in the first CTA of a pair), and a group of four epilogue warps for every 64 columns of a tile; the accumulator is
 // double-buffered in tensor memory, so a tile's epilogue runs under the next tile's products.  An epilogue has about 20 issue slots a value
-// (K = 640): its arithmetic runs on pairs of fp32 values, an instruction for two.
+// (K = 640); with gelu and the pre-activation in 8 bits it takes 24: its arithmetic runs on pairs of fp32 values, an instruction for two.
 //
 // Every SM is busy for the same time whatever the number of tiles: as many tiles as make whole rounds of the machine are dealt out whole,
 // the K axes of the others are laid end to end and cut into equal runs, one for each pair.  A run that ends inside a tile
@@ -17,9 +17,10 @@
 //
 // What bounds it: an SM takes in about 64 bytes a cycle, 256 rows of 128 bytes a chunk in 512 cycles, which is also what the matrix
 // instructions of a 256 x 256 tile take.  Narrower tiles load nearly as much for half the products; they serve where there
-// are few tiles.  Measured (M x K x N, bf16): 32768 x 640 x 2560 89 us (1200 TFLOP/s; cuBLAS 87), with gelu 94 to 99, with gelu and the
-// pre-activation in 8 bits 121 to 127 and in 16 bits 117; 8192 x 1280 x 5120 79 us (1360 TFLOP/s; 84); 8192 x 1280 x 1280 24 us
-// (21); 128 x 1280 x 1280 6.0 us (3.8).  Of a small call's time 3 us are the launch, the first loads and the last tile's way out.
+// are few tiles.  Measured (M x K x N, bf16; in brackets cuBLAS, the product alone): 32768 x 640 x 2560 88 us (1220 TFLOP/s; 86), with gelu 96 to
+// 100, with gelu and the pre-activation in 8 bits 128 to 131 and in 16 bits 119; 8192 x 1280 x 5120 77 us (1390 TFLOP/s; 80); 8192 x 1280 x
+// 1280 26 us (22); 2048 x 1280 x 1280 11.7 us (6.8); 128 x 1280 x 1280 5.9 us (3.8).  Of a small call's time 3 us are the launch, the first
+// loads and the last tile's way out.
 #pragma once
 
 #include "block_kernels.cuh"
@@ -696,8 +697,8 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
 // du = dy act'(u), rounded once to the 16 bits that the products take, and its sums over the rows from the unrounded values.
 // A block takes 256 columns, a thread eight of them; eight rows at a time, four times unrolled; blocks that all run at once (600 of them in
 // two rounds took 118 us where 440 take 99).  Six bytes a value, five where u is a checkpoint, two where there is no activation (the sums
-// alone).  32768 x 2560 with gelu: 99 us, 110 from a checkpoint (77 and 64 at the copy rate); its 20 to 25 instructions a value keep
-// the issue slots as busy as DRAM.
+// alone).  32768 x 2560 with gelu and the sums' joining: 94 to 97 us, 119 to 123 from a checkpoint (77 and 64 at the copy rate); its 20 to 27
+// instructions a value keep the issue slots (56 %) busier than DRAM (39 %).  From a checkpoint 8 to 36 bytes a thread are spilled.
 constexpr int kDuThreads = 256, kDuColumns = 256, kDuUnroll = 4;
 struct DuParams {
     const char *dy, *u;

@@ -15,8 +15,11 @@
 // 131072 x 640, 49 against 42 for 2 x 4096 x 1280, and 145 against 108 backward for 2 x 16384 x 640; its blocks spent two thirds of
 // their time waiting or at barriers, and registers allow but two on an SM.
 //
-// What bounds it now: issue slots, not DRAM (15 to 40 % of its rate): a value takes 30 instructions in the maps, 36 in the forward pass and
-// 72 in the backward pass (89 from checkpoints), of which the arithmetic proper is half; it runs on pairs of fp32 values.
+// What bounds it now: latency.  Neither DRAM (15 to 40 % of its rate) nor the issue slots (48 to 59 %) are full; the registers allow 16 to 24
+// warps an SM, and each block loads, waits and meets three to five barriers once.  A value takes 32 instructions in the maps, 37 in the
+// forward pass and 77 in the backward pass (93 from checkpoints), of which the arithmetic proper is half; it runs on pairs of fp32 values.
+// The maps of the states alone spill 170 to 210 bytes a thread (80 registers, 24 warps an SM), those of both kinds from checkpoints
+// 112 to 320, the gated backward pass 24.
 #pragma once
 
 #include "column_sums.cuh"

@@ -285,7 +285,8 @@ class GatedRecurrence(_Fixed):
         h_t = a_t h_(t-1) + (1 - a_t) v_t
 
     x, decay, gate: 16-bit CUDA tensors [B, N, C] with any batch and row strides that are multiples of 8 elements (windows of
-    one projection are fine); rate: fp32 [C], a negative one counts as NaN; h0: fp32 [B, C], the state before the first token (None: zero).
+    one projection are fine); rate: fp32 [C], a negative one counts as NaN, an infinite one as fp32's largest number; h0: fp32
+    [B, C], the state before the first token (None: zero).
     A token with decay = -inf leaves the state as it is, whatever its x and gate hold: padding (in a checkpoint of decay, a token whose
     decay was not finite: give a finite one of 17 or more for +inf).  One token at a time, with h0 the state that the call before
     returned, gives what one call over all tokens gives (up to the rounding of fp32).

@@ -261,3 +261,14 @@ def test_long_sums_keep_their_digits(layers, case):
         assert fast or off(got["h0"], grads["h0"]) <= 6e-6
         for n in ("x", "decay", "gate"):
             assert off(got[n], grads[n]) <= 0.7 * ref.HALF_STEP[TYPES[dtype]] + 6e-6  # and one rounding: half a step at most, 0.6 of that in the mean
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("act", ["silu", "gelu_tanh"])
+def test_silu_and_gelu_tanh_of_every_value_are_rounded_once(layers, act, dtype):
+    x = _all_values(dtype, -80.0 if act == "silu" else -9.0, 8.0)
+    y, _ = layers.Linear(64, 64, act, dtype).forward(x, torch.eye(64, device="cuda", dtype=TYPES[dtype]))
+    u = x.double()
+    want = u * torch.sigmoid(u if act == "silu" else 2 * math.sqrt(2 / math.pi) * (u + 0.044715 * u ** 3))
+    # the exponent (116 binary digits at -80 and 96 at -9) is rounded twice, or four times: 96 * 4 * 2^-24 ln 2 = 1.6e-5
+    ref.assert_rounded(y, want, 2e-5 * want.abs(), act)
