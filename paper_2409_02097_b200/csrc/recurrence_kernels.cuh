@@ -348,6 +348,7 @@ __global__ void __launch_bounds__(kRecMapsThreads, WHAT == kRecMapBoth ? 4 : 6) 
     constexpr int R = kRecMapsR, WARPS = rec_warps(R);
     constexpr bool STATE = (WHAT & kRecMapState) != 0, GRAD = (WHAT & kRecMapGrad) != 0;
     __shared__ __align__(16) float2 totals[2][WARPS][kRecSlab];
+    __shared__ __align__(16) float decays[WARPS][kRecSlab];
     const RecPlace<R> at(p);
     pdl_wait();
     pdl_launch_dependents();
@@ -411,17 +412,29 @@ __global__ void __launch_bounds__(kRecMapsThreads, WHAT == kRecMapBoth ? 4 : 6) 
         pass(RecBool<false>(), RecBool<false>());
         if (STATE && __any_sync(0xffffffffu, least == 0.0f)) pass(RecBool<false>(), RecBool<true>());
     }
+    // The tile's decay is exp(-L) of the sum over all its tokens, rounded once: a product of its sixteen segments' would be off by some units in the
+    // last place of one, which is a good part of 1 - A where memories are long, and shows in the rates' gradients.
     f32x2 B[kRecP];
 #pragma unroll
-    for (int i = 0; i < kRecP; ++i) A[i] = B[i] = rec_keep(A[i]);
+    for (int i = 0; i < kRecP; ++i) {
+        f32x2 L = A[i];
+#pragma unroll
+        for (int off = kRecLanes; off < 32; off *= 2) L = add2(L, __shfl_xor_sync(0xffffffffu, L, off));
+        if (at.lane < kRecLanes) *reinterpret_cast<float2*>(&decays[at.warp][at.cl + 2 * i]) = unpack2(L);
+        A[i] = B[i] = rec_keep(A[i]);
+    }
     if constexpr (STATE) rec_tile_map<true>(A, H, totals[0], at.lane, at.warp, at.cl);
     if constexpr (GRAD) rec_tile_map<false>(B, G, totals[1], at.lane, at.warp, at.cl);
     __syncthreads();
     const int c = threadIdx.x % kRecSlab, which = threadIdx.x / kRecSlab;
     const long long to = (static_cast<long long>(at.b) * p.tiles + at.tile) * p.width + at.slab * kRecSlab + c;
     if (at.tile >= p.tiles) return;
-    if (STATE && which == 0) p.maps[to] = rec_join<true>(totals[0], c);
-    if (GRAD && which == 1) p.grad_maps[to] = rec_join<false>(totals[1], c);
+    float L = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) L += decays[w][c];
+    const float decay = unpack2(rec_keep(both(L))).x;
+    if (STATE && which == 0) p.maps[to] = make_float2(decay, rec_join<true>(totals[0], c).y);
+    if (GRAD && which == 1) p.grad_maps[to] = make_float2(decay, rec_join<false>(totals[1], c).y);
 }
 
 // ------------------------------------------------------------------------------------------ from tile to tile

@@ -272,3 +272,17 @@ def test_silu_and_gelu_tanh_of_every_value_are_rounded_once(layers, act, dtype):
     want = u * torch.sigmoid(u if act == "silu" else 2 * math.sqrt(2 / math.pi) * (u + 0.044715 * u ** 3))
     # the exponent (116 binary digits at -80 and 96 at -9) is rounded twice, or four times: 96 * 4 * 2^-24 ln 2 = 1.6e-5
     ref.assert_rounded(y, want, 2e-5 * want.abs(), act)
+
+
+def test_the_rates_gradient_over_many_tiles(layers):
+    """States that remember dozens of tiles, over a thousand of them: what a tile's decay is off by adds up in the rates' gradients."""
+    B, N, C = 2, 40001, 96
+    g = torch.Generator(device="cuda").manual_seed(71)
+    x, decay, dh = ((_randn(g, B, N, C) * f + a).bfloat16() for f, a in ((1, 0.2), (1.5, 0), (1, 0)))
+    rate = torch.exp(-7 * torch.sigmoid(1.5 * _randn(g, C)))
+    px, pd = layers.pack8(x), layers.pack8(decay)
+    got = layers.GatedRecurrence(C).backward(dh, px, pd, rate)
+    want, _, _ = ref.recurrence_backward(dh, px.unpack(), pd.unpack(), rate)
+    # a decay next to one is off by 2^-26 in the mean, a state by that of the 2 e^7 / 64 = 34 tiles it remembers, sqrt(17) 2^-26 = 6e-8, and as much
+    # again by its own rounding; G alike.  The mean of x is ten times what the states' differences from it sum to: some 4e-7 in all, and twice that
+    assert ((got["rate"].double() - want["rate"]).norm() / want["rate"].norm()).item() <= 8e-7
