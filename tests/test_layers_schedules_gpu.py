@@ -131,3 +131,25 @@ def test_every_backward_pass_above_has_a_cut_product(layers):
         sums = 3 * 148 * 4 * (N + 16) // -(-N // 256) + 512
         most = max(layers.Linear(K, N).workspace_bytes(M, True, transposed=side, sm_count=148) for side in (False, True))
         assert most > 2 * sums, (M, K, N)
+
+
+def test_cut_products_on_two_streams_at_once(layers):
+    """Each with a workspace of its own; the blocks of both share the machine, and each waits for its own."""
+    sets = []
+    for i, (M, K, N) in enumerate([(512, 4096, 1272), (19239, 1800, 144)]):
+        x, w = _randn(100 + i, M, K).bfloat16(), (_randn(110 + i, K, N) / math.sqrt(K)).bfloat16()
+        dy = _randn(120 + i, M, N).bfloat16()
+        lin = layers.Linear(K, N)
+        want = lin.forward(x, w)[0], lin.backward(dy, x, w)
+        sets.append((lin, x, w, dy, want, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for out, (lin, x, w, dy, _, stream) in zip(got, sets):
+            with torch.cuda.stream(stream):
+                out.append((lin.forward(x, w)[0], lin.backward(dy, x, w)))
+    torch.cuda.synchronize()
+    for out, (_, _, _, _, (y, grads), _) in zip(got, sets):
+        for a, b in out:
+            assert torch.equal(a, y) and all(torch.equal(b[n], grads[n]) for n in grads)
+    assert layers.expired() == 0
