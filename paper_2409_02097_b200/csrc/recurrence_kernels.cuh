@@ -18,8 +18,8 @@
 // What bounds it now: latency.  Neither DRAM (15 to 40 % of its rate) nor the issue slots (48 to 59 %) are full; the registers allow 16 to 24
 // warps an SM, and each block loads, waits and meets three to five barriers once.  A value takes 32 instructions in the maps, 37 in the
 // forward pass and 77 in the backward pass (93 from checkpoints), of which the arithmetic proper is half; it runs on pairs of fp32 values.
-// The maps of the states alone spill 170 to 210 bytes a thread (80 registers, 24 warps an SM), those of both kinds from checkpoints
-// 112 to 320, the gated backward pass 24.
+// The maps of the states alone spill 196 bytes a thread (80 registers, 24 warps an SM), those of both kinds from checkpoints
+// 112 and 312, the gated backward pass 24.
 #pragma once
 
 #include "column_sums.cuh"
